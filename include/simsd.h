@@ -80,6 +80,18 @@ extern "C" {
 #define SIMSD_EW_DRAFT 8u       /* a draft id is outside [0, vocab) */
 #define SIMSD_EW_TIMEOUT 16u    /* a bounded on-device wait expired */
 #define SIMSD_EW_ACCEPT_LEN 32u /* an accepted length is outside [0, gamma] */
+#define SIMSD_EW_TOKENS 64u     /* token offsets not in order or outside [0, T] */
+#define SIMSD_EW_SAMPLE 128u    /* a row's sampling parameters are out of range, or no logit is above -inf */
+
+/* rotary layouts: which components make a pair (r = rot_dim) */
+#define SIMSD_ROPE_HALF 0        /* (x_i, x_{i + r/2}) */
+#define SIMSD_ROPE_INTERLEAVED 1 /* (x_{2i}, x_{2i+1}) */
+
+/* frequency scaling for contexts longer than a model was trained on */
+#define SIMSD_ROPE_UNSCALED 0
+#define SIMSD_ROPE_LINEAR 1 /* positions divided by the factor */
+#define SIMSD_ROPE_NTK 2    /* theta times factor^(r / (r - 2)) */
+#define SIMSD_ROPE_YARN 3   /* by parts: fast pairs kept, slow ones divided, the rest between */
 
 /*
  * simsd_build_mask -- per-slot metadata of the verification input.
@@ -332,6 +344,171 @@ SIMSD_API int simsd_kv_commit(int dtype, const void* k_new, const void* v_new, i
                               const int32_t* accepted_len, void* k_cache, void* v_cache, int num_pages,
                               const int32_t* block_table, int max_pages, int page_size, int32_t* prefix_len, int Bt,
                               int gamma, int Hkv, int d, int32_t* err_word, void* stream);
+
+/*
+ * Prompts.  The calls below fill the paged cache before a step can verify
+ * against it and draw tokens from logits.  Their tokens come as ragged
+ * chunks: the new tokens of sequence b are rows token_start[b] ..
+ * token_start[b+1]-1 of arrays of T tokens (token_start: [Bt+1] int32 in
+ * [0, T], not decreasing; a chunk may be empty).  Offsets out of order or
+ * range set SIMSD_EW_TOKENS and make that sequence's chunk empty; tokens
+ * that no chunk holds are left untouched.
+ */
+
+/*
+ * simsd_rope_plan -- the rotation of a model's heads, laid out on the host
+ * by simsd_rope_plan_init and read by the calls it is passed to (the paper
+ * has no counterpart: SimSD uses its model's rotary embedding).
+ *
+ * Pair i < r/2 of a token at position p turns by p f_i, r = rot_dim:
+ *   UNSCALED  f_i = theta^(-2i/r)
+ *   LINEAR    f_i / s                                 (s = factor)
+ *   NTK       f_i with theta s^(r/(r-2)) for theta    (r > 2)
+ *   YARN      (1 - g) f_i / s + g f_i, g = (rho_i - beta_slow) / (beta_fast
+ *             - beta_slow) clamped to [0, 1], rho_i = context f_i / 2 pi the
+ *             turns pair i makes over the trained context
+ * and is multiplied by `magnitude` (0.1 ln s + 1 for YARN, else 1; the
+ * caller may set another).  Components r .. d-1 of a head are not changed.
+ * The angle of a 32-bit position, negative ones included, is formed in
+ * 64-bit fixed point, so it does not lose digits in long contexts.
+ */
+typedef struct simsd_rope_plan {
+  int32_t layout;   /* SIMSD_ROPE_HALF or SIMSD_ROPE_INTERLEAVED */
+  int32_t rot_dim;  /* r: even, 2 .. 128 */
+  float magnitude;  /* positive and finite */
+  int32_t reserved; /* 0 */
+  uint64_t turn[64]; /* frequency of pair i in 2^-64 turns a position */
+} simsd_rope_plan;
+
+/*
+ * simsd_rope_plan_init -- fills *plan (host memory).  factor >= 1 for a
+ * scaled rotation; context > 0 and beta_fast > beta_slow >= 0 for YARN (32
+ * and 1 are usual); each is ignored where its scaling does not use it.
+ */
+SIMSD_API int simsd_rope_plan_init(simsd_rope_plan* plan, int layout, int rot_dim, double theta, int scaling,
+                                   double factor, int context, double beta_fast, double beta_slow);
+
+/*
+ * simsd_rope_rotate -- rotates the q and k rows of T tokens at given
+ * positions, for models whose rotation simsd_verify_attention does not do
+ * itself (interleaved, partial or scaled): rotate q and k_new at the
+ * RoPE-copy positions of simsd_build_mask, then verify and commit with
+ * rope_pos = NULL.
+ *   q, q_out  [T][Hq][d] dtype, token strides q_stride / q_out_stride in
+ *             elements; k, k_out [T][Hkv][d] likewise, or both NULL with
+ *             Hkv = 0.  Heads of a token are dense.  q_out may be q and k_out
+ *             k (in place); other overlaps are not allowed.
+ *   positions [T] int32
+ * dtype SIMSD_BF16 or SIMSD_F32 (fp32 arithmetic, rounded once); rows of d
+ * elements and token strides are multiples of 16 bytes, rot_dim <= d.
+ */
+SIMSD_API int simsd_rope_rotate(int dtype, const simsd_rope_plan* plan, const int32_t* positions, const void* q,
+                                int64_t q_stride, void* q_out, int64_t q_out_stride, int Hq, const void* k,
+                                int64_t k_stride, void* k_out, int64_t k_out_stride, int Hkv, int T, int d,
+                                void* stream);
+
+/*
+ * simsd_rope_append -- the way of a prompt chunk into the paged cache
+ * (Sec. 3.3: the prefix is read from a KV cache; its keys are cached
+ * rotated): rotates the chunk's q rows, and writes its keys, rotated, and
+ * its values to cache rows prefix_len[b] + i of their sequences.
+ *   q [T][Hq][d], k, v [T][Hkv][d] dtype with token strides in elements
+ *            (parts of one projection's rows, for instance)
+ *   prefix_len [Bt] rows cached before the chunk; it is not advanced (every
+ *            layer of a model appends at the same place): add the chunk
+ *            lengths once all layers are done
+ *   positions [T] int32 or NULL: prefix_len[b] + i
+ *   q_out    [T][Hq][d] dense; may be q where q is dense
+ *   k_cache, v_cache [num_pages][Hkv][page_size][d]
+ * A prefix length that is negative or leaves no room for the chunk in the
+ * block table sets SIMSD_EW_PREFIX_LEN: the sequence's q_out rows are zero
+ * and nothing is cached.  A destination page outside the pool sets
+ * SIMSD_EW_PAGE and that token is not cached.
+ */
+SIMSD_API int simsd_rope_append(int dtype, const simsd_rope_plan* plan, const void* q, int64_t q_stride,
+                                const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                const int32_t* token_start, const int32_t* prefix_len, const int32_t* positions,
+                                int T, int Bt, int Hq, int Hkv, int d, void* q_out, void* k_cache, void* v_cache,
+                                int num_pages, const int32_t* block_table, int max_pages, int page_size,
+                                int32_t* err_word, void* stream);
+
+/*
+ * simsd_chunk_workspace_bytes -- bytes of scratch simsd_chunk_attention
+ * needs for these sizes on the current device (0: none).
+ *
+ * simsd_chunk_attention -- attention of ragged chunks of new tokens over the
+ * paged cache that already holds their keys and values (simsd_rope_append):
+ * prompts, chunks of prompts, blocks and single tokens (Sec. 3.3).
+ *
+ * Token i of sequence b sits at cache row p = prefix_len[b] + i, N =
+ * prefix_len[b] + chunk length, and sees the rows lo <= j < hi,
+ *   hi = N                                       mask_block = 0
+ *        min(N, (p / mask_block + 1) mask_block) otherwise (1: causal; B: the
+ *        block-causal rule of a block-diffusion model with block length B)
+ *   lo = max(key_start[b], p + 1 - window)       (window only where > 0)
+ * out = softmax(scale q.k) v over them.  A token that sees nothing gets a
+ * zero row (and lse -inf).
+ *   q        [T][Hq][d] dtype, rotated, token stride q_stride in elements
+ *   key_start [Bt] int32 or NULL: earlier cache rows are hidden (evicted or
+ *            padding; their pages and contents are never used)
+ *   k_cache, v_cache, block_table as for simsd_verify_attention
+ *   out      [T][Hq][d] dense; lse [T][Hq] fp32 or NULL: natural logarithm
+ *            of the softmax denominator, scores included
+ *   softmax_scale 0 selects 1/sqrt(d)
+ *   workspace simsd_chunk_workspace_bytes() bytes, 16-byte aligned; two
+ *            calls that share it must not overlap on the GPU
+ * d is 64 or 128; page_size as for simsd_verify_attention; Hq/Hkv at most
+ * 128, Bt at most 16384 (SIMSD_BF16).  A bad prefix length (as for
+ * simsd_rope_append) sets SIMSD_EW_PREFIX_LEN and zeroes the sequence's
+ * rows; a page id outside the pool among the rows that a group of
+ * neighbouring tokens sees sets SIMSD_EW_PAGE and zeroes the rows of that
+ * group.  With SIMSD_BF16 a value row that is not finite may also reach the
+ * rows of tokens up to 256 Hkv/Hq places before the first that sees it.
+ */
+SIMSD_API size_t simsd_chunk_workspace_bytes(int dtype, int T, int Bt, int Hq, int Hkv, int d, int max_pages,
+                                             int page_size);
+SIMSD_API int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, const int32_t* token_start,
+                                    const int32_t* prefix_len, const int32_t* key_start, const void* k_cache,
+                                    const void* v_cache, int num_pages, const int32_t* block_table, int max_pages,
+                                    int page_size, int T, int Bt, int Hq, int Hkv, int d, int mask_block, int window,
+                                    float softmax_scale, void* out, float* lse, void* workspace,
+                                    size_t workspace_bytes, int32_t* err_word, void* stream);
+
+/*
+ * simsd_sample -- draws one token from each row of logits with a given
+ * random number (Sec. 3.2: drafts are drawn from the draft model; R rows are
+ * the next tokens of sequences or all masked positions of their blocks).
+ *
+ * With m the row's maximum, w_v = exp((x_v - m) / temperature) for x_v >
+ * -inf (NaN counts as -inf).  Of the tokens in the order of falling logits
+ * (ties: lower index first) the first top_k are kept, of those the shortest
+ * prefix whose weight is at least top_p of theirs, of those the ones with
+ * w_v >= min_p.  The token is the smallest index whose cumulative kept weight
+ * (in index order) exceeds u times their sum.  temperature 0 keeps the first
+ * token of that order alone (greedy).
+ *   logits   [R][vocab] dtype (SIMSD_F32 or SIMSD_BF16), row stride in
+ *            elements; vocab in [1, 2^24]
+ *   u        [R] fp32 in [0, 1)
+ *   temperature [R] fp32 >= 0 or NULL (1); top_k [R] int32 or NULL (a value
+ *            < 1 keeps all); top_p [R] fp32 or NULL (>= 1 keeps all, <= 0 the
+ *            first token); min_p [R] fp32 or NULL
+ *   token    [R] int32 out; kept [R] int32 out or NULL: number of kept tokens
+ *   log_prob [R] fp32 out or NULL: log-probability of the token among the
+ *            kept (a denoising step's confidence)
+ *   log_probs [R][vocab] fp32 out or NULL: of every token, -inf where not
+ *            kept: the target or draft logits (at temperature 1) of
+ *            simsd_accept_sampled for models that sample from truncated
+ *            distributions
+ * Weights are fp32; their sums are 64-bit fixed point, so they do not depend
+ * on the order of summation.  A row without a logit above -inf, or with
+ * parameters outside these ranges (NaN, a negative or infinite temperature,
+ * u outside [0, 1)) sets SIMSD_EW_SAMPLE and gets token -1, kept 0 and
+ * log-probabilities -inf.
+ */
+SIMSD_API int simsd_sample(int dtype, const void* logits, int64_t row_stride, int R, int vocab, const float* u,
+                           const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                           int32_t* token, int32_t* kept, float* log_prob, float* log_probs, int32_t* err_word,
+                           void* stream);
 
 /*
  * simsd_check_error -- synchronises `stream`, copies the device error word

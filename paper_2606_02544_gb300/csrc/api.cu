@@ -465,6 +465,261 @@ int simsd_kv_commit(int dtype, const void* k_new, const void* v_new, int L, cons
   return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "kv_commit launch");
 }
 
+int simsd_rope_plan_init(simsd_rope_plan* plan, int layout, int rot_dim, double theta, int scaling, double factor,
+                         int context, double beta_fast, double beta_slow) {
+  if (!plan) return arg_fail("null plan");
+  if (layout != SIMSD_ROPE_HALF && layout != SIMSD_ROPE_INTERLEAVED) return arg_fail("layout");
+  if (rot_dim < 2 || rot_dim > 128 || rot_dim % 2 != 0) return arg_fail("rot_dim must be even, 2 .. 128");
+  if (!(theta > 0.0) || std::isinf(theta)) return arg_fail("theta must be positive and finite");
+  if (scaling < SIMSD_ROPE_UNSCALED || scaling > SIMSD_ROPE_YARN) return arg_fail("scaling");
+  if (scaling != SIMSD_ROPE_UNSCALED && (!(factor >= 1.0) || std::isinf(factor)))
+    return arg_fail("factor must be at least 1 and finite");
+  if (scaling == SIMSD_ROPE_NTK && rot_dim == 2) return arg_fail("NTK scaling needs rot_dim > 2");
+  if (scaling == SIMSD_ROPE_YARN &&
+      (context <= 0 || !(beta_slow >= 0.0) || !(beta_fast > beta_slow) || std::isinf(beta_fast)))
+    return arg_fail("YARN needs a positive context and beta_fast > beta_slow >= 0");
+  const double kTwoPi = 6.283185307179586476925286766559;
+  const double r = rot_dim;
+  if (scaling == SIMSD_ROPE_NTK) theta *= std::pow(factor, r / (r - 2.0));
+  std::memset(plan, 0, sizeof(*plan));
+  plan->layout = layout;
+  plan->rot_dim = rot_dim;
+  plan->magnitude = scaling == SIMSD_ROPE_YARN ? static_cast<float>(0.1 * std::log(factor) + 1.0) : 1.0f;
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    double f = std::pow(theta, -2.0 * i / r);
+    if (scaling == SIMSD_ROPE_LINEAR) f /= factor;
+    if (scaling == SIMSD_ROPE_YARN) {
+      const double rho = context * f / kTwoPi;
+      const double g = std::fmin(1.0, std::fmax(0.0, (rho - beta_slow) / (beta_fast - beta_slow)));
+      f = (1.0 - g) * f / factor + g * f;
+    }
+    // whole turns of a position (theta < 1 only) do not change the angle
+    double turns = f / kTwoPi;
+    turns -= std::floor(turns);
+    const double scaled = std::ldexp(turns, 64);
+    plan->turn[i] = scaled >= 18446744073709551616.0 ? 0 : static_cast<uint64_t>(scaled);
+  }
+  return SIMSD_OK;
+}
+
+namespace {
+
+int check_rope_plan(const simsd_rope_plan* plan, int d) {
+  if (!plan) return arg_fail("null plan");
+  if ((plan->layout != SIMSD_ROPE_HALF && plan->layout != SIMSD_ROPE_INTERLEAVED) || plan->rot_dim < 2 ||
+      plan->rot_dim > 128 || plan->rot_dim % 2 != 0 || !(plan->magnitude > 0.f) || std::isinf(plan->magnitude) ||
+      plan->reserved != 0)
+    return arg_fail("plan not made by simsd_rope_plan_init");
+  if (plan->rot_dim > d) return arg_fail("rot_dim larger than the head");
+  return SIMSD_OK;
+}
+
+// a [T][H][d] array with dense heads and the given token stride
+bool rows_ok(const void* p, int64_t stride, int H, int d, int eb) {
+  return p && aligned16(p) && stride >= static_cast<int64_t>(H) * d && stride * eb % 16 == 0;
+}
+
+bool page_size_ok(int P) { return P >= 8 && (P % 64 == 0 || 64 % P == 0); }
+
+}  // namespace
+
+int simsd_rope_rotate(int dtype, const simsd_rope_plan* plan, const int32_t* positions, const void* q,
+                      int64_t q_stride, void* q_out, int64_t q_out_stride, int Hq, const void* k, int64_t k_stride,
+                      void* k_out, int64_t k_out_stride, int Hkv, int T, int d, void* stream) {
+  if (dtype != SIMSD_F32 && dtype != SIMSD_BF16) return unsupported("dtype");
+  const int eb = dtype == SIMSD_F32 ? 4 : 2;
+  if (T < 0 || Hq <= 0 || Hkv < 0 || d <= 0) return arg_fail("sizes");
+  if ((d * eb) % 16 != 0) return arg_fail("d * element size must be a multiple of 16 bytes");
+  int rc = check_rope_plan(plan, d);
+  if (rc != SIMSD_OK) return rc;
+  if (T == 0) return SIMSD_OK;
+  if (!positions) return arg_fail("null pointer");
+  if (!rows_ok(q, q_stride, Hq, d, eb) || !rows_ok(q_out, q_out_stride, Hq, d, eb))
+    return arg_fail("q / q_out: null, misaligned or overlapping rows");
+  if (Hkv > 0 ? !rows_ok(k, k_stride, Hkv, d, eb) || !rows_ok(k_out, k_out_stride, Hkv, d, eb) : (k || k_out))
+    return arg_fail("k / k_out: null, misaligned or overlapping rows, or Hkv = 0");
+  DeviceInfo info;
+  rc = require_sm103(&info);
+  if (rc != SIMSD_OK) return rc;
+  simsd::RopeArgs a{};
+  a.plan = *plan;
+  a.positions = positions;
+  a.q = q;
+  a.q_stride = q_stride;
+  a.q_out = q_out;
+  a.q_out_stride = q_out_stride;
+  a.k = k;
+  a.k_stride = k_stride;
+  a.k_out = k_out;
+  a.k_out_stride = k_out_stride;
+  a.T = T;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.d = d;
+  cudaError_t e = simsd::launch_rope(eb, a, info.num_sms, as_stream(stream));
+  return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "rope_rotate launch");
+}
+
+int simsd_rope_append(int dtype, const simsd_rope_plan* plan, const void* q, int64_t q_stride, const void* k,
+                      int64_t k_stride, const void* v, int64_t v_stride, const int32_t* token_start,
+                      const int32_t* prefix_len, const int32_t* positions, int T, int Bt, int Hq, int Hkv, int d,
+                      void* q_out, void* k_cache, void* v_cache, int num_pages, const int32_t* block_table,
+                      int max_pages, int page_size, int32_t* err_word, void* stream) {
+  if (dtype != SIMSD_F32 && dtype != SIMSD_BF16) return unsupported("dtype");
+  const int eb = dtype == SIMSD_F32 ? 4 : 2;
+  if (T < 0 || Bt < 0 || Hq <= 0 || Hkv <= 0 || d <= 0 || num_pages < 0 || max_pages < 0 || page_size <= 0)
+    return arg_fail("sizes");
+  if ((d * eb) % 16 != 0) return arg_fail("d * element size must be a multiple of 16 bytes");
+  int rc = check_rope_plan(plan, d);
+  if (rc != SIMSD_OK) return rc;
+  if (T == 0 || Bt == 0) return SIMSD_OK;
+  if (!token_start || !prefix_len || !block_table || !k_cache || !v_cache) return arg_fail("null pointer");
+  if (!rows_ok(q, q_stride, Hq, d, eb) || !rows_ok(k, k_stride, Hkv, d, eb) || !rows_ok(v, v_stride, Hkv, d, eb))
+    return arg_fail("q / k / v: null, misaligned or overlapping rows");
+  if (!q_out || !aligned16(q_out) || !aligned16(k_cache) || !aligned16(v_cache))
+    return arg_fail("tensor pointers must be 16-byte aligned");
+  DeviceInfo info;
+  rc = require_sm103(&info);
+  if (rc != SIMSD_OK) return rc;
+  simsd::RopeArgs a{};
+  a.plan = *plan;
+  a.q = q;
+  a.q_stride = q_stride;
+  a.k = k;
+  a.k_stride = k_stride;
+  a.v = v;
+  a.v_stride = v_stride;
+  a.q_out = q_out;
+  a.q_out_stride = static_cast<long long>(Hq) * d;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.token_start = token_start;
+  a.prefix_len = prefix_len;
+  a.positions = positions;
+  a.block_table = block_table;
+  a.err_word = err_word;
+  a.T = T;
+  a.Bt = Bt;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.num_pages = num_pages;
+  a.max_pages = max_pages;
+  a.page_size = page_size;
+  cudaError_t e = simsd::launch_rope(eb, a, info.num_sms, as_stream(stream));
+  return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "rope_append launch");
+}
+
+size_t simsd_chunk_workspace_bytes(int dtype, int T, int Bt, int Hq, int Hkv, int d, int max_pages, int page_size) {
+  if (dtype != SIMSD_BF16 || T <= 0 || Bt <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || (d != 64 && d != 128) ||
+      max_pages < 0 || page_size <= 0)
+    return 0;
+  DeviceInfo info;
+  if (device_info(&info) != SIMSD_OK) return 0;
+  return simsd::chunk_tc_workspace_bytes(T, Bt, Hq, Hkv, d, static_cast<long long>(max_pages) * page_size,
+                                         info.num_sms);
+}
+
+int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, const int32_t* token_start,
+                          const int32_t* prefix_len, const int32_t* key_start, const void* k_cache,
+                          const void* v_cache, int num_pages, const int32_t* block_table, int max_pages,
+                          int page_size, int T, int Bt, int Hq, int Hkv, int d, int mask_block, int window,
+                          float softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                          int32_t* err_word, void* stream) {
+  if (dtype != SIMSD_F32 && dtype != SIMSD_BF16) return unsupported("dtype");
+  const int eb = dtype == SIMSD_F32 ? 4 : 2;
+  if (T < 0 || Bt < 0) return arg_fail("T < 0 or Bt < 0");
+  if (Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0) return arg_fail("Hq must be a positive multiple of Hkv");
+  if (num_pages < 0 || max_pages < 0 || mask_block < 0 || window < 0) return arg_fail("negative size");
+  if (!page_size_ok(page_size)) return unsupported("page_size must be a multiple of 64 or a divisor of 64 (>= 8)");
+  if (d != 64 && d != 128) return unsupported("d must be 64 or 128");
+  if (!(softmax_scale >= 0.f) || std::isinf(softmax_scale)) return arg_fail("softmax_scale");
+  if (static_cast<long long>(max_pages) * page_size > 0x7fffff00ll) return unsupported("more than 2^31 rows a sequence");
+  if (static_cast<long long>(T) * Hq >= (1ll << 31)) return unsupported("too many query rows");
+  if (T == 0 || Bt == 0) return SIMSD_OK;
+  if (!token_start || !prefix_len || !block_table || !k_cache || !v_cache || !out) return arg_fail("null pointer");
+  if (num_pages == 0 || max_pages == 0) return arg_fail("no pages");
+  if (!rows_ok(q, q_stride, Hq, d, eb)) return arg_fail("q: null, misaligned or overlapping rows");
+  if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out))
+    return arg_fail("tensor pointers must be 16-byte aligned");
+  DeviceInfo info;
+  int rc = require_sm103(&info);
+  if (rc != SIMSD_OK) return rc;
+  simsd::ChunkArgs a{};
+  a.q = q;
+  a.q_stride = q_stride;
+  a.token_start = token_start;
+  a.prefix_len = prefix_len;
+  a.key_start = key_start;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.block_table = block_table;
+  a.out = out;
+  a.lse = lse;
+  a.err_word = err_word;
+  a.T = T;
+  a.Bt = Bt;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.num_pages = num_pages;
+  a.max_pages = max_pages;
+  a.page_size = page_size;
+  a.mask_block = mask_block;
+  a.window = window;
+  a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt(static_cast<float>(d));
+  if (dtype == SIMSD_F32) {
+    cudaError_t e = simsd::launch_chunk_attention_f32(a, as_stream(stream));
+    return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "chunk_attention_f32 launch");
+  }
+  if (Hq / Hkv > 128) return unsupported("Hq / Hkv above 128");
+  if (Bt > simsd::kChunkMaxSeqs) return unsupported("more than 16384 sequences");
+  if (static_cast<long long>(num_pages) * Hkv * page_size >= (1ll << 31))
+    return unsupported("page pool too large for 32-bit TMA row coordinates");
+  const size_t need = simsd::chunk_tc_workspace_bytes(T, Bt, Hq, Hkv, d, static_cast<long long>(max_pages) * page_size,
+                                                      info.num_sms);
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+    return arg_fail("workspace smaller than simsd_chunk_workspace_bytes()");
+  a.workspace = workspace;
+  simsd::EncodeTiledFn enc = encoder();
+  if (!enc) return cuda_fail(cudaErrorNotSupported, "cuTensorMapEncodeTiled entry point");
+  cudaError_t e = simsd::launch_chunk_attention_tc(a, info.num_sms, enc, as_stream(stream));
+  return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "chunk_attention_tc launch");
+}
+
+int simsd_sample(int dtype, const void* logits, int64_t row_stride, int R, int vocab, const float* u,
+                 const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                 int32_t* token, int32_t* kept, float* log_prob, float* log_probs, int32_t* err_word, void* stream) {
+  if (dtype != SIMSD_F32 && dtype != SIMSD_BF16) return unsupported("dtype");
+  if (R < 0) return arg_fail("R < 0");
+  if (vocab < 1 || vocab > (1 << 24)) return arg_fail("vocab must be in [1, 2^24]");
+  if (row_stride < vocab) return arg_fail("row_stride smaller than the vocabulary");
+  if (R == 0) return SIMSD_OK;
+  if (!logits || !u || !token) return arg_fail("null pointer");
+  if (!aligned16(logits) || (log_probs && !aligned16(log_probs)))
+    return arg_fail("tensor pointers must be 16-byte aligned");
+  DeviceInfo info;
+  int rc = require_sm103(&info);
+  if (rc != SIMSD_OK) return rc;
+  simsd::SampleArgs a{};
+  a.logits = logits;
+  a.row_stride = row_stride;
+  a.R = R;
+  a.V = vocab;
+  a.u = u;
+  a.temperature = temperature;
+  a.top_k = top_k;
+  a.top_p = top_p;
+  a.min_p = min_p;
+  a.token = token;
+  a.kept = kept;
+  a.log_prob = log_prob;
+  a.log_probs = log_probs;
+  a.err_word = err_word;
+  cudaError_t e = simsd::launch_sample(dtype == SIMSD_F32 ? 4 : 2, a, info.num_sms, as_stream(stream));
+  return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "sample launch");
+}
+
 int simsd_debug_expire_next_wait(int which, unsigned int limit_us) {
   if (which != SIMSD_DEBUG_WAIT_ATTENTION && which != SIMSD_DEBUG_WAIT_ACCEPT) return arg_fail("which");
   if (limit_us < 10 || limit_us > 1000000) return arg_fail("limit_us must be in [10, 10^6]");

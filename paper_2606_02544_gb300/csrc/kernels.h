@@ -6,6 +6,8 @@
 #include <cstddef>
 #include <cstdint>
 
+#include "../../include/simsd.h"
+
 namespace simsd {
 
 // Rotary embedding frequencies theta^(-2i/d), i < d/2 <= 64, each as an
@@ -129,6 +131,53 @@ cudaError_t launch_attention_tc256(const AttnTcArgs& a, const AttnTcPlan& pl, En
                                    cudaStream_t stream);
 // Merge of split partials (workspace layout of the plan) into the output.
 cudaError_t launch_attention_combine(const AttnTcArgs& a, const AttnTcPlan& pl, cudaStream_t stream);
+
+// Rotary positions of T tokens' q (and k) rows, and with k_cache the append
+// of k and v to the paged cache (rope_append.cu).
+struct RopeArgs {
+  simsd_rope_plan plan;
+  const void *q, *k, *v;              // v: append only
+  long long q_stride, k_stride, v_stride;  // elements from token to token
+  void *q_out, *k_out;                // k_out: rotate only
+  long long q_out_stride, k_out_stride;
+  void *k_cache, *v_cache;            // null: rotate only
+  const int32_t *token_start, *prefix_len, *positions, *block_table;
+  int32_t* err_word;
+  int T, Bt, Hq, Hkv, d, num_pages, max_pages, page_size;
+  int groups, tokens_block;  // set by the launcher: head groups of a token, tokens of a block
+};
+cudaError_t launch_rope(int elem_bytes, const RopeArgs& a, int num_sms, cudaStream_t stream);
+
+// Attention of chunks of new tokens over the paged cache.
+struct ChunkArgs {
+  const void *q, *k_cache, *v_cache;
+  long long q_stride;  // elements from token to token
+  const int32_t *token_start, *prefix_len, *key_start, *block_table;  // key_start: null or [Bt]
+  void* out;
+  float* lse;  // null or [T][Hq]
+  void* workspace;
+  int32_t* err_word;
+  int T, Bt, Hq, Hkv, d, num_pages, max_pages, page_size, mask_block, window;
+  float scale;
+};
+cudaError_t launch_chunk_attention_f32(const ChunkArgs& a, cudaStream_t stream);
+// bf16 on the tensor cores; Hq / Hkv <= 128, d 64 or 128, Bt <= kChunkMaxSeqs
+constexpr int kChunkMaxSeqs = 16384;
+size_t chunk_tc_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, long long max_keys, int num_sms);
+cudaError_t launch_chunk_attention_tc(const ChunkArgs& a, int num_sms, EncodeTiledFn encode, cudaStream_t stream);
+
+// One token from each row of logits (sample.cu).
+struct SampleArgs {
+  const void* logits;
+  long long row_stride;
+  int R, V;
+  const float *u, *temperature, *top_p, *min_p;  // the last three may be null
+  const int32_t* top_k;                          // may be null
+  int32_t *token, *kept;                         // kept may be null
+  float *log_prob, *log_probs;                   // may be null
+  int32_t* err_word;
+};
+cudaError_t launch_sample(int elem_bytes, const SampleArgs& a, int num_sms, cudaStream_t stream);
 
 // Static device scratch of simsd_verify_attention_noalloc.
 size_t noalloc_scratch_capacity();
