@@ -33,6 +33,7 @@ __device__ __forceinline__ int key_hi(const ChunkArgs& a, const ChunkSeq& s, int
   const int N = s.n + s.C;
   if (a.mask_block == 0) return N;
   const int p = s.n + i;
+  if (a.mask_block == 1) return p + 1;
   const long long h = static_cast<long long>(p / a.mask_block + 1) * a.mask_block;
   return static_cast<int>(min(static_cast<long long>(N), h));
 }

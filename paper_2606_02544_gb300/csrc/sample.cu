@@ -5,8 +5,8 @@
 // Mathematics.  w_v = exp((x_v - m) / T), m = max x.  The kept set is a
 // prefix of the order (x falling, index rising): {x > kappa} and the tokens
 // x = kappa up to some index, cut by w >= min_p.  Sums of weights are 64-bit
-// integers in units of 2^-38 of the largest weight; a thread adds at most
-// kBatch weights in fp32 before it converts.
+// integers in units of 2^-38 of the largest weight (a token whose number hangs
+// on the last bits of a sum of 150,000 weights is still the right one).
 //
 // A row is read twice.  The first pass (from HBM) takes the maximum and a
 // histogram of counts over bins 1/128 wide in x / T.  A bin's weights differ
@@ -61,11 +61,25 @@ __device__ __forceinline__ float from_ordered(uint32_t k) {
 }
 __device__ __forceinline__ u64 units(float w) { return __float2ull_rn(w * kUnit); }
 
-// The part f of a sum, f in [0, 1) taken to 2^-32: floor and ceiling.
-__device__ __forceinline__ u64 frac32(float f) { return __float2ull_rz(f * 4294967296.0f) << 32; }
-__device__ __forceinline__ u64 part_floor(float f, u64 sum) { return __umul64hi(sum, frac32(f)); }
+// A sum of a batch of weights, exact to 2^-34: the parts of the weights that
+// are multiples of 2^-13 add up exactly, the rests are below 2^-13.
+struct BatchSum {
+  float hi = 0.f, lo = 0.f;
+  __device__ __forceinline__ void add(float w) {
+    const float h = __fsub_rn(__fadd_rn(w, 1536.f), 1536.f);
+    hi = __fadd_rn(hi, h);
+    lo = __fadd_rn(lo, __fsub_rn(w, h));
+  }
+  __device__ __forceinline__ u64 total() const {
+    return static_cast<u64>(__float2ll_rn(hi * kUnit) + __float2ll_rn(lo * kUnit));
+  }
+};
+
+// The part f of a sum, f in [0, 1): floor and ceiling.
+__device__ __forceinline__ u64 fraction(float f) { return __float2ull_rz(f * 18446744073709551616.0f); }
+__device__ __forceinline__ u64 part_floor(float f, u64 sum) { return __umul64hi(sum, fraction(f)); }
 __device__ __forceinline__ u64 part_ceil(float f, u64 sum) {
-  const u64 q = frac32(f);
+  const u64 q = fraction(f);
   return __umul64hi(sum, q) + (sum * q ? 1 : 0);
 }
 // Natural logarithm of a sum of weights in units of 2^-38 (no 64-bit floating point).
@@ -574,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const bool need_all = !by_count && set_mass == 0;
     u64 n = 0, q = 0, qa = 0;
     row.batches(rank, [&](float (&x)[kUnroll][kVec], int i0) {
-      float s = 0.f, sa = 0.f;
+      BatchSum s, sa;
       int cnt = 0;
 #pragma unroll
       for (int i = 0; i < kUnroll; ++i)
@@ -584,8 +598,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           const bool above = y >= y1;
           if (need_all || above) {
             const float w = wt.w(x[i][e]);
-            sa += w;
-            s += above ? w : 0.f;
+            sa.add(w);
+            s.add(above ? w : 0.f);
           }
           cnt += above ? 1 : 0;
           if (!above && y >= y0) {
@@ -595,8 +609,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           }
         }
       n += cnt;
-      q += units(s);
-      qa += units(sa);
+      q += s.total();
+      qa += sa.total();
     });
     const u64 seg = warp_sum(q);
     if (lane == 0) st_rank(&sm.seg[rank * kWarps + warp], 0, seg);
@@ -747,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   if (!have_seg || mp > 0.f) {
     u64 n = 0, q = 0;
     row.batches(rank, [&](float (&x)[kUnroll][kVec], int i0) {
-      float s = 0.f;
+      BatchSum s;
       int cnt = 0;
 #pragma unroll
       for (int i = 0; i < kUnroll; ++i)
@@ -756,11 +770,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           const float w = wt.w(x[i][e]);
           const bool in = x[i][e] != -INFINITY && w >= mp &&
                           kept.in_prefix(ordered(x[i][e]), Row<E>::index(i0, i, e));
-          s += in ? w : 0.f;
+          s.add(in ? w : 0.f);
           cnt += in ? 1 : 0;
         }
       n += cnt;
-      q += units(s);
+      q += s.total();
     });
     const u64 seg = warp_sum(q);
     if (lane == 0) st_rank(&sm.seg[rank * kWarps + warp], 0, seg);
