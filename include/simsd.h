@@ -462,8 +462,9 @@ SIMSD_API int simsd_rope_append(int dtype, const simsd_rope_plan* plan, const vo
  * simsd_rope_append) sets SIMSD_EW_PREFIX_LEN and zeroes the sequence's
  * rows; a page id outside the pool among the rows that a group of
  * neighbouring tokens sees sets SIMSD_EW_PAGE and zeroes the rows of that
- * group.  With SIMSD_BF16 a value row that is not finite may also reach the
- * rows of tokens up to 256 Hkv/Hq places before the first that sees it.
+ * group.  A value row that is not finite may also reach the rows of tokens
+ * up to 256 Hkv/Hq places before the first that sees it (0 times it is not 0);
+ * rows that no token of such a group sees are never used.
  */
 SIMSD_API size_t simsd_chunk_workspace_bytes(int dtype, int T, int Bt, int Hq, int Hkv, int d, int max_pages,
                                              int page_size);

@@ -611,11 +611,14 @@ int simsd_rope_append(int dtype, const simsd_rope_plan* plan, const void* q, int
 }
 
 size_t simsd_chunk_workspace_bytes(int dtype, int T, int Bt, int Hq, int Hkv, int d, int max_pages, int page_size) {
-  if (dtype != SIMSD_BF16 || T <= 0 || Bt <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || (d != 64 && d != 128) ||
-      max_pages < 0 || page_size <= 0)
+  if ((dtype != SIMSD_BF16 && dtype != SIMSD_F32) || T <= 0 || Bt <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 ||
+      (d != 64 && d != 128) || max_pages < 0 || page_size <= 0)
     return 0;
   DeviceInfo info;
   if (device_info(&info) != SIMSD_OK) return 0;
+  if (dtype == SIMSD_F32)
+    return simsd::chunk_f32_workspace_bytes(T, Bt, Hq, Hkv, d, static_cast<long long>(max_pages) * page_size,
+                                            info.num_sms);
   return simsd::chunk_tc_workspace_bytes(T, Bt, Hq, Hkv, d, static_cast<long long>(max_pages) * page_size,
                                          info.num_sms);
 }
@@ -668,19 +671,24 @@ int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, const int3
   a.mask_block = mask_block;
   a.window = window;
   a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt(static_cast<float>(d));
+  const long long max_keys = static_cast<long long>(max_pages) * page_size;
+  const size_t need = dtype == SIMSD_F32
+                          ? simsd::chunk_f32_workspace_bytes(T, Bt, Hq, Hkv, d, max_keys, info.num_sms)
+                          : simsd::chunk_tc_workspace_bytes(T, Bt, Hq, Hkv, d, max_keys, info.num_sms);
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+    return arg_fail("workspace smaller than simsd_chunk_workspace_bytes()");
+  a.workspace = workspace;
   if (dtype == SIMSD_F32) {
-    cudaError_t e = simsd::launch_chunk_attention_f32(a, as_stream(stream));
+    cudaError_t e = simsd::launch_chunk_attention_f32(a, info.num_sms, as_stream(stream));
     return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "chunk_attention_f32 launch");
   }
   if (Hq / Hkv > 128) return unsupported("Hq / Hkv above 128");
   if (Bt > simsd::kChunkMaxSeqs) return unsupported("more than 16384 sequences");
   if (static_cast<long long>(num_pages) * Hkv * page_size >= (1ll << 31))
     return unsupported("page pool too large for 32-bit TMA row coordinates");
-  const size_t need = simsd::chunk_tc_workspace_bytes(T, Bt, Hq, Hkv, d, static_cast<long long>(max_pages) * page_size,
-                                                      info.num_sms);
-  if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
-    return arg_fail("workspace smaller than simsd_chunk_workspace_bytes()");
-  a.workspace = workspace;
+  // key tiles are counted in 32 bits (2^31 of them would take hours)
+  if ((static_cast<long long>(T) * Hq / 128 + static_cast<long long>(Bt) * Hkv + 1) * (max_keys / 128 + 1) >= (1ll << 31))
+    return unsupported("too many key tiles in one call");
   simsd::EncodeTiledFn enc = encoder();
   if (!enc) return cuda_fail(cudaErrorNotSupported, "cuTensorMapEncodeTiled entry point");
   cudaError_t e = simsd::launch_chunk_attention_tc(a, info.num_sms, enc, as_stream(stream));

@@ -160,7 +160,8 @@ struct ChunkArgs {
   int T, Bt, Hq, Hkv, d, num_pages, max_pages, page_size, mask_block, window;
   float scale;
 };
-cudaError_t launch_chunk_attention_f32(const ChunkArgs& a, cudaStream_t stream);
+size_t chunk_f32_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, long long max_keys, int num_sms);
+cudaError_t launch_chunk_attention_f32(const ChunkArgs& a, int num_sms, cudaStream_t stream);
 // bf16 on the tensor cores; Hq / Hkv <= 128, d 64 or 128, Bt <= kChunkMaxSeqs
 constexpr int kChunkMaxSeqs = 16384;
 size_t chunk_tc_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, long long max_keys, int num_sms);
