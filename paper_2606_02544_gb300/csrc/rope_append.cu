@@ -13,8 +13,11 @@
 // thread owns one pair of VE-wide vectors (the two halves of VE pairs, or
 // two vectors of interleaved pairs) of one token and walks over heads, so
 // the VE angles it forms serve every head it visits; kHeadsInFlight heads'
-// loads are issued together.  Few tokens are spread over more threads by
-// giving each fewer heads (down to one).
+// loads are issued together (two: with four the registers leave half the
+// threads, 108 us instead of 87 for 16384 tokens of 32/8 heads, bf16; angles
+// formed once a block in shared memory, 91 us).  Few tokens are spread over
+// more threads by giving each fewer heads (down to one).  403 MB in 87 us:
+// 4.6 TB/s; what remains is the latency of a thread's loads.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -28,8 +31,8 @@ namespace simsd {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxTokens = 32;  // tokens of a block
-constexpr int kHeadsInFlight = 4;
+constexpr int kMaxTokens = 64;  // tokens of a block
+constexpr int kHeadsInFlight = 2;
 
 template <typename E, int VE>
 struct alignas(sizeof(E) * VE) Vec {
@@ -87,7 +90,7 @@ __device__ Token resolve(const RopeArgs& a, int tok) {
 // interleaved pairs are taken one component at a time), then pairs of
 // vectors of the rest; a row of V is copied over the same tasks.
 template <typename E, int VE>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(kThreads, 3) rope_kernel(const __grid_constant__ RopeArgs a) {
   using V = Vec<E, VE>;
   __shared__ Token toks[kMaxTokens];
   pdl_wait();
@@ -210,8 +213,11 @@ cudaError_t launch_ve(RopeArgs a, int num_sms, cudaStream_t stream) {
   const long long want = 2ll * 2048 * num_sms;
   const long long per_head = std::max<long long>(1, static_cast<long long>(a.T) * tasks);
   a.groups = static_cast<int>(std::min<long long>(heads, std::max<long long>(1, want / per_head)));
-  // a block's threads all busy, at most kMaxTokens tokens
-  a.tokens_block = std::max(1, std::min(kMaxTokens, kThreads / (tasks * a.groups)));
+  // a block's threads all busy, and of many tokens so many that the blocks
+  // (three a SM) make one wave: finding a token's sequence and page is a
+  // chain of loads, on which a block of few tokens spends most of its time
+  a.tokens_block = std::max(kThreads / (tasks * a.groups), (a.T + 3 * num_sms - 1) / (3 * num_sms));
+  a.tokens_block = std::max(1, std::min(kMaxTokens, a.tokens_block));
   const unsigned blocks = static_cast<unsigned>((a.T + a.tokens_block - 1) / a.tokens_block);
   return launch_overlapped(rope_kernel<E, VE>, dim3(blocks), dim3(kThreads), 0, stream, 1u, a);
 }

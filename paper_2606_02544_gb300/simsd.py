@@ -285,38 +285,54 @@ def simsd_accept_sampled_ws(target_logits, draft_logits, draft, u_accept, u_samp
 
 
 # ------------------------------------------------------------------ prompts
+# (These calls sit in decoding loops of a few microseconds, so their checks
+# are written out: no message is built and no helper called unless one fails.)
+_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _raw_stream(stream):
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+def _raw_stream(stream, t):
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+def _wrong(what):
+    raise ValueError(what)
 
 
-def _rows(t, name):
+def _code(dtype):
+    if dtype is _BF16:
+        return SIMSD_BF16
+    if dtype is _F32:
+        return SIMSD_F32
+    raise TypeError(f"unsupported dtype {dtype}")
+
+
+def _rows(t, H, d, name):
     """Token stride of a [T][H][d] tensor whose heads are dense."""
-    T, H, d = t.shape
-    s = t.stride()
-    _need((s[2] == 1 or d == 1) and (s[1] == d or H == 1), f"{name}: the heads of a token must be dense")
-    return s[0] if T > 1 else H * d
+    s0, s1, s2 = t.stride()
+    if (s2 != 1 and d > 1) or (s1 != d and H > 1):
+        raise ValueError(f"{name}: the heads of a token must be dense")
+    return s0 if t.shape[0] > 1 else H * d
 
 
-def _int32(t, n, name):
-    _need(t.dtype == torch.int32 and t.numel() == n and t.is_contiguous(), f"{name}: {n} dense int32 wanted")
+def _dense_i32(t, n):
+    return t.dtype is _I32 and t.numel() == n and t.is_contiguous()
 
 
 def _cache_sizes(k_cache, v_cache, block_table, Bt, Hkv, d, dtype):
-    _need(k_cache.shape == v_cache.shape and k_cache.dim() == 4 and k_cache.shape[1] == Hkv
-          and k_cache.shape[3] == d and k_cache.dtype == dtype and v_cache.dtype == dtype
-          and k_cache.is_contiguous() and v_cache.is_contiguous(), "k_cache / v_cache: [num_pages][Hkv][P][d] wanted")
-    _need(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.shape[0] == Bt
-          and block_table.is_contiguous(), "block_table: dense int32 [Bt][max_pages] wanted")
-    return k_cache.shape[0], block_table.shape[1], k_cache.shape[2]
+    N, h, P, dd = k_cache.shape
+    if not (h == Hkv and dd == d and v_cache.shape == k_cache.shape and k_cache.dtype is dtype
+            and v_cache.dtype is dtype and k_cache.is_contiguous() and v_cache.is_contiguous()):
+        raise ValueError("k_cache / v_cache: dense [num_pages][Hkv][P][d] of q's type wanted")
+    n, max_pages = block_table.shape
+    if not (n == Bt and block_table.dtype is _I32 and block_table.is_contiguous()):
+        raise ValueError("block_table: dense int32 [Bt][max_pages] wanted")
+    return N, max_pages, P
 
 
 def simsd_rope_plan_init(layout, rot_dim, theta, scaling="none", factor=1.0, context=0, beta_fast=32.0,
@@ -324,6 +340,8 @@ def simsd_rope_plan_init(layout, rot_dim, theta, scaling="none", factor=1.0, con
     """The rotation of a model's heads: layout "half" or "interleaved" over the
     first rot_dim components; scaling "none", "linear", "ntk" or "yarn" by
     ``factor`` (YaRN: over a trained ``context``).  Host only; keep the plan."""
+    if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
+        _wrong(f"layout {sorted(ROPE_LAYOUTS)}, scaling {sorted(ROPE_SCALINGS)}")
     plan = RopePlan()
     rc = load_library().simsd_rope_plan_init(ctypes.addressof(plan), ROPE_LAYOUTS[layout], rot_dim, theta,
                                              ROPE_SCALINGS[scaling], factor, context, beta_fast, beta_slow)
@@ -335,19 +353,25 @@ def simsd_rope_rotate(plan, positions, q, q_out, k=None, k_out=None, stream=None
     """q/q_out [T][Hq][d], k/k_out [T][Hkv][d] (token strides allowed, in place
     allowed); positions [T] int32."""
     T, Hq, d = q.shape
-    _need(q_out.shape == q.shape and q_out.dtype == q.dtype, "q_out: shape and type of q wanted")
-    _int32(positions, T, "positions")
+    dt = q.dtype
+    if q_out.shape != q.shape or q_out.dtype is not dt:
+        _wrong("q_out: shape and type of q wanted")
+    if not _dense_i32(positions, T):
+        _wrong("positions: dense int32 [T] wanted")
     Hkv = ks = kos = 0
+    kp = kop = None
     if k is not None:
-        Hkv, ks = k.shape[1], _rows(k, "k")
-        _need(k.shape == (T, Hkv, d) and k_out is not None and k_out.shape == k.shape and k.dtype == q.dtype
-              and k_out.dtype == q.dtype, "k / k_out: [T][Hkv][d] of q's type wanted")
-        kos = _rows(k_out, "k_out")
-    rc = load_library().simsd_rope_rotate(_dtype_code(q), ctypes.addressof(plan), positions.data_ptr(), q.data_ptr(),
-                                          _rows(q, "q"), q_out.data_ptr(), _rows(q_out, "q_out"), Hq, _ptr(k), ks,
-                                          _ptr(k_out) if k is not None else None, kos, Hkv, T, d,
-                                          _raw_stream(stream))
-    _check(rc, "simsd_rope_rotate")
+        Hkv = k.shape[1]
+        if (k_out is None or k.shape != (T, Hkv, d) or k_out.shape != k.shape or k.dtype is not dt
+                or k_out.dtype is not dt):
+            _wrong("k / k_out: [T][Hkv][d] of q's type wanted")
+        ks, kos = _rows(k, Hkv, d, "k"), _rows(k_out, Hkv, d, "k_out")
+        kp, kop = k.data_ptr(), k_out.data_ptr()
+    rc = (_lib or load_library()).simsd_rope_rotate(
+        _code(dt), ctypes.addressof(plan), positions.data_ptr(), q.data_ptr(), _rows(q, Hq, d, "q"),
+        q_out.data_ptr(), _rows(q_out, Hq, d, "q_out"), Hq, kp, ks, kop, kos, Hkv, T, d, _raw_stream(stream, q))
+    if rc:
+        _check(rc, "simsd_rope_rotate")
 
 
 def simsd_rope_append(plan, q, k, v, token_start, prefix_len, q_out, k_cache, v_cache, block_table, positions=None,
@@ -356,21 +380,23 @@ def simsd_rope_append(plan, q, k, v, token_start, prefix_len, q_out, k_cache, v_
     [Bt+1], prefix_len [Bt]; q_out [T][Hq][d] dense; k_cache/v_cache
     [num_pages][Hkv][P][d].  prefix_len is not advanced."""
     T, Hq, d = q.shape
-    Hkv, Bt = k.shape[1], prefix_len.shape[0]
-    _need(k.shape == (T, Hkv, d) and v.shape == k.shape and k.dtype == q.dtype and v.dtype == q.dtype,
-          "k / v: [T][Hkv][d] of q's type wanted")
-    _need(q_out.shape == q.shape and q_out.dtype == q.dtype and q_out.is_contiguous(), "q_out: dense, like q")
-    _int32(token_start, Bt + 1, "token_start")
-    _int32(prefix_len, Bt, "prefix_len")
-    if positions is not None:
-        _int32(positions, T, "positions")
-    num_pages, max_pages, P = _cache_sizes(k_cache, v_cache, block_table, Bt, Hkv, d, q.dtype)
-    rc = load_library().simsd_rope_append(
-        _dtype_code(q), ctypes.addressof(plan), q.data_ptr(), _rows(q, "q"), k.data_ptr(), _rows(k, "k"),
-        v.data_ptr(), _rows(v, "v"), token_start.data_ptr(), prefix_len.data_ptr(), _ptr(positions), T, Bt, Hq, Hkv,
-        d, q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), num_pages, block_table.data_ptr(), max_pages, P,
-        _ptr(err_word), _raw_stream(stream))
-    _check(rc, "simsd_rope_append")
+    Hkv, Bt, dt = k.shape[1], prefix_len.shape[0], q.dtype
+    if k.shape != (T, Hkv, d) or v.shape != k.shape or k.dtype is not dt or v.dtype is not dt:
+        _wrong("k / v: [T][Hkv][d] of q's type wanted")
+    if q_out.shape != q.shape or q_out.dtype is not dt or not q_out.is_contiguous():
+        _wrong("q_out: dense, like q")
+    if not _dense_i32(token_start, Bt + 1) or not _dense_i32(prefix_len, Bt):
+        _wrong("token_start / prefix_len: dense int32 [Bt+1] / [Bt] wanted")
+    if positions is not None and not _dense_i32(positions, T):
+        _wrong("positions: dense int32 [T] wanted")
+    num_pages, max_pages, P = _cache_sizes(k_cache, v_cache, block_table, Bt, Hkv, d, dt)
+    rc = (_lib or load_library()).simsd_rope_append(
+        _code(dt), ctypes.addressof(plan), q.data_ptr(), _rows(q, Hq, d, "q"), k.data_ptr(), _rows(k, Hkv, d, "k"),
+        v.data_ptr(), _rows(v, Hkv, d, "v"), token_start.data_ptr(), prefix_len.data_ptr(), _ptr(positions), T, Bt,
+        Hq, Hkv, d, q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), num_pages, block_table.data_ptr(),
+        max_pages, P, _ptr(err_word), _raw_stream(stream, q))
+    if rc:
+        _check(rc, "simsd_rope_append")
 
 
 def simsd_chunk_workspace_bytes(dtype_code, T, Bt, Hq, Hkv, d, max_pages, page_size) -> int:
@@ -384,23 +410,42 @@ def simsd_chunk_attention(q, token_start, prefix_len, k_cache, v_cache, block_ta
     window > 0: that many rows back; key_start [Bt]: earlier rows hidden.
     out [T][Hq][d], lse [T][Hq] fp32."""
     T, Hq, d = q.shape
-    Bt, Hkv = prefix_len.shape[0], k_cache.shape[1]
-    _need(out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous(), "out: dense, like q")
-    _int32(token_start, Bt + 1, "token_start")
-    _int32(prefix_len, Bt, "prefix_len")
-    if key_start is not None:
-        _int32(key_start, Bt, "key_start")
-    if lse is not None:
-        _need(lse.shape == (T, Hq) and lse.dtype == torch.float32 and lse.is_contiguous(),
-              "lse: dense float32 [T][Hq] wanted")
-    num_pages, max_pages, P = _cache_sizes(k_cache, v_cache, block_table, Bt, Hkv, d, q.dtype)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = load_library().simsd_chunk_attention(
-        _dtype_code(q), q.data_ptr(), _rows(q, "q"), token_start.data_ptr(), prefix_len.data_ptr(), _ptr(key_start),
-        k_cache.data_ptr(), v_cache.data_ptr(), num_pages, block_table.data_ptr(), max_pages, P, T, Bt, Hq, Hkv, d,
-        mask_block, window, softmax_scale, out.data_ptr(), _ptr(lse), _ptr(workspace), ws_bytes, _ptr(err_word),
-        _raw_stream(stream))
-    _check(rc, "simsd_chunk_attention")
+    Bt, Hkv, dt = prefix_len.shape[0], k_cache.shape[1], q.dtype
+    if out.shape != q.shape or out.dtype is not dt or not out.is_contiguous():
+        _wrong("out: dense, like q")
+    if not _dense_i32(token_start, Bt + 1) or not _dense_i32(prefix_len, Bt):
+        _wrong("token_start / prefix_len: dense int32 [Bt+1] / [Bt] wanted")
+    if key_start is not None and not _dense_i32(key_start, Bt):
+        _wrong("key_start: dense int32 [Bt] wanted")
+    if lse is not None and (lse.shape != (T, Hq) or lse.dtype is not _F32 or not lse.is_contiguous()):
+        _wrong("lse: dense float32 [T][Hq] wanted")
+    num_pages, max_pages, P = _cache_sizes(k_cache, v_cache, block_table, Bt, Hkv, d, dt)
+    ws = ws_bytes = 0
+    if workspace is not None:
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    rc = (_lib or load_library()).simsd_chunk_attention(
+        _code(dt), q.data_ptr(), _rows(q, Hq, d, "q"), token_start.data_ptr(), prefix_len.data_ptr(),
+        _ptr(key_start), k_cache.data_ptr(), v_cache.data_ptr(), num_pages, block_table.data_ptr(), max_pages, P, T,
+        Bt, Hq, Hkv, d, mask_block, window, softmax_scale, out.data_ptr(), _ptr(lse), ws, ws_bytes, _ptr(err_word),
+        _raw_stream(stream, q))
+    if rc:
+        _check(rc, "simsd_chunk_attention")
+
+
+def _row_f32(t, R, name):
+    if t is None:
+        return None
+    if t.dtype is not _F32 or t.numel() != R or not t.is_contiguous():
+        _wrong(name + ": dense float32 [R] wanted")
+    return t.data_ptr()
+
+
+def _row_i32(t, R, name):
+    if t is None:
+        return None
+    if t.dtype is not _I32 or t.numel() != R or not t.is_contiguous():
+        _wrong(name + ": dense int32 [R] wanted")
+    return t.data_ptr()
 
 
 def simsd_sample(logits, u, token, temperature=None, top_k=None, top_p=None, min_p=None, kept=None, log_prob=None,
@@ -410,17 +455,16 @@ def simsd_sample(logits, u, token, temperature=None, top_k=None, top_p=None, min
     log_prob [R] and log_probs [R][V] float32 (outputs; all but token
     optional)."""
     R, V = logits.shape
-    _need(logits.stride(1) == 1 or V == 1, "logits: dense rows wanted")
-    for t, name in ((u, "u"), (temperature, "temperature"), (top_p, "top_p"), (min_p, "min_p"), (log_prob, "log_prob")):
-        _need(t is None or (t.dtype == torch.float32 and t.numel() == R and t.is_contiguous()),
-              f"{name}: {R} dense float32 wanted")
-    for t, name in ((token, "token"), (top_k, "top_k"), (kept, "kept")):
-        if t is not None:
-            _int32(t, R, name)
-    _need(log_probs is None or (log_probs.shape == (R, V) and log_probs.dtype == torch.float32
-                                and log_probs.is_contiguous()), "log_probs: dense float32 [R][V] wanted")
-    rc = load_library().simsd_sample(
-        _dtype_code(logits), logits.data_ptr(), logits.stride(0) if R > 1 else V, R, V, u.data_ptr(),
-        _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), token.data_ptr(), _ptr(kept), _ptr(log_prob),
-        _ptr(log_probs), _ptr(err_word), _raw_stream(stream))
-    _check(rc, "simsd_sample")
+    s0, s1 = logits.stride()
+    if s1 != 1 and V > 1:
+        _wrong("logits: dense rows wanted")
+    if log_probs is not None and (log_probs.shape != (R, V) or log_probs.dtype is not _F32
+                                  or not log_probs.is_contiguous()):
+        _wrong("log_probs: dense float32 [R][V] wanted")
+    rc = (_lib or load_library()).simsd_sample(
+        _code(logits.dtype), logits.data_ptr(), s0 if R > 1 else V, R, V, _row_f32(u, R, "u"),
+        _row_f32(temperature, R, "temperature"), _row_i32(top_k, R, "top_k"), _row_f32(top_p, R, "top_p"),
+        _row_f32(min_p, R, "min_p"), _row_i32(token, R, "token"), _row_i32(kept, R, "kept"),
+        _row_f32(log_prob, R, "log_prob"), _ptr(log_probs), _ptr(err_word), _raw_stream(stream, logits))
+    if rc:
+        _check(rc, "simsd_sample")
