@@ -496,7 +496,7 @@ int simsd_rope_plan_init(simsd_rope_plan* plan, int layout, int rot_dim, double 
     // whole turns of a position (theta < 1 only) do not change the angle
     double turns = f / kTwoPi;
     turns -= std::floor(turns);
-    const double scaled = std::ldexp(turns, 64);
+    const double scaled = std::nearbyint(std::ldexp(turns, 64));
     plan->turn[i] = scaled >= 18446744073709551616.0 ? 0 : static_cast<uint64_t>(scaled);
   }
   return SIMSD_OK;

@@ -1,0 +1,82 @@
+"""The prompt path as a whole: chunks into the cache, drafts with their
+distribution, a verified block."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_02544_gb300 import prompt, simsd
+from tests import _prompt as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def test_command_runs(capsys):
+    assert prompt.main() == 0
+    assert "error word 0" in capsys.readouterr().out
+
+
+def _fill(sizes, dtype, seed=3):
+    plan = simsd.simsd_rope_plan_init("interleaved", 64, 1.0e6, "yarn", factor=4.0, context=256)
+    c = prompt.PromptCache(2, 2, 4, 2, 64, 16, 400, plan, mask_block=8, dtype=dtype)
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn(2, 2, 300, 8, 64, generator=g) * 0.5).to(dtype).cuda()  # [layer][sequence][token]
+    outs, done = [], 0
+    for n in sizes:
+        qkv = torch.cat([x[:, 0, done:done + n], x[:, 1, done:done + n]], 1)
+        start = torch.tensor([0, n, 2 * n], dtype=torch.int32, device="cuda")
+        o = c.append_chunk(qkv, start)
+        outs.append(o.view(2, 2, n, 4, 64))
+        done += n
+    assert simsd.simsd_check_error(c.err) == 0
+    return c, torch.cat(outs, 2)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_chunking_does_not_change_the_cache(dtype):
+    """One chunk or many: the cached rows are the same bits, the attention
+    outputs agree within the rounding of both."""
+    a, oa = _fill([300], dtype)
+    b, ob = _fill([8, 120, 1, 7, 164], dtype)
+    assert a.prefix_len.tolist() == b.prefix_len.tolist() == [300, 300]
+    rows = torch.arange(300)
+    for s in range(2):
+        page = a.block_table[s][rows.cuda() // 16].long()
+        for x, y in ((a.k_cache, b.k_cache), (a.v_cache, b.v_cache)):
+            assert torch.equal(x[:, page, :, rows.cuda() % 16], y[:, page, :, rows.cuda() % 16])
+    # mask_block 8 with chunk ends inside a block: a token then misses the
+    # rest of its block, so compare blocks that lie inside one chunk of both
+    inside = [t for t in range(300) if (t // 8 * 8 + 8 <= 8) or (8 <= t // 8 * 8 and t // 8 * 8 + 8 <= 128)
+              or (136 <= t // 8 * 8)]
+    # rounding of P and O to bf16 on both sides: 4 u (A + |r|), |v| <= 3; fp32: 2^-15
+    tol = 4 * 2.0 ** -8 * 3 if dtype == torch.bfloat16 else 2.0 ** -15
+    assert (oa[:, :, inside].double() - ob[:, :, inside].double()).abs().max().item() <= tol
+
+
+def test_drafts_from_a_truncated_distribution_keep_the_target():
+    """Draft and target logits both truncated by simsd_sample: the emitted
+    first token follows the target's truncated distribution (Eq. (2) with
+    residual resampling), and no token outside it ever comes out."""
+    g = torch.Generator().manual_seed(5)
+    Bt, V, gamma = 20000, 24, 1
+    t1, d1 = torch.randn(V, generator=g) * 1.5, torch.randn(V, generator=g) * 1.5
+    plan = simsd.simsd_rope_plan_init("half", 64, 1.0e4)
+    c = prompt.PromptCache(1, 1, 1, 1, 64, 16, 16, plan)
+    f = lambda v, n: torch.full((n,), v, device="cuda")  # noqa: E731
+    k = lambda v, n: torch.full((n,), v, dtype=torch.int32, device="cuda")  # noqa: E731
+    draft, dlp = c.draw(d1.cuda().expand(Bt, gamma, V).contiguous(), torch.rand(Bt, gamma, generator=g).cuda(),
+                        top_k=k(9, Bt), top_p=f(0.9, Bt))
+    n = Bt * (gamma + 1)
+    _, tlp = c.draw(t1.cuda().expand(Bt, gamma + 1, V).contiguous(), torch.rand(Bt, gamma + 1, generator=g).cuda(),
+                    top_k=k(12, n), top_p=f(0.8, n))
+    a = torch.empty(Bt, dtype=torch.int32, device="cuda")
+    ot = torch.empty(Bt, gamma + 1, dtype=torch.int32, device="cuda")
+    simsd.simsd_accept_sampled(tlp, dlp, draft, torch.rand(Bt, gamma, generator=g).cuda(),
+                               torch.rand(Bt, generator=g).cuda(), a, ot, err_word=c.err)
+    assert simsd.simsd_check_error(c.err) == 0
+    _, idx, lp = ref.sample_row(t1.double().numpy(), 0.5, k=12, p=0.8)
+    want = np.zeros(V)
+    want[idx] = np.exp(lp)
+    got = np.bincount(ot[:, 0].cpu().numpy(), minlength=V) / Bt
+    assert (got[want == 0] == 0).all()
+    # five standard deviations of a share
+    assert np.all(np.abs(got - want) <= 5 * np.sqrt(want * (1 - want) / Bt) + 1e-12)

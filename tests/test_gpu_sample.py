@@ -1,0 +1,181 @@
+"""Sampling with temperature, top-k, top-p and min-p from given random numbers
+on the GPU, against the plain 64-bit form."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_02544_gb300 import simsd
+from tests import _prompt as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def run(x, u, T=None, k=None, p=None, mp=None, probs=True):
+    R, V = x.shape
+    dev = dict(device="cuda")
+    f = lambda v: None if v is None else torch.as_tensor(np.asarray(v, dtype=np.float32), **dev)  # noqa: E731
+    token = torch.full((R,), -9, dtype=torch.int32, **dev)
+    kept = torch.full((R,), -9, dtype=torch.int32, **dev)
+    lp = torch.full((R,), float("nan"), **dev)
+    lps = torch.full((R, V), float("nan"), **dev) if probs else None
+    err = torch.zeros(1, dtype=torch.int32, **dev)
+    simsd.simsd_sample(x, f(u), token, temperature=f(T),
+                       top_k=None if k is None else torch.as_tensor(np.asarray(k, dtype=np.int32), **dev), top_p=f(p),
+                       min_p=f(mp), kept=kept, log_prob=lp, log_probs=lps, err_word=err)
+    word = simsd.simsd_check_error(err)
+    return token.cpu().numpy(), kept.cpu().numpy(), lp.cpu().numpy(), lps.cpu().numpy() if probs else None, word
+
+
+def check(x, seed, T=1.0, k=0, p=1.0, mp=0.0, probs=True):
+    """Every row with its own random number (and, as given, parameters)."""
+    R, V = x.shape
+    r = np.random.default_rng(seed)
+    full = lambda v: np.broadcast_to(np.asarray(v, dtype=np.float64), (R,)).astype(np.float32).astype(np.float64).copy()  # noqa: E731
+    T, p, mp = full(T), full(p), full(mp)
+    k = np.broadcast_to(np.asarray(k), (R,)).copy()
+    u = r.random(R)
+    rows = x.double().cpu().numpy()
+    for i in range(R):
+        u[i], p[i], mp[i] = ref.settle(rows[i], u[i], T[i], k[i], p[i], mp[i])
+    u, p, mp = (v.astype(np.float32) for v in (u, p, mp))
+    token, kept, lp, lps, word = run(x, u, T, k, p, mp, probs)
+    assert word == 0
+    for i in range(R):
+        t, idx, logp = ref.sample_row(rows[i], float(u[i]), T[i], k[i], float(p[i]), float(mp[i]))
+        assert token[i] == t, i
+        assert kept[i] == len(idx), i
+        want = logp[list(idx).index(t)]
+        # fp32: z = (x - m) / T correctly rounded, the logarithm of the sum to 2^-22 of a few tens
+        tol = 2.0 ** -20 * (1 + abs(want))
+        assert abs(lp[i] - want) <= tol, i
+        if probs:
+            dist = np.full(V, -np.inf)
+            dist[idx] = logp
+            assert np.array_equal(np.isfinite(lps[i]), np.isfinite(dist)), i
+            ok = np.isfinite(dist)
+            assert np.all(np.abs(lps[i][ok] - dist[ok]) <= 2.0 ** -20 * (1 + np.abs(dist[ok]))), i
+
+
+def logits(R, V, spread, seed, dtype=torch.float32, banned=0.01):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(R, V, generator=g) * spread
+    x.masked_fill_(torch.rand(V, generator=g) < banned, float("-inf"))
+    x[:, seed % V] = 0.5  # a row with at least one logit
+    return x.to(dtype).cuda()
+
+
+LIMITS = [dict(), dict(k=1), dict(k=7), dict(k=100), dict(p=0.9), dict(p=0.999), dict(p=0.0), dict(mp=0.05),
+          dict(k=40, p=0.8), dict(k=90, p=0.95, mp=0.01), dict(T=0.0), dict(T=0.0, k=5, p=0.5)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [1, 2, 33, 1000, 5003])
+@pytest.mark.parametrize("limits", range(len(LIMITS)))
+def test_limits(dtype, V, limits):
+    check(logits(6, V, 2.0, 3 * V + limits, dtype), V, **{"T": 0.8, **LIMITS[limits]})
+
+
+@pytest.mark.parametrize("V,spread,limits", [
+    (40001, 2.0, dict(p=0.9)), (40001, 1.0, dict(p=0.99)), (40001, 4.0, dict(p=0.95)), (40001, 2.0, dict(k=50, p=0.95)),
+    (40001, 0.05, dict(p=0.9)),           # almost flat: bins of the histogram hold more than the list
+    (40001, 0.02, dict(k=20000)), (40001, 1.0, dict(k=9000, p=0.9)), (151936, 2.0, dict(k=1000)),
+    (151936, 3.0, dict(p=0.9)), (300007, 2.0, dict(p=0.5)), (151936, 2.0, dict()), (151936, 2.0, dict(mp=0.02))])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_large_vocabularies(V, spread, limits, dtype):
+    check(logits(3, V, spread, V % 1000 + 1, dtype), V, **{"T": 0.9, **limits}, probs=False)
+
+
+def test_many_rows_and_row_stride():
+    """More rows than clusters of several CTAs are made for; rows that are not
+    16-byte aligned."""
+    wide = logits(700, 1201, 2.0, 5)
+    check(wide[:, :1199], 1, k=30, p=0.9)
+
+
+def test_a_temperature_of_every_size():
+    x = logits(8, 3001, 2.0, 8)
+    check(x, 2, T=[0.0, 1e-3, 0.1, 0.5, 1.0, 3.0, 50.0, 1e4], p=0.9)
+    # so low that 1 / T overflows: only the first token (and its equals) have weight
+    token, kept, lp, _, word = run(x, [0.5] * 8, T=[1e-42] * 8)
+    assert word == 0 and np.array_equal(token, x.argmax(1).cpu().numpy()) and np.all(lp == 0)
+
+
+def test_ties_go_to_the_lowest_index():
+    x = torch.zeros(4, 50, device="cuda")
+    x[:, 10:20] = 3.0
+    x[1] = x[1].flip(0)
+    token, kept, lp, lps, word = run(x, [0.99, 0.99, 0.0, 0.5], k=[4, 4, 15, 1])
+    assert word == 0 and list(kept) == [4, 4, 15, 1]
+    assert list(np.flatnonzero(np.isfinite(lps[0]))) == [10, 11, 12, 13]
+    assert list(np.flatnonzero(np.isfinite(lps[1]))) == [30, 31, 32, 33]
+    assert list(np.flatnonzero(np.isfinite(lps[2]))) == list(range(5)) + list(range(10, 20))
+    assert list(token) == [13, 33, 0, 10]
+    # top_p among equals: half of fifty equal tokens and no more
+    y = torch.full((2, 50), -2.5, device="cuda")
+    _, kept, _, lps, _ = run(y, [0.1, 0.9], p=[0.49, 0.5 + 1e-3])
+    assert list(kept) == [25, 26]
+    assert list(np.flatnonzero(np.isfinite(lps[0]))) == list(range(25))
+
+
+@pytest.mark.parametrize("V", [70000, 1 << 20])
+def test_ties_beyond_the_list(V):
+    """More equal tokens than the list holds: found by index."""
+    x = torch.zeros(2, V, device="cuda")
+    x[:, V // 2] = 1.0
+    token, kept, _, lps, word = run(x, [0.0, 0.999], k=[20001, 20001])
+    assert word == 0 and list(kept) == [20001, 20001]
+    assert np.isfinite(lps[0][:20000]).all() and not np.isfinite(lps[0][20000:V // 2]).any()
+    assert token[0] == 0
+    if V // 2 > 20000:
+        w = np.where(np.arange(V) == V // 2, np.e, 1.0)[np.isfinite(lps[1])]
+        at = np.flatnonzero(np.isfinite(lps[1]))
+        assert token[1] == at[np.flatnonzero(np.cumsum(w) > np.float32(0.999) * w.sum())[0]]
+
+
+def test_infinite_and_nan_logits():
+    V = 300
+    x = torch.randn(5, V, device="cuda")
+    x[0, 7] = float("nan")                      # never drawn
+    x[1, 3] = x[1, 200] = float("inf")          # share the weight
+    x[2] = float("-inf")
+    x[2, 250] = -1e30                           # the only one
+    x[3] = float("-inf")                        # none: an error
+    x[4, ::2] = torch.finfo(torch.float32).min  # masks of the type's lowest value
+    token, kept, lp, lps, word = run(x, [0.9] * 5)
+    assert word == simsd.EW_SAMPLE
+    assert kept[0] == V - 1 and np.isneginf(lps[0, 7])
+    assert token[1] == 200 and lp[1] == pytest.approx(-np.log(2), abs=1e-6)
+    assert token[2] == 250 and kept[2] == 1 and lp[2] == 0
+    assert token[3] == -1 and kept[3] == 0 and np.isneginf(lp[3]) and np.isneginf(lps[3]).all()
+    assert token[4] % 2 == 1
+    assert np.isfinite(lps[[0, 4]].max(1)).all()
+
+
+def test_parameters_out_of_range():
+    x = logits(8, 500, 1.0, 1)
+    ok = run(x, [0.5] * 8)[0]
+    nan, inf = float("nan"), float("inf")
+    token, kept, lp, lps, word = run(x, [0.5, 1.0, -0.1, nan, 0.5, 0.5, 0.5, 0.5], T=[1, 1, 1, 1, -1.0, inf, nan, 1])
+    assert word == simsd.EW_SAMPLE
+    assert list(token[1:7]) == [-1] * 6 and list(kept[1:7]) == [0] * 6
+    assert token[0] == ok[0] and token[7] == ok[7]
+    token, _, _, _, word = run(x, [0.5] * 8, p=[nan] + [1.5] * 7, mp=[0.0, nan] + [0.0] * 6, k=[-3] * 8)
+    assert word == simsd.EW_SAMPLE and list(token[:2]) == [-1, -1] and np.array_equal(token[2:], ok[2:])
+
+
+def test_same_tokens_every_time():
+    x = logits(20, 40000, 1.0, 2)
+    u = np.random.default_rng(0).random(20)
+    a, b = run(x, u, p=[0.9] * 20), run(x, u, p=[0.9] * 20)
+    for s, t in zip(a[:4], b[:4]):
+        assert np.array_equal(s, t)
+
+
+def test_shares_over_a_grid_of_random_numbers():
+    """One row under 20000 random numbers: every kept token in its share."""
+    n, V = 20000, 200
+    x = logits(1, V, 1.5, 4)
+    u = (np.arange(n) + 0.5) / n
+    token, kept, _, lps, _ = run(x.expand(n, V).contiguous(), u, k=[60] * n, p=[0.9] * n)
+    got = np.bincount(token, minlength=V) / n
+    assert np.allclose(got, np.exp(lps[0]), atol=2.0 / n)
