@@ -44,6 +44,7 @@ struct SmemF32 {
   float k[kTile][D];  // 16-byte chunk c of row r lies at chunk c ^ (r & 7)
   float v[kTile][D];
   float p[RB][kTile];
+  long long row[2][kTile];  // per tile parity: a key's row in the pool, in 16-byte units (-1: hidden)
 };
 
 __device__ __forceinline__ void cp_async16(void* dst, const void* src, bool real) {
@@ -142,20 +143,30 @@ __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_consta
   const int t_begin = T0 + static_cast<int>(static_cast<long long>(blockIdx.z) * nt / p.nsplit);
   const int t_end = T0 + static_cast<int>(static_cast<long long>(blockIdx.z + 1) * nt / p.nsplit);
 
-  auto load_tile = [&](int t, bool is_k) {
-    for (int i = tid; i < kTile * (D / 4); i += kThreads) {
-      const int r = i / (D / 4), c = i - r * (D / 4), key = t * kTile + r;
-      const bool real = key >= lo && key < hi;
-      size_t off = 0;
-      if (real) {
+  // where the keys of tile t lie (the page arithmetic once a key, not once a copy)
+  auto find_rows = [&](int t) {
+    if (tid < kTile) {
+      const int key = t * kTile + tid;
+      long long off = -1;
+      if (key >= lo && key < hi) {
         const int pi = key / a.page_size;
-        off = ((static_cast<size_t>(bt[pi]) * a.Hkv + kvh) * a.page_size + (key - pi * a.page_size)) * D + 4 * c;
+        off = ((static_cast<long long>(bt[pi]) * a.Hkv + kvh) * a.page_size + (key - pi * a.page_size)) * (D / 4);
       }
-      const float* src = static_cast<const float*>(is_k ? a.k_cache : a.v_cache) + off;
-      cp_async16(is_k ? &sm.k[r][4 * (c ^ (r & 7))] : &sm.v[r][4 * c], src, real);
+      sm.row[t & 1][tid] = off;
+    }
+  };
+  auto load_tile = [&](int t, bool is_k) {
+    const float4* src = static_cast<const float4*>(is_k ? a.k_cache : a.v_cache);
+    const int c = tid % (D / 4);
+#pragma unroll 4
+    for (int r = tid / (D / 4); r < kTile; r += kThreads / (D / 4)) {
+      const long long off = sm.row[t & 1][r];
+      cp_async16(is_k ? &sm.k[r][4 * (c ^ (r & 7))] : &sm.v[r][4 * c], src + (off < 0 ? 0 : off + c), off >= 0);
     }
     cp_async_commit();
   };
+  if (t_begin < t_end) find_rows(t_begin);
+  __syncthreads();
   if (t_begin < t_end) load_tile(t_begin, true);
   for (int i = tid; i < RB * (D / 4); i += kThreads) {
     const int r = i / (D / 4), c = i - r * (D / 4), tl = r / p.gb, hh = r - tl * p.gb;
@@ -187,6 +198,7 @@ __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_consta
   for (int t = t_begin; t < t_end; ++t) {
     cp_async_wait<1>();  // K of this tile (V may be on its way)
     __syncthreads();
+    if (t + 1 < t_end) find_rows(t + 1);
     float sc[RT][4];
 #pragma unroll
     for (int r = 0; r < RT; ++r)

@@ -908,6 +908,22 @@ __global__ void __launch_bounds__(2 * D) chunk_merge_kernel(const __grid_constan
     const int x = e >= p.tb * p.g ? 1 : 0, row = e - x * p.tb * p.g;
     const int tl = row / p.g, hl = row - tl * p.g;
     auto entry = [&](int j) { return ((rec.c0 + j) * 2 + (j == 0 ? rec.slot : 0)) * 2 + x; };
+    const size_t out_row = static_cast<size_t>(rec.tok0 + x * p.tb + tl) * p.a.Hq + rec.kvh * p.g + hl;
+    uint2* dst = reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.a.out) + out_row * D) + col4;
+    if (np == 2) {
+      // cut once, as nearly always: all loads together
+      const float2 ma = *partial_ml<D>(p, entry(0), row), mb = *partial_ml<D>(p, entry(1), row);
+      const float4 oa = *partial_o<D>(p, entry(0), col4, row), ob = *partial_o<D>(p, entry(1), col4, row);
+      const bool ha = ma.y != 0.f, hb = mb.y != 0.f, poison = ma.y == -1.f || mb.y == -1.f;
+      const float M = fmaxf(ha ? ma.x : -INFINITY, hb ? mb.x : -INFINITY);
+      const float wa = ha && !poison ? exp2f(ma.x - M) : 0.f, wb = hb && !poison ? exp2f(mb.x - M) : 0.f;
+      const float L = fmaf(wa, ma.y, wb * mb.y), inv = L != 0.f ? 1.f / L : 0.f;
+      *dst = L == 0.f ? make_uint2(0u, 0u)
+                      : make_uint2(pack_bf16x2(fmaf(wa, oa.x, wb * ob.x) * inv, fmaf(wa, oa.y, wb * ob.y) * inv),
+                                   pack_bf16x2(fmaf(wa, oa.z, wb * ob.z) * inv, fmaf(wa, oa.w, wb * ob.w) * inv));
+      if (p.a.lse && col4 == 0) p.a.lse[out_row] = L != 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
+      continue;
+    }
     float M = -INFINITY;
     bool poison = false;
 #pragma unroll 4
@@ -930,9 +946,8 @@ __global__ void __launch_bounds__(2 * D) chunk_merge_kernel(const __grid_constan
       acc.w = fmaf(w, o.w, acc.w);
     }
     const float inv = L != 0.f ? 1.f / L : 0.f;
-    const size_t out_row = static_cast<size_t>(rec.tok0 + x * p.tb + tl) * p.a.Hq + rec.kvh * p.g + hl;
-    reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.a.out) + out_row * D)[col4] =
-        make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+    *dst = L == 0.f ? make_uint2(0u, 0u)
+                    : make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
     if (p.a.lse && col4 == 0) p.a.lse[out_row] = L != 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
   }
   pdl_launch_next();
@@ -980,7 +995,9 @@ cudaError_t launch_d(const ChunkArgs& a, int num_sms, EncodeTiledFn encode, cuda
   cudaError_t e = launch_overlapped(chunk_tc_kernel<D>, dim3(static_cast<unsigned>(p.ctas)), dim3(kThreads),
                                     smem_bytes<D>(), stream, 1u, tq, tk, tv, p);
   if (e != cudaSuccess || p.ctas == 1) return e;
-  return launch_overlapped(chunk_merge_kernel<D>, dim3(static_cast<unsigned>(p.ctas - 1), 4u), dim3(2 * D), 0,
+  // units of many rows: 16 blocks to a boundary (two passes over 256 rows)
+  const unsigned y = static_cast<long long>(a.T) * p.g > 32ll * a.Bt ? 16u : 2u;
+  return launch_overlapped(chunk_merge_kernel<D>, dim3(static_cast<unsigned>(p.ctas - 1), y), dim3(2 * D), 0,
                            stream, 1u, p);
 }
 
