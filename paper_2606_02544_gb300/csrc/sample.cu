@@ -34,6 +34,7 @@
 #include <cfloat>
 #include <cmath>
 #include <mutex>
+#include <type_traits>
 
 #include "common.cuh"
 #include "kernels.h"
@@ -48,14 +49,11 @@ constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kBatch = 16;         // elements of a lane in flight
-constexpr int kCoarse = 2048;     // bins of the first pass
-constexpr float kBinsPerUnit = 32.f;
-constexpr int kSampleFrom = 16384;  // vocabularies from here on are sampled
-constexpr int kList = 8192;       // tokens of the list
-constexpr int kRegion = kList / kWarps;  // of a warp
-constexpr int kAim = 2500;        // tokens that a bracket aims at where the sample is too coarse
+constexpr int kBins = 2048;       // bins of the first pass
+constexpr int kLower = 1536;      // of them below the base, over at most kBelow in x / T ...
+constexpr float kBelow = 48.f, kAbove = 48.f;  // ... the others above it, over kAbove
+constexpr int kList = 4096;       // tokens of the list
 constexpr int kFine = 2048;       // bins of the searches
-constexpr int kFirst = 2048;      // elements that place the window of the first pass
 constexpr float kUnit = 274877906944.0f;  // 2^38
 constexpr unsigned kFull = 0xffffffffu;
 
@@ -140,21 +138,18 @@ struct Kept {
 
 struct alignas(16) Smem {
   union {
-    struct {
-      float x[kList];
-      int idx[kList];
-    } list;
+    u64 list[kList];  // ordered pattern, then the lower index first
     u64 mass[kFine];  // searches over the row
   };
-  uint32_t coarse[kCoarse], part[kCoarse];          // sample: counts, weights in 2^-16 of their bin's upper edge
-  uint32_t count[kFine], low[kFine], high[kFine];   // searches: counts, weight units modulo 2^19 and above
+  uint32_t hist[kBins];  // pass 1: counts, or weights in 2^-16 of their bin's middle
+  uint32_t count[kFine];
   u64 seg[kMaxCluster * kWarps];  // weights of the row's segments (rank 0 holds all)
   u64 warp_a[kWarps], warp_b[kWarps], warp_c[kWarps];
   u64 x_max[kMaxCluster];                          // exchanges over the cluster: one slot per CTA
   u64 x_sum[4][kMaxCluster];
   u64 x_out[4];
   u64 found[5];
-  int list_n[kWarps], pick_lo, pick_hi, token;
+  int list_n, pick_lo, pick_hi, token;
 };
 
 // ------------------------------------------------------------- the cluster
@@ -165,9 +160,6 @@ __device__ __forceinline__ uint32_t map_rank(const void* p, int rank) {
 }
 __device__ __forceinline__ void st_rank(void* p, int rank, u64 v) {
   asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_rank(p, rank)), "l"(v) : "memory");
-}
-__device__ __forceinline__ void st_rank(void* p, int rank, uint32_t v) {
-  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_rank(p, rank)), "r"(v) : "memory");
 }
 __device__ __forceinline__ uint32_t ld_rank_u32(const void* p, int rank) {
   uint32_t v;
@@ -206,23 +198,27 @@ struct Row {
   int lead, V;
   int vecs, per, per_warp;  // vectors of the row, of a CTA, of a segment
 
+  // (a NaN counts as -inf)
+  __device__ static __forceinline__ void unpack(const uint4& q, float (&x)[kVec]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int e = 0; e < kVec; ++e)
+      x[e] = fmaxf(sizeof(E) == 4 ? __uint_as_float(w[e])
+                                  : __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16),
+                   -INFINITY);
+  }
+  __device__ __forceinline__ uint4 vector(int v) const { return reinterpret_cast<const uint4*>(base)[v]; }
+  // (elements outside the row count as -inf)
   __device__ __forceinline__ void load(int v, float (&x)[kVec]) const {
     const int i0 = v * kVec - lead;
-    const E* p = base + static_cast<size_t>(v) * kVec;
     if (i0 >= 0 && i0 + kVec <= V) {
-      const uint4 q = *reinterpret_cast<const uint4*>(p);
-      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+      unpack(vector(v), x);
+    } else {
+      const E* p = base + static_cast<size_t>(v) * kVec;
 #pragma unroll
       for (int e = 0; e < kVec; ++e)
-        x[e] = sizeof(E) == 4 ? __uint_as_float(w[e])
-                              : __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
-    } else {
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) x[e] = i0 + e >= 0 && i0 + e < V ? static_cast<float>(p[e]) : -INFINITY;
+        x[e] = i0 + e >= 0 && i0 + e < V ? fmaxf(static_cast<float>(p[e]), -INFINITY) : -INFINITY;
     }
-    // (elements outside the row and NaN count as -inf)
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) x[e] = fmaxf(x[e], -INFINITY);
   }
   __device__ __forceinline__ int seg_begin(int rank, int warp) const {
     return min(min(vecs, rank * per + per), min(vecs, rank * per) + warp * per_warp);
@@ -232,9 +228,18 @@ struct Row {
   __device__ __forceinline__ void batches(int rank, F&& f) const {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int a = seg_begin(rank, warp), b = min(seg_begin(rank, warp + 1), min(vecs, rank * per + per));
+    const int whole = min(b, (V + lead) / kVec);  // vectors with nothing past the row's end
     // (all lanes stay in the loop: what it calls may exchange within the warp)
     for (int v = a + lane; v - lane < b; v += 32 * kUnroll) {
       float x[kUnroll][kVec];
+      const int v0 = v - lane;
+      if (v0 * kVec >= lead && v0 + 32 * kUnroll <= whole) {
+        uint4 q[kUnroll];
+#pragma unroll
+        for (int i = 0; i < kUnroll; ++i) q[i] = vector(v + 32 * i);
+#pragma unroll
+        for (int i = 0; i < kUnroll; ++i) unpack(q[i], x[i]);
+      } else
 #pragma unroll
       for (int i = 0; i < kUnroll; ++i) {
         if (v + 32 * i < b) {
@@ -328,14 +333,11 @@ struct Found {
 };
 
 // Search over keys in [lo, hi], a digit of up to 11 bits per round.
-// visit(f) calls f(key, weight units) for the elements.  kRow: every CTA of
-// the cluster visits its own part of the row, and all get the result; else
-// one CTA searches its list (at most kList elements, each below 2^51 units:
-// their sums are kept as two 32-bit words).
-template <bool kRow, typename Visit>
+// visit(f) calls f(key, weight units) for the elements of this CTA's part of
+// the row; all CTAs of the cluster get the result.
+template <typename Visit>
 __device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 target, uint32_t lo, uint32_t hi,
                                         Visit&& visit) {
-  if (!kRow) CL = 1;
   Found f{0u, 0, 0, 0, true};
   for (;;) {
     const uint32_t span = hi - lo;
@@ -344,25 +346,14 @@ __device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 tar
     sync_all(CL);
     for (int i = threadIdx.x; i < kFine; i += kThreads) {
       sm.count[i] = 0;
-      if (kRow) {
-        sm.mass[i] = 0;
-      } else {
-        sm.low[i] = 0;
-        sm.high[i] = 0;
-      }
+      sm.mass[i] = 0;
     }
     sync_all(CL);
     visit([&](uint32_t key, u64 q) {
       if (key < lo || key > hi) return;
       const uint32_t bin = (key - lo) >> shift;
       atomicAdd(&sm.count[bin], 1u);
-      if (q == 0) return;
-      if (kRow) {
-        atomicAdd(&sm.mass[bin], q);
-      } else {
-        atomicAdd(&sm.low[bin], static_cast<uint32_t>(q) & 0x7ffffu);
-        atomicAdd(&sm.high[bin], static_cast<uint32_t>(q >> 19));
-      }
+      if (q) atomicAdd(&sm.mass[bin], q);
     });
     sync_all(CL);
     // thread t: bins 4 t .. 4 t + 3 from the top
@@ -371,14 +362,9 @@ __device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 tar
     for (int e = 0; e < 4; ++e) {
       const int bin = kFine - 1 - (4 * static_cast<int>(threadIdx.x) + e);
       c[e] = q[e] = 0;
-      if (!kRow) {
-        c[e] = sm.count[bin];
-        q[e] = (static_cast<u64>(sm.high[bin]) << 19) + sm.low[bin];
-      } else {
-        for (int r = 0; r < CL; ++r) {
-          c[e] += ld_rank_u32(&sm.count[bin], r);
-          q[e] += ld_rank_u64(&sm.mass[bin], r);
-        }
+      for (int r = 0; r < CL; ++r) {
+        c[e] += ld_rank_u32(&sm.count[bin], r);
+        q[e] += ld_rank_u64(&sm.mass[bin], r);
       }
       sc += c[e];
       sq += q[e];
@@ -420,6 +406,46 @@ __device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 tar
   }
 }
 
+// Sorts n keys (a power of two, at least 32), the highest first: a bitonic
+// network whose strides below 32 are taken in registers, 32 keys a warp.
+__device__ __noinline__ void sort_keys(u64* key, int n) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  auto in_warp = [&](u64 x, int i, int size, int stride) {
+    const u64 y = __shfl_xor_sync(kFull, x, stride);
+    return ((i & stride) == 0) == ((i & size) == 0) ? max(x, y) : min(x, y);
+  };
+  __syncthreads();
+  for (int b = 32 * warp; b < n; b += kThreads) {
+    u64 x = key[b + lane];
+#pragma unroll
+    for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+      for (int stride = size / 2; stride > 0; stride >>= 1) x = in_warp(x, b + lane, size, stride);
+    key[b + lane] = x;
+  }
+  for (int size = 64; size <= n; size <<= 1) {
+    for (int stride = size / 2; stride >= 32; stride >>= 1) {
+      __syncthreads();
+      for (int i = threadIdx.x; i < n / 2; i += kThreads) {
+        const int lo = 2 * i - (i & (stride - 1)), hi = lo + stride;
+        const u64 x = key[lo], y = key[hi];
+        if ((x < y) == ((lo & size) == 0)) {
+          key[lo] = y;
+          key[hi] = x;
+        }
+      }
+    }
+    __syncthreads();
+    for (int b = 32 * warp; b < n; b += kThreads) {
+      u64 x = key[b + lane];
+#pragma unroll
+      for (int stride = 16; stride > 0; stride >>= 1) x = in_warp(x, b + lane, size, stride);
+      key[b + lane] = x;
+    }
+  }
+  __syncthreads();
+}
+
 template <typename E>
 __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ SampleArgs a, const int CL) {
   extern __shared__ uint4 smem_raw[];
@@ -453,69 +479,100 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   const bool cut = !bad && (k > 0 || p < 1.f);
   const float inv = 1.0f / T;
 
-  // ---- pass 1: the maximum, and of a sample counts and weights over bins of x / T
-  // sampled: the first vector of every other batch, about an eighth; fs: what
-  // one sampled vector stands for
-  const bool sampled = a.V >= kSampleFrom;
-  float fs = 1.f;
-  if (sampled) {
-    int n = 0;
-    for (int i = lane; i < CL * kWarps; i += 32) {
-      const int rk = i / kWarps, w = i - rk * kWarps;
-      const int len = min(row.seg_begin(rk, w + 1), min(row.vecs, rk * row.per + row.per)) - row.seg_begin(rk, w);
-      const int pairs = len / (64 * kUnroll), rest = len - pairs * 64 * kUnroll;
-      n += 32 * pairs + min(max(rest, 0), 32);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(kFull, n, o);
-    fs = static_cast<float>(row.vecs) / static_cast<float>(max(n, 1));
-  }
-  const float scale = inv * kBinsPerUnit;
-  float base = 0.f;
+  // ---- pass 1: the maximum, and counts or weights over bins of x / T.  The
+  // bins are laid by a vector a thread from all over the row: the base is their
+  // maximum, the lower bins end three times as far below it as they lie on
+  // average (a flat row has narrower bins), the upper ones reach far up (the
+  // few tokens above a sample's maximum, and a single one far above all).
+  const bool by_count = k > 0;
+  float base = 0.f, below = kBelow;
   if (cut) {
-    for (int i = tid; i < kCoarse; i += kThreads) sm.coarse[i] = sm.part[i] = 0;
-    // the window lies around the maximum of the row's first elements
-    float f = -INFINITY;
-    for (int i = tid; i < min(a.V, kFirst); i += kThreads)
-      f = fmaxf(f, static_cast<float>(row.base[row.lead + i]));
+    for (int i = tid; i < kBins; i += kThreads) sm.hist[i] = 0;
+    float x[kVec], f = -INFINITY, d = 0.f;
+    row.load(static_cast<int>(static_cast<long long>(tid) * row.vecs / kThreads), x);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) f = fmaxf(f, x[e]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) f = fmaxf(f, __shfl_xor_sync(kFull, f, o));
     if (lane == 0) sm.warp_a[warp] = __float_as_uint(f);
     __syncthreads();
-    f = -INFINITY;
-    for (int w = 0; w < kWarps; ++w) f = fmaxf(f, __uint_as_float(static_cast<uint32_t>(sm.warp_a[w])));
+    f = __uint_as_float(static_cast<uint32_t>(sm.warp_a[lane & (kWarps - 1)]));
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) f = fmaxf(f, __shfl_xor_sync(kFull, f, o));
     base = isinf(f) ? 0.f : f;
+    // (what lies below every window does not count)
+    int n = 0;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      const float z = (base - x[e]) * inv;
+      if (z >= 0.f && z < kBelow) {
+        d += z;
+        ++n;
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      d += __shfl_xor_sync(kFull, d, o);
+      n += __shfl_xor_sync(kFull, n, o);
+    }
+    if (lane == 0) sm.warp_b[warp] = static_cast<u64>(__float_as_uint(d)) << 32 | static_cast<uint32_t>(n);
     __syncthreads();
+    const u64 dn = sm.warp_b[lane & (kWarps - 1)];
+    d = __uint_as_float(static_cast<uint32_t>(dn >> 32));
+    n = static_cast<int>(static_cast<uint32_t>(dn));
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) {
+      d += __shfl_xor_sync(kFull, d, o);
+      n += __shfl_xor_sync(kFull, n, o);
+    }
+    // (few tokens say nothing: most are masked)
+    if (n >= 32) below = fminf(fmaxf(3.f * d / static_cast<float>(n), 1e-3f), kBelow);
   }
-  auto count_in = [&](float x) {
-    const float y = fminf(fmaxf(fmaf(x - base, scale, 0.5f * kCoarse), 0.f), kCoarse - 0.01f);
-    const float b = floorf(y), d = (b + 1.f - y) * (1.f / kBinsPerUnit);  // e^-d = 1 - d + d^2 / 2 to 5e-6
-    const int bin = static_cast<int>(b);
-    atomicAdd(&sm.coarse[bin], 1u);
-    atomicAdd(&sm.part[bin], static_cast<uint32_t>(fmaf(d, fmaf(d, 0.5f, -1.f), 1.f) * 65536.f));
-  };
+  // bins per unit of x, their width in x / T
+  const float scale_lo = inv * (kLower / below), scale_hi = inv * ((kBins - kLower) / kAbove);
+  const float width_lo = below / kLower, width_hi = kAbove / (kBins - kLower);
   float mx = -INFINITY;
   {
-    int nb = 0;
-    row.batches(rank, [&](float (&x)[kUnroll][kVec], int) {
-#pragma unroll
-      for (int i = 0; i < kUnroll; ++i)
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) mx = fmaxf(mx, x[i][e]);
-      if (cut) {
-        if (!sampled) {
-#pragma unroll
-          for (int i = 0; i < kUnroll; ++i)
-#pragma unroll
-            for (int e = 0; e < kVec; ++e)
-              if (x[i][e] != -INFINITY) count_in(x[i][e]);
-        } else if ((nb++ & 1) == 0) {
-#pragma unroll
-          for (int e = 0; e < kVec; ++e)
-            if (x[0][e] != -INFINITY) count_in(x[0][e]);
-        }
+    // in units of the whole window, so that one instruction clamps: bin b holds
+    // what rounds to b, and a token's weight is taken against its middle
+    const float s_lo = scale_lo / (kBins - 1), s_hi = scale_hi / (kBins - 1);
+    const float c_lo = width_lo * 1.4426950408889634f, c_hi = width_hi * 1.4426950408889634f;
+    // the last bits of a sum with 2^23 are an integer (a conversion is four
+    // times as dear): the bin's address is those bits, shifted, and a constant
+    const uint32_t at = smem_u32(sm.hist) - (0x4b000000u << 2);
+    auto count_in = [&](float x, bool count) {
+      const float t = x - base;  // (first: base and x may be large against a bin)
+      const bool upper = t >= 0.f;
+      const float y = __saturatef(fmaf(t, upper ? s_hi : s_lo, static_cast<float>(kLower) / (kBins - 1)));
+      const float f = fmaf(y, static_cast<float>(kBins - 1), 8388608.f);
+      uint32_t q = 1;
+      if (!count) {
+        const float r = fmaf(y, static_cast<float>(kBins - 1), 8388608.f - f);
+        q = __float_as_uint(fmaf(fast_exp2(r * (upper ? c_hi : c_lo)), 65536.f, 8388608.f)) & 0x3ffffu;
       }
-    });
+      // (what lies below the window, as masked tokens do, is left out)
+      asm volatile("{\n\t.reg .pred p;\n\tsetp.gt.f32 p, %2, 0f00000000;\n\t@p red.shared.add.u32 [%0], %1;\n\t}" ::"r"(
+                       at + (__float_as_uint(f) << 2)),
+                   "r"(q), "f"(y)
+                   : "memory");
+    };
+    auto one = [&](auto kind) {
+      row.batches(rank, [&](float (&x)[kUnroll][kVec], int) {
+#pragma unroll
+        for (int i = 0; i < kUnroll; ++i)
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            mx = fmaxf(mx, x[i][e]);
+            if (decltype(kind)::value) count_in(x[i][e], decltype(kind)::value == 1);
+          }
+      });
+    };
+    if (!cut)
+      one(std::integral_constant<int, 0>{});
+    else if (by_count)
+      one(std::integral_constant<int, 1>{});
+    else
+      one(std::integral_constant<int, 2>{});
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, o));
@@ -565,469 +622,240 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   };
   const uint32_t key_max = ordered(m);
 
-  // ---- the bracket of kappa, from the sample.  Thread t holds 4 bins from
-  // the top; c and w: what the sample says of the whole row.
+  // ---- the bracket of kappa.  Thread t holds 4 bins from the top.
   struct Bracket {
     float x0, x1;  // tokens x0 <= x < x1 are to be listed
     bool all;      // x1 lies above all tokens
-    bool listing;  // false: too many, their weight is taken to narrow the bracket
     bool ok;
   };
-  float hc[4], hw[4];
-  float hz = 0.f;  // weight of the whole row
-  if (cut) {
-    uint4 cn = make_uint4(0, 0, 0, 0), pn = cn;
-    const int j4 = kCoarse - 4 - 4 * tid;  // bins j4 .. j4 + 3; entry e is bin j4 + 3 - e
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
+  auto edge = [&](int bin) {
+    const float y = static_cast<float>(bin - kLower) - 0.5f;  // (its lower edge)
+    return base + y / (y > 0.f ? scale_hi : scale_lo);
+  };
+  auto estimate = [&] {
+    uint4 t = make_uint4(0, 0, 0, 0);
+    const int j4 = kBins - 4 - 4 * tid;  // bins j4 .. j4 + 3; entry e is bin j4 + 3 - e
+    {
       uint4 x[kMaxCluster];
 #pragma unroll
-      for (int q = 0; q < kMaxCluster; ++q)
-        x[q] = q < CL ? ld_rank_v4(h == 0 ? &sm.coarse[j4] : &sm.part[j4], q) : make_uint4(0, 0, 0, 0);
-      uint4& t = h == 0 ? cn : pn;
+      for (int q = 0; q < kMaxCluster; ++q) x[q] = q < CL ? ld_rank_v4(&sm.hist[j4], q) : make_uint4(0, 0, 0, 0);
 #pragma unroll
       for (int q = 0; q < kMaxCluster; ++q) t.x += x[q].x, t.y += x[q].y, t.z += x[q].z, t.w += x[q].w;
     }
-    const uint32_t cs[4] = {cn.w, cn.z, cn.y, cn.x}, ps[4] = {pn.w, pn.z, pn.y, pn.x};
+    const uint32_t h[4] = {t.w, t.z, t.y, t.x};
+    u64 c[4], w[4], sc = 0, sw = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      // weight of the bin's upper edge (at most that of its tokens times e^(1/32))
-      const float top = (static_cast<float>(j4 + 4 - e) - 0.5f * kCoarse) / kBinsPerUnit - (m - base) * inv;
-      hc[e] = static_cast<float>(cs[e]);
-      hw[e] = cs[e] ? static_cast<float>(ps[e]) * (1.f / 65536.f) * expf(fminf(top, 1.f)) : 0.f;
+      // a bin's weight is its sum times that of its middle (kLower's has two halves, and its
+      // middle is the base), its count at most the sum times e^(width / 2)
+      const int up = j4 + 3 - e - kLower;
+      const float mid = static_cast<float>(up) * (up > 0 ? width_hi : width_lo) - (m - base) * inv;
+      const float share = static_cast<float>(h[e]) * (1.f / 65536.f);
+      c[e] = by_count ? h[e] : static_cast<u64>(share * 1.1f);
+      w[e] = by_count || h[e] == 0 ? 0 : units(share * expf(fminf(mid, 1.f)));
+      sc += c[e];
+      sw += w[e];
     }
-  }
-  auto edge = [&](int bin) { return base + (static_cast<float>(bin) - 0.5f * kCoarse) / scale; };
-  const bool window_ok = scale < 1e30f && fmaf(m - base, scale, 0.5f * kCoarse) < kCoarse - 1;
-  auto estimate = [&](bool by_count) {
-    float sw = 0.f, sv = 0.f;
-    u64 sc = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      sc += static_cast<u64>(hc[e]);
-      sw += hw[e];
-      sv += hc[e] > 0.f ? hw[e] * hw[e] / hc[e] : 0.f;
-    }
-    u64 pc, pq, pv, none;
-    block_scan(sm, sc, units(sw), pc, pq);
-    __syncthreads();
+    u64 pc, pw;
+    block_scan(sm, sc, sw, pc, pw);
     if (tid == kThreads - 1) {
-      sm.found[3] = pq + units(sw);
+      sm.found[3] = pw + sw;
+      sm.found[0] = 0;
       sm.pick_lo = sm.pick_hi = -1;
     }
-    block_scan(sm, units(sv), 0, pv, none);
-    if (tid == kThreads - 1) sm.found[4] = pv + units(sv);
     __syncthreads();
-    const float all_w = __ull2float_rn(sm.found[3]) / kUnit, all_v = __ull2float_rn(sm.found[4]) / kUnit;
-    hz = all_w * fs;
-    // `lo`: the last bin by which the target is surely reached, `hi`: the
-    // first where it may be (4 standard deviations of a count, 3 of a weight:
-    // a miss costs another way through the row, not the result)
-    const float pp = fmaxf(p, 0.f), noise = fs > 1.f ? fs * sqrtf(1.f - 1.f / fs) : 0.f;
-    float rc = static_cast<float>(pc), rw = __ull2float_rn(pq) / kUnit, rv = __ull2float_rn(pv) / kUnit;
-    float reach[4];
+    // kappa's bin is the first by which the target is reached; a weight is
+    // known to 2^-16.8, and the bins that this leaves open are listed too
+    // (a miss costs the searches over the row, not the result)
+    const u64 all_w = sm.found[3], slack = by_count ? 0 : all_w >> 16;
+    const u64 goal = by_count ? static_cast<u64>(k) : max(1ull, part_ceil(fmaxf(p, 0.f), all_w));
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      rc += hc[e];
-      rw += hw[e];
-      rv += hc[e] > 0.f ? hw[e] * hw[e] / hc[e] : 0.f;
-      const int bin = kCoarse - 1 - (4 * tid + e);
-      float d, sd;
-      if (by_count) {
-        d = rc * fs - static_cast<float>(k);
-        sd = 4.f * noise * sqrtf(rc);
-      } else {
-        d = (rw - pp * all_w) * fs;
-        sd = 3.f * noise * sqrtf(fmaxf((1.f - pp) * (1.f - pp) * rv + pp * pp * (all_v - rv), 0.f)) + 1e-4f * hz;
+      const u64 before = by_count ? pc : pw, after = by_count ? pc + c[e] : pw + w[e];
+      if (before < goal + slack && after >= goal + slack) {
+        sm.pick_lo = j4 + 3 - e;
+        sm.found[0] = pc + c[e];
       }
-      reach[e] = rc * fs + 4.f * noise * sqrtf(rc);
-      if (d + sd >= 0.f) atomicMax(&sm.pick_hi, bin);
-      if (d - sd >= 0.f) atomicMax(&sm.pick_lo, bin);
+      if (before + slack < goal && after + slack >= goal) sm.pick_hi = j4 + 3 - e;
+      pc += c[e];
+      pw += w[e];
     }
     __syncthreads();
+    // (the target lies so near the whole weight that only the lowest token is certain to reach it)
     const int lo = sm.pick_lo, hi = sm.pick_hi;
-    // tokens up to the bottom of the bracket: a list of all of them, where it fits
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-    {
-      const int bin = kCoarse - 1 - (4 * tid + e);
-      if (bin == max(lo, 0)) sm.found[0] = static_cast<u64>(reach[e]);
-      if (bin == max(hi, 0)) sm.found[1] = static_cast<u64>(fmaxf(reach[e] - hc[e] * fs, 0.f));
-    }
-    __syncthreads();
     Bracket b;
-    b.all = lo > 0 && sm.found[0] + 64 <= (by_count ? kList / 2 : kList / 8);
+    // tokens down to the bottom of the bracket: a list of all of them, where it fits
+    b.all = hi >= 0 && lo >= 0 && sm.found[0] <= (by_count ? kList : kThreads);
     // (never -inf: what counts as -inf lies below every bracket)
-    b.x0 = lo > 0 ? edge(lo) : -FLT_MAX;
-    b.x1 = b.all || hi < 0 ? INFINITY : edge(hi + 1);
-    b.listing = by_count || sm.found[0] - min(sm.found[0], sm.found[1]) <= 2 * kAim;
-    b.ok = window_ok && hi > 0 && b.x0 < b.x1;
-    __syncthreads();
+    b.x0 = lo >= 0 ? edge(lo) : -FLT_MAX;
+    b.x1 = b.all || hi == kBins - 1 ? INFINITY : edge(hi + 1);
+    b.ok = hi >= 0 && (lo >= 0 || !by_count) && b.x0 < b.x1 && scale_lo < 1e30f && m < INFINITY;
     return b;
   };
-  // A bracket of about kAim tokens inside b, whose weight (or count) is
-  // `whole`: the target lies `part` below its top.
-  auto narrow = [&](const Bracket& b, bool by_count, float part, float whole) {
-    float in[4], n[4], si = 0.f, sn = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int bin = kCoarse - 1 - (4 * tid + e);
-      const bool inside = edge(bin) >= b.x0 && edge(bin) < b.x1;
-      n[e] = inside ? hc[e] : 0.f;
-      in[e] = inside ? (by_count ? hc[e] : hw[e]) : 0.f;
-      si += in[e];
-      sn += n[e];
-    }
-    u64 pi, pn;
-    block_scan(sm, units(si), static_cast<u64>(sn), pi, pn);
-    __syncthreads();
-    if (tid == kThreads - 1) {
-      sm.found[3] = pi + units(si);
-      sm.pick_lo = kCoarse;
-      sm.pick_hi = -1;
-      sm.found[0] = 0;
-    }
-    __syncthreads();
-    const float goal = part / whole * __ull2float_rn(sm.found[3]);
-    float r = __ull2float_rn(pi), c = static_cast<float>(pn);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (r < goal && r + in[e] * kUnit >= goal) sm.found[0] = static_cast<u64>(c + 0.5f * n[e]) + 1;
-      r += in[e] * kUnit;
-      c += n[e];
-    }
-    __syncthreads();
-    // half of kAim tokens to either side
-    const float mid = static_cast<float>(sm.found[0]), half = 0.5f * kAim / fs;
-    c = static_cast<float>(pn);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int bin = kCoarse - 1 - (4 * tid + e);
-      if (n[e] > 0.f && c + n[e] >= mid - half && c <= mid + half) {
-        atomicMax(&sm.pick_hi, bin);
-        atomicMin(&sm.pick_lo, bin);
-      }
-      c += n[e];
-    }
-    __syncthreads();
-    Bracket t;
-    t.x0 = fmaxf(b.x0, edge(sm.pick_lo));
-    t.x1 = fminf(b.x1, edge(sm.pick_hi + 1));
-    t.all = false;
-    t.listing = true;
-    t.ok = sm.found[0] > 0 && t.x0 < t.x1;
-    __syncthreads();
-    return t;
-  };
 
-  // ---- pass 2: adds up the tokens x1 <= x < top (top: what is counted
-  // already) and lists those in [x0, x1).  v: count and weight above, count
-  // and weight of the list; `need_all`: v[1] is the row's whole weight and
-  // what lies above is left in the segments alone.
+  auto key_x = [](u64 key) { return from_ordered(static_cast<uint32_t>(key >> 32)); };
+
+  // ---- pass 2: adds up the tokens x1 <= x and lists those in [x0, x1).
+  // v: count above (and, above 2^32, of the list), weight above, weight of the
+  // list, weight of the row (the last three only where they are used).
   const float c_exp = inv * 1.4426950408889634f;
-  u64 above_n = 0, above_q = 0;
-  bool fits = false;  // the list holds all that it should
-  auto pass = [&](const Bracket& b, float top, bool need_all, u64 (&v)[4]) {
-    // fp32 weights: 2^((x - m) c) on tokens that are certain to be kept, or to
-    // be part of a total (the list's are taken again with all their digits).
-    // Straight code for every token, no branches but for the list's stores.
-    LongSum fq, fa, fl;
-    uint32_t n = 0, nl = 0;
+  auto pass = [&](const Bracket& b, u64 (&v)[4]) {
+    if (tid == 0) sm.list_n = 0;
+    __syncthreads();
     const float x0 = b.x0, x1 = b.x1;
-    const bool listing = b.listing;
-    int at = 0;  // tokens of the warp's region of the list
-    row.batches(rank, [&](float (&x)[kUnroll][kVec], int i0) {
-      float s = 0.f, sa = 0.f, sl = 0.f;
+    auto list = [&](float x, int idx) {
+      const int to = atomicAdd(&sm.list_n, 1);
+      if (to < kList) sm.list[to] = static_cast<u64>(ordered(x)) << 32 | ~static_cast<uint32_t>(idx);
+    };
+    // fp32 weights: 2^((x - m) c) on tokens that are certain to be kept, or to
+    // be part of a total (the list's are taken with all their digits).
+    LongSum fq, fa;
+    uint32_t n = 0;
+    if (b.all && by_count) {
+      row.batches(rank, [&](float (&x)[kUnroll][kVec], int i0) {
 #pragma unroll
-      for (int i = 0; i < kUnroll; ++i)
+        for (int i = 0; i < kUnroll; ++i)
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const float xe = x[i][e];
-          const float w = fast_exp2((xe - m) * c_exp);
-          const bool above = xe >= x1 && xe < top, in = xe >= x0 && xe < x1;
-          sa += w;
-          s += above ? w : 0.f;
-          sl += in ? w : 0.f;
-          n += above ? 1u : 0u;
-          nl += in ? 1u : 0u;
-          if (listing) {
-            const unsigned who = __ballot_sync(kFull, in);
-            if (who) {
-              const int to = at + __popc(who & ((1u << lane) - 1u));
-              if (in && to < kRegion) {
-                sm.list.x[warp * kRegion + to] = xe;
-                sm.list.idx[warp * kRegion + to] = Row<E>::index(i0, i, e);
-              }
-              at += __popc(who);
+          for (int e = 0; e < kVec; ++e)
+            if (x[i][e] >= x0) list(x[i][e], Row<E>::index(i0, i, e));
+      });
+    } else {
+      row.batches(rank, [&](float (&x)[kUnroll][kVec], int i0) {
+        float s = 0.f, sa = 0.f;
+#pragma unroll
+        for (int i = 0; i < kUnroll; ++i) {
+          bool some = false;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            const float xe = x[i][e], w = fast_exp2((xe - m) * c_exp);
+            sa += w;
+            if (xe >= x1) {
+              s += w;
+              ++n;
             }
+            some |= xe >= x0 && xe < x1;
+          }
+          if (some) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+              if (x[i][e] >= x0 && x[i][e] < x1) list(x[i][e], Row<E>::index(i0, i, e));
           }
         }
-      fq.add(s);
-      fl.add(sl);
-      fa.add(sa);
-    });
-    const u64 q = fq.total(), qa = fa.total(), ql = fl.total();
-    if (lane == 0) sm.list_n[warp] = at;
+        fq.add(s);
+        fa.add(sa);
+      });
+    }
+    const u64 q = fq.total();
     const u64 seg = warp_sum(q);
-    if (lane == 0) {
-      if (top == INFINITY)
-        st_rank(&sm.seg[rank * kWarps + warp], 0, seg);
-      else  // (only this warp writes its entry; rank 0 reads it after the exchange)
-        st_rank(&sm.seg[rank * kWarps + warp], 0, seg + ld_rank_u64(&sm.seg[rank * kWarps + warp], 0));
-    }
-    // tokens listed, and (above 2^32) regions that overflowed
-    v[0] = n;
+    if (lane == 0) st_rank(&sm.seg[rank * kWarps + warp], 0, seg);
+    __syncthreads();
+    u64 ql = 0;
+    const int own = sm.list_n;
+    if (!by_count)
+      for (int i = tid; i < min(own, kList); i += kThreads) ql += units(wt.w(key_x(sm.list[i])));
+    v[0] = n + (tid == 0 ? static_cast<u64>(own) << 32 : 0);
     v[1] = q;
-    v[2] = (lane == 0 && at > kRegion ? 1ull << 32 : 0ull) + nl;
-    v[3] = need_all ? qa : ql;
+    v[2] = ql;
+    v[3] = fa.total();
     cluster_sum(sm, CL, rank, v);
-    if (need_all) {  // the list's weight, in an exchange of its own
-      u64 t[4] = {ql, 0, 0, 0};
-      cluster_sum(sm, CL, rank, t);
-      set_mass = v[3];
-      v[3] = t[0];
-    }
-    fits = b.listing && v[2] >> 32 == 0 && v[2] <= kList;
-    v[2] &= 0xffffffffull;
   };
 
-  // The bracket of one limit, exact sums around it, and the search of the
-  // list.  False: not settled (nothing changed).
-  auto by_list = [&](bool by_count, bool& both) {
-    Bracket b = estimate(by_count);
+  // The bracket of a limit, exact sums around it, and the search of the list.
+  // False: not settled (nothing changed).
+  auto by_list = [&](bool& both) {
+    const Bracket b = estimate();
     if (!b.ok) return false;
-    both = by_count && p < 1.f && b.all;
-    float top = INFINITY;
     u64 v[4];
-    above_n = above_q = 0;
-    for (int round = 0;; ++round) {
-      pass(b, top, !by_count && round == 0, v);
-      above_n += v[0];
-      above_q += v[1];
-      const u64 target = by_count ? static_cast<u64>(k) : max(1ull, part_ceil(fmaxf(p, 0.f), set_mass));
-      const u64 above = by_count ? above_n : above_q, upto = above + (by_count ? v[2] : v[3]);
-      // kappa is in the list: less than the target lies above it, and no less with it
-      const bool here = above < target && upto >= target;
-      if (here && fits) break;
-      if (round == 4) return false;
-      both = false;
-      // the part of the row that holds it, and its exact weight
-      Bracket c = b;
-      if (here) {
-        top = b.x1;
-        b = narrow(c, by_count, __ull2float_rn(target - above), __ull2float_rn(upto - above));
-      } else {
-        top = INFINITY;
-        above_n = above_q = 0;
-        if (above >= target) {
-          c.x0 = b.x1;
-          c.x1 = INFINITY;
-          b = narrow(c, by_count, __ull2float_rn(target), __ull2float_rn(above));
-        } else {
-          // (the count of all tokens is not known: the histogram's will do)
-          const float rest = by_count ? 0.f : __ull2float_rn(set_mass - min(set_mass, upto));
-          c.x0 = -FLT_MAX;
-          c.x1 = b.x0;
-          if (!(rest > 0.f)) return false;
-          b = narrow(c, by_count, __ull2float_rn(target - upto), rest);
-        }
-      }
-      if (!b.ok) return false;
-    }
-    // this CTA's list without gaps
+    pass(b, v);
+    const u64 above_n = v[0] & 0xffffffffull, above_q = v[1];
+    const int total = static_cast<int>(v[0] >> 32);
+    if (!by_count) set_mass = v[3];
     {
-      float lx[kWarps];
-      int li[kWarps];
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w)
-        if (tid < sm.list_n[w]) {
-          lx[w] = sm.list.x[w * kRegion + tid];
-          li[w] = sm.list.idx[w * kRegion + tid];
-        }
-      __syncthreads();
-      int to = 0;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const int n = sm.list_n[w];
-        if (tid < n) {
-          sm.list.x[to + tid] = lx[w];
-          sm.list.idx[to + tid] = li[w];
-        }
-        to += n;
-      }
+      // kappa is in the list: less than the target lies above it, and no less with it
+      const u64 target = by_count ? static_cast<u64>(k) : max(1ull, part_ceil(fmaxf(p, 0.f), set_mass));
+      const u64 above = by_count ? above_n : above_q, upto = above + (by_count ? total : v[2]);
+      if (total > kList || above >= target || upto < target) return false;
     }
-    __syncthreads();
+    both = by_count && p < 1.f && b.all;
+    // min_p cuts below all that lies above the list: the list settles it
+    // (not where top_p is still to look at the whole set)
+    const bool min_p_too = mp > 0.f && (b.all || wt.w(b.x1) >= mp) && (!by_count || p >= 1.f || both);
     // all lists go to rank 0, in the order of the CTAs
     if (CL > 1) {
-      int own = 0;
-      for (int w = 0; w < kWarps; ++w) own += sm.list_n[w];
+      const int own = sm.list_n;
       if (tid < CL) st_rank(&sm.x_sum[0][rank], tid, static_cast<u64>(own));
       sync_all(CL);
       int at = 0;
       for (int c = 0; c < rank; ++c) at += static_cast<int>(sm.x_sum[0][c]);
       if (rank > 0)
         for (int i = tid; i < own; i += kThreads) {
-          st_rank(&sm.list.x[at + i], 0, __float_as_uint(sm.list.x[i]));
-          st_rank(&sm.list.idx[at + i], 0, static_cast<uint32_t>(sm.list.idx[i]));
+          st_rank(&sm.list[at + i], 0, sm.list[i]);
         }
       sync_all(CL);
     }
     if (rank == 0) {
-      const int total = static_cast<int>(v[2]);
-      const uint32_t key_lo = max(kKeyMin, ordered(b.x0));
-      const uint32_t key_hi = b.x1 < m ? ordered(b.x1) : key_max;
-      auto visit_list = [&](auto&& f) {
-        for (int i = tid; i < total; i += kThreads) {
-          const uint32_t key = ordered(sm.list.x[i]);
-          if (kept.in_prefix(key, sm.list.idx[i])) f(key, units(wt.w(sm.list.x[i])));
-        }
-      };
-      u64 set = set_mass;
-      if (total <= kThreads) {
-        // a thread per token: its rank and the weight before it, by comparing
-        // it with all others (the histograms' memory holds keys and weights)
-        u64* sk = reinterpret_cast<u64*>(sm.coarse);  // key, then lower index first
-        u64* sq = reinterpret_cast<u64*>(sm.part);
-        u64 mine = 0, own = 0;
-        if (tid < total) {
-          mine = static_cast<u64>(ordered(sm.list.x[tid])) << 32 | (0xffffffffu - static_cast<uint32_t>(sm.list.idx[tid]));
-          own = units(wt.w(sm.list.x[tid]));
-          sk[tid] = mine;
-          sq[tid] = own;
-        }
-        __syncthreads();
-        u64 before = 0;
-        int place = 0;
-        if (tid < total) {
-#pragma unroll 8
-          for (int j = 0; j < total; ++j) {
-            const bool ahead = sk[j] > mine;
-            place += ahead ? 1 : 0;
-            before += ahead ? sq[j] : 0;
-          }
-        }
-        const int limit = by_count ? static_cast<int>(min(static_cast<u64>(k) - above_n, static_cast<u64>(total))) : total;
-        u64 none, s;
-        block_scan(sm, 0, tid < total && place < limit ? own : 0, none, s);
-        __syncthreads();
-        if (tid == kThreads - 1) sm.found[4] = s + (tid < total && place < limit ? own : 0);
-        __syncthreads();
-        if (by_count) set = above_q + sm.found[4];
-        u64 goal = ~0ull;
-        if (!by_count || both) {
-          goal = max(1ull, part_ceil(fmaxf(p, 0.f), set));
-          goal = goal > above_q ? goal - above_q : 1;
-        }
-        // the last kept token: the last within the limit that begins before the goal
-        const bool in = tid < total && place < limit && before < goal;
-        if (tid == 0) sm.pick_lo = -1;
-        __syncthreads();
-        if (in) atomicMax(&sm.pick_lo, place);
-        __syncthreads();
-        if (in && place == sm.pick_lo) {
-          sm.found[0] = mine;
-          sm.pick_hi = place;
-        }
-        __syncthreads();
-        kept.kappa = static_cast<uint32_t>(sm.found[0] >> 32);
-        kept.last = static_cast<int>(0xffffffffu - static_cast<uint32_t>(sm.found[0]));
-        if (in) {
-          const int v2 = (sm.list.idx[tid] + row.lead) / kVec, c = v2 / row.per, w = (v2 - c * row.per) / row.per_warp;
-          atomicAdd(&sm.seg[c * kWarps + w], own);
-        }
-        if (tid < CL) {
-          st_rank(&sm.x_out[0], tid, sm.found[0] >> 32 << 32 | static_cast<uint32_t>(kept.last));
-          st_rank(&sm.x_out[1], tid, set);
-          st_rank(&sm.x_out[2], tid, above_n + sm.pick_hi + 1);
-        }
-      } else {
-      // keep `quota` of the tokens at kappa: the lowest indices
-      auto take = [&](const Found& f, u64 quota) {
-        kept.move_to(f.key);
-        if (quota >= f.at_count) return;
-        const uint32_t kappa = f.key;
-        auto visit_ties = [&](auto&& g) {
-          for (int i = tid; i < total; i += kThreads)
-            if (ordered(sm.list.x[i]) == kappa && sm.list.idx[i] <= kept.last)
-              g(0xffffffffu - static_cast<uint32_t>(sm.list.idx[i]), 0ull);
-        };
-        const Found t =
-            search<false>(sm, 1, true, quota, 0xffffffffu - static_cast<uint32_t>(a.V), 0xffffffffu, visit_ties);
-        kept.last = static_cast<int>(0xffffffffu - t.key);
-      };
-      bool p_left = !by_count;
-      if (by_count) {
-        const u64 rest = static_cast<u64>(k) - above_n;
-        const Found f = search<false>(sm, 1, true, rest, key_lo, key_hi, visit_list);
-        if (f.ok) take(f, rest - f.above_count);
-        p_left = both;
-        // weight of the kept part of the list
-        u64 s = 0, none, before;
-        visit_list([&](uint32_t, u64 q2) { s += q2; });
-        block_scan(sm, 0, s, none, before);
-        __syncthreads();
-        if (tid == kThreads - 1) sm.found[4] = before + s;
-        __syncthreads();
-        set = above_q + sm.found[4];
-        __syncthreads();
+      // the list in order, a run of it to each thread
+      int n2 = 32;
+      while (n2 < total) n2 <<= 1;
+      for (int i = total + tid; i < n2; i += kThreads) sm.list[i] = 0;
+      sort_keys(sm.list, n2);
+      const int each = max(1, n2 / kThreads), i0 = tid * each, i1 = min(total, i0 + each);
+      const int limit = by_count ? min(static_cast<int>(static_cast<u64>(k) - above_n), total) : total;
+      u64 own = 0, in_limit = 0, before, rest;
+      for (int i = i0; i < i1; ++i) {
+        const u64 q = units(wt.w(key_x(sm.list[i])));
+        own += q;
+        in_limit += i < limit ? q : 0;
       }
-      if (p_left) {
-        const u64 goal = max(1ull, part_ceil(fmaxf(p, 0.f), set));
-        const u64 target = goal > above_q ? goal - above_q : 1;
-        const Found f = search<false>(sm, 1, false, target, key_lo, key_hi, visit_list);
-        if (f.ok) {
-          const u64 one = max(units(wt.w(from_ordered(f.key))), 1ull);
-          take(f, (target - f.above_mass + one - 1) / one);
-        }
-      }
-      // the kept part of the list joins its segments
-      // (neighbours in the list are mostly of one segment: one atomic a warp)
-      u64 cnt = 0, none, before;
-      for (int i0 = 32 * warp; i0 < total; i0 += kThreads) {
-        const int i = i0 + lane;
-        const bool in = i < total && kept.in_prefix(ordered(sm.list.x[i]), sm.list.idx[i]);
-        const u64 one = in ? units(wt.w(sm.list.x[i])) : 0;
-        int to = -1;
-        if (in) {
-          const int v2 = (sm.list.idx[i] + row.lead) / kVec, c = v2 / row.per;
-          to = c * kWarps + (v2 - c * row.per) / row.per_warp;
-        }
-        cnt += in ? 1 : 0;
-        const int first = __reduce_max_sync(kFull, to);
-        if (first < 0) continue;
-        if (__all_sync(kFull, !in || to == first)) {
-          const u64 sum = warp_sum(one);
-          if (lane == 0) atomicAdd(&sm.seg[first], sum);
-        } else if (in) {
-          atomicAdd(&sm.seg[to], one);
-        }
-      }
-      block_scan(sm, cnt, 0, before, none);
+      block_scan(sm, own, in_limit, before, rest);
       if (tid == kThreads - 1) {
-        const u64 all = above_n + before + cnt;
-        for (int c = 0; c < CL; ++c) {
-          st_rank(&sm.x_out[0], c, static_cast<u64>(kept.kappa) << 32 | static_cast<uint32_t>(kept.last));
-          st_rank(&sm.x_out[1], c, set);
-          st_rank(&sm.x_out[2], c, all);
-        }
+        sm.found[4] = rest + in_limit;
+        sm.pick_lo = -1;
       }
+      __syncthreads();
+      const u64 set = by_count ? above_q + sm.found[4] : set_mass;
+      u64 goal = ~0ull;
+      if (!by_count || both) {
+        goal = max(1ull, part_ceil(fmaxf(p, 0.f), set));
+        goal = goal > above_q ? goal - above_q : 1;
+      }
+      // the last kept token: the last within the limit that begins before the
+      // goal (and, where that settles it, is not below min_p)
+      int mine = -1;
+      for (int i = i0; i < min(i1, limit) && before < goal; ++i) {
+        const float w = wt.w(key_x(sm.list[i]));
+        if (min_p_too && w < mp) break;
+        const u64 q = units(w);
+        before += q;
+        mine = i;
+        const int v2 = (static_cast<int>(~static_cast<uint32_t>(sm.list[i])) + row.lead) / kVec, c = v2 / row.per;
+        atomicAdd(&sm.seg[c * kWarps + (v2 - c * row.per) / row.per_warp], q);
+      }
+      if (mine >= 0) atomicMax(&sm.pick_lo, mine);
+      __syncthreads();
+      if (tid < CL) {
+        // (none: min_p cuts between the list and what lies above it)
+        const int last = sm.pick_lo;
+        st_rank(&sm.x_out[0], tid, last >= 0 ? sm.list[last] : static_cast<u64>(ordered(b.x1)) << 32 | 0x80000000u);
+        st_rank(&sm.x_out[1], tid, set);
+        st_rank(&sm.x_out[2], tid, above_n + static_cast<u64>(last + 1));
       }
     }
     sync_all(CL);
     kept.kappa = static_cast<uint32_t>(sm.x_out[0] >> 32);
-    kept.last = static_cast<int>(static_cast<uint32_t>(sm.x_out[0]));
+    kept.last = static_cast<int>(~static_cast<uint32_t>(sm.x_out[0]));
     set_mass = sm.x_out[1];
     kept_count = sm.x_out[2];
-    have_seg = true;
+    have_seg = mp <= 0.f || min_p_too;
     sync_all(CL);
     return true;
   };
 
   // the same by radix searches over the row
-  auto by_row = [&](bool by_count) {
+  auto by_row = [&](bool count) {
     have_seg = false;
     u64 target = static_cast<u64>(k);
-    if (!by_count) {
+    if (!count) {
       if (set_mass == 0) {
         u64 v[4] = {0, 0, 0, 0};
         visit_row([&](uint32_t, u64 w) { v[0] += w; });
@@ -1036,10 +864,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       }
       target = max(1ull, part_ceil(fmaxf(p, 0.f), set_mass));
     }
-    const Found f = search<true>(sm, CL, by_count, target, kKeyMin, key_max, visit_row);
+    const Found f = search(sm, CL, count, target, kKeyMin, key_max, visit_row);
     if (!f.ok) return;
     const u64 one = max(units(wt.w(from_ordered(f.key))), 1ull);
-    const u64 quota = by_count ? target - f.above_count : (target - f.above_mass + one - 1) / one;
+    const u64 quota = count ? target - f.above_count : (target - f.above_mass + one - 1) / one;
     set_mass = f.above_mass + min(quota, f.at_count) * units(wt.w(from_ordered(f.key)));
     kept.move_to(f.key);
     if (quota < f.at_count) {
@@ -1056,28 +884,23 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         });
       };
       const Found t =
-          search<true>(sm, CL, true, quota, 0xffffffffu - static_cast<uint32_t>(a.V), 0xffffffffu, visit_ties);
+          search(sm, CL, true, quota, 0xffffffffu - static_cast<uint32_t>(a.V), 0xffffffffu, visit_ties);
       kept.last = static_cast<int>(0xffffffffu - t.key);
     }
   };
 
-  if (k > 0) {
+  if (cut) {
     bool both = false;
-    if (!by_list(true, both)) {
+    if (!by_list(both)) {
       both = false;
-      by_row(true);
-    }
-    if (p < 1.f && !both) by_row(false);
-  } else if (p < 1.f) {
-    bool both = false;
-    if (!by_list(false, both)) {
       set_mass = 0;
-      by_row(false);
+      by_row(by_count);
     }
+    if (by_count && p < 1.f && !both) by_row(false);
   }
 
   // ---- the segments' weights, where pass 2 has not left them or min_p cuts
-  if (!have_seg || mp > 0.f) {
+  if (!have_seg) {
     u64 n = 0, q = 0;
     const float least = from_ordered(kept.kappa);
     row.batches(rank, [&](float (&x)[kUnroll][kVec], int i0) {
@@ -1196,21 +1019,23 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     sync_all(CL);
     const float logz = __uint_as_float(static_cast<uint32_t>(sm.x_out[3]));
     float* out = a.log_probs + static_cast<size_t>(r) * a.V;
-    row.batches(rank, [&](float (&x)[kUnroll][kVec], int i0) {
+    // (element by element: rows of the result need not begin at a vector)
+    const E* from = row.base + row.lead;
+    for (int i0 = rank * kThreads + tid; i0 < a.V; i0 += kBatch * CL * kThreads) {
+      float x[kBatch];
 #pragma unroll
-      for (int i = 0; i < kUnroll; ++i)
+      for (int j = 0; j < kBatch; ++j) {
+        const int idx = i0 + j * CL * kThreads;
+        x[j] = idx < a.V ? fmaxf(static_cast<float>(from[idx]), -INFINITY) : -INFINITY;
+      }
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const int idx = Row<E>::index(i0, i, e);
-          // (vectors past the segment's end hold -inf but are not this warp's)
-          const int v = (idx + row.lead) / kVec;
-          if (idx < 0 || idx >= a.V || v >= min(row.seg_begin(rank, warp + 1), min(row.vecs, rank * row.per + row.per)))
-            continue;
-          const float z = wt.z(x[i][e]);
-          const bool in = x[i][e] != -INFINITY && kept.in_prefix(ordered(x[i][e]), idx) && (mp <= 0.f || expf(z) >= mp);
-          out[idx] = in ? z - logz : -INFINITY;
-        }
-    });
+      for (int j = 0; j < kBatch; ++j) {
+        const int idx = i0 + j * CL * kThreads;
+        const float z = wt.z(x[j]);
+        const bool in = x[j] != -INFINITY && kept.in_prefix(ordered(x[j]), idx) && (mp <= 0.f || expf(z) >= mp);
+        if (idx < a.V) out[idx] = in ? z - logz : -INFINITY;
+      }
+    }
   }
   pdl_launch_next();
   sync_all(CL);  // no CTA leaves while another may write to its shared memory
