@@ -406,42 +406,68 @@ __device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 tar
   }
 }
 
-// Sorts n keys (a power of two, at least 32), the highest first: a bitonic
-// network whose strides below 32 are taken in registers, 32 keys a warp.
+// Sorts n keys, the highest first (n: a power of two, 32 K to 512 K): a
+// bitonic network.  A warp takes strides below 32 K in registers, its lanes
+// holding K keys of a run of 32 K; longer ones go through shared memory.
+// (1024 keys: 14 K cycles with K = 1 and two runs a warp, see the caller.)
+template <int K>
 __device__ __noinline__ void sort_keys(u64* key, int n) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  auto in_warp = [&](u64 x, int i, int size, int stride) {
-    const u64 y = __shfl_xor_sync(kFull, x, stride);
-    return ((i & stride) == 0) == ((i & size) == 0) ? max(x, y) : min(x, y);
-  };
-  __syncthreads();
-  for (int b = 32 * warp; b < n; b += kThreads) {
-    u64 x = key[b + lane];
+  const int lane = threadIdx.x & 31, first = (threadIdx.x >> 5) * 32 * K;
+  u64 x[K];
+  auto in_warp = [&](int size) {
 #pragma unroll
-    for (int size = 2; size <= 32; size <<= 1)
+    for (int stride = 16 * K; stride > 0; stride >>= 1) {
+      if (stride >= size) continue;
+      if (stride >= 32) {
 #pragma unroll
-      for (int stride = size / 2; stride > 0; stride >>= 1) x = in_warp(x, b + lane, size, stride);
-    key[b + lane] = x;
-  }
-  for (int size = 64; size <= n; size <<= 1) {
-    for (int stride = size / 2; stride >= 32; stride >>= 1) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < n / 2; i += kThreads) {
-        const int lo = 2 * i - (i & (stride - 1)), hi = lo + stride;
-        const u64 x = key[lo], y = key[hi];
-        if ((x < y) == ((lo & size) == 0)) {
-          key[lo] = y;
-          key[hi] = x;
+        for (int e = 0; e < K; ++e) {
+          const int f = e ^ (stride / 32);
+          if (f > e && f < K) {
+            const bool down = ((first + 32 * e) & size) == 0;
+            if ((x[e] < x[f]) == down) {
+              const u64 t = x[e];
+              x[e] = x[f];
+              x[f] = t;
+            }
+          }
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < K; ++e) {
+          const int i = first + 32 * e + lane;
+          const u64 y = __shfl_xor_sync(kFull, x[e], stride);
+          const bool high = ((i & stride) == 0) == ((i & size) == 0);
+          x[e] = (x[e] < y) == high ? y : x[e];
         }
       }
     }
-    __syncthreads();
-    for (int b = 32 * warp; b < n; b += kThreads) {
-      u64 x = key[b + lane];
+  };
+  __syncthreads();
+  for (int size = 2; size <= n; size <<= 1) {
+    for (int stride = size / 2; stride >= 32 * K; stride >>= 1) {
+      __syncthreads();
 #pragma unroll
-      for (int stride = 16; stride > 0; stride >>= 1) x = in_warp(x, b + lane, size, stride);
-      key[b + lane] = x;
+      for (int k = 0; k < K; ++k) {
+        const int i = threadIdx.x + k * kThreads;
+        if (i >= n / 2) break;
+        const int lo = 2 * i - (i & (stride - 1)), hi = lo + stride;
+        const u64 a = key[lo], b = key[hi];
+        if ((a < b) == ((lo & size) == 0)) {
+          key[lo] = b;
+          key[hi] = a;
+        }
+      }
     }
+    if (size == 2 || size > 32 * K) {
+      __syncthreads();
+      if (first < n)
+#pragma unroll
+        for (int e = 0; e < K; ++e) x[e] = key[first + 32 * e + lane];
+    }
+    if (first < n) in_warp(size);
+    if (size >= 32 * K && first < n)
+#pragma unroll
+      for (int e = 0; e < K; ++e) key[first + 32 * e + lane] = x[e];
   }
   __syncthreads();
 }
@@ -798,7 +824,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       int n2 = 32;
       while (n2 < total) n2 <<= 1;
       for (int i = total + tid; i < n2; i += kThreads) sm.list[i] = 0;
-      sort_keys(sm.list, n2);
+      // (a warp's run as long as keeps all warps at work)
+      if (n2 <= kThreads)
+        sort_keys<1>(sm.list, n2);
+      else if (n2 == 2 * kThreads)
+        sort_keys<2>(sm.list, n2);
+      else if (n2 == 4 * kThreads)
+        sort_keys<4>(sm.list, n2);
+      else
+        sort_keys<8>(sm.list, n2);
       const int each = max(1, n2 / kThreads), i0 = tid * each, i1 = min(total, i0 + each);
       const int limit = by_count ? min(static_cast<int>(static_cast<u64>(k) - above_n), total) : total;
       u64 own = 0, in_limit = 0, before, rest;
