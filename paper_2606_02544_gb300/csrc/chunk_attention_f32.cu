@@ -36,6 +36,7 @@ struct F32Params {
   int hblocks;    // units that the heads of a KV head make
   int tb;         // tokens of a unit
   int nsplit;
+  int heads, units;  // CTAs of a token's heads, and of the call's tokens
 };
 
 template <int D, int RB>
@@ -83,7 +84,7 @@ __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_consta
   const ChunkArgs& a = p.a;
   const unsigned full = 0xffffffffu;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) {
+  if (blockIdx.x == 0 && blockIdx.z == 0) {
     uint32_t e = 0;
     for (int b = tid; b < a.Bt; b += kThreads) {
       const ChunkSeq s = chunk_seq(a, b);
@@ -91,9 +92,12 @@ __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_consta
     }
     if (e) raise_error(a.err_word, e);
   }
+  // heads first, then units from the last down: the later tokens of a chunk
+  // see more keys, and what starts last should be short
+  const int head = blockIdx.x % p.heads;
   // the unit: sequences in turn, each of ceil(C / tb) units
   if (warp == 0) {
-    int at = blockIdx.x, b = -1, j = 0;
+    int at = p.units - 1 - blockIdx.x / p.heads, b = -1, j = 0;
     for (int b0 = 0; b0 < a.Bt && b < 0; b0 += 32) {
       const int n = b0 + lane < a.Bt ? (chunk_of(a.token_start, b0 + lane, a.T).count + p.tb - 1) / p.tb : 0;
       int inc = n;
@@ -121,7 +125,7 @@ __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_consta
   if (b < 0) return;
   const ChunkSeq s = chunk_seq(a, b);
   const int i0 = unit_s[1] * p.tb, i1 = min(s.C, i0 + p.tb);
-  const int kvh = blockIdx.y / p.hblocks, h0 = kvh * p.g + (blockIdx.y - kvh * p.hblocks) * p.gb;
+  const int kvh = head / p.hblocks, h0 = kvh * p.g + (head - kvh * p.hblocks) * p.gb;
   const int heads = min(p.gb, kvh * p.g + p.g - h0);
   const int rows = (i1 - i0) * p.gb;  // row r: token i0 + r / gb, head h0 + r % gb (if below `heads`)
   int lo = 0, hi = 0;
@@ -348,19 +352,25 @@ struct F32Plan {
   int rb, gb, hblocks, tb, units, nsplit;
 };
 
-// RB 64 where a sequence has more than 16 query rows a KV head on average
-// (the wider block reads K and V a quarter as often), else 16.  Ranges of
-// keys until about two CTAs a SM are at work, none shorter than 4 tiles of
-// the longest possible key range.
+// RB 16 where a sequence has up to 16 query rows a KV head on average, 64
+// where it has more (the wider block reads K and V a quarter as often), 128
+// where even such blocks are two a SM (4 chunks of 512 tokens, 32 heads: 675
+// us, with 64 rows 777 us).  Ranges of keys until about two CTAs a SM are at
+// work, none shorter than 4 tiles of the longest possible key range.
 F32Plan f32_plan(int T, int Bt, int Hq, int Hkv, long long max_keys, int num_sms) {
   F32Plan f;
   const int g = Hq / Hkv;
-  f.rb = g > 16 || static_cast<long long>(T) * g > 16ll * Bt ? 64 : 16;
-  f.gb = std::min(g, f.rb);
-  f.hblocks = (g + f.gb - 1) / f.gb;
-  f.tb = f.rb / f.gb;
-  f.units = static_cast<int>(std::min<long long>(T, T / f.tb + static_cast<long long>(Bt)));
-  const long long ctas = static_cast<long long>(f.units) * Hkv * f.hblocks;
+  auto lay = [&](int rb) {
+    f.rb = rb;
+    f.gb = std::min(g, rb);
+    f.hblocks = (g + f.gb - 1) / f.gb;
+    f.tb = rb / f.gb;
+    f.units = static_cast<int>(std::min<long long>(T, T / f.tb + static_cast<long long>(Bt)));
+    return static_cast<long long>(f.units) * Hkv * f.hblocks;
+  };
+  long long ctas = lay(128);
+  if (ctas < 2ll * num_sms || static_cast<long long>(T) * g <= 64ll * Bt)
+    ctas = lay(g > 16 || static_cast<long long>(T) * g > 16ll * Bt ? 64 : 16);
   const long long most = std::max<long long>(1, (max_keys + kTile - 1) / kTile / 4);
   f.nsplit = static_cast<int>(std::max<long long>(1, std::min<long long>({2ll * num_sms / ctas, most, 64})));
   return f;
@@ -383,7 +393,7 @@ cudaError_t launch_rb(const F32Params& p, const F32Plan& f, cudaStream_t stream)
       done[dev] = true;
     }
   }
-  const dim3 grid(static_cast<unsigned>(f.units), static_cast<unsigned>(p.a.Hkv * f.hblocks), static_cast<unsigned>(f.nsplit));
+  const dim3 grid(static_cast<unsigned>(f.units) * static_cast<unsigned>(p.heads), 1u, static_cast<unsigned>(f.nsplit));
   cudaError_t e = launch_overlapped(chunk_f32_kernel<D, RB>, grid, dim3(kThreads), sizeof(SmemF32<D, RB>), stream, 1u, p);
   if (e != cudaSuccess || f.nsplit == 1) return e;
   const unsigned blocks = static_cast<unsigned>((static_cast<long long>(p.a.T) * p.a.Hq + 3) / 4);
@@ -408,6 +418,10 @@ cudaError_t launch_chunk_attention_f32(const ChunkArgs& a, int num_sms, cudaStre
   p.hblocks = f.hblocks;
   p.tb = f.tb;
   p.nsplit = f.nsplit;
+  p.heads = a.Hkv * f.hblocks;
+  p.units = f.units;
+  if (f.rb == 128)
+    return a.d == 128 ? launch_rb<128, 128>(p, f, stream) : launch_rb<64, 128>(p, f, stream);
   if (f.rb == 64)
     return a.d == 128 ? launch_rb<128, 64>(p, f, stream) : launch_rb<64, 64>(p, f, stream);
   return a.d == 128 ? launch_rb<128, 16>(p, f, stream) : launch_rb<64, 16>(p, f, stream);
