@@ -10,10 +10,10 @@
 // one run, V while its S does) and keeps O in registers: a thread owns RB /
 // 16 rows and, of S, 4 columns, of O, d / 16 columns, so a value read from
 // shared memory serves 4 to 8 products and the rows' rescaling is local.
-// RB is 64 for chunks of many rows (bound by the FMA pipes), 16 for single
-// tokens (bound by memory, then by the reads of K and V from shared memory).
-// Few units are split over their keys into nsplit ranges, whose partial
-// (O, m, l) a second launch merges.
+// Bound by the FMA pipes where blocks are wide: 4 chunks of 512 tokens over
+// 500 to 1000 keys, 32 heads, take 675 us, about 37 TFLOP/s of 74.  Few units
+// are split over their keys into nsplit ranges, whose partial (O, m, l) a
+// second launch merges.  Few rows have a kernel of their own (below).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -29,6 +29,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTile = 64;  // keys per tile
+constexpr int kFewTile = kThreads;  // of the kernel for few rows
 
 struct F32Params {
   ChunkArgs a;
@@ -45,7 +46,7 @@ struct SmemF32 {
   float k[kTile][D];  // 16-byte chunk c of row r lies at chunk c ^ (r & 7)
   float v[kTile][D];
   float p[RB][kTile];
-  long long row[2][kTile];  // per tile parity: a key's row in the pool, in 16-byte units (-1: hidden)
+  uint32_t row[2][kTile];  // per tile parity: the keys' rows in the pool
 };
 
 __device__ __forceinline__ void cp_async16(void* dst, const void* src, bool real) {
@@ -72,15 +73,20 @@ __device__ __forceinline__ float2* partial_ml(const F32Params& p, size_t row, in
          row * p.nsplit + split;
 }
 
-template <int D, int RB>
-__global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_constant__ F32Params p) {
-  constexpr int RT = RB / 16;   // rows of a thread
-  constexpr int OC = D / 64;    // four-column groups of O of a thread
-  extern __shared__ uint4 smem_raw[];
-  SmemF32<D, RB>& sm = *reinterpret_cast<SmemF32<D, RB>*>(smem_raw);
+// A CTA's share of the call: query rows of one sequence and KV head, and a
+// range of key tiles.
+struct Unit {
+  ChunkSeq s;
+  int i0, rows;       // row r: token i0 + r / gb, head h0 + r % gb (if below `heads`)
+  int kvh, h0, heads;
+  int lo, hi;         // keys that any of the rows sees
+  int t_begin, t_end;
+  const int32_t* bt;
+};
+
+// False: nothing to do.  Called by all threads.
+__device__ __forceinline__ bool unit_of(const F32Params& p, const int tile, Unit& u) {
   __shared__ int unit_s[2];
-  pdl_wait();
-  pdl_launch_next();
   const ChunkArgs& a = p.a;
   const unsigned full = 0xffffffffu;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -122,50 +128,75 @@ __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_consta
   }
   __syncthreads();
   const int b = unit_s[0];
-  if (b < 0) return;
-  const ChunkSeq s = chunk_seq(a, b);
-  const int i0 = unit_s[1] * p.tb, i1 = min(s.C, i0 + p.tb);
-  const int kvh = head / p.hblocks, h0 = kvh * p.g + (head - kvh * p.hblocks) * p.gb;
-  const int heads = min(p.gb, kvh * p.g + p.g - h0);
-  const int rows = (i1 - i0) * p.gb;  // row r: token i0 + r / gb, head h0 + r % gb (if below `heads`)
-  int lo = 0, hi = 0;
-  if (!s.bad) {
-    lo = key_lo(a, s, i0);
-    hi = key_hi(a, s, i1 - 1);
+  if (b < 0) return false;
+  u.s = chunk_seq(a, b);
+  u.i0 = unit_s[1] * p.tb;
+  const int i1 = min(u.s.C, u.i0 + p.tb);
+  u.kvh = head / p.hblocks;
+  u.h0 = u.kvh * p.g + (head - u.kvh * p.hblocks) * p.gb;
+  u.heads = min(p.gb, u.kvh * p.g + p.g - u.h0);
+  u.rows = (i1 - u.i0) * p.gb;
+  u.lo = u.hi = 0;
+  if (!u.s.bad) {
+    u.lo = key_lo(a, u.s, u.i0);
+    u.hi = key_hi(a, u.s, i1 - 1);
   }
-  if (lo >= hi) lo = hi = 0;
-  const int32_t* bt = a.block_table + static_cast<size_t>(b) * a.max_pages;
+  if (u.lo >= u.hi) u.lo = u.hi = 0;
+  u.bt = a.block_table + static_cast<size_t>(b) * a.max_pages;
   bool bad = false;
-  if (hi > lo)
-    for (int i = lo / a.page_size + tid; i <= (hi - 1) / a.page_size; i += kThreads)
-      bad |= bt[i] < 0 || bt[i] >= a.num_pages;
+  if (u.hi > u.lo)
+    for (int i = u.lo / a.page_size + tid; i <= (u.hi - 1) / a.page_size; i += kThreads)
+      bad |= u.bt[i] < 0 || u.bt[i] >= a.num_pages;
   bad = __syncthreads_or(bad);
   if (bad && tid == 0) raise_error(a.err_word, SIMSD_EW_PAGE);
-  if (bad) hi = lo;
-  // this CTA's tiles
-  const int T0 = lo / kTile, nt = hi > lo ? (hi + kTile - 1) / kTile - T0 : 0;
-  const int t_begin = T0 + static_cast<int>(static_cast<long long>(blockIdx.z) * nt / p.nsplit);
-  const int t_end = T0 + static_cast<int>(static_cast<long long>(blockIdx.z + 1) * nt / p.nsplit);
+  if (bad) u.hi = u.lo;
+  const int T0 = u.lo / tile, nt = u.hi > u.lo ? (u.hi + tile - 1) / tile - T0 : 0;
+  u.t_begin = T0 + static_cast<int>(static_cast<long long>(blockIdx.z) * nt / p.nsplit);
+  u.t_end = T0 + static_cast<int>(static_cast<long long>(blockIdx.z + 1) * nt / p.nsplit);
+  return true;
+}
+
+// The keys that row r of the unit sees.
+__device__ __forceinline__ void row_keys(const F32Params& p, const Unit& u, int r, int& lo, int& hi) {
+  const bool real = r < u.rows && u.hi > u.lo;
+  lo = real ? key_lo(p.a, u.s, u.i0 + r / p.gb) : 0;
+  hi = real ? key_hi(p.a, u.s, u.i0 + r / p.gb) : 0;
+}
+
+// A key's row in the pool (~0: not among [lo, hi); 2^32 rows would be a terabyte).
+__device__ __forceinline__ uint32_t pool_row(const F32Params& p, const Unit& u, int key) {
+  if (key < u.lo || key >= u.hi) return ~0u;
+  const int pi = key / p.a.page_size;
+  return (static_cast<uint32_t>(u.bt[pi]) * p.a.Hkv + u.kvh) * p.a.page_size + (key - pi * p.a.page_size);
+}
+
+template <int D, int RB>
+__global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_constant__ F32Params p) {
+  constexpr int RT = RB / 16;   // rows of a thread
+  constexpr int OC = D / 64;    // four-column groups of O of a thread
+  extern __shared__ uint4 smem_raw[];
+  SmemF32<D, RB>& sm = *reinterpret_cast<SmemF32<D, RB>*>(smem_raw);
+  pdl_wait();
+  pdl_launch_next();
+  const ChunkArgs& a = p.a;
+  const unsigned full = 0xffffffffu;
+  const int tid = threadIdx.x;
+  Unit u;
+  if (!unit_of(p, kTile, u)) return;
+  const ChunkSeq& s = u.s;
+  const int t_begin = u.t_begin, t_end = u.t_end, rows = u.rows, heads = u.heads, h0 = u.h0, i0 = u.i0;
 
   // where the keys of tile t lie (the page arithmetic once a key, not once a copy)
   auto find_rows = [&](int t) {
-    if (tid < kTile) {
-      const int key = t * kTile + tid;
-      long long off = -1;
-      if (key >= lo && key < hi) {
-        const int pi = key / a.page_size;
-        off = ((static_cast<long long>(bt[pi]) * a.Hkv + kvh) * a.page_size + (key - pi * a.page_size)) * (D / 4);
-      }
-      sm.row[t & 1][tid] = off;
-    }
+    if (tid < kTile) sm.row[t & 1][tid] = pool_row(p, u, t * kTile + tid);
   };
   auto load_tile = [&](int t, bool is_k) {
     const float4* src = static_cast<const float4*>(is_k ? a.k_cache : a.v_cache);
     const int c = tid % (D / 4);
 #pragma unroll 4
     for (int r = tid / (D / 4); r < kTile; r += kThreads / (D / 4)) {
-      const long long off = sm.row[t & 1][r];
-      cp_async16(is_k ? &sm.k[r][4 * (c ^ (r & 7))] : &sm.v[r][4 * c], src + (off < 0 ? 0 : off + c), off >= 0);
+      const uint32_t at = sm.row[t & 1][r];
+      cp_async16(is_k ? &sm.k[r][4 * (c ^ (r & 7))] : &sm.v[r][4 * c], src + (at == ~0u ? 0 : static_cast<size_t>(at) * (D / 4) + c), at != ~0u);
     }
     cp_async_commit();
   };
@@ -188,10 +219,7 @@ __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_consta
   float m[RT], l[RT], o[RT][OC][4];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const int row = ty * RT + r;
-    const bool real = row < rows && nt > 0;
-    klo[r] = real ? key_lo(a, s, i0 + row / p.gb) : 0;
-    khi[r] = real ? key_hi(a, s, i0 + row / p.gb) : 0;
+    row_keys(p, u, ty * RT + r, klo[r], khi[r]);
     m[r] = -INFINITY;
     l[r] = 0.f;
 #pragma unroll
@@ -315,6 +343,150 @@ __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_consta
   }
 }
 
+// Few rows (single tokens, short drafts): a warp takes keys for itself, four
+// at a time, its lanes the columns, with Q, O and the running maximum and sum
+// of R rows in registers; K and V go from the cache straight to registers,
+// the next four keys' while these are worked on.  The warps' results are
+// merged through shared memory.  Bound by memory and by the sums over the
+// lanes (20 shuffles a key): 32 single tokens over 4096 keys, 32 heads on 8,
+// read 1.07 GB in 260 us (4.1 TB/s); tiles of 16 rows took 650.
+template <int D>
+__global__ void __launch_bounds__(kThreads, 2) chunk_f32_few_kernel(const __grid_constant__ F32Params p) {
+  constexpr int E = D / 32, kWarps = kThreads / 32, kKeys = 4, R = 4;
+  struct alignas(4 * E) Vec {
+    float x[E];
+  };
+  // (three: a warp may still be at a tile while another is past the barrier of the next)
+  __shared__ uint32_t key_row[3][kFewTile];
+  __shared__ alignas(16) float part_o[kWarps][R][D];
+  __shared__ float part_m[kWarps][R], part_l[kWarps][R];
+  __shared__ int2 sees[R];  // the keys that a row sees
+  pdl_wait();
+  pdl_launch_next();
+  const ChunkArgs& a = p.a;
+  const unsigned full = 0xffffffffu;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  Unit u;
+  if (!unit_of(p, kFewTile, u)) return;
+  Vec q[R], o[R];
+  float m[R], l[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int tl = r / p.gb, hh = r - tl * p.gb;
+    const bool real = r < u.rows && hh < u.heads;
+    if (real)
+      q[r] = *reinterpret_cast<const Vec*>(static_cast<const float*>(a.q) +
+                                           static_cast<long long>(u.s.start + u.i0 + tl) * a.q_stride +
+                                           static_cast<long long>(u.h0 + hh) * D + E * lane);
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      o[r].x[e] = 0.f;
+      q[r].x[e] = real ? q[r].x[e] * a.scale : 0.f;
+    }
+  }
+  const Vec* kp = static_cast<const Vec*>(a.k_cache);
+  const Vec* vp = static_cast<const Vec*>(a.v_cache);
+  if (tid < R) row_keys(p, u, tid, sees[tid].x, sees[tid].y);
+  if (u.t_begin < u.t_end) key_row[u.t_begin % 3][tid] = pool_row(p, u, u.t_begin * kFewTile + tid);
+  __syncthreads();
+  Vec k[kKeys], v[kKeys];
+  // (hidden keys: zeros)
+  auto load = [&](Vec (&to)[kKeys], const Vec* from, const uint32_t* rows) {
+#pragma unroll
+    for (int j = 0; j < kKeys; ++j) {
+      const uint32_t at = rows[j];
+#pragma unroll
+      for (int e = 0; e < E; ++e) to[j].x[e] = 0.f;
+      if (at != ~0u) to[j] = from[static_cast<size_t>(at) * 32 + lane];
+    }
+  };
+  constexpr int kRun = kFewTile / kWarps;  // keys of a warp in a tile
+  if (u.t_begin < u.t_end) {
+    load(k, kp, &key_row[u.t_begin % 3][warp * kRun]);
+    load(v, vp, &key_row[u.t_begin % 3][warp * kRun]);
+  }
+  for (int t = u.t_begin; t < u.t_end; ++t) {
+    if (t + 1 < u.t_end) key_row[(t + 1) % 3][tid] = pool_row(p, u, (t + 1) * kFewTile + tid);
+    __syncthreads();
+#pragma unroll 1
+    for (int c = 0; c < kRun; c += kKeys) {
+      float sc[R][kKeys];
+#pragma unroll
+      for (int j = 0; j < kKeys; ++j) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          float x = 0.f;
+#pragma unroll
+          for (int e = 0; e < E; ++e) x = fmaf(q[r].x[e], k[j].x[e], x);
+          sc[r][j] = x;
+        }
+      }
+      const bool more = c + kKeys < kRun || t + 1 < u.t_end;
+      const uint32_t* next = c + kKeys < kRun ? &key_row[t % 3][warp * kRun + c + kKeys] : &key_row[(t + 1) % 3][warp * kRun];
+      if (more) load(k, kp, next);
+      const int key0 = t * kFewTile + warp * kRun + c;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float mx = m[r];
+#pragma unroll
+        for (int j = 0; j < kKeys; ++j) {
+#pragma unroll
+          for (int w = 16; w > 0; w >>= 1) sc[r][j] += __shfl_xor_sync(full, sc[r][j], w);
+          if (key0 + j < sees[r].x || key0 + j >= sees[r].y) sc[r][j] = -INFINITY;
+          mx = fmaxf(mx, sc[r][j]);
+        }
+        // (nothing seen so far: every weight is zero)
+        const float ref = mx == -INFINITY ? 0.f : mx, corr = expf(m[r] - ref);
+        l[r] *= corr;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[r].x[e] *= corr;
+#pragma unroll
+        for (int j = 0; j < kKeys; ++j) {
+          const float w = expf(sc[r][j] - ref);
+          l[r] += w;
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[r].x[e] = fmaf(w, v[j].x[e], o[r].x[e]);
+        }
+        m[r] = mx;
+      }
+      if (more) load(v, vp, next);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    *reinterpret_cast<Vec*>(&part_o[warp][r][E * lane]) = o[r];
+    if (lane == 0) {
+      part_m[warp][r] = m[r];
+      part_l[warp][r] = l[r];
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < R * D; i += kThreads) {
+    const int r = i / D, c = i - r * D, tl = r / p.gb, hh = r - tl * p.gb;
+    if (r >= u.rows || hh >= u.heads) continue;
+    float M = -INFINITY, L = 0.f, acc = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) M = fmaxf(M, part_m[w][r]);
+    const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float x = expf(part_m[w][r] - ref);
+      L = fmaf(x, part_l[w][r], L);
+      acc = fmaf(x, part_o[w][r][c], acc);
+    }
+    const size_t out_row = static_cast<size_t>(u.s.start + u.i0 + tl) * a.Hq + u.h0 + hh;
+    if (p.nsplit > 1) {
+      partial_o<D>(p, out_row, blockIdx.z)[c] = L != 0.f ? acc : 0.f;
+      if (c == 0) *partial_ml<D>(p, out_row, blockIdx.z) = make_float2(M, L);
+    } else {
+      static_cast<float*>(a.out)[out_row * D + c] = L != 0.f ? acc * (1.f / L) : 0.f;
+      if (a.lse && c == 0) a.lse[out_row] = L != 0.f ? M + logf(L) : -INFINITY;
+    }
+  }
+}
+
 // A warp per (token, head): O = sum_i e^(m_i - M) O_i / sum_i e^(m_i - M) l_i.
 template <int D>
 __global__ void __launch_bounds__(128) chunk_f32_merge_kernel(const __grid_constant__ F32Params p) {
@@ -348,15 +520,19 @@ __global__ void __launch_bounds__(128) chunk_f32_merge_kernel(const __grid_const
   if (p.a.lse && lane == 0) p.a.lse[row] = L != 0.f ? M + logf(L) : -INFINITY;
 }
 
+static_assert(2 * (sizeof(SmemF32<128, 64>) + 1024 + 64) <= 228 * 1024, "two CTAs a SM");
+
 struct F32Plan {
   int rb, gb, hblocks, tb, units, nsplit;
 };
 
-// RB 16 where a sequence has up to 16 query rows a KV head on average, 64
-// where it has more (the wider block reads K and V a quarter as often), 128
-// where even such blocks are two a SM (4 chunks of 512 tokens, 32 heads: 675
-// us, with 64 rows 777 us).  Ranges of keys until about two CTAs a SM are at
-// work, none shorter than 4 tiles of the longest possible key range.
+// Blocks of 4 rows (in registers) where a sequence has up to 8 query rows a KV
+// head on average, of 16 up to 16, of 64 where it has more (K and V are read a
+// quarter as often), of 128 where even such blocks are two a SM.  32 sequences
+// over 4096 keys, 32 heads on 8: 2 tokens 505 us with 4 rows, 646 with 16; 4
+// tokens 878 and 646.  4 chunks of 512 tokens: 675 us with 128 rows, 777 with
+// 64.  Ranges of keys until about four CTAs a SM are at work, none shorter
+// than 3 tiles (for 4 rows, one of theirs) of the longest possible key range.
 F32Plan f32_plan(int T, int Bt, int Hq, int Hkv, long long max_keys, int num_sms) {
   F32Plan f;
   const int g = Hq / Hkv;
@@ -370,19 +546,24 @@ F32Plan f32_plan(int T, int Bt, int Hq, int Hkv, long long max_keys, int num_sms
   };
   long long ctas = lay(128);
   if (ctas < 2ll * num_sms || static_cast<long long>(T) * g <= 64ll * Bt)
-    ctas = lay(g > 16 || static_cast<long long>(T) * g > 16ll * Bt ? 64 : 16);
-  const long long most = std::max<long long>(1, (max_keys + kTile - 1) / kTile / 4);
-  f.nsplit = static_cast<int>(std::max<long long>(1, std::min<long long>({2ll * num_sms / ctas, most, 64})));
+    ctas = lay(static_cast<long long>(T) * g > 16ll * Bt ? 64 : static_cast<long long>(T) * g > 8ll * Bt ? 16 : 4);
+  const long long least = f.rb == 4 ? kFewTile : 3 * kTile;
+  const long long most = std::max<long long>(1, (max_keys + least - 1) / least);
+  f.nsplit = static_cast<int>(std::max<long long>(1, std::min<long long>({4ll * num_sms / ctas, most, 64})));
   return f;
 }
 
 template <int D, int RB>
 cudaError_t launch_rb(const F32Params& p, const F32Plan& f, cudaStream_t stream) {
-  {
+  const dim3 grid(static_cast<unsigned>(f.units) * static_cast<unsigned>(p.heads), 1u, static_cast<unsigned>(f.nsplit));
+  cudaError_t e;
+  if constexpr (RB == 4) {
+    e = launch_overlapped(chunk_f32_few_kernel<D>, grid, dim3(kThreads), 0, stream, 1u, p);
+  } else {
     static std::mutex mu;
     static bool done[64] = {};
     int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     std::lock_guard<std::mutex> lk(mu);
@@ -392,9 +573,8 @@ cudaError_t launch_rb(const F32Params& p, const F32Plan& f, cudaStream_t stream)
       if (e != cudaSuccess) return e;
       done[dev] = true;
     }
+    e = launch_overlapped(chunk_f32_kernel<D, RB>, grid, dim3(kThreads), sizeof(SmemF32<D, RB>), stream, 1u, p);
   }
-  const dim3 grid(static_cast<unsigned>(f.units) * static_cast<unsigned>(p.heads), 1u, static_cast<unsigned>(f.nsplit));
-  cudaError_t e = launch_overlapped(chunk_f32_kernel<D, RB>, grid, dim3(kThreads), sizeof(SmemF32<D, RB>), stream, 1u, p);
   if (e != cudaSuccess || f.nsplit == 1) return e;
   const unsigned blocks = static_cast<unsigned>((static_cast<long long>(p.a.T) * p.a.Hq + 3) / 4);
   return launch_overlapped(chunk_f32_merge_kernel<D>, dim3(blocks), dim3(128), 0, stream, 1u, p);
@@ -422,9 +602,9 @@ cudaError_t launch_chunk_attention_f32(const ChunkArgs& a, int num_sms, cudaStre
   p.units = f.units;
   if (f.rb == 128)
     return a.d == 128 ? launch_rb<128, 128>(p, f, stream) : launch_rb<64, 128>(p, f, stream);
-  if (f.rb == 64)
-    return a.d == 128 ? launch_rb<128, 64>(p, f, stream) : launch_rb<64, 64>(p, f, stream);
-  return a.d == 128 ? launch_rb<128, 16>(p, f, stream) : launch_rb<64, 16>(p, f, stream);
+  if (f.rb == 64) return a.d == 128 ? launch_rb<128, 64>(p, f, stream) : launch_rb<64, 64>(p, f, stream);
+  if (f.rb == 16) return a.d == 128 ? launch_rb<128, 16>(p, f, stream) : launch_rb<64, 16>(p, f, stream);
+  return a.d == 128 ? launch_rb<128, 4>(p, f, stream) : launch_rb<64, 4>(p, f, stream);
 }
 
 }  // namespace simsd
