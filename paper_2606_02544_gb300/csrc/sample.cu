@@ -402,7 +402,7 @@ __device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 tar
       sync_all(CL);  // the histograms are read by all before anything else is written there
       return f;
     }
-    hi = min(hi, lo + ((1u << shift) - 1u));
+    hi = lo + min(hi - lo, (1u << shift) - 1u);  // (lo plus a bin may pass 2^32)
   }
 }
 

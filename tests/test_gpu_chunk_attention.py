@@ -245,3 +245,21 @@ def test_chunks_of_a_prompt_equal_the_whole():
     got = torch.cat(parts).double()
     # each side rounds P and O to bf16: twice the bound's leading terms, |v| <= 3.5 std here
     assert (got - whole.double()).abs().max().item() <= 2 * 2.0 ** -8 * 2 * 3.5 * 0.5
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (4, 2), (12, 2), (16, 2), (18, 2)])
+def test_few_rows_over_long_caches(dtype, d, Hq, Hkv):
+    """Single tokens and short drafts; the fp32 kernel for few rows takes its
+    keys 256 at a time, four to a warp's step."""
+    prefix = [255, 256, 1030, 3, 700]
+    check(make(dtype, [1] * 5, prefix, Hq, Hkv, d, 16, 11))
+    check(make(dtype, [2, 1, 0, 3, 1], prefix, Hq, Hkv, d, 8, 12, key_start=[0, 250, 0, 2, 699]), window=300)
+    check(make(dtype, [1, 2, 1, 1, 1], prefix, Hq, Hkv, d, 128, 13), mask_block=2, window=7)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_many_heads_and_long_chunks(dtype):
+    """So many query rows that the fp32 kernel takes them 128 at a time."""
+    check(make(dtype, [300, 130, 40], [100, 0, 333], 64, 64, 64, 32, 14), mask_block=4)

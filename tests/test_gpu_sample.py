@@ -179,3 +179,42 @@ def test_shares_over_a_grid_of_random_numbers():
     token, kept, _, lps, _ = run(x.expand(n, V).contiguous(), u, k=[60] * n, p=[0.9] * n)
     got = np.bincount(token, minlength=V) / n
     assert np.allclose(got, np.exp(lps[0]), atol=2.0 / n)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("limits", [dict(p=0.9), dict(p=0.999), dict(k=30, p=0.95), dict(p=0.99, mp=0.01)])
+def test_a_few_tokens_far_above_all_others(dtype, limits):
+    """A certain next token: the sample that lays the histogram's bins need
+    not hold it, whether it lies inside them or above them all."""
+    x = logits(6, 40001, 2.0, 21, dtype)
+    x[0, 77] = 19.0
+    x[1, 30000] = x[1, 30001] = 25.0
+    x[2, 4] = 60.0
+    x[3, 40000], x[3, 39] = 400.0, 399.0
+    x[4, 5000:5003] = 1e4
+    check(x, 22, T=0.8, probs=False, **limits)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("hidden", [float("-inf"), -1e30, -1e4])
+@pytest.mark.parametrize("limits", [dict(p=0.9), dict(k=3), dict(k=500, p=0.9), dict(p=0.95, mp=0.05)])
+def test_all_but_a_few_tokens_masked(dtype, hidden, limits):
+    """As under a grammar: none, one or some of the sampled tokens are open."""
+    x = logits(5, 40001, 2.0, 23, torch.float32, banned=0.0)
+    r = np.random.default_rng(24)
+    for i, n in enumerate([1, 3, 40, 700, 9000]):
+        open_ = torch.as_tensor(r.permutation(40001)[:n]).cuda()
+        keep = x[i, open_].clone()
+        x[i] = hidden
+        x[i, open_] = keep
+    check(x.to(dtype), 25, T=0.9, probs=False, **limits)
+
+
+@pytest.mark.parametrize("V,spread,limits", [
+    (40001, 1.0, dict(k=600)), (40001, 1.0, dict(k=1100, p=0.9)), (40001, 2.0, dict(k=2500, p=0.97, mp=0.001)),
+    (40001, 1.0, dict(k=4096, p=0.9)), (40001, 1.0, dict(k=4097)), (5000, 0.5, dict(k=4900, p=0.99)),
+    (40001, 0.5, dict(p=0.99, mp=0.4)),    # min_p cuts above what top_p leaves open
+    (40001, 0.5, dict(k=30000, mp=0.3)), (40001, 2.0, dict(p=0.9999)), (40001, 2.0, dict(T=200.0, p=0.8)),
+    (40001, 2.0, dict(T=0.01, p=0.9))])
+def test_lists_of_every_length(V, spread, limits):
+    check(logits(4, V, spread, 26), 27, **{"T": 1.0, **limits}, probs=False)
