@@ -223,14 +223,17 @@ struct Row {
   __device__ __forceinline__ int seg_begin(int rank, int warp) const {
     return min(min(vecs, rank * per + per), min(vecs, rank * per) + warp * per_warp);
   }
-  // batches of kUnroll vectors of this thread's segment: f(x, first index of each vector)
-  template <typename F>
+  // batches of kUnroll vectors of this thread's segment: f(x, first index of each vector);
+  // kBack: the last first
+  template <bool kBack = false, typename F>
   __device__ __forceinline__ void batches(int rank, F&& f) const {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int a = seg_begin(rank, warp), b = min(seg_begin(rank, warp + 1), min(vecs, rank * per + per));
     const int whole = min(b, (V + lead) / kVec);  // vectors with nothing past the row's end
     // (all lanes stay in the loop: what it calls may exchange within the warp)
-    for (int v = a + lane; v - lane < b; v += 32 * kUnroll) {
+    const int step = 32 * kUnroll, runs = b > a ? (b - a + step - 1) / step : 0;
+    for (int run = 0; run < runs; ++run) {
+      const int v = a + lane + (kBack ? runs - 1 - run : run) * step;
       float x[kUnroll][kVec];
       const int v0 = v - lane;
       if (v0 * kVec >= lead && v0 + 32 * kUnroll <= whole) {
@@ -738,7 +741,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     LongSum fq, fa;
     uint32_t n = 0;
     if (b.all && by_count) {
-      row.batches(rank, [&](float (&x)[kUnroll][kVec], int i0) {
+      row.template batches<true>(rank, [&](float (&x)[kUnroll][kVec], int i0) {
 #pragma unroll
         for (int i = 0; i < kUnroll; ++i)
 #pragma unroll
@@ -746,7 +749,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             if (x[i][e] >= x0) list(x[i][e], Row<E>::index(i0, i, e));
       });
     } else {
-      row.batches(rank, [&](float (&x)[kUnroll][kVec], int i0) {
+      row.template batches<true>(rank, [&](float (&x)[kUnroll][kVec], int i0) {
         float s = 0.f, sa = 0.f;
 #pragma unroll
         for (int i = 0; i < kUnroll; ++i) {
