@@ -144,9 +144,9 @@ struct alignas(16) Smem {
   uint32_t hist[kBins];  // pass 1: counts, or weights in 2^-16 of their bin's middle
   uint32_t count[kFine];
   u64 seg[kMaxCluster * kWarps];  // weights of the row's segments (rank 0 holds all)
-  u64 warp_a[kWarps], warp_b[kWarps], warp_c[kWarps];
+  u64 warp_a[kWarps], warp_b[kWarps], warp_v[4][kWarps];
   u64 x_max[kMaxCluster];                          // exchanges over the cluster: one slot per CTA
-  u64 x_sum[4][kMaxCluster];
+  u64 x_sum[2][4][kMaxCluster];                    // (in turn, so that a sum costs one barrier)
   u64 x_out[4];
   u64 found[5];
   int list_n, pick_lo, pick_hi, token;
@@ -265,36 +265,26 @@ __device__ __forceinline__ u64 warp_sum(u64 v) {
   return v;
 }
 
-// Sums over the cluster of four values; every CTA gets them.
-__device__ __noinline__ void cluster_sum(Smem& sm, int CL, int rank, u64 (&v)[4]) {
+// Sums over the cluster of four values; every CTA gets them, and the CTAs'
+// own in x_sum[turn].  A buffer's next use lies behind the next sum's barrier.
+__device__ __noinline__ void cluster_sum(Smem& sm, int CL, int rank, int turn, u64 (&v)[4]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = warp_sum(v[k]);
-  __syncthreads();
-  if (lane == 0) {
-    sm.warp_a[warp] = v[0];
-    sm.warp_b[warp] = v[1];
-    sm.warp_c[warp] = v[2];
-    sm.found[0] = 0;
+  for (int k = 0; k < 4; ++k) {
+    const u64 x = warp_sum(v[k]);
+    if (lane == 0) sm.warp_v[k][warp] = x;
   }
   __syncthreads();
-  if (lane == 0) atomicAdd(&sm.found[0], v[3]);
-  __syncthreads();
-  if (warp < 3) {
-    const u64* src = warp == 0 ? sm.warp_a : warp == 1 ? sm.warp_b : sm.warp_c;
-    const u64 x = warp_sum(lane < kWarps ? src[lane] : 0);
-    if (lane < CL) {
-      st_rank(&sm.x_sum[warp][rank], lane, x);
-      if (warp == 0) st_rank(&sm.x_sum[3][rank], lane, sm.found[0]);
-    }
+  if (warp < 4) {
+    const u64 x = warp_sum(lane < kWarps ? sm.warp_v[warp][lane] : 0);
+    if (lane < CL) st_rank(&sm.x_sum[turn][warp][rank], lane, x);
   }
   sync_all(CL);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     v[k] = 0;
-    for (int r = 0; r < CL; ++r) v[k] += sm.x_sum[k][r];
+    for (int r = 0; r < CL; ++r) v[k] += sm.x_sum[turn][k][r];
   }
-  sync_all(CL);
 }
 
 // Exclusive scan over the block of (c, q) in thread order.
@@ -483,6 +473,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   constexpr uint32_t kKeyMin = 0x00800000u;  // ordered(-inf) + 1: the lowest key a token can have
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int r = blockIdx.x / CL, rank = blockIdx.x - r * CL;
+  // (no CTA writes to another before that one has begun)
+  if (CL > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   pdl_wait();
   Row<E> row;
   {
@@ -607,6 +599,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, o));
   if (lane == 0) sm.warp_a[warp] = __float_as_uint(mx);
   __syncthreads();
+  if (CL > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
   if (warp == 0) {
     mx = -INFINITY;
     for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, __uint_as_float(static_cast<uint32_t>(sm.warp_a[w])));
@@ -635,6 +628,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   u64 set_mass = 0;     // of the tokens that top_p is a share of (0: not known yet)
   bool have_seg = false;  // the segments' weights (and the kept count) come from pass 2
   u64 kept_count = 0;
+  int turn = 0;         // of cluster_sum
 
   // visits this CTA's elements that the prefix kept so far holds
   auto visit_row = [&](auto&& f) {
@@ -786,7 +780,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     v[1] = q;
     v[2] = ql;
     v[3] = fa.total();
-    cluster_sum(sm, CL, rank, v);
+    cluster_sum(sm, CL, rank, turn ^= 1, v);
   };
 
   // The bracket of a limit, exact sums around it, and the search of the list.
@@ -811,15 +805,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const bool min_p_too = mp > 0.f && (b.all || wt.w(b.x1) >= mp) && (!by_count || p >= 1.f || both);
     // all lists go to rank 0, in the order of the CTAs
     if (CL > 1) {
-      const int own = sm.list_n;
-      if (tid < CL) st_rank(&sm.x_sum[0][rank], tid, static_cast<u64>(own));
-      sync_all(CL);
       int at = 0;
-      for (int c = 0; c < rank; ++c) at += static_cast<int>(sm.x_sum[0][c]);
+      for (int c = 0; c < rank; ++c) at += static_cast<int>(sm.x_sum[turn][0][c] >> 32);
       if (rank > 0)
-        for (int i = tid; i < own; i += kThreads) {
-          st_rank(&sm.list[at + i], 0, sm.list[i]);
-        }
+        for (int i = tid; i < sm.list_n; i += kThreads) st_rank(&sm.list[at + i], 0, sm.list[i]);
       sync_all(CL);
     }
     if (rank == 0) {
@@ -884,7 +873,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     set_mass = sm.x_out[1];
     kept_count = sm.x_out[2];
     have_seg = mp <= 0.f || min_p_too;
-    sync_all(CL);
     return true;
   };
 
@@ -896,7 +884,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       if (set_mass == 0) {
         u64 v[4] = {0, 0, 0, 0};
         visit_row([&](uint32_t, u64 w) { v[0] += w; });
-        cluster_sum(sm, CL, rank, v);
+        cluster_sum(sm, CL, rank, turn ^= 1, v);
         set_mass = v[0];
       }
       target = max(1ull, part_ceil(fmaxf(p, 0.f), set_mass));
@@ -965,7 +953,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const u64 seg = warp_sum(q);
     if (lane == 0) st_rank(&sm.seg[rank * kWarps + warp], 0, seg);
     u64 v[4] = {n, 0, 0, 0};
-    cluster_sum(sm, CL, rank, v);
+    cluster_sum(sm, CL, rank, turn ^= 1, v);
     kept_count = v[0];
   }
 
