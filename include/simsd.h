@@ -500,8 +500,9 @@ SIMSD_API int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, 
  *            kept: the target or draft logits (at temperature 1) of
  *            simsd_accept_sampled for models that sample from truncated
  *            distributions
- * Weights are fp32; their sums are 64-bit fixed point, so they do not depend
- * on the order of summation.  A row without a logit above -inf, or with
+ * Weights are fp32, the sums that decide are 64-bit fixed point over fp32
+ * batches taken in a fixed order, so a call gives the same result every
+ * time.  A row without a logit above -inf, or with
  * parameters outside these ranges (NaN, a negative or infinite temperature,
  * u outside [0, 1)) sets SIMSD_EW_SAMPLE and gets token -1, kept 0 and
  * log-probabilities -inf.

@@ -619,8 +619,7 @@ size_t simsd_chunk_workspace_bytes(int dtype, int T, int Bt, int Hq, int Hkv, in
   if (dtype == SIMSD_F32)
     return simsd::chunk_f32_workspace_bytes(T, Bt, Hq, Hkv, d, static_cast<long long>(max_pages) * page_size,
                                             info.num_sms);
-  return simsd::chunk_tc_workspace_bytes(T, Bt, Hq, Hkv, d, static_cast<long long>(max_pages) * page_size,
-                                         info.num_sms);
+  return simsd::chunk_tc_workspace_bytes(T, Bt, d, info.num_sms);
 }
 
 int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, const int32_t* token_start,
@@ -674,7 +673,7 @@ int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, const int3
   const long long max_keys = static_cast<long long>(max_pages) * page_size;
   const size_t need = dtype == SIMSD_F32
                           ? simsd::chunk_f32_workspace_bytes(T, Bt, Hq, Hkv, d, max_keys, info.num_sms)
-                          : simsd::chunk_tc_workspace_bytes(T, Bt, Hq, Hkv, d, max_keys, info.num_sms);
+                          : simsd::chunk_tc_workspace_bytes(T, Bt, d, info.num_sms);
   if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
     return arg_fail("workspace smaller than simsd_chunk_workspace_bytes()");
   a.workspace = workspace;

@@ -24,13 +24,23 @@
 //
 // Warp roles (384 threads): warps 0-3 softmax of row block A, 4-7 of B
 // (thread i of a block owns query row i = TMEM lane i); warp 8 TMA producer
-// of Q and K, warp 10 of V; warp 9 issues the MMAs; warp 11 walks the run
-// and passes unit by unit to the others through shared memory.
-// The one MMA warp keeps the order PV_A(i) S_A(i+1) PV_B(i) S_B(i+1): S of
-// a block is issued once its PV (whose P lies in the same columns) is done,
-// and while one block's softmax runs, the other's two products fill the
-// tensor pipe.  (With a warp per product the two blocks' MMAs interleave,
-// both blocks wait and compute in step, and a tile takes twice as long.)
+// of Q, K and V; warps 9 and 10 issue the MMAs of block A and of block B;
+// warp 11 walks the run and passes unit by unit to the others through shared
+// memory.  An MMA warp keeps the order PV(i) S(i+1) of its block, S as soon
+// as PV (whose P lies in the same columns) is done; the two warps are not
+// tied to each other and settle in antiphase, one block's products under the
+// other's softmax (about 2530 cycles for a tile of both; made to take turns,
+// 3150).  A softmax warp begins with the probabilities of the first half of
+// the keys before the tile's maximum is known, against the old reference,
+// and starts again where the reference has to move.
+//
+// Bound: the softmax (exponentials, conversions and maxima of 2 x 128 x 128
+// scores: about 2000 of the 2530 cycles, the two products 1024) for prompts,
+// HBM for single tokens.  Measured, 32 heads on 8, d 128: 8192 tokens of one
+// prompt 422 us (1.3 PFLOP/s of the two products, causal), 2048 after 32768
+// 750 us (1.5); 64 single tokens over 2048 to 8192 rows 216 us (6.2 TB/s); 8
+// over 512 to 1024, 16 heads, 21 us, most of it one CTA's chain from the
+// tokens' offsets to its first tile and the second launch.
 // TMEM (512 columns): S_A [0,128), S_B [128,256), O_A [256,384), O_B
 // [384,512); P (bf16) overwrites the first 64 columns of its S.
 // Shared memory: Q of both blocks, a ring of 128-key K tiles and one of V.
@@ -995,7 +1005,8 @@ cudaError_t launch_d(const ChunkArgs& a, int num_sms, EncodeTiledFn encode, cuda
   cudaError_t e = launch_overlapped(chunk_tc_kernel<D>, dim3(static_cast<unsigned>(p.ctas)), dim3(kThreads),
                                     smem_bytes<D>(), stream, 1u, tq, tk, tv, p);
   if (e != cudaSuccess || p.ctas == 1) return e;
-  // units of many rows: 16 blocks to a boundary (two passes over 256 rows)
+  // units of many rows: 16 blocks to a boundary (two passes over 256 rows; the
+  // launch after an 8192-token prompt takes 8 us, with 4 blocks 24)
   const unsigned y = static_cast<long long>(a.T) * p.g > 32ll * a.Bt ? 16u : 2u;
   return launch_overlapped(chunk_merge_kernel<D>, dim3(static_cast<unsigned>(p.ctas - 1), y), dim3(2 * D), 0,
                            stream, 1u, p);
@@ -1003,11 +1014,8 @@ cudaError_t launch_d(const ChunkArgs& a, int num_sms, EncodeTiledFn encode, cuda
 
 }  // namespace
 
-size_t chunk_tc_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, long long max_keys, int num_sms) {
+size_t chunk_tc_workspace_bytes(int T, int Bt, int d, int num_sms) {
   if (T <= 0 || Bt <= 0) return 0;
-  (void)Hq;
-  (void)Hkv;
-  (void)max_keys;
   // two partial pieces per CTA, two row blocks each: O and (m, l) of 128
   // rows; then a record per run boundary
   return static_cast<size_t>(num_sms) * (4ull * kRows * (d + 2) * sizeof(float) + sizeof(Record));

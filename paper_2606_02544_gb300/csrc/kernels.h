@@ -164,7 +164,7 @@ size_t chunk_f32_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, long lon
 cudaError_t launch_chunk_attention_f32(const ChunkArgs& a, int num_sms, cudaStream_t stream);
 // bf16 on the tensor cores; Hq / Hkv <= 128, d 64 or 128, Bt <= kChunkMaxSeqs
 constexpr int kChunkMaxSeqs = 16384;
-size_t chunk_tc_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, long long max_keys, int num_sms);
+size_t chunk_tc_workspace_bytes(int T, int Bt, int d, int num_sms);
 cudaError_t launch_chunk_attention_tc(const ChunkArgs& a, int num_sms, EncodeTiledFn encode, cudaStream_t stream);
 
 // One token from each row of logits (sample.cu).

@@ -143,16 +143,6 @@ __device__ __forceinline__ bool mbar_wait_poll(uint32_t bar, uint32_t parity, vo
   }
 }
 
-// The same for a thread that must react at once: the clock is not read before
-// a thousand polls have failed (reading it delays the next poll).
-__device__ __forceinline__ bool mbar_wait_spin(uint32_t bar, uint32_t parity, volatile int* abort,
-                                               unsigned long long limit_ns = kWaitLimitNs) {
-#pragma unroll 1
-  for (int i = 0; i < 1024; ++i)
-    if (mbar_test_wait(bar, parity)) return true;
-  return mbar_wait_poll(bar, parity, abort, limit_ns);
-}
-
 // Warp-uniform bounded wait: every lane polls, all lanes leave together.
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort,
                                                unsigned long long limit_ns = kWaitLimitNs) {

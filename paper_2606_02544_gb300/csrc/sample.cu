@@ -8,22 +8,27 @@
 // integers in units of 2^-38 of the largest weight (a token whose number hangs
 // on the last bits of a sum of 150,000 weights is still the right one).
 //
-// A row is read twice.  The first pass (from HBM) takes the maximum and, of
-// an eighth of the row, counts and weights over bins 1/32 wide in x / T.
-// From this sample the place of kappa is known within its statistical error;
-// the second pass (from L2) adds up exactly what lies above that bracket and
-// lists the tokens inside it, which tells whether kappa is there (else the
-// row goes on to the searches below), and one CTA searches the list in shared
-// memory.  A bracket with more tokens than the list holds is narrowed by
-// another pass.  What no bracket settles (a bin with more tokens than the
-// list, as at very high temperatures) goes through radix searches over the
-// row.  The random number is placed by the weights of the row's segments (one
-// per warp), and only the segment it falls in is read again.
+// A row is read twice.  The first pass (from HBM) takes the maximum and a
+// histogram over 2048 bins of x / T: counts for top_k, weights to 2^-17 of
+// themselves for top_p.  That names the bin of kappa (a bracket of a few where
+// top_p falls near a bin's edge).  The second pass (the last vectors first,
+// which are still in L2) adds up exactly what lies above the bin and lists
+// the tokens inside it; one CTA sorts the list (bitonic, mostly in registers)
+// and cuts it.  Sums that contradict the histogram, or more tokens in the bin
+// than the list holds (many equal logits), send the row through radix
+// searches.  The random number is placed by the weights of the row's segments
+// (one per warp), and only the segment it falls in is read again.
 //
-// Bound by memory for many rows (HBM once, L2 once) and by the chain of
-// passes and exchanges for few.  Counting an eighth of the row instead of
-// all of it matters: shared-memory atomics run at about 4 tokens a cycle and
-// SM, and HBM delivers 12.
+// Counting all of a row costs one shared-memory reduction a token, which HBM
+// can feed; counts of an eighth of it left brackets of thousands of tokens
+// under heavy-tailed weights and a third pass over the row (1024 rows of
+// 151936: 898 us, this way 321).
+//
+// Measured, 151936 logits of fp32: 1024 rows 321 us (1.94 TB/s of the bytes
+// read once, 3.9 of those read; each pass about 70% of the time in the
+// instructions of a token, 16 and 11, and HBM), 8 rows 24 us (a chain of
+// passes and exchanges over a cluster); 132 rows of 32003 in bf16 with their
+// distribution 52 us.
 //
 // A thread-block cluster serves a row: one CTA where there are many rows,
 // up to eight where there are few.
@@ -242,14 +247,15 @@ struct Row {
         for (int i = 0; i < kUnroll; ++i) q[i] = vector(v + 32 * i);
 #pragma unroll
         for (int i = 0; i < kUnroll; ++i) unpack(q[i], x[i]);
-      } else
+      } else {
 #pragma unroll
-      for (int i = 0; i < kUnroll; ++i) {
-        if (v + 32 * i < b) {
-          load(v + 32 * i, x[i]);
-        } else {
+        for (int i = 0; i < kUnroll; ++i) {
+          if (v + 32 * i < b) {
+            load(v + 32 * i, x[i]);
+          } else {
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) x[i][e] = -INFINITY;
+            for (int e = 0; e < kVec; ++e) x[i][e] = -INFINITY;
+          }
         }
       }
       f(x, v * kVec - lead);
@@ -402,7 +408,7 @@ __device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 tar
 // Sorts n keys, the highest first (n: a power of two, 32 K to 512 K): a
 // bitonic network.  A warp takes strides below 32 K in registers, its lanes
 // holding K keys of a run of 32 K; longer ones go through shared memory.
-// (1024 keys: 14 K cycles with K = 1 and two runs a warp, see the caller.)
+// (132 rows with lists of about 1000 tokens: 53.8 us, with K = 1 throughout 58.7.)
 template <int K>
 __device__ __noinline__ void sort_keys(u64* key, int n) {
   const int lane = threadIdx.x & 31, first = (threadIdx.x >> 5) * 32 * K;
@@ -1086,7 +1092,8 @@ cudaError_t launch_e(const SampleArgs& a, int num_sms, cudaStream_t stream) {
   // Two CTAs fit a SM: as many CTAs a row as fit at once, none for less than
   // 4096 tokens.  (More CTAs for many rows would keep the rows in work within
   // L2 between the passes, but cost more in exchanges than that gains: 1024
-  // rows of 151936 take 0.87 ms with one, 0.95 ms with two, 1.27 ms with four.)
+  // rows of 151936 took 0.87 ms with one, 0.95 with two, 1.27 with four when a
+  // row took three passes.)
   int CL = kMaxCluster;
   while (CL > 1 && (a.R * static_cast<long long>(CL) > 2ll * num_sms || a.V < 4096 * CL)) CL >>= 1;
   return launch_overlapped(sample_kernel<E>, dim3(static_cast<unsigned>(a.R) * CL), dim3(kThreads), sizeof(Smem),
