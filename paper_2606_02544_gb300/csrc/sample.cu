@@ -1092,8 +1092,8 @@ cudaError_t launch_e(const SampleArgs& a, int num_sms, cudaStream_t stream) {
   // Two CTAs fit a SM: as many CTAs a row as fit at once, none for less than
   // 4096 tokens.  (More CTAs for many rows would keep the rows in work within
   // L2 between the passes, but cost more in exchanges than that gains: 1024
-  // rows of 151936 took 0.87 ms with one, 0.95 with two, 1.27 with four when a
-  // row took three passes.)
+  // rows of 151936 take 321 us with one, 380 with two, 537 with four; 400 rows
+  // 165, 169 and 224.)
   int CL = kMaxCluster;
   while (CL > 1 && (a.R * static_cast<long long>(CL) > 2ll * num_sms || a.V < 4096 * CL)) CL >>= 1;
   return launch_overlapped(sample_kernel<E>, dim3(static_cast<unsigned>(a.R) * CL), dim3(kThreads), sizeof(Smem),
