@@ -16,16 +16,19 @@
 // the tokens inside it; one CTA sorts the list (bitonic, mostly in registers)
 // and cuts it.  Sums that contradict the histogram, or more tokens in the bin
 // than the list holds (many equal logits), send the row through radix
-// searches.  The random number is placed by the weights of the row's segments
-// (one per warp), and only the segment it falls in is read again.
+// searches (400 rows of 151936 equal logits: 1.9 ms); a row whose open tokens
+// the sample missed, as nearly all are masked, has its histogram taken once
+// more around the maximum (8 rows with 10 open tokens: 44 us).  The random
+// number is placed by the weights of the row's segments (one per warp), and
+// only the segment it falls in is read again.
 //
 // Counting all of a row costs one shared-memory reduction a token, which HBM
 // can feed; counts of an eighth of it left brackets of thousands of tokens
 // under heavy-tailed weights and a third pass over the row (1024 rows of
-// 151936: 898 us, this way 321).
+// 151936: 898 us, this way 325).
 //
-// Measured, 151936 logits of fp32: 1024 rows 321 us (1.94 TB/s of the bytes
-// read once, 3.9 of those read; each pass about 70% of the time in the
+// Measured, 151936 logits of fp32: 1024 rows 325 us (1.9 TB/s of the bytes
+// read once, 3.8 of those read; each pass about 70% of the time in the
 // instructions of a token, 16 and 11, and HBM), 8 rows 24 us (a chain of
 // passes and exchanges over a cluster); 132 rows of 32003 in bf16 with their
 // distribution 52 us.
@@ -332,7 +335,7 @@ struct Found {
 };
 
 // Search over keys in [lo, hi], a digit of up to 11 bits per round.
-// visit(f) calls f(key, weight units) for the elements of this CTA's part of
+// visit(f) calls f(counts, key, weight units) for the elements of this CTA's part of
 // the row; all CTAs of the cluster get the result.
 template <typename Visit>
 __device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 target, uint32_t lo, uint32_t hi,
@@ -348,11 +351,23 @@ __device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 tar
       sm.mass[i] = 0;
     }
     sync_all(CL);
-    visit([&](uint32_t key, u64 q) {
-      if (key < lo || key > hi) return;
-      const uint32_t bin = (key - lo) >> shift;
-      atomicAdd(&sm.count[bin], 1u);
-      if (q) atomicAdd(&sm.mass[bin], q);
+    // (all lanes call it.  Where they agree on a bin, as many equal tokens do,
+    // one adds for all: a 64-bit sum in shared memory is a loop of exchanges)
+    visit([&](bool real, uint32_t key, u64 q) {
+      const int bin = real && key >= lo && key <= hi ? static_cast<int>((key - lo) >> shift) : -1;
+      const unsigned who = __ballot_sync(kFull, bin >= 0);
+      if (!who) return;
+      const int first = __shfl_sync(kFull, bin, __ffs(who) - 1);
+      if (__all_sync(kFull, bin < 0 || bin == first)) {
+        const u64 sum = warp_sum(bin >= 0 ? q : 0);
+        if ((threadIdx.x & 31) == __ffs(who) - 1) {
+          atomicAdd(&sm.count[bin], static_cast<uint32_t>(__popc(who)));
+          if (sum) atomicAdd(&sm.mass[bin], sum);
+        }
+      } else if (bin >= 0) {
+        atomicAdd(&sm.count[bin], 1u);
+        if (q) atomicAdd(&sm.mass[bin], q);
+      }
     });
     sync_all(CL);
     // thread t: bins 4 t .. 4 t + 3 from the top
@@ -555,52 +570,56 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     // (few tokens say nothing: most are masked)
     if (n >= 32) below = fminf(fmaxf(3.f * d / static_cast<float>(n), 1e-3f), kBelow);
   }
-  // bins per unit of x, their width in x / T
-  const float scale_lo = inv * (kLower / below), scale_hi = inv * ((kBins - kLower) / kAbove);
-  const float width_lo = below / kLower, width_hi = kAbove / (kBins - kLower);
+  // bins per unit of x, their width in x / T; in units of the whole window
+  // (so that one instruction clamps: bin b holds what rounds to b, and a
+  // token's weight is taken against its middle)
+  const float scale_hi = inv * ((kBins - kLower) / kAbove), width_hi = kAbove / (kBins - kLower);
+  const float s_hi = scale_hi / (kBins - 1), c_hi = width_hi * 1.4426950408889634f;
+  float scale_lo, width_lo, s_lo, c_lo;
+  auto lay = [&] {
+    scale_lo = inv * (kLower / below);
+    width_lo = below / kLower;
+    s_lo = scale_lo / (kBins - 1);
+    c_lo = width_lo * 1.4426950408889634f;
+  };
+  lay();
   float mx = -INFINITY;
-  {
-    // in units of the whole window, so that one instruction clamps: bin b holds
-    // what rounds to b, and a token's weight is taken against its middle
-    const float s_lo = scale_lo / (kBins - 1), s_hi = scale_hi / (kBins - 1);
-    const float c_lo = width_lo * 1.4426950408889634f, c_hi = width_hi * 1.4426950408889634f;
-    // the last bits of a sum with 2^23 are an integer (a conversion is four
-    // times as dear): the bin's address is those bits, shifted, and a constant
-    const uint32_t at = smem_u32(sm.hist) - (0x4b000000u << 2);
-    auto count_in = [&](float x, bool count) {
-      const float t = x - base;  // (first: base and x may be large against a bin)
-      const bool upper = t >= 0.f;
-      const float y = __saturatef(fmaf(t, upper ? s_hi : s_lo, static_cast<float>(kLower) / (kBins - 1)));
-      const float f = fmaf(y, static_cast<float>(kBins - 1), 8388608.f);
-      uint32_t q = 1;
-      if (!count) {
-        const float r = fmaf(y, static_cast<float>(kBins - 1), 8388608.f - f);
-        q = __float_as_uint(fmaf(fast_exp2(r * (upper ? c_hi : c_lo)), 65536.f, 8388608.f)) & 0x3ffffu;
-      }
-      // (what lies below the window, as masked tokens do, is left out)
-      asm volatile("{\n\t.reg .pred p;\n\tsetp.gt.f32 p, %2, 0f00000000;\n\t@p red.shared.add.u32 [%0], %1;\n\t}" ::"r"(
-                       at + (__float_as_uint(f) << 2)),
-                   "r"(q), "f"(y)
-                   : "memory");
-    };
-    auto one = [&](auto kind) {
-      row.batches(rank, [&](float (&x)[kUnroll][kVec], int) {
+  // the last bits of a sum with 2^23 are an integer (a conversion is four
+  // times as dear): the bin's address is those bits, shifted, and a constant
+  const uint32_t at = smem_u32(sm.hist) - (0x4b000000u << 2);
+  auto count_in = [&](float x, bool count) {
+    const float t = x - base;  // (first: base and x may be large against a bin)
+    const bool upper = t >= 0.f;
+    const float y = __saturatef(fmaf(t, upper ? s_hi : s_lo, static_cast<float>(kLower) / (kBins - 1)));
+    const float f = fmaf(y, static_cast<float>(kBins - 1), 8388608.f);
+    uint32_t q = 1;
+    if (!count) {
+      const float r = fmaf(y, static_cast<float>(kBins - 1), 8388608.f - f);
+      q = __float_as_uint(fmaf(fast_exp2(r * (upper ? c_hi : c_lo)), 65536.f, 8388608.f)) & 0x3ffffu;
+    }
+    // (what lies below the window, as masked tokens do, is left out)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.gt.f32 p, %2, 0f00000000;\n\t@p red.shared.add.u32 [%0], %1;\n\t}" ::"r"(
+                     at + (__float_as_uint(f) << 2)),
+                 "r"(q), "f"(y)
+                 : "memory");
+  };
+  auto one = [&](auto kind) {
+    row.batches(rank, [&](float (&x)[kUnroll][kVec], int) {
 #pragma unroll
-        for (int i = 0; i < kUnroll; ++i)
+      for (int i = 0; i < kUnroll; ++i)
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) {
-            mx = fmaxf(mx, x[i][e]);
-            if (decltype(kind)::value) count_in(x[i][e], decltype(kind)::value == 1);
-          }
-      });
-    };
-    if (!cut)
-      one(std::integral_constant<int, 0>{});
-    else if (by_count)
-      one(std::integral_constant<int, 1>{});
-    else
-      one(std::integral_constant<int, 2>{});
-  }
+        for (int e = 0; e < kVec; ++e) {
+          mx = fmaxf(mx, x[i][e]);
+          if (decltype(kind)::value) count_in(x[i][e], decltype(kind)::value == 1);
+        }
+    });
+  };
+  if (!cut)
+    one(std::integral_constant<int, 0>{});
+  else if (by_count)
+    one(std::integral_constant<int, 1>{});
+  else
+    one(std::integral_constant<int, 2>{});
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, o));
   if (lane == 0) sm.warp_a[warp] = __float_as_uint(mx);
@@ -644,8 +663,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
           const uint32_t key = ordered(x[i][e]);
-          if (x[i][e] != -INFINITY && kept.in_prefix(key, Row<E>::index(i0, i, e)))
-            f(key, units(wt.w(x[i][e])));
+          const bool in = x[i][e] != -INFINITY && kept.in_prefix(key, Row<E>::index(i0, i, e));
+          f(in, key, in ? units(wt.w(x[i][e])) : 0);
         }
     });
   };
@@ -655,6 +674,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   struct Bracket {
     float x0, x1;  // tokens x0 <= x < x1 are to be listed
     bool all;      // x1 lies above all tokens
+    bool few;      // fewer than top_k tokens have a weight: top_p cuts among them
     bool ok;
   };
   auto edge = [&](int bin) {
@@ -688,7 +708,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     u64 pc, pw;
     block_scan(sm, sc, sw, pc, pw);
     if (tid == kThreads - 1) {
-      sm.found[3] = pw + sw;
+      sm.found[3] = by_count ? pc + sc : pw + sw;
       sm.found[0] = 0;
       sm.pick_lo = sm.pick_hi = -1;
     }
@@ -696,7 +716,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     // kappa's bin is the first by which the target is reached; a weight is
     // known to 2^-16.8, and the bins that this leaves open are listed too
     // (a miss costs the searches over the row, not the result)
-    const u64 all_w = sm.found[3], slack = by_count ? 0 : all_w >> 16;
+    const u64 all_w = sm.found[3], slack = by_count ? 0 : all_w >> 16;  // (top_k: all tokens of the window)
     const u64 goal = by_count ? static_cast<u64>(k) : max(1ull, part_ceil(fmaxf(p, 0.f), all_w));
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -717,8 +737,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     b.all = hi >= 0 && lo >= 0 && sm.found[0] <= (by_count ? kList : kThreads);
     // (never -inf: what counts as -inf lies below every bracket)
     b.x0 = lo >= 0 ? edge(lo) : -FLT_MAX;
+    // (a window of kBelow under the maximum ends where weights do)
+    b.few = by_count && lo < 0 && base == m && below == kBelow && p < 1.f && all_w <= kList;
+    if (b.few) {
+      b.x0 = edge(0);
+      b.all = true;
+    }
     b.x1 = b.all || hi == kBins - 1 ? INFINITY : edge(hi + 1);
-    b.ok = hi >= 0 && (lo >= 0 || !by_count) && b.x0 < b.x1 && scale_lo < 1e30f && m < INFINITY;
+    b.ok = (hi >= 0 || b.few) && (lo >= 0 || b.few || !by_count) && b.x0 < b.x1 && scale_lo < 1e30f && m < INFINITY;
     return b;
   };
 
@@ -801,7 +827,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     if (!by_count) set_mass = v[3];
     {
       // kappa is in the list: less than the target lies above it, and no less with it
-      const u64 target = by_count ? static_cast<u64>(k) : max(1ull, part_ceil(fmaxf(p, 0.f), set_mass));
+      const u64 target = by_count ? static_cast<u64>(b.few ? min(k, total) : k)
+                                  : max(1ull, part_ceil(fmaxf(p, 0.f), set_mass));
       const u64 above = by_count ? above_n : above_q, upto = above + (by_count ? total : v[2]);
       if (total > kList || above >= target || upto < target) return false;
     }
@@ -889,7 +916,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     if (!count) {
       if (set_mass == 0) {
         u64 v[4] = {0, 0, 0, 0};
-        visit_row([&](uint32_t, u64 w) { v[0] += w; });
+        visit_row([&](bool, uint32_t, u64 w) { v[0] += w; });
         cluster_sum(sm, CL, rank, turn ^= 1, v);
         set_mass = v[0];
       }
@@ -909,8 +936,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
               const int idx = Row<E>::index(i0, i, e);
-              if (x[i][e] != -INFINITY && ordered(x[i][e]) == f.key && idx <= kept.last)
-                g(0xffffffffu - static_cast<uint32_t>(idx), 0ull);
+              g(x[i][e] != -INFINITY && ordered(x[i][e]) == f.key && idx <= kept.last,
+                0xffffffffu - static_cast<uint32_t>(idx), 0ull);
             }
         });
       };
@@ -920,12 +947,35 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     }
   };
 
+  // the histogram once more, around the maximum itself
+  auto again = [&] {
+    base = m;
+    below = kBelow;
+    lay();
+    sync_all(CL);  // the first one is read by all
+    for (int i = tid; i < kBins; i += kThreads) sm.hist[i] = 0;
+    __syncthreads();
+    row.batches(rank, [&](float (&x)[kUnroll][kVec], int) {
+#pragma unroll
+      for (int i = 0; i < kUnroll; ++i)
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) count_in(x[i][e], by_count);
+    });
+    sync_all(CL);
+  };
+
   if (cut) {
     bool both = false;
-    if (!by_list(both)) {
+    for (int round = 0; !by_list(both); ++round) {
+      // (nearly all masked, and no open token in the sample)
+      if (round == 0 && m < INFINITY) {
+        again();
+        continue;
+      }
       both = false;
       set_mass = 0;
       by_row(by_count);
+      break;
     }
     if (by_count && p < 1.f && !both) by_row(false);
   }

@@ -218,3 +218,30 @@ def test_all_but_a_few_tokens_masked(dtype, hidden, limits):
     (40001, 2.0, dict(T=0.01, p=0.9))])
 def test_lists_of_every_length(V, spread, limits):
     check(logits(4, V, spread, 26), 27, **{"T": 1.0, **limits}, probs=False)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [5000, 40001])
+@pytest.mark.parametrize("limits", [dict(k=50, p=0.9), dict(k=50, p=0.9, mp=0.3), dict(k=20000, p=0.5), dict(p=0.999)])
+def test_fewer_open_tokens_than_top_k(dtype, V, limits):
+    """Masked tokens fill top_k but have no weight; top_p cuts among the open
+    ones.  One row has a weight just above and one just below nothing."""
+    r = np.random.default_rng(31)
+    x = torch.full((6, V), -1e30)
+    for i, n in enumerate([1, 2, 10, 10, 49, 50]):
+        x[i, torch.as_tensor(r.permutation(V)[:n])] = torch.randn(n, generator=torch.Generator().manual_seed(i))
+    x[2, 11] = float(x[2].max()) - 20.0
+    x[3, 11] = float(x[3].max()) - 60.0
+    check(x.to(dtype).cuda(), 32, T=0.9, probs=False, **limits)
+
+
+def test_equal_logits():
+    """All of a row on one value: kept by index."""
+    V = 151936
+    x = torch.full((3, V), 0.25, device="cuda", dtype=torch.bfloat16)
+    token, kept, lp, _, word = run(x, [0.0, 0.5, 0.999], p=[0.5 + 0.25 / V] * 3, probs=False)
+    # float32 cannot hold the place between two tokens: within its rounding of half the vocabulary
+    assert word == 0 and np.all(np.abs(kept - V / 2) <= 1 + V * 2.0 ** -24)
+    assert token[0] == 0 and abs(token[1] - V / 4) <= 2 and np.allclose(lp, -np.log(kept), atol=1e-5)
+    token, kept, _, _, _ = run(x, [0.0, 0.5, 0.999], k=[1, 70, V - 1], probs=False)
+    assert list(kept) == [1, 70, V - 1] and token[0] == 0 and token[1] == 35
