@@ -33,8 +33,8 @@
 // passes and exchanges over a cluster); 132 rows of 32003 in bf16 with their
 // distribution 52 us.
 //
-// A thread-block cluster serves a row: one CTA where there are many rows,
-// up to eight where there are few.
+// A thread-block cluster serves a row: one CTA where there are many rows (of
+// 256 threads where they are short), up to eight where there are few.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -53,14 +53,15 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
+constexpr int kMaxWarps = 16;    // of a CTA: 512 threads (NT) for few rows, 256 for many
 constexpr int kMaxCluster = 8;
 constexpr int kBatch = 16;         // elements of a lane in flight
 constexpr int kBins = 2048;       // bins of the first pass
 constexpr int kLower = 1536;      // of them below the base, over at most kBelow in x / T ...
 constexpr float kBelow = 48.f, kAbove = 48.f;  // ... the others above it, over kAbove
 constexpr int kList = 4096;       // tokens of the list
+constexpr int kAll = 512;         // a list of no more tokens may hold all of the set
+constexpr int kSmallV = 32768;
 constexpr int kFine = 2048;       // bins of the searches
 constexpr float kUnit = 274877906944.0f;  // 2^38
 constexpr unsigned kFull = 0xffffffffu;
@@ -144,14 +145,16 @@ struct Kept {
   }
 };
 
+template <int NT>
 struct alignas(16) Smem {
+  static constexpr int kWarps = NT / 32;
   union {
     u64 list[kList];  // ordered pattern, then the lower index first
     u64 mass[kFine];  // searches over the row
   };
   uint32_t hist[kBins];  // pass 1: counts, or weights in 2^-16 of their bin's middle
   uint32_t count[kFine];
-  u64 seg[kMaxCluster * kWarps];  // weights of the row's segments (rank 0 holds all)
+  u64 seg[kMaxCluster * kMaxWarps];  // weights of the row's segments (rank 0 holds all)
   u64 warp_a[kWarps], warp_b[kWarps], warp_v[4][kWarps];
   u64 x_max[kMaxCluster];                          // exchanges over the cluster: one slot per CTA
   u64 x_sum[2][4][kMaxCluster];                    // (in turn, so that a sum costs one barrier)
@@ -199,7 +202,7 @@ __device__ __forceinline__ void sync_all(int CL) {
 // -------------------------------------------------------------------- rows
 // The vectors [v0, v1) of a row belong to this CTA, and of those a run to
 // each warp (a segment), so that a warp's elements are consecutive.
-template <typename E>
+template <typename E, int NT>
 struct Row {
   static constexpr int kVec = 16 / sizeof(E), kUnroll = kBatch / kVec;
   const E* base;  // 16-byte aligned; `lead` elements before the row
@@ -276,7 +279,9 @@ __device__ __forceinline__ u64 warp_sum(u64 v) {
 
 // Sums over the cluster of four values; every CTA gets them, and the CTAs'
 // own in x_sum[turn].  A buffer's next use lies behind the next sum's barrier.
-__device__ __noinline__ void cluster_sum(Smem& sm, int CL, int rank, int turn, u64 (&v)[4]) {
+template <int NT>
+__device__ __noinline__ void cluster_sum(Smem<NT>& sm, int CL, int rank, int turn, u64 (&v)[4]) {
+  constexpr int kWarps = NT / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -297,7 +302,8 @@ __device__ __noinline__ void cluster_sum(Smem& sm, int CL, int rank, int turn, u
 }
 
 // Exclusive scan over the block of (c, q) in thread order.
-__device__ __forceinline__ void block_scan(Smem& sm, u64 c, u64 q, u64& pc, u64& pq) {
+template <int NT>
+__device__ __forceinline__ void block_scan(Smem<NT>& sm, u64 c, u64 q, u64& pc, u64& pq) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   u64 ic = c, iq = q;
 #pragma unroll
@@ -320,11 +326,10 @@ __device__ __forceinline__ void block_scan(Smem& sm, u64 c, u64 q, u64& pc, u64&
     ta += __shfl_xor_sync(kFull, ta, o);
     tb += __shfl_xor_sync(kFull, tb, o);
   }
-  // (lanes 16 .. 31 hold nothing: kWarps is 16)
+  // (lanes 16 .. 31 hold nothing)
   pc = ic - c + __shfl_sync(kFull, ta, 0);
   pq = iq - q + __shfl_sync(kFull, tb, 0);
 }
-static_assert(kWarps == 16, "the scan of the warps' totals");
 
 // What a search finds: the key at which the count (or the weight) from the
 // highest key down first reaches the target, what lies above it, and at it.
@@ -337,8 +342,8 @@ struct Found {
 // Search over keys in [lo, hi], a digit of up to 11 bits per round.
 // visit(f) calls f(counts, key, weight units) for the elements of this CTA's part of
 // the row; all CTAs of the cluster get the result.
-template <typename Visit>
-__device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 target, uint32_t lo, uint32_t hi,
+template <int NT, typename Visit>
+__device__ __forceinline__ Found search(Smem<NT>& sm, int CL, bool by_count, u64 target, uint32_t lo, uint32_t hi,
                                         Visit&& visit) {
   Found f{0u, 0, 0, 0, true};
   for (;;) {
@@ -346,7 +351,7 @@ __device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 tar
     const int bits = 32 - __clz(span);  // (clz(0) = 32)
     const int shift = max(0, bits - 11);
     sync_all(CL);
-    for (int i = threadIdx.x; i < kFine; i += kThreads) {
+    for (int i = threadIdx.x; i < kFine; i += NT) {
       sm.count[i] = 0;
       sm.mass[i] = 0;
     }
@@ -370,11 +375,12 @@ __device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 tar
       }
     });
     sync_all(CL);
-    // thread t: bins 4 t .. 4 t + 3 from the top
-    u64 c[4], q[4], sc = 0, sq = 0;
+    // thread t: bins B t .. B t + B - 1 from the top
+    constexpr int B = kFine / NT;
+    u64 c[B], q[B], sc = 0, sq = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int bin = kFine - 1 - (4 * static_cast<int>(threadIdx.x) + e);
+    for (int e = 0; e < B; ++e) {
+      const int bin = kFine - 1 - (B * static_cast<int>(threadIdx.x) + e);
       c[e] = q[e] = 0;
       for (int r = 0; r < CL; ++r) {
         c[e] += ld_rank_u32(&sm.count[bin], r);
@@ -389,10 +395,10 @@ __device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 tar
     pc += f.above_count;
     pq += f.above_mass;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < B; ++e) {
       const u64 before = by_count ? pc : pq, after = by_count ? pc + c[e] : pq + q[e];
       if (before < target && after >= target) {
-        sm.found[0] = kFine - 1 - (4 * threadIdx.x + e);
+        sm.found[0] = kFine - 1 - (B * threadIdx.x + e);
         sm.found[1] = pc;
         sm.found[2] = pq;
         sm.found[3] = c[e];
@@ -424,7 +430,7 @@ __device__ __forceinline__ Found search(Smem& sm, int CL, bool by_count, u64 tar
 // bitonic network.  A warp takes strides below 32 K in registers, its lanes
 // holding K keys of a run of 32 K; longer ones go through shared memory.
 // (132 rows with lists of about 1000 tokens: 53.8 us, with K = 1 throughout 58.7.)
-template <int K>
+template <int K, int NT>
 __device__ __noinline__ void sort_keys(u64* key, int n) {
   const int lane = threadIdx.x & 31, first = (threadIdx.x >> 5) * 32 * K;
   u64 x[K];
@@ -462,7 +468,7 @@ __device__ __noinline__ void sort_keys(u64* key, int n) {
       __syncthreads();
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const int i = threadIdx.x + k * kThreads;
+        const int i = threadIdx.x + k * NT;
         if (i >= n / 2) break;
         const int lo = 2 * i - (i & (stride - 1)), hi = lo + stride;
         const u64 a = key[lo], b = key[hi];
@@ -486,18 +492,19 @@ __device__ __noinline__ void sort_keys(u64* key, int n) {
   __syncthreads();
 }
 
-template <typename E>
-__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ SampleArgs a, const int CL) {
+template <typename E, int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const __grid_constant__ SampleArgs a, const int CL) {
   extern __shared__ uint4 smem_raw[];
-  Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
-  constexpr int kVec = Row<E>::kVec, kUnroll = Row<E>::kUnroll;
+  Smem<NT>& sm = *reinterpret_cast<Smem<NT>*>(smem_raw);
+  constexpr int kWarps = NT / 32;
+  constexpr int kVec = Row<E, NT>::kVec, kUnroll = Row<E, NT>::kUnroll;
   constexpr uint32_t kKeyMin = 0x00800000u;  // ordered(-inf) + 1: the lowest key a token can have
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int r = blockIdx.x / CL, rank = blockIdx.x - r * CL;
   // (no CTA writes to another before that one has begun)
   if (CL > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   pdl_wait();
-  Row<E> row;
+  Row<E, NT> row;
   {
     const E* first = static_cast<const E*>(a.logits) + static_cast<size_t>(r) * static_cast<size_t>(a.row_stride);
     row.lead = static_cast<int>((reinterpret_cast<uintptr_t>(first) & 15u) / sizeof(E));
@@ -529,9 +536,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   const bool by_count = k > 0;
   float base = 0.f, below = kBelow;
   if (cut) {
-    for (int i = tid; i < kBins; i += kThreads) sm.hist[i] = 0;
+    for (int i = tid; i < kBins; i += NT) sm.hist[i] = 0;
     float x[kVec], f = -INFINITY, d = 0.f;
-    row.load(static_cast<int>(static_cast<long long>(tid) * row.vecs / kThreads), x);
+    row.load(static_cast<int>(static_cast<long long>(tid) * row.vecs / NT), x);
 #pragma unroll
     for (int e = 0; e < kVec; ++e) f = fmaxf(f, x[e]);
 #pragma unroll
@@ -643,7 +650,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       if (a.log_prob) a.log_prob[r] = -INFINITY;
     }
     if (a.log_probs)
-      for (int i = rank * kThreads + tid; i < a.V; i += CL * kThreads)
+      for (int i = rank * NT + tid; i < a.V; i += CL * NT)
         a.log_probs[static_cast<size_t>(r) * a.V + i] = -INFINITY;
     sync_all(CL);
     return;
@@ -663,14 +670,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
           const uint32_t key = ordered(x[i][e]);
-          const bool in = x[i][e] != -INFINITY && kept.in_prefix(key, Row<E>::index(i0, i, e));
+          const bool in = x[i][e] != -INFINITY && kept.in_prefix(key, Row<E, NT>::index(i0, i, e));
           f(in, key, in ? units(wt.w(x[i][e])) : 0);
         }
     });
   };
   const uint32_t key_max = ordered(m);
 
-  // ---- the bracket of kappa.  Thread t holds 4 bins from the top.
+  // ---- the bracket of kappa.  Thread t holds B bins from the top.
   struct Bracket {
     float x0, x1;  // tokens x0 <= x < x1 are to be listed
     bool all;      // x1 lies above all tokens
@@ -682,22 +689,29 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     return base + y / (y > 0.f ? scale_hi : scale_lo);
   };
   auto estimate = [&] {
-    uint4 t = make_uint4(0, 0, 0, 0);
-    const int j4 = kBins - 4 - 4 * tid;  // bins j4 .. j4 + 3; entry e is bin j4 + 3 - e
-    {
+    constexpr int B = kBins / NT;        // bins of a thread
+    const int first = kBins - B - B * tid;  // entry e is bin first + B - 1 - e
+    uint32_t h[B] = {};
+#pragma unroll
+    for (int f = 0; f < B / 4; ++f) {
       uint4 x[kMaxCluster];
 #pragma unroll
-      for (int q = 0; q < kMaxCluster; ++q) x[q] = q < CL ? ld_rank_v4(&sm.hist[j4], q) : make_uint4(0, 0, 0, 0);
+      for (int q = 0; q < kMaxCluster; ++q)
+        x[q] = q < CL ? ld_rank_v4(&sm.hist[first + 4 * f], q) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-      for (int q = 0; q < kMaxCluster; ++q) t.x += x[q].x, t.y += x[q].y, t.z += x[q].z, t.w += x[q].w;
+      for (int q = 0; q < kMaxCluster; ++q) {
+        h[B - 1 - 4 * f] += x[q].x;
+        h[B - 2 - 4 * f] += x[q].y;
+        h[B - 3 - 4 * f] += x[q].z;
+        h[B - 4 - 4 * f] += x[q].w;
+      }
     }
-    const uint32_t h[4] = {t.w, t.z, t.y, t.x};
-    u64 c[4], w[4], sc = 0, sw = 0;
+    u64 c[B], w[B], sc = 0, sw = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < B; ++e) {
       // a bin's weight is its sum times that of its middle (kLower's has two halves, and its
       // middle is the base), its count at most the sum times e^(width / 2)
-      const int up = j4 + 3 - e - kLower;
+      const int up = first + B - 1 - e - kLower;
       const float mid = static_cast<float>(up) * (up > 0 ? width_hi : width_lo) - (m - base) * inv;
       const float share = static_cast<float>(h[e]) * (1.f / 65536.f);
       c[e] = by_count ? h[e] : static_cast<u64>(share * 1.1f);
@@ -707,7 +721,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     }
     u64 pc, pw;
     block_scan(sm, sc, sw, pc, pw);
-    if (tid == kThreads - 1) {
+    if (tid == NT - 1) {
       sm.found[3] = by_count ? pc + sc : pw + sw;
       sm.found[0] = 0;
       sm.pick_lo = sm.pick_hi = -1;
@@ -719,13 +733,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const u64 all_w = sm.found[3], slack = by_count ? 0 : all_w >> 16;  // (top_k: all tokens of the window)
     const u64 goal = by_count ? static_cast<u64>(k) : max(1ull, part_ceil(fmaxf(p, 0.f), all_w));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < B; ++e) {
       const u64 before = by_count ? pc : pw, after = by_count ? pc + c[e] : pw + w[e];
       if (before < goal + slack && after >= goal + slack) {
-        sm.pick_lo = j4 + 3 - e;
+        sm.pick_lo = first + B - 1 - e;
         sm.found[0] = pc + c[e];
       }
-      if (before + slack < goal && after + slack >= goal) sm.pick_hi = j4 + 3 - e;
+      if (before + slack < goal && after + slack >= goal) sm.pick_hi = first + B - 1 - e;
       pc += c[e];
       pw += w[e];
     }
@@ -734,7 +748,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const int lo = sm.pick_lo, hi = sm.pick_hi;
     Bracket b;
     // tokens down to the bottom of the bracket: a list of all of them, where it fits
-    b.all = hi >= 0 && lo >= 0 && sm.found[0] <= (by_count ? kList : kThreads);
+    b.all = hi >= 0 && lo >= 0 && sm.found[0] <= (by_count ? kList : kAll);
     // (never -inf: what counts as -inf lies below every bracket)
     b.x0 = lo >= 0 ? edge(lo) : -FLT_MAX;
     // (a window of kBelow under the maximum ends where weights do)
@@ -772,7 +786,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         for (int i = 0; i < kUnroll; ++i)
 #pragma unroll
           for (int e = 0; e < kVec; ++e)
-            if (x[i][e] >= x0) list(x[i][e], Row<E>::index(i0, i, e));
+            if (x[i][e] >= x0) list(x[i][e], Row<E, NT>::index(i0, i, e));
       });
     } else {
       row.template batches<true>(rank, [&](float (&x)[kUnroll][kVec], int i0) {
@@ -793,7 +807,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           if (some) {
 #pragma unroll
             for (int e = 0; e < kVec; ++e)
-              if (x[i][e] >= x0 && x[i][e] < x1) list(x[i][e], Row<E>::index(i0, i, e));
+              if (x[i][e] >= x0 && x[i][e] < x1) list(x[i][e], Row<E, NT>::index(i0, i, e));
           }
         }
         fq.add(s);
@@ -807,7 +821,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     u64 ql = 0;
     const int own = sm.list_n;
     if (!by_count)
-      for (int i = tid; i < min(own, kList); i += kThreads) ql += units(wt.w(key_x(sm.list[i])));
+      for (int i = tid; i < min(own, kList); i += NT) ql += units(wt.w(key_x(sm.list[i])));
     v[0] = n + (tid == 0 ? static_cast<u64>(own) << 32 : 0);
     v[1] = q;
     v[2] = ql;
@@ -841,24 +855,26 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       int at = 0;
       for (int c = 0; c < rank; ++c) at += static_cast<int>(sm.x_sum[turn][0][c] >> 32);
       if (rank > 0)
-        for (int i = tid; i < sm.list_n; i += kThreads) st_rank(&sm.list[at + i], 0, sm.list[i]);
+        for (int i = tid; i < sm.list_n; i += NT) st_rank(&sm.list[at + i], 0, sm.list[i]);
       sync_all(CL);
     }
     if (rank == 0) {
       // the list in order, a run of it to each thread
       int n2 = 32;
       while (n2 < total) n2 <<= 1;
-      for (int i = total + tid; i < n2; i += kThreads) sm.list[i] = 0;
+      for (int i = total + tid; i < n2; i += NT) sm.list[i] = 0;
       // (a warp's run as long as keeps all warps at work)
-      if (n2 <= kThreads)
-        sort_keys<1>(sm.list, n2);
-      else if (n2 == 2 * kThreads)
-        sort_keys<2>(sm.list, n2);
-      else if (n2 == 4 * kThreads)
-        sort_keys<4>(sm.list, n2);
+      if (n2 <= NT)
+        sort_keys<1, NT>(sm.list, n2);
+      else if (n2 == 2 * NT)
+        sort_keys<2, NT>(sm.list, n2);
+      else if (n2 == 4 * NT)
+        sort_keys<4, NT>(sm.list, n2);
+      else if (n2 == 8 * NT)
+        sort_keys<8, NT>(sm.list, n2);
       else
-        sort_keys<8>(sm.list, n2);
-      const int each = max(1, n2 / kThreads), i0 = tid * each, i1 = min(total, i0 + each);
+        sort_keys<kList / NT, NT>(sm.list, n2);
+      const int each = max(1, n2 / NT), i0 = tid * each, i1 = min(total, i0 + each);
       const int limit = by_count ? min(static_cast<int>(static_cast<u64>(k) - above_n), total) : total;
       u64 own = 0, in_limit = 0, before, rest;
       for (int i = i0; i < i1; ++i) {
@@ -867,7 +883,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         in_limit += i < limit ? q : 0;
       }
       block_scan(sm, own, in_limit, before, rest);
-      if (tid == kThreads - 1) {
+      if (tid == NT - 1) {
         sm.found[4] = rest + in_limit;
         sm.pick_lo = -1;
       }
@@ -935,7 +951,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           for (int i = 0; i < kUnroll; ++i)
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
-              const int idx = Row<E>::index(i0, i, e);
+              const int idx = Row<E, NT>::index(i0, i, e);
               g(x[i][e] != -INFINITY && ordered(x[i][e]) == f.key && idx <= kept.last,
                 0xffffffffu - static_cast<uint32_t>(idx), 0ull);
             }
@@ -953,7 +969,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     below = kBelow;
     lay();
     sync_all(CL);  // the first one is read by all
-    for (int i = tid; i < kBins; i += kThreads) sm.hist[i] = 0;
+    for (int i = tid; i < kBins; i += NT) sm.hist[i] = 0;
     __syncthreads();
     row.batches(rank, [&](float (&x)[kUnroll][kVec], int) {
 #pragma unroll
@@ -999,7 +1015,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         for (int e = 0; e < kVec; ++e) {
           const float w = wt.w(x[i][e]);
           const bool in = x[i][e] != -INFINITY && w >= mp &&
-                          kept.in_prefix(ordered(x[i][e]), Row<E>::index(i0, i, e));
+                          kept.in_prefix(ordered(x[i][e]), Row<E, NT>::index(i0, i, e));
           s.add(in ? w : 0.f);
           cnt += in ? 1 : 0;
         }
@@ -1051,7 +1067,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     __syncthreads();
     const int sr = s / kWarps, sw = s - sr * kWarps;
     const int va = row.seg_begin(sr, sw), vb = min(row.seg_begin(sr, sw + 1), min(row.vecs, sr * row.per + row.per));
-    for (int v0 = va; v0 < vb; v0 += kThreads) {
+    for (int v0 = va; v0 < vb; v0 += NT) {
       const int v = v0 + tid;
       float x[kVec];
       u64 own = 0, q[kVec];
@@ -1102,16 +1118,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     float* out = a.log_probs + static_cast<size_t>(r) * a.V;
     // (element by element: rows of the result need not begin at a vector)
     const E* from = row.base + row.lead;
-    for (int i0 = rank * kThreads + tid; i0 < a.V; i0 += kBatch * CL * kThreads) {
+    for (int i0 = rank * NT + tid; i0 < a.V; i0 += kBatch * CL * NT) {
       float x[kBatch];
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const int idx = i0 + j * CL * kThreads;
+        const int idx = i0 + j * CL * NT;
         x[j] = idx < a.V ? fmaxf(static_cast<float>(from[idx]), -INFINITY) : -INFINITY;
       }
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const int idx = i0 + j * CL * kThreads;
+        const int idx = i0 + j * CL * NT;
         const float z = wt.z(x[j]);
         const bool in = x[j] != -INFINITY && kept.in_prefix(ordered(x[j]), idx) && (mp <= 0.f || expf(z) >= mp);
         if (idx < a.V) out[idx] = in ? z - logz : -INFINITY;
@@ -1122,8 +1138,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   sync_all(CL);  // no CTA leaves while another may write to its shared memory
 }
 
-template <typename E>
-cudaError_t launch_e(const SampleArgs& a, int num_sms, cudaStream_t stream) {
+template <typename E, int NT>
+cudaError_t launch_nt(const SampleArgs& a, int CL, cudaStream_t stream) {
   {
     static std::mutex mu;
     static bool done[64] = {};
@@ -1133,12 +1149,23 @@ cudaError_t launch_e(const SampleArgs& a, int num_sms, cudaStream_t stream) {
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     std::lock_guard<std::mutex> lk(mu);
     if (!done[dev]) {
-      e = cudaFuncSetAttribute(sample_kernel<E>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                               static_cast<int>(sizeof(Smem)));
+      e = cudaFuncSetAttribute(sample_kernel<E, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               static_cast<int>(sizeof(Smem<NT>)));
       if (e != cudaSuccess) return e;
       done[dev] = true;
     }
   }
+  return launch_overlapped(sample_kernel<E, NT>, dim3(static_cast<unsigned>(a.R) * CL), dim3(NT), sizeof(Smem<NT>),
+                           stream, static_cast<unsigned>(CL), a, CL);
+}
+
+template <typename E>
+cudaError_t launch_e(const SampleArgs& a, int num_sms, cudaStream_t stream) {
+  // Short rows that are more than two CTAs a SM: their time is the chain of
+  // steps of a row, of which four CTAs of 256 threads overlap more (1783 rows
+  // of 1066: 81 us, with 512 threads 132; 2000 of 32003: 204, 230; but 610 of
+  // 65536: 118, 113; 1024 of 151936: 356, 330, as fewer rows stay in L2).
+  if (a.R > 2ll * num_sms && a.V <= kSmallV) return launch_nt<E, 256>(a, 1, stream);
   // Two CTAs fit a SM: as many CTAs a row as fit at once, none for less than
   // 4096 tokens.  (More CTAs for many rows would keep the rows in work within
   // L2 between the passes, but cost more in exchanges than that gains: 1024
@@ -1146,8 +1173,7 @@ cudaError_t launch_e(const SampleArgs& a, int num_sms, cudaStream_t stream) {
   // 165, 169 and 224.)
   int CL = kMaxCluster;
   while (CL > 1 && (a.R * static_cast<long long>(CL) > 2ll * num_sms || a.V < 4096 * CL)) CL >>= 1;
-  return launch_overlapped(sample_kernel<E>, dim3(static_cast<unsigned>(a.R) * CL), dim3(kThreads), sizeof(Smem),
-                           stream, static_cast<unsigned>(CL), a, CL);
+  return launch_nt<E, 512>(a, CL, stream);
 }
 
 }  // namespace

@@ -245,3 +245,11 @@ def test_equal_logits():
     assert token[0] == 0 and abs(token[1] - V / 4) <= 2 and np.allclose(lp, -np.log(kept), atol=1e-5)
     token, kept, _, _, _ = run(x, [0.0, 0.5, 0.999], k=[1, 70, V - 1], probs=False)
     assert list(kept) == [1, 70, V - 1] and token[0] == 0 and token[1] == 35
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,limits", [(1066, dict(k=79, p=0.95)), (1066, dict(p=0.9, mp=0.05)), (9000, dict(k=3000, p=0.99)),
+                                      (9000, dict(p=0.999)), (9000, dict(T=50.0, p=0.7)), (9000, dict(k=7000))])
+def test_many_short_rows(dtype, V, limits):
+    """More short rows than two to a SM: smaller blocks, longer runs of the sort."""
+    check(logits(400, V, 1.5, V, dtype), 33, **{"T": 0.9, **limits}, probs=V < 2000)
