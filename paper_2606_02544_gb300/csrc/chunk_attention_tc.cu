@@ -100,8 +100,9 @@ template <int D>
 struct alignas(1024) SmemChunk {
   static constexpr int kHalves = D / 64;
   static constexpr int kTileBytes = kHalves * kHalfBytes;  // one K or V tile
-  // K and V have rings of their own: whoever waits on a slot's barrier waits
-  // for every use of it in turn, so a parity is never read a phase early
+  // K and V have rings of their own: the producer and the MMA warps wait for
+  // every use of a slot in turn, so they never read a parity a phase early (the
+  // softmax warps wait for V only where they zero rows, and after the tile's S)
   static constexpr int kStagesK = D == 128 ? 3 : 5, kStagesV = D == 128 ? 2 : 5;
   static constexpr int kStages = kStagesK + kStagesV;
   uint8_t ring[kStages][kTileBytes];  // K, then V
@@ -699,9 +700,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (u.tiles > 0 && has) {
         for (int i = 0; i < u.tiles; ++i, ++c) {
           const int key0 = (u.t0 + i) * kTile;
-          // rows of V outside the unit's keys may hold anything: zeroed, so
+          if (!mbar_wait_warp(smem_u32(&sm.bar_s[x]), c & 1, abort_flag)) {
+            ok = false;
+            break;
+          }
+          // Rows of V outside the unit's keys may hold anything: zeroed, so
           // that 0 * NaN cannot reach O.  Both blocks write the same zeros,
-          // so each block's PV sees them.
+          // so each block's PV sees them.  Not before S of the tile: block
+          // B's warps skip units that have no block B without a wait, and
+          // then lag behind the ring by many uses of a slot, which a parity
+          // does not tell apart.  The block's MMA warp, which has waited for
+          // every use of V in turn, issues this S after the last one before
+          // this tile's, so from here the parity names one use.
           if (key0 < u.lo || key0 + kTile > u.hi) {
             const uint32_t gt = g + i, vst = kStagesK + gt % kStagesV;  // the tile's V slot
             if (!mbar_wait_warp(smem_u32(&sm.bar_full[vst]), (gt / kStagesV) & 1, abort_flag)) {
@@ -718,10 +728,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
             }
             fence_proxy_async_smem();
-          }
-          if (!mbar_wait_warp(smem_u32(&sm.bar_s[x]), c & 1, abort_flag)) {
-            ok = false;
-            break;
           }
           if (!work) {
             __syncwarp();

@@ -263,3 +263,23 @@ def test_few_rows_over_long_caches(dtype, d, Hq, Hkv):
 def test_many_heads_and_long_chunks(dtype):
     """So many query rows that the fp32 kernel takes them 128 at a time."""
     check(make(dtype, [300, 130, 40], [100, 0, 333], 64, 64, 64, 32, 14), mask_block=4)
+
+
+# (chunk, prefix, Hq, Hkv, key_start, mask arguments): so many key tiles a SM that a CTA's run holds several units,
+# a unit of one row block (few tokens, many keys) before one of two blocks whose first tile is seen in part
+RUNS = {
+    "single tokens before fresh chunks": ([1, 100] * 6, [600, 0, 333, 0, 1900, 0, 1000, 0, 256, 0, 1290, 27], 128, 64,
+                                          None, {}),
+    "short chunks before windows and hidden keys": (
+        [3, 90, 1, 70, 5, 127, 2, 66], [1500, 333, 700, 50, 1100, 900, 2000, 0], 96, 48,
+        [77, 0, 0, 51, 300, 901, 1000, 3], dict(window=200, mask_block=4)),
+    "prompts that end in a short unit": ([1096, 8, 200], [0, 1000, 0], 64, 16, None, {}),
+    "prompts that end in a short unit, unmasked": ([70, 520], [700, 24], 32, 8, [0, 100], dict(mask_block=0)),
+}
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("case", list(RUNS))
+def test_runs_of_several_units(case, d):
+    chunk, prefix, Hq, Hkv, key_start, mask = RUNS[case]
+    check(make(torch.bfloat16, chunk, prefix, Hq, Hkv, d, 16, 17, key_start=key_start), **mask)
