@@ -812,6 +812,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           const float mx = row_max();
           const bool move = seen && mx != -INFINITY && (m_ref == -INFINITY || mx > m_ref + kRescaleThreshold);
           if (__any_sync(0xffffffffu, move)) {
+            // the first stores of the half are complete before those that
+            // replace them are issued (stores to TMEM are asynchronous, and
+            // only a wait orders two of them)
+            tmem_wait_st();
             // O holds the piece's earlier tiles, all complete (S of this tile
             // was issued after the PV before it had finished)
             const float f = move && m_ref != -INFINITY ? fast_exp2(m_ref - mx) : 1.0f;

@@ -283,3 +283,21 @@ RUNS = {
 def test_runs_of_several_units(case, d):
     chunk, prefix, Hq, Hkv, key_start, mask = RUNS[case]
     check(make(torch.bfloat16, chunk, prefix, Hq, Hkv, d, 16, 17, key_start=key_start), **mask)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_reference_moves_in_some_rows_of_every_tile(d):
+    """Each tile of keys holds a few that lie far above all before them for
+    some of the rows: the first half of the probabilities is stored against
+    the old reference, then again against the new one."""
+    a = make(torch.bfloat16, [150, 60], [900, 0], 8, 4, d, 64, 18)
+    P, scale = 64, 0.5
+    k = a["k_cache"].cpu()
+    q = a["q"].cpu()
+    for b, (n, C, s) in enumerate([(900, 150, 0), (0, 60, 150)]):
+        for j in range(5, n + C, 37):
+            page = a["block_table"][b].cpu()[j // P].long()
+            # along the query of one token: its score grows from tile to tile
+            k[page, :, j % P] = (q[s + (7 * j) % C, ::2].float() * (0.2 + 0.8 * j / 1050)).to(torch.bfloat16)
+    a["k_cache"] = k.cuda()
+    check(a, softmax_scale=scale, mask_block=16)
