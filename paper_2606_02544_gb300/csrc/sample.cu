@@ -52,6 +52,7 @@ namespace simsd {
 namespace {
 
 typedef unsigned long long u64;
+typedef unsigned __int128 u128;
 
 constexpr int kMaxWarps = 16;    // of a CTA: 512 threads (NT) for few rows, 256 for many
 constexpr int kMaxCluster = 8;
@@ -63,6 +64,7 @@ constexpr int kList = 4096;       // tokens of the list
 constexpr int kAll = 512;         // a list of no more tokens may hold all of the set
 constexpr int kSmallV = 32768;
 constexpr int kFine = 2048;       // bins of the searches
+constexpr int kUnitBits = 38;
 constexpr float kUnit = 274877906944.0f;  // 2^38
 constexpr unsigned kFull = 0xffffffffu;
 
@@ -85,9 +87,6 @@ struct BatchSum {
     hi = __fadd_rn(hi, h);
     lo = __fadd_rn(lo, __fsub_rn(w, h));
   }
-  __device__ __forceinline__ u64 total() const {
-    return static_cast<u64>(__float2ll_rn(hi * kUnit) + __float2ll_rn(lo * kUnit));
-  }
 };
 
 // A running sum of such batches' fp32 sums with its rounding errors (two-sum).
@@ -103,9 +102,38 @@ struct LongSum {
   }
 };
 
-// The part f of a sum, f in [0, 1): floor and ceiling.
+// What the random number is placed by: units of 2^-88, so that tokens far
+// below the largest keep their share (a row may be one token of weight 1 and
+// 150,000 of 2^-40: the first 2^-24 of the random numbers fall on those), as
+// whole units of 2^-38 and the rest where they are added up apart.
+constexpr int kFineBits = 50;
+struct Parts {
+  u64 coarse, fine;
+};
+__device__ __forceinline__ Parts parts(float w) {
+  const float t = w * kUnit, f = floorf(t);
+  return Parts{__float2ull_rz(f), __float2ull_rn((t - f) * 1125899906842624.0f)};
+}
+// (added up modulo 2^64, the rests as signed numbers: they may have come out negative)
+__device__ __forceinline__ Parts parts(const LongSum& s) {
+  const Parts h = parts(s.hi), l = parts(fabsf(s.lo));
+  return s.lo < 0.f ? Parts{h.coarse - l.coarse, h.fine - l.fine} : Parts{h.coarse + l.coarse, h.fine + l.fine};
+}
+__device__ __forceinline__ u128 join(u64 coarse, u64 fine) {
+  return (static_cast<u128>(coarse) << kFineBits) + static_cast<u128>(static_cast<__int128>(static_cast<long long>(fine)));
+}
+// The floor of a sum's part f, f in [0, 1), exact: the 24 bits of f times the
+// sum, which is below 2^112, shifted by the exponent.
+__device__ __forceinline__ u128 part_floor(float f, u128 sum) {
+  const uint32_t b = __float_as_uint(f) & 0x7fffffffu;  // (-0 is in range)
+  const int shift = b >> 23 ? 150 - static_cast<int>(b >> 23) : 149;  // 24 .. 149
+  const uint32_t m = (b & 0x7fffffu) | (b >> 23 ? 0x800000u : 0u);
+  const u128 low = static_cast<u128>(static_cast<u64>(sum)) * m, high = static_cast<u128>(static_cast<u64>(sum >> 64)) * m;
+  return shift < 64 ? (high << (64 - shift)) + (low >> shift) : (high + (low >> 64)) >> (shift - 64);
+}
+
+// The part f of a sum in units of 2^-38, f in [0, 1): ceiling.
 __device__ __forceinline__ u64 fraction(float f) { return __float2ull_rz(f * 18446744073709551616.0f); }
-__device__ __forceinline__ u64 part_floor(float f, u64 sum) { return __umul64hi(sum, fraction(f)); }
 __device__ __forceinline__ u64 part_ceil(float f, u64 sum) {
   const u64 q = fraction(f);
   return __umul64hi(sum, q) + (sum * q ? 1 : 0);
@@ -154,7 +182,8 @@ struct alignas(16) Smem {
   };
   uint32_t hist[kBins];  // pass 1: counts, or weights in 2^-16 of their bin's middle
   uint32_t count[kFine];
-  u64 seg[kMaxCluster * kMaxWarps];  // weights of the row's segments (rank 0 holds all)
+  u64 seg[kMaxCluster * kMaxWarps];  // weights of the row's segments (rank 0 holds all): units of 2^-38 ...
+  u64 seg_fine[kMaxCluster * kMaxWarps];  // ... and of 2^-88
   u64 warp_a[kWarps], warp_b[kWarps], warp_v[4][kWarps];
   u64 x_max[kMaxCluster];                          // exchanges over the cluster: one slot per CTA
   u64 x_sum[2][4][kMaxCluster];                    // (in turn, so that a sum costs one barrier)
@@ -275,6 +304,18 @@ __device__ __forceinline__ u64 warp_sum(u64 v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
   return v;
+}
+
+// A segment's weight, from its warp's lanes to rank 0.
+template <int NT>
+__device__ __forceinline__ void put_segment(Smem<NT>& sm, int rank, const LongSum& own) {
+  const Parts p = parts(own);
+  const u64 coarse = warp_sum(p.coarse), fine = warp_sum(p.fine);
+  if ((threadIdx.x & 31) == 0) {
+    const int i = rank * (NT / 32) + (threadIdx.x >> 5);
+    st_rank(&sm.seg[i], 0, coarse);
+    st_rank(&sm.seg_fine[i], 0, fine);
+  }
 }
 
 // Sums over the cluster of four values; every CTA gets them, and the CTAs'
@@ -815,8 +856,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const __grid_cons
       });
     }
     const u64 q = fq.total();
-    const u64 seg = warp_sum(q);
-    if (lane == 0) st_rank(&sm.seg[rank * kWarps + warp], 0, seg);
+    put_segment(sm, rank, fq);
     __syncthreads();
     u64 ql = 0;
     const int own = sm.list_n;
@@ -904,7 +944,14 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const __grid_cons
         before += q;
         mine = i;
         const int v2 = (static_cast<int>(~static_cast<uint32_t>(sm.list[i])) + row.lead) / kVec, c = v2 / row.per;
-        atomicAdd(&sm.seg[c * kWarps + (v2 - c * row.per) / row.per_warp], q);
+        const int seg = c * kWarps + (v2 - c * row.per) / row.per_warp;
+        if (w >= 0x1p-15f) {
+          atomicAdd(&sm.seg[seg], q);  // (a whole number of units)
+        } else {
+          const Parts f = parts(w);
+          atomicAdd(&sm.seg[seg], f.coarse);
+          atomicAdd(&sm.seg_fine[seg], f.fine);
+        }
       }
       if (mine >= 0) atomicMax(&sm.pick_lo, mine);
       __syncthreads();
@@ -998,7 +1045,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const __grid_cons
 
   // ---- the segments' weights, where pass 2 has not left them or min_p cuts
   if (!have_seg) {
-    u64 n = 0, q = 0;
+    u64 n = 0;
+    LongSum sum;
     const float least = from_ordered(kept.kappa);
     row.batches(rank, [&](float (&x)[kUnroll][kVec], int i0) {
       float any = -INFINITY;
@@ -1020,10 +1068,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const __grid_cons
           cnt += in ? 1 : 0;
         }
       n += cnt;
-      q += s.total();
+      sum.add(s.hi);
+      sum.add(s.lo);
     });
-    const u64 seg = warp_sum(q);
-    if (lane == 0) st_rank(&sm.seg[rank * kWarps + warp], 0, seg);
+    put_segment(sm, rank, sum);
     u64 v[4] = {n, 0, 0, 0};
     cluster_sum(sm, CL, rank, turn ^= 1, v);
     kept_count = v[0];
@@ -1031,83 +1079,114 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const __grid_cons
 
   // ---- rank 0 places the random number
   if (rank == 0) {
-    // every warp for itself: lane i sums segments 4 i .. 4 i + 3
-    u64 four[4], own4 = 0;
+    if (warp == 0) {
+      // lane i: segments 4 i .. 4 i + 3
+      u128 four[4], own4 = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      four[e] = 4 * lane + e < CL * kWarps ? sm.seg[4 * lane + e] : 0;
-      own4 += four[e];
-    }
-    u64 inc = own4;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const u64 y = __shfl_up_sync(kFull, inc, o);
-      if (lane >= o) inc += y;
-    }
-    const u64 all = __shfl_sync(kFull, inc, 31);
-    const float logz = log_units(all);
-    const u64 thr = part_floor(u, all);
-    const int who = __ffs(__ballot_sync(kFull, inc > thr)) - 1;  // (thr < all)
-    u64 at = inc - own4;
-    int s = 4 * lane;
-#pragma unroll
-    for (int e = 0; e < 3; ++e)
-      if (s == 4 * lane + e && thr >= at + four[e]) {
-        at += four[e];
-        ++s;
+      for (int e = 0; e < 4; ++e) {
+        four[e] = 4 * lane + e < CL * kWarps ? join(sm.seg[4 * lane + e], sm.seg_fine[4 * lane + e]) : 0;
+        own4 += four[e];
       }
-    at = __shfl_sync(kFull, at, who);
-    s = __shfl_sync(kFull, s, who);
-    if (tid == 0) {
-      sm.token = -1;
-      sm.pick_lo = -1;
-      if (a.kept) a.kept[r] = static_cast<int>(kept_count);
-      for (int c = 0; c < CL; ++c) st_rank(&sm.x_out[3], c, static_cast<u64>(__float_as_uint(logz)));
+      u128 inc = own4;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const u64 yl = __shfl_up_sync(kFull, static_cast<u64>(inc), o);
+        const u64 yh = __shfl_up_sync(kFull, static_cast<u64>(inc >> 64), o);
+        if (lane >= o) inc += static_cast<u128>(yh) << 64 | yl;
+      }
+      const u128 all = static_cast<u128>(__shfl_sync(kFull, static_cast<u64>(inc >> 64), 31)) << 64 |
+                       __shfl_sync(kFull, static_cast<u64>(inc), 31);
+      const float logz = log_units(static_cast<u64>(all >> kFineBits));
+      if (lane < CL) st_rank(&sm.x_out[3], lane, static_cast<u64>(__float_as_uint(logz)));
+      const u128 thr = part_floor(u, all);
+      if (lane == __ffs(__ballot_sync(kFull, inc > thr)) - 1) {  // (thr < all)
+        u128 rem = thr - (inc - own4), sum = four[0];
+        int s = 0;
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          if (s == e && rem >= four[e]) {
+            rem -= four[e];
+            sum = four[e + 1];
+            ++s;
+          }
+        // within the segment: units in which its sum has 62 bits
+        const u64 top = static_cast<u64>(sum >> 62);
+        const int drop = top ? 64 - __clzll(static_cast<long long>(top)) : 0;
+        sm.found[0] = thr == 0 ? ~0ull : static_cast<u64>(4 * lane + s);
+        sm.found[1] = static_cast<u64>(rem >> drop);
+        sm.found[2] = static_cast<u64>(drop);
+        sm.token = sm.pick_lo = -1;
+        sm.pick_hi = 0x7fffffff;
+        if (a.kept) a.kept[r] = static_cast<int>(kept_count);
+      }
     }
     __syncthreads();
+    const bool nought = sm.found[0] == ~0ull;  // below the smallest unit
+    const int s = nought ? 0 : static_cast<int>(sm.found[0]);
+    u64 left = sm.found[1];  // of the number, in the segment
+    const float unit = exp2f(static_cast<float>(kUnitBits + kFineBits - static_cast<int>(sm.found[2])));
+    const float logz = __uint_as_float(static_cast<uint32_t>(sm.x_out[3]));
+    // a token's weight among the kept
+    auto kept_weight = [&](float x, int idx) {
+      const float w = wt.w(x);
+      return x != -INFINITY && w >= mp && kept.in_prefix(ordered(x), idx) ? w : 0.f;
+    };
     const int sr = s / kWarps, sw = s - sr * kWarps;
     const int va = row.seg_begin(sr, sw), vb = min(row.seg_begin(sr, sw + 1), min(row.vecs, sr * row.per + row.per));
-    for (int v0 = va; v0 < vb; v0 += NT) {
+    for (int v0 = va; !nought && v0 < vb; v0 += NT) {
       const int v = v0 + tid;
       float x[kVec];
-      u64 own = 0, q[kVec];
+      u64 own = 0;
       int last = -1;
-      if (v < vb) row.load(v, x);
+      if (v < vb) {
+        row.load(v, x);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        q[e] = 0;
-        const int idx = v * kVec - row.lead + e;
-        if (v < vb && x[e] != -INFINITY && kept.in_prefix(ordered(x[e]), idx)) {
-          const float w = wt.w(x[e]);
-          if (w >= mp) {
-            q[e] = units(w);
-            if (q[e]) last = idx;
-          }
+        for (int e = 0; e < kVec; ++e) {
+          const int idx = v * kVec - row.lead + e;
+          x[e] = kept_weight(x[e], idx);
+          if (x[e] > 0.f) last = idx;
+          own += __float2ull_rn(x[e] * unit);
         }
-        own += q[e];
       }
       if (last >= 0) atomicMax(&sm.pick_lo, last);  // the last kept token of the segment
       u64 before, none;
       block_scan(sm, own, 0, before, none);
-      before += at;
-      if (own && thr >= before && thr < before + own) {
+      if (left >= before && left - before < own) {
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-          if (q[e] && thr >= before && thr < before + q[e]) sm.token = v * kVec - row.lead + e;
-          before += q[e];
+          const u64 q = __float2ull_rn(x[e] * unit);
+          if (left >= before && left - before < q) sm.token = v * kVec - row.lead + e;
+          before += q;
         }
       }
       __syncthreads();
       if (sm.token >= 0) break;
-      // the sum so far, from the warps' totals of the scan
-      u64 t = lane < kWarps ? sm.warp_a[lane] : 0;
-      t = warp_sum(t);
-      at += t;
+      // what is left of the number, from the warps' totals of the scan
+      left -= warp_sum(lane < kWarps ? sm.warp_a[lane] : 0);
     }
-    __syncthreads();
+    // rounding of the segment's sum may leave the number just past its last token
+    int tok = sm.token >= 0 ? sm.token : sm.pick_lo;
+    if (tok < 0) {
+      // Zero (or what is below the smallest unit) falls on the first kept token
+      // that has a weight at all; the row's maximum has one.
+      for (int v0 = 0; v0 < row.vecs; v0 += NT) {
+        const int v = v0 + tid;
+        int first = -1;
+        if (v < row.vecs) {
+          float x[kVec];
+          row.load(v, x);
+#pragma unroll
+          for (int e = kVec - 1; e >= 0; --e) {
+            const int idx = v * kVec - row.lead + e;
+            if (kept_weight(x[e], idx) > 0.f) first = idx;
+          }
+        }
+        if (first >= 0) atomicMin(&sm.pick_hi, first);
+        if (__syncthreads_or(first >= 0)) break;
+      }
+      tok = sm.pick_hi;
+    }
     if (tid == 0) {
-      // rounding of the segment's sum may leave the number just past its last token
-      const int tok = sm.token >= 0 ? sm.token : sm.pick_lo;
       a.token[r] = tok;
       if (a.log_prob) a.log_prob[r] = wt.z(static_cast<float>(row.base[row.lead + tok])) - logz;
     }

@@ -253,3 +253,76 @@ def test_equal_logits():
 def test_many_short_rows(dtype, V, limits):
     """More short rows than two to a SM: smaller blocks, longer runs of the sort."""
     check(logits(400, V, 1.5, V, dtype), 33, **{"T": 0.9, **limits}, probs=V < 2000)
+
+
+def between(x, us, T=1.0, k=0, mp=0.0):
+    """For each u the first and the last token that it may fall on, and the
+    number kept: cumulative weights in whole numbers of 2^-120 (a sum in
+    doubles loses 2^-53 beside 1 with every token), all weights but the
+    largest, which is exactly 1, within 2^-20 of themselves.  That covers the
+    kernel's: z is exact in these tests, expf good to 2^-22, a sum of 16
+    weights to 16 2^-24 / 2."""
+    _, idx, _ = ref.sample_row(x, 0.5, T, k, 1.0, mp)
+    by = np.sort(idx)
+    w = np.exp((x[by] - x[by].max()) / T)
+    top = x[by] == x[by].max()
+    at = []
+    for f in ((1 << 20) - 1, (1 << 20) + 1):
+        c = np.cumsum(np.array([(1 << 120) if t else (int(v * 2.0 ** 100) << 20) * f >> 20 for v, t in zip(w, top)],
+                               dtype=object))
+        j = [int(np.searchsorted(c, int(float(u) * 2.0 ** 149) * c[-1] >> 149, side="right")) for u in us]
+        at.append([int(by[min(i, len(by) - 1)]) for i in j])
+    return np.minimum(*at), np.maximum(*at), len(idx)
+
+
+ENDS = [0.0, 1e-45, 2.0 ** -24, 3 * 2.0 ** -24, 0.5, 1 - 2.0 ** -23, 1 - 2.0 ** -24]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,rows", [(4096, 7), (1201, 400), (151936, 7)])
+@pytest.mark.parametrize("limits", [dict(), dict(k=1000), dict(k=100000), dict(mp=1e-30), dict(p=1 - 2.0 ** -24)])
+def test_random_numbers_at_the_ends(dtype, V, rows, limits):
+    """One token far above equal others, which together hold what the first
+    or the last 2^-24 of the random numbers fall on: a token is drawn from
+    them, by index, however small one of them is against the largest."""
+    for gap in (26.5, 27.5, 28.5, 29.5, 31.0):
+        for at in (0, V // 3, V - 1):
+            x = torch.zeros(rows, V)
+            x[:, at] = gap
+            u = np.resize(np.asarray(ENDS, dtype=np.float32), rows)
+            full = lambda v: None if v is None else [v] * rows  # noqa: E731
+            token, kept, lp, _, word = run(x.to(dtype).cuda(), u, k=full(limits.get("k")), p=full(limits.get("p")),
+                                           mp=full(limits.get("mp")), probs=False)
+            assert word == 0
+            assert (token >= 0).all() and np.array_equal(token, np.resize(token[:7], rows))
+            if "p" in limits:  # (where that cuts hangs on the last bits of the sum)
+                assert (kept >= 1).all() and np.isfinite(lp).all()
+                continue
+            row = x[0].to(dtype).double().numpy()
+            lo, hi, n = between(row, u[:7], k=limits.get("k", 0), mp=limits.get("mp", 0.0))
+            assert (lo <= token[:7]).all() and (token[:7] <= hi).all(), (gap, at)
+            assert (kept == n).all()
+            want = row[token[:7]] - gap - np.log1p((n - 1) * np.exp(-gap))
+            assert (np.abs(lp[:7] - want) <= 2.0 ** -20 * (1 + np.abs(want))).all()
+
+
+@pytest.mark.parametrize("V,rows", [(5003, 7), (1201, 400), (40001, 7)])
+@pytest.mark.parametrize("limits", [dict(), dict(k=1), dict(k=900), dict(p=0.9), dict(mp=0.01), dict(T=0.0)])
+def test_the_ends_of_ordinary_rows(V, rows, limits):
+    """Zero (of either sign) falls on the first kept token, the largest number
+    on a kept one; a weight that fp32 holds is a weight."""
+    x = logits(rows, V, 2.0, 41)
+    x[:, 0] = x.amax(1) - 90.0  # e^-90: below any sum's last bit, above zero
+    full = lambda v: None if v is None else [v] * rows  # noqa: E731
+    args = dict(T=full(limits.get("T")), k=full(limits.get("k")), p=full(limits.get("p")), mp=full(limits.get("mp")))
+    rows64 = x[:7].double().cpu().numpy()
+    for u in (0.0, -0.0, 1 - 2.0 ** -24):
+        token, kept, lp, _, word = run(x, [u] * rows, probs=False, **args)
+        assert word == 0
+        for i in range(7):
+            if limits.get("p"):
+                continue  # (its cut hangs on the last bits of the sum)
+            _, idx, _ = ref.sample_row(rows64[i], 0.5, limits.get("T", 1.0), limits.get("k", 0), 1.0,
+                                       limits.get("mp", 0.0))
+            assert token[i] == idx.min() if u == 0 else token[i] in idx
+        assert (token >= 0).all() and np.isfinite(lp).all()
