@@ -146,15 +146,17 @@ __device__ __forceinline__ float log_units(u64 sum) {
 }
 
 // z = (x - m) / T as a correctly rounded quotient (one Newton step on the
-// product with 1 / T); infinite m: the tokens at m share the weight.
+// product with 1 / T, where that has not passed the largest number, as with
+// masks of the type's lowest value and T < 1); infinite m: the tokens at m
+// share the weight.
 struct Weight {
   float m, T, inv;
   __device__ __forceinline__ float z(float x) const {
     const float d = x - m;
     const float q = d * inv;
     const float r = fmaf(-q, T, d);
-    const float c = T > 1e-18f ? fmaf(r, inv, q) : d / T;
-    return x == m ? 0.f : (isinf(d) ? d : c);
+    const float c = T > 1e-18f ? (isinf(q) ? q : fmaf(r, inv, q)) : d / T;
+    return x == m ? 0.f : c;
   }
   __device__ __forceinline__ float w(float x) const { return expf(z(x)); }
 };

@@ -326,3 +326,38 @@ def test_the_ends_of_ordinary_rows(V, rows, limits):
                                        limits.get("mp", 0.0))
             assert token[i] == idx.min() if u == 0 else token[i] in idx
         assert (token >= 0).all() and np.isfinite(lp).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,rows", [(1201, 400), (9000, 4), (40001, 4)])
+@pytest.mark.parametrize("T", [1e-10, 0.3, 1.0])
+@pytest.mark.parametrize("limits", [dict(), dict(k=50), dict(k=700), dict(p=0.9), dict(k=700, p=0.9), dict(mp=0.01)])
+def test_masks_of_the_lowest_value(dtype, V, rows, T, limits):
+    """Finite masks so low that their distance over the temperature is past
+    the largest number: no weight, and no NaN."""
+    r = np.random.default_rng(51)
+    low = torch.finfo(dtype).min
+    x = torch.full((rows, V), low)
+    for i in range(rows):
+        n = [1, 40, 300, 900][i % 4]
+        x[i, torch.as_tensor(r.permutation(V)[:n])] = torch.randn(n, generator=torch.Generator().manual_seed(i)) * 2
+    x = x.to(dtype)
+    x[1, 5] = -1e30
+    rows64 = x.double().numpy()
+    u, p, mp = (np.empty(rows) for _ in range(3))
+    lim = dict(k=limits.get("k", 0), p=limits.get("p", 1.0), min_p=limits.get("mp", 0.0))
+    T32 = float(np.float32(T))
+    for i in range(rows):
+        u[i], p[i], mp[i] = ref.settle(rows64[i], r.random(), T32, **lim)
+    u, p, mp = (v.astype(np.float32) for v in (u, p, mp))
+    token, kept, lp, lps, word = run(x.cuda(), u, [T] * rows, [lim["k"]] * rows, p, mp)
+    assert word == 0 and not np.isnan(lps).any() and not np.isnan(lp).any()
+    for i in range(rows):
+        t, idx, logp = ref.sample_row(rows64[i], float(u[i]), T32, lim["k"], float(p[i]), float(mp[i]))
+        assert token[i] == t and kept[i] == len(idx), i
+        dist = np.full(V, -np.inf)
+        with np.errstate(over="ignore"):
+            dist[idx] = logp.astype(np.float32)  # (-inf where it is below fp32's range)
+        ok = np.isfinite(dist)
+        assert np.array_equal(np.isfinite(lps[i]), ok), i
+        assert np.all(np.abs(lps[i][ok] - dist[ok]) <= 2.0 ** -20 * (1 + np.abs(dist[ok]))), i
