@@ -419,7 +419,8 @@ SIMSD_API int simsd_rope_rotate(int dtype, const simsd_rope_plan* plan, const in
  *            lengths once all layers are done
  *   positions [T] int32 or NULL: prefix_len[b] + i
  *   q_out    [T][Hq][d] dense; may be q where q is dense
- *   k_cache, v_cache [num_pages][Hkv][page_size][d]
+ *   k_cache, v_cache [num_pages][Hkv][page_size][d]; max_pages * page_size
+ *            at most 2^31 - 256
  * A prefix length that is negative or leaves no room for the chunk in the
  * block table sets SIMSD_EW_PREFIX_LEN: the sequence's q_out rows are zero
  * and nothing is cached.  A destination page outside the pool sets

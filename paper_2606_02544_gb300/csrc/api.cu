@@ -570,6 +570,7 @@ int simsd_rope_append(int dtype, const simsd_rope_plan* plan, const void* q, int
   if (T < 0 || Bt < 0 || Hq <= 0 || Hkv <= 0 || d <= 0 || num_pages < 0 || max_pages < 0 || page_size <= 0)
     return arg_fail("sizes");
   if ((d * eb) % 16 != 0) return arg_fail("d * element size must be a multiple of 16 bytes");
+  if (static_cast<long long>(max_pages) * page_size > 0x7fffff00ll) return unsupported("more than 2^31 rows a sequence");
   int rc = check_rope_plan(plan, d);
   if (rc != SIMSD_OK) return rc;
   if (T == 0 || Bt == 0) return SIMSD_OK;

@@ -171,3 +171,20 @@ def test_reference_sampling_shares():
     want[idx] = np.exp(lp)
     assert np.allclose(got, want, atol=2.0 / n)
     assert list(idx) == [1, 3, 2]  # the tie goes to the lower index; top_p ends before 0.5
+
+
+def test_append_refuses_rows_past_32_bits(simsd):
+    """A sequence whose block table reaches past 2^31 rows: its row numbers
+    are 32-bit on the device.  (Refused before any CUDA work: with T = 0 a
+    call that is not refused returns at once.)"""
+    lib = simsd.load_library()
+    plan = simsd.simsd_rope_plan_init("half", 64, 1e4)
+    one = ctypes.c_void_p(16)
+
+    def append(max_pages, page_size):
+        return lib.simsd_rope_append(1, ctypes.addressof(plan), one, 512, one, 128, one, 128, one, one, None, 0, 2, 8, 2,
+                                     64, one, one, one, 9, one, max_pages, page_size, None, None)
+
+    for max_pages, page_size in ((1 << 25, 64), (1 << 27, 64), ((1 << 31) - 1, (1 << 31) - 1), (1 << 21, 1024)):
+        assert append(max_pages, page_size) == simsd.SIMSD_ERR_UNSUPPORTED
+    assert append((1 << 25) - 4, 64) == 0 and append(1, 0x7fffff00) == 0
