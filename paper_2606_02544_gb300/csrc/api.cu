@@ -519,6 +519,9 @@ bool rows_ok(const void* p, int64_t stride, int H, int d, int eb) {
   return p && aligned16(p) && stride >= static_cast<int64_t>(H) * d && stride * eb % 16 == 0;
 }
 
+// token numbers, rounded up to a block of tokens, stay within 32 bits
+constexpr int kMaxRopeTokens = 0x7fffff00;
+
 bool page_size_ok(int P) { return P >= 8 && (P % 64 == 0 || 64 % P == 0); }
 
 }  // namespace
@@ -532,6 +535,7 @@ int simsd_rope_rotate(int dtype, const simsd_rope_plan* plan, const int32_t* pos
   if ((d * eb) % 16 != 0) return arg_fail("d * element size must be a multiple of 16 bytes");
   int rc = check_rope_plan(plan, d);
   if (rc != SIMSD_OK) return rc;
+  if (T > kMaxRopeTokens) return unsupported("too many tokens");
   if (T == 0) return SIMSD_OK;
   if (!positions) return arg_fail("null pointer");
   if (!rows_ok(q, q_stride, Hq, d, eb) || !rows_ok(q_out, q_out_stride, Hq, d, eb))
@@ -573,6 +577,7 @@ int simsd_rope_append(int dtype, const simsd_rope_plan* plan, const void* q, int
   if (static_cast<long long>(max_pages) * page_size > 0x7fffff00ll) return unsupported("more than 2^31 rows a sequence");
   int rc = check_rope_plan(plan, d);
   if (rc != SIMSD_OK) return rc;
+  if (T > kMaxRopeTokens) return unsupported("too many tokens");
   if (T == 0 || Bt == 0) return SIMSD_OK;
   if (!token_start || !prefix_len || !block_table || !k_cache || !v_cache) return arg_fail("null pointer");
   if (!rows_ok(q, q_stride, Hq, d, eb) || !rows_ok(k, k_stride, Hkv, d, eb) || !rows_ok(v, v_stride, Hkv, d, eb))

@@ -188,3 +188,15 @@ def test_append_refuses_rows_past_32_bits(simsd):
     for max_pages, page_size in ((1 << 25, 64), (1 << 27, 64), ((1 << 31) - 1, (1 << 31) - 1), (1 << 21, 1024)):
         assert append(max_pages, page_size) == simsd.SIMSD_ERR_UNSUPPORTED
     assert append((1 << 25) - 4, 64) == 0 and append(1, 0x7fffff00) == 0
+
+
+def test_rope_refuses_token_numbers_past_32_bits(simsd):
+    """A block of tokens at the end of 2^31 - 1 would pass 32 bits."""
+    lib = simsd.load_library()
+    plan = simsd.simsd_rope_plan_init("half", 64, 1e4)
+    one, pl = ctypes.c_void_p(16), ctypes.addressof(plan)
+    for T in (0x7fffff01, 0x7fffffff):
+        assert lib.simsd_rope_rotate(1, pl, one, one, 64, one, 64, 1, None, 0, None, 0, 0, T, 64,
+                                     None) == simsd.SIMSD_ERR_UNSUPPORTED
+        assert lib.simsd_rope_append(1, pl, one, 64, one, 64, one, 64, one, one, None, T, 1, 1, 1, 64, one, one, one, 9,
+                                     one, 9, 16, None, None) == simsd.SIMSD_ERR_UNSUPPORTED
