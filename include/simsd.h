@@ -352,7 +352,10 @@ SIMSD_API int simsd_kv_commit(int dtype, const void* k_new, const void* v_new, i
  * token_start[b+1]-1 of arrays of T tokens (token_start: [Bt+1] int32 in
  * [0, T], not decreasing; a chunk may be empty).  Offsets out of order or
  * range set SIMSD_EW_TOKENS and make that sequence's chunk empty; tokens
- * that no chunk holds are left untouched.
+ * that no chunk holds are left untouched.  Where offsets are out of order,
+ * tokens at or past the lowest such offset may be taken for another
+ * sequence's or left untouched, and chunks that overlap many times over may
+ * all be left untouched; nothing outside the arrays is read or written.
  */
 
 /*

@@ -691,7 +691,7 @@ int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, const int3
   if (Bt > simsd::kChunkMaxSeqs) return unsupported("more than 16384 sequences");
   if (static_cast<long long>(num_pages) * Hkv * page_size >= (1ll << 31))
     return unsupported("page pool too large for 32-bit TMA row coordinates");
-  // key tiles are counted in 32 bits (2^31 of them would take hours)
+  // key tiles are counted in 32 bits (2^31 of them take some 20 s)
   if ((static_cast<long long>(T) * Hq / 128 + static_cast<long long>(Bt) * Hkv + 1) * (max_keys / 128 + 1) >= (1ll << 31))
     return unsupported("too many key tiles in one call");
   simsd::EncodeTiledFn enc = encoder();

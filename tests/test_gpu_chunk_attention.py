@@ -301,3 +301,27 @@ def test_the_reference_moves_in_some_rows_of_every_tile(d):
             k[page, :, j % P] = (q[s + (7 * j) % C, ::2].float() * (0.2 + 0.8 * j / 1050)).to(torch.bfloat16)
     a["k_cache"] = k.cuda()
     check(a, softmax_scale=scale, mask_block=16)
+
+
+def test_offsets_that_overlap_many_times_over():
+    """8192 chunks of the same 8192 tokens over 300,000 rows: about 5 10^9 key
+    tiles, past the 32 bits that they are counted in.  Nothing is computed and
+    nothing written."""
+    Bt, T, Hkv, d, P = 16384, 8192, 8, 64, 1024
+    i32 = dict(dtype=torch.int32, device="cuda")
+    n = 300 * P
+    tiles = Bt // 2 * sum(-(-(n + 256 * (j + 1)) // 128) for j in range(T // 256)) * Hkv
+    assert tiles > 2 * 2 ** 31
+    q = torch.zeros(T, Hkv, d, dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.full_like(q, 7.0), torch.full((T, Hkv), 7.0, device="cuda")
+    start = torch.zeros(Bt + 1, **i32)
+    start[1::2] = T
+    kc = torch.zeros(1, Hkv, P, d, dtype=torch.bfloat16, device="cuda")
+    table = torch.zeros(Bt, n // P + T // P, **i32)
+    err = torch.zeros(1, **i32)
+    nbytes = simsd.simsd_chunk_workspace_bytes(simsd.SIMSD_BF16, T, Bt, Hkv, Hkv, d, table.shape[1], P)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    simsd.simsd_chunk_attention(q, start, torch.full((Bt,), n, **i32), kc, kc, table, out, lse=lse, workspace=ws,
+                                err_word=err)
+    assert simsd.simsd_check_error(err) == simsd.EW_TOKENS
+    assert (out == 7).all() and (lse == 7).all()
