@@ -58,7 +58,7 @@
 #include "chunk_mask.cuh"
 #include "common.cuh"
 #include "kernels.h"
-#include "ptx.cuh"
+#include "ptx_chunk.cuh"
 
 namespace simsd {
 namespace {
