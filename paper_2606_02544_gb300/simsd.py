@@ -286,7 +286,7 @@ def simsd_accept_sampled_ws(target_logits, draft_logits, draft, u_accept, u_samp
 
 # ------------------------------------------------------------------ prompts
 # (These calls sit in decoding loops of a few microseconds, so their checks
-# are written out: no message is built and no helper called unless one fails.)
+# are written out, and no message is built unless one fails.)
 _F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
 
 
@@ -294,14 +294,33 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _raw_stream(stream, t):
-    if stream is not None:
-        return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(t.get_device())
-
-
 def _wrong(what):
     raise ValueError(what)
+
+
+def _elsewhere():
+    _wrong("tensors on the current CUDA device wanted")
+
+
+def _device(t):
+    """The device that the library will plan for and launch on, which has to
+    be the tensor's."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        _elsewhere()
+    return dev
+
+
+def _error_word(t, dev):
+    if t is None:
+        return None
+    if t.dtype is not _I32 or t.get_device() != dev or t.numel() < 1:
+        _wrong("err_word: int32 on the current CUDA device wanted")
+    return t.data_ptr()
+
+
+def _raw_stream(stream, dev):
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev)
 
 
 def _code(dtype):
@@ -326,7 +345,7 @@ def _dense_i32(t, n):
 
 def _cache_sizes(k_cache, v_cache, block_table, Bt, Hkv, d, dtype):
     N, h, P, dd = k_cache.shape
-    if not (h == Hkv and dd == d and v_cache.shape == k_cache.shape and k_cache.dtype is dtype
+    if not (h == Hkv and dd == d and v_cache.shape == (N, h, P, d) and k_cache.dtype is dtype
             and v_cache.dtype is dtype and k_cache.is_contiguous() and v_cache.is_contiguous()):
         raise ValueError("k_cache / v_cache: dense [num_pages][Hkv][P][d] of q's type wanted")
     n, max_pages = block_table.shape
@@ -354,7 +373,7 @@ def simsd_rope_rotate(plan, positions, q, q_out, k=None, k_out=None, stream=None
     allowed); positions [T] int32."""
     T, Hq, d = q.shape
     dt = q.dtype
-    if q_out.shape != q.shape or q_out.dtype is not dt:
+    if q_out.shape != (T, Hq, d) or q_out.dtype is not dt:
         _wrong("q_out: shape and type of q wanted")
     if not _dense_i32(positions, T):
         _wrong("positions: dense int32 [T] wanted")
@@ -362,14 +381,18 @@ def simsd_rope_rotate(plan, positions, q, q_out, k=None, k_out=None, stream=None
     kp = kop = None
     if k is not None:
         Hkv = k.shape[1]
-        if (k_out is None or k.shape != (T, Hkv, d) or k_out.shape != k.shape or k.dtype is not dt
+        if (k_out is None or k.shape != (T, Hkv, d) or k_out.shape != (T, Hkv, d) or k.dtype is not dt
                 or k_out.dtype is not dt):
             _wrong("k / k_out: [T][Hkv][d] of q's type wanted")
         ks, kos = _rows(k, Hkv, d, "k"), _rows(k_out, Hkv, d, "k_out")
         kp, kop = k.data_ptr(), k_out.data_ptr()
+    dev = _device(q)
+    if not (dev == positions.get_device() == q_out.get_device() and
+            (k is None or dev == k.get_device() == k_out.get_device())):
+        _elsewhere()
     rc = (_lib or load_library()).simsd_rope_rotate(
         _code(dt), ctypes.addressof(plan), positions.data_ptr(), q.data_ptr(), _rows(q, Hq, d, "q"),
-        q_out.data_ptr(), _rows(q_out, Hq, d, "q_out"), Hq, kp, ks, kop, kos, Hkv, T, d, _raw_stream(stream, q))
+        q_out.data_ptr(), _rows(q_out, Hq, d, "q_out"), Hq, kp, ks, kop, kos, Hkv, T, d, _raw_stream(stream, dev))
     if rc:
         _check(rc, "simsd_rope_rotate")
 
@@ -381,20 +404,25 @@ def simsd_rope_append(plan, q, k, v, token_start, prefix_len, q_out, k_cache, v_
     [num_pages][Hkv][P][d].  prefix_len is not advanced."""
     T, Hq, d = q.shape
     Hkv, Bt, dt = k.shape[1], prefix_len.shape[0], q.dtype
-    if k.shape != (T, Hkv, d) or v.shape != k.shape or k.dtype is not dt or v.dtype is not dt:
+    if k.shape != (T, Hkv, d) or v.shape != (T, Hkv, d) or k.dtype is not dt or v.dtype is not dt:
         _wrong("k / v: [T][Hkv][d] of q's type wanted")
-    if q_out.shape != q.shape or q_out.dtype is not dt or not q_out.is_contiguous():
+    if q_out.shape != (T, Hq, d) or q_out.dtype is not dt or not q_out.is_contiguous():
         _wrong("q_out: dense, like q")
     if not _dense_i32(token_start, Bt + 1) or not _dense_i32(prefix_len, Bt):
         _wrong("token_start / prefix_len: dense int32 [Bt+1] / [Bt] wanted")
     if positions is not None and not _dense_i32(positions, T):
         _wrong("positions: dense int32 [T] wanted")
     num_pages, max_pages, P = _cache_sizes(k_cache, v_cache, block_table, Bt, Hkv, d, dt)
+    dev = _device(q)
+    if not (dev == k.get_device() == v.get_device() == token_start.get_device() == prefix_len.get_device()
+            == q_out.get_device() == k_cache.get_device() == v_cache.get_device() == block_table.get_device()
+            and (positions is None or positions.get_device() == dev)):
+        _elsewhere()
     rc = (_lib or load_library()).simsd_rope_append(
         _code(dt), ctypes.addressof(plan), q.data_ptr(), _rows(q, Hq, d, "q"), k.data_ptr(), _rows(k, Hkv, d, "k"),
         v.data_ptr(), _rows(v, Hkv, d, "v"), token_start.data_ptr(), prefix_len.data_ptr(), _ptr(positions), T, Bt,
         Hq, Hkv, d, q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), num_pages, block_table.data_ptr(),
-        max_pages, P, _ptr(err_word), _raw_stream(stream, q))
+        max_pages, P, _error_word(err_word, dev), _raw_stream(stream, dev))
     if rc:
         _check(rc, "simsd_rope_append")
 
@@ -411,7 +439,7 @@ def simsd_chunk_attention(q, token_start, prefix_len, k_cache, v_cache, block_ta
     out [T][Hq][d], lse [T][Hq] fp32."""
     T, Hq, d = q.shape
     Bt, Hkv, dt = prefix_len.shape[0], k_cache.shape[1], q.dtype
-    if out.shape != q.shape or out.dtype is not dt or not out.is_contiguous():
+    if out.shape != (T, Hq, d) or out.dtype is not dt or not out.is_contiguous():
         _wrong("out: dense, like q")
     if not _dense_i32(token_start, Bt + 1) or not _dense_i32(prefix_len, Bt):
         _wrong("token_start / prefix_len: dense int32 [Bt+1] / [Bt] wanted")
@@ -420,31 +448,41 @@ def simsd_chunk_attention(q, token_start, prefix_len, k_cache, v_cache, block_ta
     if lse is not None and (lse.shape != (T, Hq) or lse.dtype is not _F32 or not lse.is_contiguous()):
         _wrong("lse: dense float32 [T][Hq] wanted")
     num_pages, max_pages, P = _cache_sizes(k_cache, v_cache, block_table, Bt, Hkv, d, dt)
+    dev = _device(q)
+    if not (dev == token_start.get_device() == prefix_len.get_device() == out.get_device() == k_cache.get_device()
+            == v_cache.get_device() == block_table.get_device() and (lse is None or lse.get_device() == dev)
+            and (key_start is None or key_start.get_device() == dev)
+            and (workspace is None or workspace.get_device() == dev)):
+        _elsewhere()
     ws = ws_bytes = 0
     if workspace is not None:
         ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     rc = (_lib or load_library()).simsd_chunk_attention(
         _code(dt), q.data_ptr(), _rows(q, Hq, d, "q"), token_start.data_ptr(), prefix_len.data_ptr(),
         _ptr(key_start), k_cache.data_ptr(), v_cache.data_ptr(), num_pages, block_table.data_ptr(), max_pages, P, T,
-        Bt, Hq, Hkv, d, mask_block, window, softmax_scale, out.data_ptr(), _ptr(lse), ws, ws_bytes, _ptr(err_word),
-        _raw_stream(stream, q))
+        Bt, Hq, Hkv, d, mask_block, window, softmax_scale, out.data_ptr(), _ptr(lse), ws, ws_bytes,
+        _error_word(err_word, dev), _raw_stream(stream, dev))
     if rc:
         _check(rc, "simsd_chunk_attention")
 
 
-def _row_f32(t, R, name):
+def _row_f32(t, R, dev, name):
     if t is None:
         return None
     if t.dtype is not _F32 or t.numel() != R or not t.is_contiguous():
         _wrong(name + ": dense float32 [R] wanted")
+    if t.get_device() != dev:
+        _elsewhere()
     return t.data_ptr()
 
 
-def _row_i32(t, R, name):
+def _row_i32(t, R, dev, name):
     if t is None:
         return None
     if t.dtype is not _I32 or t.numel() != R or not t.is_contiguous():
         _wrong(name + ": dense int32 [R] wanted")
+    if t.get_device() != dev:
+        _elsewhere()
     return t.data_ptr()
 
 
@@ -461,10 +499,15 @@ def simsd_sample(logits, u, token, temperature=None, top_k=None, top_p=None, min
     if log_probs is not None and (log_probs.shape != (R, V) or log_probs.dtype is not _F32
                                   or not log_probs.is_contiguous()):
         _wrong("log_probs: dense float32 [R][V] wanted")
+    code, dev = _code(logits.dtype), logits.get_device()
+    args = (_row_f32(u, R, dev, "u"), _row_f32(temperature, R, dev, "temperature"), _row_i32(top_k, R, dev, "top_k"),
+            _row_f32(top_p, R, dev, "top_p"), _row_f32(min_p, R, dev, "min_p"), _row_i32(token, R, dev, "token"),
+            _row_i32(kept, R, dev, "kept"), _row_f32(log_prob, R, dev, "log_prob"))
+    _device(logits)
+    if log_probs is not None and log_probs.get_device() != dev:
+        _elsewhere()
     rc = (_lib or load_library()).simsd_sample(
-        _code(logits.dtype), logits.data_ptr(), s0 if R > 1 else V, R, V, _row_f32(u, R, "u"),
-        _row_f32(temperature, R, "temperature"), _row_i32(top_k, R, "top_k"), _row_f32(top_p, R, "top_p"),
-        _row_f32(min_p, R, "min_p"), _row_i32(token, R, "token"), _row_i32(kept, R, "kept"),
-        _row_f32(log_prob, R, "log_prob"), _ptr(log_probs), _ptr(err_word), _raw_stream(stream, logits))
+        code, logits.data_ptr(), s0 if R > 1 else V, R, V, *args, _ptr(log_probs), _error_word(err_word, dev),
+        _raw_stream(stream, dev))
     if rc:
         _check(rc, "simsd_sample")

@@ -80,3 +80,34 @@ def test_drafts_from_a_truncated_distribution_keep_the_target():
     assert (got[want == 0] == 0).all()
     # five standard deviations of a share
     assert np.all(np.abs(got - want) <= 5 * np.sqrt(want * (1 - want) / Bt) + 1e-12)
+
+
+def test_one_tensor_off_the_gpu_is_refused():
+    """Any tensor of a call left in host memory, and an error word of another
+    type: refused before anything is launched."""
+    T, Hq, Hkv, d, P = 4, 4, 2, 64, 16
+    z = lambda *s: torch.zeros(*s, device="cuda")  # noqa: E731
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")  # noqa: E731
+    plan = simsd.simsd_rope_plan_init("half", 64, 1e4)
+    calls = [
+        (lambda **a: simsd.simsd_rope_rotate(plan, **a), dict(positions=i(T), q=z(T, Hq, d), q_out=z(T, Hq, d),
+                                                              k=z(T, Hkv, d), k_out=z(T, Hkv, d))),
+        (lambda **a: simsd.simsd_rope_append(plan, **a),
+         dict(q=z(T, Hq, d), k=z(T, Hkv, d), v=z(T, Hkv, d), token_start=i(3), prefix_len=i(2), positions=i(T),
+              q_out=z(T, Hq, d), k_cache=z(5, Hkv, P, d), v_cache=z(5, Hkv, P, d), block_table=i(2, 3), err_word=i(1))),
+        (simsd.simsd_chunk_attention,
+         dict(q=z(T, Hq, d), token_start=i(3), prefix_len=i(2), k_cache=z(5, Hkv, P, d), v_cache=z(5, Hkv, P, d),
+              block_table=i(2, 3), out=z(T, Hq, d), lse=z(T, Hq), key_start=i(2), err_word=i(1),
+              workspace=torch.zeros(1 << 20, dtype=torch.uint8, device="cuda"))),
+        (simsd.simsd_sample,
+         dict(logits=z(3, 7), u=z(3), token=i(3), temperature=z(3), top_k=i(3), top_p=z(3), min_p=z(3), kept=i(3),
+              log_prob=z(3), log_probs=z(3, 7), err_word=i(1)))]
+    for call, args in calls:
+        call(**args)
+        for name, t in args.items():
+            with pytest.raises(ValueError):
+                call(**{**args, name: t.cpu()})
+        if "err_word" in args:
+            with pytest.raises(ValueError):
+                call(**{**args, "err_word": args["err_word"].to(torch.uint8)})
+    torch.cuda.synchronize()

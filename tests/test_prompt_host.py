@@ -200,3 +200,20 @@ def test_rope_refuses_token_numbers_past_32_bits(simsd):
                                      None) == simsd.SIMSD_ERR_UNSUPPORTED
         assert lib.simsd_rope_append(1, pl, one, 64, one, 64, one, 64, one, one, None, T, 1, 1, 1, 64, one, one, one, 9,
                                      one, 9, 16, None, None) == simsd.SIMSD_ERR_UNSUPPORTED
+
+
+def test_tensors_off_the_gpu_are_refused(simsd):
+    """Pointers to host memory never reach the library."""
+    T, Hq, Hkv, d, P = 4, 4, 2, 64, 16
+    q, k, kc = torch.zeros(T, Hq, d), torch.zeros(T, Hkv, d), torch.zeros(5, Hkv, P, d)
+    i32 = dict(dtype=torch.int32)
+    ts, n, bt, pos = torch.zeros(3, **i32), torch.zeros(2, **i32), torch.zeros(2, 3, **i32), torch.zeros(T, **i32)
+    plan = simsd.simsd_rope_plan_init("half", 64, 1e4)
+    with pytest.raises(ValueError, match="CUDA device"):
+        simsd.simsd_rope_rotate(plan, pos, q, q, k, k)
+    with pytest.raises(ValueError, match="CUDA device"):
+        simsd.simsd_rope_append(plan, q, k, k, ts, n, q, kc, kc, bt)
+    with pytest.raises(ValueError, match="CUDA device"):
+        simsd.simsd_chunk_attention(q, ts, n, kc, kc, bt, q)
+    with pytest.raises(ValueError, match="CUDA device"):
+        simsd.simsd_sample(torch.zeros(3, 7), torch.zeros(3), torch.zeros(3, **i32))
