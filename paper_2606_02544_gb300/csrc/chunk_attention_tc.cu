@@ -635,11 +635,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           continue;
         }
         ok = wait(sm.bar_q[x], ju & 1);
-        if (x == 1) {
-          // block B starts half a tile behind block A, so that one's softmax
-          // meets the other's MMAs; they keep that distance by themselves
-          for (int i = 0; i < 0 && !*abort_flag; ++i) __nanosleep(32);
-        }
         ok = ok && issue_s(n == 1);
         for (int i = 0; ok && i < n; ++i) {
           ok = wait(sm.bar_full[kStagesK + vs], vp);
