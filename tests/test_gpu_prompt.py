@@ -111,3 +111,64 @@ def test_one_tensor_off_the_gpu_is_refused():
             with pytest.raises(ValueError):
                 call(**{**args, "err_word": args["err_word"].to(torch.uint8)})
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_calls_in_a_cuda_graph(dtype):
+    """Rotation, append, attention and sampling captured once and replayed on
+    other inputs (lengths and offsets too): the bits of the calls made one by
+    one.  Long enough a cache that the attention merges pieces."""
+    T, Bt, Hq, Hkv, d, P, V, pages = 70, 3, 8, 2, 64, 64, 9001, 40
+    code = simsd.SIMSD_F32 if dtype == torch.float32 else simsd.SIMSD_BF16
+    plan = simsd.simsd_rope_plan_init("half", 64, 1.0e6, "linear", factor=2.0)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    g = torch.Generator().manual_seed(8)
+    table = torch.randperm(Bt * pages, generator=g).to(torch.int32).view(Bt, pages).cuda()
+    nbytes = simsd.simsd_chunk_workspace_bytes(code, T, Bt, Hq, Hkv, d, pages, P)
+    ws = torch.empty(max(16, nbytes), dtype=torch.uint8, device="cuda")
+    qkv = torch.zeros(T, Hq + 2 * Hkv, d, dtype=dtype, device="cuda")
+    start, n, pos = torch.zeros(Bt + 1, **i32), torch.zeros(Bt, **i32), torch.zeros(T, **i32)
+    logits, u = torch.zeros(T, V, dtype=dtype, device="cuda"), torch.zeros(T, device="cuda")
+    k0 = (torch.randn(Bt * pages, Hkv, P, d, generator=g) * 0.5).to(dtype).cuda()
+    kc, vc = k0.clone(), k0.flip(0).contiguous()
+    q, turned, out = (torch.zeros(T, Hq, d, dtype=dtype, device="cuda") for _ in range(3))
+    lse, lps = torch.zeros(T, Hq, device="cuda"), torch.zeros(T, V, device="cuda")
+    token, err = torch.zeros(T, **i32), torch.zeros(1, **i32)
+    top_k = torch.full((T,), 300, **i32)
+
+    def step():
+        simsd.simsd_rope_append(plan, qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:], start, n, q, kc, vc, table,
+                                err_word=err)
+        simsd.simsd_chunk_attention(q, start, n, kc, vc, table, out, lse=lse, workspace=ws, err_word=err)
+        simsd.simsd_rope_rotate(plan, pos, out, turned)
+        simsd.simsd_sample(logits, u, token, top_k=top_k, log_probs=lps, err_word=err)
+
+    def fill(seed, lengths, prefix):
+        gg = torch.Generator().manual_seed(seed)
+        for t, std in ((qkv, 1.0), (logits, 3.0)):
+            t.copy_((torch.randn(t.shape, generator=gg) * std).to(dtype))
+        u.copy_(torch.rand(T, generator=gg))
+        pos.copy_(torch.randint(0, 9999, (T,), generator=gg, dtype=torch.int32))
+        start.copy_(torch.tensor([0, lengths[0], lengths[0] + lengths[1], T], dtype=torch.int32))
+        n.copy_(torch.tensor(prefix, dtype=torch.int32))
+        kc.copy_(k0)
+        for t in (q, turned, out, lse, lps, token):
+            t.zero_()
+
+    results = lambda: [t.clone() for t in (q, kc, out, lse, turned, token, lps)]  # noqa: E731
+    fill(0, [1, 1], [2000, 0, 5])
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed, lengths, prefix in ((1, [1, 60], [2400, 7]), (2, [40, 0], [100, 2490]), (3, [1, 1], [0, 2000])):
+        prefix = prefix + [1234]
+        fill(seed, lengths, prefix)
+        step()
+        want = results()
+        fill(seed, lengths, prefix)
+        graph.replay()
+        for a, b in zip(want, results()):
+            assert torch.equal(a, b)
+    assert simsd.simsd_check_error(err) == 0

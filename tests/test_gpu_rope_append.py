@@ -184,3 +184,21 @@ def test_on_a_stream_of_its_own():
     first = a["q_out"].clone()
     simsd.simsd_rope_append(plan, **a)
     assert torch.equal(first, a["q_out"])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("layout,rot,d", [("half", 128, 128), ("interleaved", 128, 128), ("half", 24, 64), ("interleaved", 6, 64)])
+def test_rotate_against_the_plain_form(dtype, layout, rot, d):
+    """The rows of a verification step (many tokens, scaled frequencies) and a
+    single one; the type's own vectors and rounding."""
+    g = torch.Generator().manual_seed(2)
+    kw = dict(scaling="yarn", factor=4.0, context=8192)
+    plan, f = simsd.simsd_rope_plan_init(layout, rot, THETA, **kw), ref.frequencies(rot, THETA, **kw)
+    for T in (1, 1025):
+        x = torch.randn(T, 10, d, generator=g).to(dtype).cuda()
+        pos = torch.randint(0, 40000, (T,), generator=g, dtype=torch.int32).cuda()
+        qo, ko = torch.full_like(x[:, :8], float("nan")), torch.full_like(x[:, 8:], float("nan"))
+        simsd.simsd_rope_rotate(plan, pos, x[:, :8], qo, x[:, 8:], ko)
+        want, size = ref.rotate(x.double().cpu().numpy(), pos.cpu().numpy(), layout, rot, f)
+        got = torch.cat([qo, ko], 1).double().cpu().numpy()
+        assert np.all(np.abs(got - want) <= ref.rope_tolerance(want, size, dtype == torch.bfloat16))

@@ -361,3 +361,11 @@ def test_masks_of_the_lowest_value(dtype, V, rows, T, limits):
         ok = np.isfinite(dist)
         assert np.array_equal(np.isfinite(lps[i]), ok), i
         assert np.all(np.abs(lps[i][ok] - dist[ok]) <= 2.0 ** -20 * (1 + np.abs(dist[ok]))), i
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,rows", [(9001, 3), (40001, 3), (151936, 3), (40001, 60)])
+@pytest.mark.parametrize("limits", [dict(), dict(p=0.9), dict(k=1000, p=0.98, mp=0.001)])
+def test_distributions_of_rows_on_several_ctas(dtype, V, rows, limits):
+    """Two, four and eight CTAs a row: the values of the distribution."""
+    check(logits(rows, V, 2.5, 61, dtype), 62, **{"T": 0.8, **limits})
