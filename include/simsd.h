@@ -369,18 +369,22 @@ SIMSD_API int simsd_kv_commit(int dtype, const void* k_new, const void* v_new, i
  *   NTK       f_i with theta s^(r/(r-2)) for theta    (r > 2)
  *   YARN      (1 - g) f_i / s + g f_i, g = (rho_i - beta_slow) / (beta_fast
  *             - beta_slow) clamped to [0, 1], rho_i = context f_i / 2 pi the
- *             turns pair i makes over the trained context
+ *             turns pair i makes over the trained context (a ramp in turns;
+ *             checkpoints whose ramp is in the pair's index, between two
+ *             rounded corners, need other frequencies: see turn)
  * and is multiplied by `magnitude` (0.1 ln s + 1 for YARN, else 1; the
  * caller may set another).  Components r .. d-1 of a head are not changed.
  * The angle of a 32-bit position, negative ones included, is formed in
- * 64-bit fixed point, so it does not lose digits in long contexts.
+ * 64-bit fixed point from frequencies in double, so it does not lose digits in
+ * long contexts (fp32's last bit up to position 2^27, 2^-20 rad at 2^31).
  */
 typedef struct simsd_rope_plan {
   int32_t layout;   /* SIMSD_ROPE_HALF or SIMSD_ROPE_INTERLEAVED */
   int32_t rot_dim;  /* r: even, 2 .. 128 */
   float magnitude;  /* positive and finite */
   int32_t reserved; /* 0 */
-  uint64_t turn[64]; /* frequency of pair i in 2^-64 turns a position */
+  uint64_t turn[64]; /* frequency of pair i in 2^-64 turns a position; the
+                        caller may set others than simsd_rope_plan_init's */
 } simsd_rope_plan;
 
 /*
@@ -488,9 +492,9 @@ SIMSD_API int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, 
  * -inf (NaN counts as -inf).  Of the tokens in the order of falling logits
  * (ties: lower index first) the first top_k are kept, of those the shortest
  * prefix whose weight is at least top_p of theirs, of those the ones with
- * w_v >= min_p.  The token is the smallest index whose cumulative kept weight
- * (in index order) exceeds u times their sum.  temperature 0 keeps the first
- * token of that order alone (greedy).
+ * w_v >= min_p (above 1: as 1).  The token is the smallest index whose
+ * cumulative kept weight (in index order) exceeds u times their sum.
+ * temperature 0 keeps the first token of that order alone (greedy).
  *   logits   [R][vocab] dtype (SIMSD_F32 or SIMSD_BF16), row stride in
  *            elements; vocab in [1, 2^24]
  *   u        [R] fp32 in [0, 1)
@@ -501,15 +505,16 @@ SIMSD_API int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, 
  *   log_prob [R] fp32 out or NULL: log-probability of the token among the
  *            kept (a denoising step's confidence)
  *   log_probs [R][vocab] fp32 out or NULL: of every token, -inf where not
- *            kept: the target or draft logits (at temperature 1) of
- *            simsd_accept_sampled for models that sample from truncated
- *            distributions
- * Weights are fp32, the sums that decide are 64-bit fixed point over fp32
- * batches taken in a fixed order, so a call gives the same result every
- * time.  A row without a logit above -inf, or with
- * parameters outside these ranges (NaN, a negative or infinite temperature,
- * u outside [0, 1)) sets SIMSD_EW_SAMPLE and gets token -1, kept 0 and
- * log-probabilities -inf.
+ *            kept (or below fp32's range): the target or draft logits (at
+ *            temperature 1) of simsd_accept_sampled for models that sample
+ *            from truncated distributions
+ * Weights are fp32; the sums that decide are fixed point over fp32 batches
+ * taken in a fixed order (top_p's in units of 2^-38 of the largest weight, the
+ * random number's in 2^-88; zero falls on the first kept token whose weight
+ * fp32 holds), so a call gives the same result every time.  A row without a
+ * logit above -inf, or with parameters outside these ranges (NaN, a negative
+ * or infinite temperature, u outside [0, 1)) sets SIMSD_EW_SAMPLE and gets
+ * token -1, kept 0 and log-probabilities -inf.
  */
 SIMSD_API int simsd_sample(int dtype, const void* logits, int64_t row_stride, int R, int vocab, const float* u,
                            const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,

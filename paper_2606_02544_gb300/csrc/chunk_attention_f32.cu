@@ -349,7 +349,7 @@ __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_consta
 // the next four keys' while these are worked on.  The warps' results are
 // merged through shared memory.  Bound by memory and by the sums over the
 // lanes (20 shuffles a key): 32 single tokens over 4096 keys, 32 heads on 8,
-// read 1.07 GB in 260 us (4.1 TB/s); tiles of 16 rows took 650.
+// read 1.07 GB in 266 us (4.0 TB/s); tiles of 16 rows took 650.
 template <int D>
 __global__ void __launch_bounds__(kThreads, 2) chunk_f32_few_kernel(const __grid_constant__ F32Params p) {
   constexpr int E = D / 32, kWarps = kThreads / 32, kKeys = 4, R = 4;

@@ -4,20 +4,22 @@
 //
 // Mathematics.  The pair i < r/2 of a token at position p turns by p f_i
 // (rotary embedding of RoFormer over the first r components; f_i as scaled
-// by simsd_rope_plan_init).  The plan holds F_i = round(2^64 f_i / 2 pi), so
-// p F_i mod 2^64 is the fraction of a turn, exact to 2^-64 p for any 32-bit
-// position; its top 32 bits, read as a signed number of 2^-31 half turns, go
-// to sincospif.  Products and sums are fp32, rounded once to the type.
+// by simsd_rope_plan_init).  The plan holds F_i = round(2^64 f_i / 2 pi), f_i
+// a double, and p F_i mod 2^64 is the fraction of a turn.  That product is
+// exact; what is lost is the double's rounding, about 4 2^-53 f_i p radians
+// (f_i <= 1): below fp32's last bit up to p = 2^27, 2^-20 at p = 2^31.  Its top
+// 32 bits, read as a signed number of 2^-31 half turns, go to sincospif.
+// Products and sums are fp32, rounded once to the type.
 //
 // Bound by memory: a token reads and writes (Hq + 2 Hkv) d elements.  A
 // thread owns one pair of VE-wide vectors (the two halves of VE pairs, or
 // two vectors of interleaved pairs) of one token and walks over heads, so
 // the VE angles it forms serve every head it visits; kHeadsInFlight heads'
 // loads are issued together (two: with four the registers leave half the
-// threads, 108 us instead of 87 for 16384 tokens of 32/8 heads, bf16; angles
+// threads, 108 us instead of 85 for 16384 tokens of 32/8 heads, bf16; angles
 // formed once a block in shared memory, 91 us).  Few tokens are spread over
-// more threads by giving each fewer heads (down to one).  403 MB in 87 us:
-// 4.6 TB/s; what remains is the latency of a thread's loads.
+// more threads by giving each fewer heads (down to one).  403 MB in 85 us:
+// 4.7 TB/s; what remains is the latency of a thread's loads.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

@@ -4,32 +4,40 @@
 //
 // Mathematics.  w_v = exp((x_v - m) / T), m = max x.  The kept set is a
 // prefix of the order (x falling, index rising): {x > kappa} and the tokens
-// x = kappa up to some index, cut by w >= min_p.  Sums of weights are 64-bit
-// integers in units of 2^-38 of the largest weight (a token whose number hangs
-// on the last bits of a sum of 150,000 weights is still the right one).
+// x = kappa up to some index, cut by w >= min_p.  The sums that top_p decides
+// by are 64-bit integers in units of 2^-38 of the largest weight; the random
+// number is placed in units of 2^-88, so that the smallest weights have their
+// share of it.
 //
 // A row is read twice.  The first pass (from HBM) takes the maximum and a
 // histogram over 2048 bins of x / T: counts for top_k, weights to 2^-17 of
 // themselves for top_p.  That names the bin of kappa (a bracket of a few where
 // top_p falls near a bin's edge).  The second pass (the last vectors first,
-// which are still in L2) adds up exactly what lies above the bin and lists
-// the tokens inside it; one CTA sorts the list (bitonic, mostly in registers)
-// and cuts it.  Sums that contradict the histogram, or more tokens in the bin
-// than the list holds (many equal logits), send the row through radix
-// searches (400 rows of 151936 equal logits: 1.9 ms); a row whose open tokens
-// the sample missed, as nearly all are masked, has its histogram taken once
-// more around the maximum (8 rows with 10 open tokens: 44 us).  The random
-// number is placed by the weights of the row's segments (one per warp), and
-// only the segment it falls in is read again.
+// which are still in L2) adds up what lies above the bin and lists the tokens
+// inside it; one CTA sorts the list (bitonic, mostly in registers) and cuts
+// it.  Sums that contradict the histogram, or more tokens in the bin than the
+// list holds (many equal logits), send the row through radix searches (400
+// rows of 151936 equal logits: 1.9 ms); a row whose open tokens the sample
+// missed, as nearly all are masked, has its histogram taken once more around
+// the maximum (8 rows with 10 open tokens: 45 us).  The random number is placed
+// by the weights of the row's segments (one per warp), and only the segment it
+// falls in is read again.
+//
+// The second pass takes a weight as 2^(c (x - m)), c = log2(e) / T in fp32,
+// which is good to (|z| + 1) 2^-22 of itself, z = (x - m) / T; the list, the
+// searches and the place within a segment take e^z of the correctly rounded z.
+// Against 64-bit sums, normal logits in rows of 1066 to 151936: all of 8192
+// random numbers gave the same token; under top_p 12 of 5096 rows kept one
+// token more or less.
 //
 // Counting all of a row costs one shared-memory reduction a token, which HBM
 // can feed; counts of an eighth of it left brackets of thousands of tokens
 // under heavy-tailed weights and a third pass over the row (1024 rows of
-// 151936: 898 us, this way 325).
+// 151936: 898 us, this way 327).
 //
-// Measured, 151936 logits of fp32: 1024 rows 325 us (1.9 TB/s of the bytes
+// Measured, 151936 logits of fp32: 1024 rows 327 us (1.9 TB/s of the bytes
 // read once, 3.8 of those read; each pass about 70% of the time in the
-// instructions of a token, 16 and 11, and HBM), 8 rows 24 us (a chain of
+// instructions of a token, 16 and 11, and HBM), 8 rows 25 us (a chain of
 // passes and exchanges over a cluster); 132 rows of 32003 in bf16 with their
 // distribution 52 us.
 //
@@ -1246,6 +1254,8 @@ cudaError_t launch_e(const SampleArgs& a, int num_sms, cudaStream_t stream) {
   // steps of a row, of which four CTAs of 256 threads overlap more (1783 rows
   // of 1066: 81 us, with 512 threads 132; 2000 of 32003: 204, 230; but 610 of
   // 65536: 118, 113; 1024 of 151936: 356, 330, as fewer rows stay in L2).
+  // Four CTAs a SM leave a thread 64 registers, with spills of about 480 bytes
+  // stored and 720 loaded (512 threads: 80 and 50); the figures include them.
   if (a.R > 2ll * num_sms && a.V <= kSmallV) return launch_nt<E, 256>(a, 1, stream);
   // Two CTAs fit a SM: as many CTAs a row as fit at once, none for less than
   // 4096 tokens.  (More CTAs for many rows would keep the rows in work within
