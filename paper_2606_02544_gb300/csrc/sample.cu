@@ -328,16 +328,24 @@ __device__ __forceinline__ void put_segment(Smem<NT>& sm, int rank, const LongSu
   }
 }
 
-// Sums over the cluster of four values; every CTA gets them, and the CTAs'
-// own in x_sum[turn].  A buffer's next use lies behind the next sum's barrier.
+// Sums over the cluster of four values: the CTAs' own sums in x_sum[turn] of
+// every CTA, which sum_of adds up.  A buffer's next use lies behind the next
+// sum's barrier.  (By value, and the sums left in shared memory: with an array
+// by reference the fp32 kernel of 256 threads, which spills, went on with a
+// wrong low half of one of them.)
 template <int NT>
-__device__ __noinline__ void cluster_sum(Smem<NT>& sm, int CL, int rank, int turn, u64 (&v)[4]) {
+__device__ __noinline__ void cluster_sum(Smem<NT>& sm, int CL, int rank, int turn, u64 a, u64 b, u64 c, u64 d) {
   constexpr int kWarps = NT / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const u64 x = warp_sum(v[k]);
-    if (lane == 0) sm.warp_v[k][warp] = x;
+  a = warp_sum(a);
+  b = warp_sum(b);
+  c = warp_sum(c);
+  d = warp_sum(d);
+  if (lane == 0) {
+    sm.warp_v[0][warp] = a;
+    sm.warp_v[1][warp] = b;
+    sm.warp_v[2][warp] = c;
+    sm.warp_v[3][warp] = d;
   }
   __syncthreads();
   if (warp < 4) {
@@ -345,11 +353,12 @@ __device__ __noinline__ void cluster_sum(Smem<NT>& sm, int CL, int rank, int tur
     if (lane < CL) st_rank(&sm.x_sum[turn][warp][rank], lane, x);
   }
   sync_all(CL);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    v[k] = 0;
-    for (int r = 0; r < CL; ++r) v[k] += sm.x_sum[turn][k][r];
-  }
+}
+template <int NT>
+__device__ __forceinline__ u64 sum_of(const Smem<NT>& sm, int CL, int turn, int k) {
+  u64 s = 0;
+  for (int r = 0; r < CL; ++r) s += sm.x_sum[turn][k][r];
+  return s;
 }
 
 // Exclusive scan over the block of (c, q) in thread order.
@@ -816,10 +825,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const __grid_cons
   auto key_x = [](u64 key) { return from_ordered(static_cast<uint32_t>(key >> 32)); };
 
   // ---- pass 2: adds up the tokens x1 <= x and lists those in [x0, x1).
-  // v: count above (and, above 2^32, of the list), weight above, weight of the
+  // Sums: count above (and, above 2^32, of the list), weight above, weight of the
   // list, weight of the row (the last three only where they are used).
   const float c_exp = inv * 1.4426950408889634f;
-  auto pass = [&](const Bracket& b, u64 (&v)[4]) {
+  auto pass = [&](const Bracket& b) {
     if (tid == 0) sm.list_n = 0;
     __syncthreads();
     const float x0 = b.x0, x1 = b.x1;
@@ -872,11 +881,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const __grid_cons
     const int own = sm.list_n;
     if (!by_count)
       for (int i = tid; i < min(own, kList); i += NT) ql += units(wt.w(key_x(sm.list[i])));
-    v[0] = n + (tid == 0 ? static_cast<u64>(own) << 32 : 0);
-    v[1] = q;
-    v[2] = ql;
-    v[3] = fa.total();
-    cluster_sum(sm, CL, rank, turn ^= 1, v);
+    turn ^= 1;
+    cluster_sum(sm, CL, rank, turn, n + (tid == 0 ? static_cast<u64>(own) << 32 : 0), q, ql, fa.total());
   };
 
   // The bracket of a limit, exact sums around it, and the search of the list.
@@ -884,16 +890,16 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const __grid_cons
   auto by_list = [&](bool& both) {
     const Bracket b = estimate();
     if (!b.ok) return false;
-    u64 v[4];
-    pass(b, v);
-    const u64 above_n = v[0] & 0xffffffffull, above_q = v[1];
-    const int total = static_cast<int>(v[0] >> 32);
-    if (!by_count) set_mass = v[3];
+    pass(b);
+    const u64 counts = sum_of(sm, CL, turn, 0), above_n = counts & 0xffffffffull;
+    const u64 above_q = sum_of(sm, CL, turn, 1);
+    const int total = static_cast<int>(counts >> 32);
+    if (!by_count) set_mass = sum_of(sm, CL, turn, 3);
     {
       // kappa is in the list: less than the target lies above it, and no less with it
       const u64 target = by_count ? static_cast<u64>(b.few ? min(k, total) : k)
                                   : max(1ull, part_ceil(fmaxf(p, 0.f), set_mass));
-      const u64 above = by_count ? above_n : above_q, upto = above + (by_count ? total : v[2]);
+      const u64 above = by_count ? above_n : above_q, upto = above + (by_count ? total : sum_of(sm, CL, turn, 2));
       if (total > kList || above >= target || upto < target) return false;
     }
     both = by_count && p < 1.f && b.all;
@@ -988,10 +994,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const __grid_cons
     u64 target = static_cast<u64>(k);
     if (!count) {
       if (set_mass == 0) {
-        u64 v[4] = {0, 0, 0, 0};
-        visit_row([&](bool, uint32_t, u64 w) { v[0] += w; });
-        cluster_sum(sm, CL, rank, turn ^= 1, v);
-        set_mass = v[0];
+        u64 all = 0;
+        visit_row([&](bool, uint32_t, u64 w) { all += w; });
+        turn ^= 1;
+        cluster_sum(sm, CL, rank, turn, all, 0, 0, 0);
+        set_mass = sum_of(sm, CL, turn, 0);
       }
       target = max(1ull, part_ceil(fmaxf(p, 0.f), set_mass));
     }
@@ -1082,9 +1089,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) sample_kernel(const __grid_cons
       sum.add(s.lo);
     });
     put_segment(sm, rank, sum);
-    u64 v[4] = {n, 0, 0, 0};
-    cluster_sum(sm, CL, rank, turn ^= 1, v);
-    kept_count = v[0];
+    turn ^= 1;
+    cluster_sum(sm, CL, rank, turn, n, 0, 0, 0);
+    kept_count = sum_of(sm, CL, turn, 0);
   }
 
   // ---- rank 0 places the random number
@@ -1254,8 +1261,9 @@ cudaError_t launch_e(const SampleArgs& a, int num_sms, cudaStream_t stream) {
   // steps of a row, of which four CTAs of 256 threads overlap more (1783 rows
   // of 1066: 81 us, with 512 threads 132; 2000 of 32003: 204, 230; but 610 of
   // 65536: 118, 113; 1024 of 151936: 356, 330, as fewer rows stay in L2).
-  // Four CTAs a SM leave a thread 64 registers, with spills of about 480 bytes
-  // stored and 720 loaded (512 threads: 80 and 50); the figures include them.
+  // Four CTAs a SM leave a thread 64 registers, with spills of about 490 bytes
+  // stored and 800 loaded (512 threads: 28); three, with a fifth of the spills,
+  // take 5% longer.
   if (a.R > 2ll * num_sms && a.V <= kSmallV) return launch_nt<E, 256>(a, 1, stream);
   // Two CTAs fit a SM: as many CTAs a row as fit at once, none for less than
   // 4096 tokens.  (More CTAs for many rows would keep the rows in work within

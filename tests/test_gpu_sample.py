@@ -369,3 +369,12 @@ def test_masks_of_the_lowest_value(dtype, V, rows, T, limits):
 def test_distributions_of_rows_on_several_ctas(dtype, V, rows, limits):
     """Two, four and eight CTAs a row: the values of the distribution."""
     check(logits(rows, V, 2.5, 61, dtype), 62, **{"T": 0.8, **limits})
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,rows", [(9000, 400), (32003, 310), (32769, 310), (32003, 20)])
+@pytest.mark.parametrize("limits", [dict(k=4500, p=0.9), dict(k=8000, p=0.99, mp=1e-4), dict(k=4097, p=0.5)])
+def test_top_p_of_more_tokens_than_the_list_holds(dtype, V, rows, limits):
+    """top_k beyond the list, then top_p of their sum, found by the search
+    over the row: in blocks of 256 and of 512 threads and in clusters."""
+    check(logits(rows, V, 2.0, 71, dtype), 72, **{"T": 0.7, **limits}, probs=False)
