@@ -298,6 +298,9 @@ def _wrong(what):
     raise ValueError(what)
 
 
+_devices = torch.cuda.device_count()  # (with one, a tensor on a GPU is on the current one)
+
+
 def _elsewhere():
     _wrong("tensors on the current CUDA device wanted")
 
@@ -306,7 +309,7 @@ def _device(t):
     """The device that the library will plan for and launch on, which has to
     be the tensor's."""
     dev = t.get_device()
-    if dev < 0 or dev != torch._C._cuda_getDevice():
+    if dev < 0 or (_devices > 1 and dev != torch._C._cuda_getDevice()):
         _elsewhere()
     return dev
 
@@ -403,15 +406,22 @@ def simsd_rope_append(plan, q, k, v, token_start, prefix_len, q_out, k_cache, v_
     [Bt+1], prefix_len [Bt]; q_out [T][Hq][d] dense; k_cache/v_cache
     [num_pages][Hkv][P][d].  prefix_len is not advanced."""
     T, Hq, d = q.shape
-    Hkv, Bt, dt = k.shape[1], prefix_len.shape[0], q.dtype
-    if k.shape != (T, Hkv, d) or v.shape != (T, Hkv, d) or k.dtype is not dt or v.dtype is not dt:
+    Tk, Hkv, dk = k.shape
+    Bt, dt = prefix_len.shape[0], q.dtype
+    if Tk != T or dk != d or v.shape != (T, Hkv, d) or k.dtype is not dt or v.dtype is not dt:
         _wrong("k / v: [T][Hkv][d] of q's type wanted")
     if q_out.shape != (T, Hq, d) or q_out.dtype is not dt or not q_out.is_contiguous():
         _wrong("q_out: dense, like q")
-    if not _dense_i32(token_start, Bt + 1) or not _dense_i32(prefix_len, Bt):
+    if (token_start.dtype is not _I32 or token_start.numel() != Bt + 1 or not token_start.is_contiguous()
+            or prefix_len.dtype is not _I32 or prefix_len.numel() != Bt or not prefix_len.is_contiguous()):
         _wrong("token_start / prefix_len: dense int32 [Bt+1] / [Bt] wanted")
     if positions is not None and not _dense_i32(positions, T):
         _wrong("positions: dense int32 [T] wanted")
+    (qs, q1, q2), (ks, k1, k2), (vs, v1, v2) = q.stride(), k.stride(), v.stride()
+    if (q1 != d and Hq > 1) or ((k1 != d or v1 != d) and Hkv > 1) or not (q2 == k2 == v2 == 1 or d == 1):
+        _wrong("q / k / v: the heads of a token must be dense")
+    if T <= 1:
+        qs, ks, vs = Hq * d, Hkv * d, Hkv * d
     num_pages, max_pages, P = _cache_sizes(k_cache, v_cache, block_table, Bt, Hkv, d, dt)
     dev = _device(q)
     if not (dev == k.get_device() == v.get_device() == token_start.get_device() == prefix_len.get_device()
@@ -419,10 +429,10 @@ def simsd_rope_append(plan, q, k, v, token_start, prefix_len, q_out, k_cache, v_
             and (positions is None or positions.get_device() == dev)):
         _elsewhere()
     rc = (_lib or load_library()).simsd_rope_append(
-        _code(dt), ctypes.addressof(plan), q.data_ptr(), _rows(q, Hq, d, "q"), k.data_ptr(), _rows(k, Hkv, d, "k"),
-        v.data_ptr(), _rows(v, Hkv, d, "v"), token_start.data_ptr(), prefix_len.data_ptr(), _ptr(positions), T, Bt,
-        Hq, Hkv, d, q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), num_pages, block_table.data_ptr(),
-        max_pages, P, _error_word(err_word, dev), _raw_stream(stream, dev))
+        _code(dt), ctypes.addressof(plan), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
+        token_start.data_ptr(), prefix_len.data_ptr(), _ptr(positions), T, Bt, Hq, Hkv, d, q_out.data_ptr(),
+        k_cache.data_ptr(), v_cache.data_ptr(), num_pages, block_table.data_ptr(), max_pages, P,
+        _error_word(err_word, dev), _raw_stream(stream, dev))
     if rc:
         _check(rc, "simsd_rope_append")
 
