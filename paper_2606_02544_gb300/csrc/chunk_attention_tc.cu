@@ -37,8 +37,8 @@
 // Bound: the softmax (exponentials, conversions and maxima of 2 x 128 x 128
 // scores: about 2000 of the 2530 cycles, the two products 1024) for prompts,
 // HBM for single tokens.  Measured, 32 heads on 8, d 128: 8192 tokens of one
-// prompt 433 us (1.3 PFLOP/s of the two products, causal), 2048 after 32768
-// 762 us (1.5); 64 single tokens over 2048 to 8192 rows 214 us (6.3 TB/s); 8
+// prompt 434 us (1.3 PFLOP/s of the two products, causal), 2048 after 32768
+// 765 us (1.5); 64 single tokens over 2048 to 8192 rows 214 us (6.3 TB/s); 8
 // over 512 to 1024, 16 heads, 20 us, most of it one CTA's chain from the
 // tokens' offsets to its first tile and the second launch.
 // TMEM (512 columns): S_A [0,128), S_B [128,256), O_A [256,384), O_B

@@ -33,13 +33,13 @@
 // Counting all of a row costs one shared-memory reduction a token, which HBM
 // can feed; counts of an eighth of it left brackets of thousands of tokens
 // under heavy-tailed weights and a third pass over the row (1024 rows of
-// 151936: 898 us, this way 327).
+// 151936: 898 us, this way 320).
 //
-// Measured, 151936 logits of fp32: 1024 rows 327 us (1.9 TB/s of the bytes
+// Measured, 151936 logits of fp32: 1024 rows 320 us (1.9 TB/s of the bytes
 // read once, 3.8 of those read; each pass about 70% of the time in the
-// instructions of a token, 16 and 11, and HBM), 8 rows 25 us (a chain of
+// instructions of a token, 16 and 11, and HBM), 8 rows 23 us (a chain of
 // passes and exchanges over a cluster); 132 rows of 32003 in bf16 with their
-// distribution 52 us.
+// distribution 51 us.
 //
 // A thread-block cluster serves a row: one CTA where there are many rows (of
 // 256 threads where they are short), up to eight where there are few.
