@@ -82,6 +82,9 @@ extern "C" {
 #define SIMSD_EW_ACCEPT_LEN 32u /* an accepted length is outside [0, gamma] */
 #define SIMSD_EW_TOKENS 64u     /* token offsets not in order or outside [0, T] */
 #define SIMSD_EW_SAMPLE 128u    /* a row's sampling parameters are out of range, or no logit is above -inf */
+#define SIMSD_EW_POOL 256u      /* fewer free pages than a call wants: it has changed nothing */
+#define SIMSD_EW_SEQ 512u       /* a sequence number out of range, or a fork's destination named twice or also a source */
+#define SIMSD_EW_SHARED 1024u   /* a page that is to be written is held by more than one sequence */
 
 /* rotary layouts: which components make a pair (r = rot_dim) */
 #define SIMSD_ROPE_HALF 0        /* (x_i, x_{i + r/2}) */
@@ -482,6 +485,179 @@ SIMSD_API int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, 
                                     int page_size, int T, int Bt, int Hq, int Hkv, int d, int mask_block, int window,
                                     float softmax_scale, void* out, float* lse, void* workspace,
                                     size_t workspace_bytes, int32_t* err_word, void* stream);
+
+/*
+ * Long caches.  The calls below keep the cache of long sequences small: rows
+ * in 4 bits, windows whose first rows stay visible (so that the pages between
+ * can be released), pages shared by forked sequences.  The paper has no
+ * counterpart; they extend its Sec. 3.3 cache.
+ */
+
+/*
+ * simsd_chunk_attention_sinks -- simsd_chunk_attention through a window whose
+ * first rows stay visible: token i of sequence b, at row p = prefix_len[b] +
+ * i, sees the rows j < hi with
+ *   lo <= j   or   ks <= j < ks + sinks,   ks = max(0, key_start[b]),
+ * hi and lo as there.  sinks >= 0; 0, or no window (window = 0), makes it
+ * simsd_chunk_attention.  Rows that no token of a group of neighbouring
+ * tokens sees are never used, nor their pages: between the first rows and the
+ * window the block table may hold -1 (simsd_pages_release).  All else,
+ * workspace and limits included, is as for simsd_chunk_attention.
+ */
+SIMSD_API int simsd_chunk_attention_sinks(int dtype, const void* q, int64_t q_stride, const int32_t* token_start,
+                                          const int32_t* prefix_len, const int32_t* key_start, const void* k_cache,
+                                          const void* v_cache, int num_pages, const int32_t* block_table,
+                                          int max_pages, int page_size, int T, int Bt, int Hq, int Hkv, int d,
+                                          int mask_block, int window, int sinks, float softmax_scale, void* out,
+                                          float* lse, void* workspace, size_t workspace_bytes, int32_t* err_word,
+                                          void* stream);
+
+/*
+ * simsd_q4_cache -- a paged cache in 4 bits (host struct, device pointers).
+ * The d components of a row are held in groups of 16:
+ *   x = unit * scale * code
+ * with code one of 0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives (4 bits: sign,
+ * two of exponent, one of fraction; component 2i in the low half of byte i),
+ * scale an 8-bit number with 4 bits of exponent and 3 of fraction (the sign
+ * bit is 0), and unit one number for all keys or all values.
+ *   k_codes, v_codes   [num_pages][Hkv][page_size][d/2] bytes
+ *   k_scales, v_scales [num_pages][Hkv][page_size][d/16] bytes
+ * 72 bytes a row of 128 components.  scale * code has 6 significant bits, so
+ * it is exact in bf16.  A unit > 0 (1 is usual) places the range of the scales,
+ * 2^-9 to 448, where the groups' largest values over 6 lie.
+ */
+typedef struct simsd_q4_cache {
+  void *k_codes, *k_scales, *v_codes, *v_scales;
+  float k_unit, v_unit;
+} simsd_q4_cache;
+
+/*
+ * simsd_rope_append_q4 -- simsd_rope_append to a cache in 4 bits.  A group's
+ * scale is the largest magnitude of (rotated) x / unit over 6, rounded to the
+ * nearest 8-bit number, at least 2^-9 and at most 448; a code is the nearest
+ * to x / (unit scale), ties to the even one, at most 6 in magnitude.  Keys are
+ * rotated in fp32 and not rounded to dtype before.  A group that holds NaN
+ * reads back as NaN.  d is 64 or 128; all else, q_out and the error rules
+ * included, is as for simsd_rope_append.
+ */
+SIMSD_API int simsd_rope_append_q4(int dtype, const simsd_rope_plan* plan, const void* q, int64_t q_stride,
+                                   const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                   const int32_t* token_start, const int32_t* prefix_len, const int32_t* positions,
+                                   int T, int Bt, int Hq, int Hkv, int d, void* q_out, const simsd_q4_cache* cache,
+                                   int num_pages, const int32_t* block_table, int max_pages, int page_size,
+                                   int32_t* err_word, void* stream);
+
+/*
+ * simsd_q4_expand -- writes what the cache holds in rows [first[b], last[b])
+ * of each sequence to the same rows of a cache in dtype with the same pages
+ * (for calls that read such a cache, simsd_verify_attention for one).
+ *   first, last [Bt] int32; an empty or reversed range is no row
+ *   k_cache, v_cache [num_pages][Hkv][page_size][d] dtype
+ * A range outside the block table sets SIMSD_EW_PREFIX_LEN, and a page id out
+ * of the pool SIMSD_EW_PAGE; the sequence, or the rows of that page, are left
+ * as they were.  A row that two sequences share is written with the same
+ * values by both.
+ */
+SIMSD_API int simsd_q4_expand(int dtype, const simsd_q4_cache* cache, int num_pages, const int32_t* block_table,
+                              int max_pages, int page_size, const int32_t* first, const int32_t* last, int Bt,
+                              int Hkv, int d, void* k_cache, void* v_cache, int32_t* err_word, void* stream);
+
+/*
+ * simsd_chunk_q4_workspace_bytes -- bytes of scratch simsd_chunk_attention_q4
+ * needs for these sizes on the current device.
+ *
+ * simsd_chunk_attention_q4 -- simsd_chunk_attention_sinks over a cache in 4
+ * bits (sinks = 0: simsd_chunk_attention).  q and out are dtype.  The same
+ * masks, error rules and limits.
+ * SIMSD_BF16 with up to 64 query rows a sequence and KV head on average (T Hq
+ * <= 64 Bt Hkv, Hq / Hkv <= 64) reads the codes; keys and values are exact in
+ * the products' fp16, q is scaled by a power of two to its row's largest
+ * component, probabilities are rounded to fp16.  More rows, and SIMSD_F32, go
+ * through an image of the rows that are seen in dtype, with the cache's page
+ * ids, in the workspace (num_pages Hkv page_size d elements of keys and of
+ * values): make the workspace once for all layers of a model.
+ */
+SIMSD_API size_t simsd_chunk_q4_workspace_bytes(int dtype, int T, int Bt, int Hq, int Hkv, int d, int max_pages,
+                                                int page_size, int num_pages);
+SIMSD_API int simsd_chunk_attention_q4(int dtype, const void* q, int64_t q_stride, const int32_t* token_start,
+                                       const int32_t* prefix_len, const int32_t* key_start,
+                                       const simsd_q4_cache* cache, int num_pages, const int32_t* block_table,
+                                       int max_pages, int page_size, int T, int Bt, int Hq, int Hkv, int d,
+                                       int mask_block, int window, int sinks, float softmax_scale, void* out,
+                                       float* lse, void* workspace, size_t workspace_bytes, int32_t* err_word,
+                                       void* stream);
+
+/*
+ * Pages.  refs [num_pages] int32 counts the block-table entries that name a
+ * page; a page is free where it is 0, and an entry that names none is -1.
+ * Zeroed counts and a table of -1 are an empty pool.  The calls work on the
+ * device alone (a CUDA graph of them does the same with other lengths), take
+ * the lowest free pages first and give the same result every time.  A table
+ * entry that is neither -1 nor a page id sets SIMSD_EW_PAGE and counts as -1.
+ * block_table is [Bt][max_pages], Bt at most 65536.
+ */
+
+/* One array of a cache: layer l of page p is the page_bytes bytes at base + l
+ * layer_bytes + p page_bytes (all multiples of 16; layers >= 1). */
+typedef struct simsd_page_array {
+  void* base;
+  int64_t page_bytes;
+  int64_t layer_bytes;
+  int64_t layers;
+} simsd_page_array;
+#define SIMSD_MAX_PAGE_ARRAYS 8
+
+/*
+ * simsd_pages_extend -- room for the next rows: every entry of the rows
+ * [lens[b], lens[b] + add[b]) of a sequence that names no page gets a free
+ * one (in the order of sequences, then rows).  lens is not changed.
+ * Fewer free pages than wanted set SIMSD_EW_POOL and nothing is changed.  A
+ * length or addend that is negative or passes the table sets
+ * SIMSD_EW_PREFIX_LEN, a page among them that another entry shares (a
+ * sequence cut back into pages that it shares with a fork)
+ * SIMSD_EW_SHARED: that sequence gets no page.
+ */
+SIMSD_API int simsd_pages_extend(const int32_t* lens, const int32_t* add, int32_t* block_table, int32_t* refs,
+                                 int num_pages, int Bt, int max_pages, int page_size, int32_t* err_word,
+                                 void* stream);
+
+/*
+ * simsd_pages_release -- sequence seq[i] (NULL: i, n = Bt) lets go of the
+ * pages that lie wholly within its rows [first[i], last[i]): 0 and 2^31 - 1
+ * release all of it, the first visible rows and the window's start what is
+ * no longer seen.  The entries become -1.  seq may name a sequence twice.
+ */
+SIMSD_API int simsd_pages_release(const int32_t* seq, const int32_t* first, const int32_t* last, int n,
+                                  int32_t* block_table, int32_t* refs, int num_pages, int Bt, int max_pages,
+                                  int page_size, int32_t* err_word, void* stream);
+
+/*
+ * simsd_pages_workspace_bytes -- bytes of scratch (16-byte aligned) that
+ * simsd_pages_fork of `pairs` pairs and simsd_pages_compact need.
+ *
+ * simsd_pages_fork -- sequence dst[i] becomes a copy of sequence src[i]: the
+ * pages that src[i]'s lens rows fill are shared, the last one where it is
+ * filled in part is copied to a free page (pairs in order), so that both
+ * may go on, and lens[dst[i]] = lens[src[i]].  What dst[i] held is released
+ * (and is not yet free to this call).  One src may have many dst.
+ *   arrays  n_arrays host structs: all that the pages hold, in every layer
+ * A pair whose dst is named twice or is also a src, or with a number outside
+ * [0, Bt), sets SIMSD_EW_SEQ, one with a bad length SIMSD_EW_PREFIX_LEN: it is
+ * left out.  Too few free pages set SIMSD_EW_POOL and nothing is changed.
+ *
+ * simsd_pages_compact -- moves the live pages to the lowest ids: the k-th
+ * live page above the count of live ones goes to the k-th free one below it,
+ * in contents, tables and counts.  live [1] int32 out or NULL: that count.
+ * Pages at and above it are free then; their contents are left as they were.
+ */
+SIMSD_API size_t simsd_pages_workspace_bytes(int num_pages, int pairs);
+SIMSD_API int simsd_pages_fork(const simsd_page_array* arrays, int n_arrays, const int32_t* src, const int32_t* dst,
+                               int n, int32_t* lens, int32_t* block_table, int32_t* refs, int num_pages, int Bt,
+                               int max_pages, int page_size, void* workspace, size_t workspace_bytes,
+                               int32_t* err_word, void* stream);
+SIMSD_API int simsd_pages_compact(const simsd_page_array* arrays, int n_arrays, int32_t* block_table, int32_t* refs,
+                                  int num_pages, int Bt, int max_pages, int32_t* live, void* workspace,
+                                  size_t workspace_bytes, int32_t* err_word, void* stream);
 
 /*
  * simsd_sample -- draws one token from each row of logits with a given

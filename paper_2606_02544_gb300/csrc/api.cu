@@ -628,30 +628,56 @@ size_t simsd_chunk_workspace_bytes(int dtype, int T, int Bt, int Hq, int Hkv, in
   return simsd::chunk_tc_workspace_bytes(T, Bt, d, info.num_sms);
 }
 
-int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, const int32_t* token_start,
-                          const int32_t* prefix_len, const int32_t* key_start, const void* k_cache,
-                          const void* v_cache, int num_pages, const int32_t* block_table, int max_pages,
-                          int page_size, int T, int Bt, int Hq, int Hkv, int d, int mask_block, int window,
-                          float softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
-                          int32_t* err_word, void* stream) {
+namespace {
+
+int check_chunk(int dtype, const void* q, int64_t q_stride, const int32_t* token_start, const int32_t* prefix_len,
+                int num_pages, const int32_t* block_table, int max_pages, int page_size, int T, int Bt, int Hq,
+                int Hkv, int d, int mask_block, int window, int sinks, float softmax_scale, const void* out) {
   if (dtype != SIMSD_F32 && dtype != SIMSD_BF16) return unsupported("dtype");
   const int eb = dtype == SIMSD_F32 ? 4 : 2;
   if (T < 0 || Bt < 0) return arg_fail("T < 0 or Bt < 0");
   if (Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0) return arg_fail("Hq must be a positive multiple of Hkv");
-  if (num_pages < 0 || max_pages < 0 || mask_block < 0 || window < 0) return arg_fail("negative size");
+  if (num_pages < 0 || max_pages < 0 || mask_block < 0 || window < 0 || sinks < 0) return arg_fail("negative size");
   if (!page_size_ok(page_size)) return unsupported("page_size must be a multiple of 64 or a divisor of 64 (>= 8)");
   if (d != 64 && d != 128) return unsupported("d must be 64 or 128");
   if (!(softmax_scale >= 0.f) || std::isinf(softmax_scale)) return arg_fail("softmax_scale");
   if (static_cast<long long>(max_pages) * page_size > 0x7fffff00ll) return unsupported("more than 2^31 rows a sequence");
   if (static_cast<long long>(T) * Hq >= (1ll << 31)) return unsupported("too many query rows");
   if (T == 0 || Bt == 0) return SIMSD_OK;
-  if (!token_start || !prefix_len || !block_table || !k_cache || !v_cache || !out) return arg_fail("null pointer");
+  if (!token_start || !prefix_len || !block_table || !out) return arg_fail("null pointer");
   if (num_pages == 0 || max_pages == 0) return arg_fail("no pages");
   if (!rows_ok(q, q_stride, Hq, d, eb)) return arg_fail("q: null, misaligned or overlapping rows");
-  if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out))
-    return arg_fail("tensor pointers must be 16-byte aligned");
+  if (!aligned16(out)) return arg_fail("tensor pointers must be 16-byte aligned");
+  return SIMSD_OK;
+}
+// the limits of the tensor-core kernel
+int check_chunk_tc(int T, int Bt, int Hq, int Hkv, int num_pages, int max_pages, int page_size) {
+  if (Hq / Hkv > 128) return unsupported("Hq / Hkv above 128");
+  if (Bt > simsd::kChunkMaxSeqs) return unsupported("more than 16384 sequences");
+  if (static_cast<long long>(num_pages) * Hkv * page_size >= (1ll << 31))
+    return unsupported("page pool too large for 32-bit TMA row coordinates");
+  // key tiles are counted in 32 bits (2^31 of them take some 20 s)
+  const long long max_keys = static_cast<long long>(max_pages) * page_size;
+  if ((static_cast<long long>(T) * Hq / 128 + static_cast<long long>(Bt) * Hkv + 1) * (max_keys / 128 + 1) >= (1ll << 31))
+    return unsupported("too many key tiles in one call");
+  return SIMSD_OK;
+}
+
+// simsd_chunk_attention (sinks 0) and simsd_chunk_attention_sinks.
+int chunk_attention_impl(int dtype, const void* q, int64_t q_stride, const int32_t* token_start,
+                          const int32_t* prefix_len, const int32_t* key_start, const void* k_cache,
+                          const void* v_cache, int num_pages, const int32_t* block_table, int max_pages,
+                          int page_size, int T, int Bt, int Hq, int Hkv, int d, int mask_block, int window,
+                         int sinks, float softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                          int32_t* err_word, void* stream) {
+  int rc = check_chunk(dtype, q, q_stride, token_start, prefix_len, num_pages, block_table, max_pages, page_size, T, Bt,
+                       Hq, Hkv, d, mask_block, window, sinks, softmax_scale, out);
+  if (rc != SIMSD_OK) return rc;
+  if (T == 0 || Bt == 0) return SIMSD_OK;
+  if (!k_cache || !v_cache) return arg_fail("null pointer");
+  if (!aligned16(k_cache) || !aligned16(v_cache)) return arg_fail("tensor pointers must be 16-byte aligned");
   DeviceInfo info;
-  int rc = require_sm103(&info);
+  rc = require_sm103(&info);
   if (rc != SIMSD_OK) return rc;
   simsd::ChunkArgs a{};
   a.q = q;
@@ -675,6 +701,7 @@ int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, const int3
   a.page_size = page_size;
   a.mask_block = mask_block;
   a.window = window;
+  a.sinks = window > 0 ? sinks : 0;
   a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt(static_cast<float>(d));
   const long long max_keys = static_cast<long long>(max_pages) * page_size;
   const size_t need = dtype == SIMSD_F32
@@ -687,17 +714,364 @@ int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, const int3
     cudaError_t e = simsd::launch_chunk_attention_f32(a, info.num_sms, as_stream(stream));
     return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "chunk_attention_f32 launch");
   }
-  if (Hq / Hkv > 128) return unsupported("Hq / Hkv above 128");
-  if (Bt > simsd::kChunkMaxSeqs) return unsupported("more than 16384 sequences");
-  if (static_cast<long long>(num_pages) * Hkv * page_size >= (1ll << 31))
-    return unsupported("page pool too large for 32-bit TMA row coordinates");
-  // key tiles are counted in 32 bits (2^31 of them take some 20 s)
-  if ((static_cast<long long>(T) * Hq / 128 + static_cast<long long>(Bt) * Hkv + 1) * (max_keys / 128 + 1) >= (1ll << 31))
-    return unsupported("too many key tiles in one call");
+  rc = check_chunk_tc(T, Bt, Hq, Hkv, num_pages, max_pages, page_size);
+  if (rc != SIMSD_OK) return rc;
   simsd::EncodeTiledFn enc = encoder();
   if (!enc) return cuda_fail(cudaErrorNotSupported, "cuTensorMapEncodeTiled entry point");
   cudaError_t e = simsd::launch_chunk_attention_tc(a, info.num_sms, enc, as_stream(stream));
   return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "chunk_attention_tc launch");
+}
+
+}  // namespace
+
+int simsd_chunk_attention(int dtype, const void* q, int64_t q_stride, const int32_t* token_start,
+                          const int32_t* prefix_len, const int32_t* key_start, const void* k_cache,
+                          const void* v_cache, int num_pages, const int32_t* block_table, int max_pages,
+                          int page_size, int T, int Bt, int Hq, int Hkv, int d, int mask_block, int window,
+                          float softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                          int32_t* err_word, void* stream) {
+  return chunk_attention_impl(dtype, q, q_stride, token_start, prefix_len, key_start, k_cache, v_cache, num_pages,
+                              block_table, max_pages, page_size, T, Bt, Hq, Hkv, d, mask_block, window, 0,
+                              softmax_scale, out, lse, workspace, workspace_bytes, err_word, stream);
+}
+
+int simsd_chunk_attention_sinks(int dtype, const void* q, int64_t q_stride, const int32_t* token_start,
+                                const int32_t* prefix_len, const int32_t* key_start, const void* k_cache,
+                                const void* v_cache, int num_pages, const int32_t* block_table, int max_pages,
+                                int page_size, int T, int Bt, int Hq, int Hkv, int d, int mask_block, int window,
+                                int sinks, float softmax_scale, void* out, float* lse, void* workspace,
+                                size_t workspace_bytes, int32_t* err_word, void* stream) {
+  return chunk_attention_impl(dtype, q, q_stride, token_start, prefix_len, key_start, k_cache, v_cache, num_pages,
+                              block_table, max_pages, page_size, T, Bt, Hq, Hkv, d, mask_block, window, sinks,
+                              softmax_scale, out, lse, workspace, workspace_bytes, err_word, stream);
+}
+
+namespace {
+
+bool q4_ok(const simsd_q4_cache* c) {
+  return c && c->k_codes && c->k_scales && c->v_codes && c->v_scales && aligned16(c->k_codes) &&
+         aligned16(c->k_scales) && aligned16(c->v_codes) && aligned16(c->v_scales) && c->k_unit > 0.f &&
+         c->v_unit > 0.f && !std::isinf(c->k_unit) && !std::isinf(c->v_unit);
+}
+int q4_fail() { return arg_fail("cache: null or misaligned arrays, or a unit that is not positive and finite"); }
+
+}  // namespace
+
+int simsd_rope_append_q4(int dtype, const simsd_rope_plan* plan, const void* q, int64_t q_stride, const void* k,
+                         int64_t k_stride, const void* v, int64_t v_stride, const int32_t* token_start,
+                         const int32_t* prefix_len, const int32_t* positions, int T, int Bt, int Hq, int Hkv, int d,
+                         void* q_out, const simsd_q4_cache* cache, int num_pages, const int32_t* block_table,
+                         int max_pages, int page_size, int32_t* err_word, void* stream) {
+  if (dtype != SIMSD_F32 && dtype != SIMSD_BF16) return unsupported("dtype");
+  const int eb = dtype == SIMSD_F32 ? 4 : 2;
+  if (T < 0 || Bt < 0 || Hq <= 0 || Hkv <= 0 || num_pages < 0 || max_pages < 0) return arg_fail("sizes");
+  if (d != 64 && d != 128) return unsupported("d must be 64 or 128");
+  if (!page_size_ok(page_size)) return unsupported("page_size must be a multiple of 64 or a divisor of 64 (>= 8)");
+  if (static_cast<long long>(max_pages) * page_size > 0x7fffff00ll) return unsupported("more than 2^31 rows a sequence");
+  int rc = check_rope_plan(plan, d);
+  if (rc != SIMSD_OK) return rc;
+  if (T > kMaxRopeTokens) return unsupported("too many tokens");
+  if (T == 0 || Bt == 0) return SIMSD_OK;
+  if (!token_start || !prefix_len || !block_table) return arg_fail("null pointer");
+  if (!q4_ok(cache)) return q4_fail();
+  if (!rows_ok(q, q_stride, Hq, d, eb) || !rows_ok(k, k_stride, Hkv, d, eb) || !rows_ok(v, v_stride, Hkv, d, eb))
+    return arg_fail("q / k / v: null, misaligned or overlapping rows");
+  if (!q_out || !aligned16(q_out)) return arg_fail("tensor pointers must be 16-byte aligned");
+  DeviceInfo info;
+  rc = require_sm103(&info);
+  if (rc != SIMSD_OK) return rc;
+  simsd::RopeArgs a{};
+  a.plan = *plan;
+  a.q = q;
+  a.q_stride = q_stride;
+  a.k = k;
+  a.k_stride = k_stride;
+  a.v = v;
+  a.v_stride = v_stride;
+  a.q_out = q_out;
+  a.q_out_stride = static_cast<long long>(Hq) * d;
+  a.token_start = token_start;
+  a.prefix_len = prefix_len;
+  a.positions = positions;
+  a.block_table = block_table;
+  a.err_word = err_word;
+  a.T = T;
+  a.Bt = Bt;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.num_pages = num_pages;
+  a.max_pages = max_pages;
+  a.page_size = page_size;
+  cudaError_t e = simsd::launch_rope_q4(eb, a, *cache, info.num_sms, as_stream(stream));
+  return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "rope_append_q4 launch");
+}
+
+int simsd_q4_expand(int dtype, const simsd_q4_cache* cache, int num_pages, const int32_t* block_table, int max_pages,
+                    int page_size, const int32_t* first, const int32_t* last, int Bt, int Hkv, int d, void* k_cache,
+                    void* v_cache, int32_t* err_word, void* stream) {
+  if (dtype != SIMSD_F32 && dtype != SIMSD_BF16) return unsupported("dtype");
+  if (Bt < 0 || Hkv <= 0 || num_pages < 0 || max_pages < 0) return arg_fail("sizes");
+  if (d != 64 && d != 128) return unsupported("d must be 64 or 128");
+  if (!page_size_ok(page_size)) return unsupported("page_size must be a multiple of 64 or a divisor of 64 (>= 8)");
+  if (static_cast<long long>(max_pages) * page_size > 0x7fffff00ll) return unsupported("more than 2^31 rows a sequence");
+  if (static_cast<long long>(Hkv) * page_size * d >= (1ll << 31)) return unsupported("page too large");
+  if (Bt == 0) return SIMSD_OK;
+  if (!first || !last || !block_table || !k_cache || !v_cache) return arg_fail("null pointer");
+  if (!q4_ok(cache)) return q4_fail();
+  if (!aligned16(k_cache) || !aligned16(v_cache)) return arg_fail("tensor pointers must be 16-byte aligned");
+  DeviceInfo info;
+  const int rc = require_sm103(&info);
+  if (rc != SIMSD_OK) return rc;
+  simsd::ExpandArgs a{};
+  a.c = *cache;
+  a.first = first;
+  a.last = last;
+  a.block_table = block_table;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.err_word = err_word;
+  a.num_pages = num_pages;
+  a.max_pages = max_pages;
+  a.page_size = page_size;
+  a.Bt = Bt;
+  a.Hkv = Hkv;
+  a.d = d;
+  cudaError_t e = simsd::launch_q4_expand(dtype == SIMSD_F32 ? 4 : 2, a, info.num_sms, as_stream(stream));
+  return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "q4_expand launch");
+}
+
+namespace {
+
+// The image of keys (and again of values) that longer chunks are attended
+// through: its bytes, to the next multiple of 256.
+size_t q4_image_bytes(int dtype, int num_pages, int Hkv, int page_size, int d) {
+  const size_t n = static_cast<size_t>(num_pages) * Hkv * page_size * d * (dtype == SIMSD_F32 ? 4 : 2);
+  return (n + 255) / 256 * 256;
+}
+
+}  // namespace
+
+size_t simsd_chunk_q4_workspace_bytes(int dtype, int T, int Bt, int Hq, int Hkv, int d, int max_pages, int page_size,
+                                      int num_pages) {
+  if ((dtype != SIMSD_BF16 && dtype != SIMSD_F32) || T <= 0 || Bt <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 ||
+      (d != 64 && d != 128) || max_pages < 0 || page_size <= 0 || num_pages < 0)
+    return 0;
+  DeviceInfo info;
+  if (device_info(&info) != SIMSD_OK) return 0;
+  if (simsd::chunk_q4_few(dtype, T, Bt, Hq, Hkv)) return simsd::chunk_q4_workspace_bytes(T, Bt, Hq, Hkv, d, info.num_sms);
+  return 2 * q4_image_bytes(dtype, num_pages, Hkv, page_size, d) +
+         simsd_chunk_workspace_bytes(dtype, T, Bt, Hq, Hkv, d, max_pages, page_size);
+}
+
+int simsd_chunk_attention_q4(int dtype, const void* q, int64_t q_stride, const int32_t* token_start,
+                             const int32_t* prefix_len, const int32_t* key_start, const simsd_q4_cache* cache,
+                             int num_pages, const int32_t* block_table, int max_pages, int page_size, int T, int Bt,
+                             int Hq, int Hkv, int d, int mask_block, int window, int sinks, float softmax_scale,
+                             void* out, float* lse, void* workspace, size_t workspace_bytes, int32_t* err_word,
+                             void* stream) {
+  simsd::ChunkArgs a{};
+  const int eb = dtype == SIMSD_F32 ? 4 : 2;
+  int rc = check_chunk(dtype, q, q_stride, token_start, prefix_len, num_pages, block_table, max_pages, page_size, T, Bt,
+                       Hq, Hkv, d, mask_block, window, sinks, softmax_scale, out);
+  if (rc != SIMSD_OK) return rc;
+  if (T == 0 || Bt == 0) return SIMSD_OK;
+  if (!q4_ok(cache)) return q4_fail();
+  if (static_cast<long long>(Hkv) * page_size * d >= (1ll << 31)) return unsupported("page too large");
+  DeviceInfo info;
+  rc = require_sm103(&info);
+  if (rc != SIMSD_OK) return rc;
+  const size_t need = simsd_chunk_q4_workspace_bytes(dtype, T, Bt, Hq, Hkv, d, max_pages, page_size, num_pages);
+  if (!workspace || workspace_bytes < need || !aligned16(workspace))
+    return arg_fail("workspace smaller than simsd_chunk_q4_workspace_bytes()");
+  a.q = q;
+  a.q_stride = q_stride;
+  a.token_start = token_start;
+  a.prefix_len = prefix_len;
+  a.key_start = key_start;
+  a.block_table = block_table;
+  a.out = out;
+  a.lse = lse;
+  a.err_word = err_word;
+  a.T = T;
+  a.Bt = Bt;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.num_pages = num_pages;
+  a.max_pages = max_pages;
+  a.page_size = page_size;
+  a.mask_block = mask_block;
+  a.window = window;
+  a.sinks = window > 0 ? sinks : 0;
+  a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt(static_cast<float>(d));
+  if (simsd::chunk_q4_few(dtype, T, Bt, Hq, Hkv)) {
+    if (Bt > simsd::kChunkMaxSeqs) return unsupported("more than 16384 sequences");
+    // units of at least Hq / Hkv rows, key tiles of 128 rows, counted in 32 bits
+    const long long max_keys = static_cast<long long>(max_pages) * page_size;
+    if ((static_cast<long long>(T) * Hkv + static_cast<long long>(Bt) * Hkv + 1) * (max_keys / 128 + 1) >= (1ll << 31))
+      return unsupported("too many key tiles in one call");
+    a.workspace = workspace;
+    cudaError_t e = simsd::launch_chunk_attention_q4(a, *cache, info.num_sms, as_stream(stream));
+    return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "chunk_attention_q4 launch");
+  }
+  const size_t image = q4_image_bytes(dtype, num_pages, Hkv, page_size, d);
+  uint8_t *k_image = static_cast<uint8_t*>(workspace), *v_image = k_image + image;
+  const size_t rest = workspace_bytes - 2 * image;
+  // (the limits of the call that reads the image are checked before it is made)
+  if (dtype == SIMSD_BF16) {
+    rc = check_chunk_tc(T, Bt, Hq, Hkv, num_pages, max_pages, page_size);
+    if (rc != SIMSD_OK) return rc;
+  }
+  cudaError_t e = simsd::launch_q4_expand_seen(eb, a, *cache, k_image, v_image, info.num_sms, as_stream(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "q4_expand launch");
+  return chunk_attention_impl(dtype, q, q_stride, token_start, prefix_len, key_start, k_image, v_image, num_pages,
+                              block_table, max_pages, page_size, T, Bt, Hq, Hkv, d, mask_block, window, sinks,
+                              softmax_scale, out, lse, rest ? v_image + image : nullptr, rest, err_word, stream);
+}
+
+namespace {
+
+int check_pages(int32_t* block_table, int32_t* refs, int num_pages, int Bt, int max_pages) {
+  if (num_pages < 0 || Bt < 0 || max_pages < 0) return arg_fail("sizes");
+  if (Bt > simsd::kPagesMaxSeqs) return unsupported("more than 65536 sequences");
+  if (num_pages > 0x7fff0000) return unsupported("too many pages");
+  if (Bt == 0 || max_pages == 0) return SIMSD_OK;
+  if (!block_table || (num_pages > 0 && !refs)) return arg_fail("null pointer");
+  if (!aligned16(refs)) return arg_fail("refs must be 16-byte aligned");
+  return SIMSD_OK;
+}
+int check_rows(int max_pages, int page_size) {
+  if (page_size <= 0) return arg_fail("page_size");
+  if (static_cast<long long>(max_pages) * page_size > 0x7fffff00ll) return unsupported("more than 2^31 rows a sequence");
+  return SIMSD_OK;
+}
+int check_arrays(const simsd_page_array* arrays, int n, int num_pages, simsd::PageArrays* out) {
+  if (n < 0 || n > SIMSD_MAX_PAGE_ARRAYS || (n > 0 && !arrays)) return arg_fail("arrays: 0 to 8");
+  out->n = n;
+  for (int i = 0; i < n; ++i) {
+    const simsd_page_array& x = arrays[i];
+    if (!x.base || !aligned16(x.base) || x.page_bytes <= 0 || x.page_bytes % 16 != 0 || x.layers < 1 ||
+        x.layer_bytes % 16 != 0 || (x.layers > 1 && x.layer_bytes / x.page_bytes < num_pages))
+      return arg_fail("arrays: null or misaligned, sizes no multiples of 16 bytes, or layers that overlap");
+    out->array[i] = x;
+  }
+  return SIMSD_OK;
+}
+
+}  // namespace
+
+int simsd_pages_extend(const int32_t* lens, const int32_t* add, int32_t* block_table, int32_t* refs, int num_pages,
+                       int Bt, int max_pages, int page_size, int32_t* err_word, void* stream) {
+  int rc = check_pages(block_table, refs, num_pages, Bt, max_pages);
+  if (rc == SIMSD_OK) rc = check_rows(max_pages, page_size);
+  if (rc != SIMSD_OK) return rc;
+  if (Bt == 0) return SIMSD_OK;
+  if (!lens || !add) return arg_fail("null pointer");
+  DeviceInfo info;
+  rc = require_sm103(&info);
+  if (rc != SIMSD_OK) return rc;
+  simsd::PagesArgs a{};
+  a.lens = const_cast<int32_t*>(lens);
+  a.add = add;
+  a.block_table = block_table;
+  a.refs = refs;
+  a.err_word = err_word;
+  a.num_pages = num_pages;
+  a.Bt = Bt;
+  a.max_pages = max_pages;
+  a.page_size = page_size;
+  cudaError_t e = simsd::launch_pages_extend(a, as_stream(stream));
+  return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "pages_extend launch");
+}
+
+int simsd_pages_release(const int32_t* seq, const int32_t* first, const int32_t* last, int n, int32_t* block_table,
+                        int32_t* refs, int num_pages, int Bt, int max_pages, int page_size, int32_t* err_word,
+                        void* stream) {
+  int rc = check_pages(block_table, refs, num_pages, Bt, max_pages);
+  if (rc == SIMSD_OK) rc = check_rows(max_pages, page_size);
+  if (rc != SIMSD_OK) return rc;
+  if (n < 0 || (!seq && n != Bt)) return arg_fail("n: the length of seq, or Bt without it");
+  if (n == 0 || max_pages == 0) return SIMSD_OK;
+  if (!first || !last) return arg_fail("null pointer");
+  DeviceInfo info;
+  rc = require_sm103(&info);
+  if (rc != SIMSD_OK) return rc;
+  simsd::PagesArgs a{};
+  a.seq = seq;
+  a.first = first;
+  a.last = last;
+  a.n = n;
+  a.block_table = block_table;
+  a.refs = refs;
+  a.err_word = err_word;
+  a.num_pages = num_pages;
+  a.Bt = Bt;
+  a.max_pages = max_pages;
+  a.page_size = page_size;
+  cudaError_t e = simsd::launch_pages_release(a, info.num_sms, as_stream(stream));
+  return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "pages_release launch");
+}
+
+size_t simsd_pages_workspace_bytes(int num_pages, int pairs) {
+  return num_pages < 0 || pairs < 0 ? 0 : simsd::pages_workspace_bytes(num_pages, pairs);
+}
+
+int simsd_pages_fork(const simsd_page_array* arrays, int n_arrays, const int32_t* src, const int32_t* dst, int n,
+                     int32_t* lens, int32_t* block_table, int32_t* refs, int num_pages, int Bt, int max_pages,
+                     int page_size, void* workspace, size_t workspace_bytes, int32_t* err_word, void* stream) {
+  simsd::PagesArgs a{};
+  int rc = check_pages(block_table, refs, num_pages, Bt, max_pages);
+  if (rc == SIMSD_OK) rc = check_rows(max_pages, page_size);
+  if (rc == SIMSD_OK) rc = check_arrays(arrays, n_arrays, num_pages, &a.pages);
+  if (rc != SIMSD_OK) return rc;
+  if (n < 0) return arg_fail("n < 0");
+  if (n == 0 || Bt == 0) return SIMSD_OK;
+  if (!src || !dst || !lens || !block_table) return arg_fail("null pointer");
+  if (!workspace || !aligned16(workspace) || workspace_bytes < simsd::pages_workspace_bytes(0, n))
+    return arg_fail("workspace smaller than simsd_pages_workspace_bytes()");
+  DeviceInfo info;
+  rc = require_sm103(&info);
+  if (rc != SIMSD_OK) return rc;
+  a.src = src;
+  a.dst = dst;
+  a.n = n;
+  a.lens = lens;
+  a.block_table = block_table;
+  a.refs = refs;
+  a.workspace = workspace;
+  a.err_word = err_word;
+  a.num_pages = num_pages;
+  a.Bt = Bt;
+  a.max_pages = max_pages;
+  a.page_size = page_size;
+  cudaError_t e = simsd::launch_pages_fork(a, info.num_sms, as_stream(stream));
+  return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "pages_fork launch");
+}
+
+int simsd_pages_compact(const simsd_page_array* arrays, int n_arrays, int32_t* block_table, int32_t* refs,
+                        int num_pages, int Bt, int max_pages, int32_t* live, void* workspace, size_t workspace_bytes,
+                        int32_t* err_word, void* stream) {
+  simsd::PagesArgs a{};
+  int rc = check_pages(block_table, refs, num_pages, Bt, max_pages);
+  if (rc == SIMSD_OK) rc = check_arrays(arrays, n_arrays, num_pages, &a.pages);
+  if (rc != SIMSD_OK) return rc;
+  if (num_pages > 0 && (!refs || !aligned16(refs))) return arg_fail("refs: null or misaligned");
+  if (!workspace || !aligned16(workspace) || workspace_bytes < simsd::pages_workspace_bytes(num_pages, 0))
+    return arg_fail("workspace smaller than simsd_pages_workspace_bytes()");
+  DeviceInfo info;
+  rc = require_sm103(&info);
+  if (rc != SIMSD_OK) return rc;
+  a.block_table = block_table;
+  a.refs = refs;
+  a.live = live;
+  a.workspace = workspace;
+  a.err_word = err_word;
+  a.num_pages = num_pages;
+  a.Bt = Bt;
+  a.max_pages = max_pages;
+  cudaError_t e = simsd::launch_pages_compact(a, info.num_sms, as_stream(stream));
+  return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "pages_compact launch");
 }
 
 int simsd_sample(int dtype, const void* logits, int64_t row_stride, int R, int vocab, const float* u,

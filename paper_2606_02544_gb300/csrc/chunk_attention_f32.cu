@@ -19,7 +19,7 @@
 #include <algorithm>
 #include <mutex>
 
-#include "chunk_mask.cuh"
+#include "chunk_walk.cuh"
 #include "common.cuh"
 #include "kernels.h"
 #include "ptx.cuh"
@@ -79,13 +79,15 @@ struct Unit {
   ChunkSeq s;
   int i0, rows;       // row r: token i0 + r / gb, head h0 + r % gb (if below `heads`)
   int kvh, h0, heads;
-  int lo, hi;         // keys that any of the rows sees
+  Keys k;             // keys that any of the rows sees
   int t_begin, t_end;
   const int32_t* bt;
 };
 
-// False: nothing to do.  Called by all threads.
-__device__ __forceinline__ bool unit_of(const F32Params& p, const int tile, Unit& u) {
+// SINKS, here and below: the first rows of a sequence stay visible through
+// the window.  False: nothing to do.  Called by all threads.
+template <bool SINKS, int kTile>
+__device__ __forceinline__ bool unit_of(const F32Params& p, Unit& u) {
   __shared__ int unit_s[2];
   const ChunkArgs& a = p.a;
   const unsigned full = 0xffffffffu;
@@ -136,41 +138,54 @@ __device__ __forceinline__ bool unit_of(const F32Params& p, const int tile, Unit
   u.h0 = u.kvh * p.g + (head - u.kvh * p.hblocks) * p.gb;
   u.heads = min(p.gb, u.kvh * p.g + p.g - u.h0);
   u.rows = (i1 - u.i0) * p.gb;
-  u.lo = u.hi = 0;
-  if (!u.s.bad) {
-    u.lo = key_lo(a, u.s, u.i0);
-    u.hi = key_hi(a, u.s, i1 - 1);
-  }
-  if (u.lo >= u.hi) u.lo = u.hi = 0;
+  u.k = keys_of<SINKS>(a, u.s, u.i0, i1);
   u.bt = a.block_table + static_cast<size_t>(b) * a.max_pages;
   bool bad = false;
-  if (u.hi > u.lo)
-    for (int i = u.lo / a.page_size + tid; i <= (u.hi - 1) / a.page_size; i += kThreads)
-      bad |= u.bt[i] < 0 || u.bt[i] >= a.num_pages;
+  auto check = [&](int lo, int hi) {
+    if (hi > lo)
+      for (int i = lo / a.page_size + tid; i <= (hi - 1) / a.page_size; i += kThreads)
+        bad |= u.bt[i] < 0 || u.bt[i] >= a.num_pages;
+  };
+  if constexpr (SINKS) check(u.k.lo, u.k.se);
+  check(u.k.w0, u.k.hi);
   bad = __syncthreads_or(bad);
   if (bad && tid == 0) raise_error(a.err_word, SIMSD_EW_PAGE);
-  if (bad) u.hi = u.lo;
-  const int T0 = u.lo / tile, nt = u.hi > u.lo ? (u.hi + tile - 1) / tile - T0 : 0;
+  if (bad) u.k = Keys{0, 0, 0, 0};
+  const int T0 = u.k.lo / kTile, nt = tiles_of<SINKS, kTile>(u.k);
   u.t_begin = T0 + static_cast<int>(static_cast<long long>(blockIdx.z) * nt / p.nsplit);
   u.t_end = T0 + static_cast<int>(static_cast<long long>(blockIdx.z + 1) * nt / p.nsplit);
   return true;
 }
 
-// The keys that row r of the unit sees.
-__device__ __forceinline__ void row_keys(const F32Params& p, const Unit& u, int r, int& lo, int& hi) {
-  const bool real = r < u.rows && u.hi > u.lo;
-  lo = real ? key_lo(p.a, u.s, u.i0 + r / p.gb) : 0;
-  hi = real ? key_hi(p.a, u.s, u.i0 + r / p.gb) : 0;
+// The first row of key tile t.
+template <bool SINKS, int kTile>
+__device__ __forceinline__ int tile_row(const Unit& u, int t) {
+  if constexpr (SINKS) t += t >= (u.k.se + kTile - 1) / kTile ? tiles_skipped<SINKS, kTile>(u.k) : 0;
+  return t * kTile;
 }
 
-// A key's row in the pool (~0: not among [lo, hi); 2^32 rows would be a terabyte).
+// The keys that row r of the unit sees: [lo, hi), and of the first rows that
+// stay visible those below se.
+__device__ __forceinline__ void row_keys(const F32Params& p, const Unit& u, int r, int& lo, int& hi, int& se) {
+  const bool real = r < u.rows && u.k.hi > u.k.lo;
+  lo = real ? key_lo(p.a, u.s, u.i0 + r / p.gb) : 0;
+  hi = real ? key_hi(p.a, u.s, u.i0 + r / p.gb) : 0;
+  se = real ? sink_end(p.a, u.s, hi) : 0;
+}
+template <bool SINKS>
+__device__ __forceinline__ bool row_sees(const Unit& u, int key, int lo, int hi, int se) {
+  return (key >= lo && key < hi) || (SINKS && key >= u.s.ks && key < se);
+}
+
+// A key's row in the pool (~0: seen by no row; 2^32 rows would be a terabyte).
+template <bool SINKS>
 __device__ __forceinline__ uint32_t pool_row(const F32Params& p, const Unit& u, int key) {
-  if (key < u.lo || key >= u.hi) return ~0u;
+  if (key < u.k.lo || key >= u.k.hi || (SINKS && key >= u.k.se && key < u.k.w0)) return ~0u;
   const int pi = key / p.a.page_size;
   return (static_cast<uint32_t>(u.bt[pi]) * p.a.Hkv + u.kvh) * p.a.page_size + (key - pi * p.a.page_size);
 }
 
-template <int D, int RB>
+template <int D, int RB, bool SINKS>
 __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_constant__ F32Params p) {
   constexpr int RT = RB / 16;   // rows of a thread
   constexpr int OC = D / 64;    // four-column groups of O of a thread
@@ -182,13 +197,13 @@ __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_consta
   const unsigned full = 0xffffffffu;
   const int tid = threadIdx.x;
   Unit u;
-  if (!unit_of(p, kTile, u)) return;
+  if (!unit_of<SINKS, kTile>(p, u)) return;
   const ChunkSeq& s = u.s;
   const int t_begin = u.t_begin, t_end = u.t_end, rows = u.rows, heads = u.heads, h0 = u.h0, i0 = u.i0;
 
   // where the keys of tile t lie (the page arithmetic once a key, not once a copy)
   auto find_rows = [&](int t) {
-    if (tid < kTile) sm.row[t & 1][tid] = pool_row(p, u, t * kTile + tid);
+    if (tid < kTile) sm.row[t & 1][tid] = pool_row<SINKS>(p, u, tile_row<SINKS, kTile>(u, t) + tid);
   };
   auto load_tile = [&](int t, bool is_k) {
     const float4* src = static_cast<const float4*>(is_k ? a.k_cache : a.v_cache);
@@ -215,11 +230,11 @@ __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_consta
   if (t_begin < t_end) load_tile(t_begin, false);
 
   const int tx = tid & 15, ty = tid >> 4;
-  int klo[RT], khi[RT];
+  int klo[RT], khi[RT], kse[RT];
   float m[RT], l[RT], o[RT][OC][4];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    row_keys(p, u, ty * RT + r, klo[r], khi[r]);
+    row_keys(p, u, ty * RT + r, klo[r], khi[r], kse[r]);
     m[r] = -INFINITY;
     l[r] = 0.f;
 #pragma unroll
@@ -258,14 +273,14 @@ __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_consta
       load_tile(t + 1, true);
     else
       cp_async_commit();  // (keeps the count of groups)
+    const int key0 = tile_row<SINKS, kTile>(u, t);
     // softmax of this thread's rows (sixteen lanes share a row)
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       float mx = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int key = t * kTile + tx + 16 * j;
-        const bool in = key >= klo[r] && key < khi[r];
+        const bool in = row_sees<SINKS>(u, key0 + tx + 16 * j, klo[r], khi[r], kse[r]);
         sc[r][j] = in ? sc[r][j] * a.scale : -INFINITY;
         mx = fmaxf(mx, sc[r][j]);
       }
@@ -350,7 +365,7 @@ __global__ void __launch_bounds__(kThreads) chunk_f32_kernel(const __grid_consta
 // merged through shared memory.  Bound by memory and by the sums over the
 // lanes (20 shuffles a key): 32 single tokens over 4096 keys, 32 heads on 8,
 // read 1.07 GB in 266 us (4.0 TB/s); tiles of 16 rows took 650.
-template <int D>
+template <int D, bool SINKS>
 __global__ void __launch_bounds__(kThreads, 2) chunk_f32_few_kernel(const __grid_constant__ F32Params p) {
   constexpr int E = D / 32, kWarps = kThreads / 32, kKeys = 4, R = 4;
   struct alignas(4 * E) Vec {
@@ -360,14 +375,14 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_f32_few_kernel(const __grid
   __shared__ uint32_t key_row[3][kFewTile];
   __shared__ alignas(16) float part_o[kWarps][R][D];
   __shared__ float part_m[kWarps][R], part_l[kWarps][R];
-  __shared__ int2 sees[R];  // the keys that a row sees
+  __shared__ int sees[R][3];  // the keys that a row sees
   pdl_wait();
   pdl_launch_next();
   const ChunkArgs& a = p.a;
   const unsigned full = 0xffffffffu;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   Unit u;
-  if (!unit_of(p, kFewTile, u)) return;
+  if (!unit_of<SINKS, kFewTile>(p, u)) return;
   Vec q[R], o[R];
   float m[R], l[R];
 #pragma unroll
@@ -388,8 +403,9 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_f32_few_kernel(const __grid
   }
   const Vec* kp = static_cast<const Vec*>(a.k_cache);
   const Vec* vp = static_cast<const Vec*>(a.v_cache);
-  if (tid < R) row_keys(p, u, tid, sees[tid].x, sees[tid].y);
-  if (u.t_begin < u.t_end) key_row[u.t_begin % 3][tid] = pool_row(p, u, u.t_begin * kFewTile + tid);
+  if (tid < R) row_keys(p, u, tid, sees[tid][0], sees[tid][1], sees[tid][2]);
+  if (u.t_begin < u.t_end)
+    key_row[u.t_begin % 3][tid] = pool_row<SINKS>(p, u, tile_row<SINKS, kFewTile>(u, u.t_begin) + tid);
   __syncthreads();
   Vec k[kKeys], v[kKeys];
   // (hidden keys: zeros)
@@ -408,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_f32_few_kernel(const __grid
     load(v, vp, &key_row[u.t_begin % 3][warp * kRun]);
   }
   for (int t = u.t_begin; t < u.t_end; ++t) {
-    if (t + 1 < u.t_end) key_row[(t + 1) % 3][tid] = pool_row(p, u, (t + 1) * kFewTile + tid);
+    if (t + 1 < u.t_end) key_row[(t + 1) % 3][tid] = pool_row<SINKS>(p, u, tile_row<SINKS, kFewTile>(u, t + 1) + tid);
     __syncthreads();
 #pragma unroll 1
     for (int c = 0; c < kRun; c += kKeys) {
@@ -426,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_f32_few_kernel(const __grid
       const bool more = c + kKeys < kRun || t + 1 < u.t_end;
       const uint32_t* next = c + kKeys < kRun ? &key_row[t % 3][warp * kRun + c + kKeys] : &key_row[(t + 1) % 3][warp * kRun];
       if (more) load(k, kp, next);
-      const int key0 = t * kFewTile + warp * kRun + c;
+      const int key0 = tile_row<SINKS, kFewTile>(u, t) + warp * kRun + c;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         float mx = m[r];
@@ -434,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_f32_few_kernel(const __grid
         for (int j = 0; j < kKeys; ++j) {
 #pragma unroll
           for (int w = 16; w > 0; w >>= 1) sc[r][j] += __shfl_xor_sync(full, sc[r][j], w);
-          if (key0 + j < sees[r].x || key0 + j >= sees[r].y) sc[r][j] = -INFINITY;
+          if (!row_sees<SINKS>(u, key0 + j, sees[r][0], sees[r][1], sees[r][2])) sc[r][j] = -INFINITY;
           mx = fmaxf(mx, sc[r][j]);
         }
         // (nothing seen so far: every weight is zero)
@@ -553,12 +569,12 @@ F32Plan f32_plan(int T, int Bt, int Hq, int Hkv, long long max_keys, int num_sms
   return f;
 }
 
-template <int D, int RB>
+template <int D, int RB, bool SINKS>
 cudaError_t launch_rb(const F32Params& p, const F32Plan& f, cudaStream_t stream) {
   const dim3 grid(static_cast<unsigned>(f.units) * static_cast<unsigned>(p.heads), 1u, static_cast<unsigned>(f.nsplit));
   cudaError_t e;
   if constexpr (RB == 4) {
-    e = launch_overlapped(chunk_f32_few_kernel<D>, grid, dim3(kThreads), 0, stream, 1u, p);
+    e = launch_overlapped(chunk_f32_few_kernel<D, SINKS>, grid, dim3(kThreads), 0, stream, 1u, p);
   } else {
     static std::mutex mu;
     static bool done[64] = {};
@@ -568,16 +584,24 @@ cudaError_t launch_rb(const F32Params& p, const F32Plan& f, cudaStream_t stream)
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     std::lock_guard<std::mutex> lk(mu);
     if (!done[dev]) {
-      e = cudaFuncSetAttribute(chunk_f32_kernel<D, RB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+      e = cudaFuncSetAttribute(chunk_f32_kernel<D, RB, SINKS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                static_cast<int>(sizeof(SmemF32<D, RB>)));
       if (e != cudaSuccess) return e;
       done[dev] = true;
     }
-    e = launch_overlapped(chunk_f32_kernel<D, RB>, grid, dim3(kThreads), sizeof(SmemF32<D, RB>), stream, 1u, p);
+    e = launch_overlapped(chunk_f32_kernel<D, RB, SINKS>, grid, dim3(kThreads), sizeof(SmemF32<D, RB>), stream, 1u, p);
   }
   if (e != cudaSuccess || f.nsplit == 1) return e;
   const unsigned blocks = static_cast<unsigned>((static_cast<long long>(p.a.T) * p.a.Hq + 3) / 4);
   return launch_overlapped(chunk_f32_merge_kernel<D>, dim3(blocks), dim3(128), 0, stream, 1u, p);
+}
+
+template <int D, bool SINKS>
+cudaError_t launch_f32(const F32Params& p, const F32Plan& f, cudaStream_t stream) {
+  if (f.rb == 128) return launch_rb<D, 128, SINKS>(p, f, stream);
+  if (f.rb == 64) return launch_rb<D, 64, SINKS>(p, f, stream);
+  if (f.rb == 16) return launch_rb<D, 16, SINKS>(p, f, stream);
+  return launch_rb<D, 4, SINKS>(p, f, stream);
 }
 
 }  // namespace
@@ -600,11 +624,8 @@ cudaError_t launch_chunk_attention_f32(const ChunkArgs& a, int num_sms, cudaStre
   p.nsplit = f.nsplit;
   p.heads = a.Hkv * f.hblocks;
   p.units = f.units;
-  if (f.rb == 128)
-    return a.d == 128 ? launch_rb<128, 128>(p, f, stream) : launch_rb<64, 128>(p, f, stream);
-  if (f.rb == 64) return a.d == 128 ? launch_rb<128, 64>(p, f, stream) : launch_rb<64, 64>(p, f, stream);
-  if (f.rb == 16) return a.d == 128 ? launch_rb<128, 16>(p, f, stream) : launch_rb<64, 16>(p, f, stream);
-  return a.d == 128 ? launch_rb<128, 4>(p, f, stream) : launch_rb<64, 4>(p, f, stream);
+  if (a.sinks > 0) return a.d == 128 ? launch_f32<128, true>(p, f, stream) : launch_f32<64, true>(p, f, stream);
+  return a.d == 128 ? launch_f32<128, false>(p, f, stream) : launch_f32<64, false>(p, f, stream);
 }
 
 }  // namespace simsd

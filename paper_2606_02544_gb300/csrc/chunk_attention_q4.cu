@@ -1,0 +1,760 @@
+// chunk_attention_q4.cu -- attention of single tokens and short chunks over a
+// paged cache in 4 bits (Sec. 3.3: the prefix is read from a KV cache).
+//
+// Mathematics.  As in chunk_attention_tc.cu: one pass over the keys with a
+// running reference maximum and sum (fp32; the reference moves only when a
+// score exceeds it by 2^8).  Keys and values are scale times code: 6
+// significant bits, exact in fp16.  q is multiplied by a power of two that
+// brings its row's largest component to [1, 4) and is then exact in fp16 too,
+// but for components below 2^-14 of the largest (off by 2^-25 of it at most).
+// Probabilities are rounded to fp16, their sum is not; products are
+// accumulated in fp32.
+//
+// Few query rows meet many keys, so the keys are the wide side of the
+// products: S^T = K Q^T and O^T += V^T P^T with 16 keys (channels) by 8 rows
+// a matrix instruction, mma.sync m16n8k16.  Its operands come from registers:
+// a thread turns 16 bytes of codes into the fragments of 8 instructions
+// (convert, times scale) without a way through shared memory, where the
+// tcgen05 instructions would have them, 64 KB a tile written and read again.
+// The order of components within a product and of keys within 16 is free, so
+// each thread takes the components, channels and keys that lie together.
+//
+// Work.  The walk of chunk_walk.cuh over units of (KV head, sequence, up to
+// RB query rows).  One warp walks the run and brings the tiles' codes and
+// scales (128 keys, 18 KB) by bulk copies, each a page's contiguous rows of a
+// head; eight warps share a tile's keys (RG groups of rows by 8 / RG of keys),
+// each with a softmax of its own, merged at the end of a unit through shared
+// memory.  A unit cut by a run's end leaves partial (O, m, l), which a second
+// launch merges.
+//
+// Every mbarrier wait is bounded; after one expires the CTA raises
+// SIMSD_EW_TIMEOUT, every warp leaves its loop and the copies in flight are
+// waited for.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "chunk_walk.cuh"
+#include "common.cuh"
+#include "kernels.h"
+#include "ptx.cuh"
+#include "q4.cuh"
+
+namespace simsd {
+namespace {
+
+constexpr int kTile = 128;  // keys per tile
+constexpr int kWarps = 8;   // of the softmax
+constexpr int kThreads = 32 * (kWarps + 1);
+constexpr float kRescaleThreshold = 8.0f;  // log2 units
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct Q4Params {
+  ChunkArgs a;
+  simsd_q4_cache c;
+  int g, ub, ctas;    // heads per KV head, tokens of a unit, grid size
+  int sub;            // keys per copy: a page, or part of one
+  float scale_log2;   // scores to log2 units, the keys' unit included
+};
+
+// What the walking warp says of a tile, beside its codes.
+struct alignas(16) TileInfo {
+  int key0, full, first, last;   // full: every row sees every key; first / last tile of a piece
+  int lo, se, w0, hi;            // keys that any row of the unit sees
+  int tok0, ntok, kvh, i0;
+  int n, C, ks, empty;           // empty: no key at all (or, with tok0 < 0, the end of the run)
+  int part, slot, bad, last_piece;
+};
+
+template <int D, int NB, int RG>
+struct Cfg {
+  static constexpr int kRows = 8 * NB * RG;      // query rows of a unit
+  static constexpr int kKeyGroups = kWarps / RG;
+  static constexpr int kWarpKeys = kTile / kKeyGroups;
+  static constexpr int kCtas = NB == 1 ? 2 : 1;  // an SM
+  static constexpr int kStages = (NB == 1 ? 4 : 7) * (128 / D);
+};
+
+template <int D>
+struct alignas(128) Stage {
+  uint8_t kc[kTile * D / 2], vc[kTile * D / 2];
+  uint8_t ks[kTile * D / kQ4Group], vs[kTile * D / kQ4Group];
+};
+
+template <int D, int NB, int RG>
+struct SmemQ4 {
+  using C = Cfg<D, NB, RG>;
+  Stage<D> ring[C::kStages];
+  __nv_bfloat16 q[2][C::kRows * D];
+  float4 fold[kWarps / 2][NB * (D / 16)][32];  // O of half the warps
+  float2 ml[kWarps][8 * NB];
+  float2 fin[C::kRows];
+  TileInfo info[C::kStages];
+  uint64_t bar_full[C::kStages], bar_free[C::kStages], bar_qfree[2], bar_merge[3];
+  int abort_flag;
+};
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                         uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The transpose of an 8 x 8 matrix of fp16, two neighbours of a row a thread.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Partial results: O (without the values' unit) [entries][RB][D], then (m, l)
+// [entries][RB], entry cta * 2 + slot, m in log2 units, l = -1 where a page id
+// of the piece is out of range; then one Record per run boundary.
+template <int D, int RB>
+__device__ __forceinline__ float* partial_o(const Q4Params& p, int entry, int row) {
+  return static_cast<float*>(p.a.workspace) + (static_cast<size_t>(entry) * RB + row) * D;
+}
+template <int D, int RB>
+__device__ __forceinline__ float2* partial_ml(const Q4Params& p, int entry, int row) {
+  return reinterpret_cast<float2*>(partial_o<D, RB>(p, 2 * p.ctas, 0)) + static_cast<size_t>(entry) * RB + row;
+}
+template <int D, int RB>
+__device__ __forceinline__ Record* records(const Q4Params& p) {
+  return reinterpret_cast<Record*>(partial_ml<D, RB>(p, 2 * p.ctas, 0));
+}
+
+// A thread's codes of K: the D / 4 components (D / 8 bytes) from t D / 4 on.
+template <int D>
+struct KCodes {
+  uint32_t w[D / 32];
+  uint32_t s;  // their scales, a byte each
+};
+template <int D>
+__device__ __forceinline__ KCodes<D> load_k(const Stage<D>& st, int key, int t) {
+  KCodes<D> c;
+  if constexpr (D == 128) {
+    const uint4 v = *reinterpret_cast<const uint4*>(&st.kc[key * 64 + 16 * t]);
+    c.w[0] = v.x, c.w[1] = v.y, c.w[2] = v.z, c.w[3] = v.w;
+    c.s = *reinterpret_cast<const uint16_t*>(&st.ks[key * 8 + 2 * t]);
+  } else {
+    const uint2 v = *reinterpret_cast<const uint2*>(&st.kc[key * 32 + 8 * t]);
+    c.w[0] = v.x, c.w[1] = v.y;
+    c.s = st.ks[key * 4 + t];
+  }
+  return c;
+}
+// The codes of V of one key, D / 8 channels from g D / 8 on.
+template <int D>
+struct VCodes {
+  uint32_t w[D / 64];
+};
+template <int D>
+__device__ __forceinline__ VCodes<D> load_v(const Stage<D>& st, int key, int g) {
+  VCodes<D> c;
+  if constexpr (D == 128) {
+    const uint2 v = *reinterpret_cast<const uint2*>(&st.vc[key * 64 + 8 * g]);
+    c.w[0] = v.x, c.w[1] = v.y;
+  } else {
+    c.w[0] = *reinterpret_cast<const uint32_t*>(&st.vc[key * 32 + 4 * g]);
+  }
+  return c;
+}
+
+template <int D, int NB, int RG, bool SINKS>
+__global__ void __launch_bounds__(kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kernel(const __grid_constant__ Q4Params p) {
+  using C = Cfg<D, NB, RG>;
+  using Smem = SmemQ4<D, NB, RG>;
+  constexpr int RB = C::kRows, kStages = C::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~static_cast<uintptr_t>(127));
+  static_assert(sizeof(sm.ring) >= kChunkMaxSeqs * 4, "the ring holds the tile counts of all sequences");
+  volatile int* abort_flag = &sm.abort_flag;
+  const unsigned full = 0xffffffffu;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    sm.abort_flag = 0;
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(smem_u32(&sm.bar_full[s]), 1);
+      mbar_init(smem_u32(&sm.bar_free[s]), kWarps);
+    }
+    mbar_init(smem_u32(&sm.bar_qfree[0]), kWarps);
+    mbar_init(smem_u32(&sm.bar_qfree[1]), kWarps);
+    for (int i = 0; i < 3; ++i) mbar_init(smem_u32(&sm.bar_merge[i]), kWarps);
+    fence_mbar_init();
+  }
+  pdl_wait();
+  int32_t* tiles = reinterpret_cast<int32_t*>(&sm.ring[0]);
+  plan_tiles<SINKS, kTile, kThreads>(p.a, p.ub, tiles);
+  Place start{0, 0, 0, 0};
+  int total = 0;
+  ChunkSeq seq{};
+  if (warp == kWarps) start = plan_start<SINKS, kTile>(p.a, p.ub, p.ctas, tiles, total, seq);
+  fence_proxy_async_smem();  // the ring was written here and is filled by bulk copies next
+  __syncthreads();
+  auto give_up = [&]() {
+    if (lane == 0) {
+      raise_error(p.a.err_word, SIMSD_EW_TIMEOUT);
+      *abort_flag = 1;
+    }
+  };
+
+  if (warp == kWarps) {
+    // -------------------------------------------------------- walk and copies
+    Walk<SINKS, kTile> k;
+    k.begin(p.a, p.ub, p.ctas, start, seq, total);
+    typename Walk<SINKS, kTile>::Step piece;
+    const int P = p.a.page_size, sub = p.sub;
+    uint32_t it = 0, units = 0;  // tiles passed on, of them with a Q
+    bool ok = true;
+    auto slot_free = [&]() {
+      if (it >= kStages) ok = mbar_wait_warp(smem_u32(&sm.bar_free[it % kStages]), ((it / kStages) - 1) & 1, abort_flag);
+      return ok;
+    };
+    while (ok && k.peek(p.a, p.ub, piece)) {
+      TileInfo u;
+      u.i0 = k.w.j * p.ub;
+      u.tok0 = k.s.start + u.i0;
+      u.ntok = min(p.ub, k.s.C - u.i0);
+      u.kvh = k.w.kvh;
+      u.lo = piece.keys.lo;
+      u.se = piece.keys.se;
+      u.w0 = piece.keys.w0;
+      u.hi = piece.keys.hi;
+      u.n = k.s.n;
+      u.C = k.s.C;
+      u.ks = k.s.ks;
+      u.empty = piece.tiles == 0;
+      u.part = piece.take < piece.weight;
+      u.slot = piece.slot;
+      u.last_piece = piece.last;
+      u.bad = 0;
+      // rows that every token of the unit sees
+      const int all_lo = u.empty ? 0 : key_lo(p.a, k.s, u.i0 + u.ntok - 1), all_hi = u.empty ? 0 : key_hi(p.a, k.s, u.i0);
+      const int all_se = SINKS && !u.empty ? sink_end(p.a, k.s, all_hi) : 0;
+      const int skip = tiles_skipped<SINKS, kTile>(piece.keys), tse = (u.se + kTile - 1) / kTile;
+      const int32_t* bt = p.a.block_table + static_cast<size_t>(k.w.b) * p.a.max_pages;
+      const int t0 = u.lo / kTile + k.w.t;
+      int win_base = -(1 << 30), win = -1;  // lane i holds the page id of page win_base + i
+      for (int i = 0; i < piece.take; ++i) {
+        const uint32_t st = it % kStages;
+        const int t = t0 + i;
+        u.key0 = (t + (SINKS && t >= tse ? skip : 0)) * kTile;
+        u.first = i == 0;
+        u.last = i + 1 == piece.take;
+        u.full = !u.empty && ((u.key0 >= all_lo && u.key0 + kTile <= all_hi) ||
+                              (SINKS && u.key0 >= u.ks && u.key0 + kTile <= all_se));
+        // copy s of the tile is lane s's
+        const int nsub = kTile / sub, key = u.key0 + min(lane, nsub - 1) * sub, pi = key / P;
+        const int pi0 = u.key0 / P, pi1 = (u.key0 + kTile - 1) / P;
+        if (pi0 < win_base || pi1 >= win_base + 32) {
+          win_base = pi0;
+          win = win_base + lane < p.a.max_pages ? bt[win_base + lane] : -1;
+        }
+        const int pg = __shfl_sync(full, win, (pi - win_base) & 31);
+        bool load = !u.empty && lane < nsub && key + sub > u.lo && key < u.hi && (!SINKS || key < u.se || key + sub > u.w0);
+        const bool wrong = load && (pg < 0 || pg >= p.a.num_pages);
+        load = load && !wrong;
+        if (__any_sync(full, wrong)) {
+          if (lane == 0) raise_error(p.a.err_word, SIMSD_EW_PAGE);
+          u.bad = 1;
+        }
+        if (!slot_free()) break;
+        const bool with_q = u.first && !u.empty;
+        const uint32_t qb = units & 1;
+        if (with_q && units >= 2) {
+          ok = mbar_wait_warp(smem_u32(&sm.bar_qfree[qb]), ((units >> 1) - 1) & 1, abort_flag);
+          if (!ok) break;
+        }
+        const uint32_t bar = smem_u32(&sm.bar_full[st]);
+        const uint32_t code_bytes = static_cast<uint32_t>(sub * (D / 2)), scale_bytes = static_cast<uint32_t>(sub * (D / kQ4Group));
+        const uint32_t q_bytes = static_cast<uint32_t>(p.g * D * 2);
+        const uint32_t bytes = __popc(__ballot_sync(full, load)) * 2u * (code_bytes + scale_bytes) + (with_q ? u.ntok * q_bytes : 0u);
+        if (lane == 0) {
+          sm.info[st] = u;
+          mbar_arrive_expect_tx(bar, bytes);
+        }
+        __syncwarp();
+        if (load) {
+          Stage<D>& s = sm.ring[st];
+          const size_t row = (static_cast<size_t>(pg) * p.a.Hkv + u.kvh) * P + (key - pi * P);
+          const int at = lane * sub;
+          bulk_load(smem_u32(&s.kc[at * (D / 2)]), static_cast<const uint8_t*>(p.c.k_codes) + row * (D / 2), code_bytes, bar);
+          bulk_load(smem_u32(&s.ks[at * (D / kQ4Group)]), static_cast<const uint8_t*>(p.c.k_scales) + row * (D / kQ4Group), scale_bytes, bar);
+          bulk_load(smem_u32(&s.vc[at * (D / 2)]), static_cast<const uint8_t*>(p.c.v_codes) + row * (D / 2), code_bytes, bar);
+          bulk_load(smem_u32(&s.vs[at * (D / kQ4Group)]), static_cast<const uint8_t*>(p.c.v_scales) + row * (D / kQ4Group), scale_bytes, bar);
+        }
+        if (with_q) {
+          for (int x = lane; x < u.ntok; x += 32)
+            bulk_load(smem_u32(&sm.q[qb][x * p.g * D]),
+                      static_cast<const __nv_bfloat16*>(p.a.q) + static_cast<long long>(u.tok0 + x) * p.a.q_stride +
+                          static_cast<long long>(u.kvh) * p.g * D,
+                      q_bytes, bar);
+          ++units;
+        }
+        ++it;
+      }
+      if (!ok) break;
+      k.pop(p.a, p.ub, piece);
+    }
+    if (ok && slot_free()) {
+      // the end of the run
+      if (lane == 0) {
+        TileInfo u{};
+        u.tok0 = -1;
+        u.empty = 1;
+        sm.info[it % kStages] = u;
+        mbar_arrive(smem_u32(&sm.bar_full[it % kStages]));
+      }
+      ++it;
+    }
+    if (!ok) give_up();
+    if (lane == 0 && blockIdx.x > 0) records<D, RB>(p)[blockIdx.x] = boundary_record<SINKS, kTile>(k, p.a, p.ub);
+    // every copy must have landed before the CTA may exit
+    if (lane == 0)
+      for (uint32_t j = it > kStages ? it - kStages : 0; j < it; ++j)
+        mbar_wait(smem_u32(&sm.bar_full[j % kStages]), (j / kStages) & 1, nullptr);
+    __syncwarp();
+    return;
+  }
+
+  // ------------------------------------------------------------------ softmax
+  const int g = lane >> 2, t = lane & 3;  // the thread's place in the fragments
+  const int rg = warp % RG, kg = warp / RG;
+  const int perm = g ^ ((g >> 1) & 1);    // place of key g among 8: neighbours in pairs, pairs turned in turns
+  const int va = (2 * t) ^ (t & 1), vb = (2 * t + 1) ^ (t & 1);
+  constexpr int kSteps = D / 16;          // products of 16 components; blocks of 16 channels
+  uint32_t q[NB][kSteps][2];
+  float o[NB][kSteps][4], m[NB][2], l[NB][2], rs[NB][2];
+  uint32_t units = 0, pieces = 0;
+  bool ok = true;
+  for (uint32_t it = 0; ok; ++it) {
+    const uint32_t st = it % kStages;
+    if (!mbar_wait_warp(smem_u32(&sm.bar_full[st]), (it / kStages) & 1, abort_flag)) {
+      ok = false;
+      break;
+    }
+    const Stage<D>& s = sm.ring[st];
+    const TileInfo& info = sm.info[st];
+    const int tok0 = info.tok0, ntok = info.ntok, key0 = info.key0;
+    const bool empty = info.empty != 0, last = info.last != 0;
+    if (tok0 < 0) break;
+    if (info.first) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) o[nb][k][0] = o[nb][k][1] = o[nb][k][2] = o[nb][k][3] = 0.f;
+        m[nb][0] = m[nb][1] = -INFINITY;
+        l[nb][0] = l[nb][1] = 0.f;
+      }
+      if (!empty) {
+        const uint32_t qb = units & 1;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          // row (rg NB + nb) 8 + g: its components from t D / 4 on
+          const int row = (rg * NB + nb) * 8 + g;
+          const bool real = row < ntok * p.g;
+          uint4 raw[D / 32];
+          uint32_t top = 0;
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) {
+            raw[j] = make_uint4(0u, 0u, 0u, 0u);
+            if (real) raw[j] = *reinterpret_cast<const uint4*>(&sm.q[qb][row * D + t * (D / 4) + 8 * j]);
+            const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7fffu, w[e] >> 16 & 0x7fffu));
+          }
+          top = max(top, __shfl_xor_sync(full, top, 1));
+          top = max(top, __shfl_xor_sync(full, top, 2));
+          const uint32_t ex = min(max(top >> 7, 1u), 253u);  // 2^(ex - 127) <= the largest < 2^(ex - 126)
+          const float down = __uint_as_float((254u - ex) << 23), up = __uint_as_float(ex << 23);
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) {
+            const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              q[nb][2 * j + e / 2][e & 1] = pack_f16x2(__uint_as_float(w[e] << 16) * down, __uint_as_float(w[e] & 0xffff0000u) * down);
+          }
+          // scores of rows 2t and 2t + 1, whose q lies with lanes of g = 2t and 2t + 1
+          rs[nb][0] = __shfl_sync(full, up, 8 * t) * p.scale_log2;
+          rs[nb][1] = __shfl_sync(full, up, 8 * t + 4) * p.scale_log2;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.bar_qfree[qb]));
+        ++units;
+      }
+    }
+    if (!empty) {
+      const bool masked = info.full == 0;
+      const int lo = info.lo, se = info.se, w0 = info.w0, hi = info.hi, ks = info.ks;
+      int klo[NB][2], khi[NB][2], kse[NB][2];
+      if (masked) {
+        ChunkSeq cs;
+        cs.n = info.n;
+        cs.C = info.C;
+        cs.ks = ks;
+        const int i0 = info.i0;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int tl = min(((rg * NB + nb) * 8 + 2 * t + e) / p.g, ntok - 1);
+            klo[nb][e] = key_lo(p.a, cs, i0 + tl);
+            khi[nb][e] = key_hi(p.a, cs, i0 + tl);
+            kse[nb][e] = SINKS ? sink_end(p.a, cs, khi[nb][e]) : 0;
+          }
+      }
+#pragma unroll
+      for (int sub = 0; sub < C::kWarpKeys / 16; ++sub) {
+        const int kb = kg * C::kWarpKeys + 16 * sub;
+        const KCodes<D> ka = load_k(s, kb + perm, t), kc = load_k(s, kb + 8 + perm, t);
+        // S^T of keys perm(g) and 8 + perm(g), rows 2t and 2t + 1
+        float sc[NB][4];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) sc[nb][0] = sc[nb][1] = sc[nb][2] = sc[nb][3] = 0.f;
+        uint32_t sa[D / 64], sb[D / 64];
+        {
+          const uint32_t x = q4_scale_pair(ka.s), y = q4_scale_pair(kc.s);
+          sa[0] = __byte_perm(x, 0, 0x1010);
+          sb[0] = __byte_perm(y, 0, 0x1010);
+          if constexpr (D == 128) {
+            sa[1] = __byte_perm(x, 0, 0x3232);
+            sb[1] = __byte_perm(y, 0, 0x3232);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+          const uint32_t u = ka.w[k / 2], v = kc.w[k / 2], fa = sa[k / 4], fb = sb[k / 4];
+          const uint32_t a0 = mul_f16x2(k & 1 ? q4_pair<2>(u) : q4_pair<0>(u), fa);
+          const uint32_t a1 = mul_f16x2(k & 1 ? q4_pair<2>(v) : q4_pair<0>(v), fb);
+          const uint32_t a2 = mul_f16x2(k & 1 ? q4_pair<3>(u) : q4_pair<1>(u), fa);
+          const uint32_t a3 = mul_f16x2(k & 1 ? q4_pair<3>(v) : q4_pair<1>(v), fb);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) mma16816(sc[nb], a0, a1, a2, a3, q[nb][k][0], q[nb][k][1]);
+        }
+        // scores in log2 units, hidden ones -inf
+        bool above = false;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            sc[nb][e] *= rs[nb][e & 1];
+            if (masked) {
+              const int key = key0 + kb + perm + (e & 2 ? 8 : 0);
+              const bool in = (key >= klo[nb][e & 1] && key < khi[nb][e & 1]) || (SINKS && key >= ks && key < kse[nb][e & 1]);
+              sc[nb][e] = in ? sc[nb][e] : -INFINITY;
+            }
+            above |= sc[nb][e] > m[nb][e & 1] + kRescaleThreshold;
+          }
+        }
+        // (the first scores of a piece lie above -inf)
+        if (__any_sync(full, above)) {
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float mx = fmaxf(m[nb][e], fmaxf(sc[nb][e], sc[nb][e + 2]));
+              mx = fmaxf(mx, __shfl_xor_sync(full, mx, 4));
+              mx = fmaxf(mx, __shfl_xor_sync(full, mx, 8));
+              mx = fmaxf(mx, __shfl_xor_sync(full, mx, 16));
+              const float f = m[nb][e] == -INFINITY ? 0.f : exp2_approx(m[nb][e] - mx);
+              m[nb][e] = mx;
+              l[nb][e] *= f;
+#pragma unroll
+              for (int k = 0; k < kSteps; ++k) {
+                o[nb][k][e] *= f;
+                o[nb][k][e + 2] *= f;
+              }
+            }
+        }
+        uint32_t pb[NB][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          float pr[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float ref = m[nb][e & 1] == -INFINITY ? 0.f : m[nb][e & 1];
+            pr[e] = exp2_approx(sc[nb][e] - ref);
+          }
+          l[nb][0] += pr[0] + pr[2];
+          l[nb][1] += pr[1] + pr[3];
+          pb[nb][0] = transpose8(pack_f16x2(pr[0], pr[1]));
+          pb[nb][1] = transpose8(pack_f16x2(pr[2], pr[3]));
+        }
+        // V^T of keys va, vb and 8 + va, 8 + vb, channels from g D / 8 on (all of one scale)
+        const VCodes<D> v0 = load_v(s, kb + va, g), v1 = load_v(s, kb + vb, g);
+        const VCodes<D> v2 = load_v(s, kb + 8 + va, g), v3 = load_v(s, kb + 8 + vb, g);
+        constexpr int kScales = D / kQ4Group;
+        const int vg = D == 128 ? g : g >> 1;
+        uint32_t s01 = s.vs[(kb + va) * kScales + vg] | s.vs[(kb + vb) * kScales + vg] << 8;
+        uint32_t s23 = s.vs[(kb + 8 + va) * kScales + vg] | s.vs[(kb + 8 + vb) * kScales + vg] << 8;
+        if (masked) {
+          // values of rows that no token of the unit sees may be anything: 0
+          auto seen = [&](int key) { return key >= lo && key < hi && (!SINKS || key < se || key >= w0); };
+          s01 &= (seen(key0 + kb + va) ? 0xffu : 0u) | (seen(key0 + kb + vb) ? 0xff00u : 0u);
+          s23 &= (seen(key0 + kb + 8 + va) ? 0xffu : 0u) | (seen(key0 + kb + 8 + vb) ? 0xff00u : 0u);
+        }
+        const uint32_t f01 = q4_scale_pair(s01), f23 = q4_scale_pair(s23);
+        constexpr uint32_t kLow = 0x0f0f0f0fu;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          // bytes of two keys' codes of one channel
+          const uint32_t e01 = (v0.w[i] & kLow) | (v1.w[i] << 4 & ~kLow), d01 = (v0.w[i] >> 4 & kLow) | (v1.w[i] & ~kLow);
+          const uint32_t e23 = (v2.w[i] & kLow) | (v3.w[i] << 4 & ~kLow), d23 = (v2.w[i] >> 4 & kLow) | (v3.w[i] & ~kLow);
+          auto block = [&](float (&acc)[NB][kSteps][4], int k, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+            a0 = mul_f16x2(a0, f01);
+            a1 = mul_f16x2(a1, f01);
+            a2 = mul_f16x2(a2, f23);
+            a3 = mul_f16x2(a3, f23);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma16816(acc[nb][k], a0, a1, a2, a3, pb[nb][0], pb[nb][1]);
+          };
+          block(o, 4 * i, q4_pair<0>(e01), q4_pair<0>(d01), q4_pair<0>(e23), q4_pair<0>(d23));
+          block(o, 4 * i + 1, q4_pair<1>(e01), q4_pair<1>(d01), q4_pair<1>(e23), q4_pair<1>(d23));
+          block(o, 4 * i + 2, q4_pair<2>(e01), q4_pair<2>(d01), q4_pair<2>(e23), q4_pair<2>(d23));
+          block(o, 4 * i + 3, q4_pair<3>(e01), q4_pair<3>(d01), q4_pair<3>(e23), q4_pair<3>(d23));
+        }
+      }
+    }
+    // what the end of a piece needs is read before the slot is given back
+    const bool part = info.part != 0, bad = info.bad != 0;
+    const int kvh = info.kvh, entry = static_cast<int>(blockIdx.x) * 2 + info.slot;
+    const bool last_piece = last && info.last_piece != 0;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&sm.bar_free[st]));
+    if (last_piece) pdl_launch_next();
+    if (!last) continue;
+
+    // ---- the warps' results, merged: maxima and sums first
+    const uint32_t par = pieces & 1;
+    auto meet = [&](int i) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sm.bar_merge[i]));
+      ok = ok && mbar_wait_warp(smem_u32(&sm.bar_merge[i]), par, abort_flag);
+    };
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float x = l[nb][e];
+        x += __shfl_xor_sync(full, x, 4);
+        x += __shfl_xor_sync(full, x, 8);
+        x += __shfl_xor_sync(full, x, 16);
+        if (g == 0) sm.ml[warp][8 * nb + 2 * t + e] = make_float2(m[nb][e], x);
+      }
+    meet(0);
+    if (!ok) break;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float M = -INFINITY, L = 0.f;
+#pragma unroll
+        for (int w = 0; w < C::kKeyGroups; ++w) M = fmaxf(M, sm.ml[w * RG + rg][8 * nb + 2 * t + e].x);
+        const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int w = 0; w < C::kKeyGroups; ++w) {
+          const float2 x = sm.ml[w * RG + rg][8 * nb + 2 * t + e];
+          L = fmaf(exp2_approx(x.x - ref), x.y, L);
+        }
+        const float f = exp2_approx(m[nb][e] - ref);
+        if (kg == 0 && g == 0) sm.fin[(rg * NB + nb) * 8 + 2 * t + e] = make_float2(M, L);
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+          o[nb][k][e] *= f;
+          o[nb][k][e + 2] *= f;
+        }
+      }
+    // then O: the upper half of the warps' onto the lower half's, those summed by all
+    constexpr int kHalf = C::kKeyGroups / 2;
+    float4(*fold)[32] = sm.fold[(kg % kHalf) * RG + rg];
+    if (kg >= kHalf) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k)
+          fold[nb * kSteps + k][lane] = make_float4(o[nb][k][0], o[nb][k][1], o[nb][k][2], o[nb][k][3]);
+    }
+    meet(1);
+    if (!ok) break;
+    if (kg < kHalf) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+          float4 x = fold[nb * kSteps + k][lane];
+          x.x += o[nb][k][0], x.y += o[nb][k][1], x.z += o[nb][k][2], x.w += o[nb][k][3];
+          fold[nb * kSteps + k][lane] = x;
+        }
+    }
+    meet(2);
+    if (!ok) break;
+    // two blocks of channels (four channels side by side) of two rows a turn
+    const int rows = ntok * p.g;
+    for (int i = tid; i < RG * NB * (kSteps / 2) * 32; i += 32 * kWarps) {
+      const int ln = i & 31, j = i >> 5, k2 = j % (kSteps / 2), nb = j / (kSteps / 2) % NB, r = j / (kSteps / 2) / NB;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
+#pragma unroll
+      for (int w = 0; w < kHalf; ++w) {
+        const float4 a = sm.fold[w * RG + r][nb * kSteps + 2 * k2][ln], b = sm.fold[w * RG + r][nb * kSteps + 2 * k2 + 1][ln];
+        x.x += a.x, x.y += a.y, x.z += a.z, x.w += a.w;
+        y.x += b.x, y.y += b.y, y.z += b.z, y.w += b.w;
+      }
+      const int ch = (ln >> 2) * (D / 8) + 4 * k2;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int row = (r * NB + nb) * 8 + 2 * (ln & 3) + e;
+        if (row >= rows) continue;
+        const float2 ml = sm.fin[row];
+        // (a sum that is NaN is passed on, not hidden)
+        const bool any = ml.y != 0.f && !bad;
+        const float o0 = e ? x.y : x.x, o1 = e ? x.w : x.z, o2 = e ? y.y : y.x, o3 = e ? y.w : y.z;
+        if (part) {
+          *reinterpret_cast<float4*>(partial_o<D, RB>(p, entry, row) + ch) = any ? make_float4(o0, o1, o2, o3) : make_float4(0.f, 0.f, 0.f, 0.f);
+          if (ch == 0) *partial_ml<D, RB>(p, entry, row) = make_float2(any ? ml.x : -INFINITY, any ? ml.y : bad ? -1.f : 0.f);
+        } else {
+          const float inv = any ? p.c.v_unit / ml.y : 0.f;
+          const int tl = row / p.g;
+          const size_t out_row = static_cast<size_t>(tok0 + tl) * p.a.Hq + kvh * p.g + (row - tl * p.g);
+          const __nv_bfloat162 lo2 = __floats2bfloat162_rn(o0 * inv, o1 * inv), hi2 = __floats2bfloat162_rn(o2 * inv, o3 * inv);
+          *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.a.out) + out_row * D + ch) =
+              any ? make_uint2(*reinterpret_cast<const uint32_t*>(&lo2), *reinterpret_cast<const uint32_t*>(&hi2)) : make_uint2(0u, 0u);
+          if (p.a.lse && ch == 0) p.a.lse[out_row] = any ? (ml.x + log2f(ml.y)) * kLn2 : -INFINITY;
+        }
+      }
+    }
+    ++pieces;
+  }
+  if (!ok) give_up();
+}
+
+// Merge of cut units: block (c - 1, y) takes run boundary c and, of its unit's
+// query rows, every gridDim.y-th group of 1024 / D; a thread owns four columns.
+template <int D, int RB>
+__global__ void __launch_bounds__(256) chunk_q4_merge_kernel(const __grid_constant__ Q4Params p) {
+  pdl_wait();
+  pdl_launch_next();
+  const Record rec = records<D, RB>(p)[blockIdx.x + 1];
+  const int np = rec.c1 - rec.c0 + 1, rows = rec.ntok * p.g, ch = 4 * (threadIdx.x % (D / 4));
+  for (int row = blockIdx.y * (1024 / D) + threadIdx.x / (D / 4); row < rows; row += gridDim.y * (1024 / D)) {
+    auto entry = [&](int j) { return (rec.c0 + j) * 2 + (j == 0 ? rec.slot : 0); };
+    float M = -INFINITY, L = 0.f;
+    bool bad = false;
+#pragma unroll 4
+    for (int j = 0; j < np; ++j) {
+      const float2 ml = *partial_ml<D, RB>(p, entry(j), row);
+      if (ml.y != 0.f) M = fmaxf(M, ml.x);
+      bad |= ml.y == -1.f;
+    }
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int j = 0; j < np; ++j) {
+      const float2 ml = *partial_ml<D, RB>(p, entry(j), row);
+      const float4 o = *reinterpret_cast<const float4*>(partial_o<D, RB>(p, entry(j), row) + ch);
+      const float w = ml.y != 0.f && !bad ? exp2f(ml.x - (M == -INFINITY ? 0.f : M)) : 0.f;
+      L = fmaf(w, ml.y, L);
+      acc.x = fmaf(w, o.x, acc.x);
+      acc.y = fmaf(w, o.y, acc.y);
+      acc.z = fmaf(w, o.z, acc.z);
+      acc.w = fmaf(w, o.w, acc.w);
+    }
+    const bool any = L != 0.f && !bad;
+    const float inv = any ? p.c.v_unit / L : 0.f;
+    const int tl = row / p.g;
+    const size_t out_row = static_cast<size_t>(rec.tok0 + tl) * p.a.Hq + rec.kvh * p.g + (row - tl * p.g);
+    const __nv_bfloat162 lo2 = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi2 = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.a.out) + out_row * D + ch) =
+        any ? make_uint2(*reinterpret_cast<const uint32_t*>(&lo2), *reinterpret_cast<const uint32_t*>(&hi2)) : make_uint2(0u, 0u);
+    if (p.a.lse && ch == 0) p.a.lse[out_row] = any ? (M + log2f(L)) * kLn2 : -INFINITY;
+  }
+}
+
+// Query rows of a unit: the fewest that hold a sequence's rows on average and
+// a token's heads.
+int q4_rows(int T, int Bt, int g) {
+  for (int rb : {8, 16, 32})
+    if (g <= rb && static_cast<long long>(T) * g <= static_cast<long long>(rb) * Bt) return rb;
+  return 64;
+}
+constexpr int q4_ctas(int rows, int num_sms) { return (rows == 8 ? 2 : 1) * num_sms; }
+
+template <int D, int NB, int RG, bool SINKS>
+cudaError_t launch_rows(Q4Params p, int num_sms, cudaStream_t stream) {
+  using C = Cfg<D, NB, RG>;
+  constexpr size_t bytes = sizeof(SmemQ4<D, NB, RG>) + 128;
+  static_assert(C::kCtas * (bytes + 1024) <= 228 * 1024, "shared memory of an SM");
+  p.ub = C::kRows / p.g;
+  p.ctas = C::kCtas * num_sms;
+  static std::mutex mu;
+  static bool done[64] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  {
+    std::lock_guard<std::mutex> lk(mu);
+    if (!done[dev]) {
+      e = cudaFuncSetAttribute(chunk_q4_kernel<D, NB, RG, SINKS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               static_cast<int>(bytes));
+      if (e != cudaSuccess) return e;
+      done[dev] = true;
+    }
+  }
+  e = launch_overlapped(chunk_q4_kernel<D, NB, RG, SINKS>, dim3(static_cast<unsigned>(p.ctas)), dim3(kThreads), bytes,
+                        stream, 1u, p);
+  if (e != cudaSuccess || p.ctas == 1) return e;
+  return launch_overlapped(chunk_q4_merge_kernel<D, C::kRows>, dim3(static_cast<unsigned>(p.ctas - 1), C::kRows > 16 ? 4u : 1u),
+                           dim3(256), 0, stream, 1u, p);
+}
+
+template <int D, bool SINKS>
+cudaError_t launch_d(const Q4Params& p, int num_sms, cudaStream_t stream) {
+  switch (q4_rows(p.a.T, p.a.Bt, p.g)) {
+    case 8: return launch_rows<D, 1, 1, SINKS>(p, num_sms, stream);
+    case 16: return launch_rows<D, 2, 1, SINKS>(p, num_sms, stream);
+    case 32: return launch_rows<D, 2, 2, SINKS>(p, num_sms, stream);
+    default: return launch_rows<D, 2, 4, SINKS>(p, num_sms, stream);
+  }
+}
+
+}  // namespace
+
+bool chunk_q4_few(int dtype, int T, int Bt, int Hq, int Hkv) {
+  return dtype == SIMSD_BF16 && Hq / Hkv <= 64 && static_cast<long long>(T) * Hq <= 64ll * Bt * Hkv;
+}
+
+size_t chunk_q4_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, int num_sms) {
+  const int rows = q4_rows(T, Bt, Hq / Hkv);
+  return static_cast<size_t>(q4_ctas(rows, num_sms)) * (2ull * rows * (d + 2) * sizeof(float) + sizeof(Record));
+}
+
+cudaError_t launch_chunk_attention_q4(const ChunkArgs& a, const simsd_q4_cache& c, int num_sms, cudaStream_t stream) {
+  Q4Params p{};
+  p.a = a;
+  p.c = c;
+  p.g = a.Hq / a.Hkv;
+  p.sub = a.page_size % kTile == 0 ? kTile : std::min(a.page_size, 64);
+  p.scale_log2 = a.scale * c.k_unit * 1.4426950408889634f;
+  if (a.sinks > 0) return a.d == 128 ? launch_d<128, true>(p, num_sms, stream) : launch_d<64, true>(p, num_sms, stream);
+  return a.d == 128 ? launch_d<128, false>(p, num_sms, stream) : launch_d<64, false>(p, num_sms, stream);
+}
+
+}  // namespace simsd

@@ -55,7 +55,7 @@
 #include <algorithm>
 #include <mutex>
 
-#include "chunk_mask.cuh"
+#include "chunk_walk.cuh"
 #include "common.cuh"
 #include "kernels.h"
 #include "ptx_chunk.cuh"
@@ -94,7 +94,15 @@ struct alignas(16) Piece {
   int n, C, ks, i0;    // the sequence (chunk_mask.cuh) and the unit's first token in it
   int part, slot;      // writes partial results (slot 0: the piece at the start of the run)
   int last, flag;      // the CTA's last piece; its entry in `bad`
+  // first rows that stay visible through the window (only where there are any)
+  int se, w0;          // rows [se, w0) are seen by none of the unit's tokens
+  int tse, skip;       // tile t lies `skip` tiles further from tile tse on
 };
+template <bool SINKS>
+__device__ __forceinline__ int tile_row(const Piece& u, int t) {
+  if constexpr (SINKS) t += t >= u.tse ? u.skip : 0;
+  return t * kTile;
+}
 
 template <int D>
 struct alignas(1024) SmemChunk {
@@ -132,138 +140,11 @@ __device__ __forceinline__ void signal_abort(SmemChunk<D>& sm, int32_t* err_word
   *reinterpret_cast<volatile int*>(&sm.abort_flag) = 1;
 }
 
-// The keys that unit j of a sequence sees, and its weight in the walk: its
-// key tiles, one where it sees none (somebody has to zero its rows).
-struct Range {
-  int lo, hi;
-};
-__device__ __forceinline__ Range unit_range(const ChunkTcParams& p, const ChunkSeq& s, int j) {
-  if (s.bad) return Range{0, 0};
-  const int ub = 2 * p.tb, i0 = j * ub, i1 = min(s.C, i0 + ub);
-  const int lo = key_lo(p.a, s, i0), hi = key_hi(p.a, s, i1 - 1);
-  return lo < hi ? Range{lo, hi} : Range{0, 0};
-}
-__device__ __forceinline__ int range_tiles(const Range& r) {
-  return r.hi > 0 ? (r.hi + kTile - 1) / kTile - r.lo / kTile : 0;
-}
-__device__ __forceinline__ int unit_weight(const ChunkTcParams& p, const ChunkSeq& s, int j) {
-  return max(1, range_tiles(unit_range(p, s, j)));
-}
-
-// Tiles of every sequence in `tiles` (shared, kChunkMaxSeqs ints).  Every
-// thread of the block takes part.
-__device__ __forceinline__ void plan_tiles(const ChunkTcParams& p, int32_t* tiles) {
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int ub = 2 * p.tb;
-  uint32_t err = 0;
-  bool is_long = false;
-  // short chunks: a thread per sequence; chunks of more than two units: a warp
-  for (int b = tid; b < p.a.Bt; b += kThreads) {
-    const ChunkSeq s = chunk_seq(p.a, b);
-    err |= (s.bad_off ? SIMSD_EW_TOKENS : 0u) | (s.bad && s.C > 0 ? SIMSD_EW_PREFIX_LEN : 0u);
-    int v = 0;
-    if (s.C > 2 * ub) {
-      v = -1;
-      is_long = true;
-    } else if (s.C > 0) {
-      v = unit_weight(p, s, 0);
-      if (s.C > ub) v += unit_weight(p, s, 1);
-    }
-    tiles[b] = v;
-  }
-  if (err && blockIdx.x == 0) raise_error(p.a.err_word, err);
-  if (__syncthreads_or(is_long)) {
-    for (int b = warp; b < p.a.Bt; b += kThreads / 32) {
-      if (tiles[b] >= 0) continue;
-      const ChunkSeq s = chunk_seq(p.a, b);
-      const int units = (s.C + ub - 1) / ub;
-      int v = 0;
-      for (int j = lane; j < units; j += 32) v += unit_weight(p, s, j);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-      if (lane == 0) tiles[b] = v;
-    }
-  }
-  // The host's bound on the tiles of a call holds for offsets in order; those
-  // that are not may make chunks overlap beyond it, and then nothing is done.
-  // (Checked only where some are not: in plan_start, for every call, long
-  // prompts came out 5 to 9% slower.)
-  if (!__syncthreads_or(err & SIMSD_EW_TOKENS)) return;
-  long long all = 0;
-  for (int b = 0; b < p.a.Bt; ++b) all += tiles[b];
-  __syncthreads();
-  if (all * p.a.Hkv >= (1ll << 31))
-    for (int b = tid; b < p.a.Bt; b += kThreads) tiles[b] = 0;
-  __syncthreads();
-}
-
-__device__ __forceinline__ int warp_inclusive(int v) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, v, o);
-    if (lane >= o) v += y;
-  }
-  return v;
-}
-
-// A place in the walk: tile t of unit (b, j) for a KV head.
-struct Place {
-  int b, j, kvh, t;
-};
-
-// The total (per KV head), and the place of the CTA's run start.  One warp.
-__device__ __forceinline__ Place plan_start(const ChunkTcParams& p, const int32_t* tiles, int& total, ChunkSeq& s) {
-  const unsigned full = 0xffffffffu;
-  const int lane = threadIdx.x & 31, ub = 2 * p.tb;
-  int sum = 0;
-  for (int b = lane; b < p.a.Bt; b += 32) sum += tiles[b];
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(full, sum, o);
-  total = sum;
-  Place w{0, 0, 0, 0};
-  const int all = sum * p.a.Hkv, W = (all + p.ctas - 1) / p.ctas;
-  const long long R0 = static_cast<long long>(W) * blockIdx.x;
-  if (R0 >= all) return w;
-  w.kvh = static_cast<int>(R0) / sum;
-  int at = static_cast<int>(R0) - w.kvh * sum;  // tiles before the run within the head
-  for (int b0 = 0; b0 < p.a.Bt; b0 += 32) {
-    const int v = b0 + lane < p.a.Bt ? tiles[b0 + lane] : 0;
-    const int inc = warp_inclusive(v);
-    const unsigned m = __ballot_sync(full, inc > at);
-    if (m) {
-      const int k = __ffs(m) - 1;
-      w.b = b0 + k;
-      at -= __shfl_sync(full, inc - v, k);
-      break;
-    }
-    at -= __shfl_sync(full, inc, 31);
-  }
-  s = chunk_seq(p.a, w.b);
-  for (int j0 = 0; j0 * ub < s.C; j0 += 32) {
-    const int v = (j0 + lane) * ub < s.C ? unit_weight(p, s, j0 + lane) : 0;
-    const int inc = warp_inclusive(v);
-    const unsigned m = __ballot_sync(full, inc > at);
-    if (m) {
-      const int k = __ffs(m) - 1;
-      w.j = j0 + k;
-      w.t = at - __shfl_sync(full, inc - v, k);
-      break;
-    }
-    at -= __shfl_sync(full, inc, 31);
-  }
-  return w;
-}
-
 // Partial results: O (unnormalised, fp32) as [ctas * 4 entries][D / 4][128
 // rows] vectors of four (a warp's 32 rows are adjacent, so they are written
 // and read in whole lines), (m, l) [entries][128], entry (cta * 2 + slot) * 2
 // + block, m in log2 units, l = -1 where a page id of the piece is out of
-// range (the row is zero then); then one record per run boundary.
-struct Record {
-  int tok0, ntok, kvh, c0;  // ntok 0: the boundary cuts no unit, or not as the first
-  int c1, slot, pad0, pad1;
-};
+// range (the row is zero then); then one Record per run boundary.
 template <int D>
 __device__ __forceinline__ float4* partial_o(const ChunkTcParams& p, int entry, int col4, int row) {
   return static_cast<float4*>(p.a.workspace) + (static_cast<size_t>(entry) * (D / 4) + col4) * kRows + row;
@@ -288,7 +169,7 @@ __device__ __forceinline__ void st_global_256(void* p, const uint32_t (&v)[8]) {
 
 // The next message of the unit queue, copied to the registers of a warp;
 // false when a wait expired.
-template <int D>
+template <int D, bool SINKS>
 __device__ __forceinline__ bool next_piece(SmemChunk<D>& sm, uint32_t& at, Piece& u) {
   volatile int* abort_flag = &sm.abort_flag;
   const uint32_t st = at % kQueue, par = (at / kQueue) & 1;
@@ -311,13 +192,21 @@ __device__ __forceinline__ bool next_piece(SmemChunk<D>& sm, uint32_t& at, Piece
   u.slot = d.y;
   u.last = d.z;
   u.flag = d.w;
+  if constexpr (SINKS) {
+    const int4 e = src[4];
+    u.se = e.x;
+    u.w0 = e.y;
+    u.tse = e.z;
+    u.skip = e.w;
+  }
   __syncwarp();
   if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&sm.bar_msgfree[st]));
   ++at;
   return true;
 }
 
-template <int D>
+// SINKS: the first rows of a sequence stay visible through the window
+template <int D, bool SINKS>
 __global__ void __launch_bounds__(kThreads, 1)
     chunk_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ ChunkTcParams p) {
@@ -362,11 +251,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   pdl_wait();
   int32_t* tiles = reinterpret_cast<int32_t*>(sm.ring[0]);
-  plan_tiles(p, tiles);
+  plan_tiles<SINKS, kTile, kThreads>(p.a, 2 * p.tb, tiles);
   Place start{0, 0, 0, 0};
   int total = 0;
   ChunkSeq seq{};
-  if (warp == kWarpWalk) start = plan_start(p, tiles, total, seq);
+  if (warp == kWarpWalk) start = plan_start<SINKS, kTile>(p.a, 2 * p.tb, p.ctas, tiles, total, seq);
   fence_proxy_async_smem();  // the ring was written here and is filled by TMA next
   tc_fence_before();
   __syncthreads();
@@ -378,70 +267,39 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == kWarpWalk) {
       // ---------------------------------------------------------------- walk
-      // the run [R0, R1): from the first unit that starts in it to R1, then
-      // the unit cut at R0, so that both pieces of a cut unit are written
-      // near the end of the launch
-      const int all = total * p.a.Hkv, W = (all + p.ctas - 1) / p.ctas;
-      const long long R0 = static_cast<long long>(W) * blockIdx.x;
-      int left = R0 < all ? min(W, all - static_cast<int>(R0)) : 0;
-      Place w = start;
-      ChunkSeq s = seq;
-      int head = 0;
-      bool first = true;
-      auto advance = [&]() {
-        // to the next unit that exists
-        ++w.j;
-        w.t = 0;
-        if (w.j * 2 * p.tb < s.C) return;
-        w.j = 0;
-        do {
-          if (++w.b == p.a.Bt) {
-            w.b = 0;
-            if (++w.kvh == p.a.Hkv) return;
-          }
-          s = chunk_seq(p.a, w.b);
-        } while (s.C == 0);
-      };
-      if (left > 0 && w.t > 0) {
-        head = min(left, unit_weight(p, s, w.j) - w.t);
-        left -= head;
-        first = false;
-        if (left > 0) advance();
-      }
+      const int ub = 2 * p.tb;
+      Walk<SINKS, kTile> k;
+      k.begin(p.a, ub, p.ctas, start, seq, total);
+      typename Walk<SINKS, kTile>::Step piece;
       uint32_t at = 0;
       bool ok = true;
       for (;;) {
-        if (left == 0 && head > 0) {
-          left = head;
-          head = 0;
-          w = start;
-          s = seq;
-          first = true;
-        }
         Piece u;
         u.tiles = -1;
-        if (left > 0) {
-          const Range r = unit_range(p, s, w.j);
-          const int n = range_tiles(r), weight = max(1, n), take = min(weight - w.t, left);
-          u.i0 = w.j * 2 * p.tb;
-          u.tok0 = s.start + u.i0;
-          u.ntok = min(2 * p.tb, s.C - u.i0);
-          u.kvh = w.kvh;
-          u.b = w.b;
-          u.t0 = r.lo / kTile + w.t;
-          u.tiles = n == 0 ? 0 : take;
-          u.lo = r.lo;
-          u.hi = r.hi;
-          u.n = s.n;
-          u.C = s.C;
-          u.ks = s.ks;
-          u.part = take < weight;
-          u.slot = first ? 0 : 1;
-          first = false;
-          left -= take;
-          u.last = left == 0 && head == 0;
+        if (k.peek(p.a, ub, piece)) {
+          u.i0 = k.w.j * ub;
+          u.tok0 = k.s.start + u.i0;
+          u.ntok = min(ub, k.s.C - u.i0);
+          u.kvh = k.w.kvh;
+          u.b = k.w.b;
+          u.t0 = piece.keys.lo / kTile + k.w.t;
+          u.tiles = piece.tiles == 0 ? 0 : piece.take;
+          u.lo = piece.keys.lo;
+          u.hi = piece.keys.hi;
+          u.n = k.s.n;
+          u.C = k.s.C;
+          u.ks = k.s.ks;
+          u.part = piece.take < piece.weight;
+          u.slot = piece.slot;
+          u.last = piece.last;
           u.flag = at % kFlags;
-          if (left > 0) advance();
+          if constexpr (SINKS) {
+            u.se = piece.keys.se;
+            u.w0 = piece.keys.w0;
+            u.tse = (u.se + kTile - 1) / kTile;
+            u.skip = tiles_skipped<SINKS, kTile>(piece.keys);
+          }
+          k.pop(p.a, ub, piece);
         }
         const uint32_t st = at % kQueue, use = at / kQueue;
         if (use > 0) ok = mbar_wait_warp(smem_u32(&sm.bar_msgfree[st]), (use - 1) & 1, abort_flag);
@@ -454,29 +312,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (u.tiles < 0) break;
       }
       if (!ok && lane == 0) signal_abort(sm, p.a.err_word);
-      // the record of run boundary blockIdx.x: the unit that it is the first to cut
-      if (lane == 0 && blockIdx.x > 0) {
-        Record rec{};
-        if (R0 < all && start.t > 0) {
-          const int weight = unit_weight(p, seq, start.j), begin = static_cast<int>(R0) - start.t, c0 = begin / W;
-          if (c0 + 1 == static_cast<int>(blockIdx.x)) {
-            rec.tok0 = seq.start + start.j * 2 * p.tb;
-            rec.ntok = min(2 * p.tb, seq.C - start.j * 2 * p.tb);
-            rec.kvh = start.kvh;
-            rec.c0 = c0;
-            rec.c1 = (begin + weight - 1) / W;
-            rec.slot = begin != c0 * W ? 1 : 0;
-          }
-        }
-        records<D>(p)[blockIdx.x] = rec;
-      }
+      if (lane == 0 && blockIdx.x > 0) records<D>(p)[blockIdx.x] = boundary_record<SINKS, kTile>(k, p.a, ub);
     } else if (warp == kWarpProducer) {
       // ------------------------------------------------------------ producer
       uint32_t at = 0, jq[2] = {0, 0};
       uint32_t slot[2] = {0, 0}, par[2] = {0, 0}, used[2] = {0, 0};  // K, V: next slot, its parity, slots filled
       bool ok = true;
       Piece u;
-      while (ok && (ok = next_piece<D>(sm, at, u)) && u.tiles >= 0) {
+      while (ok && (ok = next_piece<D, SINKS>(sm, at, u)) && u.tiles >= 0) {
         if (u.tiles == 0) continue;
         const int nblk = u.ntok > p.tb ? 2 : 1;
         if (lane == 0) {
@@ -502,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         int win_base = -(1 << 30), win = -1;  // lane i holds the page id of page win_base + i
         bool bad = false;
         for (int t = u.t0; ok && t < u.t0 + u.tiles; ++t) {
-          const int key0 = t * kTile, valid = min(kTile, u.hi - key0);
+          const int key0 = tile_row<SINKS>(u, t), valid = min(kTile, u.hi - key0);
           const int nsub = (valid + sub - 1) / sub;
           const int pi0 = key0 / P, pi1 = (key0 + valid - 1) / P;  // at most 16 pages a tile
           if (pi0 < win_base || pi1 >= win_base + 32) {
@@ -515,8 +358,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           int pg = __shfl_sync(0xffffffffu, win, (pi - win_base) & 31);
           // a page id out of range is replaced by page 0, and the softmax
           // warps, which see this flag no later than the S of this tile, zero
-          // the piece's rows (hidden keys before the first need no page)
-          const bool wrong = (pg < 0 || pg >= p.a.num_pages) && key + sub > u.lo;
+          // the piece's rows (rows that no token sees need no page)
+          const bool wrong = (pg < 0 || pg >= p.a.num_pages) && key + sub > u.lo &&
+                             (!SINKS || key < u.se || key + sub > u.w0);
           if (pg < 0 || pg >= p.a.num_pages) pg = 0;
           bad |= __any_sync(0xffffffffu, wrong);
           if (lane == 0 && (t == u.t0 || bad)) {
@@ -618,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       Piece u;
       bool ok = true;
-      while (ok && (ok = next_piece<D>(sm, at, u)) && u.tiles >= 0) {
+      while (ok && (ok = next_piece<D, SINKS>(sm, at, u)) && u.tiles >= 0) {
         const int n = u.tiles;
         if (n == 0) continue;
         if (x == 1 && u.ntok <= p.tb) {
@@ -682,12 +526,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t g = 0, c = 0, at = 0;
     bool ok = true;
     Piece u;
-    while ((ok = ok && next_piece<D>(sm, at, u)) && u.tiles >= 0) {
+    while ((ok = ok && next_piece<D, SINKS>(sm, at, u)) && u.tiles >= 0) {
       const int xt = x * p.tb + tl;  // token of this row within the unit
       const bool row_exists = tl < p.tb && xt < u.ntok;
       const bool has = x == 0 || u.ntok > p.tb;
       const bool active = row_exists && u.tiles > 0;
-      int klo = 0, khi = 0;  // this row's keys
+      int klo = 0, khi = 0, kse = 0;  // this row's keys: [klo, khi), and [u.ks, kse) where first rows stay visible
       if (active) {
         ChunkSeq s;
         s.n = u.n;
@@ -695,6 +539,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         s.ks = u.ks;
         klo = key_lo(p.a, s, u.i0 + xt);
         khi = key_hi(p.a, s, u.i0 + xt);
+        if constexpr (SINKS) kse = sink_end(p.a, s, khi);
       }
       const bool seen = klo < khi;
       // a warp without a row that sees a key only keeps the hand-offs going
@@ -705,7 +550,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool have_o = false;
       if (u.tiles > 0 && has) {
         for (int i = 0; i < u.tiles; ++i, ++c) {
-          const int key0 = (u.t0 + i) * kTile;
+          const int key0 = tile_row<SINKS>(u, u.t0 + i);
           if (!mbar_wait_warp(smem_u32(&sm.bar_s[x]), c & 1, abort_flag)) {
             ok = false;
             break;
@@ -718,13 +563,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           // does not tell apart.  The block's MMA warp, which has waited for
           // every use of V in turn, issues this S after the last one before
           // this tile's, so from here the parity names one use.
-          if (key0 < u.lo || key0 + kTile > u.hi) {
+          if (key0 < u.lo || key0 + kTile > u.hi || (SINKS && key0 < u.w0 && key0 + kTile > u.se)) {
             const uint32_t gt = g + i, vst = kStagesK + gt % kStagesV;  // the tile's V slot
             if (!mbar_wait_warp(smem_u32(&sm.bar_full[vst]), (gt / kStagesV) & 1, abort_flag)) {
               ok = false;
               break;
             }
-            if (key0 + row < u.lo || key0 + row >= u.hi) {
+            const int key = key0 + row;
+            if (key < u.lo || key >= u.hi || (SINKS && key >= u.se && key < u.w0)) {
               const uint4 z = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
               for (int hf = 0; hf < kHalves; ++hf) {
@@ -755,7 +601,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int wd = 0; wd < 4; ++wd) {
               const int f = min(max(from - 32 * wd, 0), 32), e = min(max(to - 32 * wd, 0), 32);
               // bits f .. e-1
-              const uint32_t keep = e > f ? (0xffffffffu >> (32 - (e - f))) << f : 0u;
+              uint32_t keep = e > f ? (0xffffffffu >> (32 - (e - f))) << f : 0u;
+              if constexpr (SINKS) {
+                const int sf = min(max(u.ks - key0 - 32 * wd, 0), 32), se = min(max(kse - key0 - 32 * wd, 0), 32);
+                keep |= se > sf ? (0xffffffffu >> (32 - (se - sf))) << sf : 0u;
+              }
 #pragma unroll
               for (int k = 0; k < 32; ++k) xs[wd][k] = (keep >> k) & 1u ? xs[wd][k] : 0xff800000u;
             }
@@ -1012,13 +862,15 @@ cudaError_t launch_d(const ChunkArgs& a, int num_sms, EncodeTiledFn encode, cuda
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     std::lock_guard<std::mutex> lk(mu);
     if (!done[dev]) {
-      e = cudaFuncSetAttribute(chunk_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                               static_cast<int>(smem_bytes<D>()));
+      const int bytes = static_cast<int>(smem_bytes<D>());
+      e = cudaFuncSetAttribute(chunk_tc_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+      if (e != cudaSuccess) return e;
+      e = cudaFuncSetAttribute(chunk_tc_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
       if (e != cudaSuccess) return e;
       done[dev] = true;
     }
   }
-  cudaError_t e = launch_overlapped(chunk_tc_kernel<D>, dim3(static_cast<unsigned>(p.ctas)), dim3(kThreads),
+  cudaError_t e = launch_overlapped(a.sinks > 0 ? chunk_tc_kernel<D, true> : chunk_tc_kernel<D, false>, dim3(static_cast<unsigned>(p.ctas)), dim3(kThreads),
                                     smem_bytes<D>(), stream, 1u, tq, tk, tv, p);
   if (e != cudaSuccess || p.ctas == 1) return e;
   // units of many rows: 16 blocks to a boundary (two passes over 256 rows; the

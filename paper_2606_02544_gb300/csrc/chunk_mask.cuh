@@ -4,6 +4,8 @@
 //   hi = N (mask_block 0), else min(N, (p / mask_block + 1) mask_block),
 //   lo = max(0, key_start, p + 1 - window where window > 0);
 // both grow with p, so a range of tokens sees [lo of the first, hi of the last).
+// With `sinks` the rows ks <= j < min(ks + sinks, hi), ks = max(0, key_start),
+// stay visible to it through the window.
 #pragma once
 #include "common.cuh"
 #include "kernels.h"
@@ -40,6 +42,11 @@ __device__ __forceinline__ int key_hi(const ChunkArgs& a, const ChunkSeq& s, int
 
 __device__ __forceinline__ int key_lo(const ChunkArgs& a, const ChunkSeq& s, int i) {
   return a.window > 0 ? max(s.ks, s.n + i + 1 - a.window) : s.ks;
+}
+
+// End of the first rows that stay visible to a token that sees rows below hi.
+__device__ __forceinline__ int sink_end(const ChunkArgs& a, const ChunkSeq& s, int hi) {
+  return static_cast<int>(min(static_cast<long long>(hi), static_cast<long long>(s.ks) + a.sinks));
 }
 
 }  // namespace simsd

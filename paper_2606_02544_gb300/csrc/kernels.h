@@ -159,6 +159,7 @@ struct ChunkArgs {
   int32_t* err_word;
   int T, Bt, Hq, Hkv, d, num_pages, max_pages, page_size, mask_block, window;
   float scale;
+  int sinks;  // first rows that stay visible through the window (0 without one)
 };
 size_t chunk_f32_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, long long max_keys, int num_sms);
 cudaError_t launch_chunk_attention_f32(const ChunkArgs& a, int num_sms, cudaStream_t stream);
@@ -166,6 +167,47 @@ cudaError_t launch_chunk_attention_f32(const ChunkArgs& a, int num_sms, cudaStre
 constexpr int kChunkMaxSeqs = 16384;
 size_t chunk_tc_workspace_bytes(int T, int Bt, int d, int num_sms);
 cudaError_t launch_chunk_attention_tc(const ChunkArgs& a, int num_sms, EncodeTiledFn encode, cudaStream_t stream);
+
+// The way of a chunk into a cache in 4 bits, and back (q4_cache.cu).  k_cache
+// and v_cache of RopeArgs are not used; d 64 or 128.
+cudaError_t launch_rope_q4(int elem_bytes, const RopeArgs& a, const simsd_q4_cache& c, int num_sms,
+                           cudaStream_t stream);
+struct ExpandArgs {
+  simsd_q4_cache c;
+  const int32_t *first, *last, *block_table;  // rows [first, last) of each sequence
+  void *k_cache, *v_cache;
+  int32_t* err_word;
+  int num_pages, max_pages, page_size, Bt, Hkv, d;
+};
+cudaError_t launch_q4_expand(int elem_bytes, const ExpandArgs& a, int num_sms, cudaStream_t stream);
+// the rows that a call of attention sees, without errors raised
+cudaError_t launch_q4_expand_seen(int elem_bytes, const ChunkArgs& a, const simsd_q4_cache& c, void* k_image,
+                                  void* v_image, int num_sms, cudaStream_t stream);
+
+// Attention over a cache in 4 bits, few rows a sequence (chunk_attention_q4.cu).
+bool chunk_q4_few(int dtype, int T, int Bt, int Hq, int Hkv);
+size_t chunk_q4_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, int num_sms);
+cudaError_t launch_chunk_attention_q4(const ChunkArgs& a, const simsd_q4_cache& c, int num_sms, cudaStream_t stream);
+
+// Pages of a cache (pages.cu).
+struct PageArrays {
+  simsd_page_array array[SIMSD_MAX_PAGE_ARRAYS];
+  int n;
+};
+struct PagesArgs {
+  PageArrays pages;
+  const int32_t *seq, *src, *dst, *first, *last, *add;
+  int32_t *lens, *block_table, *refs, *live;
+  void* workspace;
+  int32_t* err_word;
+  int n, num_pages, Bt, max_pages, page_size;
+};
+constexpr int kPagesMaxSeqs = 65536;
+size_t pages_workspace_bytes(int num_pages, int pairs);
+cudaError_t launch_pages_extend(const PagesArgs& a, cudaStream_t stream);
+cudaError_t launch_pages_release(const PagesArgs& a, int num_sms, cudaStream_t stream);
+cudaError_t launch_pages_fork(const PagesArgs& a, int num_sms, cudaStream_t stream);
+cudaError_t launch_pages_compact(const PagesArgs& a, int num_sms, cudaStream_t stream);
 
 // One token from each row of logits (sample.cu).
 struct SampleArgs {

@@ -1,0 +1,328 @@
+// q4_cache.cu -- the way of a chunk of tokens into a paged cache in 4 bits,
+// and the rows of such a cache written out again (Sec. 3.3: the prefix is
+// read from a KV cache; keys are cached rotated).
+//
+// Mathematics.  The rotation is that of rope_append.cu.  A group of 16
+// components becomes s = (max |x| / 6) to nearest in 8 bits and codes (x / s)
+// to nearest in 4 bits; the rotated key is divided as it is in fp32, without
+// a rounding to the type before, and the quotient is correctly rounded (a
+// product with 1 / s would put ties of 16-bit values on the wrong side).
+// Written out, s times a code has 6 significant bits: exact in fp16 and bf16.
+//
+// A thread owns four components: a row of 128 is a warp's (of 64, half a
+// warp's), a group four lanes', so a row's angles are formed once a lane and
+// serve every head of the token that the warp visits, a rotation's partner
+// comes by shuffle and a group's largest by two.
+//
+// Bound by memory: a token reads (Hq + 2 Hkv) d elements and writes Hq d and
+// 2 Hkv (d / 2 + d / 16) bytes.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "chunk_walk.cuh"
+#include "common.cuh"
+#include "kernels.h"
+#include "q4.cuh"
+#include "rope_token.cuh"
+
+namespace simsd {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxTokens = 64;  // tokens of a block
+constexpr int kInFlight = 4;    // rows of a warp whose loads are issued together
+
+struct alignas(8) Bf16x4 {
+  __nv_bfloat162 a, b;
+};
+__device__ __forceinline__ void load4(const float* p, float (&x)[4]) {
+  const float4 v = *reinterpret_cast<const float4*>(p);
+  x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+}
+__device__ __forceinline__ void load4(const __nv_bfloat16* p, float (&x)[4]) {
+  const Bf16x4 v = *reinterpret_cast<const Bf16x4*>(p);
+  const float2 a = __bfloat1622float2(v.a), b = __bfloat1622float2(v.b);
+  x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+}
+__device__ __forceinline__ void store4(float* p, const float (&x)[4]) {
+  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&x)[4]) {
+  *reinterpret_cast<Bf16x4*>(p) = Bf16x4{__floats2bfloat162_rn(x[0], x[1]), __floats2bfloat162_rn(x[2], x[3])};
+}
+
+// Warp item (token, group of heads): rows of heads grp, grp + groups, ...
+// (pairs of heads where a row takes half a warp).
+template <typename E, int D>
+__global__ void __launch_bounds__(kThreads, 4) rope_q4_kernel(const __grid_constant__ RopeArgs a,
+                                                              const __grid_constant__ simsd_q4_cache c) {
+  constexpr int kLanes = D / 4, kRows = 32 / kLanes;  // lanes of a row, rows of a warp
+  __shared__ Token toks[kMaxTokens];
+  pdl_wait();
+  pdl_launch_next();
+  const unsigned full = 0xffffffffu;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int tok0 = blockIdx.x * a.tokens_block;
+  if (blockIdx.x == 0) {
+    bool bad = false;
+    for (int b = threadIdx.x; b < a.Bt; b += kThreads) bad |= chunk_of(a.token_start, b, a.T).bad;
+    if (bad) raise_error(a.err_word, SIMSD_EW_TOKENS);
+  }
+  for (int i = warp; i < a.tokens_block && tok0 + i < a.T; i += kThreads / 32) {
+    const Token t = resolve(a, tok0 + i, true);
+    if (lane == 0) toks[i] = t;
+  }
+  __syncthreads();
+  const int r = a.plan.rot_dim, half = r / 2;
+  const bool by_half = a.plan.layout == SIMSD_ROPE_HALF;
+  const int at = lane & (kLanes - 1), base = lane - at, comp = 4 * at, sub = lane / kLanes;
+  const int heads = a.Hq + 2 * a.Hkv, steps = (heads + kRows - 1) / kRows;
+  const float k_inv = 1.f / c.k_unit, v_inv = 1.f / c.v_unit;
+  // where a component's partner lies (rotate-half; its lane, whole vectors)
+  const bool whole = (half & 3) == 0;
+  const int partner = comp < half ? lane + half / 4 : comp < r ? lane - half / 4 : lane;
+  for (int w = warp; w < a.tokens_block * a.groups; w += kThreads / 32) {
+    const int i = w / a.groups, grp = w - i * a.groups, tok = tok0 + i;
+    if (tok >= a.T) break;
+    const Token tk = toks[i];
+    if (tk.state == 0) continue;
+    // x turned: x cs + partner sn (the partner's sign in sn)
+    float cs[4], sn[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int k = comp + e;
+      cs[e] = 1.f;
+      sn[e] = 0.f;
+      if (k < r) {
+        const int pair = by_half ? (k < half ? k : k - half) : k >> 1;
+        const bool first = by_half ? k < half : (k & 1) == 0;
+        const unsigned long long turn = static_cast<unsigned long long>(static_cast<long long>(tk.pos)) * a.plan.turn[pair];
+        sincospif(static_cast<float>(static_cast<int32_t>(turn >> 32)) * 0x1p-31f, &sn[e], &cs[e]);
+        sn[e] *= first ? -a.plan.magnitude : a.plan.magnitude;
+        cs[e] *= a.plan.magnitude;
+      }
+    }
+    for (int s0 = grp; s0 < steps; s0 += a.groups * kInFlight) {
+      float x[kInFlight][4];
+#pragma unroll
+      for (int k = 0; k < kInFlight; ++k) {
+        const int h = (s0 + k * a.groups) * kRows + sub;
+        x[k][0] = x[k][1] = x[k][2] = x[k][3] = 0.f;
+        if (h < heads) {
+          const E* src = h < a.Hq ? static_cast<const E*>(a.q) + static_cast<long long>(tok) * a.q_stride + static_cast<long long>(h) * D
+                         : h < a.Hq + a.Hkv
+                             ? static_cast<const E*>(a.k) + static_cast<long long>(tok) * a.k_stride + static_cast<long long>(h - a.Hq) * D
+                             : static_cast<const E*>(a.v) + static_cast<long long>(tok) * a.v_stride +
+                                   static_cast<long long>(h - a.Hq - a.Hkv) * D;
+          load4(src + comp, x[k]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kInFlight; ++k) {
+        const int h = (s0 + k * a.groups) * kRows + sub;
+        if (s0 + k * a.groups >= steps) break;  // (the warp's lanes agree)
+        float y[4], o[4];
+        if (!by_half) {
+          o[0] = x[k][1], o[1] = x[k][0], o[2] = x[k][3], o[3] = x[k][2];
+        } else if (whole) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = __shfl_sync(full, x[k][e], partner);
+        } else {
+          // halves that are no whole vectors: the partner's place within its
+          // vector differs from the component's
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int p = comp + e < half ? comp + e + half : comp + e < r ? comp + e - half : comp + e;
+            o[e] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float t = __shfl_sync(full, x[k][j], base + (p >> 2));
+              if (j == (p & 3)) o[e] = t;
+            }
+          }
+        }
+        const bool is_v = h >= a.Hq + a.Hkv;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = is_v || comp + e >= r ? x[k][e] : x[k][e] * cs[e] + o[e] * sn[e];
+        if (h < a.Hq) {
+          if (tk.state == 2) y[0] = y[1] = y[2] = y[3] = 0.f;
+          store4(static_cast<E*>(a.q_out) + static_cast<long long>(tok) * a.q_out_stride + static_cast<long long>(h) * D + comp, y);
+        }
+        if ((s0 + k * a.groups) * kRows + kRows - 1 < a.Hq) continue;  // (no key or value in the warp)
+        const float inv = is_v ? v_inv : k_inv;
+        uint32_t top = 0;  // as bits: a NaN is above every number
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          y[e] *= inv;
+          top = max(top, __float_as_uint(y[e]) & 0x7fffffffu);
+        }
+        top = max(top, __shfl_xor_sync(full, top, 1));
+        top = max(top, __shfl_xor_sync(full, top, 2));
+        if (h < a.Hq || h >= heads || tk.row < 0) continue;
+        const uint32_t sc = q4_scale(__uint_as_float(top));
+        const float s = q4_scale_value(sc);
+        const uint32_t code = q4_codes(__fdiv_rn(y[0], s), __fdiv_rn(y[1], s)) |
+                              q4_codes(__fdiv_rn(y[2], s), __fdiv_rn(y[3], s)) << 8;
+        const int hk = is_v ? h - a.Hq - a.Hkv : h - a.Hq;
+        const long long row = tk.row + static_cast<long long>(hk) * a.page_size;
+        reinterpret_cast<uint16_t*>(is_v ? c.v_codes : c.k_codes)[row * (D / 4) + at] = static_cast<uint16_t>(code);
+        if ((at & 3) == 0)
+          static_cast<uint8_t*>(is_v ? c.v_scales : c.k_scales)[row * (D / kQ4Group) + (at >> 2)] = static_cast<uint8_t>(sc);
+      }
+    }
+  }
+}
+
+template <typename E, int D>
+cudaError_t launch_d(RopeArgs a, const simsd_q4_cache& c, int num_sms, cudaStream_t stream) {
+  constexpr int kRows = 32 / (D / 4);
+  const int steps = (a.Hq + 2 * a.Hkv + kRows - 1) / kRows;
+  // two full waves of warps where there are that many (token, head) rows,
+  // more heads to a warp (fewer angles formed) beyond
+  const long long want = 2ll * 64 * num_sms;
+  a.groups = static_cast<int>(std::min<long long>(steps, std::max<long long>(1, want / std::max(1, a.T))));
+  // blocks of so many tokens that they make one wave (finding a token's
+  // sequence and page is a chain of loads)
+  a.tokens_block = std::max((kThreads / 32 + a.groups - 1) / a.groups, (a.T + 4 * num_sms - 1) / (4 * num_sms));
+  a.tokens_block = std::max(1, std::min(kMaxTokens, a.tokens_block));
+  const unsigned blocks = static_cast<unsigned>((a.T + a.tokens_block - 1) / a.tokens_block);
+  return launch_overlapped(rope_q4_kernel<E, D>, dim3(blocks), dim3(kThreads), 0, stream, 1u, a, c);
+}
+
+// ------------------------------------------------------------------ expand
+struct ExpandTo {
+  simsd_q4_cache c;
+  const int32_t* block_table;
+  void *k, *v;
+  int num_pages, max_pages, page_size, Bt, Hkv;
+  int32_t* err_word;  // null: nothing is raised
+};
+
+__device__ __forceinline__ void put16(float* to, const uint32_t (&h)[8], float unit) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h[2 * i]));
+    const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&h[2 * i + 1]));
+    reinterpret_cast<float4*>(to)[i] = make_float4(a.x * unit, a.y * unit, b.x * unit, b.y * unit);
+  }
+}
+__device__ __forceinline__ void put16(__nv_bfloat16* to, const uint32_t (&h)[8], float unit) {
+  uint32_t o[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+    const __nv_bfloat162 b = __floats2bfloat162_rn(a.x * unit, a.y * unit);
+    o[i] = *reinterpret_cast<const uint32_t*>(&b);
+  }
+  reinterpret_cast<uint4*>(to)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+  reinterpret_cast<uint4*>(to)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+}
+
+// One group: 8 bytes of codes and a scale to 16 values.
+__device__ __forceinline__ void group_values(uint2 w, uint32_t scale, uint32_t (&h)[8]) {
+  const uint32_t s = q4_scale_pair(scale | scale << 8);
+  h[0] = mul_f16x2(q4_pair<0>(w.x), s);
+  h[1] = mul_f16x2(q4_pair<1>(w.x), s);
+  h[2] = mul_f16x2(q4_pair<2>(w.x), s);
+  h[3] = mul_f16x2(q4_pair<3>(w.x), s);
+  h[4] = mul_f16x2(q4_pair<0>(w.y), s);
+  h[5] = mul_f16x2(q4_pair<1>(w.y), s);
+  h[6] = mul_f16x2(q4_pair<2>(w.y), s);
+  h[7] = mul_f16x2(q4_pair<3>(w.y), s);
+}
+
+// Rows [r0, r1) of a sequence; the block's threads take (page, head, row,
+// group) one after another, blocks of a sequence (gridDim.x) side by side.
+template <typename E, int D>
+__device__ __forceinline__ void expand_rows(const ExpandTo& t, const int32_t* table, int r0, int r1) {
+  constexpr int G = D / kQ4Group;
+  const int P = t.page_size, k0 = r0 / P, pages = (r1 + P - 1) / P - k0;
+  const long long per_page = static_cast<long long>(t.Hkv) * P * G, all = pages * per_page;
+  for (long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; i < all;
+       i += static_cast<long long>(gridDim.x) * kThreads) {
+    const int k = static_cast<int>(i / per_page), in_page = static_cast<int>(i - k * per_page);
+    const int row = in_page / G % P;
+    if (static_cast<long long>(k0 + k) * P + row < r0 || static_cast<long long>(k0 + k) * P + row >= r1) continue;
+    const int pg = table[k0 + k];
+    if (pg < 0 || pg >= t.num_pages) {
+      if (t.err_word) raise_error(t.err_word, SIMSD_EW_PAGE);
+      continue;
+    }
+    const long long g = pg * per_page + in_page;
+    const uint2 kw = static_cast<const uint2*>(t.c.k_codes)[g], vw = static_cast<const uint2*>(t.c.v_codes)[g];
+    const uint32_t ks = static_cast<const uint8_t*>(t.c.k_scales)[g], vs = static_cast<const uint8_t*>(t.c.v_scales)[g];
+    uint32_t h[8];
+    group_values(kw, ks, h);
+    put16(static_cast<E*>(t.k) + g * kQ4Group, h, t.c.k_unit);
+    group_values(vw, vs, h);
+    put16(static_cast<E*>(t.v) + g * kQ4Group, h, t.c.v_unit);
+  }
+}
+
+template <typename E, int D>
+__global__ void __launch_bounds__(kThreads) expand_kernel(const __grid_constant__ ExpandTo t, const int32_t* first,
+                                                          const int32_t* last) {
+  pdl_wait();
+  pdl_launch_next();
+  for (int b = blockIdx.y; b < t.Bt; b += gridDim.y) {
+    const int r0 = first[b], r1 = last[b];
+    if (r0 >= r1) continue;
+    if (r0 < 0 || r1 > static_cast<long long>(t.max_pages) * t.page_size) {
+      if (blockIdx.x == 0 && threadIdx.x == 0 && t.err_word) raise_error(t.err_word, SIMSD_EW_PREFIX_LEN);
+      continue;
+    }
+    expand_rows<E, D>(t, t.block_table + static_cast<size_t>(b) * t.max_pages, r0, r1);
+  }
+}
+
+// The rows that a call of attention sees.
+template <typename E, int D>
+__global__ void __launch_bounds__(kThreads) expand_seen_kernel(const __grid_constant__ ExpandTo t,
+                                                               const __grid_constant__ ChunkArgs a) {
+  pdl_wait();
+  pdl_launch_next();
+  for (int b = blockIdx.y; b < t.Bt; b += gridDim.y) {
+    const ChunkSeq s = chunk_seq(a, b);
+    if (s.C == 0) continue;
+    const Keys k = keys_of<true>(a, s, 0, s.C);
+    const int32_t* table = t.block_table + static_cast<size_t>(b) * t.max_pages;
+    if (k.lo < k.se) expand_rows<E, D>(t, table, k.lo, k.se);
+    if (k.w0 < k.hi) expand_rows<E, D>(t, table, k.w0, k.hi);
+  }
+}
+
+// About eight blocks an SM over all sequences.
+dim3 expand_grid(int Bt, int num_sms) {
+  const int y = std::min(Bt, 65535);
+  return dim3(static_cast<unsigned>(std::max(1, (8 * num_sms + y - 1) / y)), static_cast<unsigned>(y));
+}
+
+}  // namespace
+
+cudaError_t launch_rope_q4(int elem_bytes, const RopeArgs& a, const simsd_q4_cache& c, int num_sms,
+                           cudaStream_t stream) {
+  if (elem_bytes == 4) return a.d == 128 ? launch_d<float, 128>(a, c, num_sms, stream) : launch_d<float, 64>(a, c, num_sms, stream);
+  return a.d == 128 ? launch_d<__nv_bfloat16, 128>(a, c, num_sms, stream)
+                    : launch_d<__nv_bfloat16, 64>(a, c, num_sms, stream);
+}
+
+cudaError_t launch_q4_expand(int elem_bytes, const ExpandArgs& a, int num_sms, cudaStream_t stream) {
+  const ExpandTo t{a.c, a.block_table, a.k_cache, a.v_cache, a.num_pages, a.max_pages, a.page_size, a.Bt, a.Hkv, a.err_word};
+  auto* kern = elem_bytes == 4 ? (a.d == 128 ? expand_kernel<float, 128> : expand_kernel<float, 64>)
+                               : (a.d == 128 ? expand_kernel<__nv_bfloat16, 128> : expand_kernel<__nv_bfloat16, 64>);
+  return launch_overlapped(kern, expand_grid(a.Bt, num_sms), dim3(kThreads), 0, stream, 1u, t, a.first, a.last);
+}
+
+cudaError_t launch_q4_expand_seen(int elem_bytes, const ChunkArgs& a, const simsd_q4_cache& c, void* k_image,
+                                  void* v_image, int num_sms, cudaStream_t stream) {
+  const ExpandTo t{c, a.block_table, k_image, v_image, a.num_pages, a.max_pages, a.page_size, a.Bt, a.Hkv, nullptr};
+  auto* kern = elem_bytes == 4
+                   ? (a.d == 128 ? expand_seen_kernel<float, 128> : expand_seen_kernel<float, 64>)
+                   : (a.d == 128 ? expand_seen_kernel<__nv_bfloat16, 128> : expand_seen_kernel<__nv_bfloat16, 64>);
+  return launch_overlapped(kern, expand_grid(a.Bt, num_sms), dim3(kThreads), 0, stream, 1u, t, a);
+}
+
+}  // namespace simsd

@@ -27,7 +27,7 @@
 
 #include "common.cuh"
 #include "kernels.h"
-#include "ragged.cuh"
+#include "rope_token.cuh"
 
 namespace simsd {
 namespace {
@@ -45,47 +45,6 @@ __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void from_f32(float x, float& y) { y = x; }
 __device__ __forceinline__ void from_f32(float x, __nv_bfloat16& y) { y = __float2bfloat16_rn(x); }
-
-// a token of the block: its position, destination row of the cache in rows
-// of d elements at KV head 0 (-1: not written), and what its q row becomes
-struct Token {
-  long long row;
-  int pos;
-  int state;  // 0: outside every sequence (untouched), 1: rotated, 2: zeroed
-};
-
-__device__ Token resolve(const RopeArgs& a, int tok) {
-  Token t;
-  t.row = -1;
-  t.pos = 0;
-  t.state = 0;
-  if (!a.k_cache) {
-    t.pos = a.positions[tok];
-    t.state = 1;
-    return t;
-  }
-  const int lane = threadIdx.x & 31;
-  const int b = warp_find_seq(a.token_start, a.Bt, tok);
-  if (b < 0) return t;
-  const Chunk c = chunk_of(a.token_start, b, a.T);
-  if (c.bad) return t;
-  const int n = a.prefix_len[b], i = tok - c.start;
-  if (n < 0 || static_cast<long long>(n) + c.count > static_cast<long long>(a.max_pages) * a.page_size) {
-    if (lane == 0) raise_error(a.err_word, SIMSD_EW_PREFIX_LEN);
-    t.state = 2;
-    return t;
-  }
-  t.state = 1;
-  const int dst = n + i, pi = dst / a.page_size;
-  t.pos = a.positions ? a.positions[tok] : dst;
-  const int pg = a.block_table[static_cast<size_t>(b) * a.max_pages + pi];
-  if (pg < 0 || pg >= a.num_pages) {
-    if (lane == 0) raise_error(a.err_word, SIMSD_EW_PAGE);
-    return t;
-  }
-  t.row = static_cast<long long>(pg) * a.Hkv * a.page_size + (dst - pi * a.page_size);
-  return t;
-}
 
 // Thread (token, head group, task): task t of a row is the vectors t and
 // t + R of the rotated part (R = r / (2 VE) tasks; 2t and 2t + 1 where
@@ -105,7 +64,7 @@ __global__ void __launch_bounds__(kThreads, 3) rope_kernel(const __grid_constant
     if (bad) raise_error(a.err_word, SIMSD_EW_TOKENS);
   }
   for (int i = warp; i < a.tokens_block && tok0 + i < a.T; i += kThreads / 32) {
-    const Token t = resolve(a, tok0 + i);
+    const Token t = resolve(a, tok0 + i, a.k_cache != nullptr);
     if (lane == 0) toks[i] = t;
   }
   __syncthreads();

@@ -23,6 +23,8 @@ SIMSD_F32, SIMSD_BF16 = 0, 1
 SECT_DATA, SECT_MASK, SECT_PAD = 0, 1, 255
 EW_STEP_MAP, EW_PREFIX_LEN, EW_PAGE, EW_DRAFT, EW_TIMEOUT, EW_ACCEPT_LEN = 1, 2, 4, 8, 16, 32
 EW_TOKENS, EW_SAMPLE = 64, 128
+EW_POOL, EW_SEQ, EW_SHARED = 256, 512, 1024
+MAX_PAGE_ARRAYS = 8
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 STEP_UNDRAFTED, STEP_DECODED = -1, -2
@@ -32,8 +34,10 @@ EXPORTED = ("simsd_build_mask", "simsd_verify_workspace_bytes", "simsd_verify_at
             "simsd_accept_sampled", "simsd_accept_sampled_workspace_bytes", "simsd_accept_sampled_ws",
             "simsd_kv_commit", "simsd_plan_attention", "simsd_plan_accept",
             "simsd_rope_plan_init", "simsd_rope_rotate", "simsd_rope_append", "simsd_chunk_workspace_bytes",
-            "simsd_chunk_attention", "simsd_sample",
-            "simsd_check_error", "simsd_debug_expire_next_wait",
+            "simsd_chunk_attention", "simsd_chunk_attention_sinks", "simsd_rope_append_q4", "simsd_q4_expand",
+            "simsd_chunk_q4_workspace_bytes", "simsd_chunk_attention_q4", "simsd_pages_extend",
+            "simsd_pages_release", "simsd_pages_workspace_bytes", "simsd_pages_fork", "simsd_pages_compact",
+            "simsd_sample", "simsd_check_error", "simsd_debug_expire_next_wait",
             "simsd_last_error", "simsd_version")
 DEBUG_WAIT_ATTENTION, DEBUG_WAIT_ACCEPT = 1, 2
 
@@ -49,6 +53,18 @@ class RopePlan(ctypes.Structure):
     :func:`simsd_rope_plan_init` and keep it)."""
     _fields_ = [("layout", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("magnitude", ctypes.c_float),
                 ("reserved", ctypes.c_int32), ("turn", ctypes.c_uint64 * 64)]
+
+
+class _Q4Cache(ctypes.Structure):
+    """simsd_q4_cache of the C ABI."""
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("k_unit", ctypes.c_float), ("v_unit", ctypes.c_float)]
+
+
+class _PageArray(ctypes.Structure):
+    """simsd_page_array of the C ABI."""
+    _fields_ = [("base", ctypes.c_void_p), ("page_bytes", ctypes.c_int64), ("layer_bytes", ctypes.c_int64),
+                ("layers", ctypes.c_int64)]
 
 
 _lib = None
@@ -94,13 +110,30 @@ def load_library(path: str = LIB_PATH):
             lib.simsd_chunk_workspace_bytes.restype = Z
             lib.simsd_chunk_attention.argtypes = [I, P, S, P, P, P, P, P, I, P, I, I, I, I, I, I, I, I, I, F, P, P,
                                                   P, Z, P, P]
+            lib.simsd_chunk_attention_sinks.argtypes = [I, P, S, P, P, P, P, P, I, P, I, I, I, I, I, I, I, I, I, I, F,
+                                                        P, P, P, Z, P, P]
+            lib.simsd_rope_append_q4.argtypes = [I, P, P, S, P, S, P, S, P, P, P, I, I, I, I, I, P, P, I, P, I, I,
+                                                 P, P]
+            lib.simsd_q4_expand.argtypes = [I, P, I, P, I, I, P, P, I, I, I, P, P, P, P]
+            lib.simsd_chunk_q4_workspace_bytes.argtypes = [I, I, I, I, I, I, I, I, I]
+            lib.simsd_chunk_q4_workspace_bytes.restype = Z
+            lib.simsd_chunk_attention_q4.argtypes = [I, P, S, P, P, P, P, I, P, I, I, I, I, I, I, I, I, I, I, F, P, P,
+                                                     P, Z, P, P]
+            lib.simsd_pages_extend.argtypes = [P, P, P, P, I, I, I, I, P, P]
+            lib.simsd_pages_release.argtypes = [P, P, P, I, P, P, I, I, I, I, P, P]
+            lib.simsd_pages_workspace_bytes.argtypes = [I, I]
+            lib.simsd_pages_workspace_bytes.restype = Z
+            lib.simsd_pages_fork.argtypes = [P, I, P, P, I, P, P, P, I, I, I, I, P, Z, P, P]
+            lib.simsd_pages_compact.argtypes = [P, I, P, P, I, I, I, P, P, Z, P, P]
             lib.simsd_sample.argtypes = [I, P, S, I, I, P, P, P, P, P, P, P, P, P, P, P]
             lib.simsd_last_error.restype = ctypes.c_char_p
             for name in ("simsd_build_mask", "simsd_verify_attention", "simsd_verify_attention_noalloc",
                          "simsd_accept", "simsd_accept_sampled", "simsd_kv_commit", "simsd_check_error",
                          "simsd_debug_expire_next_wait", "simsd_version", "simsd_plan_attention",
                          "simsd_plan_accept", "simsd_rope_plan_init", "simsd_rope_rotate", "simsd_rope_append",
-                         "simsd_chunk_attention", "simsd_sample"):
+                         "simsd_chunk_attention", "simsd_chunk_attention_sinks", "simsd_rope_append_q4",
+                         "simsd_q4_expand", "simsd_chunk_attention_q4", "simsd_pages_extend",
+                         "simsd_pages_release", "simsd_pages_fork", "simsd_pages_compact", "simsd_sample"):
                 getattr(lib, name).restype = ctypes.c_int
             _lib = lib
     return _lib
@@ -474,6 +507,284 @@ def simsd_chunk_attention(q, token_start, prefix_len, k_cache, v_cache, block_ta
         _error_word(err_word, dev), _raw_stream(stream, dev))
     if rc:
         _check(rc, "simsd_chunk_attention")
+
+
+# --------------------------------------------------------------- long caches
+def _chunk_checks(q, token_start, prefix_len, block_table, out, lse, key_start, workspace):
+    """What the calls of chunk attention over long caches check alike: the device, and the
+    workspace's address and size."""
+    T, Hq, d = q.shape
+    Bt = prefix_len.shape[0]
+    if out.shape != (T, Hq, d) or out.dtype is not q.dtype or not out.is_contiguous():
+        _wrong("out: dense, like q")
+    if not _dense_i32(token_start, Bt + 1) or not _dense_i32(prefix_len, Bt):
+        _wrong("token_start / prefix_len: dense int32 [Bt+1] / [Bt] wanted")
+    if key_start is not None and not _dense_i32(key_start, Bt):
+        _wrong("key_start: dense int32 [Bt] wanted")
+    if lse is not None and (lse.shape != (T, Hq) or lse.dtype is not _F32 or not lse.is_contiguous()):
+        _wrong("lse: dense float32 [T][Hq] wanted")
+    dev = _device(q)
+    if not (dev == token_start.get_device() == prefix_len.get_device() == out.get_device()
+            == block_table.get_device() and (lse is None or lse.get_device() == dev)
+            and (key_start is None or key_start.get_device() == dev)
+            and (workspace is None or workspace.get_device() == dev)):
+        _elsewhere()
+    if workspace is None:
+        return dev, 0, 0
+    if not workspace.is_contiguous():
+        _wrong("workspace: dense tensor wanted")
+    return dev, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def simsd_chunk_attention_sinks(q, token_start, prefix_len, k_cache, v_cache, block_table, out, window, sinks,
+                                lse=None, mask_block=1, key_start=None, softmax_scale=0.0, workspace=None,
+                                err_word=None, stream=None):
+    """simsd_chunk_attention through a window of ``window`` rows beside which the
+    first ``sinks`` rows (from key_start on) stay visible; the workspace is
+    that of simsd_chunk_workspace_bytes."""
+    T, Hq, d = q.shape
+    Bt, Hkv, dt = prefix_len.shape[0], k_cache.shape[1], q.dtype
+    num_pages, max_pages, P = _cache_sizes(k_cache, v_cache, block_table, Bt, Hkv, d, dt)
+    dev, ws, ws_bytes = _chunk_checks(q, token_start, prefix_len, block_table, out, lse, key_start, workspace)
+    if not dev == k_cache.get_device() == v_cache.get_device():
+        _elsewhere()
+    rc = (_lib or load_library()).simsd_chunk_attention_sinks(
+        _code(dt), q.data_ptr(), _rows(q, Hq, d, "q"), token_start.data_ptr(), prefix_len.data_ptr(),
+        _ptr(key_start), k_cache.data_ptr(), v_cache.data_ptr(), num_pages, block_table.data_ptr(), max_pages, P, T,
+        Bt, Hq, Hkv, d, mask_block, window, sinks, softmax_scale, out.data_ptr(), _ptr(lse), ws, ws_bytes,
+        _error_word(err_word, dev), _raw_stream(stream, dev))
+    if rc:
+        _check(rc, "simsd_chunk_attention_sinks")
+
+
+class Q4Cache:
+    """A paged cache in 4 bits: k_codes/v_codes [num_pages][Hkv][P][d/2] and
+    k_scales/v_scales [num_pages][Hkv][P][d/16], uint8 on one GPU, and the
+    units of its keys and values.  Make it once and keep it: it holds the
+    tensors, and the calls read their addresses from it."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales, k_unit=1.0, v_unit=1.0):
+        N, H, P, half = k_codes.shape
+        d = 2 * half
+        for t, w in ((k_codes, half), (k_scales, d // 16), (v_codes, half), (v_scales, d // 16)):
+            if t.shape != (N, H, P, w) or t.dtype is not torch.uint8 or not t.is_contiguous():
+                _wrong("codes [num_pages][Hkv][P][d/2] and scales [num_pages][Hkv][P][d/16], dense uint8, wanted")
+            if t.get_device() != k_codes.get_device() or t.get_device() < 0:
+                _elsewhere()
+        self.tensors = (k_codes, k_scales, v_codes, v_scales)
+        self.num_pages, self.Hkv, self.P, self.d = N, H, P, d
+        self.k_unit, self.v_unit = float(k_unit), float(v_unit)
+        self.device_index = k_codes.get_device()
+        self._c = _Q4Cache(*(t.data_ptr() for t in self.tensors), self.k_unit, self.v_unit)
+        self._at = ctypes.addressof(self._c)
+
+    @classmethod
+    def zeros(cls, num_pages, Hkv, P, d, k_unit=1.0, v_unit=1.0, device="cuda"):
+        """An empty cache (every row reads as zero)."""
+        return cls(*(torch.zeros(num_pages, Hkv, P, w, dtype=torch.uint8, device=device)
+                     for w in (d // 2, d // 16) * 2), k_unit, v_unit)
+
+
+def _table(block_table, Bt):
+    n, max_pages = block_table.shape
+    if not (n == Bt and block_table.dtype is _I32 and block_table.is_contiguous()):
+        _wrong("block_table: dense int32 [Bt][max_pages] wanted")
+    return max_pages
+
+
+def simsd_rope_append_q4(plan, q, k, v, token_start, prefix_len, q_out, cache, block_table, positions=None,
+                         err_word=None, stream=None):
+    """simsd_rope_append to a :class:`Q4Cache`: q [T][Hq][d] rotated to q_out,
+    k [T][Hkv][d] rotated and v to the cache in 4 bits."""
+    T, Hq, d = q.shape
+    Tk, Hkv, dk = k.shape
+    Bt, dt = prefix_len.shape[0], q.dtype
+    if Tk != T or dk != d or v.shape != (T, Hkv, d) or k.dtype is not dt or v.dtype is not dt:
+        _wrong("k / v: [T][Hkv][d] of q's type wanted")
+    if q_out.shape != (T, Hq, d) or q_out.dtype is not dt or not q_out.is_contiguous():
+        _wrong("q_out: dense, like q")
+    if not _dense_i32(token_start, Bt + 1) or not _dense_i32(prefix_len, Bt):
+        _wrong("token_start / prefix_len: dense int32 [Bt+1] / [Bt] wanted")
+    if positions is not None and not _dense_i32(positions, T):
+        _wrong("positions: dense int32 [T] wanted")
+    if cache.Hkv != Hkv or cache.d != d:
+        _wrong("cache: k's heads and components wanted")
+    (qs, q1, q2), (ks, k1, k2), (vs, v1, v2) = q.stride(), k.stride(), v.stride()
+    if (q1 != d and Hq > 1) or ((k1 != d or v1 != d) and Hkv > 1) or not q2 == k2 == v2 == 1:
+        _wrong("q / k / v: the heads of a token must be dense")
+    if T <= 1:
+        qs, ks, vs = Hq * d, Hkv * d, Hkv * d
+    max_pages = _table(block_table, Bt)
+    dev = _device(q)
+    if not (dev == k.get_device() == v.get_device() == token_start.get_device() == prefix_len.get_device()
+            == q_out.get_device() == cache.device_index == block_table.get_device()
+            and (positions is None or positions.get_device() == dev)):
+        _elsewhere()
+    rc = (_lib or load_library()).simsd_rope_append_q4(
+        _code(dt), ctypes.addressof(plan), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
+        token_start.data_ptr(), prefix_len.data_ptr(), _ptr(positions), T, Bt, Hq, Hkv, d, q_out.data_ptr(),
+        cache._at, cache.num_pages, block_table.data_ptr(), max_pages, cache.P, _error_word(err_word, dev),
+        _raw_stream(stream, dev))
+    if rc:
+        _check(rc, "simsd_rope_append_q4")
+
+
+def simsd_q4_expand(cache, block_table, first, last, k_cache, v_cache, err_word=None, stream=None):
+    """Rows [first[b], last[b]) of each sequence, as a :class:`Q4Cache` holds
+    them, written to k_cache / v_cache [num_pages][Hkv][P][d] (bf16 or fp32)."""
+    Bt = first.shape[0]
+    if not _dense_i32(first, Bt) or not _dense_i32(last, Bt):
+        _wrong("first / last: dense int32 [Bt] wanted")
+    num_pages, max_pages, P = _cache_sizes(k_cache, v_cache, block_table, Bt, cache.Hkv, cache.d, k_cache.dtype)
+    if num_pages != cache.num_pages or P != cache.P:
+        _wrong("k_cache / v_cache: the pages of the cache in 4 bits wanted")
+    dev = _device(k_cache)
+    if not (dev == v_cache.get_device() == block_table.get_device() == first.get_device() == last.get_device()
+            == cache.device_index):
+        _elsewhere()
+    rc = (_lib or load_library()).simsd_q4_expand(
+        _code(k_cache.dtype), cache._at, num_pages, block_table.data_ptr(), max_pages, P, first.data_ptr(),
+        last.data_ptr(), Bt, cache.Hkv, cache.d, k_cache.data_ptr(), v_cache.data_ptr(), _error_word(err_word, dev),
+        _raw_stream(stream, dev))
+    if rc:
+        _check(rc, "simsd_q4_expand")
+
+
+def simsd_chunk_q4_workspace_bytes(dtype_code, T, Bt, Hq, Hkv, d, max_pages, page_size, num_pages) -> int:
+    return int(load_library().simsd_chunk_q4_workspace_bytes(dtype_code, T, Bt, Hq, Hkv, d, max_pages, page_size,
+                                                             num_pages))
+
+
+def simsd_chunk_attention_q4(q, token_start, prefix_len, cache, block_table, out, lse=None, mask_block=1, window=0,
+                             sinks=0, key_start=None, softmax_scale=0.0, workspace=None, err_word=None, stream=None):
+    """simsd_chunk_attention_sinks over a :class:`Q4Cache` (sinks = 0:
+    simsd_chunk_attention); the workspace is that of
+    simsd_chunk_q4_workspace_bytes."""
+    T, Hq, d = q.shape
+    Bt, dt = prefix_len.shape[0], q.dtype
+    if cache.d != d:
+        _wrong("cache: q's components wanted")
+    max_pages = _table(block_table, Bt)
+    dev, ws, ws_bytes = _chunk_checks(q, token_start, prefix_len, block_table, out, lse, key_start, workspace)
+    if dev != cache.device_index:
+        _elsewhere()
+    rc = (_lib or load_library()).simsd_chunk_attention_q4(
+        _code(dt), q.data_ptr(), _rows(q, Hq, d, "q"), token_start.data_ptr(), prefix_len.data_ptr(),
+        _ptr(key_start), cache._at, cache.num_pages, block_table.data_ptr(), max_pages, cache.P, T, Bt, Hq,
+        cache.Hkv, d, mask_block, window, sinks, softmax_scale, out.data_ptr(), _ptr(lse), ws, ws_bytes,
+        _error_word(err_word, dev), _raw_stream(stream, dev))
+    if rc:
+        _check(rc, "simsd_chunk_attention_q4")
+
+
+class PageSet:
+    """The arrays whose pages move together: tensors [num_pages][...] of four
+    dimensions or [layers][num_pages][...] of five, at most 8, all with the
+    same pages (k and v caches, or the four tensors of a :class:`Q4Cache`).
+    Make it once and keep it."""
+
+    def __init__(self, tensors):
+        self.tensors = tuple(tensors)
+        if len(self.tensors) > MAX_PAGE_ARRAYS:
+            _wrong("at most 8 arrays")
+        self._c = (_PageArray * max(1, len(self.tensors)))()
+        self.num_pages = self.device_index = None
+        for i, t in enumerate(self.tensors):
+            if t.dim() not in (4, 5) or not t.is_contiguous():
+                _wrong("dense tensors of pages [num_pages][Hkv][P][x], or [layers] of them, wanted")
+            layers, pages = (1, t.shape[0]) if t.dim() == 4 else t.shape[:2]
+            if self.num_pages not in (None, pages):
+                _wrong("arrays of the same pages wanted")
+            if self.device_index not in (None, t.get_device()) or t.get_device() < 0:
+                _elsewhere()
+            self.num_pages, self.device_index = pages, t.get_device()
+            page = t.element_size() * t.shape[-3] * t.shape[-2] * t.shape[-1]
+            self._c[i] = _PageArray(t.data_ptr(), page, page * pages, layers)
+        self._at = ctypes.addressof(self._c)
+
+
+def _pool(block_table, refs):
+    Bt, max_pages = block_table.shape
+    if not (block_table.dtype is _I32 and block_table.is_contiguous()):
+        _wrong("block_table: dense int32 [Bt][max_pages] wanted")
+    if not _dense_i32(refs, refs.shape[0]):
+        _wrong("refs: dense int32 [num_pages] wanted")
+    dev = _device(block_table)
+    if refs.get_device() != dev:
+        _elsewhere()
+    return Bt, max_pages, refs.shape[0], dev
+
+
+def _here_i32(t, n, dev, name):
+    if not _dense_i32(t, n):
+        _wrong(name + ": dense int32 of the right length wanted")
+    if t.get_device() != dev:
+        _elsewhere()
+    return t.data_ptr()
+
+
+def _pages_scratch(pages, num_pages, workspace, dev):
+    if pages.num_pages not in (None, num_pages):
+        _wrong("refs: a count for every page of the arrays wanted")
+    if pages.device_index not in (None, dev) or workspace.get_device() != dev:
+        _elsewhere()
+    if not workspace.is_contiguous():
+        _wrong("workspace: dense tensor wanted")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def simsd_pages_extend(lens, add, block_table, refs, page_size, err_word=None, stream=None):
+    """Pages for the rows [lens[b], lens[b] + add[b]) that have none."""
+    Bt, max_pages, num_pages, dev = _pool(block_table, refs)
+    rc = (_lib or load_library()).simsd_pages_extend(
+        _here_i32(lens, Bt, dev, "lens"), _here_i32(add, Bt, dev, "add"), block_table.data_ptr(), refs.data_ptr(),
+        num_pages, Bt, max_pages, page_size, _error_word(err_word, dev), _raw_stream(stream, dev))
+    if rc:
+        _check(rc, "simsd_pages_extend")
+
+
+def simsd_pages_release(block_table, refs, first, last, page_size, seq=None, err_word=None, stream=None):
+    """Lets go of the pages that lie wholly within rows [first[i], last[i]) of
+    sequence seq[i] (None: i)."""
+    Bt, max_pages, num_pages, dev = _pool(block_table, refs)
+    n = Bt if seq is None else seq.shape[0]
+    if n == 0:  # (an empty tensor has no address, which would name all sequences)
+        return
+    rc = (_lib or load_library()).simsd_pages_release(
+        None if seq is None else _here_i32(seq, n, dev, "seq"), _here_i32(first, n, dev, "first"),
+        _here_i32(last, n, dev, "last"), n, block_table.data_ptr(), refs.data_ptr(), num_pages, Bt, max_pages,
+        page_size, _error_word(err_word, dev), _raw_stream(stream, dev))
+    if rc:
+        _check(rc, "simsd_pages_release")
+
+
+def simsd_pages_workspace_bytes(num_pages, pairs=0) -> int:
+    return int(load_library().simsd_pages_workspace_bytes(num_pages, pairs))
+
+
+def simsd_pages_fork(pages, src, dst, lens, block_table, refs, page_size, workspace, err_word=None, stream=None):
+    """Sequence dst[i] becomes a copy of src[i]; pages: a :class:`PageSet`."""
+    Bt, max_pages, num_pages, dev = _pool(block_table, refs)
+    n = src.shape[0]
+    ws, ws_bytes = _pages_scratch(pages, num_pages, workspace, dev)
+    rc = (_lib or load_library()).simsd_pages_fork(
+        pages._at, len(pages.tensors), _here_i32(src, n, dev, "src"), _here_i32(dst, n, dev, "dst"), n,
+        _here_i32(lens, Bt, dev, "lens"), block_table.data_ptr(), refs.data_ptr(), num_pages, Bt, max_pages,
+        page_size, ws, ws_bytes, _error_word(err_word, dev), _raw_stream(stream, dev))
+    if rc:
+        _check(rc, "simsd_pages_fork")
+
+
+def simsd_pages_compact(pages, block_table, refs, live, workspace, err_word=None, stream=None):
+    """Moves the live pages to the lowest ids; live [1] int32 out or None."""
+    Bt, max_pages, num_pages, dev = _pool(block_table, refs)
+    ws, ws_bytes = _pages_scratch(pages, num_pages, workspace, dev)
+    rc = (_lib or load_library()).simsd_pages_compact(
+        pages._at, len(pages.tensors), block_table.data_ptr(), refs.data_ptr(), num_pages, Bt, max_pages,
+        None if live is None else _here_i32(live, 1, dev, "live"), ws, ws_bytes, _error_word(err_word, dev),
+        _raw_stream(stream, dev))
+    if rc:
+        _check(rc, "simsd_pages_compact")
 
 
 def _row_f32(t, R, dev, name):
