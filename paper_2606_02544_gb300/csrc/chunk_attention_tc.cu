@@ -86,7 +86,7 @@ struct ChunkTcParams {
 };
 
 // Key tiles [t0, t0 + tiles) of a unit, or of the CTA's piece of it.
-struct alignas(16) Piece {
+struct alignas(16) PieceBase {
   int tok0, ntok;      // first token of the unit in the chunk array, tokens of it
   int kvh, b;
   int t0, tiles;       // this piece's key tiles; tiles 0: the rows are zero; -1: no more pieces
@@ -94,17 +94,24 @@ struct alignas(16) Piece {
   int n, C, ks, i0;    // the sequence (chunk_mask.cuh) and the unit's first token in it
   int part, slot;      // writes partial results (slot 0: the piece at the start of the run)
   int last, flag;      // the CTA's last piece; its entry in `bad`
-  // first rows that stay visible through the window (only where there are any)
+};
+template <bool SINKS>
+struct Piece : PieceBase {};
+// first rows that stay visible through the window
+template <>
+struct Piece<true> : PieceBase {
   int se, w0;          // rows [se, w0) are seen by none of the unit's tokens
   int tse, skip;       // tile t lies `skip` tiles further from tile tse on
 };
-template <bool SINKS>
-__device__ __forceinline__ int tile_row(const Piece& u, int t) {
-  if constexpr (SINKS) t += t >= u.tse ? u.skip : 0;
-  return t * kTile;
-}
+// rows [from, to) lie between the first rows and the window; the tile holds such rows
+__device__ __forceinline__ bool unseen(const Piece<false>&, int, int) { return false; }
+__device__ __forceinline__ bool unseen(const Piece<true>& u, int from, int to) { return from >= u.se && to <= u.w0; }
+__device__ __forceinline__ bool gap_in_tile(const Piece<false>&, int) { return false; }
+__device__ __forceinline__ bool gap_in_tile(const Piece<true>& u, int key0) { return key0 < u.w0 && key0 + kTile > u.se; }
+__device__ __forceinline__ int tile_row(const Piece<false>&, int t) { return t * kTile; }
+__device__ __forceinline__ int tile_row(const Piece<true>& u, int t) { return (t + (t >= u.tse ? u.skip : 0)) * kTile; }
 
-template <int D>
+template <int D, bool SINKS>
 struct alignas(1024) SmemChunk {
   static constexpr int kHalves = D / 64;
   static constexpr int kTileBytes = kHalves * kHalfBytes;  // one K or V tile
@@ -120,22 +127,22 @@ struct alignas(1024) SmemChunk {
   uint64_t bar_s[2], bar_p[2][2], bar_pv[2], bar_ofree[2];
   uint64_t bar_msg[kQueue], bar_msgfree[kQueue];
   uint64_t bar_drain[2];
-  Piece queue[kQueue];
+  Piece<SINKS> queue[kQueue];
   int bad[kFlags];     // a page id of the piece is out of range (written by the producer)
   uint32_t tmem_base;
   int abort_flag;
 };
-template <int D>
+template <int D, bool SINKS>
 constexpr size_t smem_bytes() {
-  return sizeof(SmemChunk<D>) + 1024;
+  return sizeof(SmemChunk<D, SINKS>) + 1024;
 }
-static_assert(smem_bytes<128>() <= 232448 && smem_bytes<64>() <= 232448, "one CTA per SM");
-static_assert(SmemChunk<128>::kStages * SmemChunk<128>::kTileBytes >= kChunkMaxSeqs * 4 &&
-                  SmemChunk<64>::kStages * SmemChunk<64>::kTileBytes >= kChunkMaxSeqs * 4,
+static_assert(smem_bytes<128, true>() <= 232448 && smem_bytes<64, true>() <= 232448, "one CTA per SM");
+static_assert(SmemChunk<128, true>::kStages * SmemChunk<128, true>::kTileBytes >= kChunkMaxSeqs * 4 &&
+                  SmemChunk<64, true>::kStages * SmemChunk<64, true>::kTileBytes >= kChunkMaxSeqs * 4,
               "the ring holds the tile counts of all sequences while runs are planned");
 
-template <int D>
-__device__ __forceinline__ void signal_abort(SmemChunk<D>& sm, int32_t* err_word) {
+template <int D, bool SINKS>
+__device__ __forceinline__ void signal_abort(SmemChunk<D, SINKS>& sm, int32_t* err_word) {
   raise_error(err_word, SIMSD_EW_TIMEOUT);
   *reinterpret_cast<volatile int*>(&sm.abort_flag) = 1;
 }
@@ -170,7 +177,7 @@ __device__ __forceinline__ void st_global_256(void* p, const uint32_t (&v)[8]) {
 // The next message of the unit queue, copied to the registers of a warp;
 // false when a wait expired.
 template <int D, bool SINKS>
-__device__ __forceinline__ bool next_piece(SmemChunk<D>& sm, uint32_t& at, Piece& u) {
+__device__ __forceinline__ bool next_piece(SmemChunk<D, SINKS>& sm, uint32_t& at, Piece<SINKS>& u) {
   volatile int* abort_flag = &sm.abort_flag;
   const uint32_t st = at % kQueue, par = (at / kQueue) & 1;
   if (!mbar_wait_warp(smem_u32(&sm.bar_msg[st]), par, abort_flag)) return false;
@@ -210,7 +217,7 @@ template <int D, bool SINKS>
 __global__ void __launch_bounds__(kThreads, 1)
     chunk_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ ChunkTcParams p) {
-  using Smem = SmemChunk<D>;
+  using Smem = SmemChunk<D, SINKS>;
   constexpr int kHalves = Smem::kHalves, kStages = Smem::kStages, kStagesK = Smem::kStagesK, kStagesV = Smem::kStagesV;
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -274,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t at = 0;
       bool ok = true;
       for (;;) {
-        Piece u;
+        Piece<SINKS> u;
         u.tiles = -1;
         if (k.peek(p.a, ub, piece)) {
           u.i0 = k.w.j * ub;
@@ -318,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t at = 0, jq[2] = {0, 0};
       uint32_t slot[2] = {0, 0}, par[2] = {0, 0}, used[2] = {0, 0};  // K, V: next slot, its parity, slots filled
       bool ok = true;
-      Piece u;
+      Piece<SINKS> u;
       while (ok && (ok = next_piece<D, SINKS>(sm, at, u)) && u.tiles >= 0) {
         if (u.tiles == 0) continue;
         const int nblk = u.ntok > p.tb ? 2 : 1;
@@ -345,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         int win_base = -(1 << 30), win = -1;  // lane i holds the page id of page win_base + i
         bool bad = false;
         for (int t = u.t0; ok && t < u.t0 + u.tiles; ++t) {
-          const int key0 = tile_row<SINKS>(u, t), valid = min(kTile, u.hi - key0);
+          const int key0 = tile_row(u, t), valid = min(kTile, u.hi - key0);
           const int nsub = (valid + sub - 1) / sub;
           const int pi0 = key0 / P, pi1 = (key0 + valid - 1) / P;  // at most 16 pages a tile
           if (pi0 < win_base || pi1 >= win_base + 32) {
@@ -359,8 +366,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           // a page id out of range is replaced by page 0, and the softmax
           // warps, which see this flag no later than the S of this tile, zero
           // the piece's rows (rows that no token sees need no page)
-          const bool wrong = (pg < 0 || pg >= p.a.num_pages) && key + sub > u.lo &&
-                             (!SINKS || key < u.se || key + sub > u.w0);
+          const bool wrong = (pg < 0 || pg >= p.a.num_pages) && key + sub > u.lo && !unseen(u, key, key + sub);
           if (pg < 0 || pg >= p.a.num_pages) pg = 0;
           bad |= __any_sync(0xffffffffu, wrong);
           if (lane == 0 && (t == u.t0 || bad)) {
@@ -460,7 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         step_k();
         return true;
       };
-      Piece u;
+      Piece<SINKS> u;
       bool ok = true;
       while (ok && (ok = next_piece<D, SINKS>(sm, at, u)) && u.tiles >= 0) {
         const int n = u.tiles;
@@ -525,7 +531,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t s_tmem = lane_tmem + kColS + 128u * x, o_tmem = lane_tmem + kColO + 128u * x;
     uint32_t g = 0, c = 0, at = 0;
     bool ok = true;
-    Piece u;
+    Piece<SINKS> u;
     while ((ok = ok && next_piece<D, SINKS>(sm, at, u)) && u.tiles >= 0) {
       const int xt = x * p.tb + tl;  // token of this row within the unit
       const bool row_exists = tl < p.tb && xt < u.ntok;
@@ -550,7 +556,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool have_o = false;
       if (u.tiles > 0 && has) {
         for (int i = 0; i < u.tiles; ++i, ++c) {
-          const int key0 = tile_row<SINKS>(u, u.t0 + i);
+          const int key0 = tile_row(u, u.t0 + i);
           if (!mbar_wait_warp(smem_u32(&sm.bar_s[x]), c & 1, abort_flag)) {
             ok = false;
             break;
@@ -563,14 +569,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           // does not tell apart.  The block's MMA warp, which has waited for
           // every use of V in turn, issues this S after the last one before
           // this tile's, so from here the parity names one use.
-          if (key0 < u.lo || key0 + kTile > u.hi || (SINKS && key0 < u.w0 && key0 + kTile > u.se)) {
+          if (key0 < u.lo || key0 + kTile > u.hi || gap_in_tile(u, key0)) {
             const uint32_t gt = g + i, vst = kStagesK + gt % kStagesV;  // the tile's V slot
             if (!mbar_wait_warp(smem_u32(&sm.bar_full[vst]), (gt / kStagesV) & 1, abort_flag)) {
               ok = false;
               break;
             }
             const int key = key0 + row;
-            if (key < u.lo || key >= u.hi || (SINKS && key >= u.se && key < u.w0)) {
+            if (key < u.lo || key >= u.hi || unseen(u, key, key + 1)) {
               const uint4 z = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
               for (int hf = 0; hf < kHalves; ++hf) {
@@ -862,16 +868,17 @@ cudaError_t launch_d(const ChunkArgs& a, int num_sms, EncodeTiledFn encode, cuda
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     std::lock_guard<std::mutex> lk(mu);
     if (!done[dev]) {
-      const int bytes = static_cast<int>(smem_bytes<D>());
-      e = cudaFuncSetAttribute(chunk_tc_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+      e = cudaFuncSetAttribute(chunk_tc_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               static_cast<int>(smem_bytes<D, false>()));
       if (e != cudaSuccess) return e;
-      e = cudaFuncSetAttribute(chunk_tc_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+      e = cudaFuncSetAttribute(chunk_tc_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               static_cast<int>(smem_bytes<D, true>()));
       if (e != cudaSuccess) return e;
       done[dev] = true;
     }
   }
   cudaError_t e = launch_overlapped(a.sinks > 0 ? chunk_tc_kernel<D, true> : chunk_tc_kernel<D, false>, dim3(static_cast<unsigned>(p.ctas)), dim3(kThreads),
-                                    smem_bytes<D>(), stream, 1u, tq, tk, tv, p);
+                                    a.sinks > 0 ? smem_bytes<D, true>() : smem_bytes<D, false>(), stream, 1u, tq, tk, tv, p);
   if (e != cudaSuccess || p.ctas == 1) return e;
   // units of many rows: 16 blocks to a boundary (two passes over 256 rows; the
   // launch after an 8192-token prompt takes 8 us, with 4 blocks 24)

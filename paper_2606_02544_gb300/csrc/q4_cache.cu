@@ -4,15 +4,19 @@
 //
 // Mathematics.  The rotation is that of rope_append.cu.  A group of 16
 // components becomes s = (max |x| / 6) to nearest in 8 bits and codes (x / s)
-// to nearest in 4 bits; the rotated key is divided as it is in fp32, without
-// a rounding to the type before, and the quotient is correctly rounded (a
-// product with 1 / s would put ties of 16-bit values on the wrong side).
+// to nearest in 4 bits; the rotated key is taken as it is in fp32, without a
+// rounding to the type before.  x / s is x fl(1 / s) with one step of
+// correction by its residual (Markstein 1990), which makes it correctly
+// rounded, so that ties of 16-bit values go to the even code; top / 6 is a
+// product with fl(1 / 6), exact where it is a tie between two scales.
 // Written out, s times a code has 6 significant bits: exact in fp16 and bf16.
 //
-// A thread owns four components: a row of 128 is a warp's (of 64, half a
-// warp's), a group four lanes', so a row's angles are formed once a lane and
-// serve every head of the token that the warp visits, a rotation's partner
-// comes by shuffle and a group's largest by two.
+// A thread owns eight components: a row of 128 is half a warp's (of 64, a
+// quarter), a group two lanes', so that a rotation's partner comes by shuffle
+// and a group's largest by one.  A token's angles are formed once a warp,
+// one or two a lane, and serve every head that the warp visits (through
+// shared memory; four angles formed by each lane for itself, with four
+// components a lane and quotients by division, took 200 us for 16384 tokens).
 //
 // Bound by memory: a token reads (Hq + 2 Hkv) d elements and writes Hq d and
 // 2 Hkv (d / 2 + d / 16) bytes.
@@ -33,34 +37,43 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxTokens = 64;  // tokens of a block
-constexpr int kInFlight = 4;    // rows of a warp whose loads are issued together
+constexpr int kInFlight = 2;    // steps of a warp whose loads are issued together
 
-struct alignas(8) Bf16x4 {
-  __nv_bfloat162 a, b;
-};
-__device__ __forceinline__ void load4(const float* p, float (&x)[4]) {
-  const float4 v = *reinterpret_cast<const float4*>(p);
-  x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+  const float4 u = reinterpret_cast<const float4*>(p)[0], v = reinterpret_cast<const float4*>(p)[1];
+  x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
 }
-__device__ __forceinline__ void load4(const __nv_bfloat16* p, float (&x)[4]) {
-  const Bf16x4 v = *reinterpret_cast<const Bf16x4*>(p);
-  const float2 a = __bfloat1622float2(v.a), b = __bfloat1622float2(v.b);
-  x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
+  const uint4 u = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[2 * e] = __uint_as_float(w[e] << 16);
+    x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+  }
 }
-__device__ __forceinline__ void store4(float* p, const float (&x)[4]) {
-  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&x)[4]) {
-  *reinterpret_cast<Bf16x4*>(p) = Bf16x4{__floats2bfloat162_rn(x[0], x[1]), __floats2bfloat162_rn(x[2], x[3])};
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
+    w[e] = *reinterpret_cast<const uint32_t*>(&b);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Warp item (token, group of heads): rows of heads grp, grp + groups, ...
-// (pairs of heads where a row takes half a warp).
+// Warp item (token, group of heads): steps grp, grp + groups, ... of kRows
+// heads of the token (q's, then k's, then v's).
 template <typename E, int D>
 __global__ void __launch_bounds__(kThreads, 4) rope_q4_kernel(const __grid_constant__ RopeArgs a,
                                                               const __grid_constant__ simsd_q4_cache c) {
-  constexpr int kLanes = D / 4, kRows = 32 / kLanes;  // lanes of a row, rows of a warp
+  constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes of a row, rows of a warp
   __shared__ Token toks[kMaxTokens];
+  __shared__ float2 angles[kThreads / 32][D / 2];  // a warp's token: (cos, sin) of each pair
   pdl_wait();
   pdl_launch_next();
   const unsigned full = 0xffffffffu;
@@ -78,99 +91,116 @@ __global__ void __launch_bounds__(kThreads, 4) rope_q4_kernel(const __grid_const
   __syncthreads();
   const int r = a.plan.rot_dim, half = r / 2;
   const bool by_half = a.plan.layout == SIMSD_ROPE_HALF;
-  const int at = lane & (kLanes - 1), base = lane - at, comp = 4 * at, sub = lane / kLanes;
+  const int at = lane & (kLanes - 1), base = lane - at, comp = 8 * at, sub = lane / kLanes;
   const int heads = a.Hq + 2 * a.Hkv, steps = (heads + kRows - 1) / kRows;
   const float k_inv = 1.f / c.k_unit, v_inv = 1.f / c.v_unit;
-  // where a component's partner lies (rotate-half; its lane, whole vectors)
-  const bool whole = (half & 3) == 0;
-  const int partner = comp < half ? lane + half / 4 : comp < r ? lane - half / 4 : lane;
+  // the lane of a component's partner (rotate-half, halves of whole vectors)
+  const bool whole = (half & 7) == 0;
+  const int partner = comp < half ? lane + half / 8 : comp < r ? lane - half / 8 : lane;
   for (int w = warp; w < a.tokens_block * a.groups; w += kThreads / 32) {
     const int i = w / a.groups, grp = w - i * a.groups, tok = tok0 + i;
     if (tok >= a.T) break;
     const Token tk = toks[i];
     if (tk.state == 0) continue;
+    __syncwarp();
+    for (int pair = lane; pair < half; pair += 32) {
+      const unsigned long long turn = static_cast<unsigned long long>(static_cast<long long>(tk.pos)) * a.plan.turn[pair];
+      float2 cs;
+      sincospif(static_cast<float>(static_cast<int32_t>(turn >> 32)) * 0x1p-31f, &cs.y, &cs.x);
+      angles[warp][pair] = make_float2(cs.x * a.plan.magnitude, cs.y * a.plan.magnitude);
+    }
+    __syncwarp();
     // x turned: x cs + partner sn (the partner's sign in sn)
-    float cs[4], sn[4];
+    float cs[8], sn[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < 8; ++e) {
       const int k = comp + e;
       cs[e] = 1.f;
       sn[e] = 0.f;
       if (k < r) {
-        const int pair = by_half ? (k < half ? k : k - half) : k >> 1;
-        const bool first = by_half ? k < half : (k & 1) == 0;
-        const unsigned long long turn = static_cast<unsigned long long>(static_cast<long long>(tk.pos)) * a.plan.turn[pair];
-        sincospif(static_cast<float>(static_cast<int32_t>(turn >> 32)) * 0x1p-31f, &sn[e], &cs[e]);
-        sn[e] *= first ? -a.plan.magnitude : a.plan.magnitude;
-        cs[e] *= a.plan.magnitude;
+        const float2 x = angles[warp][by_half ? (k < half ? k : k - half) : k >> 1];
+        cs[e] = x.x;
+        sn[e] = (by_half ? k < half : (k & 1) == 0) ? -x.y : x.y;
       }
     }
-    for (int s0 = grp; s0 < steps; s0 += a.groups * kInFlight) {
-      float x[kInFlight][4];
+    const E* q = static_cast<const E*>(a.q) + static_cast<long long>(tok) * a.q_stride + comp;
+    const E* k = static_cast<const E*>(a.k) + static_cast<long long>(tok) * a.k_stride + comp;
+    const E* v = static_cast<const E*>(a.v) + static_cast<long long>(tok) * a.v_stride + comp;
+    E* q_out = static_cast<E*>(a.q_out) + static_cast<long long>(tok) * a.q_out_stride + comp;
+    auto turn = [&](float (&x)[8], bool turns) {
+      float o[8];
+      if (!by_half) {
 #pragma unroll
-      for (int k = 0; k < kInFlight; ++k) {
-        const int h = (s0 + k * a.groups) * kRows + sub;
-        x[k][0] = x[k][1] = x[k][2] = x[k][3] = 0.f;
-        if (h < heads) {
-          const E* src = h < a.Hq ? static_cast<const E*>(a.q) + static_cast<long long>(tok) * a.q_stride + static_cast<long long>(h) * D
-                         : h < a.Hq + a.Hkv
-                             ? static_cast<const E*>(a.k) + static_cast<long long>(tok) * a.k_stride + static_cast<long long>(h - a.Hq) * D
-                             : static_cast<const E*>(a.v) + static_cast<long long>(tok) * a.v_stride +
-                                   static_cast<long long>(h - a.Hq - a.Hkv) * D;
-          load4(src + comp, x[k]);
+        for (int e = 0; e < 8; ++e) o[e] = x[e ^ 1];
+      } else if (whole) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = __shfl_sync(full, x[e], partner);
+      } else {
+        // halves that are no whole vectors: the partner's place within its
+        // vector differs from the component's
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int p = comp + e < half ? comp + e + half : comp + e < r ? comp + e - half : comp + e;
+          o[e] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float t = __shfl_sync(full, x[j], base + (p >> 3));
+            if (j == (p & 7)) o[e] = t;
+          }
         }
       }
 #pragma unroll
-      for (int k = 0; k < kInFlight; ++k) {
-        const int h = (s0 + k * a.groups) * kRows + sub;
-        if (s0 + k * a.groups >= steps) break;  // (the warp's lanes agree)
-        float y[4], o[4];
-        if (!by_half) {
-          o[0] = x[k][1], o[1] = x[k][0], o[2] = x[k][3], o[3] = x[k][2];
-        } else if (whole) {
+      for (int e = 0; e < 8; ++e) x[e] = turns && comp + e < r ? x[e] * cs[e] + o[e] * sn[e] : x[e];
+    };
+    for (int s0 = grp; s0 < steps; s0 += a.groups * kInFlight) {
+      float x[kInFlight][8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] = __shfl_sync(full, x[k][e], partner);
-        } else {
-          // halves that are no whole vectors: the partner's place within its
-          // vector differs from the component's
+      for (int j = 0; j < kInFlight; ++j) {
+        const int h = (s0 + j * a.groups) * kRows + sub;
+        if (h < heads) load8(h < a.Hq ? q + h * D : h < a.Hq + a.Hkv ? k + (h - a.Hq) * D : v + (h - a.Hq - a.Hkv) * D, x[j]);
+      }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int p = comp + e < half ? comp + e + half : comp + e < r ? comp + e - half : comp + e;
-            o[e] = 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float t = __shfl_sync(full, x[k][j], base + (p >> 2));
-              if (j == (p & 3)) o[e] = t;
-            }
-          }
-        }
+      for (int j = 0; j < kInFlight; ++j) {
+        const int h0 = (s0 + j * a.groups) * kRows, h = h0 + sub;
+        if (h0 >= heads) break;  // (the warp's lanes agree, here and below)
         const bool is_v = h >= a.Hq + a.Hkv;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = is_v || comp + e >= r ? x[k][e] : x[k][e] * cs[e] + o[e] * sn[e];
+        if (h0 < a.Hq + a.Hkv) turn(x[j], !is_v);
         if (h < a.Hq) {
-          if (tk.state == 2) y[0] = y[1] = y[2] = y[3] = 0.f;
-          store4(static_cast<E*>(a.q_out) + static_cast<long long>(tok) * a.q_out_stride + static_cast<long long>(h) * D + comp, y);
+          float y[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = tk.state == 2 ? 0.f : x[j][e];
+          store8(q_out + h * D, y);
         }
-        if ((s0 + k * a.groups) * kRows + kRows - 1 < a.Hq) continue;  // (no key or value in the warp)
+        if (h0 + kRows <= a.Hq) continue;  // (no key or value among them)
         const float inv = is_v ? v_inv : k_inv;
         uint32_t top = 0;  // as bits: a NaN is above every number
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          y[e] *= inv;
-          top = max(top, __float_as_uint(y[e]) & 0x7fffffffu);
+        for (int e = 0; e < 8; ++e) {
+          x[j][e] *= inv;
+          top = max(top, __float_as_uint(x[j][e]) & 0x7fffffffu);
         }
         top = max(top, __shfl_xor_sync(full, top, 1));
-        top = max(top, __shfl_xor_sync(full, top, 2));
         if (h < a.Hq || h >= heads || tk.row < 0) continue;
         const uint32_t sc = q4_scale(__uint_as_float(top));
-        const float s = q4_scale_value(sc);
-        const uint32_t code = q4_codes(__fdiv_rn(y[0], s), __fdiv_rn(y[1], s)) |
-                              q4_codes(__fdiv_rn(y[2], s), __fdiv_rn(y[3], s)) << 8;
+        const float s = q4_scale_value(sc), s_inv = __frcp_rn(s);
+        if (top >= 0x7f800000u) {
+          // infinities have no residual: the largest numbers go to 6 as well
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[j][e] = fminf(fmaxf(x[j][e], -3.4e38f), 3.4e38f);
+        }
+        uint32_t code = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float y = x[j][e] * s_inv;
+          x[j][e] = fmaf(fmaf(-y, s, x[j][e]), s_inv, y);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) code |= q4_codes(x[j][2 * e], x[j][2 * e + 1]) << (8 * e);
         const int hk = is_v ? h - a.Hq - a.Hkv : h - a.Hq;
         const long long row = tk.row + static_cast<long long>(hk) * a.page_size;
-        reinterpret_cast<uint16_t*>(is_v ? c.v_codes : c.k_codes)[row * (D / 4) + at] = static_cast<uint16_t>(code);
-        if ((at & 3) == 0)
-          static_cast<uint8_t*>(is_v ? c.v_scales : c.k_scales)[row * (D / kQ4Group) + (at >> 2)] = static_cast<uint8_t>(sc);
+        reinterpret_cast<uint32_t*>(is_v ? c.v_codes : c.k_codes)[row * (D / 8) + at] = code;
+        if ((at & 1) == 0)
+          static_cast<uint8_t*>(is_v ? c.v_scales : c.k_scales)[row * (D / kQ4Group) + (at >> 1)] = static_cast<uint8_t>(sc);
       }
     }
   }
@@ -178,16 +208,16 @@ __global__ void __launch_bounds__(kThreads, 4) rope_q4_kernel(const __grid_const
 
 template <typename E, int D>
 cudaError_t launch_d(RopeArgs a, const simsd_q4_cache& c, int num_sms, cudaStream_t stream) {
-  constexpr int kRows = 32 / (D / 4);
+  constexpr int kRows = 32 / (D / 8), kWarps = kThreads / 32;
   const int steps = (a.Hq + 2 * a.Hkv + kRows - 1) / kRows;
-  // two full waves of warps where there are that many (token, head) rows,
-  // more heads to a warp (fewer angles formed) beyond
+  // two full waves of warps where there are that many steps, more steps to a
+  // warp (fewer angles formed) beyond
   const long long want = 2ll * 64 * num_sms;
   a.groups = static_cast<int>(std::min<long long>(steps, std::max<long long>(1, want / std::max(1, a.T))));
-  // blocks of so many tokens that they make one wave (finding a token's
-  // sequence and page is a chain of loads)
-  a.tokens_block = std::max((kThreads / 32 + a.groups - 1) / a.groups, (a.T + 4 * num_sms - 1) / (4 * num_sms));
-  a.tokens_block = std::max(1, std::min(kMaxTokens, a.tokens_block));
+  // items for every warp of a block, and of many tokens about eight blocks an
+  // SM (finding a token's sequence and page is a chain of loads)
+  const int per_block = std::max((kWarps + a.groups - 1) / a.groups, (a.T + 8 * num_sms - 1) / (8 * num_sms));
+  a.tokens_block = std::min(kMaxTokens, a.groups == 1 ? (per_block + kWarps - 1) / kWarps * kWarps : per_block);
   const unsigned blocks = static_cast<unsigned>((a.T + a.tokens_block - 1) / a.tokens_block);
   return launch_overlapped(rope_q4_kernel<E, D>, dim3(blocks), dim3(kThreads), 0, stream, 1u, a, c);
 }
