@@ -906,7 +906,6 @@ int simsd_chunk_attention_q4(int dtype, const void* q, int64_t q_stride, const i
   a.sinks = window > 0 ? sinks : 0;
   a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt(static_cast<float>(d));
   if (simsd::chunk_q4_few(dtype, T, Bt, Hq, Hkv)) {
-    if (Bt > simsd::kChunkMaxSeqs) return unsupported("more than 16384 sequences");
     // units of at least Hq / Hkv rows, key tiles of 128 rows, counted in 32 bits
     const long long max_keys = static_cast<long long>(max_pages) * page_size;
     if ((static_cast<long long>(T) * Hkv + static_cast<long long>(Bt) * Hkv + 1) * (max_keys / 128 + 1) >= (1ll << 31))

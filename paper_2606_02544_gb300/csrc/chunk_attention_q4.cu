@@ -22,9 +22,8 @@
 // Work.  The walk of chunk_walk.cuh over units of (KV head, sequence, up to
 // RB query rows).  One warp walks the run and brings the tiles' codes and
 // scales (128 keys, 18 KB) by bulk copies, each a page's contiguous rows of a
-// head; eight warps share a tile's keys (RG groups of rows by 8 / RG of keys),
-// each with a softmax of its own, merged at the end of a unit through shared
-// memory.  A unit cut by a run's end leaves partial (O, m, l), which a second
+// head; four or eight warps share a tile's keys (RG groups of rows), each with
+// a softmax of its own, merged at the end of a unit through shared memory.  A unit cut by a run's end leaves partial (O, m, l), which a second
 // launch merges.
 //
 // Every mbarrier wait is bounded; after one expires the CTA raises
@@ -47,9 +46,9 @@ namespace simsd {
 namespace {
 
 constexpr int kTile = 128;  // keys per tile
-constexpr int kWarps = 8;   // of the softmax
-constexpr int kThreads = 32 * (kWarps + 1);
+constexpr int kMaxSeqs = 8192;  // their tile counts fit the ring
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
+constexpr float kNoReference = -1.0e30f;   // of rows that have seen no key
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct Q4Params {
@@ -58,24 +57,42 @@ struct Q4Params {
   int g, ub, ctas;    // heads per KV head, tokens of a unit, grid size
   int sub;            // keys per copy: a page, or part of one
   float scale_log2;   // scores to log2 units, the keys' unit included
+  int one;            // 1
 };
 
 // What the walking warp says of a tile, beside its codes.
+enum : int {
+  kFirst = 1,       // of a piece
+  kLast = 2,        // of a piece
+  kLastPiece = 4,   // and that the CTA's last one
+  kFull = 8,        // every row sees every key
+  kEmpty = 16,      // no row sees any key
+  kEnd = 32,        // no tile: the end of the run
+  kPart = 64,       // the piece leaves partial results,
+  kSlot1 = 128,     // those of slot 1
+  kBad = 256        // a page id of the piece (so far) is out of range
+};
 struct alignas(16) TileInfo {
-  int key0, full, first, last;   // full: every row sees every key; first / last tile of a piece
-  int lo, se, w0, hi;            // keys that any row of the unit sees
-  int tok0, ntok, kvh, i0;
-  int n, C, ks, empty;           // empty: no key at all (or, with tok0 < 0, the end of the run)
-  int part, slot, bad, last_piece;
+  int flags, key0, ntok, tok0;
+  int kvh, i0, n, C;
+  int lo, se, w0, hi;  // keys that any row of the unit sees
+  int ks, pad0, pad1, pad2;
 };
 
+// NB blocks of 8 query rows a warp, RG groups of rows.  Up to 8 rows take few
+// registers: four CTAs an SM of four warps, whose 32 keys a tile pay for what
+// a tile costs beside its products (eight warps of 16 keys, two CTAs an SM:
+// 448 instructions for 16 keys, 113 us for 64 tokens over 2048 to 8192 rows).
 template <int D, int NB, int RG>
 struct Cfg {
-  static constexpr int kRows = 8 * NB * RG;      // query rows of a unit
+  static constexpr int kRows = 8 * NB * RG;  // query rows of a unit
+  static constexpr int kWarps = NB == 1 ? 4 : 8;
+  static constexpr int kThreads = 32 * (kWarps + 1);
   static constexpr int kKeyGroups = kWarps / RG;
   static constexpr int kWarpKeys = kTile / kKeyGroups;
-  static constexpr int kCtas = NB == 1 ? 2 : 1;  // an SM
-  static constexpr int kStages = (NB == 1 ? 4 : 7) * (128 / D);
+  static constexpr int kStep = NB == 1 ? 32 : 16;  // keys between two looks at the maxima
+  static constexpr int kCtas = NB == 1 ? 3 : 1;    // an SM
+  static constexpr int kStages = (NB == 1 ? 3 : 7) * (128 / D);
 };
 
 template <int D>
@@ -89,8 +106,8 @@ struct SmemQ4 {
   using C = Cfg<D, NB, RG>;
   Stage<D> ring[C::kStages];
   __nv_bfloat16 q[2][C::kRows * D];
-  float4 fold[kWarps / 2][NB * (D / 16)][32];  // O of half the warps
-  float2 ml[kWarps][8 * NB];
+  float4 fold[C::kWarps / 2][NB * (D / 16)][32];  // O of half the warps
+  float2 ml[C::kWarps][8 * NB];
   float2 fin[C::kRows];
   TileInfo info[C::kStages];
   uint64_t bar_full[C::kStages], bar_free[C::kStages], bar_qfree[2], bar_merge[3];
@@ -180,13 +197,13 @@ __device__ __forceinline__ VCodes<D> load_v(const Stage<D>& st, int key, int g) 
 }
 
 template <int D, int NB, int RG, bool SINKS>
-__global__ void __launch_bounds__(kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kernel(const __grid_constant__ Q4Params p) {
+__global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kernel(const __grid_constant__ Q4Params p) {
   using C = Cfg<D, NB, RG>;
   using Smem = SmemQ4<D, NB, RG>;
-  constexpr int RB = C::kRows, kStages = C::kStages;
+  constexpr int RB = C::kRows, kStages = C::kStages, kWarps = C::kWarps;
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~static_cast<uintptr_t>(127));
-  static_assert(sizeof(sm.ring) >= kChunkMaxSeqs * 4, "the ring holds the tile counts of all sequences");
+  static_assert(sizeof(sm.ring) >= kMaxSeqs * 4, "the ring holds the tile counts of all sequences");
   volatile int* abort_flag = &sm.abort_flag;
   const unsigned full = 0xffffffffu;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -203,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kern
   }
   pdl_wait();
   int32_t* tiles = reinterpret_cast<int32_t*>(&sm.ring[0]);
-  plan_tiles<SINKS, kTile, kThreads>(p.a, p.ub, tiles);
+  plan_tiles<SINKS, kTile, C::kThreads>(p.a, p.ub, tiles);
   Place start{0, 0, 0, 0};
   int total = 0;
   ChunkSeq seq{};
@@ -242,14 +259,11 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kern
       u.n = k.s.n;
       u.C = k.s.C;
       u.ks = k.s.ks;
-      u.empty = piece.tiles == 0;
-      u.part = piece.take < piece.weight;
-      u.slot = piece.slot;
-      u.last_piece = piece.last;
-      u.bad = 0;
+      const bool empty = piece.tiles == 0;
+      int flags = (empty ? kEmpty : 0) | (piece.take < piece.weight ? kPart : 0) | (piece.slot ? kSlot1 : 0);
       // rows that every token of the unit sees
-      const int all_lo = u.empty ? 0 : key_lo(p.a, k.s, u.i0 + u.ntok - 1), all_hi = u.empty ? 0 : key_hi(p.a, k.s, u.i0);
-      const int all_se = SINKS && !u.empty ? sink_end(p.a, k.s, all_hi) : 0;
+      const int all_lo = empty ? 0 : key_lo(p.a, k.s, u.i0 + u.ntok - 1), all_hi = empty ? 0 : key_hi(p.a, k.s, u.i0);
+      const int all_se = SINKS && !empty ? sink_end(p.a, k.s, all_hi) : 0;
       const int skip = tiles_skipped<SINKS, kTile>(piece.keys), tse = (u.se + kTile - 1) / kTile;
       const int32_t* bt = p.a.block_table + static_cast<size_t>(k.w.b) * p.a.max_pages;
       const int t0 = u.lo / kTile + k.w.t;
@@ -258,10 +272,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kern
         const uint32_t st = it % kStages;
         const int t = t0 + i;
         u.key0 = (t + (SINKS && t >= tse ? skip : 0)) * kTile;
-        u.first = i == 0;
-        u.last = i + 1 == piece.take;
-        u.full = !u.empty && ((u.key0 >= all_lo && u.key0 + kTile <= all_hi) ||
-                              (SINKS && u.key0 >= u.ks && u.key0 + kTile <= all_se));
+        const bool all = !empty && ((u.key0 >= all_lo && u.key0 + kTile <= all_hi) ||
+                                    (SINKS && u.key0 >= u.ks && u.key0 + kTile <= all_se));
+        u.flags = (i == 0 ? kFirst : 0) | (i + 1 == piece.take ? kLast | (piece.last ? kLastPiece : 0) : 0) | (all ? kFull : 0);
         // copy s of the tile is lane s's
         const int nsub = kTile / sub, key = u.key0 + min(lane, nsub - 1) * sub, pi = key / P;
         const int pi0 = u.key0 / P, pi1 = (u.key0 + kTile - 1) / P;
@@ -270,15 +283,16 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kern
           win = win_base + lane < p.a.max_pages ? bt[win_base + lane] : -1;
         }
         const int pg = __shfl_sync(full, win, (pi - win_base) & 31);
-        bool load = !u.empty && lane < nsub && key + sub > u.lo && key < u.hi && (!SINKS || key < u.se || key + sub > u.w0);
+        bool load = !empty && lane < nsub && key + sub > u.lo && key < u.hi && (!SINKS || key < u.se || key + sub > u.w0);
         const bool wrong = load && (pg < 0 || pg >= p.a.num_pages);
         load = load && !wrong;
         if (__any_sync(full, wrong)) {
           if (lane == 0) raise_error(p.a.err_word, SIMSD_EW_PAGE);
-          u.bad = 1;
+          flags |= kBad;
         }
         if (!slot_free()) break;
-        const bool with_q = u.first && !u.empty;
+        u.flags |= flags;
+        const bool with_q = i == 0 && !empty;
         const uint32_t qb = units & 1;
         if (with_q && units >= 2) {
           ok = mbar_wait_warp(smem_u32(&sm.bar_qfree[qb]), ((units >> 1) - 1) & 1, abort_flag);
@@ -319,8 +333,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kern
       // the end of the run
       if (lane == 0) {
         TileInfo u{};
-        u.tok0 = -1;
-        u.empty = 1;
+        u.flags = kEnd;
         sm.info[it % kStages] = u;
         mbar_arrive(smem_u32(&sm.bar_full[it % kStages]));
       }
@@ -342,7 +355,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kern
   const int perm = g ^ ((g >> 1) & 1);    // place of key g among 8: neighbours in pairs, pairs turned in turns
   const int va = (2 * t) ^ (t & 1), vb = (2 * t + 1) ^ (t & 1);
   constexpr int kSteps = D / 16;          // products of 16 components; blocks of 16 channels
+  constexpr int G = C::kStep / 16;
   uint32_t q[NB][kSteps][2];
+  // m: the reference that the probabilities are formed against, in log2 units
   float o[NB][kSteps][4], m[NB][2], l[NB][2], rs[NB][2];
   uint32_t units = 0, pieces = 0;
   bool ok = true;
@@ -354,18 +369,18 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kern
     }
     const Stage<D>& s = sm.ring[st];
     const TileInfo& info = sm.info[st];
-    const int tok0 = info.tok0, ntok = info.ntok, key0 = info.key0;
-    const bool empty = info.empty != 0, last = info.last != 0;
-    if (tok0 < 0) break;
-    if (info.first) {
+    const int4 head = *reinterpret_cast<const int4*>(&info);
+    const int flags = head.x, key0 = head.y, ntok = head.z, tok0 = head.w;
+    if (flags & kEnd) break;
+    if (flags & kFirst) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) o[nb][k][0] = o[nb][k][1] = o[nb][k][2] = o[nb][k][3] = 0.f;
-        m[nb][0] = m[nb][1] = -INFINITY;
+        m[nb][0] = m[nb][1] = kNoReference;
         l[nb][0] = l[nb][1] = 0.f;
       }
-      if (!empty) {
+      if (!(flags & kEmpty)) {
         const uint32_t qb = units & 1;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -402,80 +417,84 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kern
         ++units;
       }
     }
-    if (!empty) {
-      const bool masked = info.full == 0;
-      const int lo = info.lo, se = info.se, w0 = info.w0, hi = info.hi, ks = info.ks;
-      int klo[NB][2], khi[NB][2], kse[NB][2];
-      if (masked) {
-        ChunkSeq cs;
-        cs.n = info.n;
-        cs.C = info.C;
-        cs.ks = ks;
-        const int i0 = info.i0;
+    if (!(flags & kEmpty)) {
+      const bool masked = !(flags & kFull);
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+      for (int step = 0; step < C::kWarpKeys / C::kStep; ++step) {
+        const int kb = kg * C::kWarpKeys + C::kStep * step;
+        // S^T of keys perm(g) and 8 + perm(g) of each 16, rows 2t and 2t + 1
+        float sc[G][NB][4];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int tl = min(((rg * NB + nb) * 8 + 2 * t + e) / p.g, ntok - 1);
-            klo[nb][e] = key_lo(p.a, cs, i0 + tl);
-            khi[nb][e] = key_hi(p.a, cs, i0 + tl);
-            kse[nb][e] = SINKS ? sink_end(p.a, cs, khi[nb][e]) : 0;
-          }
-      }
+        for (int u = 0; u < G; ++u) {
 #pragma unroll
-      for (int sub = 0; sub < C::kWarpKeys / 16; ++sub) {
-        const int kb = kg * C::kWarpKeys + 16 * sub;
-        const KCodes<D> ka = load_k(s, kb + perm, t), kc = load_k(s, kb + 8 + perm, t);
-        // S^T of keys perm(g) and 8 + perm(g), rows 2t and 2t + 1
-        float sc[NB][4];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) sc[nb][0] = sc[nb][1] = sc[nb][2] = sc[nb][3] = 0.f;
-        uint32_t sa[D / 64], sb[D / 64];
-        {
+          for (int nb = 0; nb < NB; ++nb) sc[u][nb][0] = sc[u][nb][1] = sc[u][nb][2] = sc[u][nb][3] = 0.f;
+          const KCodes<D> ka = load_k(s, kb + 16 * u + perm, t), kc = load_k(s, kb + 16 * u + 8 + perm, t);
           const uint32_t x = q4_scale_pair(ka.s), y = q4_scale_pair(kc.s);
+          uint32_t sa[2], sb[2];
           sa[0] = __byte_perm(x, 0, 0x1010);
           sb[0] = __byte_perm(y, 0, 0x1010);
-          if constexpr (D == 128) {
-            sa[1] = __byte_perm(x, 0, 0x3232);
-            sb[1] = __byte_perm(y, 0, 0x3232);
+          sa[1] = __byte_perm(x, 0, 0x3232);  // (128 components: a thread's lie in two groups)
+          sb[1] = __byte_perm(y, 0, 0x3232);
+#pragma unroll
+          for (int k = 0; k < kSteps; ++k) {
+            const uint32_t wa = ka.w[k / 2], wb = kc.w[k / 2], fa = sa[k / 4], fb = sb[k / 4];
+            const uint32_t a0 = mul_f16x2(k & 1 ? q4_pair<2>(wa) : q4_pair<0>(wa), fa);
+            const uint32_t a1 = mul_f16x2(k & 1 ? q4_pair<2>(wb) : q4_pair<0>(wb), fb);
+            const uint32_t a2 = mul_f16x2(k & 1 ? q4_pair<3>(wa) : q4_pair<1>(wa), fa);
+            const uint32_t a3 = mul_f16x2(k & 1 ? q4_pair<3>(wb) : q4_pair<1>(wb), fb);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma16816(sc[u][nb], a0, a1, a2, a3, q[nb][k][0], q[nb][k][1]);
           }
         }
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-          const uint32_t u = ka.w[k / 2], v = kc.w[k / 2], fa = sa[k / 4], fb = sb[k / 4];
-          const uint32_t a0 = mul_f16x2(k & 1 ? q4_pair<2>(u) : q4_pair<0>(u), fa);
-          const uint32_t a1 = mul_f16x2(k & 1 ? q4_pair<2>(v) : q4_pair<0>(v), fb);
-          const uint32_t a2 = mul_f16x2(k & 1 ? q4_pair<3>(u) : q4_pair<1>(u), fa);
-          const uint32_t a3 = mul_f16x2(k & 1 ? q4_pair<3>(v) : q4_pair<1>(v), fb);
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) mma16816(sc[nb], a0, a1, a2, a3, q[nb][k][0], q[nb][k][1]);
-        }
-        // scores in log2 units, hidden ones -inf
-        bool above = false;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            sc[nb][e] *= rs[nb][e & 1];
-            if (masked) {
-              const int key = key0 + kb + perm + (e & 2 ? 8 : 0);
-              const bool in = (key >= klo[nb][e & 1] && key < khi[nb][e & 1]) || (SINKS && key >= ks && key < kse[nb][e & 1]);
-              sc[nb][e] = in ? sc[nb][e] : -INFINITY;
-            }
-            above |= sc[nb][e] > m[nb][e & 1] + kRescaleThreshold;
-          }
-        }
-        // (the first scores of a piece lie above -inf)
-        if (__any_sync(full, above)) {
+        // (Written as loops that run once, a number the compiler does not know:
+        // as conditions, these two and the one below become predicates on some
+        // 100 instructions that every step then issues.)
+#pragma unroll 1
+        for (int once = masked ? p.one : 0; once > 0; --once) {
+          ChunkSeq cs;
+          cs.n = info.n;
+          cs.C = info.C;
+          cs.ks = info.ks;
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float mx = fmaxf(m[nb][e], fmaxf(sc[nb][e], sc[nb][e + 2]));
+              const int tl = info.i0 + min(((rg * NB + nb) * 8 + 2 * t + e) / p.g, ntok - 1);
+              const int lo = key_lo(p.a, cs, tl), hi = key_hi(p.a, cs, tl), se = SINKS ? sink_end(p.a, cs, hi) : 0;
+#pragma unroll
+              for (int u = 0; u < G; ++u)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  const int key = key0 + kb + 16 * u + 8 * h + perm;
+                  if (!((key >= lo && key < hi) || (SINKS && key >= cs.ks && key < se))) sc[u][nb][2 * h + e] = -INFINITY;
+                }
+            }
+        }
+        // exponents; those of rows whose reference has to move again
+        float pr[G][NB][4];
+        bool above = false;
+#pragma unroll
+        for (int u = 0; u < G; ++u)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              pr[u][nb][e] = fmaf(sc[u][nb][e], rs[nb][e & 1], -m[nb][e & 1]);
+              above |= pr[u][nb][e] > kRescaleThreshold;
+            }
+#pragma unroll 1
+        for (int once = __any_sync(full, above) ? p.one : 0; once > 0; --once) {
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float mx = m[nb][e];
+#pragma unroll
+              for (int u = 0; u < G; ++u) mx = fmaxf(mx, fmaxf(sc[u][nb][e], sc[u][nb][e + 2]) * rs[nb][e]);
               mx = fmaxf(mx, __shfl_xor_sync(full, mx, 4));
               mx = fmaxf(mx, __shfl_xor_sync(full, mx, 8));
               mx = fmaxf(mx, __shfl_xor_sync(full, mx, 16));
-              const float f = m[nb][e] == -INFINITY ? 0.f : exp2_approx(m[nb][e] - mx);
+              const float f = exp2_approx(m[nb][e] - mx);
               m[nb][e] = mx;
               l[nb][e] *= f;
 #pragma unroll
@@ -483,65 +502,73 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kern
                 o[nb][k][e] *= f;
                 o[nb][k][e + 2] *= f;
               }
+#pragma unroll
+              for (int u = 0; u < G; ++u) {
+                pr[u][nb][e] = fmaf(sc[u][nb][e], rs[nb][e], -mx);
+                pr[u][nb][e + 2] = fmaf(sc[u][nb][e + 2], rs[nb][e], -mx);
+              }
             }
         }
-        uint32_t pb[NB][2];
+        uint32_t pb[G][NB][2];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          float pr[4];
+        for (int u = 0; u < G; ++u)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float ref = m[nb][e & 1] == -INFINITY ? 0.f : m[nb][e & 1];
-            pr[e] = exp2_approx(sc[nb][e] - ref);
+          for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pr[u][nb][e] = exp2_approx(pr[u][nb][e]);
+            l[nb][0] += pr[u][nb][0] + pr[u][nb][2];
+            l[nb][1] += pr[u][nb][1] + pr[u][nb][3];
+            pb[u][nb][0] = transpose8(pack_f16x2(pr[u][nb][0], pr[u][nb][1]));
+            pb[u][nb][1] = transpose8(pack_f16x2(pr[u][nb][2], pr[u][nb][3]));
           }
-          l[nb][0] += pr[0] + pr[2];
-          l[nb][1] += pr[1] + pr[3];
-          pb[nb][0] = transpose8(pack_f16x2(pr[0], pr[1]));
-          pb[nb][1] = transpose8(pack_f16x2(pr[2], pr[3]));
-        }
-        // V^T of keys va, vb and 8 + va, 8 + vb, channels from g D / 8 on (all of one scale)
-        const VCodes<D> v0 = load_v(s, kb + va, g), v1 = load_v(s, kb + vb, g);
-        const VCodes<D> v2 = load_v(s, kb + 8 + va, g), v3 = load_v(s, kb + 8 + vb, g);
-        constexpr int kScales = D / kQ4Group;
-        const int vg = D == 128 ? g : g >> 1;
-        uint32_t s01 = s.vs[(kb + va) * kScales + vg] | s.vs[(kb + vb) * kScales + vg] << 8;
-        uint32_t s23 = s.vs[(kb + 8 + va) * kScales + vg] | s.vs[(kb + 8 + vb) * kScales + vg] << 8;
-        if (masked) {
-          // values of rows that no token of the unit sees may be anything: 0
-          auto seen = [&](int key) { return key >= lo && key < hi && (!SINKS || key < se || key >= w0); };
-          s01 &= (seen(key0 + kb + va) ? 0xffu : 0u) | (seen(key0 + kb + vb) ? 0xff00u : 0u);
-          s23 &= (seen(key0 + kb + 8 + va) ? 0xffu : 0u) | (seen(key0 + kb + 8 + vb) ? 0xff00u : 0u);
-        }
-        const uint32_t f01 = q4_scale_pair(s01), f23 = q4_scale_pair(s23);
-        constexpr uint32_t kLow = 0x0f0f0f0fu;
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-          // bytes of two keys' codes of one channel
-          const uint32_t e01 = (v0.w[i] & kLow) | (v1.w[i] << 4 & ~kLow), d01 = (v0.w[i] >> 4 & kLow) | (v1.w[i] & ~kLow);
-          const uint32_t e23 = (v2.w[i] & kLow) | (v3.w[i] << 4 & ~kLow), d23 = (v2.w[i] >> 4 & kLow) | (v3.w[i] & ~kLow);
-          auto block = [&](float (&acc)[NB][kSteps][4], int k, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
-            a0 = mul_f16x2(a0, f01);
-            a1 = mul_f16x2(a1, f01);
-            a2 = mul_f16x2(a2, f23);
-            a3 = mul_f16x2(a3, f23);
+        for (int u = 0; u < G; ++u) {
+          // V^T of keys va, vb and 8 + va, 8 + vb, channels from g D / 8 on (all of one scale)
+          const int kv = kb + 16 * u;
+          const VCodes<D> v0 = load_v(s, kv + va, g), v1 = load_v(s, kv + vb, g);
+          const VCodes<D> v2 = load_v(s, kv + 8 + va, g), v3 = load_v(s, kv + 8 + vb, g);
+          constexpr int kScales = D / kQ4Group;
+          const int vg = D == 128 ? g : g >> 1;
+          uint32_t s01 = s.vs[(kv + va) * kScales + vg] | s.vs[(kv + vb) * kScales + vg] << 8;
+          uint32_t s23 = s.vs[(kv + 8 + va) * kScales + vg] | s.vs[(kv + 8 + vb) * kScales + vg] << 8;
+#pragma unroll 1
+          for (int once = masked ? p.one : 0; once > 0; --once) {
+            // values of rows that no token of the unit sees may be anything: 0
+            const int lo = info.lo, se = info.se, w0 = info.w0, hi = info.hi, at = key0 + kv;
+            auto seen = [&](int key) { return key >= lo && key < hi && (!SINKS || key < se || key >= w0); };
+            s01 &= (seen(at + va) ? 0xffu : 0u) | (seen(at + vb) ? 0xff00u : 0u);
+            s23 &= (seen(at + 8 + va) ? 0xffu : 0u) | (seen(at + 8 + vb) ? 0xff00u : 0u);
+          }
+          const uint32_t f01 = q4_scale_pair(s01), f23 = q4_scale_pair(s23);
+          constexpr uint32_t kLow = 0x0f0f0f0fu;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma16816(acc[nb][k], a0, a1, a2, a3, pb[nb][0], pb[nb][1]);
-          };
-          block(o, 4 * i, q4_pair<0>(e01), q4_pair<0>(d01), q4_pair<0>(e23), q4_pair<0>(d23));
-          block(o, 4 * i + 1, q4_pair<1>(e01), q4_pair<1>(d01), q4_pair<1>(e23), q4_pair<1>(d23));
-          block(o, 4 * i + 2, q4_pair<2>(e01), q4_pair<2>(d01), q4_pair<2>(e23), q4_pair<2>(d23));
-          block(o, 4 * i + 3, q4_pair<3>(e01), q4_pair<3>(d01), q4_pair<3>(e23), q4_pair<3>(d23));
+          for (int i = 0; i < D / 64; ++i) {
+            // bytes of two keys' codes of one channel
+            const uint32_t e01 = (v0.w[i] & kLow) | (v1.w[i] << 4 & ~kLow), d01 = (v0.w[i] >> 4 & kLow) | (v1.w[i] & ~kLow);
+            const uint32_t e23 = (v2.w[i] & kLow) | (v3.w[i] << 4 & ~kLow), d23 = (v2.w[i] >> 4 & kLow) | (v3.w[i] & ~kLow);
+            auto block = [&](int k, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+              a0 = mul_f16x2(a0, f01);
+              a1 = mul_f16x2(a1, f01);
+              a2 = mul_f16x2(a2, f23);
+              a3 = mul_f16x2(a3, f23);
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) mma16816(o[nb][k], a0, a1, a2, a3, pb[u][nb][0], pb[u][nb][1]);
+            };
+            block(4 * i, q4_pair<0>(e01), q4_pair<0>(d01), q4_pair<0>(e23), q4_pair<0>(d23));
+            block(4 * i + 1, q4_pair<1>(e01), q4_pair<1>(d01), q4_pair<1>(e23), q4_pair<1>(d23));
+            block(4 * i + 2, q4_pair<2>(e01), q4_pair<2>(d01), q4_pair<2>(e23), q4_pair<2>(d23));
+            block(4 * i + 3, q4_pair<3>(e01), q4_pair<3>(d01), q4_pair<3>(e23), q4_pair<3>(d23));
+          }
         }
       }
     }
     // what the end of a piece needs is read before the slot is given back
-    const bool part = info.part != 0, bad = info.bad != 0;
-    const int kvh = info.kvh, entry = static_cast<int>(blockIdx.x) * 2 + info.slot;
-    const bool last_piece = last && info.last_piece != 0;
+    const bool part = flags & kPart, bad = flags & kBad;
+    const int kvh = info.kvh, entry = static_cast<int>(blockIdx.x) * 2 + (flags & kSlot1 ? 1 : 0);
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&sm.bar_free[st]));
-    if (last_piece) pdl_launch_next();
-    if (!last) continue;
+    if (flags & kLastPiece) pdl_launch_next();
+    if (!(flags & kLast)) continue;
 
     // ---- the warps' results, merged: maxima and sums first
     const uint32_t par = pieces & 1;
@@ -566,16 +593,15 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kern
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float M = -INFINITY, L = 0.f;
+        float M = kNoReference, L = 0.f;
 #pragma unroll
         for (int w = 0; w < C::kKeyGroups; ++w) M = fmaxf(M, sm.ml[w * RG + rg][8 * nb + 2 * t + e].x);
-        const float ref = M == -INFINITY ? 0.f : M;
 #pragma unroll
         for (int w = 0; w < C::kKeyGroups; ++w) {
           const float2 x = sm.ml[w * RG + rg][8 * nb + 2 * t + e];
-          L = fmaf(exp2_approx(x.x - ref), x.y, L);
+          L = fmaf(exp2_approx(x.x - M), x.y, L);
         }
-        const float f = exp2_approx(m[nb][e] - ref);
+        const float f = exp2_approx(m[nb][e] - M);
         if (kg == 0 && g == 0) sm.fin[(rg * NB + nb) * 8 + 2 * t + e] = make_float2(M, L);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
@@ -694,7 +720,7 @@ int q4_rows(int T, int Bt, int g) {
     if (g <= rb && static_cast<long long>(T) * g <= static_cast<long long>(rb) * Bt) return rb;
   return 64;
 }
-constexpr int q4_ctas(int rows, int num_sms) { return (rows == 8 ? 2 : 1) * num_sms; }
+constexpr int q4_ctas(int rows, int num_sms) { return (rows == 8 ? Cfg<128, 1, 1>::kCtas : 1) * num_sms; }
 
 template <int D, int NB, int RG, bool SINKS>
 cudaError_t launch_rows(Q4Params p, int num_sms, cudaStream_t stream) {
@@ -718,7 +744,7 @@ cudaError_t launch_rows(Q4Params p, int num_sms, cudaStream_t stream) {
       done[dev] = true;
     }
   }
-  e = launch_overlapped(chunk_q4_kernel<D, NB, RG, SINKS>, dim3(static_cast<unsigned>(p.ctas)), dim3(kThreads), bytes,
+  e = launch_overlapped(chunk_q4_kernel<D, NB, RG, SINKS>, dim3(static_cast<unsigned>(p.ctas)), dim3(C::kThreads), bytes,
                         stream, 1u, p);
   if (e != cudaSuccess || p.ctas == 1) return e;
   return launch_overlapped(chunk_q4_merge_kernel<D, C::kRows>, dim3(static_cast<unsigned>(p.ctas - 1), C::kRows > 16 ? 4u : 1u),
@@ -738,7 +764,7 @@ cudaError_t launch_d(const Q4Params& p, int num_sms, cudaStream_t stream) {
 }  // namespace
 
 bool chunk_q4_few(int dtype, int T, int Bt, int Hq, int Hkv) {
-  return dtype == SIMSD_BF16 && Hq / Hkv <= 64 && static_cast<long long>(T) * Hq <= 64ll * Bt * Hkv;
+  return dtype == SIMSD_BF16 && Hq / Hkv <= 64 && Bt <= kMaxSeqs && static_cast<long long>(T) * Hq <= 64ll * Bt * Hkv;
 }
 
 size_t chunk_q4_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, int num_sms) {
@@ -750,6 +776,7 @@ cudaError_t launch_chunk_attention_q4(const ChunkArgs& a, const simsd_q4_cache& 
   Q4Params p{};
   p.a = a;
   p.c = c;
+  p.one = 1;
   p.g = a.Hq / a.Hkv;
   p.sub = a.page_size % kTile == 0 ? kTile : std::min(a.page_size, 64);
   p.scale_log2 = a.scale * c.k_unit * 1.4426950408889634f;

@@ -92,7 +92,8 @@ struct alignas(16) PieceBase {
   int t0, tiles;       // this piece's key tiles; tiles 0: the rows are zero; -1: no more pieces
   int lo, hi;          // keys that the unit's tokens see
   int n, C, ks, i0;    // the sequence (chunk_mask.cuh) and the unit's first token in it
-  int part, slot;      // writes partial results (slot 0: the piece at the start of the run)
+  int part, slot;      // writes partial results (bit 0 of slot 0: the piece at the start of the run); bit 1 of
+                       // slot: the row block that a unit of few tokens takes
   int last, flag;      // the CTA's last piece; its entry in `bad`
 };
 template <bool SINKS>
@@ -278,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       Walk<SINKS, kTile> k;
       k.begin(p.a, ub, p.ctas, start, seq, total);
       typename Walk<SINKS, kTile>::Step piece;
-      uint32_t at = 0;
+      uint32_t at = 0, solo = 0;
       bool ok = true;
       for (;;) {
         Piece<SINKS> u;
@@ -298,6 +299,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           u.ks = k.s.ks;
           u.part = piece.take < piece.weight;
           u.slot = piece.slot;
+          // units of few tokens have one row block: A and B in turns, so that
+          // the end of one unit lies under the next one's tiles
+          if (u.ntok <= p.tb && u.tiles > 0) u.slot |= (solo++ & 1) << 1;
           u.last = piece.last;
           u.flag = at % kFlags;
           if constexpr (SINKS) {
@@ -332,7 +336,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) {
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            if (x >= nblk || !ok) continue;
+            if ((nblk == 1 && x != u.slot >> 1) || !ok) continue;
             if (jq[x] > 0 && !mbar_wait(smem_u32(&sm.bar_qfree[x]), (jq[x] - 1) & 1, abort_flag)) {
               ok = false;
               continue;
@@ -341,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_arrive_expect_tx(bq, static_cast<uint32_t>(kHalves * p.g * p.tb) * 128u);
 #pragma unroll
             for (int hf = 0; hf < kHalves; ++hf)
-              tma_load_3d(smem_u32(sm.q[x]) + hf * kHalfBytes, &tm_q, bq, 64 * hf, u.kvh * p.g, u.tok0 + x * p.tb);
+              tma_load_3d(smem_u32(sm.q[x]) + hf * kHalfBytes, &tm_q, bq, 64 * hf, u.kvh * p.g, u.tok0 + (nblk == 1 ? 0 : x * p.tb));
             ++jq[x];
           }
         }
@@ -471,9 +475,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       while (ok && (ok = next_piece<D, SINKS>(sm, at, u)) && u.tiles >= 0) {
         const int n = u.tiles;
         if (n == 0) continue;
-        if (x == 1 && u.ntok <= p.tb) {
-          // a unit of few tokens has no second row block: its tiles are only
-          // passed on (each tile's release counts both blocks)
+        if (u.ntok <= p.tb && x != u.slot >> 1) {
+          // a unit of few tokens has one row block: for the other its tiles are
+          // only passed on (each tile's release counts both blocks)
           for (int i = 0; ok && i < n; ++i) {
             ok = wait(sm.bar_full[ks], kp);
             if (ok && leader) tc_commit(smem_u32(&sm.bar_free[ks]));
@@ -533,9 +537,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     Piece<SINKS> u;
     while ((ok = ok && next_piece<D, SINKS>(sm, at, u)) && u.tiles >= 0) {
-      const int xt = x * p.tb + tl;  // token of this row within the unit
+      const bool solo = u.ntok <= p.tb;
+      const int xb = solo ? 0 : x;    // which of the unit's row blocks this one is
+      const int xt = xb * p.tb + tl;  // token of this row within the unit
       const bool row_exists = tl < p.tb && xt < u.ntok;
-      const bool has = x == 0 || u.ntok > p.tb;
+      const bool has = !solo || x == u.slot >> 1;
       const bool active = row_exists && u.tiles > 0;
       int klo = 0, khi = 0, kse = 0;  // this row's keys: [klo, khi), and [u.ks, kse) where first rows stay visible
       if (active) {
@@ -563,8 +569,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           // Rows of V outside the unit's keys may hold anything: zeroed, so
           // that 0 * NaN cannot reach O.  Both blocks write the same zeros,
-          // so each block's PV sees them.  Not before S of the tile: block
-          // B's warps skip units that have no block B without a wait, and
+          // so each block's PV sees them.  Not before S of the tile: a block's
+          // warps skip units that they have no part in without a wait, and
           // then lag behind the ring by many uses of a slot, which a parity
           // does not tell apart.  The block's MMA warp, which has waited for
           // every use of V in turn, issues this S after the last one before
@@ -725,7 +731,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool poison = u.tiles > 0 && *reinterpret_cast<volatile int*>(&sm.bad[u.flag]) != 0;
       const bool any = have_o && seen && l_sum != 0.f && !poison;
       const float inv = any ? 1.0f / l_sum : 0.f;
-      const int entry = (static_cast<int>(blockIdx.x) * 2 + u.slot) * 2 + x;
+      const int entry = (static_cast<int>(blockIdx.x) * 2 + (u.slot & 1)) * 2 + xb;
       const size_t out_row = static_cast<size_t>(u.tok0 + (row_exists ? xt : 0)) * p.a.Hq + u.kvh * p.g + hl;
       uint8_t* orow = static_cast<uint8_t*>(p.a.out) + out_row * (2 * D);
 #pragma unroll 1

@@ -85,16 +85,21 @@ __device__ __forceinline__ uint32_t free_bits(const int32_t* refs, int p0, int n
 
 // The search for free pages of one CTA: `list` gets the ids of the free pages
 // numbered base .. base + kList - 1 from the lowest on.  Returns how many free
-// pages there are, counted only as far as `most`.
+// pages there are, counted only as far as `most`.  first: the thread's bits of
+// the first step, loaded while other loads were on their way.
 struct Free {
   BlockSum sum;
   int list[kList];
 };
-__device__ int find_free(Free& sm, const int32_t* refs, int num_pages, int base, int most) {
+__device__ __forceinline__ uint32_t step_bits(const int32_t* refs, int num_pages, long long s0) {
+  const long long p0 = s0 + static_cast<long long>(threadIdx.x) * kPerThread;
+  return p0 < num_pages ? free_bits(refs, static_cast<int>(p0), num_pages) : 0u;
+}
+__device__ int find_free(Free& sm, const int32_t* refs, int num_pages, uint32_t first, int base, int most) {
   int found = 0;
   for (long long s0 = 0; s0 < num_pages && found < most; s0 += kStep) {
     const int p0 = static_cast<int>(s0) + threadIdx.x * kPerThread;
-    uint32_t m = s0 + static_cast<long long>(threadIdx.x) * kPerThread < num_pages ? free_bits(refs, p0, num_pages) : 0u;
+    uint32_t m = s0 == 0 ? first : step_bits(refs, num_pages, s0);
     const int c = __popc(m);
     int total;
     int at = found + block_inclusive(sm.sum, c, total) - c - base;
@@ -126,104 +131,145 @@ __device__ __forceinline__ Span span_of(const PagesArgs& a, int b) {
   return s;
 }
 
-// Entries of the span that name no page, or -1: the span is refused.  A warp.
+// How many entries of the span name no page; 0 where the span is refused (a
+// page in it is shared, or none of the pool's).
+constexpr int kShort = 8;  // entries that a thread looks at by itself, at once
+__device__ __forceinline__ uint32_t entry_error(const PagesArgs& a, int pg) {
+  if (pg == -1) return 0u;
+  if (pg < 0 || pg >= a.num_pages) return SIMSD_EW_PAGE;
+  return a.refs[pg] > 1 ? SIMSD_EW_SHARED : 0u;
+}
 __device__ __forceinline__ int wanted(const PagesArgs& a, int b, const Span& s, uint32_t* err) {
-  const int lane = threadIdx.x & 31;
-  const int32_t* row = a.block_table + static_cast<size_t>(b) * a.max_pages;
+  const unsigned full = 0xffffffffu;
+  const int lane = threadIdx.x & 31, len = s.last - s.first;
   int n = 0;
-  uint32_t e = 0;
-  for (int k0 = s.first; k0 < s.last; k0 += 32) {
-    const int k = k0 + lane, pg = k < s.last ? row[k] : 0;
-    const bool none = k < s.last && pg == -1;
-    if (k < s.last && !none) {
-      if (pg < 0 || pg >= a.num_pages)
-        e |= SIMSD_EW_PAGE;
-      else if (a.refs[pg] > 1)
-        e |= SIMSD_EW_SHARED;
+  if (len > 0 && len <= kShort) {
+    const int32_t* row = a.block_table + static_cast<size_t>(b) * a.max_pages + s.first;
+    int pg[kShort];
+    uint32_t e = 0;
+#pragma unroll
+    for (int k = 0; k < kShort; ++k) pg[k] = k < len ? row[k] : 0;
+#pragma unroll
+    for (int k = 0; k < kShort; ++k) {
+      if (k >= len) continue;
+      n += pg[k] == -1;
+      e |= entry_error(a, pg[k]);
     }
-    n += __popc(__ballot_sync(0xffffffffu, none));
+    *err |= e;
+    if (e) n = 0;
   }
-  e = __reduce_or_sync(0xffffffffu, e);
-  *err |= e;
-  return e ? -1 : n;
+  // longer spans: the warp together
+  for (unsigned m = __ballot_sync(full, len > kShort); m; m &= m - 1) {
+    const int who = __ffs(m) - 1;
+    const int bb = __shfl_sync(full, b, who), first = __shfl_sync(full, s.first, who), last = __shfl_sync(full, s.last, who);
+    const int32_t* row = a.block_table + static_cast<size_t>(bb) * a.max_pages;
+    int c = 0;
+    uint32_t e = 0;
+    for (int k = first + lane; k < last; k += 32) {
+      const int pg = row[k];
+      c += pg == -1;
+      e |= entry_error(a, pg);
+    }
+    c = __reduce_add_sync(full, c);
+    e = __reduce_or_sync(full, e);
+    if (lane == who) {
+      n = e ? 0 : c;
+      *err |= e;
+    }
+  }
+  return n;
 }
 
 __global__ void __launch_bounds__(kPlanThreads, 1) extend_kernel(const __grid_constant__ PagesArgs a) {
   __shared__ Free sm;
-  __shared__ int sums[kPlanThreads / 32];
-  __shared__ int all;
   pdl_wait();
   pdl_launch_next();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // sequences in rounds of 32 warps; a warp keeps count of its own
+  const unsigned full = 0xffffffffu;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const uint32_t first = step_bits(a.refs, a.num_pages, 0);
+  // a thread per sequence, in rounds; of the first round it keeps what it found
   uint32_t err = 0;
-  int mine = 0;
-  for (int b = warp; b < a.Bt; b += kPlanThreads / 32) {
-    const Span s = span_of(a, b);
-    if (s.bad) err |= SIMSD_EW_PREFIX_LEN;
-    if (s.first < s.last) mine += max(0, wanted(a, b, s, &err));
+  Span mine{0, 0, true};
+  int mine_n = 0, mine_at = 0, total = 0;
+  auto look = [&](int b, Span& s, uint32_t* e) {
+    s = Span{0, 0, true};
+    if (b < a.Bt) {
+      s = span_of(a, b);
+      if (s.bad) *e |= SIMSD_EW_PREFIX_LEN;
+    }
+    return wanted(a, b, s, e);
+  };
+  for (int b0 = 0; b0 < a.Bt; b0 += kPlanThreads) {
+    Span s;
+    const int n = look(b0 + tid, s, &err);
+    int turn;
+    const int at = total + block_inclusive(sm.sum, n, turn) - n;
+    if (b0 == 0) {
+      mine = s;
+      mine_n = n;
+      mine_at = at;
+    }
+    total += turn;
   }
-  if (lane == 0) {
-    sums[warp] = mine;
-    if (err) raise_error(a.err_word, err);
-  }
-  __syncthreads();
-  if (warp == 0) {
-    const int v = __reduce_add_sync(0xffffffffu, sums[lane]);
-    if (lane == 0) all = v;
-  }
-  __syncthreads();
-  const int total = all;
+  if (err) raise_error(a.err_word, err);
   if (total == 0) return;
-  const int have = find_free(sm, a.refs, a.num_pages, 0, total);
-  if (have < total) {
+  if (find_free(sm, a.refs, a.num_pages, first, 0, total) < total) {
     if (tid == 0) raise_error(a.err_word, SIMSD_EW_POOL);
     return;
   }
   // Requests are numbered by sequence, then entry.  A round hands out the
-  // pages of the list; what an earlier round has filled in is counted by the
-  // round's base, since those entries no longer want a page.
+  // pages of the list, requests base .. base + kList - 1.
   for (int base = 0; base < total; base += kList) {
     if (base > 0) {
-      // (the pages of the last round are taken now: the list starts anew)
+      // (the pages of the last round are taken now, and its entries want none
+      // any more: list and requests are numbered anew)
       __syncthreads();
-      find_free(sm, a.refs, a.num_pages, 0, total - base);
+      find_free(sm, a.refs, a.num_pages, step_bits(a.refs, a.num_pages, 0), 0, total - base);
     }
     const int room = min(kList, total - base);
-    int before = 0;  // requests of the sequences before this round of warps
-    for (int b0 = 0; b0 < a.Bt && before < room; b0 += kPlanThreads / 32) {
-      const int b = b0 + warp;
-      Span s{0, 0, true};
-      int n = 0;
-      if (b < a.Bt) {
-        s = span_of(a, b);
+    int before = 0;
+    for (int b0 = 0; b0 < a.Bt && before < room; b0 += kPlanThreads) {
+      const int b = b0 + tid;
+      Span s = mine;
+      int n = mine_n, at = mine_at, turn = 0;
+      if (base > 0 || b0 > 0) {
         uint32_t ignored = 0;
-        if (s.first < s.last) n = max(0, wanted(a, b, s, &ignored));
+        n = look(b, s, &ignored);
+        at = before + block_inclusive(sm.sum, n, turn) - n;
+      } else if (a.Bt > kPlanThreads) {
+        block_inclusive(sm.sum, n, turn);
       }
-      __syncthreads();  // (sums has been read by all)
-      if (lane == 0) sums[warp] = n;
-      __syncthreads();
-      int at = before, turn = 0;
-      for (int w = 0; w < kPlanThreads / 32; ++w) {
-        at += w < warp ? sums[w] : 0;
-        turn += sums[w];
-      }
-      if (n > 0) {
-        int32_t* row = a.block_table + static_cast<size_t>(b) * a.max_pages;
-        for (int k0 = s.first; k0 < s.last; k0 += 32) {
-          const int k = k0 + lane;
-          const bool none = k < s.last && row[k] == -1;
-          const unsigned m = __ballot_sync(0xffffffffu, none);
-          const int mine_at = at + __popc(m & ((1u << lane) - 1u));
-          if (none && mine_at < room) {
-            const int pg = sm.list[mine_at];
-            row[k] = pg;
-            a.refs[pg] = 1;
+      const int len = s.last - s.first;
+      if (n > 0 && len <= kShort) {
+        int32_t* row = a.block_table + static_cast<size_t>(b) * a.max_pages + s.first;
+        for (int k = 0, j = at; k < len; ++k) {
+          if (row[k] != -1) continue;
+          if (j < room) {
+            row[k] = sm.list[j];
+            a.refs[sm.list[j]] = 1;
           }
-          at += __popc(m);
+          ++j;
+        }
+      }
+      for (unsigned m = __ballot_sync(full, n > 0 && len > kShort); m; m &= m - 1) {
+        const int who = __ffs(m) - 1;
+        int32_t* row = a.block_table + static_cast<size_t>(__shfl_sync(full, b, who)) * a.max_pages;
+        const int from = __shfl_sync(full, s.first, who), last = __shfl_sync(full, s.last, who);
+        int j0 = __shfl_sync(full, at, who);
+        for (int k0 = from; k0 < last; k0 += 32) {
+          const int k = k0 + lane;
+          const bool none = k < last && row[k] == -1;
+          const unsigned w = __ballot_sync(full, none);
+          const int j = j0 + __popc(w & ((1u << lane) - 1u));
+          if (none && j < room) {
+            row[k] = sm.list[j];
+            a.refs[sm.list[j]] = 1;
+          }
+          j0 += __popc(w);
         }
       }
       before += turn;
+      if (a.Bt <= kPlanThreads) break;
     }
   }
 }
@@ -283,6 +329,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) fork_plan_kernel(const __grid
   __syncthreads();
   pdl_wait();
   pdl_launch_next();
+  const uint32_t first = step_bits(a.refs, a.num_pages, 0);
   auto inside = [&](int b) { return b >= 0 && b < a.Bt; };
   for (int i = tid; i < a.n; i += kPlanThreads) {
     const int s = a.src[i], d = a.dst[i];
@@ -312,14 +359,20 @@ __global__ void __launch_bounds__(kPlanThreads, 1) fork_plan_kernel(const __grid
     }
     return pg;
   };
-  int total = 0;
+  // (of the first round a thread keeps what it found)
+  int total = 0, mine = -2, mine_at = 0;
   for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
+    const int pg = i0 + tid < a.n ? partial(i0 + tid) : -2;
     int turn;
-    block_inclusive(sm.sum, i0 + tid < a.n && partial(i0 + tid) >= 0, turn);
+    const int at = total + block_inclusive(sm.sum, pg >= 0, turn) - 1;
+    if (i0 == 0) {
+      mine = pg;
+      mine_at = at;
+    }
     total += turn;
   }
   if (err) raise_error(a.err_word, err);
-  const int have = total ? find_free(sm, a.refs, a.num_pages, 0, total) : 0;
+  const int have = total ? find_free(sm, a.refs, a.num_pages, first, 0, total) : 0;
   const bool short_of = have < total;
   if (tid == 0) {
     if (short_of) raise_error(a.err_word, SIMSD_EW_POOL);
@@ -327,19 +380,23 @@ __global__ void __launch_bounds__(kPlanThreads, 1) fork_plan_kernel(const __grid
   }
   int before = 0, base = 0;
   for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
-    const int i = i0 + tid, pg = i < a.n ? partial(i) : -2;
-    int turn;
-    const int at = before + block_inclusive(sm.sum, pg >= 0, turn) - 1;
-    if (!short_of && before + turn > base + kList) {
-      // (a turn wants at most 1024 pages, the list holds 4096)
-      base = before;
-      find_free(sm, a.refs, a.num_pages, base, base + kList);
+    const int i = i0 + tid;
+    int pg = mine, at = mine_at, turn = 0;
+    if (a.n > kPlanThreads) {
+      pg = i < a.n ? partial(i) : -2;
+      at = before + block_inclusive(sm.sum, pg >= 0, turn) - 1;
+      if (!short_of && before + turn > base + kList) {
+        // (a turn wants at most 1024 pages, the list holds 4096)
+        base = before;
+        find_free(sm, a.refs, a.num_pages, first, base, base + kList);
+      }
     }
     if (i < a.n) {
       int st = pg == -2 || short_of ? -1 : 0;
       if (st == 0 && pg >= 0) {
         const int to = sm.list[at - base];
         moves_of(a)[at] = make_int2(pg, to);
+        if (a.n <= kPlanThreads) a.refs[to] = 1;
         st = to + 1;
       }
       pair_state(a)[i] = st;
@@ -348,7 +405,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) fork_plan_kernel(const __grid
   }
   // the pages are taken once nobody looks for free ones any more
   __syncthreads();
-  if (!short_of)
+  if (!short_of && a.n > kPlanThreads)
     for (int i = tid; i < total; i += kPlanThreads) a.refs[moves_of(a)[i].y] = 1;
 }
 
@@ -432,54 +489,54 @@ __device__ __forceinline__ int* where_to(const PagesArgs& a) { return reinterpre
 // The k-th live page above the count of live ones goes to the k-th free one
 // below it.
 __global__ void __launch_bounds__(kPlanThreads, 1) compact_plan_kernel(const __grid_constant__ PagesArgs a) {
-  __shared__ BlockSum sm;
+  __shared__ Free sm;
   pdl_wait();
   pdl_launch_next();
   const int tid = threadIdx.x;
+  // the free pages of a step, loaded again only where there are more steps
+  const uint32_t first = step_bits(a.refs, a.num_pages, 0);
+  auto bits = [&](long long s0) { return s0 == 0 ? first : step_bits(a.refs, a.num_pages, s0); };
   int free_pages = 0;
-  for (long long s0 = 0; s0 < a.num_pages; s0 += kStep) {
-    const long long p = s0 + static_cast<long long>(tid) * kPerThread;
-    if (p < a.num_pages) free_pages += __popc(free_bits(a.refs, static_cast<int>(p), a.num_pages));
-  }
+  for (long long s0 = 0; s0 < a.num_pages; s0 += kStep) free_pages += __popc(bits(s0));
   int total_free;
-  block_inclusive(sm, free_pages, total_free);
+  block_inclusive(sm.sum, free_pages, total_free);
   const int live = a.num_pages - total_free;
   int2* moves = moves_of(a);
   int* to = where_to(a);
+  // bit i: page p0 + i lies below the count of live ones
+  auto below = [&](long long p0) { return p0 + kPerThread <= live ? (1u << kPerThread) - 1u : p0 < live ? (1u << (live - p0)) - 1u : 0u; };
   // holes first (they all lie below the pages that fill them), then movers
   int holes = 0;
   for (long long s0 = 0; s0 < live; s0 += kStep) {
     const long long p0 = s0 + static_cast<long long>(tid) * kPerThread;
-    uint32_t m = p0 < live ? free_bits(a.refs, static_cast<int>(p0), live) : 0u;
+    uint32_t m = bits(s0) & below(p0);
     const int c = __popc(m);
-    int turn, at = holes + block_inclusive(sm, c, turn) - c;
-    while (m) {
-      moves[at++].y = static_cast<int>(p0) + __ffs(m) - 1;
-      m &= m - 1;
+    int turn, at = holes + block_inclusive(sm.sum, c, turn) - c;
+    for (; m; m &= m - 1, ++at) {
+      const int p = static_cast<int>(p0) + __ffs(m) - 1;
+      moves[at].y = p;
+      if (at < kList) sm.list[at] = p;
     }
     holes += turn;
   }
   __syncthreads();
   int moved = 0;
-  for (long long s0 = live / kPerThread * kPerThread; s0 < a.num_pages; s0 += kStep) {
+  for (long long s0 = live / kStep * static_cast<long long>(kStep); s0 < a.num_pages; s0 += kStep) {
     const long long p0 = s0 + static_cast<long long>(tid) * kPerThread;
     const int n = p0 < a.num_pages ? static_cast<int>(min(static_cast<long long>(kPerThread), a.num_pages - p0)) : 0;
-    uint32_t used = n > 0 ? ~free_bits(a.refs, static_cast<int>(p0), a.num_pages) & ((1u << n) - 1u) : 0u;
-    if (n > 0 && p0 < live) used &= ~((1u << (live - static_cast<int>(p0))) - 1u);
+    const uint32_t above = ~below(p0) & ((1u << n) - 1u), used = n > 0 ? ~bits(s0) & above : 0u;
     const int c = __popc(used);
-    int turn, at = moved + block_inclusive(sm, c, turn) - c;
-    for (int i = 0; i < n; ++i) {
-      const int p = static_cast<int>(p0) + i;
-      if (p < live) continue;
+    int turn, at = moved + block_inclusive(sm.sum, c, turn) - c;
+    for (uint32_t m = above; m; m &= m - 1) {
+      const int i = __ffs(m) - 1, p = static_cast<int>(p0) + i;
+      int dst = p;
       if (used >> i & 1u) {
-        const int hole = moves[at].y;
+        dst = at < kList ? sm.list[at] : moves[at].y;
         moves[at++].x = p;
-        to[p] = hole;
-        a.refs[hole] = a.refs[p];
+        a.refs[dst] = a.refs[p];
         a.refs[p] = 0;
-      } else {
-        to[p] = p;
       }
+      to[p] = dst;
     }
     moved += turn;
   }

@@ -37,15 +37,30 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxTokens = 64;  // tokens of a block
-constexpr int kInFlight = 2;    // steps of a warp whose loads are issued together
 
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const float4 u = reinterpret_cast<const float4*>(p)[0], v = reinterpret_cast<const float4*>(p)[1];
-  x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+// Eight components as they lie in memory.
+template <typename E>
+struct Raw8 {
+  uint4 v[sizeof(E) / 2];
+};
+template <typename E>
+__device__ __forceinline__ Raw8<E> load8(const E* p) {
+  Raw8<E> r;
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(sizeof(E) / 2); ++i) r.v[i] = reinterpret_cast<const uint4*>(p)[i];
+  return r;
 }
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+__device__ __forceinline__ void unpack8(const Raw8<float>& r, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    x[4 * i] = __uint_as_float(r.v[i].x);
+    x[4 * i + 1] = __uint_as_float(r.v[i].y);
+    x[4 * i + 2] = __uint_as_float(r.v[i].z);
+    x[4 * i + 3] = __uint_as_float(r.v[i].w);
+  }
+}
+__device__ __forceinline__ void unpack8(const Raw8<__nv_bfloat16>& r, float (&x)[8]) {
+  const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     x[2 * e] = __uint_as_float(w[e] << 16);
@@ -66,12 +81,70 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
   *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Warp item (token, group of heads): steps grp, grp + groups, ... of kRows
-// heads of the token (q's, then k's, then v's).
-template <typename E, int D>
-__global__ void __launch_bounds__(kThreads, 4) rope_q4_kernel(const __grid_constant__ RopeArgs a,
+// The ways in which pairs can lie: rotate-half with halves of whole vectors of
+// eight, interleaved with a rotated part of whole vectors, anything else.
+enum { kHalves = 0, kPairs = 1, kOther = 2 };
+
+// A lane's share of a rotation: components comp .. comp + 7 of a row.
+template <int kWay>
+struct Turner {
+  float cs[8], sn[8];  // x turned: x cs + partner sn (the partner's sign in sn)
+  int comp, lane, base, r, half, partner;
+  bool by_half;
+
+  __device__ __forceinline__ void set(const float2* angles) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int k = comp + e;
+      cs[e] = 1.f;
+      sn[e] = 0.f;
+      if (k < r) {
+        const float2 x = angles[by_half ? (k < half ? k : k - half) : k >> 1];
+        cs[e] = x.x;
+        sn[e] = (by_half ? k < half : (k & 1) == 0) ? -x.y : x.y;
+      }
+    }
+  }
+  __device__ __forceinline__ void turn(float (&x)[8]) const {
+    const unsigned full = 0xffffffffu;
+    float o[8];
+    if constexpr (kWay == kPairs) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = x[e ^ 1];
+    } else if constexpr (kWay == kHalves) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = __shfl_sync(full, x[e], partner);
+    } else if (!by_half) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = x[e ^ 1];
+    } else {
+      // the partner's place within its vector differs from the component's
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int p = comp + e < half ? comp + e + half : comp + e < r ? comp + e - half : comp + e;
+        o[e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float t = __shfl_sync(full, x[j], base + (p >> 3));
+          if (j == (p & 7)) o[e] = t;
+        }
+      }
+    }
+    if (kWay == kOther || comp < r) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (kWay != kOther || comp + e < r) x[e] = x[e] * cs[e] + o[e] * sn[e];
+    }
+  }
+};
+
+// Warp item (token, group of heads): of the token's q rows, then of its keys
+// and values, every groups-th step of kRows rows.
+template <typename E, int D, int kWay>
+__global__ void __launch_bounds__(kThreads, 3) rope_q4_kernel(const __grid_constant__ RopeArgs a,
                                                               const __grid_constant__ simsd_q4_cache c) {
   constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes of a row, rows of a warp
+  constexpr int kInFlight = 8 / sizeof(E);            // steps of q whose loads are issued together
   __shared__ Token toks[kMaxTokens];
   __shared__ float2 angles[kThreads / 32][D / 2];  // a warp's token: (cos, sin) of each pair
   pdl_wait();
@@ -89,119 +162,99 @@ __global__ void __launch_bounds__(kThreads, 4) rope_q4_kernel(const __grid_const
     if (lane == 0) toks[i] = t;
   }
   __syncthreads();
-  const int r = a.plan.rot_dim, half = r / 2;
-  const bool by_half = a.plan.layout == SIMSD_ROPE_HALF;
-  const int at = lane & (kLanes - 1), base = lane - at, comp = 8 * at, sub = lane / kLanes;
-  const int heads = a.Hq + 2 * a.Hkv, steps = (heads + kRows - 1) / kRows;
-  const float k_inv = 1.f / c.k_unit, v_inv = 1.f / c.v_unit;
-  // the lane of a component's partner (rotate-half, halves of whole vectors)
-  const bool whole = (half & 7) == 0;
-  const int partner = comp < half ? lane + half / 8 : comp < r ? lane - half / 8 : lane;
+  const int at = lane & (kLanes - 1), sub = lane / kLanes;
+  Turner<kWay> tr;
+  tr.r = a.plan.rot_dim;
+  tr.half = tr.r / 2;
+  tr.by_half = kWay == kHalves || (kWay == kOther && a.plan.layout == SIMSD_ROPE_HALF);
+  tr.lane = lane;
+  tr.base = lane - at;
+  tr.comp = 8 * at;
+  tr.partner = tr.comp < tr.half ? lane + tr.half / 8 : tr.comp < tr.r ? lane - tr.half / 8 : lane;
   for (int w = warp; w < a.tokens_block * a.groups; w += kThreads / 32) {
     const int i = w / a.groups, grp = w - i * a.groups, tok = tok0 + i;
     if (tok >= a.T) break;
     const Token tk = toks[i];
     if (tk.state == 0) continue;
+    const E* q = static_cast<const E*>(a.q) + static_cast<long long>(tok) * a.q_stride + tr.comp;
+    E* q_out = static_cast<E*>(a.q_out) + static_cast<long long>(tok) * a.q_out_stride + tr.comp;
+    if (tk.state == 2) {
+      const float zero[8] = {};
+      for (int h = grp * kRows + sub; h < a.Hq; h += a.groups * kRows) store8(q_out + h * D, zero);
+      continue;
+    }
     __syncwarp();
-    for (int pair = lane; pair < half; pair += 32) {
+    for (int pair = lane; pair < tr.half; pair += 32) {
       const unsigned long long turn = static_cast<unsigned long long>(static_cast<long long>(tk.pos)) * a.plan.turn[pair];
       float2 cs;
       sincospif(static_cast<float>(static_cast<int32_t>(turn >> 32)) * 0x1p-31f, &cs.y, &cs.x);
       angles[warp][pair] = make_float2(cs.x * a.plan.magnitude, cs.y * a.plan.magnitude);
     }
     __syncwarp();
-    // x turned: x cs + partner sn (the partner's sign in sn)
-    float cs[8], sn[8];
+    tr.set(angles[warp]);
+    for (int h0 = grp * kRows; h0 < a.Hq; h0 += a.groups * kRows * kInFlight) {
+      Raw8<E> raw[kInFlight];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int k = comp + e;
-      cs[e] = 1.f;
-      sn[e] = 0.f;
-      if (k < r) {
-        const float2 x = angles[warp][by_half ? (k < half ? k : k - half) : k >> 1];
-        cs[e] = x.x;
-        sn[e] = (by_half ? k < half : (k & 1) == 0) ? -x.y : x.y;
+      for (int j = 0; j < kInFlight; ++j) {
+        const int h = h0 + j * a.groups * kRows + sub;
+        if (h < a.Hq) raw[j] = load8(q + h * D);
+      }
+#pragma unroll
+      for (int j = 0; j < kInFlight; ++j) {
+        const int h = h0 + j * a.groups * kRows + sub;
+        if (h - sub >= a.Hq) break;  // (the warp's lanes agree)
+        float x[8];
+        unpack8(raw[j], x);
+        tr.turn(x);
+        if (h < a.Hq) store8(q_out + h * D, x);
       }
     }
-    const E* q = static_cast<const E*>(a.q) + static_cast<long long>(tok) * a.q_stride + comp;
-    const E* k = static_cast<const E*>(a.k) + static_cast<long long>(tok) * a.k_stride + comp;
-    const E* v = static_cast<const E*>(a.v) + static_cast<long long>(tok) * a.v_stride + comp;
-    E* q_out = static_cast<E*>(a.q_out) + static_cast<long long>(tok) * a.q_out_stride + comp;
-    auto turn = [&](float (&x)[8], bool turns) {
-      float o[8];
-      if (!by_half) {
+    if (tk.row < 0) continue;
+    const E* k = static_cast<const E*>(a.k) + static_cast<long long>(tok) * a.k_stride + tr.comp;
+    const E* v = static_cast<const E*>(a.v) + static_cast<long long>(tok) * a.v_stride + tr.comp;
+    auto put = [&](float (&x)[8], int h, float unit, void* codes, void* scales) {
+      if (unit != 1.f) {
+        const float inv = 1.f / unit;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = x[e ^ 1];
-      } else if (whole) {
+        for (int e = 0; e < 8; ++e) x[e] *= inv;
+      }
+      uint32_t top = 0;  // as bits: a NaN is above every number
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = __shfl_sync(full, x[e], partner);
-      } else {
-        // halves that are no whole vectors: the partner's place within its
-        // vector differs from the component's
+      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+      top = max(top, __shfl_xor_sync(full, top, 1));
+      const uint32_t sc = q4_scale(__uint_as_float(top));
+      const float s = q4_scale_value(sc), s_inv = __frcp_rn(s);
+      if (top >= 0x7f800000u) {
+        // infinities have no residual: the largest numbers go to 6 as well
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int p = comp + e < half ? comp + e + half : comp + e < r ? comp + e - half : comp + e;
-          o[e] = 0.f;
+        for (int e = 0; e < 8; ++e) x[e] = fminf(fmaxf(x[e], -3.4e38f), 3.4e38f);
+      }
+      uint32_t code = 0;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float t = __shfl_sync(full, x[j], base + (p >> 3));
-            if (j == (p & 7)) o[e] = t;
-          }
-        }
+      for (int e = 0; e < 8; ++e) {
+        const float y = x[e] * s_inv;
+        x[e] = fmaf(fmaf(-y, s, x[e]), s_inv, y);
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = turns && comp + e < r ? x[e] * cs[e] + o[e] * sn[e] : x[e];
+      for (int e = 0; e < 4; ++e) code |= q4_codes(x[2 * e], x[2 * e + 1]) << (8 * e);
+      if (h >= a.Hkv) return;
+      const long long row = tk.row + static_cast<long long>(h) * a.page_size;
+      static_cast<uint32_t*>(codes)[row * (D / 8) + at] = code;
+      if ((at & 1) == 0) static_cast<uint8_t*>(scales)[row * (D / kQ4Group) + (at >> 1)] = static_cast<uint8_t>(sc);
     };
-    for (int s0 = grp; s0 < steps; s0 += a.groups * kInFlight) {
-      float x[kInFlight][8];
-#pragma unroll
-      for (int j = 0; j < kInFlight; ++j) {
-        const int h = (s0 + j * a.groups) * kRows + sub;
-        if (h < heads) load8(h < a.Hq ? q + h * D : h < a.Hq + a.Hkv ? k + (h - a.Hq) * D : v + (h - a.Hq - a.Hkv) * D, x[j]);
+    for (int h0 = grp * kRows; h0 < a.Hkv; h0 += a.groups * kRows) {
+      const int h = h0 + sub;
+      Raw8<E> rk{}, rv{};
+      if (h < a.Hkv) {
+        rk = load8(k + h * D);
+        rv = load8(v + h * D);
       }
-#pragma unroll
-      for (int j = 0; j < kInFlight; ++j) {
-        const int h0 = (s0 + j * a.groups) * kRows, h = h0 + sub;
-        if (h0 >= heads) break;  // (the warp's lanes agree, here and below)
-        const bool is_v = h >= a.Hq + a.Hkv;
-        if (h0 < a.Hq + a.Hkv) turn(x[j], !is_v);
-        if (h < a.Hq) {
-          float y[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = tk.state == 2 ? 0.f : x[j][e];
-          store8(q_out + h * D, y);
-        }
-        if (h0 + kRows <= a.Hq) continue;  // (no key or value among them)
-        const float inv = is_v ? v_inv : k_inv;
-        uint32_t top = 0;  // as bits: a NaN is above every number
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[j][e] *= inv;
-          top = max(top, __float_as_uint(x[j][e]) & 0x7fffffffu);
-        }
-        top = max(top, __shfl_xor_sync(full, top, 1));
-        if (h < a.Hq || h >= heads || tk.row < 0) continue;
-        const uint32_t sc = q4_scale(__uint_as_float(top));
-        const float s = q4_scale_value(sc), s_inv = __frcp_rn(s);
-        if (top >= 0x7f800000u) {
-          // infinities have no residual: the largest numbers go to 6 as well
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[j][e] = fminf(fmaxf(x[j][e], -3.4e38f), 3.4e38f);
-        }
-        uint32_t code = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float y = x[j][e] * s_inv;
-          x[j][e] = fmaf(fmaf(-y, s, x[j][e]), s_inv, y);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) code |= q4_codes(x[j][2 * e], x[j][2 * e + 1]) << (8 * e);
-        const int hk = is_v ? h - a.Hq - a.Hkv : h - a.Hq;
-        const long long row = tk.row + static_cast<long long>(hk) * a.page_size;
-        reinterpret_cast<uint32_t*>(is_v ? c.v_codes : c.k_codes)[row * (D / 8) + at] = code;
-        if ((at & 1) == 0)
-          static_cast<uint8_t*>(is_v ? c.v_scales : c.k_scales)[row * (D / kQ4Group) + (at >> 1)] = static_cast<uint8_t>(sc);
-      }
+      float x[8];
+      unpack8(rk, x);
+      tr.turn(x);
+      put(x, h, c.k_unit, c.k_codes, c.k_scales);
+      unpack8(rv, x);
+      put(x, h, c.v_unit, c.v_codes, c.v_scales);
     }
   }
 }
@@ -209,7 +262,7 @@ __global__ void __launch_bounds__(kThreads, 4) rope_q4_kernel(const __grid_const
 template <typename E, int D>
 cudaError_t launch_d(RopeArgs a, const simsd_q4_cache& c, int num_sms, cudaStream_t stream) {
   constexpr int kRows = 32 / (D / 8), kWarps = kThreads / 32;
-  const int steps = (a.Hq + 2 * a.Hkv + kRows - 1) / kRows;
+  const int steps = (std::max(a.Hq, a.Hkv) + kRows - 1) / kRows;
   // two full waves of warps where there are that many steps, more steps to a
   // warp (fewer angles formed) beyond
   const long long want = 2ll * 64 * num_sms;
@@ -219,7 +272,11 @@ cudaError_t launch_d(RopeArgs a, const simsd_q4_cache& c, int num_sms, cudaStrea
   const int per_block = std::max((kWarps + a.groups - 1) / a.groups, (a.T + 8 * num_sms - 1) / (8 * num_sms));
   a.tokens_block = std::min(kMaxTokens, a.groups == 1 ? (per_block + kWarps - 1) / kWarps * kWarps : per_block);
   const unsigned blocks = static_cast<unsigned>((a.T + a.tokens_block - 1) / a.tokens_block);
-  return launch_overlapped(rope_q4_kernel<E, D>, dim3(blocks), dim3(kThreads), 0, stream, 1u, a, c);
+  const int r = a.plan.rot_dim;
+  auto* kern = a.plan.layout == SIMSD_ROPE_HALF && r % 16 == 0  ? rope_q4_kernel<E, D, kHalves>
+               : a.plan.layout != SIMSD_ROPE_HALF && r % 8 == 0 ? rope_q4_kernel<E, D, kPairs>
+                                                                : rope_q4_kernel<E, D, kOther>;
+  return launch_overlapped(kern, dim3(blocks), dim3(kThreads), 0, stream, 1u, a, c);
 }
 
 // ------------------------------------------------------------------ expand
