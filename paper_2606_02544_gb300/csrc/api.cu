@@ -859,7 +859,9 @@ size_t simsd_chunk_q4_workspace_bytes(int dtype, int T, int Bt, int Hq, int Hkv,
     return 0;
   DeviceInfo info;
   if (device_info(&info) != SIMSD_OK) return 0;
-  if (simsd::chunk_q4_few(dtype, T, Bt, Hq, Hkv)) return simsd::chunk_q4_workspace_bytes(T, Bt, Hq, Hkv, d, info.num_sms);
+  const simsd::Q4Way way = simsd::chunk_q4_way(dtype, T, Bt, Hq, Hkv);
+  if (way == simsd::Q4Way::kCodes) return simsd::chunk_q4_workspace_bytes(T, Bt, Hq, Hkv, d, info.num_sms);
+  if (way == simsd::Q4Way::kTiles) return simsd::chunk_q4_tc_workspace_bytes(d, info.num_sms);
   return 2 * q4_image_bytes(dtype, num_pages, Hkv, page_size, d) +
          simsd_chunk_workspace_bytes(dtype, T, Bt, Hq, Hkv, d, max_pages, page_size);
 }
@@ -905,13 +907,21 @@ int simsd_chunk_attention_q4(int dtype, const void* q, int64_t q_stride, const i
   a.window = window;
   a.sinks = window > 0 ? sinks : 0;
   a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt(static_cast<float>(d));
-  if (simsd::chunk_q4_few(dtype, T, Bt, Hq, Hkv)) {
-    // units of at least Hq / Hkv rows, key tiles of 128 rows, counted in 32 bits
+  const simsd::Q4Way way = simsd::chunk_q4_way(dtype, T, Bt, Hq, Hkv);
+  if (way != simsd::Q4Way::kImage) {
+    // units of at least one token, key tiles of 128 rows, counted in 32 bits
     const long long max_keys = static_cast<long long>(max_pages) * page_size;
     if ((static_cast<long long>(T) * Hkv + static_cast<long long>(Bt) * Hkv + 1) * (max_keys / 128 + 1) >= (1ll << 31))
       return unsupported("too many key tiles in one call");
     a.workspace = workspace;
-    cudaError_t e = simsd::launch_chunk_attention_q4(a, *cache, info.num_sms, as_stream(stream));
+    cudaError_t e;
+    if (way == simsd::Q4Way::kCodes) {
+      e = simsd::launch_chunk_attention_q4(a, *cache, info.num_sms, as_stream(stream));
+    } else {
+      simsd::EncodeTiledFn enc = encoder();
+      if (!enc) return cuda_fail(cudaErrorNotSupported, "cuTensorMapEncodeTiled entry point");
+      e = simsd::launch_chunk_attention_q4_tc(a, *cache, info.num_sms, enc, as_stream(stream));
+    }
     return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "chunk_attention_q4 launch");
   }
   const size_t image = q4_image_bytes(dtype, num_pages, Hkv, page_size, d);

@@ -36,16 +36,14 @@
 #include <algorithm>
 #include <mutex>
 
-#include "chunk_walk.cuh"
 #include "common.cuh"
 #include "kernels.h"
-#include "ptx.cuh"
-#include "q4.cuh"
+#include "q4_tiles.cuh"
 
 namespace simsd {
 namespace {
 
-constexpr int kTile = 128;  // keys per tile
+constexpr int kTile = kQ4Tile;
 constexpr int kMaxSeqs = 8192;  // their tile counts fit the ring
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr float kNoReference = -1.0e30f;   // of rows that have seen no key
@@ -58,25 +56,6 @@ struct Q4Params {
   int sub;            // keys per copy: a page, or part of one
   float scale_log2;   // scores to log2 units, the keys' unit included
   int one;            // 1
-};
-
-// What the walking warp says of a tile, beside its codes.
-enum : int {
-  kFirst = 1,       // of a piece
-  kLast = 2,        // of a piece
-  kLastPiece = 4,   // and that the CTA's last one
-  kFull = 8,        // every row sees every key
-  kEmpty = 16,      // no row sees any key
-  kEnd = 32,        // no tile: the end of the run
-  kPart = 64,       // the piece leaves partial results,
-  kSlot1 = 128,     // those of slot 1
-  kBad = 256        // a page id of the piece (so far) is out of range
-};
-struct alignas(16) TileInfo {
-  int flags, key0, ntok, tok0;
-  int kvh, i0, n, C;
-  int lo, se, w0, hi;  // keys that any row of the unit sees
-  int ks, pad0, pad1, pad2;
 };
 
 // NB blocks of 8 query rows a warp, RG groups of rows.  Up to 8 rows take few
@@ -95,12 +74,6 @@ struct Cfg {
   static constexpr int kStages = (NB == 1 ? 3 : 7) * (128 / D);
 };
 
-template <int D>
-struct alignas(128) Stage {
-  uint8_t kc[kTile * D / 2], vc[kTile * D / 2];
-  uint8_t ks[kTile * D / kQ4Group], vs[kTile * D / kQ4Group];
-};
-
 template <int D, int NB, int RG>
 struct SmemQ4 {
   using C = Cfg<D, NB, RG>;
@@ -114,11 +87,6 @@ struct SmemQ4 {
   int abort_flag;
 };
 
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-               "l"(src), "r"(bytes), "r"(bar)
-               : "memory");
-}
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                          uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -132,17 +100,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ float exp2_approx(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // Partial results: O (without the values' unit) [entries][RB][D], then (m, l)
 // [entries][RB], entry cta * 2 + slot, m in log2 units, l = -1 where a page id
 // of the piece is out of range; then one Record per run boundary.
@@ -236,98 +193,47 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
 
   if (warp == kWarps) {
     // -------------------------------------------------------- walk and copies
-    Walk<SINKS, kTile> k;
-    k.begin(p.a, p.ub, p.ctas, start, seq, total);
-    typename Walk<SINKS, kTile>::Step piece;
-    const int P = p.a.page_size, sub = p.sub;
+    TileWalk<D, SINKS> tw;
+    tw.ub = p.ub;
+    tw.sub = p.sub;
+    tw.k.begin(p.a, p.ub, p.ctas, start, seq, total);
     uint32_t it = 0, units = 0;  // tiles passed on, of them with a Q
     bool ok = true;
     auto slot_free = [&]() {
       if (it >= kStages) ok = mbar_wait_warp(smem_u32(&sm.bar_free[it % kStages]), ((it / kStages) - 1) & 1, abort_flag);
       return ok;
     };
-    while (ok && k.peek(p.a, p.ub, piece)) {
-      TileInfo u;
-      u.i0 = k.w.j * p.ub;
-      u.tok0 = k.s.start + u.i0;
-      u.ntok = min(p.ub, k.s.C - u.i0);
-      u.kvh = k.w.kvh;
-      u.lo = piece.keys.lo;
-      u.se = piece.keys.se;
-      u.w0 = piece.keys.w0;
-      u.hi = piece.keys.hi;
-      u.n = k.s.n;
-      u.C = k.s.C;
-      u.ks = k.s.ks;
-      const bool empty = piece.tiles == 0;
-      int flags = (empty ? kEmpty : 0) | (piece.take < piece.weight ? kPart : 0) | (piece.slot ? kSlot1 : 0);
-      // rows that every token of the unit sees
-      const int all_lo = empty ? 0 : key_lo(p.a, k.s, u.i0 + u.ntok - 1), all_hi = empty ? 0 : key_hi(p.a, k.s, u.i0);
-      const int all_se = SINKS && !empty ? sink_end(p.a, k.s, all_hi) : 0;
-      const int skip = tiles_skipped<SINKS, kTile>(piece.keys), tse = (u.se + kTile - 1) / kTile;
-      const int32_t* bt = p.a.block_table + static_cast<size_t>(k.w.b) * p.a.max_pages;
-      const int t0 = u.lo / kTile + k.w.t;
-      int win_base = -(1 << 30), win = -1;  // lane i holds the page id of page win_base + i
-      for (int i = 0; i < piece.take; ++i) {
+    while (ok && tw.next_piece(p.a)) {
+      for (int i = 0; i < tw.piece.take; ++i) {
         const uint32_t st = it % kStages;
-        const int t = t0 + i;
-        u.key0 = (t + (SINKS && t >= tse ? skip : 0)) * kTile;
-        const bool all = !empty && ((u.key0 >= all_lo && u.key0 + kTile <= all_hi) ||
-                                    (SINKS && u.key0 >= u.ks && u.key0 + kTile <= all_se));
-        u.flags = (i == 0 ? kFirst : 0) | (i + 1 == piece.take ? kLast | (piece.last ? kLastPiece : 0) : 0) | (all ? kFull : 0);
-        // copy s of the tile is lane s's
-        const int nsub = kTile / sub, key = u.key0 + min(lane, nsub - 1) * sub, pi = key / P;
-        const int pi0 = u.key0 / P, pi1 = (u.key0 + kTile - 1) / P;
-        if (pi0 < win_base || pi1 >= win_base + 32) {
-          win_base = pi0;
-          win = win_base + lane < p.a.max_pages ? bt[win_base + lane] : -1;
-        }
-        const int pg = __shfl_sync(full, win, (pi - win_base) & 31);
-        bool load = !empty && lane < nsub && key + sub > u.lo && key < u.hi && (!SINKS || key < u.se || key + sub > u.w0);
-        const bool wrong = load && (pg < 0 || pg >= p.a.num_pages);
-        load = load && !wrong;
-        if (__any_sync(full, wrong)) {
-          if (lane == 0) raise_error(p.a.err_word, SIMSD_EW_PAGE);
-          flags |= kBad;
-        }
+        tw.tile(p.a, i);
         if (!slot_free()) break;
-        u.flags |= flags;
-        const bool with_q = i == 0 && !empty;
-        const uint32_t qb = units & 1;
+        const bool with_q = i == 0 && !(tw.flags & kEmpty);
+        const uint32_t qb = units & 1, q_bytes = static_cast<uint32_t>(p.g * D * 2);
         if (with_q && units >= 2) {
           ok = mbar_wait_warp(smem_u32(&sm.bar_qfree[qb]), ((units >> 1) - 1) & 1, abort_flag);
           if (!ok) break;
         }
         const uint32_t bar = smem_u32(&sm.bar_full[st]);
-        const uint32_t code_bytes = static_cast<uint32_t>(sub * (D / 2)), scale_bytes = static_cast<uint32_t>(sub * (D / kQ4Group));
-        const uint32_t q_bytes = static_cast<uint32_t>(p.g * D * 2);
-        const uint32_t bytes = __popc(__ballot_sync(full, load)) * 2u * (code_bytes + scale_bytes) + (with_q ? u.ntok * q_bytes : 0u);
+        const uint32_t bytes = tw.bytes() + (with_q ? tw.u.ntok * q_bytes : 0u);
         if (lane == 0) {
-          sm.info[st] = u;
+          sm.info[st] = tw.u;
           mbar_arrive_expect_tx(bar, bytes);
         }
         __syncwarp();
-        if (load) {
-          Stage<D>& s = sm.ring[st];
-          const size_t row = (static_cast<size_t>(pg) * p.a.Hkv + u.kvh) * P + (key - pi * P);
-          const int at = lane * sub;
-          bulk_load(smem_u32(&s.kc[at * (D / 2)]), static_cast<const uint8_t*>(p.c.k_codes) + row * (D / 2), code_bytes, bar);
-          bulk_load(smem_u32(&s.ks[at * (D / kQ4Group)]), static_cast<const uint8_t*>(p.c.k_scales) + row * (D / kQ4Group), scale_bytes, bar);
-          bulk_load(smem_u32(&s.vc[at * (D / 2)]), static_cast<const uint8_t*>(p.c.v_codes) + row * (D / 2), code_bytes, bar);
-          bulk_load(smem_u32(&s.vs[at * (D / kQ4Group)]), static_cast<const uint8_t*>(p.c.v_scales) + row * (D / kQ4Group), scale_bytes, bar);
-        }
+        tw.copy(p.c, sm.ring[st], bar);
         if (with_q) {
-          for (int x = lane; x < u.ntok; x += 32)
+          for (int x = lane; x < tw.u.ntok; x += 32)
             bulk_load(smem_u32(&sm.q[qb][x * p.g * D]),
-                      static_cast<const __nv_bfloat16*>(p.a.q) + static_cast<long long>(u.tok0 + x) * p.a.q_stride +
-                          static_cast<long long>(u.kvh) * p.g * D,
+                      static_cast<const __nv_bfloat16*>(p.a.q) + static_cast<long long>(tw.u.tok0 + x) * p.a.q_stride +
+                          static_cast<long long>(tw.u.kvh) * p.g * D,
                       q_bytes, bar);
           ++units;
         }
         ++it;
       }
       if (!ok) break;
-      k.pop(p.a, p.ub, piece);
+      tw.k.pop(p.a, p.ub, tw.piece);
     }
     if (ok && slot_free()) {
       // the end of the run
@@ -340,7 +246,7 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
       ++it;
     }
     if (!ok) give_up();
-    if (lane == 0 && blockIdx.x > 0) records<D, RB>(p)[blockIdx.x] = boundary_record<SINKS, kTile>(k, p.a, p.ub);
+    if (lane == 0 && blockIdx.x > 0) records<D, RB>(p)[blockIdx.x] = boundary_record<SINKS, kTile>(tw.k, p.a, p.ub);
     // every copy must have landed before the CTA may exit
     if (lane == 0)
       for (uint32_t j = it > kStages ? it - kStages : 0; j < it; ++j)
@@ -399,8 +305,8 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
           }
           top = max(top, __shfl_xor_sync(full, top, 1));
           top = max(top, __shfl_xor_sync(full, top, 2));
-          const uint32_t ex = min(max(top >> 7, 1u), 253u);  // 2^(ex - 127) <= the largest < 2^(ex - 126)
-          const float down = __uint_as_float((254u - ex) << 23), up = __uint_as_float(ex << 23);
+          float down, up;
+          q_powers(top, down, up);
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) {
             const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
@@ -494,7 +400,7 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
               mx = fmaxf(mx, __shfl_xor_sync(full, mx, 4));
               mx = fmaxf(mx, __shfl_xor_sync(full, mx, 8));
               mx = fmaxf(mx, __shfl_xor_sync(full, mx, 16));
-              const float f = exp2_approx(m[nb][e] - mx);
+              const float f = fast_exp2(m[nb][e] - mx);
               m[nb][e] = mx;
               l[nb][e] *= f;
 #pragma unroll
@@ -515,7 +421,7 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) pr[u][nb][e] = exp2_approx(pr[u][nb][e]);
+            for (int e = 0; e < 4; ++e) pr[u][nb][e] = fast_exp2(pr[u][nb][e]);
             l[nb][0] += pr[u][nb][0] + pr[u][nb][2];
             l[nb][1] += pr[u][nb][1] + pr[u][nb][3];
             pb[u][nb][0] = transpose8(pack_f16x2(pr[u][nb][0], pr[u][nb][1]));
@@ -599,9 +505,9 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
 #pragma unroll
         for (int w = 0; w < C::kKeyGroups; ++w) {
           const float2 x = sm.ml[w * RG + rg][8 * nb + 2 * t + e];
-          L = fmaf(exp2_approx(x.x - M), x.y, L);
+          L = fmaf(fast_exp2(x.x - M), x.y, L);
         }
-        const float f = exp2_approx(m[nb][e] - M);
+        const float f = fast_exp2(m[nb][e] - M);
         if (kg == 0 && g == 0) sm.fin[(rg * NB + nb) * 8 + 2 * t + e] = make_float2(M, L);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
@@ -763,8 +669,14 @@ cudaError_t launch_d(const Q4Params& p, int num_sms, cudaStream_t stream) {
 
 }  // namespace
 
-bool chunk_q4_few(int dtype, int T, int Bt, int Hq, int Hkv) {
-  return dtype == SIMSD_BF16 && Hq / Hkv <= 64 && Bt <= kMaxSeqs && static_cast<long long>(T) * Hq <= 64ll * Bt * Hkv;
+constexpr int kCodesRows = 16;   // query rows a sequence and KV head
+constexpr int kTilesRows = 256;
+Q4Way chunk_q4_way(int dtype, int T, int Bt, int Hq, int Hkv) {
+  if (dtype != SIMSD_BF16 || Bt > kChunkMaxSeqs) return Q4Way::kImage;
+  const int g = Hq / Hkv;
+  const long long rows = static_cast<long long>(T) * g;
+  if (g <= kCodesRows && rows <= static_cast<long long>(kCodesRows) * Bt && Bt <= kMaxSeqs) return Q4Way::kCodes;
+  return g <= 128 && rows <= static_cast<long long>(kTilesRows) * Bt ? Q4Way::kTiles : Q4Way::kImage;
 }
 
 size_t chunk_q4_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, int num_sms) {

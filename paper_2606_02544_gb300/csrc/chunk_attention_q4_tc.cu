@@ -1,0 +1,752 @@
+// chunk_attention_q4_tc.cu -- attention of short chunks over a paged cache in
+// 4 bits on the sm_103a tensor cores (Sec. 3.3: the prefix is read from a KV
+// cache).
+//
+// Mathematics.  As in chunk_attention_q4.cu: keys and values are exact in
+// fp16, q is brought to fp16 by a power of two a row, probabilities are
+// rounded to fp16, S and O are accumulated in fp32; the softmax is that of
+// chunk_attention_tc.cu.
+//
+// A unit is (KV head, sequence, up to 128 query rows), a tile 128 keys.  The
+// codes and scales of a tile (18 KB) come by bulk copies; eight warps turn
+// them into the fp16 tiles of K and V, each once, in the layout that the
+// matrix instructions read (rows of 128 bytes, swizzled), and set the rows of
+// V that no token sees to zero.  S has two buffers in tensor memory, so that
+// S of the next tile is formed under the softmax of this one.  The walk of
+// chunk_walk.cuh; units cut by the end of a run are merged by a second launch.
+//
+// Warp roles (512 threads): warps 0-3 softmax (thread i owns query row i =
+// TMEM lane i, and turns its row of Q into fp16 in place); warps 4-11 K and V;
+// warp 12 walks the run and issues all copies; warp 13 the MMAs, in the order
+// S(0) S(1) PV(0) S(2) PV(1) ... of a unit.
+// TMEM (512 columns): S [0,128) and [128,256), O [256, 256 + D); P (fp16)
+// overwrites the first 64 columns of its S.
+//
+// Every mbarrier wait is bounded; after one expires the CTA raises
+// SIMSD_EW_TIMEOUT, every role leaves its loops, drains its copies and MMAs
+// and frees TMEM.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "ptx_chunk.cuh"
+#include "q4_tiles.cuh"
+
+namespace simsd {
+namespace {
+
+constexpr int kTile = kQ4Tile;
+constexpr int kRows = 128;  // query rows of a unit (MMA M)
+constexpr int kThreads = 512;
+constexpr int kWarpConvert = 4, kConvertWarps = 8, kWarpWalk = 12, kWarpMma = 13;
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kColO = 256;
+constexpr int kHalfBytes = kTile * 128;  // 128 rows x 64 fp16
+constexpr int kInfos = 8;                // tiles that the walk is ahead of the last reader
+constexpr int kInfoReaders = 4 + kConvertWarps + 1;
+constexpr float kRescaleThreshold = 8.0f;  // log2 units
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct Q4TcParams {
+  ChunkArgs a;
+  simsd_q4_cache c;
+  int g, tb;          // heads per KV head, tokens of a unit
+  int ctas, sub;      // grid size; keys per copy
+  float scale_log2;   // scores to log2 units, the keys' unit included
+};
+
+template <int D>
+struct alignas(1024) SmemQ4Tc {
+  static constexpr int kHalves = D / 64;
+  static constexpr int kTileBytes = kHalves * kHalfBytes;
+  static constexpr int kSlots = D == 128 ? 2 : 4;   // of K, and of V
+  static constexpr int kStages = D == 128 ? 3 : 6;  // of codes
+  uint8_t k[kSlots][kTileBytes], v[kSlots][kTileBytes];
+  uint8_t q[kTileBytes];
+  Stage<D> ring[kStages];
+  TileInfo info[kInfos];
+  uint64_t bar_code[kStages], bar_codefree[kStages];
+  uint64_t bar_k[kSlots], bar_kfree[kSlots], bar_v[kSlots], bar_vfree[kSlots];
+  uint64_t bar_info[kInfos], bar_infofree[kInfos];
+  uint64_t bar_qraw, bar_q, bar_qfree;
+  uint64_t bar_s[2], bar_p[2][2], bar_pv, bar_ofree, bar_drain;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+template <int D>
+constexpr size_t smem_bytes() {
+  return sizeof(SmemQ4Tc<D>) + 1024;
+}
+static_assert(smem_bytes<128>() <= 232448 && smem_bytes<64>() <= 232448, "one CTA per SM");
+static_assert(2 * SmemQ4Tc<64>::kSlots * SmemQ4Tc<64>::kTileBytes >= kChunkMaxSeqs * 4 &&
+                  2 * SmemQ4Tc<128>::kSlots * SmemQ4Tc<128>::kTileBytes >= kChunkMaxSeqs * 4,
+              "the tiles of K and V hold the tile counts of all sequences while runs are planned");
+
+// kind::f16 with fp16 A and B, fp32 accumulator
+constexpr uint32_t idesc_f16_f32(int M, int N, int b_mn_major) {
+  return (1u << 4) | (static_cast<uint32_t>(b_mn_major) << 16) | (static_cast<uint32_t>(N >> 3) << 17) |
+         (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+// Partial results: O (without the values' unit) as [ctas * 2 entries][D / 4]
+// [128 rows] vectors of four, (m, l) [entries][128], entry cta * 2 + slot, m
+// in log2 units, l = -1 where a page id of the piece is out of range; then one
+// Record per run boundary.
+template <int D>
+__device__ __forceinline__ float4* partial_o(const Q4TcParams& p, int entry, int col4, int row) {
+  return static_cast<float4*>(p.a.workspace) + (static_cast<size_t>(entry) * (D / 4) + col4) * kRows + row;
+}
+template <int D>
+__device__ __forceinline__ float2* partial_ml(const Q4TcParams& p, int entry, int row) {
+  return reinterpret_cast<float2*>(partial_o<D>(p, 2 * p.ctas, 0, 0)) + static_cast<size_t>(entry) * kRows + row;
+}
+template <int D>
+__device__ __forceinline__ Record* records(const Q4TcParams& p) {
+  return reinterpret_cast<Record*>(partial_ml<D>(p, 2 * p.ctas, 0));
+}
+
+// A piece's fields that the softmax keeps while its tiles last.
+struct Unit {
+  int ntok, tok0, kvh, i0, n, C, ks;
+};
+
+template <int D, bool SINKS>
+__global__ void __launch_bounds__(kThreads, 1)
+    chunk_q4_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ Q4TcParams p) {
+  using Smem = SmemQ4Tc<D>;
+  constexpr int kHalves = Smem::kHalves, kSlots = Smem::kSlots, kStages = Smem::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  volatile int* abort_flag = &sm.abort_flag;
+  const unsigned full = 0xffffffffu;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    sm.abort_flag = 0;
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(smem_u32(&sm.bar_code[s]), 1);
+      mbar_init(smem_u32(&sm.bar_codefree[s]), kConvertWarps);
+    }
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(smem_u32(&sm.bar_k[s]), kConvertWarps);
+      mbar_init(smem_u32(&sm.bar_v[s]), kConvertWarps);
+      mbar_init(smem_u32(&sm.bar_kfree[s]), 1);
+      mbar_init(smem_u32(&sm.bar_vfree[s]), 1);
+    }
+    for (int s = 0; s < kInfos; ++s) {
+      mbar_init(smem_u32(&sm.bar_info[s]), 1);
+      mbar_init(smem_u32(&sm.bar_infofree[s]), kInfoReaders);
+    }
+    mbar_init(smem_u32(&sm.bar_qraw), 1);
+    mbar_init(smem_u32(&sm.bar_q), 4);
+    mbar_init(smem_u32(&sm.bar_qfree), 1);
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(smem_u32(&sm.bar_s[x]), 1);
+      mbar_init(smem_u32(&sm.bar_p[x][0]), 4);
+      mbar_init(smem_u32(&sm.bar_p[x][1]), 4);
+    }
+    mbar_init(smem_u32(&sm.bar_pv), 1);
+    mbar_init(smem_u32(&sm.bar_ofree), 4);
+    mbar_init(smem_u32(&sm.bar_drain), 1);
+    fence_mbar_init();
+  }
+  if (warp == kWarpMma) {
+    tmem_alloc(smem_u32(&sm.tmem_base), kTmemCols);
+    tmem_relinquish();
+  }
+  if (warp == kWarpWalk && lane == 0) tma_prefetch_desc(&tm_q);
+  pdl_wait();
+  int32_t* tiles = reinterpret_cast<int32_t*>(sm.k[0]);
+  plan_tiles<SINKS, kTile, kThreads>(p.a, p.tb, tiles);
+  Place start{0, 0, 0, 0};
+  int total = 0;
+  ChunkSeq seq{};
+  if (warp == kWarpWalk) start = plan_start<SINKS, kTile>(p.a, p.tb, p.ctas, tiles, total, seq);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem_base;
+  auto give_up = [&]() {
+    if (lane == 0) {
+      raise_error(p.a.err_word, SIMSD_EW_TIMEOUT);
+      *abort_flag = 1;
+    }
+  };
+  auto wait = [&](uint64_t& bar, uint32_t parity) { return mbar_wait_warp(smem_u32(&bar), parity, abort_flag); };
+  auto arrive = [&](uint64_t& bar) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&bar));
+  };
+  bool ok = true;
+
+  // register split: 128 x 208 + 256 x 96 + 128 x 88 = 62,464 of the launch's 512 x 128
+  if (warp >= kWarpWalk) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == kWarpWalk) {
+      // ------------------------------------------------------ walk and copies
+      TileWalk<D, SINKS> tw;
+      tw.ub = p.tb;
+      tw.sub = p.sub;
+      tw.k.begin(p.a, p.tb, p.ctas, start, seq, total);
+      uint32_t it = 0, codes = 0, units = 0;  // messages; tiles with copies; Q tiles
+      auto say = [&](const TileInfo& u) {
+        if (it >= kInfos) ok = wait(sm.bar_infofree[it % kInfos], ((it / kInfos) - 1) & 1);
+        if (!ok) return;
+        if (lane == 0) {
+          sm.info[it % kInfos] = u;
+          mbar_arrive(smem_u32(&sm.bar_info[it % kInfos]));
+        }
+        ++it;
+      };
+      while (ok && tw.next_piece(p.a)) {
+        const bool empty = tw.flags & kEmpty;
+        for (int i = 0; ok && i < tw.piece.take; ++i) {
+          tw.tile(p.a, i);
+          if (!empty) {
+            const uint32_t st = codes % kStages;
+            if (codes >= kStages) ok = wait(sm.bar_codefree[st], ((codes / kStages) - 1) & 1);
+            if (!ok) break;
+            const uint32_t bar = smem_u32(&sm.bar_code[st]), bytes = tw.bytes();
+            if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
+            __syncwarp();
+            tw.copy(p.c, sm.ring[st], bar);
+            ++codes;
+            if (i == 0) {
+              // Q, once the unit before has no use for its own any more
+              if (units > 0) ok = wait(sm.bar_qfree, (units - 1) & 1);
+              if (!ok) break;
+              if (lane == 0) {
+                const uint32_t bq = smem_u32(&sm.bar_qraw);
+                mbar_arrive_expect_tx(bq, static_cast<uint32_t>(kHalves * p.g * p.tb) * 128u);
+#pragma unroll
+                for (int hf = 0; hf < kHalves; ++hf)
+                  tma_load_3d(smem_u32(sm.q) + hf * kHalfBytes, &tm_q, bq, 64 * hf, tw.u.kvh * p.g, tw.u.tok0);
+              }
+              ++units;
+            }
+          }
+          say(tw.u);
+        }
+        if (!ok) break;
+        tw.k.pop(p.a, p.tb, tw.piece);
+      }
+      if (ok) {
+        TileInfo u{};
+        u.flags = kEnd;
+        say(u);
+      }
+      if (!ok) give_up();
+      if (lane == 0 && blockIdx.x > 0) records<D>(p)[blockIdx.x] = boundary_record<SINKS, kTile>(tw.k, p.a, p.tb);
+      // every copy must have landed before the CTA may exit
+      if (lane == 0) {
+        for (uint32_t j = codes > kStages ? codes - kStages : 0; j < codes; ++j)
+          mbar_wait(smem_u32(&sm.bar_code[j % kStages]), (j / kStages) & 1, nullptr);
+        if (units > 0) mbar_wait(smem_u32(&sm.bar_qraw), (units - 1) & 1, nullptr);
+      }
+      __syncwarp();
+    } else if (warp == kWarpMma) {
+      // ----------------------------------------------------------------- MMAs
+      constexpr uint32_t kIdescQK = idesc_f16_f32(kRows, kTile, 0);
+      constexpr uint32_t kIdescPV = idesc_f16_f32(kRows, D, 1);
+      const uint64_t dq = sdesc_sw128(smem_u32(sm.q), 16, 1024), dk = sdesc_sw128(smem_u32(sm.k[0]), 16, 1024),
+                     dv = sdesc_sw128(smem_u32(sm.v[0]), kHalfBytes, 1024);
+      const uint32_t q_lo = static_cast<uint32_t>(dq), k_lo = static_cast<uint32_t>(dk), v_lo = static_cast<uint32_t>(dv);
+      const uint32_t k_hi = static_cast<uint32_t>(dk >> 32), v_hi = static_cast<uint32_t>(dv >> 32);
+      constexpr uint32_t kTileStep = Smem::kTileBytes >> 4;
+      const bool leader = elect_one();
+      uint32_t it = 0, c = 0, units = 0;  // messages read; tiles whose PV is issued; units begun
+      auto message = [&]() {
+        int flags = kEnd;
+        ok = ok && wait(sm.bar_info[it % kInfos], (it / kInfos) & 1);
+        if (ok) {
+          flags = sm.info[it % kInfos].flags;
+          arrive(sm.bar_infofree[it % kInfos]);
+          ++it;
+        }
+        return flags;
+      };
+      // waits until the first n PVs are done; one after another, and before the
+      // next is issued, so that the parity names one of them
+      uint32_t done = 0;
+      auto pv_done = [&](uint32_t n) {
+        for (; ok && done < n; ++done) ok = wait(sm.bar_pv, done & 1);
+      };
+      // S of tile n (counted over the run): its K is there, and the PV that
+      // reads P from the same columns is done
+      auto issue_s = [&](uint32_t n, bool qdone) {
+        const uint32_t slot = n % kSlots;
+        ok = ok && wait(sm.bar_k[slot], (n / kSlots) & 1);
+        if (n >= 2) pv_done(n - 1);
+        if (ok && leader) {
+          tc_fence_after();
+          const uint32_t b = k_lo + slot * kTileStep;
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
+            tc_mma_ss_lh(tmem + 128u * (n & 1), q_lo + off, k_hi, b + off, k_hi, kIdescQK, kk > 0);
+          }
+          tc_commit(smem_u32(&sm.bar_s[n & 1]));
+          tc_commit(smem_u32(&sm.bar_kfree[slot]));
+          if (qdone) tc_commit(smem_u32(&sm.bar_qfree));
+        }
+        __syncwarp();
+      };
+      while (ok) {
+        int flags = message();
+        if (flags & kEnd) break;
+        if (flags & kEmpty) continue;
+        ok = ok && wait(sm.bar_q, units & 1);
+        issue_s(c, flags & kLast);
+        for (bool begin = true; ok; begin = false) {
+          const bool last = flags & kLast;
+          if (!last) {
+            flags = message();
+            issue_s(c + 1, flags & kLast);
+          }
+          const uint32_t slot = c % kSlots, par = (c >> 1) & 1;
+          pv_done(c);
+          ok = ok && wait(sm.bar_v[slot], (c / kSlots) & 1);
+          // the unit's first PV overwrites O: the epilogue of the unit before has read it
+          if (begin && units > 0) ok = ok && wait(sm.bar_ofree, (units - 1) & 1);
+          const uint32_t b = v_lo + slot * kTileStep, pcol = tmem + 128u * (c & 1);
+#pragma unroll
+          for (int hp = 0; hp < 2; ++hp) {
+            ok = ok && wait(sm.bar_p[c & 1][hp], par);
+            if (ok && leader) {
+              tc_fence_after();
+#pragma unroll
+              for (int kk = 4 * hp; kk < 4 * hp + 4; ++kk)
+                tc_mma_ts_lh(tmem + kColO, pcol + 8 * kk, b + kk * 128, v_hi, kIdescPV, (begin && kk == 0) ? 0u : 1u);
+              if (hp == 1) {
+                tc_commit(smem_u32(&sm.bar_pv));
+                tc_commit(smem_u32(&sm.bar_vfree[slot]));
+              }
+            }
+            __syncwarp();
+          }
+          if (!ok) break;
+          ++c;
+          if (last) break;
+        }
+        ++units;
+      }
+      if (!ok) give_up();
+      if (leader) {
+        tc_commit(smem_u32(&sm.bar_drain));
+        mbar_wait(smem_u32(&sm.bar_drain), 0, nullptr);
+      }
+      __syncwarp();
+    }
+  } else if (warp >= kWarpConvert) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    // ------------------------------------------------- codes to tiles of K and V
+    // A warp takes 16 rows; a lane one group of 16 components of a row at a
+    // time: 8 bytes of codes, a scale, two chunks of 16 bytes.  Lanes of the
+    // upper 64 components write their second chunk first: eight lanes then
+    // fill eight different chunks of 128 bytes.
+    constexpr int kGroups = D / kQ4Group, kRowsStep = 32 / kGroups;
+    const int w = warp - kWarpConvert, grp = lane & (kGroups - 1), r0 = 16 * w + lane / kGroups;
+    const int half = grp >> 2, ch = (grp & 3) * 2;
+    uint32_t c = 0;
+    for (uint32_t it = 0; ok; ++it) {
+      ok = wait(sm.bar_info[it % kInfos], (it / kInfos) & 1);
+      if (!ok) break;
+      const TileInfo& info = sm.info[it % kInfos];
+      const int flags = info.flags, key0 = info.key0, lo = info.lo, se = info.se, w0 = info.w0, hi = info.hi;
+      arrive(sm.bar_infofree[it % kInfos]);
+      if (flags & kEnd) break;
+      if (flags & kEmpty) continue;
+      const uint32_t st = c % kStages, slot = c % kSlots;
+      const Stage<D>& s = sm.ring[st];
+      ok = wait(sm.bar_code[st], (c / kStages) & 1);
+      auto convert = [&](const uint8_t* codes, const uint8_t* scales, uint8_t* tile, bool zero) {
+        uint2 cw[16 / kRowsStep];
+        uint32_t sc[16 / kRowsStep];
+#pragma unroll
+        for (int j = 0; j < 16 / kRowsStep; ++j) {
+          const int r = r0 + kRowsStep * j;
+          cw[j] = *reinterpret_cast<const uint2*>(codes + r * (D / 2) + 8 * grp);
+          sc[j] = scales[r * kGroups + grp];
+        }
+#pragma unroll
+        for (int j = 0; j < 16 / kRowsStep; ++j) {
+          const int r = r0 + kRowsStep * j;
+          if (zero) {
+            // values of rows that no token of the unit sees may be anything: 0
+            const int key = key0 + r;
+            if (key < lo || key >= hi || (SINKS && key >= se && key < w0)) sc[j] = 0u;
+          }
+          const uint32_t f = q4_scale_pair(sc[j] | sc[j] << 8);
+          const uint4 a = make_uint4(mul_f16x2(q4_pair<0>(cw[j].x), f), mul_f16x2(q4_pair<1>(cw[j].x), f),
+                                     mul_f16x2(q4_pair<2>(cw[j].x), f), mul_f16x2(q4_pair<3>(cw[j].x), f));
+          const uint4 b = make_uint4(mul_f16x2(q4_pair<0>(cw[j].y), f), mul_f16x2(q4_pair<1>(cw[j].y), f),
+                                     mul_f16x2(q4_pair<2>(cw[j].y), f), mul_f16x2(q4_pair<3>(cw[j].y), f));
+          uint8_t* row = tile + half * kHalfBytes + r * 128;
+          const int x = r & 7;
+          *reinterpret_cast<uint4*>(row + (((ch + half) ^ x) << 4)) = half ? b : a;
+          *reinterpret_cast<uint4*>(row + (((ch + 1 - half) ^ x) << 4)) = half ? a : b;
+        }
+        fence_proxy_async_smem();
+      };
+      const bool zero = !(flags & kFull);
+      if (c >= kSlots) ok = ok && wait(sm.bar_kfree[slot], ((c / kSlots) - 1) & 1);
+      if (!ok) break;
+      convert(s.kc, s.ks, sm.k[slot], false);
+      arrive(sm.bar_k[slot]);
+      if (c >= kSlots) ok = wait(sm.bar_vfree[slot], ((c / kSlots) - 1) & 1);
+      if (!ok) break;
+      convert(s.vc, s.vs, sm.v[slot], zero);
+      arrive(sm.bar_v[slot]);
+      arrive(sm.bar_codefree[st]);
+      ++c;
+    }
+    if (!ok) give_up();
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    // -------------------------------------------------------------- softmax
+    const int row = tid, tl = row / p.g, hl = row - tl * p.g;
+    const uint32_t lane_tmem = tmem + (static_cast<uint32_t>(warp * 32) << 16);
+    const uint32_t o_tmem = lane_tmem + kColO;
+    uint32_t c = 0, units = 0;
+    Unit u{};
+    bool row_exists = false, seen = false, work = false, fresh = true;
+    int klo = 0, khi = 0, kse = 0, wlo = 0, whi = 0;  // this row's keys; those that all rows of the warp see
+    float m_ref = -INFINITY, l_sum = 0.f, scale = 0.f;
+    for (uint32_t it = 0; ok; ++it) {
+      ok = wait(sm.bar_info[it % kInfos], (it / kInfos) & 1);
+      if (!ok) break;
+      const TileInfo& info = sm.info[it % kInfos];
+      const int flags = info.flags, key0 = info.key0;
+      if (flags & kFirst) u = Unit{info.ntok, info.tok0, info.kvh, info.i0, info.n, info.C, info.ks};
+      arrive(sm.bar_infofree[it % kInfos]);
+      if (flags & kEnd) break;
+      const bool empty = flags & kEmpty;
+      if (flags & kFirst) {
+        row_exists = tl < p.tb && tl < u.ntok;
+        klo = khi = kse = 0;
+        if (row_exists && !empty) {
+          ChunkSeq s;
+          s.n = u.n;
+          s.C = u.C;
+          s.ks = u.ks;
+          klo = key_lo(p.a, s, u.i0 + tl);
+          khi = key_hi(p.a, s, u.i0 + tl);
+          if constexpr (SINKS) kse = sink_end(p.a, s, khi);
+        }
+        seen = klo < khi;
+        work = __any_sync(full, seen);  // (a warp without a row that sees a key only keeps the hand-offs going)
+        wlo = __reduce_max_sync(full, klo);
+        whi = __reduce_min_sync(full, seen ? khi : (work ? 0x7fffffff : 0));
+        m_ref = -INFINITY;
+        l_sum = 0.f;
+        fresh = true;
+        if (!empty) {
+          // this thread's row of Q to fp16, in place
+          ok = wait(sm.bar_qraw, units & 1);
+          if (!ok) break;
+          uint4* qr[kHalves];
+          uint32_t top = 0;
+#pragma unroll
+          for (int hf = 0; hf < kHalves; ++hf) {
+            qr[hf] = reinterpret_cast<uint4*>(sm.q + hf * kHalfBytes + row * 128);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const uint4 x = qr[hf][k ^ (row & 7)];
+              const uint32_t a = max(max(x.x & 0x7fffu, x.x >> 16 & 0x7fffu), max(x.y & 0x7fffu, x.y >> 16 & 0x7fffu));
+              const uint32_t b = max(max(x.z & 0x7fffu, x.z >> 16 & 0x7fffu), max(x.w & 0x7fffu, x.w >> 16 & 0x7fffu));
+              top = max(top, max(a, b));
+            }
+          }
+          float down, up;
+          q_powers(top, down, up);
+          scale = up * p.scale_log2;
+          auto half2_of = [&](uint32_t w) {
+            return pack_f16x2(__uint_as_float(w << 16) * down, __uint_as_float(w & 0xffff0000u) * down);
+          };
+#pragma unroll
+          for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const uint4 x = qr[hf][k ^ (row & 7)];
+              qr[hf][k ^ (row & 7)] = make_uint4(half2_of(x.x), half2_of(x.y), half2_of(x.z), half2_of(x.w));
+            }
+          fence_proxy_async_smem();
+          arrive(sm.bar_q);
+          ++units;
+        }
+      }
+      if (!empty) {
+        const uint32_t buf = c & 1, par = (c >> 1) & 1;
+        const uint32_t s_tmem = lane_tmem + 128u * buf;
+        ok = wait(sm.bar_s[buf], par);
+        if (!ok) break;
+        if (!work) {
+          arrive(sm.bar_p[buf][0]);
+          arrive(sm.bar_p[buf][1]);
+        } else {
+          tc_fence_after();
+          uint32_t xs[4][32];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) tmem_ld32(s_tmem + 32 * q, xs[q]);
+          tmem_wait_ld();
+          if (key0 < wlo || key0 + kTile > whi) {
+            // this row's keys within the tile
+            const int from = min(max(klo - key0, 0), kTile), to = min(max(khi - key0, 0), kTile);
+#pragma unroll
+            for (int wd = 0; wd < 4; ++wd) {
+              const int f = min(max(from - 32 * wd, 0), 32), e = min(max(to - 32 * wd, 0), 32);
+              uint32_t keep = e > f ? (0xffffffffu >> (32 - (e - f))) << f : 0u;  // bits f .. e-1
+              if constexpr (SINKS) {
+                const int sf = min(max(u.ks - key0 - 32 * wd, 0), 32), se = min(max(kse - key0 - 32 * wd, 0), 32);
+                keep |= se > sf ? (0xffffffffu >> (32 - (se - sf))) << sf : 0u;
+              }
+#pragma unroll
+              for (int k = 0; k < 32; ++k) xs[wd][k] = (keep >> k) & 1u ? xs[wd][k] : 0xff800000u;
+            }
+          }
+          // The half's probabilities against the reference that the row has,
+          // and beside them the row's maximum, which tells whether that
+          // reference still serves; where it does not, and on a piece's first
+          // tile, the half is done (again) with the reference moved.
+          const unsigned long long sc2 = f32x2(scale, scale);
+          unsigned long long acc[2], nm2;
+          auto half = [&](int hp) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              uint32_t pk[16];
+#pragma unroll
+              for (int k = 0; k < 16; ++k) {
+                float e0, e1;
+                f32x2_split(fma_f32x2(f32x2(__uint_as_float(xs[2 * hp + q][2 * k]), __uint_as_float(xs[2 * hp + q][2 * k + 1])),
+                                      sc2, nm2),
+                            e0, e1);
+                const float p0 = fast_exp2(e0), p1 = fast_exp2(e1);
+                acc[k & 1] = add_f32x2(acc[k & 1], f32x2(p0, p1));
+                pk[k] = pack_f16x2(p0, p1);
+              }
+              tmem_st16(s_tmem + 32 * hp + 16 * q, pk);
+            }
+          };
+          auto row_max = [&]() {
+            float r[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) r[k] = fmax3(__uint_as_float(xs[0][k]), __uint_as_float(xs[0][k + 8]), __uint_as_float(xs[0][k + 16]));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) r[k] = fmax3(r[k], __uint_as_float(xs[0][k + 24]), __uint_as_float(xs[1][k]));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) r[k] = fmax3(r[k], __uint_as_float(xs[1][k + 8]), __uint_as_float(xs[1][k + 16]));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) r[k] = fmax3(r[k], __uint_as_float(xs[1][k + 24]), __uint_as_float(xs[2][k]));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) r[k] = fmax3(r[k], __uint_as_float(xs[2][k + 8]), __uint_as_float(xs[2][k + 16]));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) r[k] = fmax3(r[k], __uint_as_float(xs[2][k + 24]), __uint_as_float(xs[3][k]));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) r[k] = fmax3(r[k], __uint_as_float(xs[3][k + 8]), __uint_as_float(xs[3][k + 16]));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) r[k] = fmaxf(r[k], __uint_as_float(xs[3][k + 24]));
+            return fmax3(fmax3(r[0], r[1], r[2]), fmax3(r[3], r[4], r[5]), fmaxf(r[6], r[7])) * scale;
+          };
+          auto start_half = [&]() {
+            const float neg_m = m_ref != -INFINITY ? -m_ref : 0.f;
+            nm2 = f32x2(neg_m, neg_m);
+            acc[0] = acc[1] = f32x2(0.f, 0.f);
+          };
+          start_half();
+          half(0);
+          const float mx = row_max();
+          const bool move = seen && mx != -INFINITY && (m_ref == -INFINITY || mx > m_ref + kRescaleThreshold);
+          if (__any_sync(full, move)) {
+            // the first stores of the half are complete before those that
+            // replace them are issued (only a wait orders two of them)
+            tmem_wait_st();
+            const float f = move && m_ref != -INFINITY ? fast_exp2(m_ref - mx) : 1.0f;
+            l_sum *= f;
+            if (move) m_ref = mx;
+            if (!fresh) {
+              // O holds the piece's earlier tiles once the PV before this one is done
+              ok = wait(sm.bar_pv, (c - 1) & 1);
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int q = 0; q < D / 16; ++q) {
+                uint32_t o[16];
+                tmem_ld16(o_tmem + 16 * q, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                tmem_st16(o_tmem + 16 * q, o);
+              }
+            }
+            start_half();
+            half(0);
+          }
+          auto hand_over = [&](int hp) {
+            tmem_wait_st();
+            tc_fence_before();
+            arrive(sm.bar_p[buf][hp]);
+          };
+          hand_over(0);
+          half(1);
+          hand_over(1);
+          float s0, s1;
+          f32x2_split(add_f32x2(acc[0], acc[1]), s0, s1);
+          l_sum += s0 + s1;
+        }
+        fresh = false;
+        ++c;
+      }
+      if (flags & kLastPiece) pdl_launch_next();
+      if (!(flags & kLast)) continue;
+
+      // ---- epilogue (a sum that is NaN is passed on, not hidden)
+      if (!empty) {
+        ok = wait(sm.bar_pv, (c - 1) & 1);
+        if (!ok) break;
+        tc_fence_after();
+      }
+      const bool bad = flags & kBad, part = flags & kPart;
+      const bool any = !empty && seen && l_sum != 0.f && !bad;
+      const float inv = any ? p.c.v_unit / l_sum : 0.f;
+      const int entry = static_cast<int>(blockIdx.x) * 2 + (flags & kSlot1 ? 1 : 0);
+      const size_t out_row = static_cast<size_t>(u.tok0 + (row_exists ? tl : 0)) * p.a.Hq + u.kvh * p.g + hl;
+      uint4* orow = reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.a.out) + out_row * (2 * D));
+#pragma unroll 1
+      for (int q = 0; q < D / 16; ++q) {
+        uint32_t o[16];
+        if (!empty) {
+          tmem_ld16(o_tmem + 16 * q, o);
+          tmem_wait_ld();
+          if (q == D / 16 - 1) {
+            // O may be overwritten by the next unit's first PV
+            tc_fence_before();
+            arrive(sm.bar_ofree);
+          }
+        }
+        if (!row_exists) continue;
+        if (part) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            *partial_o<D>(p, entry, 4 * q + k, row) =
+                any ? make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]),
+                                  __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]))
+                    : make_float4(0.f, 0.f, 0.f, 0.f);
+        } else {
+          uint32_t wv[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            wv[e] = any ? pack_bf16x2(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
+          orow[2 * q] = make_uint4(wv[0], wv[1], wv[2], wv[3]);
+          orow[2 * q + 1] = make_uint4(wv[4], wv[5], wv[6], wv[7]);
+        }
+      }
+      if (row_exists && part) *partial_ml<D>(p, entry, row) = make_float2(any ? m_ref : -INFINITY, any ? l_sum : bad ? -1.f : 0.f);
+      if (row_exists && !part && p.a.lse) p.a.lse[out_row] = any ? (m_ref + log2f(l_sum)) * kLn2 : -INFINITY;
+    }
+    if (!ok) give_up();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kWarpMma) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// Merge of cut units: block (c - 1, y) takes run boundary c and, of its unit's
+// query rows, every gridDim.y-th group of 8; a thread owns four columns of a
+// row (8 rows x 16 bytes of a partial are one line).
+template <int D>
+__global__ void __launch_bounds__(2 * D) chunk_q4_tc_merge_kernel(const __grid_constant__ Q4TcParams p) {
+  pdl_wait();
+  pdl_launch_next();
+  const Record rec = records<D>(p)[blockIdx.x + 1];
+  const int np = rec.c1 - rec.c0 + 1, rows = rec.ntok * p.g;
+  const int r8 = threadIdx.x & 7, col4 = threadIdx.x >> 3;
+  for (int row = blockIdx.y * 8 + r8; row < rows; row += gridDim.y * 8) {
+    auto entry = [&](int j) { return (rec.c0 + j) * 2 + (j == 0 ? rec.slot : 0); };
+    float M = -INFINITY, L = 0.f;
+    bool bad = false;
+#pragma unroll 4
+    for (int j = 0; j < np; ++j) {
+      const float2 ml = *partial_ml<D>(p, entry(j), row);
+      if (ml.y != 0.f) M = fmaxf(M, ml.x);
+      bad |= ml.y == -1.f;
+    }
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int j = 0; j < np; ++j) {
+      const float2 ml = *partial_ml<D>(p, entry(j), row);
+      const float4 o = *partial_o<D>(p, entry(j), col4, row);
+      const float w = ml.y != 0.f && !bad ? exp2f(ml.x - (M == -INFINITY ? 0.f : M)) : 0.f;
+      L = fmaf(w, ml.y, L);
+      acc.x = fmaf(w, o.x, acc.x);
+      acc.y = fmaf(w, o.y, acc.y);
+      acc.z = fmaf(w, o.z, acc.z);
+      acc.w = fmaf(w, o.w, acc.w);
+    }
+    const bool any = L != 0.f && !bad;
+    const float inv = any ? p.c.v_unit / L : 0.f;
+    const int tl = row / p.g;
+    const size_t out_row = static_cast<size_t>(rec.tok0 + tl) * p.a.Hq + rec.kvh * p.g + (row - tl * p.g);
+    reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.a.out) + out_row * D)[col4] =
+        any ? make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv)) : make_uint2(0u, 0u);
+    if (p.a.lse && col4 == 0) p.a.lse[out_row] = any ? (M + log2f(L)) * kLn2 : -INFINITY;
+  }
+}
+
+template <int D, bool SINKS>
+cudaError_t launch_d(Q4TcParams p, int num_sms, EncodeTiledFn encode, cudaStream_t stream) {
+  CUtensorMap tq;
+  const cuuint64_t dims[3] = {D, static_cast<cuuint64_t>(p.a.Hq), static_cast<cuuint64_t>(p.a.T)};
+  const cuuint64_t strides[2] = {D * 2ull, static_cast<cuuint64_t>(p.a.q_stride) * 2ull};
+  const cuuint32_t box[3] = {64u, static_cast<cuuint32_t>(p.g), static_cast<cuuint32_t>(p.tb)};
+  if (!make_bf16_map(encode, &tq, p.a.q, 3, dims, strides, box)) return cudaErrorInvalidValue;
+  static std::mutex mu;
+  static bool done[64] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  {
+    std::lock_guard<std::mutex> lk(mu);
+    if (!done[dev]) {
+      e = cudaFuncSetAttribute(chunk_q4_tc_kernel<D, SINKS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               static_cast<int>(smem_bytes<D>()));
+      if (e != cudaSuccess) return e;
+      done[dev] = true;
+    }
+  }
+  p.ctas = num_sms;
+  e = launch_overlapped(chunk_q4_tc_kernel<D, SINKS>, dim3(static_cast<unsigned>(p.ctas)), dim3(kThreads), smem_bytes<D>(),
+                        stream, 1u, tq, p);
+  if (e != cudaSuccess || p.ctas == 1) return e;
+  return launch_overlapped(chunk_q4_tc_merge_kernel<D>, dim3(static_cast<unsigned>(p.ctas - 1), 8u), dim3(2 * D), 0,
+                           stream, 1u, p);
+}
+
+}  // namespace
+
+size_t chunk_q4_tc_workspace_bytes(int d, int num_sms) {
+  return static_cast<size_t>(num_sms) * (2ull * kRows * (d + 2) * sizeof(float) + sizeof(Record));
+}
+
+cudaError_t launch_chunk_attention_q4_tc(const ChunkArgs& a, const simsd_q4_cache& c, int num_sms, EncodeTiledFn encode,
+                                         cudaStream_t stream) {
+  Q4TcParams p{};
+  p.a = a;
+  p.c = c;
+  p.g = a.Hq / a.Hkv;
+  p.tb = kRows / p.g;
+  p.sub = a.page_size % kTile == 0 ? kTile : std::min(a.page_size, 64);
+  p.scale_log2 = a.scale * c.k_unit * 1.4426950408889634f;
+  if (a.sinks > 0) return a.d == 128 ? launch_d<128, true>(p, num_sms, encode, stream) : launch_d<64, true>(p, num_sms, encode, stream);
+  return a.d == 128 ? launch_d<128, false>(p, num_sms, encode, stream) : launch_d<64, false>(p, num_sms, encode, stream);
+}
+
+}  // namespace simsd

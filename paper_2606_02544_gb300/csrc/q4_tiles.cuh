@@ -1,0 +1,137 @@
+// q4_tiles.cuh -- tiles of a cache in 4 bits on their way to shared memory,
+// shared by the kernels that read one: what the walking warp says of a tile,
+// and the copies that bring its codes and scales.
+#pragma once
+#include "chunk_walk.cuh"
+#include "ptx.cuh"
+#include "q4.cuh"
+
+namespace simsd {
+
+constexpr int kQ4Tile = 128;  // keys per tile
+
+enum : int {
+  kFirst = 1,       // of a piece
+  kLast = 2,        // of a piece
+  kLastPiece = 4,   // and that the CTA's last one
+  kFull = 8,        // every row sees every key
+  kEmpty = 16,      // no row sees any key
+  kEnd = 32,        // no tile: the end of the run
+  kPart = 64,       // the piece leaves partial results,
+  kSlot1 = 128,     // those of slot 1
+  kBad = 256        // a page id of the piece (so far) is out of range
+};
+struct alignas(16) TileInfo {
+  int flags, key0, ntok, tok0;
+  int kvh, i0, n, C;
+  int lo, se, w0, hi;  // keys that any row of the unit sees
+  int ks, pad0, pad1, pad2;
+};
+
+template <int D>
+struct alignas(128) Stage {
+  uint8_t kc[kQ4Tile * D / 2], vc[kQ4Tile * D / 2];
+  uint8_t ks[kQ4Tile * D / kQ4Group], vs[kQ4Tile * D / kQ4Group];
+};
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+// The pieces of a run, tile by tile.  One warp; `sub`: keys per copy (a page,
+// or part of one).
+template <int D, bool SINKS>
+struct TileWalk {
+  Walk<SINKS, kQ4Tile> k;
+  typename Walk<SINKS, kQ4Tile>::Step piece;
+  TileInfo u;
+  int ub, sub, flags, skip, tse, all_lo, all_hi, all_se, t0;
+  int win_base, win;  // lane i holds the page id of page win_base + i
+  const int32_t* bt;
+  // this lane's copy of the tile
+  bool load;
+  size_t row;  // in the pool, in rows of a head
+
+  __device__ __forceinline__ bool next_piece(const ChunkArgs& a) {
+    if (!k.peek(a, ub, piece)) return false;
+    u.i0 = k.w.j * ub;
+    u.tok0 = k.s.start + u.i0;
+    u.ntok = min(ub, k.s.C - u.i0);
+    u.kvh = k.w.kvh;
+    u.lo = piece.keys.lo;
+    u.se = piece.keys.se;
+    u.w0 = piece.keys.w0;
+    u.hi = piece.keys.hi;
+    u.n = k.s.n;
+    u.C = k.s.C;
+    u.ks = k.s.ks;
+    const bool empty = piece.tiles == 0;
+    flags = (empty ? kEmpty : 0) | (piece.take < piece.weight ? kPart : 0) | (piece.slot ? kSlot1 : 0);
+    // rows that every token of the unit sees
+    all_lo = empty ? 0 : key_lo(a, k.s, u.i0 + u.ntok - 1);
+    all_hi = empty ? 0 : key_hi(a, k.s, u.i0);
+    all_se = SINKS && !empty ? sink_end(a, k.s, all_hi) : 0;
+    skip = tiles_skipped<SINKS, kQ4Tile>(piece.keys);
+    tse = (u.se + kQ4Tile - 1) / kQ4Tile;
+    bt = a.block_table + static_cast<size_t>(k.w.b) * a.max_pages;
+    t0 = u.lo / kQ4Tile + k.w.t;
+    win_base = -(1 << 30);
+    return true;
+  }
+  // Tile i of the piece: u, and the lane's copy.
+  __device__ __forceinline__ void tile(const ChunkArgs& a, int i) {
+    const unsigned full = 0xffffffffu;
+    const int lane = threadIdx.x & 31, P = a.page_size, t = t0 + i;
+    const bool empty = flags & kEmpty;
+    u.key0 = (t + (SINKS && t >= tse ? skip : 0)) * kQ4Tile;
+    const bool all = !empty && ((u.key0 >= all_lo && u.key0 + kQ4Tile <= all_hi) ||
+                                (SINKS && u.key0 >= u.ks && u.key0 + kQ4Tile <= all_se));
+    // copy s of the tile is lane s's
+    const int nsub = kQ4Tile / sub, key = u.key0 + min(lane, nsub - 1) * sub, pi = key / P;
+    const int pi0 = u.key0 / P, pi1 = (u.key0 + kQ4Tile - 1) / P;
+    if (pi0 < win_base || pi1 >= win_base + 32) {
+      win_base = pi0;
+      win = win_base + lane < a.max_pages ? bt[win_base + lane] : -1;
+    }
+    const int pg = __shfl_sync(full, win, (pi - win_base) & 31);
+    load = !empty && lane < nsub && key + sub > u.lo && key < u.hi && (!SINKS || key < u.se || key + sub > u.w0);
+    const bool wrong = load && (pg < 0 || pg >= a.num_pages);
+    load = load && !wrong;
+    if (__any_sync(full, wrong)) {
+      if (lane == 0) raise_error(a.err_word, SIMSD_EW_PAGE);
+      flags |= kBad;
+    }
+    row = (static_cast<size_t>(pg) * a.Hkv + u.kvh) * P + (key - pi * P);
+    u.flags = flags | (i == 0 ? kFirst : 0) | (i + 1 == piece.take ? kLast | (piece.last ? kLastPiece : 0) : 0) | (all ? kFull : 0);
+  }
+  // Bytes of all lanes' copies; then the copies themselves.
+  __device__ __forceinline__ uint32_t bytes() const {
+    return __popc(__ballot_sync(0xffffffffu, load)) * 2u * static_cast<uint32_t>(sub * (D / 2 + D / kQ4Group));
+  }
+  __device__ __forceinline__ void copy(const simsd_q4_cache& c, Stage<D>& s, uint32_t bar) const {
+    if (!load) return;
+    const uint32_t code_bytes = static_cast<uint32_t>(sub * (D / 2)), scale_bytes = static_cast<uint32_t>(sub * (D / kQ4Group));
+    const int at = (threadIdx.x & 31) * sub;
+    bulk_load(smem_u32(&s.kc[at * (D / 2)]), static_cast<const uint8_t*>(c.k_codes) + row * (D / 2), code_bytes, bar);
+    bulk_load(smem_u32(&s.ks[at * (D / kQ4Group)]), static_cast<const uint8_t*>(c.k_scales) + row * (D / kQ4Group), scale_bytes, bar);
+    bulk_load(smem_u32(&s.vc[at * (D / 2)]), static_cast<const uint8_t*>(c.v_codes) + row * (D / 2), code_bytes, bar);
+    bulk_load(smem_u32(&s.vs[at * (D / kQ4Group)]), static_cast<const uint8_t*>(c.v_scales) + row * (D / kQ4Group), scale_bytes, bar);
+  }
+};
+
+// A power of two that brings a row's largest component to [1, 4), from that
+// component's bf16 bits without the sign, and its inverse.
+__device__ __forceinline__ void q_powers(uint32_t top, float& down, float& up) {
+  const uint32_t ex = min(max(top >> 7, 1u), 253u);  // 2^(ex - 127) <= the largest < 2^(ex - 126)
+  down = __uint_as_float((254u - ex) << 23);
+  up = __uint_as_float(ex << 23);
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+}  // namespace simsd
