@@ -11,16 +11,29 @@
 // codes and scales of a tile (18 KB) come by bulk copies; eight warps turn
 // them into the fp16 tiles of K and V, each once, in the layout that the
 // matrix instructions read (rows of 128 bytes, swizzled), and set the rows of
-// V that no token sees to zero.  S has two buffers in tensor memory, so that
-// S of the next tile is formed under the softmax of this one.  The walk of
-// chunk_walk.cuh; units cut by the end of a run are merged by a second launch.
+// V that no token sees to zero.  The walk of chunk_walk.cuh; units cut by the
+// end of a run are merged by a second launch.
 //
-// Warp roles (512 threads): warps 0-3 softmax (thread i owns query row i =
-// TMEM lane i, and turns its row of Q into fp16 in place); warps 4-11 K and V;
-// warp 12 walks the run and issues all copies; warp 13 the MMAs, in the order
-// S(0) S(1) PV(0) S(2) PV(1) ... of a unit.
-// TMEM (512 columns): S [0,128) and [128,256), O [256, 256 + D); P (fp16)
-// overwrites the first 64 columns of its S.
+// A tile's softmax is one chain of waits, loads and exponentials a row, some
+// 3800 cycles where one warp does it for 32 rows by itself (127 us for 32
+// blocks of 16 tokens over 4096 rows).  So two sets of warps take a unit's
+// tiles in turns, each with a reference, a sum and an O of its own, which are
+// put together at the unit's end: the products and the waits of one set lie
+// under the exponentials of the other.
+//
+// Warp roles (640 threads): warps 0-3 softmax of the even tiles, 4-7 of the
+// odd ones (thread i of a set owns query row i = TMEM lane i; the even set
+// turns Q into fp16 in place); warps 8-15 K and V; warp 16 walks the run and
+// issues all copies; warp 17 the MMAs, in the order S(0) S(1) PV(0) S(2) PV(1)
+// ... of a unit.
+// Lean units, of up to 64 rows, have their rows of Q twice, in the lanes 0-63
+// and 64-127: the first take a tile's first 64 keys, the others the last 64,
+// and set the P of the keys that are not theirs to zero.  All four partitions
+// of the SM then share the exponentials, which else lie on two (32 blocks of
+// 16 tokens: 140 us), at the same number of matrix instructions; O comes
+// together at the unit's end through shared memory.
+// TMEM (512 columns): S of the sets [0,128), [128,256); O of the sets [256,
+// 384), [384, 512); P (fp16) overwrites the first 64 columns of its S.
 //
 // Every mbarrier wait is bounded; after one expires the CTA raises
 // SIMSD_EW_TIMEOUT, every role leaves its loops, drains its copies and MMAs
@@ -43,13 +56,13 @@ namespace {
 
 constexpr int kTile = kQ4Tile;
 constexpr int kRows = 128;  // query rows of a unit (MMA M)
-constexpr int kThreads = 512;
-constexpr int kWarpConvert = 4, kConvertWarps = 8, kWarpWalk = 12, kWarpMma = 13;
+constexpr int kThreads = 640;
+constexpr int kSoftmaxWarps = 8, kWarpConvert = 8, kConvertWarps = 8, kWarpWalk = 16, kWarpMma = 17;
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kColO = 256;
+constexpr uint32_t kColO = 256;  // + 128 per set
 constexpr int kHalfBytes = kTile * 128;  // 128 rows x 64 fp16
 constexpr int kInfos = 8;                // tiles that the walk is ahead of the last reader
-constexpr int kInfoReaders = 4 + kConvertWarps + 1;
+constexpr int kInfoReaders = kSoftmaxWarps + kConvertWarps + 1;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -61,12 +74,12 @@ struct Q4TcParams {
   float scale_log2;   // scores to log2 units, the keys' unit included
 };
 
-template <int D>
+template <int D, bool LEAN>
 struct alignas(1024) SmemQ4Tc {
   static constexpr int kHalves = D / 64;
   static constexpr int kTileBytes = kHalves * kHalfBytes;
   static constexpr int kSlots = D == 128 ? 2 : 4;   // of K, and of V
-  static constexpr int kStages = D == 128 ? 3 : 6;  // of codes
+  static constexpr int kStages = D == 64 ? 6 : LEAN ? 2 : 3;  // of codes
   uint8_t k[kSlots][kTileBytes], v[kSlots][kTileBytes];
   uint8_t q[kTileBytes];
   Stage<D> ring[kStages];
@@ -75,17 +88,24 @@ struct alignas(1024) SmemQ4Tc {
   uint64_t bar_k[kSlots], bar_kfree[kSlots], bar_v[kSlots], bar_vfree[kSlots];
   uint64_t bar_info[kInfos], bar_infofree[kInfos];
   uint64_t bar_qraw, bar_q, bar_qfree;
-  uint64_t bar_s[2], bar_p[2][2], bar_pv, bar_ofree, bar_drain;
+  uint64_t bar_s[2], bar_p[2][2], bar_pv[2], bar_ofree, bar_meet, bar_drain;
+  float2 ml[2][2][kRows];  // (m, l) of the sets, for pieces in turns
+  float q_up[2][kRows];    // the powers of two that Q was divided by, for units in turns
+  // lean units: O of the upper lanes on its way to the lower ones, 16 columns
+  // at a time, in two buffers a set
+  float o[LEAN ? 2 : 1][LEAN ? 2 : 1][16][kRows / 2];
+  uint64_t bar_x[2][2], bar_xfree[2][2];
   uint32_t tmem_base;
   int abort_flag;
 };
-template <int D>
+template <int D, bool LEAN>
 constexpr size_t smem_bytes() {
-  return sizeof(SmemQ4Tc<D>) + 1024;
+  return sizeof(SmemQ4Tc<D, LEAN>) + 1024;
 }
-static_assert(smem_bytes<128>() <= 232448 && smem_bytes<64>() <= 232448, "one CTA per SM");
-static_assert(2 * SmemQ4Tc<64>::kSlots * SmemQ4Tc<64>::kTileBytes >= kChunkMaxSeqs * 4 &&
-                  2 * SmemQ4Tc<128>::kSlots * SmemQ4Tc<128>::kTileBytes >= kChunkMaxSeqs * 4,
+static_assert(smem_bytes<128, true>() <= 232448 && smem_bytes<64, true>() <= 232448 &&
+                  smem_bytes<128, false>() <= 232448 && smem_bytes<64, false>() <= 232448, "one CTA per SM");
+static_assert(2 * SmemQ4Tc<64, false>::kSlots * SmemQ4Tc<64, false>::kTileBytes >= kChunkMaxSeqs * 4 &&
+                  2 * SmemQ4Tc<128, false>::kSlots * SmemQ4Tc<128, false>::kTileBytes >= kChunkMaxSeqs * 4,
               "the tiles of K and V hold the tile counts of all sequences while runs are planned");
 
 // kind::f16 with fp16 A and B, fp32 accumulator
@@ -111,15 +131,10 @@ __device__ __forceinline__ Record* records(const Q4TcParams& p) {
   return reinterpret_cast<Record*>(partial_ml<D>(p, 2 * p.ctas, 0));
 }
 
-// A piece's fields that the softmax keeps while its tiles last.
-struct Unit {
-  int ntok, tok0, kvh, i0, n, C, ks;
-};
-
-template <int D, bool SINKS>
+template <int D, bool SINKS, bool LEAN>
 __global__ void __launch_bounds__(kThreads, 1)
     chunk_q4_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ Q4TcParams p) {
-  using Smem = SmemQ4Tc<D>;
+  using Smem = SmemQ4Tc<D, LEAN>;
   constexpr int kHalves = Smem::kHalves, kSlots = Smem::kSlots, kStages = Smem::kStages;
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -150,9 +165,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(smem_u32(&sm.bar_p[x][0]), 4);
       mbar_init(smem_u32(&sm.bar_p[x][1]), 4);
     }
-    mbar_init(smem_u32(&sm.bar_pv), 1);
-    mbar_init(smem_u32(&sm.bar_ofree), 4);
+    mbar_init(smem_u32(&sm.bar_pv[0]), 1);
+    mbar_init(smem_u32(&sm.bar_pv[1]), 1);
+    mbar_init(smem_u32(&sm.bar_ofree), kSoftmaxWarps);
+    mbar_init(smem_u32(&sm.bar_meet), kSoftmaxWarps);
     mbar_init(smem_u32(&sm.bar_drain), 1);
+    for (int x = 0; x < 4; ++x) {
+      mbar_init(smem_u32(&sm.bar_x[x >> 1][x & 1]), 2);
+      mbar_init(smem_u32(&sm.bar_xfree[x >> 1][x & 1]), 2);
+    }
     fence_mbar_init();
   }
   if (warp == kWarpMma) {
@@ -184,9 +205,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   };
   bool ok = true;
 
-  // register split: 128 x 208 + 256 x 96 + 128 x 88 = 62,464 of the launch's 512 x 128
+  // register split: 256 x 128 + 256 x 72 + 128 x 80 = 61,440 = the launch's 640 x 96
   if (warp >= kWarpWalk) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == kWarpWalk) {
       // ------------------------------------------------------ walk and copies
       TileWalk<D, SINKS> tw;
@@ -222,10 +243,11 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (!ok) break;
               if (lane == 0) {
                 const uint32_t bq = smem_u32(&sm.bar_qraw);
-                mbar_arrive_expect_tx(bq, static_cast<uint32_t>(kHalves * p.g * p.tb) * 128u);
+                mbar_arrive_expect_tx(bq, static_cast<uint32_t>((LEAN ? 2 : 1) * kHalves * p.g * p.tb) * 128u);
 #pragma unroll
-                for (int hf = 0; hf < kHalves; ++hf)
-                  tma_load_3d(smem_u32(sm.q) + hf * kHalfBytes, &tm_q, bq, 64 * hf, tw.u.kvh * p.g, tw.u.tok0);
+                for (int hf = 0; hf < (LEAN ? 2 : 1) * kHalves; ++hf)
+                  tma_load_3d(smem_u32(sm.q) + (hf % kHalves) * kHalfBytes + (hf / kHalves) * (kHalfBytes / 2), &tm_q, bq,
+                              64 * (hf % kHalves), tw.u.kvh * p.g, tw.u.tok0);
               }
               ++units;
             }
@@ -259,10 +281,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t k_hi = static_cast<uint32_t>(dk >> 32), v_hi = static_cast<uint32_t>(dv >> 32);
       constexpr uint32_t kTileStep = Smem::kTileBytes >> 4;
       const bool leader = elect_one();
-      uint32_t it = 0, c = 0, units = 0;  // messages read; tiles whose PV is issued; units begun
+      auto poll = [&](uint64_t& bar, uint32_t parity) { return mbar_wait_poll(smem_u32(&bar), parity, abort_flag); };
+      // messages read; tiles whose S, and whose PV, is issued; units begun; of
+      // each set the tiles whose PV is issued, and known to be done
+      uint32_t it = 0, cs = 0, cp = 0, units = 0, issued[2] = {0, 0}, done[2] = {0, 0};
       auto message = [&]() {
         int flags = kEnd;
-        ok = ok && wait(sm.bar_info[it % kInfos], (it / kInfos) & 1);
+        ok = ok && poll(sm.bar_info[it % kInfos], (it / kInfos) & 1);
         if (ok) {
           flags = sm.info[it % kInfos].flags;
           arrive(sm.bar_infofree[it % kInfos]);
@@ -270,67 +295,66 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         return flags;
       };
-      // waits until the first n PVs are done; one after another, and before the
-      // next is issued, so that the parity names one of them
-      uint32_t done = 0;
-      auto pv_done = [&](uint32_t n) {
-        for (; ok && done < n; ++done) ok = wait(sm.bar_pv, done & 1);
-      };
-      // S of tile n (counted over the run): its K is there, and the PV that
-      // reads P from the same columns is done
-      auto issue_s = [&](uint32_t n, bool qdone) {
-        const uint32_t slot = n % kSlots;
-        ok = ok && wait(sm.bar_k[slot], (n / kSlots) & 1);
-        if (n >= 2) pv_done(n - 1);
+      // S of the next tile, for set x: its K is there, and the set's last PV,
+      // whose P lies in the same columns, is done
+      auto issue_s = [&](int x, bool qdone) {
+        const uint32_t slot = cs % kSlots;
+        ok = ok && poll(sm.bar_k[slot], (cs / kSlots) & 1);
+        if (done[x] < issued[x]) {
+          ok = ok && poll(sm.bar_pv[x], done[x] & 1);
+          ++done[x];
+        }
         if (ok && leader) {
           tc_fence_after();
           const uint32_t b = k_lo + slot * kTileStep;
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
             const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
-            tc_mma_ss_lh(tmem + 128u * (n & 1), q_lo + off, k_hi, b + off, k_hi, kIdescQK, kk > 0);
+            tc_mma_ss_lh(tmem + 128u * x, q_lo + off, k_hi, b + off, k_hi, kIdescQK, kk > 0);
           }
-          tc_commit(smem_u32(&sm.bar_s[n & 1]));
+          tc_commit(smem_u32(&sm.bar_s[x]));
           tc_commit(smem_u32(&sm.bar_kfree[slot]));
           if (qdone) tc_commit(smem_u32(&sm.bar_qfree));
         }
         __syncwarp();
+        ++cs;
       };
       while (ok) {
         int flags = message();
         if (flags & kEnd) break;
         if (flags & kEmpty) continue;
-        ok = ok && wait(sm.bar_q, units & 1);
-        issue_s(c, flags & kLast);
-        for (bool begin = true; ok; begin = false) {
+        ok = ok && poll(sm.bar_q, units & 1);
+        issue_s(0, flags & kLast);
+        for (int i = 0; ok; ++i) {
           const bool last = flags & kLast;
+          const int x = i & 1;
           if (!last) {
             flags = message();
-            issue_s(c + 1, flags & kLast);
+            issue_s(x ^ 1, flags & kLast);
           }
-          const uint32_t slot = c % kSlots, par = (c >> 1) & 1;
-          pv_done(c);
-          ok = ok && wait(sm.bar_v[slot], (c / kSlots) & 1);
-          // the unit's first PV overwrites O: the epilogue of the unit before has read it
-          if (begin && units > 0) ok = ok && wait(sm.bar_ofree, (units - 1) & 1);
-          const uint32_t b = v_lo + slot * kTileStep, pcol = tmem + 128u * (c & 1);
+          const uint32_t slot = cp % kSlots, par = issued[x] & 1;
+          ok = ok && poll(sm.bar_v[slot], (cp / kSlots) & 1);
+          // the unit's first PV overwrites an O: the epilogue of the unit before has read both
+          if (i == 0 && units > 0) ok = ok && poll(sm.bar_ofree, (units - 1) & 1);
+          const uint32_t b = v_lo + slot * kTileStep, pcol = tmem + 128u * x, ocol = tmem + kColO + 128u * x;
 #pragma unroll
           for (int hp = 0; hp < 2; ++hp) {
-            ok = ok && wait(sm.bar_p[c & 1][hp], par);
+            ok = ok && poll(sm.bar_p[x][hp], par);
             if (ok && leader) {
               tc_fence_after();
 #pragma unroll
               for (int kk = 4 * hp; kk < 4 * hp + 4; ++kk)
-                tc_mma_ts_lh(tmem + kColO, pcol + 8 * kk, b + kk * 128, v_hi, kIdescPV, (begin && kk == 0) ? 0u : 1u);
+                tc_mma_ts_lh(ocol, pcol + 8 * kk, b + kk * 128, v_hi, kIdescPV, (i < 2 && kk == 0) ? 0u : 1u);
               if (hp == 1) {
-                tc_commit(smem_u32(&sm.bar_pv));
+                tc_commit(smem_u32(&sm.bar_pv[x]));
                 tc_commit(smem_u32(&sm.bar_vfree[slot]));
               }
             }
             __syncwarp();
           }
           if (!ok) break;
-          ++c;
+          ++issued[x];
+          ++cp;
           if (last) break;
         }
         ++units;
@@ -343,15 +367,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
     }
   } else if (warp >= kWarpConvert) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     // ------------------------------------------------- codes to tiles of K and V
     // A warp takes 16 rows; a lane one group of 16 components of a row at a
     // time: 8 bytes of codes, a scale, two chunks of 16 bytes.  Lanes of the
     // upper 64 components write their second chunk first: eight lanes then
     // fill eight different chunks of 128 bytes.
     constexpr int kGroups = D / kQ4Group, kRowsStep = 32 / kGroups;
-    const int w = warp - kWarpConvert, grp = lane & (kGroups - 1), r0 = 16 * w + lane / kGroups;
+    const int w = warp - kWarpConvert, grp = lane & (kGroups - 1);
     const int half = grp >> 2, ch = (grp & 3) * 2;
+    const int rb = 16 * w + lane / kGroups;
     uint32_t c = 0;
     for (uint32_t it = 0; ok; ++it) {
       ok = wait(sm.bar_info[it % kInfos], (it / kInfos) & 1);
@@ -364,89 +389,90 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t st = c % kStages, slot = c % kSlots;
       const Stage<D>& s = sm.ring[st];
       ok = wait(sm.bar_code[st], (c / kStages) & 1);
-      auto convert = [&](const uint8_t* codes, const uint8_t* scales, uint8_t* tile, bool zero) {
-        uint2 cw[16 / kRowsStep];
-        uint32_t sc[16 / kRowsStep];
+#pragma unroll 1
+      for (int kv = 0; ok && kv < 2; ++kv) {
+        uint64_t& taken = kv ? sm.bar_vfree[slot] : sm.bar_kfree[slot];
+        if (c >= kSlots) ok = wait(taken, ((c / kSlots) - 1) & 1);
+        if (!ok) break;
+        const uint8_t *codes = kv ? s.vc : s.kc, *scales = kv ? s.vs : s.ks;
+        uint8_t* tile = (kv ? sm.v[slot] : sm.k[slot]) + half * kHalfBytes;
+        const bool zero = kv && !(flags & kFull);
+        {
+          uint2 cw[16 / kRowsStep];
+          uint32_t sc[16 / kRowsStep];
 #pragma unroll
-        for (int j = 0; j < 16 / kRowsStep; ++j) {
-          const int r = r0 + kRowsStep * j;
-          cw[j] = *reinterpret_cast<const uint2*>(codes + r * (D / 2) + 8 * grp);
-          sc[j] = scales[r * kGroups + grp];
-        }
-#pragma unroll
-        for (int j = 0; j < 16 / kRowsStep; ++j) {
-          const int r = r0 + kRowsStep * j;
-          if (zero) {
-            // values of rows that no token of the unit sees may be anything: 0
-            const int key = key0 + r;
-            if (key < lo || key >= hi || (SINKS && key >= se && key < w0)) sc[j] = 0u;
+          for (int j = 0; j < 16 / kRowsStep; ++j) {
+            const int r = rb + kRowsStep * j;
+            cw[j] = *reinterpret_cast<const uint2*>(codes + r * (D / 2) + 8 * grp);
+            sc[j] = scales[r * kGroups + grp];
           }
-          const uint32_t f = q4_scale_pair(sc[j] | sc[j] << 8);
-          const uint4 a = make_uint4(mul_f16x2(q4_pair<0>(cw[j].x), f), mul_f16x2(q4_pair<1>(cw[j].x), f),
-                                     mul_f16x2(q4_pair<2>(cw[j].x), f), mul_f16x2(q4_pair<3>(cw[j].x), f));
-          const uint4 b = make_uint4(mul_f16x2(q4_pair<0>(cw[j].y), f), mul_f16x2(q4_pair<1>(cw[j].y), f),
-                                     mul_f16x2(q4_pair<2>(cw[j].y), f), mul_f16x2(q4_pair<3>(cw[j].y), f));
-          uint8_t* row = tile + half * kHalfBytes + r * 128;
-          const int x = r & 7;
-          *reinterpret_cast<uint4*>(row + (((ch + half) ^ x) << 4)) = half ? b : a;
-          *reinterpret_cast<uint4*>(row + (((ch + 1 - half) ^ x) << 4)) = half ? a : b;
+#pragma unroll
+          for (int j = 0; j < 16 / kRowsStep; ++j) {
+            const int r = rb + kRowsStep * j;
+            if (zero) {
+              // values of rows that no token of the unit sees may be anything: 0
+              const int key = key0 + r;
+              if (key < lo || key >= hi || (SINKS && key >= se && key < w0)) sc[j] = 0u;
+            }
+            const uint32_t f = q4_scale_pair(sc[j] | sc[j] << 8);
+            const uint32_t w0 = half ? cw[j].y : cw[j].x, w1 = half ? cw[j].x : cw[j].y;
+            uint8_t* row = tile + r * 128;
+            const int x = r & 7;
+            *reinterpret_cast<uint4*>(row + (((ch + half) ^ x) << 4)) =
+                make_uint4(mul_f16x2(q4_pair<0>(w0), f), mul_f16x2(q4_pair<1>(w0), f), mul_f16x2(q4_pair<2>(w0), f), mul_f16x2(q4_pair<3>(w0), f));
+            *reinterpret_cast<uint4*>(row + (((ch + 1 - half) ^ x) << 4)) =
+                make_uint4(mul_f16x2(q4_pair<0>(w1), f), mul_f16x2(q4_pair<1>(w1), f), mul_f16x2(q4_pair<2>(w1), f), mul_f16x2(q4_pair<3>(w1), f));
+          }
         }
         fence_proxy_async_smem();
-      };
-      const bool zero = !(flags & kFull);
-      if (c >= kSlots) ok = ok && wait(sm.bar_kfree[slot], ((c / kSlots) - 1) & 1);
+        arrive(kv ? sm.bar_v[slot] : sm.bar_k[slot]);
+      }
       if (!ok) break;
-      convert(s.kc, s.ks, sm.k[slot], false);
-      arrive(sm.bar_k[slot]);
-      if (c >= kSlots) ok = wait(sm.bar_vfree[slot], ((c / kSlots) - 1) & 1);
-      if (!ok) break;
-      convert(s.vc, s.vs, sm.v[slot], zero);
-      arrive(sm.bar_v[slot]);
       arrive(sm.bar_codefree[st]);
       ++c;
     }
     if (!ok) give_up();
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
     // -------------------------------------------------------------- softmax
-    const int row = tid, tl = row / p.g, hl = row - tl * p.g;
-    const uint32_t lane_tmem = tmem + (static_cast<uint32_t>(warp * 32) << 16);
-    const uint32_t o_tmem = lane_tmem + kColO;
-    uint32_t c = 0, units = 0;
-    Unit u{};
-    bool row_exists = false, seen = false, work = false, fresh = true;
-    int klo = 0, khi = 0, kse = 0, wlo = 0, whi = 0;  // this row's keys; those that all rows of the warp see
+    const int set = warp >> 2, row = tid & (kRows - 1);  // row: of tensor memory
+    const int upper = LEAN ? row >> 6 : 0, ur = LEAN ? row & 63 : row, tl = ur / p.g, hl = ur - tl * p.g;
+    const uint32_t lane_tmem = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const uint32_t s_tmem = lane_tmem + 128u * set, o_tmem = lane_tmem + kColO + 128u * set;
+    uint32_t c = 0, others = 0, units = 0, in_piece = 0;  // tiles of this set and of the other; units; tiles of the piece
+    uint32_t turns = 0;                                   // of the buffers that O passes through
+    bool seen = false;  // the row sees a key
     float m_ref = -INFINITY, l_sum = 0.f, scale = 0.f;
     for (uint32_t it = 0; ok; ++it) {
       ok = wait(sm.bar_info[it % kInfos], (it / kInfos) & 1);
       if (!ok) break;
       const TileInfo& info = sm.info[it % kInfos];
-      const int flags = info.flags, key0 = info.key0;
-      if (flags & kFirst) u = Unit{info.ntok, info.tok0, info.kvh, info.i0, info.n, info.C, info.ks};
-      arrive(sm.bar_infofree[it % kInfos]);
+      const int flags = info.flags;
       if (flags & kEnd) break;
       const bool empty = flags & kEmpty;
-      if (flags & kFirst) {
-        row_exists = tl < p.tb && tl < u.ntok;
-        klo = khi = kse = 0;
-        if (row_exists && !empty) {
+      // the keys that the row sees: [lo, hi), and of the first rows that stay visible those below se
+      auto row_keys = [&](int& lo, int& hi, int& se) {
+        lo = hi = se = 0;
+        if (tl < p.tb && tl < info.ntok && !empty) {
           ChunkSeq s;
-          s.n = u.n;
-          s.C = u.C;
-          s.ks = u.ks;
-          klo = key_lo(p.a, s, u.i0 + tl);
-          khi = key_hi(p.a, s, u.i0 + tl);
-          if constexpr (SINKS) kse = sink_end(p.a, s, khi);
+          s.n = info.n;
+          s.C = info.C;
+          s.ks = info.ks;
+          lo = key_lo(p.a, s, info.i0 + tl);
+          hi = key_hi(p.a, s, info.i0 + tl);
+          if constexpr (SINKS) se = sink_end(p.a, s, hi);
         }
-        seen = klo < khi;
-        work = __any_sync(full, seen);  // (a warp without a row that sees a key only keeps the hand-offs going)
-        wlo = __reduce_max_sync(full, klo);
-        whi = __reduce_min_sync(full, seen ? khi : (work ? 0x7fffffff : 0));
+      };
+      if (flags & kFirst) {
+        int lo, hi, se;
+        row_keys(lo, hi, se);
+        seen = lo < hi;
         m_ref = -INFINITY;
         l_sum = 0.f;
-        fresh = true;
+        in_piece = 0;
         if (!empty) {
-          // this thread's row of Q to fp16, in place
+          // this thread's row of Q: the power of two that its components take,
+          // and by the even set its fp16 form, in place of itself
           ok = wait(sm.bar_qraw, units & 1);
           if (!ok) break;
           uint4* qr[kHalves];
@@ -454,85 +480,78 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int hf = 0; hf < kHalves; ++hf) {
             qr[hf] = reinterpret_cast<uint4*>(sm.q + hf * kHalfBytes + row * 128);
+            if (set == 0) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const uint4 x = qr[hf][k ^ (row & 7)];
-              const uint32_t a = max(max(x.x & 0x7fffu, x.x >> 16 & 0x7fffu), max(x.y & 0x7fffu, x.y >> 16 & 0x7fffu));
-              const uint32_t b = max(max(x.z & 0x7fffu, x.z >> 16 & 0x7fffu), max(x.w & 0x7fffu, x.w >> 16 & 0x7fffu));
-              top = max(top, max(a, b));
+              for (int k = 0; k < 8; ++k) {
+                const uint4 x = qr[hf][k ^ (row & 7)];
+                const uint32_t a = max(max(x.x & 0x7fffu, x.x >> 16 & 0x7fffu), max(x.y & 0x7fffu, x.y >> 16 & 0x7fffu));
+                const uint32_t b = max(max(x.z & 0x7fffu, x.z >> 16 & 0x7fffu), max(x.w & 0x7fffu, x.w >> 16 & 0x7fffu));
+                top = max(top, max(a, b));
+              }
             }
           }
           float down, up;
           q_powers(top, down, up);
+          if (set == 0) {
+            sm.q_up[units & 1][row] = up;
+            auto half2_of = [&](uint32_t w) {
+              return pack_f16x2(__uint_as_float(w << 16) * down, __uint_as_float(w & 0xffff0000u) * down);
+            };
+#pragma unroll
+            for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const uint4 x = qr[hf][k ^ (row & 7)];
+                qr[hf][k ^ (row & 7)] = make_uint4(half2_of(x.x), half2_of(x.y), half2_of(x.z), half2_of(x.w));
+              }
+            fence_proxy_async_smem();
+            arrive(sm.bar_q);
+          } else {
+            ok = wait(sm.bar_q, units & 1);
+            if (!ok) break;
+            up = sm.q_up[units & 1][row];
+          }
           scale = up * p.scale_log2;
-          auto half2_of = [&](uint32_t w) {
-            return pack_f16x2(__uint_as_float(w << 16) * down, __uint_as_float(w & 0xffff0000u) * down);
-          };
-#pragma unroll
-          for (int hf = 0; hf < kHalves; ++hf)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const uint4 x = qr[hf][k ^ (row & 7)];
-              qr[hf][k ^ (row & 7)] = make_uint4(half2_of(x.x), half2_of(x.y), half2_of(x.z), half2_of(x.w));
-            }
-          fence_proxy_async_smem();
-          arrive(sm.bar_q);
           ++units;
         }
       }
-      if (!empty) {
-        const uint32_t buf = c & 1, par = (c >> 1) & 1;
-        const uint32_t s_tmem = lane_tmem + 128u * buf;
-        ok = wait(sm.bar_s[buf], par);
+      if (!empty && (in_piece & 1) != static_cast<uint32_t>(set)) {
+        ++others;  // the other set's tile
+      } else if (!empty) {
+        ok = wait(sm.bar_s[set], c & 1);
         if (!ok) break;
-        if (!work) {
-          arrive(sm.bar_p[buf][0]);
-          arrive(sm.bar_p[buf][1]);
+        // (a warp without a row that sees a key only keeps the hand-offs going)
+        if (!__any_sync(full, seen)) {
+          arrive(sm.bar_p[set][0]);
+          arrive(sm.bar_p[set][1]);
         } else {
           tc_fence_after();
-          uint32_t xs[4][32];
+          // 64 columns of S, the keys that the row does not see at -inf
+          uint32_t xs[2][32];
+          auto load = [&](int hp) {
+            tmem_ld32(s_tmem + 64 * hp, xs[0]);
+            tmem_ld32(s_tmem + 64 * hp + 32, xs[1]);
+            tmem_wait_ld();
+            if (!(flags & kFull)) {
+              int lo, hi, kse;
+              row_keys(lo, hi, kse);
+              const int key0 = info.key0, ks = info.ks;
+              const int from = min(max(lo - key0, 0), kTile), to = min(max(hi - key0, 0), kTile);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) tmem_ld32(s_tmem + 32 * q, xs[q]);
-          tmem_wait_ld();
-          if (key0 < wlo || key0 + kTile > whi) {
-            // this row's keys within the tile
-            const int from = min(max(klo - key0, 0), kTile), to = min(max(khi - key0, 0), kTile);
+              for (int wd = 0; wd < 2; ++wd) {
+                const int at = 64 * hp + 32 * wd;
+                const int f = min(max(from - at, 0), 32), e = min(max(to - at, 0), 32);
+                uint32_t keep = e > f ? (0xffffffffu >> (32 - (e - f))) << f : 0u;  // bits f .. e-1
+                if constexpr (SINKS) {
+                  const int sf = min(max(ks - key0 - at, 0), 32), se = min(max(kse - key0 - at, 0), 32);
+                  keep |= se > sf ? (0xffffffffu >> (32 - (se - sf))) << sf : 0u;
+                }
 #pragma unroll
-            for (int wd = 0; wd < 4; ++wd) {
-              const int f = min(max(from - 32 * wd, 0), 32), e = min(max(to - 32 * wd, 0), 32);
-              uint32_t keep = e > f ? (0xffffffffu >> (32 - (e - f))) << f : 0u;  // bits f .. e-1
-              if constexpr (SINKS) {
-                const int sf = min(max(u.ks - key0 - 32 * wd, 0), 32), se = min(max(kse - key0 - 32 * wd, 0), 32);
-                keep |= se > sf ? (0xffffffffu >> (32 - (se - sf))) << sf : 0u;
+                for (int k = 0; k < 32; ++k) xs[wd][k] = (keep >> k) & 1u ? xs[wd][k] : 0xff800000u;
               }
-#pragma unroll
-              for (int k = 0; k < 32; ++k) xs[wd][k] = (keep >> k) & 1u ? xs[wd][k] : 0xff800000u;
-            }
-          }
-          // The half's probabilities against the reference that the row has,
-          // and beside them the row's maximum, which tells whether that
-          // reference still serves; where it does not, and on a piece's first
-          // tile, the half is done (again) with the reference moved.
-          const unsigned long long sc2 = f32x2(scale, scale);
-          unsigned long long acc[2], nm2;
-          auto half = [&](int hp) {
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              uint32_t pk[16];
-#pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                float e0, e1;
-                f32x2_split(fma_f32x2(f32x2(__uint_as_float(xs[2 * hp + q][2 * k]), __uint_as_float(xs[2 * hp + q][2 * k + 1])),
-                                      sc2, nm2),
-                            e0, e1);
-                const float p0 = fast_exp2(e0), p1 = fast_exp2(e1);
-                acc[k & 1] = add_f32x2(acc[k & 1], f32x2(p0, p1));
-                pk[k] = pack_f16x2(p0, p1);
-              }
-              tmem_st16(s_tmem + 32 * hp + 16 * q, pk);
             }
           };
-          auto row_max = [&]() {
+          auto max_of = [&]() {
             float r[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) r[k] = fmax3(__uint_as_float(xs[0][k]), __uint_as_float(xs[0][k + 8]), __uint_as_float(xs[0][k + 16]));
@@ -541,36 +560,24 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int k = 0; k < 8; ++k) r[k] = fmax3(r[k], __uint_as_float(xs[1][k + 8]), __uint_as_float(xs[1][k + 16]));
 #pragma unroll
-            for (int k = 0; k < 8; ++k) r[k] = fmax3(r[k], __uint_as_float(xs[1][k + 24]), __uint_as_float(xs[2][k]));
-#pragma unroll
-            for (int k = 0; k < 8; ++k) r[k] = fmax3(r[k], __uint_as_float(xs[2][k + 8]), __uint_as_float(xs[2][k + 16]));
-#pragma unroll
-            for (int k = 0; k < 8; ++k) r[k] = fmax3(r[k], __uint_as_float(xs[2][k + 24]), __uint_as_float(xs[3][k]));
-#pragma unroll
-            for (int k = 0; k < 8; ++k) r[k] = fmax3(r[k], __uint_as_float(xs[3][k + 8]), __uint_as_float(xs[3][k + 16]));
-#pragma unroll
-            for (int k = 0; k < 8; ++k) r[k] = fmaxf(r[k], __uint_as_float(xs[3][k + 24]));
-            return fmax3(fmax3(r[0], r[1], r[2]), fmax3(r[3], r[4], r[5]), fmaxf(r[6], r[7])) * scale;
+            for (int k = 0; k < 8; ++k) r[k] = fmaxf(r[k], __uint_as_float(xs[1][k + 24]));
+            return fmax3(fmax3(r[0], r[1], r[2]), fmax3(r[3], r[4], r[5]), fmaxf(r[6], r[7]));
           };
-          auto start_half = [&]() {
-            const float neg_m = m_ref != -INFINITY ? -m_ref : 0.f;
-            nm2 = f32x2(neg_m, neg_m);
-            acc[0] = acc[1] = f32x2(0.f, 0.f);
-          };
-          start_half();
-          half(0);
-          const float mx = row_max();
+          float mx = -INFINITY;
+          if constexpr (!LEAN) {
+            load(1);
+            mx = max_of();
+          }
+          load(upper);
+          mx = fmaxf(mx, max_of()) * scale;
           const bool move = seen && mx != -INFINITY && (m_ref == -INFINITY || mx > m_ref + kRescaleThreshold);
           if (__any_sync(full, move)) {
-            // the first stores of the half are complete before those that
-            // replace them are issued (only a wait orders two of them)
-            tmem_wait_st();
             const float f = move && m_ref != -INFINITY ? fast_exp2(m_ref - mx) : 1.0f;
             l_sum *= f;
             if (move) m_ref = mx;
-            if (!fresh) {
-              // O holds the piece's earlier tiles once the PV before this one is done
-              ok = wait(sm.bar_pv, (c - 1) & 1);
+            if (in_piece >= 2) {
+              // O holds the set's earlier tiles once its last PV is done
+              ok = wait(sm.bar_pv[set], (c - 1) & 1);
               if (!ok) break;
               tc_fence_after();
 #pragma unroll 1
@@ -583,70 +590,143 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tmem_st16(o_tmem + 16 * q, o);
               }
             }
-            start_half();
-            half(0);
           }
-          auto hand_over = [&](int hp) {
+          const float neg_m = m_ref != -INFINITY ? -m_ref : 0.f;
+          const unsigned long long sc2 = f32x2(scale, scale), nm2 = f32x2(neg_m, neg_m);
+          unsigned long long acc[2] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
+          if constexpr (LEAN) {
+            // the keys of the other half of the lanes
+            const uint32_t none[16] = {};
+            tmem_st16(s_tmem + 32 * (1 - upper), none);
+            tmem_st16(s_tmem + 32 * (1 - upper) + 16, none);
+          }
+#pragma unroll 1
+          for (int h = 0; h < (LEAN ? 1 : 2); ++h) {
+            const int hp = LEAN ? upper : h;
+            if (h == 1) load(1);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              uint32_t pk[16];
+#pragma unroll
+              for (int k = 0; k < 16; ++k) {
+                float e0, e1;
+                f32x2_split(fma_f32x2(f32x2(__uint_as_float(xs[q][2 * k]), __uint_as_float(xs[q][2 * k + 1])), sc2, nm2), e0, e1);
+                const float p0 = fast_exp2(e0), p1 = fast_exp2(e1);
+                acc[k & 1] = add_f32x2(acc[k & 1], f32x2(p0, p1));
+                pk[k] = pack_f16x2(p0, p1);
+              }
+              tmem_st16(s_tmem + 32 * hp + 16 * q, pk);
+            }
             tmem_wait_st();
             tc_fence_before();
-            arrive(sm.bar_p[buf][hp]);
-          };
-          hand_over(0);
-          half(1);
-          hand_over(1);
+            if constexpr (LEAN) arrive(sm.bar_p[set][hp ^ 1]);
+            arrive(sm.bar_p[set][hp]);
+          }
           float s0, s1;
           f32x2_split(add_f32x2(acc[0], acc[1]), s0, s1);
           l_sum += s0 + s1;
         }
-        fresh = false;
         ++c;
       }
+      if (!empty) ++in_piece;
       if (flags & kLastPiece) pdl_launch_next();
-      if (!(flags & kLast)) continue;
+      if (!(flags & kLast)) {
+        arrive(sm.bar_infofree[it % kInfos]);
+        continue;
+      }
 
-      // ---- epilogue (a sum that is NaN is passed on, not hidden)
+      // ---- epilogue: the sets' sums, and half the columns of O for each set
+      // (a sum that is NaN is passed on, not hidden)
+      const bool bad = flags & kBad, part = flags & kPart, row_exists = tl < p.tb && tl < info.ntok;
+      const size_t out_row = static_cast<size_t>(info.tok0 + (row_exists ? tl : 0)) * p.a.Hq + info.kvh * p.g + hl;
+      arrive(sm.bar_infofree[it % kInfos]);
+      float M = -INFINITY, L = 0.f, mine = 0.f, theirs = 0.f;
       if (!empty) {
-        ok = wait(sm.bar_pv, (c - 1) & 1);
+        float2(*ml)[kRows] = sm.ml[units & 1];
+        ml[set][row] = make_float2(m_ref, l_sum);
+        arrive(sm.bar_meet);
+        ok = wait(sm.bar_meet, (units - 1) & 1);
+        if (c > 0) ok = ok && wait(sm.bar_pv[set], (c - 1) & 1);
+        if (others > 0) ok = ok && wait(sm.bar_pv[set ^ 1], (others - 1) & 1);
         if (!ok) break;
         tc_fence_after();
+        const float2 x = ml[set ^ 1][row];
+        M = fmaxf(m_ref, x.x);
+        if constexpr (LEAN) M = fmaxf(M, fmaxf(ml[0][row ^ 64].x, ml[1][row ^ 64].x));
+        const float ref = M == -INFINITY ? 0.f : M;
+        mine = fast_exp2(m_ref - ref);
+        theirs = fast_exp2(x.x - ref);
+        L = fmaf(mine, l_sum, theirs * x.y);
+        if constexpr (LEAN) {
+          const float2 y = ml[0][row ^ 64], z = ml[1][row ^ 64];
+          L += fmaf(fast_exp2(y.x - ref), y.y, fast_exp2(z.x - ref) * z.y);
+        }
       }
-      const bool bad = flags & kBad, part = flags & kPart;
-      const bool any = !empty && seen && l_sum != 0.f && !bad;
-      const float inv = any ? p.c.v_unit / l_sum : 0.f;
+      const bool any = !empty && seen && L != 0.f && !bad;
+      const float norm = !any ? 0.f : part ? 1.f : p.c.v_unit / L;
+      mine *= norm;
+      theirs *= norm;
       const int entry = static_cast<int>(blockIdx.x) * 2 + (flags & kSlot1 ? 1 : 0);
-      const size_t out_row = static_cast<size_t>(u.tok0 + (row_exists ? tl : 0)) * p.a.Hq + u.kvh * p.g + hl;
       uint4* orow = reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.a.out) + out_row * (2 * D));
 #pragma unroll 1
-      for (int q = 0; q < D / 16; ++q) {
-        uint32_t o[16];
-        if (!empty) {
-          tmem_ld16(o_tmem + 16 * q, o);
-          tmem_wait_ld();
-          if (q == D / 16 - 1) {
-            // O may be overwritten by the next unit's first PV
-            tc_fence_before();
-            arrive(sm.bar_ofree);
+      for (int q = set * (D / 32); q < (set + 1) * (D / 32); ++q) {
+        float o[16];
+        {
+          uint32_t a[16], b[16];
+          // (the sets' tiles in the piece: half of them, the even set's rounded up)
+          const bool have = in_piece > static_cast<uint32_t>(set), have_other = in_piece > static_cast<uint32_t>(set ^ 1);
+          if (have) tmem_ld16(o_tmem + 16 * q, a);
+          if (have_other) tmem_ld16(lane_tmem + kColO + 128u * (set ^ 1) + 16 * q, b);
+          if (!empty) tmem_wait_ld();
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            o[k] = have ? __uint_as_float(a[k]) * mine : 0.f;
+            if (have_other) o[k] = fmaf(__uint_as_float(b[k]), theirs, o[k]);
           }
+        }
+        if (!empty && q == (set + 1) * (D / 32) - 1) {
+          // both O may be overwritten by the next unit's first PVs
+          tc_fence_before();
+          arrive(sm.bar_ofree);
+        }
+        if constexpr (LEAN) {
+          // the upper lanes' share goes to the lower ones
+          if (!empty) {
+            const uint32_t buf = turns & 1, use = turns >> 1;
+            float(*to)[kRows / 2] = sm.o[set][buf];
+            if (upper) {
+              if (use > 0) ok = ok && wait(sm.bar_xfree[set][buf], (use - 1) & 1);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) to[k][ur] = o[k];
+              arrive(sm.bar_x[set][buf]);
+            } else {
+              ok = ok && wait(sm.bar_x[set][buf], use & 1);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) o[k] += to[k][ur];
+              arrive(sm.bar_xfree[set][buf]);
+            }
+            ++turns;
+          }
+          if (upper) continue;
         }
         if (!row_exists) continue;
         if (part) {
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            *partial_o<D>(p, entry, 4 * q + k, row) =
-                any ? make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]),
-                                  __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]))
-                    : make_float4(0.f, 0.f, 0.f, 0.f);
+            *partial_o<D>(p, entry, 4 * q + k, ur) =
+                any ? make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
         } else {
           uint32_t wv[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            wv[e] = any ? pack_bf16x2(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
+          for (int e = 0; e < 8; ++e) wv[e] = any ? pack_bf16x2(o[2 * e], o[2 * e + 1]) : 0u;
           orow[2 * q] = make_uint4(wv[0], wv[1], wv[2], wv[3]);
           orow[2 * q + 1] = make_uint4(wv[4], wv[5], wv[6], wv[7]);
         }
       }
-      if (row_exists && part) *partial_ml<D>(p, entry, row) = make_float2(any ? m_ref : -INFINITY, any ? l_sum : bad ? -1.f : 0.f);
-      if (row_exists && !part && p.a.lse) p.a.lse[out_row] = any ? (m_ref + log2f(l_sum)) * kLn2 : -INFINITY;
+      if (row_exists && set == 0 && !upper) {
+        if (part) *partial_ml<D>(p, entry, ur) = make_float2(any ? M : -INFINITY, any ? L : bad ? -1.f : 0.f);
+        if (!part && p.a.lse) p.a.lse[out_row] = any ? (M + log2f(L)) * kLn2 : -INFINITY;
+      }
     }
     if (!ok) give_up();
   }
@@ -700,13 +780,15 @@ __global__ void __launch_bounds__(2 * D) chunk_q4_tc_merge_kernel(const __grid_c
   }
 }
 
-template <int D, bool SINKS>
-cudaError_t launch_d(Q4TcParams p, int num_sms, EncodeTiledFn encode, cudaStream_t stream) {
+template <int D, bool SINKS, bool LEAN>
+cudaError_t launch_lean(Q4TcParams p, int num_sms, EncodeTiledFn encode, cudaStream_t stream) {
+  p.tb = (LEAN ? kRows / 2 : kRows) / p.g;
   CUtensorMap tq;
   const cuuint64_t dims[3] = {D, static_cast<cuuint64_t>(p.a.Hq), static_cast<cuuint64_t>(p.a.T)};
   const cuuint64_t strides[2] = {D * 2ull, static_cast<cuuint64_t>(p.a.q_stride) * 2ull};
   const cuuint32_t box[3] = {64u, static_cast<cuuint32_t>(p.g), static_cast<cuuint32_t>(p.tb)};
   if (!make_bf16_map(encode, &tq, p.a.q, 3, dims, strides, box)) return cudaErrorInvalidValue;
+  constexpr size_t bytes = smem_bytes<D, LEAN>();
   static std::mutex mu;
   static bool done[64] = {};
   int dev = 0;
@@ -716,18 +798,26 @@ cudaError_t launch_d(Q4TcParams p, int num_sms, EncodeTiledFn encode, cudaStream
   {
     std::lock_guard<std::mutex> lk(mu);
     if (!done[dev]) {
-      e = cudaFuncSetAttribute(chunk_q4_tc_kernel<D, SINKS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                               static_cast<int>(smem_bytes<D>()));
+      e = cudaFuncSetAttribute(chunk_q4_tc_kernel<D, SINKS, LEAN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               static_cast<int>(bytes));
       if (e != cudaSuccess) return e;
       done[dev] = true;
     }
   }
   p.ctas = num_sms;
-  e = launch_overlapped(chunk_q4_tc_kernel<D, SINKS>, dim3(static_cast<unsigned>(p.ctas)), dim3(kThreads), smem_bytes<D>(),
+  e = launch_overlapped(chunk_q4_tc_kernel<D, SINKS, LEAN>, dim3(static_cast<unsigned>(p.ctas)), dim3(kThreads), bytes,
                         stream, 1u, tq, p);
   if (e != cudaSuccess || p.ctas == 1) return e;
   return launch_overlapped(chunk_q4_tc_merge_kernel<D>, dim3(static_cast<unsigned>(p.ctas - 1), 8u), dim3(2 * D), 0,
                            stream, 1u, p);
+}
+
+// Lean units where a sequence has up to 64 query rows a KV head on average.
+template <int D, bool SINKS>
+cudaError_t launch_d(const Q4TcParams& p, int num_sms, EncodeTiledFn encode, cudaStream_t stream) {
+  const bool lean = p.g <= kRows / 2 && static_cast<long long>(p.a.T) * p.g <= static_cast<long long>(kRows / 2) * p.a.Bt;
+  return lean ? launch_lean<D, SINKS, true>(p, num_sms, encode, stream)
+              : launch_lean<D, SINKS, false>(p, num_sms, encode, stream);
 }
 
 }  // namespace
@@ -742,7 +832,6 @@ cudaError_t launch_chunk_attention_q4_tc(const ChunkArgs& a, const simsd_q4_cach
   p.a = a;
   p.c = c;
   p.g = a.Hq / a.Hkv;
-  p.tb = kRows / p.g;
   p.sub = a.page_size % kTile == 0 ? kTile : std::min(a.page_size, 64);
   p.scale_log2 = a.scale * c.k_unit * 1.4426950408889634f;
   if (a.sinks > 0) return a.d == 128 ? launch_d<128, true>(p, num_sms, encode, stream) : launch_d<64, true>(p, num_sms, encode, stream);
