@@ -24,8 +24,8 @@
 // Warp roles (640 threads): warps 0-3 softmax of the even tiles, 4-7 of the
 // odd ones (thread i of a set owns query row i = TMEM lane i; the even set
 // turns Q into fp16 in place); warps 8-15 K and V; warp 16 walks the run and
-// issues all copies; warp 17 the MMAs, in the order S(0) S(1) PV(0) S(2) PV(1)
-// ... of a unit.
+// issues all copies; warps 17 and 18 the MMAs of the two sets, each its S and
+// PV in turns (one warp for both took 2690 cycles a tile, half of them waits).
 // Lean units, of up to 64 rows, have their rows of Q twice, in the lanes 0-63
 // and 64-127: the first take a tile's first 64 keys, the others the last 64,
 // and set the P of the keys that are not theirs to zero.  All four partitions
@@ -57,12 +57,13 @@ namespace {
 constexpr int kTile = kQ4Tile;
 constexpr int kRows = 128;  // query rows of a unit (MMA M)
 constexpr int kThreads = 640;
-constexpr int kSoftmaxWarps = 8, kWarpConvert = 8, kConvertWarps = 8, kWarpWalk = 16, kWarpMma = 17;
+constexpr int kSoftmaxWarps = 8, kWarpConvert = 8, kConvertWarps = 8,  // (half of them K, half V)
+              kWarpWalk = 16, kWarpMma = 17;  // (warp 18: the MMAs of the odd set)
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColO = 256;  // + 128 per set
 constexpr int kHalfBytes = kTile * 128;  // 128 rows x 64 fp16
 constexpr int kInfos = 8;                // tiles that the walk is ahead of the last reader
-constexpr int kInfoReaders = kSoftmaxWarps + kConvertWarps + 1;
+constexpr int kInfoReaders = kSoftmaxWarps + kConvertWarps + 2;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -88,7 +89,7 @@ struct alignas(1024) SmemQ4Tc {
   uint64_t bar_k[kSlots], bar_kfree[kSlots], bar_v[kSlots], bar_vfree[kSlots];
   uint64_t bar_info[kInfos], bar_infofree[kInfos];
   uint64_t bar_qraw, bar_q, bar_qfree;
-  uint64_t bar_s[2], bar_p[2][2], bar_pv[2], bar_ofree, bar_meet, bar_drain;
+  uint64_t bar_s[2], bar_p[2][2], bar_pv[2], bar_ofree, bar_meet, bar_drain[2];
   float2 ml[2][2][kRows];  // (m, l) of the sets, for pieces in turns
   float q_up[2][kRows];    // the powers of two that Q was divided by, for units in turns
   // lean units: O of the upper lanes on its way to the lower ones, 16 columns
@@ -148,8 +149,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(smem_u32(&sm.bar_codefree[s]), kConvertWarps);
     }
     for (int s = 0; s < kSlots; ++s) {
-      mbar_init(smem_u32(&sm.bar_k[s]), kConvertWarps);
-      mbar_init(smem_u32(&sm.bar_v[s]), kConvertWarps);
+      mbar_init(smem_u32(&sm.bar_k[s]), kConvertWarps / 2);
+      mbar_init(smem_u32(&sm.bar_v[s]), kConvertWarps / 2);
       mbar_init(smem_u32(&sm.bar_kfree[s]), 1);
       mbar_init(smem_u32(&sm.bar_vfree[s]), 1);
     }
@@ -159,7 +160,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     mbar_init(smem_u32(&sm.bar_qraw), 1);
     mbar_init(smem_u32(&sm.bar_q), 4);
-    mbar_init(smem_u32(&sm.bar_qfree), 1);
+    mbar_init(smem_u32(&sm.bar_qfree), 2);
     for (int x = 0; x < 2; ++x) {
       mbar_init(smem_u32(&sm.bar_s[x]), 1);
       mbar_init(smem_u32(&sm.bar_p[x][0]), 4);
@@ -169,7 +170,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(smem_u32(&sm.bar_pv[1]), 1);
     mbar_init(smem_u32(&sm.bar_ofree), kSoftmaxWarps);
     mbar_init(smem_u32(&sm.bar_meet), kSoftmaxWarps);
-    mbar_init(smem_u32(&sm.bar_drain), 1);
+    mbar_init(smem_u32(&sm.bar_drain[0]), 1);
+    mbar_init(smem_u32(&sm.bar_drain[1]), 1);
     for (int x = 0; x < 4; ++x) {
       mbar_init(smem_u32(&sm.bar_x[x >> 1][x & 1]), 2);
       mbar_init(smem_u32(&sm.bar_xfree[x >> 1][x & 1]), 2);
@@ -271,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (units > 0) mbar_wait(smem_u32(&sm.bar_qraw), (units - 1) & 1, nullptr);
       }
       __syncwarp();
-    } else if (warp == kWarpMma) {
+    } else if (warp <= kWarpMma + 1) {
       // ----------------------------------------------------------------- MMAs
       constexpr uint32_t kIdescQK = idesc_f16_f32(kRows, kTile, 0);
       constexpr uint32_t kIdescPV = idesc_f16_f32(kRows, D, 1);
@@ -282,69 +284,72 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr uint32_t kTileStep = Smem::kTileBytes >> 4;
       const bool leader = elect_one();
       auto poll = [&](uint64_t& bar, uint32_t parity) { return mbar_wait_poll(smem_u32(&bar), parity, abort_flag); };
-      // messages read; tiles whose S, and whose PV, is issued; units begun; of
-      // each set the tiles whose PV is issued, and known to be done
-      uint32_t it = 0, cs = 0, cp = 0, units = 0, issued[2] = {0, 0}, done[2] = {0, 0};
+      const int x = warp - kWarpMma;
+      const uint32_t scol = tmem + 128u * x, ocol = tmem + kColO + 128u * x;
+      uint32_t it = 0, tile = 0, c = 0, units = 0;  // messages read; tiles of the run; of this set; units begun
       auto message = [&]() {
-        int flags = kEnd;
         ok = ok && poll(sm.bar_info[it % kInfos], (it / kInfos) & 1);
-        if (ok) {
-          flags = sm.info[it % kInfos].flags;
-          arrive(sm.bar_infofree[it % kInfos]);
-          ++it;
-        }
+        const int flags = ok ? sm.info[it % kInfos].flags : kEnd;
+        if (ok) arrive(sm.bar_infofree[it % kInfos]);
+        ++it;
         return flags;
-      };
-      // S of the next tile, for set x: its K is there, and the set's last PV,
-      // whose P lies in the same columns, is done
-      auto issue_s = [&](int x, bool qdone) {
-        const uint32_t slot = cs % kSlots;
-        ok = ok && poll(sm.bar_k[slot], (cs / kSlots) & 1);
-        if (done[x] < issued[x]) {
-          ok = ok && poll(sm.bar_pv[x], done[x] & 1);
-          ++done[x];
-        }
-        if (ok && leader) {
-          tc_fence_after();
-          const uint32_t b = k_lo + slot * kTileStep;
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
-            const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
-            tc_mma_ss_lh(tmem + 128u * x, q_lo + off, k_hi, b + off, k_hi, kIdescQK, kk > 0);
-          }
-          tc_commit(smem_u32(&sm.bar_s[x]));
-          tc_commit(smem_u32(&sm.bar_kfree[slot]));
-          if (qdone) tc_commit(smem_u32(&sm.bar_qfree));
-        }
-        __syncwarp();
-        ++cs;
       };
       while (ok) {
         int flags = message();
         if (flags & kEnd) break;
         if (flags & kEmpty) continue;
-        ok = ok && poll(sm.bar_q, units & 1);
-        issue_s(0, flags & kLast);
-        for (int i = 0; ok; ++i) {
-          const bool last = flags & kLast;
-          const int x = i & 1;
-          if (!last) {
-            flags = message();
-            issue_s(x ^ 1, flags & kLast);
+        ++units;
+        uint32_t j = x;  // tile of the piece
+        bool more = true;
+        if (x == 1) {
+          more = !(flags & kLast);
+          if (more) flags = message();
+        }
+        const uint32_t tile0 = tile;
+        tile += x == 1 && !more ? 1 : 0;
+        for (bool begin = true; ok && more; begin = false) {
+          const uint32_t n = tile0 + j, slot = n % kSlots, par = (n / kSlots) & 1;
+          if (begin) ok = poll(sm.bar_q, (units - 1) & 1);
+          ok = ok && poll(sm.bar_k[slot], par);
+          // the set's last PV, whose P lies in the same columns, is done
+          if (c > 0) ok = ok && poll(sm.bar_pv[x], (c - 1) & 1);
+          __syncwarp();
+          if (ok && leader) {
+            tc_fence_after();
+            const uint32_t b = k_lo + slot * kTileStep;
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+              const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
+              tc_mma_ss_lh(scol, q_lo + off, k_hi, b + off, k_hi, kIdescQK, kk > 0);
+            }
+            tc_commit(smem_u32(&sm.bar_s[x]));
+            tc_commit(smem_u32(&sm.bar_kfree[slot]));
           }
-          const uint32_t slot = cp % kSlots, par = issued[x] & 1;
-          ok = ok && poll(sm.bar_v[slot], (cp / kSlots) & 1);
-          // the unit's first PV overwrites an O: the epilogue of the unit before has read both
-          if (i == 0 && units > 0) ok = ok && poll(sm.bar_ofree, (units - 1) & 1);
-          const uint32_t b = v_lo + slot * kTileStep, pcol = tmem + 128u * x, ocol = tmem + kColO + 128u * x;
+          __syncwarp();
+          // the set's next tile is looked up under the softmax of this one; not
+          // beyond the piece, whose end has to be told before the walk goes on
+          bool last = flags & kLast;
+          if (last) {
+            tile = n + 1;
+          } else {
+            last = message() & kLast;
+            tile = n + 2;
+            if (!last) flags = message();
+          }
+          more = !last;
+          ok = ok && poll(sm.bar_v[slot], par);
+          // the unit's first PV overwrites O: the epilogue of the unit before has read it
+          if (begin && units > 1) ok = ok && poll(sm.bar_ofree, (units - 2) & 1);
+          const uint32_t b = v_lo + slot * kTileStep;
 #pragma unroll
           for (int hp = 0; hp < 2; ++hp) {
-            ok = ok && poll(sm.bar_p[x][hp], par);
+            ok = ok && poll(sm.bar_p[x][hp], c & 1);
+            __syncwarp();
             if (ok && leader) {
               tc_fence_after();
 #pragma unroll
               for (int kk = 4 * hp; kk < 4 * hp + 4; ++kk)
-                tc_mma_ts_lh(ocol, pcol + 8 * kk, b + kk * 128, v_hi, kIdescPV, (i < 2 && kk == 0) ? 0u : 1u);
+                tc_mma_ts_lh(ocol, scol + 8 * kk, b + kk * 128, v_hi, kIdescPV, (begin && kk == 0) ? 0u : 1u);
               if (hp == 1) {
                 tc_commit(smem_u32(&sm.bar_pv[x]));
                 tc_commit(smem_u32(&sm.bar_vfree[slot]));
@@ -352,31 +357,30 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             __syncwarp();
           }
-          if (!ok) break;
-          ++issued[x];
-          ++cp;
-          if (last) break;
+          ++c;
+          j += 2;
         }
-        ++units;
+        // Q is free once both sets are done with it (their last P was formed from S)
+        if (ok) arrive(sm.bar_qfree);
       }
       if (!ok) give_up();
       if (leader) {
-        tc_commit(smem_u32(&sm.bar_drain));
-        mbar_wait(smem_u32(&sm.bar_drain), 0, nullptr);
+        tc_commit(smem_u32(&sm.bar_drain[x]));
+        mbar_wait(smem_u32(&sm.bar_drain[x]), 0, nullptr);
       }
       __syncwarp();
     }
   } else if (warp >= kWarpConvert) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     // ------------------------------------------------- codes to tiles of K and V
-    // A warp takes 16 rows; a lane one group of 16 components of a row at a
+    // A warp takes 32 rows; a lane one group of 16 components of a row at a
     // time: 8 bytes of codes, a scale, two chunks of 16 bytes.  Lanes of the
     // upper 64 components write their second chunk first: eight lanes then
     // fill eight different chunks of 128 bytes.
     constexpr int kGroups = D / kQ4Group, kRowsStep = 32 / kGroups;
-    const int w = warp - kWarpConvert, grp = lane & (kGroups - 1);
+    const int w = warp & 3, kv = (warp - kWarpConvert) >> 2, grp = lane & (kGroups - 1);
     const int half = grp >> 2, ch = (grp & 3) * 2;
-    const int rb = 16 * w + lane / kGroups;
+    const int r0 = 32 * w + lane / kGroups;
     uint32_t c = 0;
     for (uint32_t it = 0; ok; ++it) {
       ok = wait(sm.bar_info[it % kInfos], (it / kInfos) & 1);
@@ -389,15 +393,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t st = c % kStages, slot = c % kSlots;
       const Stage<D>& s = sm.ring[st];
       ok = wait(sm.bar_code[st], (c / kStages) & 1);
-#pragma unroll 1
-      for (int kv = 0; ok && kv < 2; ++kv) {
-        uint64_t& taken = kv ? sm.bar_vfree[slot] : sm.bar_kfree[slot];
-        if (c >= kSlots) ok = wait(taken, ((c / kSlots) - 1) & 1);
-        if (!ok) break;
+      if (c >= kSlots) ok = ok && wait(kv ? sm.bar_vfree[slot] : sm.bar_kfree[slot], ((c / kSlots) - 1) & 1);
+      if (!ok) break;
+      {
         const uint8_t *codes = kv ? s.vc : s.kc, *scales = kv ? s.vs : s.ks;
         uint8_t* tile = (kv ? sm.v[slot] : sm.k[slot]) + half * kHalfBytes;
         const bool zero = kv && !(flags & kFull);
-        {
+#pragma unroll 1
+        for (int rb = r0; rb < r0 + 32; rb += 16) {
           uint2 cw[16 / kRowsStep];
           uint32_t sc[16 / kRowsStep];
 #pragma unroll
@@ -415,13 +418,13 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (key < lo || key >= hi || (SINKS && key >= se && key < w0)) sc[j] = 0u;
             }
             const uint32_t f = q4_scale_pair(sc[j] | sc[j] << 8);
-            const uint32_t w0 = half ? cw[j].y : cw[j].x, w1 = half ? cw[j].x : cw[j].y;
+            const uint32_t ca = half ? cw[j].y : cw[j].x, cb = half ? cw[j].x : cw[j].y;
             uint8_t* row = tile + r * 128;
             const int x = r & 7;
             *reinterpret_cast<uint4*>(row + (((ch + half) ^ x) << 4)) =
-                make_uint4(mul_f16x2(q4_pair<0>(w0), f), mul_f16x2(q4_pair<1>(w0), f), mul_f16x2(q4_pair<2>(w0), f), mul_f16x2(q4_pair<3>(w0), f));
+                make_uint4(mul_f16x2(q4_pair<0>(ca), f), mul_f16x2(q4_pair<1>(ca), f), mul_f16x2(q4_pair<2>(ca), f), mul_f16x2(q4_pair<3>(ca), f));
             *reinterpret_cast<uint4*>(row + (((ch + 1 - half) ^ x) << 4)) =
-                make_uint4(mul_f16x2(q4_pair<0>(w1), f), mul_f16x2(q4_pair<1>(w1), f), mul_f16x2(q4_pair<2>(w1), f), mul_f16x2(q4_pair<3>(w1), f));
+                make_uint4(mul_f16x2(q4_pair<0>(cb), f), mul_f16x2(q4_pair<1>(cb), f), mul_f16x2(q4_pair<2>(cb), f), mul_f16x2(q4_pair<3>(cb), f));
           }
         }
         fence_proxy_async_smem();
