@@ -569,13 +569,13 @@ SIMSD_API int simsd_q4_expand(int dtype, const simsd_q4_cache* cache, int num_pa
  * simsd_chunk_attention_q4 -- simsd_chunk_attention_sinks over a cache in 4
  * bits (sinks = 0: simsd_chunk_attention).  q and out are dtype.  The same
  * masks, error rules and limits.
- * SIMSD_BF16 with up to 64 query rows a sequence and KV head on average (T Hq
- * <= 64 Bt Hkv, Hq / Hkv <= 64, Bt <= 8192) reads the codes; keys and values are exact in
- * the products' fp16, q is scaled by a power of two to its row's largest
- * component, probabilities are rounded to fp16.  More rows, and SIMSD_F32, go
- * through an image of the rows that are seen in dtype, with the cache's page
- * ids, in the workspace (num_pages Hkv page_size d elements of keys and of
- * values): make the workspace once for all layers of a model.
+ * SIMSD_BF16 with up to 256 query rows a sequence and KV head on average (T Hq
+ * <= 256 Bt Hkv) reads the codes: keys and values are exact in the products'
+ * fp16, q is scaled by a power of two to its row's largest component,
+ * probabilities are rounded to fp16.  More rows, and SIMSD_F32, go through an
+ * image of the rows that are seen in dtype, with the cache's page ids, in the
+ * workspace (num_pages Hkv page_size d elements of keys and of values): make
+ * the workspace once for all layers of a model.
  */
 SIMSD_API size_t simsd_chunk_q4_workspace_bytes(int dtype, int T, int Bt, int Hq, int Hkv, int d, int max_pages,
                                                 int page_size, int num_pages);

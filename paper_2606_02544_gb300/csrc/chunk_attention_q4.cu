@@ -20,11 +20,16 @@
 // each thread takes the components, channels and keys that lie together.
 //
 // Work.  The walk of chunk_walk.cuh over units of (KV head, sequence, up to
-// RB query rows).  One warp walks the run and brings the tiles' codes and
+// 16 query rows).  One warp walks the run and brings the tiles' codes and
 // scales (128 keys, 18 KB) by bulk copies, each a page's contiguous rows of a
-// head; four or eight warps share a tile's keys (RG groups of rows), each with
-// a softmax of its own, merged at the end of a unit through shared memory.  A unit cut by a run's end leaves partial (O, m, l), which a second
-// launch merges.
+// head; four or eight warps share a tile's keys, each with a softmax of its
+// own, merged at the end of a unit through shared memory.  A unit cut by a
+// run's end leaves partial (O, m, l), which a second launch merges.
+//
+// Bound: the issue of instructions, some 320 for 16 keys (64 conversions and
+// 64 products with a scale among them): 64 single tokens over 2048 to 8192
+// rows, 32 heads on 8 of 128, read 377 MB in 87 us (4.3 TB/s; without the
+// copies it takes 82, without the products with V 67).
 //
 // Every mbarrier wait is bounded; after one expires the CTA raises
 // SIMSD_EW_TIMEOUT, every warp leaves its loop and the copies in flight are
@@ -58,25 +63,25 @@ struct Q4Params {
   int one;            // 1
 };
 
-// NB blocks of 8 query rows a warp, RG groups of rows.  Up to 8 rows take few
-// registers: four CTAs an SM of four warps, whose 32 keys a tile pay for what
-// a tile costs beside its products (eight warps of 16 keys, two CTAs an SM:
-// 448 instructions for 16 keys, 113 us for 64 tokens over 2048 to 8192 rows).
-template <int D, int NB, int RG>
+// NB blocks of 8 query rows.  One takes few registers: three CTAs an SM of
+// four warps, whose 32 keys a tile pay for what a tile costs beside its
+// products (64 single tokens over 2048 to 8192 rows: 87 us; four CTAs, with 96
+// registers a thread, 92; eight warps of 16 keys, two CTAs, 113).  Two: one CTA
+// of eight warps.
+template <int D, int NB>
 struct Cfg {
-  static constexpr int kRows = 8 * NB * RG;  // query rows of a unit
+  static constexpr int kRows = 8 * NB;  // query rows of a unit
   static constexpr int kWarps = NB == 1 ? 4 : 8;
   static constexpr int kThreads = 32 * (kWarps + 1);
-  static constexpr int kKeyGroups = kWarps / RG;
-  static constexpr int kWarpKeys = kTile / kKeyGroups;
+  static constexpr int kWarpKeys = kTile / kWarps;
   static constexpr int kStep = NB == 1 ? 32 : 16;  // keys between two looks at the maxima
   static constexpr int kCtas = NB == 1 ? 3 : 1;    // an SM
   static constexpr int kStages = (NB == 1 ? 3 : 7) * (128 / D);
 };
 
-template <int D, int NB, int RG>
+template <int D, int NB>
 struct SmemQ4 {
-  using C = Cfg<D, NB, RG>;
+  using C = Cfg<D, NB>;
   Stage<D> ring[C::kStages];
   __nv_bfloat16 q[2][C::kRows * D];
   float4 fold[C::kWarps / 2][NB * (D / 16)][32];  // O of half the warps
@@ -153,10 +158,10 @@ __device__ __forceinline__ VCodes<D> load_v(const Stage<D>& st, int key, int g) 
   return c;
 }
 
-template <int D, int NB, int RG, bool SINKS>
-__global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCtas) chunk_q4_kernel(const __grid_constant__ Q4Params p) {
-  using C = Cfg<D, NB, RG>;
-  using Smem = SmemQ4<D, NB, RG>;
+template <int D, int NB, bool SINKS>
+__global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk_q4_kernel(const __grid_constant__ Q4Params p) {
+  using C = Cfg<D, NB>;
+  using Smem = SmemQ4<D, NB>;
   constexpr int RB = C::kRows, kStages = C::kStages, kWarps = C::kWarps;
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~static_cast<uintptr_t>(127));
@@ -257,7 +262,6 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
 
   // ------------------------------------------------------------------ softmax
   const int g = lane >> 2, t = lane & 3;  // the thread's place in the fragments
-  const int rg = warp % RG, kg = warp / RG;
   const int perm = g ^ ((g >> 1) & 1);    // place of key g among 8: neighbours in pairs, pairs turned in turns
   const int va = (2 * t) ^ (t & 1), vb = (2 * t + 1) ^ (t & 1);
   constexpr int kSteps = D / 16;          // products of 16 components; blocks of 16 channels
@@ -290,8 +294,8 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
         const uint32_t qb = units & 1;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          // row (rg NB + nb) 8 + g: its components from t D / 4 on
-          const int row = (rg * NB + nb) * 8 + g;
+          // row 8 nb + g: its components from t D / 4 on
+          const int row = nb * 8 + g;
           const bool real = row < ntok * p.g;
           uint4 raw[D / 32];
           uint32_t top = 0;
@@ -327,7 +331,7 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
       const bool masked = !(flags & kFull);
 #pragma unroll
       for (int step = 0; step < C::kWarpKeys / C::kStep; ++step) {
-        const int kb = kg * C::kWarpKeys + C::kStep * step;
+        const int kb = warp * C::kWarpKeys + C::kStep * step;
         // S^T of keys perm(g) and 8 + perm(g) of each 16, rows 2t and 2t + 1
         float sc[G][NB][4];
 #pragma unroll
@@ -365,7 +369,7 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const int tl = info.i0 + min(((rg * NB + nb) * 8 + 2 * t + e) / p.g, ntok - 1);
+              const int tl = info.i0 + min((nb * 8 + 2 * t + e) / p.g, ntok - 1);
               const int lo = key_lo(p.a, cs, tl), hi = key_hi(p.a, cs, tl), se = SINKS ? sink_end(p.a, cs, hi) : 0;
 #pragma unroll
               for (int u = 0; u < G; ++u)
@@ -501,14 +505,14 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
       for (int e = 0; e < 2; ++e) {
         float M = kNoReference, L = 0.f;
 #pragma unroll
-        for (int w = 0; w < C::kKeyGroups; ++w) M = fmaxf(M, sm.ml[w * RG + rg][8 * nb + 2 * t + e].x);
+        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm.ml[w][8 * nb + 2 * t + e].x);
 #pragma unroll
-        for (int w = 0; w < C::kKeyGroups; ++w) {
-          const float2 x = sm.ml[w * RG + rg][8 * nb + 2 * t + e];
+        for (int w = 0; w < kWarps; ++w) {
+          const float2 x = sm.ml[w][8 * nb + 2 * t + e];
           L = fmaf(fast_exp2(x.x - M), x.y, L);
         }
         const float f = fast_exp2(m[nb][e] - M);
-        if (kg == 0 && g == 0) sm.fin[(rg * NB + nb) * 8 + 2 * t + e] = make_float2(M, L);
+        if (warp == 0 && g == 0) sm.fin[nb * 8 + 2 * t + e] = make_float2(M, L);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
           o[nb][k][e] *= f;
@@ -516,9 +520,9 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
         }
       }
     // then O: the upper half of the warps' onto the lower half's, those summed by all
-    constexpr int kHalf = C::kKeyGroups / 2;
-    float4(*fold)[32] = sm.fold[(kg % kHalf) * RG + rg];
-    if (kg >= kHalf) {
+    constexpr int kHalf = kWarps / 2;
+    float4(*fold)[32] = sm.fold[warp % kHalf];
+    if (warp >= kHalf) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -527,7 +531,7 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
     }
     meet(1);
     if (!ok) break;
-    if (kg < kHalf) {
+    if (warp < kHalf) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -541,19 +545,19 @@ __global__ void __launch_bounds__(Cfg<D, NB, RG>::kThreads, Cfg<D, NB, RG>::kCta
     if (!ok) break;
     // two blocks of channels (four channels side by side) of two rows a turn
     const int rows = ntok * p.g;
-    for (int i = tid; i < RG * NB * (kSteps / 2) * 32; i += 32 * kWarps) {
-      const int ln = i & 31, j = i >> 5, k2 = j % (kSteps / 2), nb = j / (kSteps / 2) % NB, r = j / (kSteps / 2) / NB;
+    for (int i = tid; i < NB * (kSteps / 2) * 32; i += 32 * kWarps) {
+      const int ln = i & 31, j = i >> 5, k2 = j % (kSteps / 2), nb = j / (kSteps / 2);
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
 #pragma unroll
       for (int w = 0; w < kHalf; ++w) {
-        const float4 a = sm.fold[w * RG + r][nb * kSteps + 2 * k2][ln], b = sm.fold[w * RG + r][nb * kSteps + 2 * k2 + 1][ln];
+        const float4 a = sm.fold[w][nb * kSteps + 2 * k2][ln], b = sm.fold[w][nb * kSteps + 2 * k2 + 1][ln];
         x.x += a.x, x.y += a.y, x.z += a.z, x.w += a.w;
         y.x += b.x, y.y += b.y, y.z += b.z, y.w += b.w;
       }
       const int ch = (ln >> 2) * (D / 8) + 4 * k2;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int row = (r * NB + nb) * 8 + 2 * (ln & 3) + e;
+        const int row = nb * 8 + 2 * (ln & 3) + e;
         if (row >= rows) continue;
         const float2 ml = sm.fin[row];
         // (a sum that is NaN is passed on, not hidden)
@@ -619,19 +623,15 @@ __global__ void __launch_bounds__(256) chunk_q4_merge_kernel(const __grid_consta
   }
 }
 
-// Query rows of a unit: the fewest that hold a sequence's rows on average and
-// a token's heads.
-int q4_rows(int T, int Bt, int g) {
-  for (int rb : {8, 16, 32})
-    if (g <= rb && static_cast<long long>(T) * g <= static_cast<long long>(rb) * Bt) return rb;
-  return 64;
-}
-constexpr int q4_ctas(int rows, int num_sms) { return (rows == 8 ? Cfg<128, 1, 1>::kCtas : 1) * num_sms; }
+// Query rows of a unit: 8 where they hold a token's heads and a sequence's rows
+// on average, else 16.
+int q4_rows(int T, int Bt, int g) { return g <= 8 && static_cast<long long>(T) * g <= 8ll * Bt ? 8 : 16; }
+constexpr int q4_ctas(int rows, int num_sms) { return (rows == 8 ? Cfg<128, 1>::kCtas : Cfg<128, 2>::kCtas) * num_sms; }
 
-template <int D, int NB, int RG, bool SINKS>
+template <int D, int NB, bool SINKS>
 cudaError_t launch_rows(Q4Params p, int num_sms, cudaStream_t stream) {
-  using C = Cfg<D, NB, RG>;
-  constexpr size_t bytes = sizeof(SmemQ4<D, NB, RG>) + 128;
+  using C = Cfg<D, NB>;
+  constexpr size_t bytes = sizeof(SmemQ4<D, NB>) + 128;
   static_assert(C::kCtas * (bytes + 1024) <= 228 * 1024, "shared memory of an SM");
   p.ub = C::kRows / p.g;
   p.ctas = C::kCtas * num_sms;
@@ -644,32 +644,33 @@ cudaError_t launch_rows(Q4Params p, int num_sms, cudaStream_t stream) {
   {
     std::lock_guard<std::mutex> lk(mu);
     if (!done[dev]) {
-      e = cudaFuncSetAttribute(chunk_q4_kernel<D, NB, RG, SINKS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+      e = cudaFuncSetAttribute(chunk_q4_kernel<D, NB, SINKS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                static_cast<int>(bytes));
       if (e != cudaSuccess) return e;
       done[dev] = true;
     }
   }
-  e = launch_overlapped(chunk_q4_kernel<D, NB, RG, SINKS>, dim3(static_cast<unsigned>(p.ctas)), dim3(C::kThreads), bytes,
+  e = launch_overlapped(chunk_q4_kernel<D, NB, SINKS>, dim3(static_cast<unsigned>(p.ctas)), dim3(C::kThreads), bytes,
                         stream, 1u, p);
   if (e != cudaSuccess || p.ctas == 1) return e;
-  return launch_overlapped(chunk_q4_merge_kernel<D, C::kRows>, dim3(static_cast<unsigned>(p.ctas - 1), C::kRows > 16 ? 4u : 1u),
-                           dim3(256), 0, stream, 1u, p);
+  return launch_overlapped(chunk_q4_merge_kernel<D, C::kRows>, dim3(static_cast<unsigned>(p.ctas - 1)), dim3(256), 0, stream, 1u, p);
 }
 
 template <int D, bool SINKS>
 cudaError_t launch_d(const Q4Params& p, int num_sms, cudaStream_t stream) {
-  switch (q4_rows(p.a.T, p.a.Bt, p.g)) {
-    case 8: return launch_rows<D, 1, 1, SINKS>(p, num_sms, stream);
-    case 16: return launch_rows<D, 2, 1, SINKS>(p, num_sms, stream);
-    case 32: return launch_rows<D, 2, 2, SINKS>(p, num_sms, stream);
-    default: return launch_rows<D, 2, 4, SINKS>(p, num_sms, stream);
-  }
+  return q4_rows(p.a.T, p.a.Bt, p.g) == 8 ? launch_rows<D, 1, SINKS>(p, num_sms, stream)
+                                          : launch_rows<D, 2, SINKS>(p, num_sms, stream);
 }
 
 }  // namespace
 
-constexpr int kCodesRows = 16;   // query rows a sequence and KV head
+// By the query rows that a sequence has for a KV head on average.  Up to 16:
+// from the registers; up to 256: by tiles; more: through the image, which
+// costs one pass over the rows but then serves 256 of them a tile.  32
+// sequences of 4096 rows, heads of 128, 32 on 8: 20 rows 112 us from the
+// registers (in two blocks of 16) and 106 by tiles; 16 sequences: 256 rows 121
+// us by tiles and 153 through the image, 512 rows 215 and 206.
+constexpr int kCodesRows = 16;
 constexpr int kTilesRows = 256;
 Q4Way chunk_q4_way(int dtype, int T, int Bt, int Hq, int Hkv) {
   if (dtype != SIMSD_BF16 || Bt > kChunkMaxSeqs) return Q4Way::kImage;

@@ -13,6 +13,14 @@ prefix and from drafts.  This module is the way there:
   5. simsd_accept_sampled  Eq. (2) on the two truncated distributions
   6. simsd_kv_commit       the accepted drafts' keys and values
 
+Long contexts: the cache may be held in 4 bits (simsd_rope_append_q4 and
+simsd_chunk_attention_q4 in place of calls 1 and 2), attention may go through
+a window beside which the first rows stay visible
+(simsd_chunk_attention_sinks), and the pages may come from a pool that is
+smaller than all sequences together: simsd_pages_extend before a chunk,
+simsd_pages_release of what the window has left behind, simsd_pages_fork for
+several continuations of one prompt, simsd_pages_compact.
+
 The rotation may be one that the verification kernels do not do themselves
 (interleaved, partial or scaled for long contexts): q and the new keys are
 rotated by simsd_rope_rotate at the RoPE-copy positions first (Sec. 3.1).
@@ -30,16 +38,32 @@ class PromptCache:
     and read it.  PyTorch only allocates the buffers."""
 
     def __init__(self, layers, Bt, Hq, Hkv, d, page_size, max_len, plan, mask_block=1, dtype=torch.bfloat16,
-                 device="cuda"):
+                 device="cuda", window=0, sinks=0, bits=None, pages=None):
+        """window, sinks: rows back, and first rows, that a token sees (0: all);
+        bits 4: the cache in 4 bits; pages: size of a pool whose pages the
+        sequences take and let go of (None: a place for every row)."""
         self.L, self.Bt, self.Hq, self.Hkv, self.d, self.P = layers, Bt, Hq, Hkv, d, page_size
         self.plan, self.mask_block, self.dtype, self.device = plan, mask_block, dtype, device
+        self.window, self.sinks, self.bits, self.pooled = window, sinks, bits, pages is not None
         self.code = simsd.SIMSD_F32 if dtype == torch.float32 else simsd.SIMSD_BF16
         self.max_pages = (max_len + page_size - 1) // page_size
-        pages = Bt * self.max_pages
+        pages = Bt * self.max_pages if pages is None else pages
         i32 = dict(dtype=torch.int32, device=device)
-        self.k_cache = torch.empty(layers, pages, Hkv, page_size, d, dtype=dtype, device=device)
-        self.v_cache = torch.empty_like(self.k_cache)
-        self.block_table = torch.arange(pages, **i32).view(Bt, self.max_pages)
+        if bits == 4:
+            parts = [torch.zeros(layers, pages, Hkv, page_size, w, dtype=torch.uint8, device=device)
+                     for w in (d // 2, d // 16) * 2]
+            self.q4 = [simsd.Q4Cache(*(x[l] for x in parts)) for l in range(layers)]
+        else:
+            self.k_cache = torch.empty(layers, pages, Hkv, page_size, d, dtype=dtype, device=device)
+            self.v_cache = torch.empty_like(self.k_cache)
+            parts = [self.k_cache, self.v_cache]
+        if self.pooled:
+            self.page_set = simsd.PageSet(parts)
+            self.block_table = torch.full((Bt, self.max_pages), -1, **i32)
+        else:
+            self.block_table = torch.arange(pages, **i32).view(Bt, self.max_pages)
+        self.refs = torch.zeros(pages, **i32)
+        self.live = torch.zeros(1, **i32)
         self.prefix_len = torch.zeros(Bt, **i32)
         self.err = torch.zeros(1, **i32)
         self.workspace = None
@@ -55,20 +79,59 @@ class PromptCache:
         outputs [L][T][Hq][d] and advances the prefix lengths."""
         T = qkv.shape[1]
         Hq, Hkv = self.Hq, self.Hkv
+        lengths = token_start[1:] - token_start[:-1]
+        if self.pooled:
+            simsd.simsd_pages_extend(self.prefix_len, lengths, self.block_table, self.refs, self.P, err_word=self.err)
         out = torch.empty(self.L, T, Hq, self.d, dtype=self.dtype, device=self.device)
         q = torch.empty(T, Hq, self.d, dtype=self.dtype, device=self.device)
-        ws = self._scratch(simsd.simsd_chunk_workspace_bytes(self.code, T, self.Bt, Hq, Hkv, self.d, self.max_pages,
-                                                             self.P))
+        sizes = (self.code, T, self.Bt, Hq, Hkv, self.d, self.max_pages, self.P)
+        ws = self._scratch(simsd.simsd_chunk_q4_workspace_bytes(*sizes, self.refs.shape[0]) if self.bits == 4
+                           else simsd.simsd_chunk_workspace_bytes(*sizes))
         for l in range(self.L):
             x = qkv[l]
-            simsd.simsd_rope_append(self.plan, x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], token_start,
-                                    self.prefix_len, q, self.k_cache[l], self.v_cache[l], self.block_table,
-                                    err_word=self.err)
-            simsd.simsd_chunk_attention(q, token_start, self.prefix_len, self.k_cache[l], self.v_cache[l],
-                                        self.block_table, out[l], mask_block=self.mask_block, workspace=ws,
-                                        err_word=self.err)
-        self.prefix_len += token_start[1:] - token_start[:-1]
+            args = (self.plan, x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], token_start, self.prefix_len, q)
+            if self.bits == 4:
+                simsd.simsd_rope_append_q4(*args, self.q4[l], self.block_table, err_word=self.err)
+                simsd.simsd_chunk_attention_q4(q, token_start, self.prefix_len, self.q4[l], self.block_table, out[l],
+                                               mask_block=self.mask_block, window=self.window, sinks=self.sinks,
+                                               workspace=ws, err_word=self.err)
+                continue
+            cache = (self.k_cache[l], self.v_cache[l], self.block_table)
+            simsd.simsd_rope_append(*args, *cache, err_word=self.err)
+            if self.window:
+                simsd.simsd_chunk_attention_sinks(q, token_start, self.prefix_len, *cache, out[l], self.window,
+                                                  self.sinks, mask_block=self.mask_block, workspace=ws,
+                                                  err_word=self.err)
+            else:
+                simsd.simsd_chunk_attention(q, token_start, self.prefix_len, *cache, out[l],
+                                            mask_block=self.mask_block, workspace=ws, err_word=self.err)
+        self.prefix_len += lengths
+        if self.pooled and self.window:
+            # the next token sees rows from prefix_len + 1 - window on, and the first ones
+            first = torch.full_like(self.prefix_len, self.sinks)
+            simsd.simsd_pages_release(self.block_table, self.refs, first, self.prefix_len + (1 - self.window), self.P,
+                                      err_word=self.err)
         return out
+
+    def fork(self, src, dst):
+        """Sequences dst become copies of sequences src (int32 tensors)."""
+        ws = self._scratch(simsd.simsd_pages_workspace_bytes(0, src.shape[0]))
+        simsd.simsd_pages_fork(self.page_set, src, dst, self.prefix_len, self.block_table, self.refs, self.P,
+                               workspace=ws, err_word=self.err)
+
+    def release(self, seq):
+        """Sequences seq (an int32 tensor) end."""
+        zero = torch.zeros_like(seq)
+        simsd.simsd_pages_release(self.block_table, self.refs, zero, torch.full_like(seq, 2 ** 31 - 1), self.P,
+                                  seq=seq, err_word=self.err)
+        self.prefix_len[seq.long()] = 0
+
+    def compact(self):
+        """Moves the pages in use to the lowest ids; their number, on the GPU."""
+        ws = self._scratch(simsd.simsd_pages_workspace_bytes(self.refs.shape[0]))
+        simsd.simsd_pages_compact(self.page_set, self.block_table, self.refs, self.live, workspace=ws,
+                                  err_word=self.err)
+        return self.live
 
     def draw(self, logits, u, **limits):
         """Tokens of logits [..][V] under random numbers u [..], and the
@@ -84,7 +147,11 @@ class PromptCache:
         """One verification step on drafts with their distributions: q
         [L][Bt][2g][Hq][d], k_new / v_new [L][Bt][2g][Hkv][d] not rotated (they
         are rotated in place), target_log_probs [Bt][g+1][V], draft_log_probs
-        [Bt][g][V].  Returns outputs, accepted lengths and tokens."""
+        [Bt][g][V].  Returns outputs, accepted lengths and tokens.  The prefix is
+        read whole, from a cache in dtype (simsd_q4_expand makes one of a cache
+        in 4 bits)."""
+        if self.bits == 4 or self.window or self.pooled:
+            raise ValueError("verification reads a whole cache in its own type, with a place for every row")
         L, Bt, S, Hq, d = q.shape
         gamma = S // 2
         i32 = dict(dtype=torch.int32, device=self.device)
@@ -135,7 +202,31 @@ def main():
     print(f"prompts {lengths}, accepted {accepted.tolist()} of {gamma}, cached {cache.prefix_len.tolist()}, "
           f"error word {word}")
     print("tokens", tokens.tolist())
-    return 0 if word == 0 and bool(torch.isfinite(out.float()).all()) else 1
+    fine = long_context(plan)
+    return 0 if fine and word == 0 and bool(torch.isfinite(out.float()).all()) else 1
+
+
+
+def long_context(plan):
+    """One prompt, four continuations through a window over a cache in 4 bits,
+    in a pool of a few pages."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    layers, Hq, Hkv, d, i32 = 2, 16, 8, 128, dict(dtype=torch.int32, device="cuda")
+    cache = PromptCache(layers, 4, Hq, Hkv, d, 64, 65536, plan, window=1024, sinks=64, bits=4, pages=100)
+    chunk = lambda *n: (  # noqa: E731
+        (torch.randn(layers, sum(n), Hq + 2 * Hkv, d, generator=g, device="cuda") * d ** -0.25).bfloat16(),
+        torch.tensor([sum(n[:i]) for i in range(len(n) + 1)], **i32))
+    for _ in range(6):
+        out = cache.append_chunk(*chunk(1000, 0, 0, 0))
+    cache.fork(torch.zeros(3, **i32), torch.arange(1, 4, **i32))
+    for _ in range(20):
+        out = cache.append_chunk(*chunk(1, 1, 1, 1))
+    cache.release(torch.tensor([0, 2], **i32))
+    live = cache.compact()
+    out = cache.append_chunk(*chunk(0, 1, 0, 1))
+    word = simsd.simsd_check_error(cache.err)
+    print(f"continuations at {cache.prefix_len.tolist()}, {int(live)} of 100 pages in use, error word {word}")
+    return word == 0 and bool(torch.isfinite(out.float()).all())
 
 
 if __name__ == "__main__":

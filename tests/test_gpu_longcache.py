@@ -1,0 +1,137 @@
+"""The calls for long caches together, as a serving loop makes them: windows,
+4 bits, pools, forks and compaction, and the same in a CUDA graph."""
+import pytest
+import torch
+
+from paper_2606_02544_gb300 import simsd
+from paper_2606_02544_gb300.prompt import PromptCache, long_context
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+I32 = dict(dtype=torch.int32, device="cuda")
+LAYERS, HQ, HKV, D, P = 2, 8, 2, 64, 16
+
+
+def plan():
+    return simsd.simsd_rope_plan_init("half", D, 1.0e6)
+
+
+def chunk(g, dtype, *n):
+    x = torch.randn(LAYERS, sum(n), HQ + 2 * HKV, D, generator=g, device="cuda").to(dtype)
+    return x, torch.tensor([sum(n[:i]) for i in range(len(n) + 1)], **I32)
+
+
+@pytest.mark.parametrize("dtype,bits", [(BF16, None), (BF16, 4), (F32, None), (F32, 4)])
+def test_pool_and_place_for_every_row_agree(dtype, bits):
+    """Pages that the window has left behind are taken again by other
+    sequences; outputs have the bits that a place for every row gives."""
+    kw = dict(mask_block=1, dtype=dtype, window=70, sinks=20, bits=bits)
+    whole = PromptCache(LAYERS, 3, HQ, HKV, D, P, 1024, plan(), **kw)
+    pool = PromptCache(LAYERS, 3, HQ, HKV, D, P, 1024, plan(), pages=37, **kw)
+    for i, n in enumerate([(100, 1, 30), (50, 0, 1), (1, 1, 1), (140, 33, 1), (1, 1, 1), (70, 90, 100), (1, 1, 1)]):
+        g = torch.Generator(device="cuda").manual_seed(i)
+        x, start = chunk(g, dtype, *n)
+        a, b = whole.append_chunk(x, start), pool.append_chunk(x, start)
+        assert torch.equal(a, b), i
+        if i == 4:
+            pool.compact()
+    assert simsd.simsd_check_error(pool.err) == 0 and simsd.simsd_check_error(whole.err) == 0
+    assert int((pool.refs > 0).sum()) <= 3 * (2 + 6)
+    assert pool.prefix_len.tolist() == [363, 127, 135]
+
+
+@pytest.mark.parametrize("dtype,bits", [(BF16, None), (BF16, 4), (F32, 4)])
+def test_forks_continue_as_their_source(dtype, bits):
+    """A fork that gets the rows its source gets has its outputs, and one that
+    gets others does not disturb it."""
+    cache = PromptCache(LAYERS, 4, HQ, HKV, D, P, 512, plan(), dtype=dtype, bits=bits, pages=60)
+    g = torch.Generator(device="cuda").manual_seed(0)
+    cache.append_chunk(*chunk(g, dtype, 75, 0, 40, 0))
+    cache.fork(torch.tensor([0, 0], **I32), torch.tensor([1, 3], **I32))
+    assert cache.prefix_len.tolist() == [75, 75, 40, 75]
+    shared = cache.refs.max().item()
+    assert shared == 3  # four whole pages of three sequences
+    for step in range(30):
+        x, start = chunk(g, dtype, 1, 1, 1, 1)
+        x[:, 1] = x[:, 0]
+        out = cache.append_chunk(x, start)
+        assert torch.equal(out[:, 0], out[:, 1]), step
+        assert not torch.equal(out[:, 0], out[:, 3])
+    before = cache.append_chunk(*chunk(g, dtype, 0, 0, 0, 0))
+    assert before.numel() == 0
+    cache.release(torch.tensor([0, 2], **I32))
+    live = cache.compact()
+    assert int(live) == int((cache.refs > 0).sum()) and int(cache.block_table.max()) == int(live) - 1
+    x, start = chunk(g, dtype, 0, 1, 0, 1)
+    out = cache.append_chunk(x, start)
+    assert bool(torch.isfinite(out.float()).all()) and simsd.simsd_check_error(cache.err) == 0
+
+
+def test_expanded_cache_is_what_the_codes_stand_for():
+    """Attention by codes and attention over the expanded cache are the same
+    up to the rounding of the probabilities (2^-9 and 2^-12 of them) and of
+    the outputs (2^-8 at most)."""
+    cache = PromptCache(LAYERS, 2, HQ, HKV, D, P, 512, plan(), bits=4)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    cache.append_chunk(*chunk(g, BF16, 200, 77))
+    before = cache.prefix_len.clone()
+    x, start = chunk(g, BF16, 1, 1)
+    out = cache.append_chunk(x, start)
+    n = cache.refs.shape[0]
+    for l in range(LAYERS):
+        kc, vc = (torch.full((n, HKV, P, D), float("nan"), dtype=BF16, device="cuda") for _ in range(2))
+        simsd.simsd_q4_expand(cache.q4[l], cache.block_table, torch.zeros_like(before), cache.prefix_len, kc, vc,
+                              err_word=cache.err)
+        q = torch.empty(2, HQ, D, dtype=BF16, device="cuda")
+        simsd.simsd_rope_rotate(plan(), before, x[l][:, :HQ], q)
+        o2 = torch.empty_like(q)
+        ws = torch.empty(simsd.simsd_chunk_workspace_bytes(simsd.SIMSD_BF16, 2, 2, HQ, HKV, D, cache.max_pages, P),
+                         dtype=torch.uint8, device="cuda")
+        simsd.simsd_chunk_attention(q, start, before, kc, vc, cache.block_table, o2, workspace=ws)
+        top = float(torch.nan_to_num(vc.float()).abs().max())
+        err = (out[l].float() - o2.float()).abs()
+        # A <= max |v|: 2^-8 (bf16 probabilities) + 2^-11 + scores' errors, and both roundings of the outputs
+        assert bool((err <= top * (2.0 ** -8 + 2.0 ** -10) + 2 * 2.0 ** -8 * o2.float().abs()).all())
+    assert simsd.simsd_check_error(cache.err) == 0
+
+
+@pytest.mark.parametrize("bits", [None, 4])
+def test_replayed_decoding_step(bits):
+    """A step of every sequence captured once, with its pages taken and let go
+    of, and replayed on other rows; the bits of calls made one by one."""
+    caches = [PromptCache(LAYERS, 3, HQ, HKV, D, P, 512, plan(), window=50, sinks=10, bits=bits, pages=40) for _ in range(2)]
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, start = chunk(g, BF16, 61, 5, 100)
+    for c in caches:
+        c.append_chunk(x, start)
+    static, one = chunk(g, BF16, 1, 1, 1)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    state = [t.clone() for t in (caches[1].block_table, caches[1].refs, caches[1].prefix_len)]
+    with torch.cuda.stream(s):
+        caches[1].append_chunk(static, one)  # warm-up, undone below
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            out = caches[1].append_chunk(static, one)
+    torch.cuda.current_stream().wait_stream(s)
+    for t, v in zip((caches[1].block_table, caches[1].refs, caches[1].prefix_len), state):
+        t.copy_(v)
+    for step in range(25):
+        x, _ = chunk(g, BF16, 1, 1, 1)
+        static.copy_(x)
+        want = caches[0].append_chunk(x, one)
+        graph.replay()
+        assert torch.equal(out, want), step
+    for a, b in ((caches[0].block_table, caches[1].block_table), (caches[0].refs, caches[1].refs)):
+        assert torch.equal(a, b)
+    assert all(simsd.simsd_check_error(c.err) == 0 for c in caches)
+
+
+def test_verification_refuses_what_it_cannot_read():
+    cache = PromptCache(LAYERS, 2, HQ, HKV, D, P, 512, plan(), bits=4)
+    with pytest.raises(ValueError):
+        cache.verify(*[torch.zeros(1)] * 8)
+
+
+def test_example_runs():
+    assert long_context(simsd.simsd_rope_plan_init("half", 128, 1.0e6))
