@@ -523,8 +523,8 @@ SIMSD_API int simsd_chunk_attention_sinks(int dtype, const void* q, int64_t q_st
  *   k_codes, v_codes   [num_pages][Hkv][page_size][d/2] bytes
  *   k_scales, v_scales [num_pages][Hkv][page_size][d/16] bytes
  * 72 bytes a row of 128 components.  scale * code has 6 significant bits, so
- * it is exact in bf16.  A unit > 0 (1 is usual) places the range of the scales,
- * 2^-9 to 448, where the groups' largest values over 6 lie.
+ * it is exact in bf16.  A unit in [2^-64, 2^64] (1 is usual) places the range of
+ * the scales, 2^-9 to 448, where the groups' largest values over 6 lie.
  */
 typedef struct simsd_q4_cache {
   void *k_codes, *k_scales, *v_codes, *v_scales;
@@ -593,8 +593,10 @@ SIMSD_API int simsd_chunk_attention_q4(int dtype, const void* q, int64_t q_strid
  * Zeroed counts and a table of -1 are an empty pool.  The calls work on the
  * device alone (a CUDA graph of them does the same with other lengths), take
  * the lowest free pages first and give the same result every time.  A table
- * entry that is neither -1 nor a page id sets SIMSD_EW_PAGE and counts as -1.
- * block_table is [Bt][max_pages], Bt at most 65536.
+ * entry that is neither -1 nor a page id sets SIMSD_EW_PAGE: a fork gets -1 for
+ * it, a release makes it -1, compaction leaves it, and a sequence that is to be
+ * extended over it gets no page.  block_table is [Bt][max_pages], Bt at most
+ * 65536; refs is 16-byte aligned.
  */
 
 /* One array of a cache: layer l of page p is the page_bytes bytes at base + l
@@ -633,7 +635,8 @@ SIMSD_API int simsd_pages_release(const int32_t* seq, const int32_t* first, cons
 
 /*
  * simsd_pages_workspace_bytes -- bytes of scratch (16-byte aligned) that
- * simsd_pages_fork of `pairs` pairs and simsd_pages_compact need.
+ * simsd_pages_fork of `pairs` pairs and simsd_pages_compact need; two calls
+ * that share it must not overlap on the GPU.
  *
  * simsd_pages_fork -- sequence dst[i] becomes a copy of sequence src[i]: the
  * pages that src[i]'s lens rows fill are shared, the last one where it is
@@ -642,8 +645,8 @@ SIMSD_API int simsd_pages_release(const int32_t* seq, const int32_t* first, cons
  * (and is not yet free to this call).  One src may have many dst.
  *   arrays  n_arrays host structs: all that the pages hold, in every layer
  * A pair whose dst is named twice or is also a src, or with a number outside
- * [0, Bt), sets SIMSD_EW_SEQ, one with a bad length SIMSD_EW_PREFIX_LEN: it is
- * left out.  Too few free pages set SIMSD_EW_POOL and nothing is changed.
+ * [0, Bt), sets SIMSD_EW_SEQ, one with a bad length SIMSD_EW_PREFIX_LEN, one
+ * whose page to be copied is no page id SIMSD_EW_PAGE: it is left out.  Too few free pages set SIMSD_EW_POOL and nothing is changed.
  *
  * simsd_pages_compact -- moves the live pages to the lowest ids: the k-th
  * live page above the count of live ones goes to the k-th free one below it,

@@ -748,12 +748,14 @@ int simsd_chunk_attention_sinks(int dtype, const void* q, int64_t q_stride, cons
 
 namespace {
 
+// (units whose inverses and products with the scales stay within fp32)
+bool unit_ok(float u) { return u >= 0x1p-64f && u <= 0x1p64f; }
 bool q4_ok(const simsd_q4_cache* c) {
   return c && c->k_codes && c->k_scales && c->v_codes && c->v_scales && aligned16(c->k_codes) &&
-         aligned16(c->k_scales) && aligned16(c->v_codes) && aligned16(c->v_scales) && c->k_unit > 0.f &&
-         c->v_unit > 0.f && !std::isinf(c->k_unit) && !std::isinf(c->v_unit);
+         aligned16(c->k_scales) && aligned16(c->v_codes) && aligned16(c->v_scales) && unit_ok(c->k_unit) &&
+         unit_ok(c->v_unit);
 }
-int q4_fail() { return arg_fail("cache: null or misaligned arrays, or a unit that is not positive and finite"); }
+int q4_fail() { return arg_fail("cache: null or misaligned arrays, or a unit outside [2^-64, 2^64]"); }
 
 }  // namespace
 

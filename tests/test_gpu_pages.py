@@ -338,3 +338,40 @@ def test_replayed_graph():
         dev.same(contents=False)
         got = dev.caches[1][1, :, 0, 0, 0].cpu().numpy()
         assert np.array_equal(got[held], (ref.data + 1100)[held])
+
+
+@pytest.mark.parametrize("num_pages,live", [(40003, 0.5), (16384, 0.7), (16385, 0.02), (33000, 1.0), (33000, 0.0)])
+def test_large_pools_are_made_dense(num_pages, live):
+    """More pages than a step of the search, more moves than its list."""
+    rng = np.random.RandomState(num_pages)
+    ref = Pool(50, 900, num_pages, 1)
+    used = rng.permutation(num_pages)[:min(45000, int(live * num_pages))]
+    ref.refs[used] = 1
+    for b in range(50):  # (some pages are in no table)
+        row = used[b::50][:899]
+        ref.table[b, 1:1 + len(row)] = row
+    dev = Device(ref, layers=1, shape=(1, 1, 4), arrays=1)
+    assert dev.compact() == ref.compact()
+    assert dev.word() == 0
+    dev.same()
+    assert (ref.refs[:int((ref.refs > 0).sum())] > 0).all()
+
+
+def test_pools_past_four_gigabytes():
+    """Pages whose contents lie past 2^32 bytes: forked and moved from there."""
+    n, i32 = 4200, dict(dtype=torch.int32, device="cuda")
+    cache = torch.zeros(1, n, 8, 64, 2048, dtype=torch.uint8, device="cuda")  # 1 MB a page
+    cache[0, n - 1] = 7
+    cache[0, n - 2, :, :, ::3] = 9
+    table = torch.tensor([[n - 1, n - 2], [-1, -1]], **i32)
+    refs, lens = torch.zeros(n, **i32), torch.tensor([100, 0], **i32)
+    refs[n - 2:] = 1
+    pages, err, live = simsd.PageSet([cache]), torch.zeros(1, **i32), torch.zeros(1, **i32)
+    ws = torch.empty(simsd.simsd_pages_workspace_bytes(n, 1), dtype=torch.uint8, device="cuda")
+    simsd.simsd_pages_fork(pages, torch.tensor([0], **i32), torch.tensor([1], **i32), lens, table, refs, 64,
+                           workspace=ws, err_word=err)
+    assert table.tolist() == [[n - 1, n - 2], [n - 1, 0]] and torch.equal(cache[0, 0], cache[0, n - 2])
+    simsd.simsd_pages_compact(pages, table, refs, live, workspace=ws, err_word=err)
+    assert table.tolist() == [[2, 1], [2, 0]] and int(live) == 3 and refs[:3].tolist() == [1, 1, 2]
+    assert bool((cache[0, 2] == 7).all()) and torch.equal(cache[0, 1], cache[0, 0])
+    assert simsd.simsd_check_error(err) == 0

@@ -398,3 +398,69 @@ def test_workspace_too_small_is_refused():
         simsd.simsd_chunk_attention_q4(**a, out=out, workspace=torch.empty(1 << 24, dtype=torch.uint8))
     with pytest.raises(ValueError):
         simsd.simsd_chunk_attention_q4(**(a | dict(key_start=torch.zeros(2, dtype=torch.int32, device="cuda"))), out=out)
+
+
+def test_pools_past_four_gigabytes():
+    """Rows whose codes lie past 2^32 bytes and 2^31 rows of a head's scales:
+    the same bits as from the pool's start."""
+    n, Hq, Hkv, d, P = 70000, 8, 8, 128, 128
+    cache = simsd.Q4Cache.zeros(n, Hkv, P, d)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    T = 300
+    x = torch.randn(T, Hq + 2 * Hkv, d, generator=g, device="cuda").to(BF16)
+    plan = simsd.simsd_rope_plan_init("half", d, THETA)
+    start, zero, err = torch.tensor([0, T], **i32), torch.zeros(1, **i32), torch.zeros(1, **i32)
+    got = []
+    for first in (0, n - 3):
+        table = torch.arange(first, first + 3, **i32)[None].contiguous()
+        q = torch.empty(T, Hq, d, dtype=BF16, device="cuda")
+        simsd.simsd_rope_append_q4(plan, x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], start, zero, q, cache, table,
+                                   err_word=err)
+        for t in cache.tensors:
+            got.append(t[first:first + 3].clone())
+        for rows in (1, 9, 100):  # from the registers, by tiles
+            s, m = torch.tensor([0, rows], **i32), torch.tensor([T - rows], **i32)
+            out = torch.empty(rows, Hq, d, dtype=BF16, device="cuda")
+            ws = torch.empty(simsd.simsd_chunk_q4_workspace_bytes(simsd.SIMSD_BF16, rows, 1, Hq, Hkv, d, 3, P, n),
+                             dtype=torch.uint8, device="cuda")
+            simsd.simsd_chunk_attention_q4(q[T - rows:], s, m, cache, table, out, workspace=ws, err_word=err)
+            got.append(out)
+    half = len(got) // 2
+    assert simsd.simsd_check_error(err) == 0
+    assert all(torch.equal(a, b) for a, b in zip(got[:half], got[half:])) and bool(got[4].float().abs().sum() > 0)
+
+
+def test_many_sequences():
+    """More sequences than the kernel of few rows plans for, and chunks without
+    a token."""
+    Bt, Hq, Hkv, d, P = 9000, 2, 1, 64, 8
+    i32 = dict(dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(4)
+    has = torch.arange(Bt, device="cuda") % 3 != 1
+    start = torch.cat([torch.zeros(1, **i32), torch.cumsum(has.int(), 0).int()])
+    T = int(start[-1])
+    cache = simsd.Q4Cache.zeros(Bt * 3, Hkv, P, d)
+    table = torch.arange(Bt * 3, **i32).view(Bt, 3)
+    x = torch.randn(Bt * 20, Hq + 2 * Hkv, d, generator=g, device="cuda").to(BF16)
+    plan, err = simsd.simsd_rope_plan_init("half", d, THETA), torch.zeros(1, **i32)
+    q = torch.empty(Bt * 20, Hq, d, dtype=BF16, device="cuda")
+    simsd.simsd_rope_append_q4(plan, x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], torch.arange(Bt + 1, **i32) * 20,
+                               torch.zeros(Bt, **i32), q, cache, table, err_word=err)
+    q = torch.randn(T, Hq, d, generator=g, device="cuda").to(BF16)
+    outs = []
+    for part in (slice(0, Bt), slice(0, 3000), slice(3000, 6000), slice(6000, Bt)):
+        b = table[part].contiguous()
+        s = start[part.start:part.stop + 1]
+        qq = q[int(s[0]):int(s[-1])].contiguous()
+        out = torch.empty_like(qq)
+        n = len(b)
+        ws = torch.empty(simsd.simsd_chunk_q4_workspace_bytes(simsd.SIMSD_BF16, len(qq), n, Hq, Hkv, d, 3, P, Bt * 3),
+                         dtype=torch.uint8, device="cuda")
+        simsd.simsd_chunk_attention_q4(qq, s - s[0], torch.full((n,), 19, **i32), cache, b, out, workspace=ws,
+                                       err_word=err)
+        outs.append(out.float())
+    assert simsd.simsd_check_error(err) == 0
+    # two kernels, each off by 2^-11 of the probabilities and 2^-8 of the output at most
+    diff = (outs[0] - torch.cat(outs[1:])).abs()
+    assert bool((diff <= 2.0 ** -9 * 6.0 + 2.0 ** -7 * outs[0].abs()).all())

@@ -55,7 +55,7 @@ def test_attention_refusals(lib, four, change, status):
 
 @pytest.mark.parametrize("change", [dict(k_codes=0), dict(v_scales=0), dict(k_scales=264), dict(v_codes=4),
                                     dict(k_unit=0.0), dict(v_unit=-1.0), dict(k_unit=float("inf")),
-                                    dict(v_unit=float("nan"))])
+                                    dict(v_unit=float("nan")), dict(k_unit=2.0 ** -65), dict(v_unit=2.0 ** 65)])
 def test_cache_refusals(lib, change):
     c, _ = q4(**change)
     plan = simsd.simsd_rope_plan_init("half", 128, 1e4)
