@@ -603,7 +603,8 @@ def simsd_rope_append_q4(plan, q, k, v, token_start, prefix_len, q_out, cache, b
         _wrong("k / v: [T][Hkv][d] of q's type wanted")
     if q_out.shape != (T, Hq, d) or q_out.dtype is not dt or not q_out.is_contiguous():
         _wrong("q_out: dense, like q")
-    if not _dense_i32(token_start, Bt + 1) or not _dense_i32(prefix_len, Bt):
+    if (token_start.dtype is not _I32 or token_start.numel() != Bt + 1 or not token_start.is_contiguous()
+            or prefix_len.dtype is not _I32 or prefix_len.numel() != Bt or not prefix_len.is_contiguous()):
         _wrong("token_start / prefix_len: dense int32 [Bt+1] / [Bt] wanted")
     if positions is not None and not _dense_i32(positions, T):
         _wrong("positions: dense int32 [T] wanted")
@@ -632,18 +633,21 @@ def simsd_rope_append_q4(plan, q, k, v, token_start, prefix_len, q_out, cache, b
 def simsd_q4_expand(cache, block_table, first, last, k_cache, v_cache, err_word=None, stream=None):
     """Rows [first[b], last[b]) of each sequence, as a :class:`Q4Cache` holds
     them, written to k_cache / v_cache [num_pages][Hkv][P][d] (bf16 or fp32)."""
-    Bt = first.shape[0]
-    if not _dense_i32(first, Bt) or not _dense_i32(last, Bt):
+    Bt, dt = first.shape[0], k_cache.dtype
+    if (first.dtype is not _I32 or last.dtype is not _I32 or first.numel() != Bt or last.numel() != Bt
+            or not first.is_contiguous() or not last.is_contiguous()):
         _wrong("first / last: dense int32 [Bt] wanted")
-    num_pages, max_pages, P = _cache_sizes(k_cache, v_cache, block_table, Bt, cache.Hkv, cache.d, k_cache.dtype)
-    if num_pages != cache.num_pages or P != cache.P:
-        _wrong("k_cache / v_cache: the pages of the cache in 4 bits wanted")
+    num_pages, P = cache.num_pages, cache.P
+    if not (k_cache.shape == v_cache.shape == (num_pages, cache.Hkv, P, cache.d) and v_cache.dtype is dt
+            and k_cache.is_contiguous() and v_cache.is_contiguous()):
+        _wrong("k_cache / v_cache: dense, of one type, with the pages of the cache in 4 bits wanted")
+    max_pages = _table(block_table, Bt)
     dev = _device(k_cache)
     if not (dev == v_cache.get_device() == block_table.get_device() == first.get_device() == last.get_device()
             == cache.device_index):
         _elsewhere()
     rc = (_lib or load_library()).simsd_q4_expand(
-        _code(k_cache.dtype), cache._at, num_pages, block_table.data_ptr(), max_pages, P, first.data_ptr(),
+        _code(dt), cache._at, num_pages, block_table.data_ptr(), max_pages, P, first.data_ptr(),
         last.data_ptr(), Bt, cache.Hkv, cache.d, k_cache.data_ptr(), v_cache.data_ptr(), _error_word(err_word, dev),
         _raw_stream(stream, dev))
     if rc:
@@ -700,45 +704,40 @@ class PageSet:
             self.num_pages, self.device_index = pages, t.get_device()
             page = t.element_size() * t.shape[-3] * t.shape[-2] * t.shape[-1]
             self._c[i] = _PageArray(t.data_ptr(), page, page * pages, layers)
-        self._at = ctypes.addressof(self._c)
+        self._at, self.count = ctypes.addressof(self._c), len(self.tensors)
 
 
-def _pool(block_table, refs):
-    Bt, max_pages = block_table.shape
-    if not (block_table.dtype is _I32 and block_table.is_contiguous()):
+# (The calls on pages take some microseconds on the GPU, so what is right is
+# seen in one expression; _pages_wrong finds out what is not.)
+def _pages_wrong(dev, block_table, refs, tables, pages=None, workspace=None):
+    if block_table.dim() != 2 or block_table.dtype is not _I32 or not block_table.is_contiguous():
         _wrong("block_table: dense int32 [Bt][max_pages] wanted")
-    if not _dense_i32(refs, refs.shape[0]):
-        _wrong("refs: dense int32 [num_pages] wanted")
-    dev = _device(block_table)
-    if refs.get_device() != dev:
-        _elsewhere()
-    return Bt, max_pages, refs.shape[0], dev
-
-
-def _here_i32(t, n, dev, name):
-    if not _dense_i32(t, n):
-        _wrong(name + ": dense int32 of the right length wanted")
-    if t.get_device() != dev:
-        _elsewhere()
-    return t.data_ptr()
-
-
-def _pages_scratch(pages, num_pages, workspace, dev):
-    if pages.num_pages not in (None, num_pages):
+    for name, (t, n) in (tables | {"refs": (refs, refs.shape[0])}).items():
+        if not _dense_i32(t, n):
+            _wrong(f"{name}: dense int32 of {n} wanted")
+    if pages is not None and pages.num_pages not in (None, refs.shape[0]):
         _wrong("refs: a count for every page of the arrays wanted")
-    if pages.device_index not in (None, dev) or workspace.get_device() != dev:
-        _elsewhere()
-    if not workspace.is_contiguous():
+    if workspace is not None and not workspace.is_contiguous():
         _wrong("workspace: dense tensor wanted")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _elsewhere()
+
+
+def _current(dev):
+    return dev >= 0 and (_devices == 1 or dev == torch._C._cuda_getDevice())
 
 
 def simsd_pages_extend(lens, add, block_table, refs, page_size, err_word=None, stream=None):
     """Pages for the rows [lens[b], lens[b] + add[b]) that have none."""
-    Bt, max_pages, num_pages, dev = _pool(block_table, refs)
+    Bt, max_pages = block_table.shape
+    num_pages, dev = refs.shape[0], block_table.get_device()
+    if not (lens.dtype is add.dtype is refs.dtype is block_table.dtype is _I32
+            and lens.numel() == add.numel() == Bt and refs.numel() == num_pages
+            and lens.is_contiguous() and add.is_contiguous() and refs.is_contiguous() and block_table.is_contiguous()
+            and lens.get_device() == add.get_device() == refs.get_device() == dev and _current(dev)):
+        _pages_wrong(dev, block_table, refs, dict(lens=(lens, Bt), add=(add, Bt)))
     rc = (_lib or load_library()).simsd_pages_extend(
-        _here_i32(lens, Bt, dev, "lens"), _here_i32(add, Bt, dev, "add"), block_table.data_ptr(), refs.data_ptr(),
-        num_pages, Bt, max_pages, page_size, _error_word(err_word, dev), _raw_stream(stream, dev))
+        lens.data_ptr(), add.data_ptr(), block_table.data_ptr(), refs.data_ptr(), num_pages, Bt, max_pages, page_size,
+        _error_word(err_word, dev), _raw_stream(stream, dev))
     if rc:
         _check(rc, "simsd_pages_extend")
 
@@ -746,14 +745,23 @@ def simsd_pages_extend(lens, add, block_table, refs, page_size, err_word=None, s
 def simsd_pages_release(block_table, refs, first, last, page_size, seq=None, err_word=None, stream=None):
     """Lets go of the pages that lie wholly within rows [first[i], last[i]) of
     sequence seq[i] (None: i)."""
-    Bt, max_pages, num_pages, dev = _pool(block_table, refs)
-    n = Bt if seq is None else seq.shape[0]
+    Bt, max_pages = block_table.shape
+    num_pages, dev, n = refs.shape[0], block_table.get_device(), first.shape[0]
+    if not (first.dtype is last.dtype is refs.dtype is block_table.dtype is _I32
+            and last.numel() == first.numel() == n and refs.numel() == num_pages
+            and first.is_contiguous() and last.is_contiguous() and refs.is_contiguous()
+            and block_table.is_contiguous()
+            and first.get_device() == last.get_device() == refs.get_device() == dev and _current(dev)
+            and (n == Bt if seq is None else seq.dtype is _I32 and seq.numel() == n and seq.is_contiguous()
+                 and seq.get_device() == dev)):
+        n = Bt if seq is None else seq.shape[0]
+        _pages_wrong(dev, block_table, refs, dict(first=(first, n), last=(last, n))
+                     | ({} if seq is None else dict(seq=(seq, n))))
     if n == 0:  # (an empty tensor has no address, which would name all sequences)
         return
     rc = (_lib or load_library()).simsd_pages_release(
-        None if seq is None else _here_i32(seq, n, dev, "seq"), _here_i32(first, n, dev, "first"),
-        _here_i32(last, n, dev, "last"), n, block_table.data_ptr(), refs.data_ptr(), num_pages, Bt, max_pages,
-        page_size, _error_word(err_word, dev), _raw_stream(stream, dev))
+        None if seq is None else seq.data_ptr(), first.data_ptr(), last.data_ptr(), n, block_table.data_ptr(),
+        refs.data_ptr(), num_pages, Bt, max_pages, page_size, _error_word(err_word, dev), _raw_stream(stream, dev))
     if rc:
         _check(rc, "simsd_pages_release")
 
@@ -764,25 +772,38 @@ def simsd_pages_workspace_bytes(num_pages, pairs=0) -> int:
 
 def simsd_pages_fork(pages, src, dst, lens, block_table, refs, page_size, workspace, err_word=None, stream=None):
     """Sequence dst[i] becomes a copy of src[i]; pages: a :class:`PageSet`."""
-    Bt, max_pages, num_pages, dev = _pool(block_table, refs)
-    n = src.shape[0]
-    ws, ws_bytes = _pages_scratch(pages, num_pages, workspace, dev)
+    Bt, max_pages = block_table.shape
+    num_pages, dev, n = refs.shape[0], block_table.get_device(), src.shape[0]
+    if not (src.dtype is dst.dtype is lens.dtype is refs.dtype is block_table.dtype is _I32
+            and src.numel() == dst.numel() == n and lens.numel() == Bt and refs.numel() == num_pages
+            and src.is_contiguous() and dst.is_contiguous() and lens.is_contiguous() and refs.is_contiguous()
+            and block_table.is_contiguous() and workspace.is_contiguous()
+            and src.get_device() == dst.get_device() == lens.get_device() == refs.get_device()
+            == workspace.get_device() == dev and _current(dev)
+            and pages.num_pages in (num_pages, None) and pages.device_index in (dev, None)):
+        _pages_wrong(dev, block_table, refs, dict(src=(src, n), dst=(dst, n), lens=(lens, Bt)), pages, workspace)
     rc = (_lib or load_library()).simsd_pages_fork(
-        pages._at, len(pages.tensors), _here_i32(src, n, dev, "src"), _here_i32(dst, n, dev, "dst"), n,
-        _here_i32(lens, Bt, dev, "lens"), block_table.data_ptr(), refs.data_ptr(), num_pages, Bt, max_pages,
-        page_size, ws, ws_bytes, _error_word(err_word, dev), _raw_stream(stream, dev))
+        pages._at, pages.count, src.data_ptr(), dst.data_ptr(), n, lens.data_ptr(), block_table.data_ptr(),
+        refs.data_ptr(), num_pages, Bt, max_pages, page_size, workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _error_word(err_word, dev), _raw_stream(stream, dev))
     if rc:
         _check(rc, "simsd_pages_fork")
 
 
 def simsd_pages_compact(pages, block_table, refs, live, workspace, err_word=None, stream=None):
     """Moves the live pages to the lowest ids; live [1] int32 out or None."""
-    Bt, max_pages, num_pages, dev = _pool(block_table, refs)
-    ws, ws_bytes = _pages_scratch(pages, num_pages, workspace, dev)
+    Bt, max_pages = block_table.shape
+    num_pages, dev = refs.shape[0], block_table.get_device()
+    if not (refs.dtype is block_table.dtype is _I32 and refs.numel() == num_pages
+            and refs.is_contiguous() and block_table.is_contiguous() and workspace.is_contiguous()
+            and refs.get_device() == workspace.get_device() == dev and _current(dev)
+            and (live is None or live.dtype is _I32 and live.numel() == 1 and live.get_device() == dev)
+            and pages.num_pages in (num_pages, None) and pages.device_index in (dev, None)):
+        _pages_wrong(dev, block_table, refs, {} if live is None else dict(live=(live, 1)), pages, workspace)
     rc = (_lib or load_library()).simsd_pages_compact(
-        pages._at, len(pages.tensors), block_table.data_ptr(), refs.data_ptr(), num_pages, Bt, max_pages,
-        None if live is None else _here_i32(live, 1, dev, "live"), ws, ws_bytes, _error_word(err_word, dev),
-        _raw_stream(stream, dev))
+        pages._at, pages.count, block_table.data_ptr(), refs.data_ptr(), num_pages, Bt, max_pages,
+        None if live is None else live.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+        _error_word(err_word, dev), _raw_stream(stream, dev))
     if rc:
         _check(rc, "simsd_pages_compact")
 
