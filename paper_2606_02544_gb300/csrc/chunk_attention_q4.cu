@@ -60,7 +60,6 @@ struct Q4Params {
   int g, ub, ctas;    // heads per KV head, tokens of a unit, grid size
   int sub;            // keys per copy: a page, or part of one
   float scale_log2;   // scores to log2 units, the keys' unit included
-  int one;            // 1
 };
 
 // NB blocks of 8 query rows.  One takes few registers: three CTAs an SM of
@@ -98,6 +97,14 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The first of a sum's.
+__device__ __forceinline__ void mma16816_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                               uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 // The transpose of an 8 x 8 matrix of fp16, two neighbours of a row a thread.
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
@@ -329,6 +336,21 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
     }
     if (!(flags & kEmpty)) {
       const bool masked = !(flags & kFull);
+      if (masked) {
+        // values of rows that no token of the unit sees may be anything: their
+        // scales, which only this warp reads, are set to 0
+        const int lo = info.lo, se = info.se, w0 = info.w0, hi = info.hi;
+#pragma unroll 1
+        for (int i = warp * C::kWarpKeys + lane; i < (warp + 1) * C::kWarpKeys; i += 32) {
+          const int key = key0 + i;
+          if (key >= lo && key < hi && (!SINKS || key < se || key >= w0)) continue;
+          uint32_t* row = reinterpret_cast<uint32_t*>(&sm.ring[st].vs[i * (D / kQ4Group)]);
+#pragma unroll
+          for (int k = 0; k < D / kQ4Group / 4; ++k) row[k] = 0u;
+        }
+        fence_proxy_async_smem();  // (the slot is filled by bulk copies next)
+        __syncwarp();
+      }
 #pragma unroll
       for (int step = 0; step < C::kWarpKeys / C::kStep; ++step) {
         const int kb = warp * C::kWarpKeys + C::kStep * step;
@@ -336,8 +358,6 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
         float sc[G][NB][4];
 #pragma unroll
         for (int u = 0; u < G; ++u) {
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) sc[u][nb][0] = sc[u][nb][1] = sc[u][nb][2] = sc[u][nb][3] = 0.f;
           const KCodes<D> ka = load_k(s, kb + 16 * u + perm, t), kc = load_k(s, kb + 16 * u + 8 + perm, t);
           const uint32_t x = q4_scale_pair(ka.s), y = q4_scale_pair(kc.s);
           uint32_t sa[2], sb[2];
@@ -353,14 +373,15 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
             const uint32_t a2 = mul_f16x2(k & 1 ? q4_pair<3>(wa) : q4_pair<1>(wa), fa);
             const uint32_t a3 = mul_f16x2(k & 1 ? q4_pair<3>(wb) : q4_pair<1>(wb), fb);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma16816(sc[u][nb], a0, a1, a2, a3, q[nb][k][0], q[nb][k][1]);
+            for (int nb = 0; nb < NB; ++nb) {
+              if (k == 0)
+                mma16816_first(sc[u][nb], a0, a1, a2, a3, q[nb][k][0], q[nb][k][1]);
+              else
+                mma16816(sc[u][nb], a0, a1, a2, a3, q[nb][k][0], q[nb][k][1]);
+            }
           }
         }
-        // (Written as loops that run once, a number the compiler does not know:
-        // as conditions, these two and the one below become predicates on some
-        // 100 instructions that every step then issues.)
-#pragma unroll 1
-        for (int once = masked ? p.one : 0; once > 0; --once) {
+        if (masked) {
           ChunkSeq cs;
           cs.n = info.n;
           cs.C = info.C;
@@ -392,8 +413,7 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
               pr[u][nb][e] = fmaf(sc[u][nb][e], rs[nb][e & 1], -m[nb][e & 1]);
               above |= pr[u][nb][e] > kRescaleThreshold;
             }
-#pragma unroll 1
-        for (int once = __any_sync(full, above) ? p.one : 0; once > 0; --once) {
+        if (__any_sync(full, above)) {
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -439,16 +459,8 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
           const VCodes<D> v2 = load_v(s, kv + 8 + va, g), v3 = load_v(s, kv + 8 + vb, g);
           constexpr int kScales = D / kQ4Group;
           const int vg = D == 128 ? g : g >> 1;
-          uint32_t s01 = s.vs[(kv + va) * kScales + vg] | s.vs[(kv + vb) * kScales + vg] << 8;
-          uint32_t s23 = s.vs[(kv + 8 + va) * kScales + vg] | s.vs[(kv + 8 + vb) * kScales + vg] << 8;
-#pragma unroll 1
-          for (int once = masked ? p.one : 0; once > 0; --once) {
-            // values of rows that no token of the unit sees may be anything: 0
-            const int lo = info.lo, se = info.se, w0 = info.w0, hi = info.hi, at = key0 + kv;
-            auto seen = [&](int key) { return key >= lo && key < hi && (!SINKS || key < se || key >= w0); };
-            s01 &= (seen(at + va) ? 0xffu : 0u) | (seen(at + vb) ? 0xff00u : 0u);
-            s23 &= (seen(at + 8 + va) ? 0xffu : 0u) | (seen(at + 8 + vb) ? 0xff00u : 0u);
-          }
+          const uint32_t s01 = s.vs[(kv + va) * kScales + vg] | s.vs[(kv + vb) * kScales + vg] << 8;
+          const uint32_t s23 = s.vs[(kv + 8 + va) * kScales + vg] | s.vs[(kv + 8 + vb) * kScales + vg] << 8;
           const uint32_t f01 = q4_scale_pair(s01), f23 = q4_scale_pair(s23);
           constexpr uint32_t kLow = 0x0f0f0f0fu;
 #pragma unroll
@@ -689,7 +701,6 @@ cudaError_t launch_chunk_attention_q4(const ChunkArgs& a, const simsd_q4_cache& 
   Q4Params p{};
   p.a = a;
   p.c = c;
-  p.one = 1;
   p.g = a.Hq / a.Hkv;
   p.sub = a.page_size % kTile == 0 ? kTile : std::min(a.page_size, 64);
   p.scale_log2 = a.scale * c.k_unit * 1.4426950408889634f;
