@@ -15,25 +15,26 @@
 // end of a run are merged by a second launch.
 //
 // A tile's softmax is one chain of waits, loads and exponentials a row, some
-// 3800 cycles where one warp does it for 32 rows by itself (127 us for 32
-// blocks of 16 tokens over 4096 rows).  So two sets of warps take a unit's
-// tiles in turns, each with a reference, a sum and an O of its own, which are
-// put together at the unit's end: the products and the waits of one set lie
-// under the exponentials of the other.
+// 3800 cycles where a thread takes all 128 keys of a row.  So a row's keys are
+// shared by two threads, 64 each, which have a reference and a sum of their
+// own and are put together at the unit's end.  Lean units, of up to 64 rows,
+// have their rows of Q twice, in the lanes 0-63 and 64-127 of tensor memory:
+// the first take a tile's first 64 keys, the others the last 64, and set the P
+// of the keys that are not theirs to zero.  All four partitions of the SM then
+// share the exponentials, at the same number of matrix instructions.  Wider
+// units have a second set of softmax warps for the last 64 keys, with an O of
+// its own.  S has two buffers: S of the next tile is formed under the softmax
+// of this one.  32 blocks of 16 tokens over 4096 rows take 100 us (sets of warps
+// that took whole tiles in turns, each with one S:
+// 106).
 //
-// Warp roles (640 threads): warps 0-3 softmax of the even tiles, 4-7 of the
-// odd ones (thread i of a set owns query row i = TMEM lane i; the even set
-// turns Q into fp16 in place); warps 8-15 K and V; warp 16 walks the run and
-// issues all copies; warps 17 and 18 the MMAs of the two sets, each its S and
-// PV in turns (one warp for both took 2690 cycles a tile, half of them waits).
-// Lean units, of up to 64 rows, have their rows of Q twice, in the lanes 0-63
-// and 64-127: the first take a tile's first 64 keys, the others the last 64,
-// and set the P of the keys that are not theirs to zero.  All four partitions
-// of the SM then share the exponentials, which else lie on two (32 blocks of
-// 16 tokens: 140 us), at the same number of matrix instructions; O comes
-// together at the unit's end through shared memory.
-// TMEM (512 columns): S of the sets [0,128), [128,256); O of the sets [256,
-// 384), [384, 512); P (fp16) overwrites the first 64 columns of its S.
+// Warp roles (640 threads): warps 0-3 softmax (thread i owns lane i of tensor
+// memory, and turns its row of Q into fp16 in place), warps 4-7 that of the
+// last 64 keys of wide units; warps 8-11 K, 12-15 V; warp 16 walks the run and
+// issues all copies; warp 17 issues the products S, warp 18 P V.
+// TMEM (512 columns): S [0,128), [128,256); O [256,384), of the second set [384,
+// 512); P (fp16) of each half of the keys overwrites the first 32 of its own 64
+// columns of S.
 //
 // Every mbarrier wait is bounded; after one expires the CTA raises
 // SIMSD_EW_TIMEOUT, every role leaves its loops, drains its copies and MMAs
@@ -57,13 +58,12 @@ namespace {
 constexpr int kTile = kQ4Tile;
 constexpr int kRows = 128;  // query rows of a unit (MMA M)
 constexpr int kThreads = 640;
-constexpr int kSoftmaxWarps = 8, kWarpConvert = 8, kConvertWarps = 8,  // (half of them K, half V)
-              kWarpWalk = 16, kWarpMma = 17;  // (warp 18: the MMAs of the odd set)
+constexpr int kWarpConvert = 8, kConvertWarps = 8,  // (half of them K, half V)
+              kWarpWalk = 16, kWarpS = 17, kWarpPv = 18;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColO = 256;  // + 128 per set
 constexpr int kHalfBytes = kTile * 128;  // 128 rows x 64 fp16
 constexpr int kInfos = 8;                // tiles that the walk is ahead of the last reader
-constexpr int kInfoReaders = kSoftmaxWarps + kConvertWarps + 2;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -81,6 +81,7 @@ struct alignas(1024) SmemQ4Tc {
   static constexpr int kTileBytes = kHalves * kHalfBytes;
   static constexpr int kSlots = D == 128 ? 2 : 4;   // of K, and of V
   static constexpr int kStages = D == 64 ? 6 : LEAN ? 2 : 3;  // of codes
+  static constexpr int kSoftmaxWarps = LEAN ? 4 : 8;
   uint8_t k[kSlots][kTileBytes], v[kSlots][kTileBytes];
   uint8_t q[kTileBytes];
   Stage<D> ring[kStages];
@@ -90,12 +91,12 @@ struct alignas(1024) SmemQ4Tc {
   uint64_t bar_info[kInfos], bar_infofree[kInfos];
   uint64_t bar_qraw, bar_q, bar_qfree;
   uint64_t bar_s[2], bar_p[2][2], bar_pv[2], bar_ofree, bar_meet, bar_drain[2];
-  float2 ml[2][2][kRows];  // (m, l) of the sets, for pieces in turns
+  float2 ml[2][2][kRows];  // (m, l) of the sets' lanes, for pieces in turns
   float q_up[2][kRows];    // the powers of two that Q was divided by, for units in turns
   // lean units: O of the upper lanes on its way to the lower ones, 16 columns
-  // at a time, in two buffers a set
-  float o[LEAN ? 2 : 1][LEAN ? 2 : 1][16][kRows / 2];
-  uint64_t bar_x[2][2], bar_xfree[2][2];
+  // at a time, in two buffers
+  float o[LEAN ? 2 : 1][16][kRows / 2];
+  uint64_t bar_x[2], bar_xfree[2];
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -156,11 +157,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int s = 0; s < kInfos; ++s) {
       mbar_init(smem_u32(&sm.bar_info[s]), 1);
-      mbar_init(smem_u32(&sm.bar_infofree[s]), kInfoReaders);
+      mbar_init(smem_u32(&sm.bar_infofree[s]), Smem::kSoftmaxWarps + kConvertWarps + 2);
     }
     mbar_init(smem_u32(&sm.bar_qraw), 1);
     mbar_init(smem_u32(&sm.bar_q), 4);
-    mbar_init(smem_u32(&sm.bar_qfree), 2);
+    mbar_init(smem_u32(&sm.bar_qfree), 1);
     for (int x = 0; x < 2; ++x) {
       mbar_init(smem_u32(&sm.bar_s[x]), 1);
       mbar_init(smem_u32(&sm.bar_p[x][0]), 4);
@@ -168,17 +169,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     mbar_init(smem_u32(&sm.bar_pv[0]), 1);
     mbar_init(smem_u32(&sm.bar_pv[1]), 1);
-    mbar_init(smem_u32(&sm.bar_ofree), kSoftmaxWarps);
-    mbar_init(smem_u32(&sm.bar_meet), kSoftmaxWarps);
+    mbar_init(smem_u32(&sm.bar_ofree), Smem::kSoftmaxWarps);
+    mbar_init(smem_u32(&sm.bar_meet), Smem::kSoftmaxWarps);
     mbar_init(smem_u32(&sm.bar_drain[0]), 1);
     mbar_init(smem_u32(&sm.bar_drain[1]), 1);
-    for (int x = 0; x < 4; ++x) {
-      mbar_init(smem_u32(&sm.bar_x[x >> 1][x & 1]), 2);
-      mbar_init(smem_u32(&sm.bar_xfree[x >> 1][x & 1]), 2);
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(smem_u32(&sm.bar_x[x]), 2);
+      mbar_init(smem_u32(&sm.bar_xfree[x]), 2);
     }
     fence_mbar_init();
   }
-  if (warp == kWarpMma) {
+  if (warp == kWarpS) {
     tmem_alloc(smem_u32(&sm.tmem_base), kTmemCols);
     tmem_relinquish();
   }
@@ -273,100 +274,80 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (units > 0) mbar_wait(smem_u32(&sm.bar_qraw), (units - 1) & 1, nullptr);
       }
       __syncwarp();
-    } else if (warp <= kWarpMma + 1) {
-      // ----------------------------------------------------------------- MMAs
-      constexpr uint32_t kIdescQK = idesc_f16_f32(kRows, kTile, 0);
-      constexpr uint32_t kIdescPV = idesc_f16_f32(kRows, D, 1);
-      const uint64_t dq = sdesc_sw128(smem_u32(sm.q), 16, 1024), dk = sdesc_sw128(smem_u32(sm.k[0]), 16, 1024),
-                     dv = sdesc_sw128(smem_u32(sm.v[0]), kHalfBytes, 1024);
-      const uint32_t q_lo = static_cast<uint32_t>(dq), k_lo = static_cast<uint32_t>(dk), v_lo = static_cast<uint32_t>(dv);
-      const uint32_t k_hi = static_cast<uint32_t>(dk >> 32), v_hi = static_cast<uint32_t>(dv >> 32);
-      constexpr uint32_t kTileStep = Smem::kTileBytes >> 4;
+    } else if (warp <= kWarpPv) {
+      // ------------------------------------------------------------- products
+      // Tile n (counted over the run) has S buffer n & 1 and slots n % kSlots of
+      // K and V.
       const bool leader = elect_one();
       auto poll = [&](uint64_t& bar, uint32_t parity) { return mbar_wait_poll(smem_u32(&bar), parity, abort_flag); };
-      const int x = warp - kWarpMma;
-      const uint32_t scol = tmem + 128u * x, ocol = tmem + kColO + 128u * x;
-      uint32_t it = 0, tile = 0, c = 0, units = 0;  // messages read; tiles of the run; of this set; units begun
-      auto message = [&]() {
-        ok = ok && poll(sm.bar_info[it % kInfos], (it / kInfos) & 1);
-        const int flags = ok ? sm.info[it % kInfos].flags : kEnd;
-        if (ok) arrive(sm.bar_infofree[it % kInfos]);
-        ++it;
-        return flags;
-      };
-      while (ok) {
-        int flags = message();
+      constexpr uint32_t kTileStep = Smem::kTileBytes >> 4;
+      uint32_t n = 0, units = 0;
+      for (uint32_t it = 0; ok; ++it) {
+        ok = poll(sm.bar_info[it % kInfos], (it / kInfos) & 1);
+        if (!ok) break;
+        const int flags = sm.info[it % kInfos].flags;
+        arrive(sm.bar_infofree[it % kInfos]);
         if (flags & kEnd) break;
         if (flags & kEmpty) continue;
-        ++units;
-        uint32_t j = x;  // tile of the piece
-        bool more = true;
-        if (x == 1) {
-          more = !(flags & kLast);
-          if (more) flags = message();
-        }
-        const uint32_t tile0 = tile;
-        tile += x == 1 && !more ? 1 : 0;
-        for (bool begin = true; ok && more; begin = false) {
-          const uint32_t n = tile0 + j, slot = n % kSlots, par = (n / kSlots) & 1;
-          if (begin) ok = poll(sm.bar_q, (units - 1) & 1);
-          ok = ok && poll(sm.bar_k[slot], par);
-          // the set's last PV, whose P lies in the same columns, is done
-          if (c > 0) ok = ok && poll(sm.bar_pv[x], (c - 1) & 1);
+        const uint32_t slot = n % kSlots, buf = n & 1;
+        if (warp == kWarpS) {
+          constexpr uint32_t kIdesc = idesc_f16_f32(kRows, kTile, 0);
+          const uint64_t dq = sdesc_sw128(smem_u32(sm.q), 16, 1024), dk = sdesc_sw128(smem_u32(sm.k[0]), 16, 1024);
+          const uint32_t q_lo = static_cast<uint32_t>(dq), hi = static_cast<uint32_t>(dk >> 32);
+          const uint32_t k_lo = static_cast<uint32_t>(dk) + slot * kTileStep;
+          if (flags & kFirst) ok = poll(sm.bar_q, units & 1);
+          ok = ok && poll(sm.bar_k[slot], (n / kSlots) & 1);
+          // the PV whose P lies in the same columns is done
+          if (n >= 2) ok = ok && poll(sm.bar_pv[buf], ((n >> 1) - 1) & 1);
           __syncwarp();
           if (ok && leader) {
             tc_fence_after();
-            const uint32_t b = k_lo + slot * kTileStep;
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
               const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
-              tc_mma_ss_lh(scol, q_lo + off, k_hi, b + off, k_hi, kIdescQK, kk > 0);
+              tc_mma_ss_lh(tmem + 128u * buf, q_lo + off, hi, k_lo + off, hi, kIdesc, kk > 0);
             }
-            tc_commit(smem_u32(&sm.bar_s[x]));
+            tc_commit(smem_u32(&sm.bar_s[buf]));
             tc_commit(smem_u32(&sm.bar_kfree[slot]));
+            if (flags & kLast) tc_commit(smem_u32(&sm.bar_qfree));
           }
           __syncwarp();
-          // the set's next tile is looked up under the softmax of this one; not
-          // beyond the piece, whose end has to be told before the walk goes on
-          bool last = flags & kLast;
-          if (last) {
-            tile = n + 1;
-          } else {
-            last = message() & kLast;
-            tile = n + 2;
-            if (!last) flags = message();
-          }
-          more = !last;
-          ok = ok && poll(sm.bar_v[slot], par);
+        } else {
+          constexpr uint32_t kIdesc = idesc_f16_f32(kRows, D, 1);
+          const uint64_t dv = sdesc_sw128(smem_u32(sm.v[0]), kHalfBytes, 1024);
+          const uint32_t v_lo = static_cast<uint32_t>(dv) + slot * kTileStep, hi = static_cast<uint32_t>(dv >> 32);
+          ok = poll(sm.bar_v[slot], (n / kSlots) & 1);
           // the unit's first PV overwrites O: the epilogue of the unit before has read it
-          if (begin && units > 1) ok = ok && poll(sm.bar_ofree, (units - 2) & 1);
-          const uint32_t b = v_lo + slot * kTileStep;
+          if ((flags & kFirst) && units > 0) ok = ok && poll(sm.bar_ofree, (units - 1) & 1);
 #pragma unroll
           for (int hp = 0; hp < 2; ++hp) {
-            ok = ok && poll(sm.bar_p[x][hp], c & 1);
+            ok = ok && poll(sm.bar_p[buf][hp], (n >> 1) & 1);
             __syncwarp();
             if (ok && leader) {
               tc_fence_after();
 #pragma unroll
-              for (int kk = 4 * hp; kk < 4 * hp + 4; ++kk)
-                tc_mma_ts_lh(ocol, scol + 8 * kk, b + kk * 128, v_hi, kIdescPV, (begin && kk == 0) ? 0u : 1u);
+              for (int kk = 4 * hp; kk < 4 * hp + 4; ++kk) {
+                // (the first products of an O; wide units have one for each half of the keys)
+                const bool first = (flags & kFirst) && (kk == 0 || (!LEAN && kk == 4));
+                tc_mma_ts_lh(tmem + kColO + (LEAN ? 0u : 128u * hp), tmem + 128u * buf + 32 * hp + 8 * kk, v_lo + kk * 128, hi, kIdesc,
+                             first ? 0u : 1u);
+              }
               if (hp == 1) {
-                tc_commit(smem_u32(&sm.bar_pv[x]));
+                tc_commit(smem_u32(&sm.bar_pv[buf]));
                 tc_commit(smem_u32(&sm.bar_vfree[slot]));
               }
             }
             __syncwarp();
           }
-          ++c;
-          j += 2;
         }
-        // Q is free once both sets are done with it (their last P was formed from S)
-        if (ok) arrive(sm.bar_qfree);
+        ++n;
+        if (flags & kLast) ++units;
       }
       if (!ok) give_up();
       if (leader) {
-        tc_commit(smem_u32(&sm.bar_drain[x]));
-        mbar_wait(smem_u32(&sm.bar_drain[x]), 0, nullptr);
+        uint64_t& drain = sm.bar_drain[warp - kWarpS];
+        tc_commit(smem_u32(&drain));
+        mbar_wait(smem_u32(&drain), 0, nullptr);
       }
       __syncwarp();
     }
@@ -438,15 +419,16 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
     // -------------------------------------------------------------- softmax
-    const int set = warp >> 2, row = tid & (kRows - 1);  // row: of tensor memory
-    const int upper = LEAN ? row >> 6 : 0, ur = LEAN ? row & 63 : row, tl = ur / p.g, hl = ur - tl * p.g;
+    // (lean units: the warps of the second set have nothing to do)
+    const int set = warp >> 2, row = tid & (kRows - 1);        // row: the lane of tensor memory
+    const int upper = LEAN ? row >> 6 : 0, half = LEAN ? upper : set;  // which 64 keys of a tile
+    const int ur = LEAN ? row & 63 : row, tl = ur / p.g, hl = ur - tl * p.g;
     const uint32_t lane_tmem = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-    const uint32_t s_tmem = lane_tmem + 128u * set, o_tmem = lane_tmem + kColO + 128u * set;
-    uint32_t c = 0, others = 0, units = 0, in_piece = 0;  // tiles of this set and of the other; units; tiles of the piece
-    uint32_t turns = 0;                                   // of the buffers that O passes through
+    const uint32_t o_tmem = lane_tmem + kColO + 128u * set;
+    uint32_t c = 0, units = 0, turns = 0;  // tiles; units; turns of the buffers that O passes through
     bool seen = false;  // the row sees a key
     float m_ref = -INFINITY, l_sum = 0.f, scale = 0.f;
-    for (uint32_t it = 0; ok; ++it) {
+    for (uint32_t it = 0; ok && (!LEAN || set == 0); ++it) {
       ok = wait(sm.bar_info[it % kInfos], (it / kInfos) & 1);
       if (!ok) break;
       const TileInfo& info = sm.info[it % kInfos];
@@ -472,11 +454,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         seen = lo < hi;
         m_ref = -INFINITY;
         l_sum = 0.f;
-        in_piece = 0;
         if (!empty) {
           // this thread's row of Q: the power of two that its components take,
-          // and by the even set its fp16 form, in place of itself
-          ok = wait(sm.bar_qraw, units & 1);
+          // and by the first set its fp16 form, in place of itself (the other set
+          // does not wait for the copy, which may be a unit ahead of it)
+          if (set == 0) ok = wait(sm.bar_qraw, units & 1);
           if (!ok) break;
           uint4* qr[kHalves];
           uint32_t top = 0;
@@ -518,42 +500,38 @@ __global__ void __launch_bounds__(kThreads, 1)
           ++units;
         }
       }
-      if (!empty && (in_piece & 1) != static_cast<uint32_t>(set)) {
-        ++others;  // the other set's tile
-      } else if (!empty) {
-        ok = wait(sm.bar_s[set], c & 1);
+      if (!empty) {
+        const uint32_t buf = c & 1, s_tmem = lane_tmem + 128u * buf;
+        ok = wait(sm.bar_s[buf], (c >> 1) & 1);
         if (!ok) break;
         // (a warp without a row that sees a key only keeps the hand-offs going)
         if (!__any_sync(full, seen)) {
-          arrive(sm.bar_p[set][0]);
-          arrive(sm.bar_p[set][1]);
+          if constexpr (LEAN) arrive(sm.bar_p[buf][half ^ 1]);
+          arrive(sm.bar_p[buf][half]);
         } else {
           tc_fence_after();
           // 64 columns of S, the keys that the row does not see at -inf
           uint32_t xs[2][32];
-          auto load = [&](int hp) {
-            tmem_ld32(s_tmem + 64 * hp, xs[0]);
-            tmem_ld32(s_tmem + 64 * hp + 32, xs[1]);
-            tmem_wait_ld();
-            if (!(flags & kFull)) {
-              int lo, hi, kse;
-              row_keys(lo, hi, kse);
-              const int key0 = info.key0, ks = info.ks;
-              const int from = min(max(lo - key0, 0), kTile), to = min(max(hi - key0, 0), kTile);
+          tmem_ld32(s_tmem + 64 * half, xs[0]);
+          tmem_ld32(s_tmem + 64 * half + 32, xs[1]);
+          tmem_wait_ld();
+          if (!(flags & kFull)) {
+            int lo, hi, kse;
+            row_keys(lo, hi, kse);
+            const int key0 = info.key0 + 64 * half, ks = info.ks;
+            const int from = min(max(lo - key0, 0), 64), to = min(max(hi - key0, 0), 64);
 #pragma unroll
-              for (int wd = 0; wd < 2; ++wd) {
-                const int at = 64 * hp + 32 * wd;
-                const int f = min(max(from - at, 0), 32), e = min(max(to - at, 0), 32);
-                uint32_t keep = e > f ? (0xffffffffu >> (32 - (e - f))) << f : 0u;  // bits f .. e-1
-                if constexpr (SINKS) {
-                  const int sf = min(max(ks - key0 - at, 0), 32), se = min(max(kse - key0 - at, 0), 32);
-                  keep |= se > sf ? (0xffffffffu >> (32 - (se - sf))) << sf : 0u;
-                }
-#pragma unroll
-                for (int k = 0; k < 32; ++k) xs[wd][k] = (keep >> k) & 1u ? xs[wd][k] : 0xff800000u;
+            for (int wd = 0; wd < 2; ++wd) {
+              const int f = min(max(from - 32 * wd, 0), 32), e = min(max(to - 32 * wd, 0), 32);
+              uint32_t keep = e > f ? (0xffffffffu >> (32 - (e - f))) << f : 0u;  // bits f .. e-1
+              if constexpr (SINKS) {
+                const int sf = min(max(ks - key0 - 32 * wd, 0), 32), se = min(max(kse - key0 - 32 * wd, 0), 32);
+                keep |= se > sf ? (0xffffffffu >> (32 - (se - sf))) << sf : 0u;
               }
+#pragma unroll
+              for (int k = 0; k < 32; ++k) xs[wd][k] = (keep >> k) & 1u ? xs[wd][k] : 0xff800000u;
             }
-          };
+          }
           auto max_of = [&]() {
             float r[8];
 #pragma unroll
@@ -566,21 +544,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int k = 0; k < 8; ++k) r[k] = fmaxf(r[k], __uint_as_float(xs[1][k + 24]));
             return fmax3(fmax3(r[0], r[1], r[2]), fmax3(r[3], r[4], r[5]), fmaxf(r[6], r[7]));
           };
-          float mx = -INFINITY;
-          if constexpr (!LEAN) {
-            load(1);
-            mx = max_of();
-          }
-          load(upper);
-          mx = fmaxf(mx, max_of()) * scale;
+          const float mx = max_of() * scale;
           const bool move = seen && mx != -INFINITY && (m_ref == -INFINITY || mx > m_ref + kRescaleThreshold);
           if (__any_sync(full, move)) {
             const float f = move && m_ref != -INFINITY ? fast_exp2(m_ref - mx) : 1.0f;
             l_sum *= f;
             if (move) m_ref = mx;
-            if (in_piece >= 2) {
-              // O holds the set's earlier tiles once its last PV is done
-              ok = wait(sm.bar_pv[set], (c - 1) & 1);
+            if (!(flags & kFirst)) {
+              // O holds the piece's earlier tiles once the PV before this one is done
+              ok = wait(sm.bar_pv[buf ^ 1], ((c - 1) >> 1) & 1);
               if (!ok) break;
               tc_fence_after();
 #pragma unroll 1
@@ -600,38 +572,32 @@ __global__ void __launch_bounds__(kThreads, 1)
           if constexpr (LEAN) {
             // the keys of the other half of the lanes
             const uint32_t none[16] = {};
-            tmem_st16(s_tmem + 32 * (1 - upper), none);
-            tmem_st16(s_tmem + 32 * (1 - upper) + 16, none);
+            tmem_st16(s_tmem + 64 * (1 - half), none);
+            tmem_st16(s_tmem + 64 * (1 - half) + 16, none);
           }
-#pragma unroll 1
-          for (int h = 0; h < (LEAN ? 1 : 2); ++h) {
-            const int hp = LEAN ? upper : h;
-            if (h == 1) load(1);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              uint32_t pk[16];
+          for (int q = 0; q < 2; ++q) {
+            uint32_t pk[16];
 #pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                float e0, e1;
-                f32x2_split(fma_f32x2(f32x2(__uint_as_float(xs[q][2 * k]), __uint_as_float(xs[q][2 * k + 1])), sc2, nm2), e0, e1);
-                const float p0 = fast_exp2(e0), p1 = fast_exp2(e1);
-                acc[k & 1] = add_f32x2(acc[k & 1], f32x2(p0, p1));
-                pk[k] = pack_f16x2(p0, p1);
-              }
-              tmem_st16(s_tmem + 32 * hp + 16 * q, pk);
+            for (int k = 0; k < 16; ++k) {
+              float e0, e1;
+              f32x2_split(fma_f32x2(f32x2(__uint_as_float(xs[q][2 * k]), __uint_as_float(xs[q][2 * k + 1])), sc2, nm2), e0, e1);
+              const float p0 = fast_exp2(e0), p1 = fast_exp2(e1);
+              acc[k & 1] = add_f32x2(acc[k & 1], f32x2(p0, p1));
+              pk[k] = pack_f16x2(p0, p1);
             }
-            tmem_wait_st();
-            tc_fence_before();
-            if constexpr (LEAN) arrive(sm.bar_p[set][hp ^ 1]);
-            arrive(sm.bar_p[set][hp]);
+            tmem_st16(s_tmem + 64 * half + 16 * q, pk);
           }
+          tmem_wait_st();
+          tc_fence_before();
+          if constexpr (LEAN) arrive(sm.bar_p[buf][half ^ 1]);
+          arrive(sm.bar_p[buf][half]);
           float s0, s1;
           f32x2_split(add_f32x2(acc[0], acc[1]), s0, s1);
           l_sum += s0 + s1;
         }
         ++c;
       }
-      if (!empty) ++in_piece;
       if (flags & kLastPiece) pdl_launch_next();
       if (!(flags & kLast)) {
         arrive(sm.bar_infofree[it % kInfos]);
@@ -649,21 +615,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         ml[set][row] = make_float2(m_ref, l_sum);
         arrive(sm.bar_meet);
         ok = wait(sm.bar_meet, (units - 1) & 1);
-        if (c > 0) ok = ok && wait(sm.bar_pv[set], (c - 1) & 1);
-        if (others > 0) ok = ok && wait(sm.bar_pv[set ^ 1], (others - 1) & 1);
+        ok = ok && wait(sm.bar_pv[(c - 1) & 1], ((c - 1) >> 1) & 1);
         if (!ok) break;
         tc_fence_after();
-        const float2 x = ml[set ^ 1][row];
+        const float2 x = LEAN ? ml[0][row ^ 64] : ml[set ^ 1][row];
         M = fmaxf(m_ref, x.x);
-        if constexpr (LEAN) M = fmaxf(M, fmaxf(ml[0][row ^ 64].x, ml[1][row ^ 64].x));
         const float ref = M == -INFINITY ? 0.f : M;
         mine = fast_exp2(m_ref - ref);
         theirs = fast_exp2(x.x - ref);
         L = fmaf(mine, l_sum, theirs * x.y);
-        if constexpr (LEAN) {
-          const float2 y = ml[0][row ^ 64], z = ml[1][row ^ 64];
-          L += fmaf(fast_exp2(y.x - ref), y.y, fast_exp2(z.x - ref) * z.y);
-        }
       }
       const bool any = !empty && seen && L != 0.f && !bad;
       const float norm = !any ? 0.f : part ? 1.f : p.c.v_unit / L;
@@ -672,23 +632,23 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int entry = static_cast<int>(blockIdx.x) * 2 + (flags & kSlot1 ? 1 : 0);
       uint4* orow = reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.a.out) + out_row * (2 * D));
 #pragma unroll 1
-      for (int q = set * (D / 32); q < (set + 1) * (D / 32); ++q) {
+      for (int q = LEAN ? 0 : set * (D / 32); q < (LEAN ? D / 16 : (set + 1) * (D / 32)); ++q) {
         float o[16];
         {
           uint32_t a[16], b[16];
-          // (the sets' tiles in the piece: half of them, the even set's rounded up)
-          const bool have = in_piece > static_cast<uint32_t>(set), have_other = in_piece > static_cast<uint32_t>(set ^ 1);
-          if (have) tmem_ld16(o_tmem + 16 * q, a);
-          if (have_other) tmem_ld16(lane_tmem + kColO + 128u * (set ^ 1) + 16 * q, b);
-          if (!empty) tmem_wait_ld();
+          if (!empty) {
+            tmem_ld16(o_tmem + 16 * q, a);
+            if constexpr (!LEAN) tmem_ld16(lane_tmem + kColO + 128u * (set ^ 1) + 16 * q, b);
+            tmem_wait_ld();
+          }
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            o[k] = have ? __uint_as_float(a[k]) * mine : 0.f;
-            if (have_other) o[k] = fmaf(__uint_as_float(b[k]), theirs, o[k]);
+            o[k] = empty ? 0.f : __uint_as_float(a[k]) * mine;
+            if constexpr (!LEAN) o[k] = empty ? 0.f : fmaf(__uint_as_float(b[k]), theirs, o[k]);
           }
         }
-        if (!empty && q == (set + 1) * (D / 32) - 1) {
-          // both O may be overwritten by the next unit's first PVs
+        if (!empty && q == (LEAN ? D / 16 : (set + 1) * (D / 32)) - 1) {
+          // O may be overwritten by the next unit's first PV
           tc_fence_before();
           arrive(sm.bar_ofree);
         }
@@ -696,17 +656,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           // the upper lanes' share goes to the lower ones
           if (!empty) {
             const uint32_t buf = turns & 1, use = turns >> 1;
-            float(*to)[kRows / 2] = sm.o[set][buf];
+            float(*to)[kRows / 2] = sm.o[buf];
             if (upper) {
-              if (use > 0) ok = ok && wait(sm.bar_xfree[set][buf], (use - 1) & 1);
+              if (use > 0) ok = ok && wait(sm.bar_xfree[buf], (use - 1) & 1);
 #pragma unroll
               for (int k = 0; k < 16; ++k) to[k][ur] = o[k];
-              arrive(sm.bar_x[set][buf]);
+              arrive(sm.bar_x[buf]);
             } else {
-              ok = ok && wait(sm.bar_x[set][buf], use & 1);
+              ok = ok && wait(sm.bar_x[buf], use & 1);
 #pragma unroll
               for (int k = 0; k < 16; ++k) o[k] += to[k][ur];
-              arrive(sm.bar_xfree[set][buf]);
+              arrive(sm.bar_xfree[buf]);
             }
             ++turns;
           }
@@ -735,7 +695,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == kWarpMma) {
+  if (warp == kWarpS) {
     tc_fence_after();
     tmem_dealloc(tmem, kTmemCols);
   }
