@@ -28,7 +28,7 @@
 //
 // Bound: the issue of instructions, some 320 for 16 keys (64 conversions and
 // 64 products with a scale among them): 64 single tokens over 2048 to 8192
-// rows, 32 heads on 8 of 128, read 377 MB in 87 us (4.3 TB/s; without the
+// rows, 32 heads on 8 of 128, read 377 MB in 85 us (4.4 TB/s; without the
 // copies it takes 82, without the products with V 67).
 //
 // Every mbarrier wait is bounded; after one expires the CTA raises
@@ -64,7 +64,7 @@ struct Q4Params {
 
 // NB blocks of 8 query rows.  One takes few registers: three CTAs an SM of
 // four warps, whose 32 keys a tile pay for what a tile costs beside its
-// products (64 single tokens over 2048 to 8192 rows: 87 us; four CTAs, with 96
+// products (64 single tokens over 2048 to 8192 rows: 85 us; four CTAs, with 96
 // registers a thread, 92; eight warps of 16 keys, two CTAs, 113).  Two: one CTA
 // of eight warps.
 template <int D, int NB>
@@ -206,8 +206,7 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
   if (warp == kWarps) {
     // -------------------------------------------------------- walk and copies
     TileWalk<D, SINKS> tw;
-    tw.ub = p.ub;
-    tw.sub = p.sub;
+    tw.sizes(p.ub, p.sub, p.a.page_size);
     tw.k.begin(p.a, p.ub, p.ctas, start, seq, total);
     uint32_t it = 0, units = 0;  // tiles passed on, of them with a Q
     bool ok = true;
@@ -227,13 +226,14 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
           if (!ok) break;
         }
         const uint32_t bar = smem_u32(&sm.bar_full[st]);
-        const uint32_t bytes = tw.bytes() + (with_q ? tw.u.ntok * q_bytes : 0u);
+        const uint32_t bytes = 2 * tw.bytes() + (with_q ? tw.u.ntok * q_bytes : 0u);
         if (lane == 0) {
           sm.info[st] = tw.u;
           mbar_arrive_expect_tx(bar, bytes);
         }
         __syncwarp();
-        tw.copy(p.c, sm.ring[st], bar);
+        tw.copy_k(p.c, sm.ring[st], bar);
+        tw.copy_v(p.c, sm.ring[st], bar);
         if (with_q) {
           for (int x = lane; x < tw.u.ntok; x += 32)
             bulk_load(smem_u32(&sm.q[qb][x * p.g * D]),

@@ -24,17 +24,26 @@
 // share the exponentials, at the same number of matrix instructions.  Wider
 // units have a second set of softmax warps for the last 64 keys, with an O of
 // its own.  S has two buffers: S of the next tile is formed under the softmax
-// of this one.  32 blocks of 16 tokens over 4096 rows take 100 us (sets of warps
-// that took whole tiles in turns, each with one S:
-// 106).
+// of this one.
+//
+// Bound and measured.  32 blocks of 16 tokens over 4096 rows (32 heads on 8,
+// D = 128; 155 MB, 23 us of copies) take 95 us, of 32 tokens 103.  The matrix
+// instructions of a tile take half of its 2300 cycles; the rest are the chains
+// beside them, each of which is about as long: one warp of an SM partition
+// turns 32 rows of K and one 32 rows of V (1500 cycles, 900 of hand-offs), one
+// does the softmax, one looks up pages and copies.  Without the turning 80 us,
+// without the softmax 85, without both 71.  Not faster: twelve turning warps
+// and the softmax of a tile over eight warps (96: as many instructions more);
+// more rows in flight for each turning warp (110 to 118).  Sets of softmax warps
+// that took whole tiles in turns, each with one S: 106.
 //
 // Warp roles (640 threads): warps 0-3 softmax (thread i owns lane i of tensor
-// memory, and turns its row of Q into fp16 in place), warps 4-7 that of the
-// last 64 keys of wide units; warps 8-11 K, 12-15 V; warp 16 walks the run and
-// issues all copies; warp 17 issues the products S, warp 18 P V.
-// TMEM (512 columns): S [0,128), [128,256); O [256,384), of the second set [384,
-// 512); P (fp16) of each half of the keys overwrites the first 32 of its own 64
-// columns of S.
+// memory, and turns its row of Q into fp16), warps 4-7 that of the last 64 keys
+// of wide units; warps 8-11 K, 12-15 V; warps 16 and 19 walk the run and issue
+// the copies of K and Q, and of V; warp 17 issues the products S, warp 18 P V.
+// TMEM (512 columns): S [0,128), [128,256); O [256,384); [384,512) O of the
+// second set, or the Q of lean units (else Q stays in shared memory); P (fp16)
+// of each half of the keys overwrites the first 32 of its own 64 columns of S.
 //
 // Every mbarrier wait is bounded; after one expires the CTA raises
 // SIMSD_EW_TIMEOUT, every role leaves its loops, drains its copies and MMAs
@@ -59,9 +68,10 @@ constexpr int kTile = kQ4Tile;
 constexpr int kRows = 128;  // query rows of a unit (MMA M)
 constexpr int kThreads = 640;
 constexpr int kWarpConvert = 8, kConvertWarps = 8,  // (half of them K, half V)
-              kWarpWalk = 16, kWarpS = 17, kWarpPv = 18;
+              kWarpWalk = 16, kWarpS = 17, kWarpPv = 18, kWarpWalkV = 19;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColO = 256;  // + 128 per set
+constexpr uint32_t kColQ = 384;  // lean units: Q
 constexpr int kHalfBytes = kTile * 128;  // 128 rows x 64 fp16
 constexpr int kInfos = 8;                // tiles that the walk is ahead of the last reader
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
@@ -79,11 +89,12 @@ template <int D, bool LEAN>
 struct alignas(1024) SmemQ4Tc {
   static constexpr int kHalves = D / 64;
   static constexpr int kTileBytes = kHalves * kHalfBytes;
+  static constexpr int kQHalf = LEAN ? kHalfBytes / 2 : kHalfBytes;
   static constexpr int kSlots = D == 128 ? 2 : 4;   // of K, and of V
-  static constexpr int kStages = D == 64 ? 6 : LEAN ? 2 : 3;  // of codes
+  static constexpr int kStages = D == 64 ? 6 : 3;  // of codes
   static constexpr int kSoftmaxWarps = LEAN ? 4 : 8;
   uint8_t k[kSlots][kTileBytes], v[kSlots][kTileBytes];
-  uint8_t q[kTileBytes];
+  uint8_t q[kHalves * kQHalf];
   Stage<D> ring[kStages];
   TileInfo info[kInfos];
   uint64_t bar_code[kStages], bar_codefree[kStages];
@@ -91,7 +102,7 @@ struct alignas(1024) SmemQ4Tc {
   uint64_t bar_info[kInfos], bar_infofree[kInfos];
   uint64_t bar_qraw, bar_q, bar_qfree;
   uint64_t bar_s[2], bar_p[2][2], bar_pv[2], bar_ofree, bar_meet, bar_drain[2];
-  float2 ml[2][2][kRows];  // (m, l) of the sets' lanes, for pieces in turns
+  float2 ml[2][LEAN ? 1 : 2][kRows];  // (m, l) of the sets' lanes, for pieces in turns
   float q_up[2][kRows];    // the powers of two that Q was divided by, for units in turns
   // lean units: O of the upper lanes on its way to the lower ones, 16 columns
   // at a time, in two buffers
@@ -146,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (tid == 0) {
     sm.abort_flag = 0;
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(smem_u32(&sm.bar_code[s]), 1);
+      mbar_init(smem_u32(&sm.bar_code[s]), 2);
       mbar_init(smem_u32(&sm.bar_codefree[s]), kConvertWarps);
     }
     for (int s = 0; s < kSlots; ++s) {
@@ -161,7 +172,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     mbar_init(smem_u32(&sm.bar_qraw), 1);
     mbar_init(smem_u32(&sm.bar_q), 4);
-    mbar_init(smem_u32(&sm.bar_qfree), 1);
+    mbar_init(smem_u32(&sm.bar_qfree), LEAN ? 4 : 1);
     for (int x = 0; x < 2; ++x) {
       mbar_init(smem_u32(&sm.bar_s[x]), 1);
       mbar_init(smem_u32(&sm.bar_p[x][0]), 4);
@@ -190,7 +201,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   Place start{0, 0, 0, 0};
   int total = 0;
   ChunkSeq seq{};
-  if (warp == kWarpWalk) start = plan_start<SINKS, kTile>(p.a, p.tb, p.ctas, tiles, total, seq);
+  if (warp == kWarpWalk || warp == kWarpWalkV) start = plan_start<SINKS, kTile>(p.a, p.tb, p.ctas, tiles, total, seq);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -211,14 +222,17 @@ __global__ void __launch_bounds__(kThreads, 1)
   // register split: 256 x 128 + 256 x 72 + 128 x 80 = 61,440 = the launch's 640 x 96
   if (warp >= kWarpWalk) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (warp == kWarpWalk) {
+    if (warp == kWarpWalk || warp == kWarpWalkV) {
       // ------------------------------------------------------ walk and copies
+      // Both warps walk the run; one copies K and Q and tells the others of the
+      // tiles, one copies V.
+      const bool tells = warp == kWarpWalk;
       TileWalk<D, SINKS> tw;
-      tw.ub = p.tb;
-      tw.sub = p.sub;
+      tw.sizes(p.tb, p.sub, p.a.page_size);
       tw.k.begin(p.a, p.tb, p.ctas, start, seq, total);
       uint32_t it = 0, codes = 0, units = 0;  // messages; tiles with copies; Q tiles
       auto say = [&](const TileInfo& u) {
+        if (!tells) return;
         if (it >= kInfos) ok = wait(sm.bar_infofree[it % kInfos], ((it / kInfos) - 1) & 1);
         if (!ok) return;
         if (lane == 0) {
@@ -238,19 +252,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t bar = smem_u32(&sm.bar_code[st]), bytes = tw.bytes();
             if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
             __syncwarp();
-            tw.copy(p.c, sm.ring[st], bar);
+            if (tells) tw.copy_k(p.c, sm.ring[st], bar);
+            else tw.copy_v(p.c, sm.ring[st], bar);
             ++codes;
-            if (i == 0) {
+            if (i == 0 && tells) {
               // Q, once the unit before has no use for its own any more
               if (units > 0) ok = wait(sm.bar_qfree, (units - 1) & 1);
               if (!ok) break;
               if (lane == 0) {
                 const uint32_t bq = smem_u32(&sm.bar_qraw);
-                mbar_arrive_expect_tx(bq, static_cast<uint32_t>((LEAN ? 2 : 1) * kHalves * p.g * p.tb) * 128u);
+                mbar_arrive_expect_tx(bq, static_cast<uint32_t>(kHalves * p.g * p.tb) * 128u);
 #pragma unroll
-                for (int hf = 0; hf < (LEAN ? 2 : 1) * kHalves; ++hf)
-                  tma_load_3d(smem_u32(sm.q) + (hf % kHalves) * kHalfBytes + (hf / kHalves) * (kHalfBytes / 2), &tm_q, bq,
-                              64 * (hf % kHalves), tw.u.kvh * p.g, tw.u.tok0);
+                for (int hf = 0; hf < kHalves; ++hf)
+                  tma_load_3d(smem_u32(sm.q) + hf * Smem::kQHalf, &tm_q, bq, 64 * hf, tw.u.kvh * p.g, tw.u.tok0);
               }
               ++units;
             }
@@ -266,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         say(u);
       }
       if (!ok) give_up();
-      if (lane == 0 && blockIdx.x > 0) records<D>(p)[blockIdx.x] = boundary_record<SINKS, kTile>(tw.k, p.a, p.tb);
+      if (tells && lane == 0 && blockIdx.x > 0) records<D>(p)[blockIdx.x] = boundary_record<SINKS, kTile>(tw.k, p.a, p.tb);
       // every copy must have landed before the CTA may exit
       if (lane == 0) {
         for (uint32_t j = codes > kStages ? codes - kStages : 0; j < codes; ++j)
@@ -279,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // Tile n (counted over the run) has S buffer n & 1 and slots n % kSlots of
       // K and V.
       const bool leader = elect_one();
-      auto poll = [&](uint64_t& bar, uint32_t parity) { return mbar_wait_poll(smem_u32(&bar), parity, abort_flag); };
+      auto poll = [&](uint64_t& bar, uint32_t parity) { return mbar_wait(smem_u32(&bar), parity, abort_flag); };
       constexpr uint32_t kTileStep = Smem::kTileBytes >> 4;
       uint32_t n = 0, units = 0;
       for (uint32_t it = 0; ok; ++it) {
@@ -305,11 +319,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
               const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
-              tc_mma_ss_lh(tmem + 128u * buf, q_lo + off, hi, k_lo + off, hi, kIdesc, kk > 0);
+              if constexpr (LEAN) tc_mma_ts_lh(tmem + 128u * buf, tmem + kColQ + 8 * kk, k_lo + off, hi, kIdesc, kk > 0);
+              else tc_mma_ss_lh(tmem + 128u * buf, q_lo + off, hi, k_lo + off, hi, kIdesc, kk > 0);
             }
             tc_commit(smem_u32(&sm.bar_s[buf]));
             tc_commit(smem_u32(&sm.bar_kfree[slot]));
-            if (flags & kLast) tc_commit(smem_u32(&sm.bar_qfree));
+            if (!LEAN && (flags & kLast)) tc_commit(smem_u32(&sm.bar_qfree));
           }
           __syncwarp();
         } else {
@@ -456,15 +471,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         l_sum = 0.f;
         if (!empty) {
           // this thread's row of Q: the power of two that its components take,
-          // and by the first set its fp16 form, in place of itself (the other set
-          // does not wait for the copy, which may be a unit ahead of it)
+          // and by the first set its fp16 form, in place of itself or in tensor
+          // memory (the other set does not wait for the copy, which may be a unit
+          // ahead of it)
           if (set == 0) ok = wait(sm.bar_qraw, units & 1);
           if (!ok) break;
           uint4* qr[kHalves];
           uint32_t top = 0;
 #pragma unroll
           for (int hf = 0; hf < kHalves; ++hf) {
-            qr[hf] = reinterpret_cast<uint4*>(sm.q + hf * kHalfBytes + row * 128);
+            qr[hf] = reinterpret_cast<uint4*>(sm.q + hf * Smem::kQHalf + (LEAN ? ur : row) * 128);
             if (set == 0) {
 #pragma unroll
               for (int k = 0; k < 8; ++k) {
@@ -482,14 +498,35 @@ __global__ void __launch_bounds__(kThreads, 1)
             auto half2_of = [&](uint32_t w) {
               return pack_f16x2(__uint_as_float(w << 16) * down, __uint_as_float(w & 0xffff0000u) * down);
             };
+            if constexpr (LEAN) {
 #pragma unroll
-            for (int hf = 0; hf < kHalves; ++hf)
+              for (int hf = 0; hf < kHalves; ++hf)
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const uint4 x = qr[hf][k ^ (row & 7)];
-                qr[hf][k ^ (row & 7)] = make_uint4(half2_of(x.x), half2_of(x.y), half2_of(x.z), half2_of(x.w));
-              }
-            fence_proxy_async_smem();
+                for (int q = 0; q < 2; ++q) {
+                  uint32_t w[16];
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) {
+                    const uint4 x = qr[hf][(4 * q + k) ^ (row & 7)];
+                    w[4 * k] = half2_of(x.x);
+                    w[4 * k + 1] = half2_of(x.y);
+                    w[4 * k + 2] = half2_of(x.z);
+                    w[4 * k + 3] = half2_of(x.w);
+                  }
+                  tmem_st16(lane_tmem + kColQ + 32 * hf + 16 * q, w);
+                }
+              arrive(sm.bar_qfree);
+              tmem_wait_st();
+              tc_fence_before();
+            } else {
+#pragma unroll
+              for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                  const uint4 x = qr[hf][k ^ (row & 7)];
+                  qr[hf][k ^ (row & 7)] = make_uint4(half2_of(x.x), half2_of(x.y), half2_of(x.z), half2_of(x.w));
+                }
+              fence_proxy_async_smem();
+            }
             arrive(sm.bar_q);
           } else {
             ok = wait(sm.bar_q, units & 1);
@@ -568,7 +605,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           const float neg_m = m_ref != -INFINITY ? -m_ref : 0.f;
           const unsigned long long sc2 = f32x2(scale, scale), nm2 = f32x2(neg_m, neg_m);
-          unsigned long long acc[2] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
+          unsigned long long acc[4] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f), f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
           if constexpr (LEAN) {
             // the keys of the other half of the lanes
             const uint32_t none[16] = {};
@@ -583,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               float e0, e1;
               f32x2_split(fma_f32x2(f32x2(__uint_as_float(xs[q][2 * k]), __uint_as_float(xs[q][2 * k + 1])), sc2, nm2), e0, e1);
               const float p0 = fast_exp2(e0), p1 = fast_exp2(e1);
-              acc[k & 1] = add_f32x2(acc[k & 1], f32x2(p0, p1));
+              acc[k & 3] = add_f32x2(acc[k & 3], f32x2(p0, p1));
               pk[k] = pack_f16x2(p0, p1);
             }
             tmem_st16(s_tmem + 64 * half + 16 * q, pk);
@@ -593,7 +630,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if constexpr (LEAN) arrive(sm.bar_p[buf][half ^ 1]);
           arrive(sm.bar_p[buf][half]);
           float s0, s1;
-          f32x2_split(add_f32x2(acc[0], acc[1]), s0, s1);
+          f32x2_split(add_f32x2(add_f32x2(acc[0], acc[1]), add_f32x2(acc[2], acc[3])), s0, s1);
           l_sum += s0 + s1;
         }
         ++c;
@@ -611,14 +648,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       arrive(sm.bar_infofree[it % kInfos]);
       float M = -INFINITY, L = 0.f, mine = 0.f, theirs = 0.f;
       if (!empty) {
-        float2(*ml)[kRows] = sm.ml[units & 1];
+        auto& ml = sm.ml[units & 1];
         ml[set][row] = make_float2(m_ref, l_sum);
         arrive(sm.bar_meet);
         ok = wait(sm.bar_meet, (units - 1) & 1);
         ok = ok && wait(sm.bar_pv[(c - 1) & 1], ((c - 1) >> 1) & 1);
         if (!ok) break;
         tc_fence_after();
-        const float2 x = LEAN ? ml[0][row ^ 64] : ml[set ^ 1][row];
+        const float2 x = ml[LEAN ? 0 : set ^ 1][LEAN ? row ^ 64 : row];
         M = fmaxf(m_ref, x.x);
         const float ref = M == -INFINITY ? 0.f : M;
         mine = fast_exp2(m_ref - ref);

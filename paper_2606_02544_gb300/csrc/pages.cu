@@ -15,7 +15,9 @@
 //
 // Bound: the copies by memory (each byte read once, where a source page is
 // copied many times from L2, and written once), the bookkeeping by the
-// latency of a chain of dependent loads and barriers in one CTA.
+// latency of a chain of dependent loads and barriers in one CTA, some 8 us.
+// 32 forks of a sequence whose last page is filled in part, 268 MB, copy in 46 us
+// (5.8 TB/s), 500 pages, 457 MB read and written, in 66 (6.9 TB/s).
 #include <cuda_runtime.h>
 
 #include <algorithm>

@@ -19,7 +19,10 @@
 // components a lane and quotients by division, took 200 us for 16384 tokens).
 //
 // Bound by memory: a token reads (Hq + 2 Hkv) d elements and writes Hq d and
-// 2 Hkv (d / 2 + d / 16) bytes.
+// 2 Hkv (d / 2 + d / 16) bytes.  16404 tokens of 32 heads on 8 of 128 in bf16
+// (355 MB) take 77 us, 4.6 TB/s, and the cache written out again as keys and
+// values (86 MB) 23 us more; a single token a sequence takes as long as the
+// host's two calls, 15 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>

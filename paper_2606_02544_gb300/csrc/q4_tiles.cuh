@@ -50,9 +50,21 @@ struct TileWalk {
   int ub, sub, flags, skip, tse, all_lo, all_hi, all_se, t0;
   int win_base, win;  // lane i holds the page id of page win_base + i
   const int32_t* bt;
-  // this lane's copy of the tile
+  // this lane's copy of the tile: its first key is u.key0 + at, row off of page
+  // pi (kept from tile to tile, of which each is pages, rest further: a divide
+  // would be a good part of the walk's time)
   bool load;
+  int at, pi, off, pages, rest;
   size_t row;  // in the pool, in rows of a head
+
+  // Tokens of a unit, keys of a copy, and the page size that they hold for.
+  __device__ __forceinline__ void sizes(int unit_tokens, int copy_keys, int P) {
+    ub = unit_tokens;
+    sub = copy_keys;
+    at = min(static_cast<int>(threadIdx.x & 31), kQ4Tile / sub - 1) * sub;
+    pages = kQ4Tile / P;
+    rest = kQ4Tile - pages * P;
+  }
 
   __device__ __forceinline__ bool next_piece(const ChunkArgs& a) {
     if (!k.peek(a, ub, piece)) return false;
@@ -85,39 +97,56 @@ struct TileWalk {
     const unsigned full = 0xffffffffu;
     const int lane = threadIdx.x & 31, P = a.page_size, t = t0 + i;
     const bool empty = flags & kEmpty;
+    const int before = u.key0;
     u.key0 = (t + (SINKS && t >= tse ? skip : 0)) * kQ4Tile;
     const bool all = !empty && ((u.key0 >= all_lo && u.key0 + kQ4Tile <= all_hi) ||
                                 (SINKS && u.key0 >= u.ks && u.key0 + kQ4Tile <= all_se));
     // copy s of the tile is lane s's
-    const int nsub = kQ4Tile / sub, key = u.key0 + min(lane, nsub - 1) * sub, pi = key / P;
-    const int pi0 = u.key0 / P, pi1 = (u.key0 + kQ4Tile - 1) / P;
-    if (pi0 < win_base || pi1 >= win_base + 32) {
-      win_base = pi0;
+    const int key = u.key0 + at;
+    if (i == 0 || u.key0 != before + kQ4Tile) {
+      pi = key / P;
+      off = key - pi * P;
+    } else {
+      pi += pages;
+      off += rest;
+      if (off >= P) {
+        off -= P;
+        ++pi;
+      }
+    }
+    if (__any_sync(full, static_cast<unsigned>(pi - win_base) >= 32u)) {
+      win_base = __shfl_sync(full, pi, 0);
       win = win_base + lane < a.max_pages ? bt[win_base + lane] : -1;
     }
     const int pg = __shfl_sync(full, win, (pi - win_base) & 31);
-    load = !empty && lane < nsub && key + sub > u.lo && key < u.hi && (!SINKS || key < u.se || key + sub > u.w0);
+    load = !empty && lane * sub < kQ4Tile && key + sub > u.lo && key < u.hi && (!SINKS || key < u.se || key + sub > u.w0);
     const bool wrong = load && (pg < 0 || pg >= a.num_pages);
     load = load && !wrong;
     if (__any_sync(full, wrong)) {
       if (lane == 0) raise_error(a.err_word, SIMSD_EW_PAGE);
       flags |= kBad;
     }
-    row = (static_cast<size_t>(pg) * a.Hkv + u.kvh) * P + (key - pi * P);
+    row = (static_cast<size_t>(pg) * a.Hkv + u.kvh) * P + off;
     u.flags = flags | (i == 0 ? kFirst : 0) | (i + 1 == piece.take ? kLast | (piece.last ? kLastPiece : 0) : 0) | (all ? kFull : 0);
   }
-  // Bytes of all lanes' copies; then the copies themselves.
+  // Bytes of all lanes' copies of K, or of V; then the copies themselves.
   __device__ __forceinline__ uint32_t bytes() const {
-    return __popc(__ballot_sync(0xffffffffu, load)) * 2u * static_cast<uint32_t>(sub * (D / 2 + D / kQ4Group));
+    return __popc(__ballot_sync(0xffffffffu, load)) * static_cast<uint32_t>(sub * (D / 2 + D / kQ4Group));
   }
-  __device__ __forceinline__ void copy(const simsd_q4_cache& c, Stage<D>& s, uint32_t bar) const {
+  __device__ __forceinline__ void copy_k(const simsd_q4_cache& c, Stage<D>& s, uint32_t bar) const {
+    copy(c.k_codes, c.k_scales, s.kc, s.ks, bar);
+  }
+  __device__ __forceinline__ void copy_v(const simsd_q4_cache& c, Stage<D>& s, uint32_t bar) const {
+    copy(c.v_codes, c.v_scales, s.vc, s.vs, bar);
+  }
+  __device__ __forceinline__ void copy(const void* codes, const void* scales, uint8_t* to_codes, uint8_t* to_scales,
+                                       uint32_t bar) const {
     if (!load) return;
-    const uint32_t code_bytes = static_cast<uint32_t>(sub * (D / 2)), scale_bytes = static_cast<uint32_t>(sub * (D / kQ4Group));
     const int at = (threadIdx.x & 31) * sub;
-    bulk_load(smem_u32(&s.kc[at * (D / 2)]), static_cast<const uint8_t*>(c.k_codes) + row * (D / 2), code_bytes, bar);
-    bulk_load(smem_u32(&s.ks[at * (D / kQ4Group)]), static_cast<const uint8_t*>(c.k_scales) + row * (D / kQ4Group), scale_bytes, bar);
-    bulk_load(smem_u32(&s.vc[at * (D / 2)]), static_cast<const uint8_t*>(c.v_codes) + row * (D / 2), code_bytes, bar);
-    bulk_load(smem_u32(&s.vs[at * (D / kQ4Group)]), static_cast<const uint8_t*>(c.v_scales) + row * (D / kQ4Group), scale_bytes, bar);
+    bulk_load(smem_u32(to_codes + at * (D / 2)), static_cast<const uint8_t*>(codes) + row * (D / 2),
+              static_cast<uint32_t>(sub * (D / 2)), bar);
+    bulk_load(smem_u32(to_scales + at * (D / kQ4Group)), static_cast<const uint8_t*>(scales) + row * (D / kQ4Group),
+              static_cast<uint32_t>(sub * (D / kQ4Group)), bar);
   }
 };
 
