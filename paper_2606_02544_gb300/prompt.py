@@ -42,6 +42,8 @@ class PromptCache:
         """window, sinks: rows back, and first rows, that a token sees (0: all);
         bits 4: the cache in 4 bits; pages: size of a pool whose pages the
         sequences take and let go of (None: a place for every row)."""
+        if bits not in (None, 4) or window < 0 or sinks < 0:
+            raise ValueError("bits: None or 4; window and sinks: 0 or more")
         self.L, self.Bt, self.Hq, self.Hkv, self.d, self.P = layers, Bt, Hq, Hkv, d, page_size
         self.plan, self.mask_block, self.dtype, self.device = plan, mask_block, dtype, device
         self.window, self.sinks, self.bits, self.pooled = window, sinks, bits, pages is not None
@@ -66,12 +68,21 @@ class PromptCache:
         self.live = torch.zeros(1, **i32)
         self.prefix_len = torch.zeros(Bt, **i32)
         self.err = torch.zeros(1, **i32)
-        self.workspace = None
+        self.workspace, self.captured = None, []
 
     def _scratch(self, nbytes):
         if nbytes and (self.workspace is None or self.workspace.numel() < nbytes):
             self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        return self.workspace if nbytes else None
+        if not nbytes:
+            return None
+        # a graph goes on writing to the workspace it was captured with: it is kept
+        if torch.cuda.is_current_stream_capturing() and not any(w is self.workspace for w in self.captured):
+            self.captured.append(self.workspace)
+        return self.workspace
+
+    def _pool(self):
+        if not self.pooled:
+            raise ValueError("a cache with a place for every row has no pool: make it with pages")
 
     def append_chunk(self, qkv, token_start):
         """One chunk of every layer: qkv [L][T][Hq + 2 Hkv][d] (rows of the
@@ -115,19 +126,24 @@ class PromptCache:
 
     def fork(self, src, dst):
         """Sequences dst become copies of sequences src (int32 tensors)."""
+        self._pool()
         ws = self._scratch(simsd.simsd_pages_workspace_bytes(0, src.shape[0]))
         simsd.simsd_pages_fork(self.page_set, src, dst, self.prefix_len, self.block_table, self.refs, self.P,
                                workspace=ws, err_word=self.err)
 
     def release(self, seq):
         """Sequences seq (an int32 tensor) end."""
+        self._pool()
         zero = torch.zeros_like(seq)
         simsd.simsd_pages_release(self.block_table, self.refs, zero, torch.full_like(seq, 2 ** 31 - 1), self.P,
                                   seq=seq, err_word=self.err)
-        self.prefix_len[seq.long()] = 0
+        # (a number out of range, which sets SIMSD_EW_SEQ, is none of the rows)
+        rows = torch.arange(self.Bt, dtype=torch.int32, device=self.device)
+        self.prefix_len.masked_fill_((rows[:, None] == seq).any(1), 0)
 
     def compact(self):
         """Moves the pages in use to the lowest ids; their number, on the GPU."""
+        self._pool()
         ws = self._scratch(simsd.simsd_pages_workspace_bytes(self.refs.shape[0]))
         simsd.simsd_pages_compact(self.page_set, self.block_table, self.refs, self.live, workspace=ws,
                                   err_word=self.err)
@@ -204,7 +220,6 @@ def main():
     print("tokens", tokens.tolist())
     fine = long_context(plan)
     return 0 if fine and word == 0 and bool(torch.isfinite(out.float()).all()) else 1
-
 
 
 def long_context(plan):

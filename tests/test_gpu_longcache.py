@@ -135,3 +135,45 @@ def test_verification_refuses_what_it_cannot_read():
 
 def test_example_runs():
     assert long_context(simsd.simsd_rope_plan_init("half", 128, 1.0e6))
+
+
+def test_cache_without_a_pool_refuses_the_pools_calls():
+    cache = PromptCache(1, 2, HQ, HKV, D, P, 64, plan())
+    one = torch.tensor([1], **I32)
+    for call in (lambda: cache.fork(one, one), lambda: cache.release(one), cache.compact):
+        with pytest.raises(ValueError):
+            call()
+    for kw in (dict(bits=8), dict(window=-1), dict(window=4, sinks=-1)):
+        with pytest.raises(ValueError):
+            PromptCache(1, 2, HQ, HKV, D, P, 64, plan(), **kw)
+
+
+def test_release_of_a_sequence_out_of_range():
+    cache = PromptCache(LAYERS, 2, HQ, HKV, D, P, 64, plan(), pages=8)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    cache.append_chunk(*chunk(g, BF16, 20, 30))
+    cache.release(torch.tensor([1, 5, -1], **I32))
+    assert simsd.simsd_check_error(cache.err) == simsd.EW_SEQ
+    assert cache.prefix_len.tolist() == [20, 0] and int((cache.refs > 0).sum()) == 2
+
+
+def test_graph_outlives_a_larger_workspace():
+    """A step captured with a small workspace gives the same after a longer
+    chunk has made a larger one."""
+    x, start = chunk(torch.Generator(device="cuda").manual_seed(4), BF16, 1, 1)
+    cache = PromptCache(LAYERS, 2, HQ, HKV, D, P, 2048, plan(), bits=4)
+    cache.append_chunk(*chunk(torch.Generator(device="cuda").manual_seed(5), BF16, 300, 400))
+    cache.workspace = None
+    lens = cache.prefix_len.clone()
+    want = cache.append_chunk(x, start)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        got = cache.append_chunk(x, start)
+    small = cache.workspace
+    cache.prefix_len.copy_(lens)
+    cache.append_chunk(*chunk(torch.Generator(device="cuda").manual_seed(6), BF16, 600, 500))
+    assert cache.workspace is not small and any(w is small for w in cache.captured)
+    cache.prefix_len.copy_(lens)
+    graph.replay()
+    assert torch.equal(got, want) and simsd.simsd_check_error(cache.err) == 0

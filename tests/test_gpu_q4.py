@@ -323,6 +323,25 @@ def test_long_chunks(dtype, window, sinks):
     check(a, window, sinks)
 
 
+@pytest.mark.parametrize("n,Hq,Hkv,d,window,sinks", [(1, 32, 8, 128, 0, 0), (16, 32, 8, 128, 0, 0), (32, 32, 8, 128, 0, 0),
+                                                     (16, 32, 8, 128, 1500, 40), (29, 32, 8, 128, 1500, 40),
+                                                     (9, 28, 4, 64, 0, 0), (17, 28, 4, 64, 900, 200)])
+def test_long_runs(n, Hq, Hkv, d, window, sinks):
+    """Tens of tiles and several units a CTA, with queries of their own for
+    sequences that share their pages."""
+    seqs = 40
+    a = attention_case(BF16, [n], [2600], Hq, Hkv, d, 64, n + d, window, sinks)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(n)
+    a["q"] = torch.randn(seqs * n, Hq + 2, d, generator=g, device="cuda").to(BF16)[:, 1:-1]
+    a["token_start"] = torch.arange(seqs + 1, **i32) * n
+    a["prefix_len"] = torch.full((seqs,), 2600, **i32)
+    a["block_table"] = a["block_table"].repeat(seqs, 1)
+    check(a, window, sinks)
+    first, again = run(a, window=window, sinks=sinks), run(a, window=window, sinks=sinks)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
 @pytest.mark.parametrize("units,scale", [((0.25, 8.0), 0.0), ((1.7, 0.3), 0.02), ((1.0, 1.0), 0.5)])
 def test_units_and_scale(units, scale):
     check(attention_case(BF16, [1, 3], [300, 140], 8, 2, 128, 64, 9, units=units), softmax_scale=scale)
