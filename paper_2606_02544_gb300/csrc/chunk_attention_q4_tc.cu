@@ -27,12 +27,12 @@
 // of this one.
 //
 // Bound and measured.  32 blocks of 16 tokens over 4096 rows (32 heads on 8,
-// D = 128; 155 MB, 23 us of copies) take 95 us, of 32 tokens 103.  The matrix
-// instructions of a tile take half of its 2300 cycles; the rest are the chains
+// D = 128; 155 MB, 23 us of copies) take 88 us, of 32 tokens 101.  The matrix
+// instructions of a tile take half of its 2100 cycles; the rest are the chains
 // beside them, each of which is about as long: one warp of an SM partition
-// turns 32 rows of K and one 32 rows of V (1500 cycles, 900 of hand-offs), one
-// does the softmax, one looks up pages and copies.  Without the turning 80 us,
-// without the softmax 85, without both 71.  Not faster: twelve turning warps
+// turns 32 rows of K and one 32 rows of V (29 instructions for 16 components;
+// with generic addresses 47, and 95 us), one does the softmax, one looks up
+// pages and copies.  Without the turning 80 us, without both 71.  Not faster: twelve turning warps
 // and the softmax of a tile over eight warps (96: as many instructions more);
 // more rows in flight for each turning warp (110 to 118).  Sets of softmax warps
 // that took whole tiles in turns, each with one S: 106.
@@ -125,6 +125,20 @@ static_assert(2 * SmemQ4Tc<64, false>::kSlots * SmemQ4Tc<64, false>::kTileBytes 
 constexpr uint32_t idesc_f16_f32(int M, int N, int b_mn_major) {
   return (1u << 4) | (static_cast<uint32_t>(b_mn_major) << 16) | (static_cast<uint32_t>(N >> 3) << 17) |
          (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
 // Partial results: O (without the values' unit) as [ctas * 2 entries][D / 4]
@@ -377,6 +391,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int w = warp & 3, kv = (warp - kWarpConvert) >> 2, grp = lane & (kGroups - 1);
     const int half = grp >> 2, ch = (grp & 3) * 2;
     const int r0 = 32 * w + lane / kGroups;
+    // Places of the lane's row r0 in a tile: of its first and its second chunk
+    // (rows 4 and 8 further have them in the same column, of 8, or 4 columns on).
+    const uint32_t to = static_cast<uint32_t>(half * kHalfBytes + r0 * 128), x = r0 & 7;
+    const uint32_t to_a = to + (((ch + half) ^ x) << 4), to_b = to + (((ch + 1 - half) ^ x) << 4);
     uint32_t c = 0;
     for (uint32_t it = 0; ok; ++it) {
       ok = wait(sm.bar_info[it % kInfos], (it / kInfos) & 1);
@@ -392,36 +410,41 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (c >= kSlots) ok = ok && wait(kv ? sm.bar_vfree[slot] : sm.bar_kfree[slot], ((c / kSlots) - 1) & 1);
       if (!ok) break;
       {
-        const uint8_t *codes = kv ? s.vc : s.kc, *scales = kv ? s.vs : s.ks;
-        uint8_t* tile = (kv ? sm.v[slot] : sm.k[slot]) + half * kHalfBytes;
+        uint32_t codes = smem_u32(kv ? s.vc : s.kc) + r0 * (D / 2) + 8 * grp;
+        uint32_t scales = smem_u32(kv ? s.vs : s.ks) + r0 * kGroups + grp;
+        uint32_t tile = smem_u32(kv ? sm.v[slot] : sm.k[slot]);
         const bool zero = kv && !(flags & kFull);
+        constexpr int kSteps = 16 / kRowsStep;
 #pragma unroll 1
-        for (int rb = r0; rb < r0 + 32; rb += 16) {
-          uint2 cw[16 / kRowsStep];
-          uint32_t sc[16 / kRowsStep];
+        for (int rb = 0; rb < 32; rb += 16) {
+          uint2 cw[kSteps];
+          uint32_t sc[kSteps];
 #pragma unroll
-          for (int j = 0; j < 16 / kRowsStep; ++j) {
-            const int r = rb + kRowsStep * j;
-            cw[j] = *reinterpret_cast<const uint2*>(codes + r * (D / 2) + 8 * grp);
-            sc[j] = scales[r * kGroups + grp];
+          for (int j = 0; j < kSteps; ++j) {
+            cw[j] = lds64(codes + kRowsStep * j * (D / 2));
+            sc[j] = lds8(scales + kRowsStep * j * kGroups);
           }
+          if (zero) {
+            // values of rows that no token of the unit sees may be anything: 0
 #pragma unroll
-          for (int j = 0; j < 16 / kRowsStep; ++j) {
-            const int r = rb + kRowsStep * j;
-            if (zero) {
-              // values of rows that no token of the unit sees may be anything: 0
-              const int key = key0 + r;
+            for (int j = 0; j < kSteps; ++j) {
+              const int key = key0 + r0 + rb + kRowsStep * j;
               if (key < lo || key >= hi || (SINKS && key >= se && key < w0)) sc[j] = 0u;
             }
-            const uint32_t f = q4_scale_pair(sc[j] | sc[j] << 8);
-            const uint32_t ca = half ? cw[j].y : cw[j].x, cb = half ? cw[j].x : cw[j].y;
-            uint8_t* row = tile + r * 128;
-            const int x = r & 7;
-            *reinterpret_cast<uint4*>(row + (((ch + half) ^ x) << 4)) =
-                make_uint4(mul_f16x2(q4_pair<0>(ca), f), mul_f16x2(q4_pair<1>(ca), f), mul_f16x2(q4_pair<2>(ca), f), mul_f16x2(q4_pair<3>(ca), f));
-            *reinterpret_cast<uint4*>(row + (((ch + 1 - half) ^ x) << 4)) =
-                make_uint4(mul_f16x2(q4_pair<0>(cb), f), mul_f16x2(q4_pair<1>(cb), f), mul_f16x2(q4_pair<2>(cb), f), mul_f16x2(q4_pair<3>(cb), f));
           }
+#pragma unroll
+          for (int j = 0; j < kSteps; ++j) {
+            const uint32_t f = q4_scale_pair(sc[j] * 0x101u);
+            const uint32_t ca = half ? cw[j].y : cw[j].x, cb = half ? cw[j].x : cw[j].y;
+            const uint32_t turn = kRowsStep == 4 && (j & 1) ? 64u : 0u, at = tile + 128 * kRowsStep * j;
+            sts128(at + (to_a ^ turn), mul_f16x2(q4_pair<0>(ca), f), mul_f16x2(q4_pair<1>(ca), f), mul_f16x2(q4_pair<2>(ca), f),
+                   mul_f16x2(q4_pair<3>(ca), f));
+            sts128(at + (to_b ^ turn), mul_f16x2(q4_pair<0>(cb), f), mul_f16x2(q4_pair<1>(cb), f), mul_f16x2(q4_pair<2>(cb), f),
+                   mul_f16x2(q4_pair<3>(cb), f));
+          }
+          codes += 16 * (D / 2);
+          scales += 16 * kGroups;
+          tile += 16 * 128;
         }
         fence_proxy_async_smem();
         arrive(kv ? sm.bar_v[slot] : sm.bar_k[slot]);
