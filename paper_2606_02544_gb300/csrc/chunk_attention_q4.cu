@@ -171,7 +171,8 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
   using Smem = SmemQ4<D, NB>;
   constexpr int RB = C::kRows, kStages = C::kStages, kWarps = C::kWarps;
   extern __shared__ uint8_t smem_raw[];
-  Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~static_cast<uintptr_t>(127));
+  // (an offset from the array: through a number the compiler no longer knows that it is shared memory)
+  Smem& sm = *reinterpret_cast<Smem*>(smem_raw + (0u - smem_u32(smem_raw) & 127u));
   static_assert(sizeof(sm.ring) >= kMaxSeqs * 4, "the ring holds the tile counts of all sequences");
   volatile int* abort_flag = &sm.abort_flag;
   const unsigned full = 0xffffffffu;

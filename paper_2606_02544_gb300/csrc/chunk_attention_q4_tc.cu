@@ -164,7 +164,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   using Smem = SmemQ4Tc<D, LEAN>;
   constexpr int kHalves = Smem::kHalves, kSlots = Smem::kSlots, kStages = Smem::kStages;
   extern __shared__ uint8_t smem_raw[];
-  Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  // (an offset from the array: through a number the compiler no longer knows that it is shared memory)
+  Smem& sm = *reinterpret_cast<Smem*>(smem_raw + (0u - smem_u32(smem_raw) & 1023u));
   volatile int* abort_flag = &sm.abort_flag;
   const unsigned full = 0xffffffffu;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
