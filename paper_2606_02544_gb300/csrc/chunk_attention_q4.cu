@@ -22,14 +22,14 @@
 // Work.  The walk of chunk_walk.cuh over units of (KV head, sequence, up to
 // 16 query rows).  One warp walks the run and brings the tiles' codes and
 // scales (128 keys, 18 KB) by bulk copies, each a page's contiguous rows of a
-// head; four or eight warps share a tile's keys, each with a softmax of its
+// head; four warps share a tile's keys, each with a softmax of its
 // own, merged at the end of a unit through shared memory.  A unit cut by a
 // run's end leaves partial (O, m, l), which a second launch merges.
 //
-// Bound: the issue of instructions, some 320 for 16 keys (64 conversions and
-// 64 products with a scale among them): 64 single tokens over 2048 to 8192
-// rows, 32 heads on 8 of 128, read 377 MB in 85 us (4.4 TB/s; without the
-// copies it takes 82, without the products with V 67).
+// Bound: the issue of instructions, some 280 for 16 keys (64 conversions and
+// 64 products with a scale among them), and what few warps can hide of their
+// latencies: 64 single tokens over 2048 to 8192 rows, 32 heads on 8 of 128, read
+// 377 MB in 77 us (4.9 TB/s).
 //
 // Every mbarrier wait is bounded; after one expires the CTA raises
 // SIMSD_EW_TIMEOUT, every warp leaves its loop and the copies in flight are
@@ -62,20 +62,19 @@ struct Q4Params {
   float scale_log2;   // scores to log2 units, the keys' unit included
 };
 
-// NB blocks of 8 query rows.  One takes few registers: three CTAs an SM of
-// four warps, whose 32 keys a tile pay for what a tile costs beside its
-// products (64 single tokens over 2048 to 8192 rows: 85 us; four CTAs, with 96
-// registers a thread, 92; eight warps of 16 keys, two CTAs, 113).  Two: one CTA
-// of eight warps.
+// NB blocks of 8 query rows.  CTAs of four warps, whose 32 keys a tile pay for
+// what a tile costs beside its products; as many an SM as registers allow.
+// One block, 64 single tokens over 2048 to 8192 rows: 77 us (four CTAs, with 96
+// registers a thread, 81; eight warps of 16 keys, two CTAs, then 113 for 87).  Two,
+// 32 blocks of 4 tokens over these: 67 us (eight warps of 16 keys, one CTA, 84).
 template <int D, int NB>
 struct Cfg {
   static constexpr int kRows = 8 * NB;  // query rows of a unit
-  static constexpr int kWarps = NB == 1 ? 4 : 8;
+  static constexpr int kWarps = 4;
   static constexpr int kThreads = 32 * (kWarps + 1);
   static constexpr int kWarpKeys = kTile / kWarps;
-  static constexpr int kStep = NB == 1 ? 32 : 16;  // keys between two looks at the maxima
-  static constexpr int kCtas = NB == 1 ? 3 : 1;    // an SM
-  static constexpr int kStages = (NB == 1 ? 3 : 7) * (128 / D);
+  static constexpr int kCtas = NB == 1 ? 3 : 2;  // an SM
+  static constexpr int kStages = (NB == 1 ? 3 : 4) * (128 / D);
 };
 
 template <int D, int NB>
@@ -273,7 +272,7 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
   const int perm = g ^ ((g >> 1) & 1);    // place of key g among 8: neighbours in pairs, pairs turned in turns
   const int va = (2 * t) ^ (t & 1), vb = (2 * t + 1) ^ (t & 1);
   constexpr int kSteps = D / 16;          // products of 16 components; blocks of 16 channels
-  constexpr int G = C::kStep / 16;
+  constexpr int G = C::kWarpKeys / 16;
   uint32_t q[NB][kSteps][2];
   // m: the reference that the probabilities are formed against, in log2 units
   float o[NB][kSteps][4], m[NB][2], l[NB][2], rs[NB][2];
@@ -352,136 +351,133 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
         fence_proxy_async_smem();  // (the slot is filled by bulk copies next)
         __syncwarp();
       }
+      const int kb = warp * C::kWarpKeys;
+      // S^T of keys perm(g) and 8 + perm(g) of each 16, rows 2t and 2t + 1
+      float sc[G][NB][4];
 #pragma unroll
-      for (int step = 0; step < C::kWarpKeys / C::kStep; ++step) {
-        const int kb = warp * C::kWarpKeys + C::kStep * step;
-        // S^T of keys perm(g) and 8 + perm(g) of each 16, rows 2t and 2t + 1
-        float sc[G][NB][4];
+      for (int u = 0; u < G; ++u) {
+        const KCodes<D> ka = load_k(s, kb + 16 * u + perm, t), kc = load_k(s, kb + 16 * u + 8 + perm, t);
+        const uint32_t x = q4_scale_pair(ka.s), y = q4_scale_pair(kc.s);
+        uint32_t sa[2], sb[2];
+        sa[0] = __byte_perm(x, 0, 0x1010);
+        sb[0] = __byte_perm(y, 0, 0x1010);
+        sa[1] = __byte_perm(x, 0, 0x3232);  // (128 components: a thread's lie in two groups)
+        sb[1] = __byte_perm(y, 0, 0x3232);
 #pragma unroll
-        for (int u = 0; u < G; ++u) {
-          const KCodes<D> ka = load_k(s, kb + 16 * u + perm, t), kc = load_k(s, kb + 16 * u + 8 + perm, t);
-          const uint32_t x = q4_scale_pair(ka.s), y = q4_scale_pair(kc.s);
-          uint32_t sa[2], sb[2];
-          sa[0] = __byte_perm(x, 0, 0x1010);
-          sb[0] = __byte_perm(y, 0, 0x1010);
-          sa[1] = __byte_perm(x, 0, 0x3232);  // (128 components: a thread's lie in two groups)
-          sb[1] = __byte_perm(y, 0, 0x3232);
-#pragma unroll
-          for (int k = 0; k < kSteps; ++k) {
-            const uint32_t wa = ka.w[k / 2], wb = kc.w[k / 2], fa = sa[k / 4], fb = sb[k / 4];
-            const uint32_t a0 = mul_f16x2(k & 1 ? q4_pair<2>(wa) : q4_pair<0>(wa), fa);
-            const uint32_t a1 = mul_f16x2(k & 1 ? q4_pair<2>(wb) : q4_pair<0>(wb), fb);
-            const uint32_t a2 = mul_f16x2(k & 1 ? q4_pair<3>(wa) : q4_pair<1>(wa), fa);
-            const uint32_t a3 = mul_f16x2(k & 1 ? q4_pair<3>(wb) : q4_pair<1>(wb), fb);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-              if (k == 0)
-                mma16816_first(sc[u][nb], a0, a1, a2, a3, q[nb][k][0], q[nb][k][1]);
-              else
-                mma16816(sc[u][nb], a0, a1, a2, a3, q[nb][k][0], q[nb][k][1]);
-            }
-          }
-        }
-        if (masked) {
-          ChunkSeq cs;
-          cs.n = info.n;
-          cs.C = info.C;
-          cs.ks = info.ks;
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int tl = info.i0 + min((nb * 8 + 2 * t + e) / p.g, ntok - 1);
-              const int lo = key_lo(p.a, cs, tl), hi = key_hi(p.a, cs, tl), se = SINKS ? sink_end(p.a, cs, hi) : 0;
-#pragma unroll
-              for (int u = 0; u < G; ++u)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  const int key = key0 + kb + 16 * u + 8 * h + perm;
-                  if (!((key >= lo && key < hi) || (SINKS && key >= cs.ks && key < se))) sc[u][nb][2 * h + e] = -INFINITY;
-                }
-            }
-        }
-        // exponents; those of rows whose reference has to move again
-        float pr[G][NB][4];
-        bool above = false;
-#pragma unroll
-        for (int u = 0; u < G; ++u)
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              pr[u][nb][e] = fmaf(sc[u][nb][e], rs[nb][e & 1], -m[nb][e & 1]);
-              above |= pr[u][nb][e] > kRescaleThreshold;
-            }
-        if (__any_sync(full, above)) {
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float mx = m[nb][e];
-#pragma unroll
-              for (int u = 0; u < G; ++u) mx = fmaxf(mx, fmaxf(sc[u][nb][e], sc[u][nb][e + 2]) * rs[nb][e]);
-              mx = fmaxf(mx, __shfl_xor_sync(full, mx, 4));
-              mx = fmaxf(mx, __shfl_xor_sync(full, mx, 8));
-              mx = fmaxf(mx, __shfl_xor_sync(full, mx, 16));
-              const float f = fast_exp2(m[nb][e] - mx);
-              m[nb][e] = mx;
-              l[nb][e] *= f;
-#pragma unroll
-              for (int k = 0; k < kSteps; ++k) {
-                o[nb][k][e] *= f;
-                o[nb][k][e + 2] *= f;
-              }
-#pragma unroll
-              for (int u = 0; u < G; ++u) {
-                pr[u][nb][e] = fmaf(sc[u][nb][e], rs[nb][e], -mx);
-                pr[u][nb][e + 2] = fmaf(sc[u][nb][e + 2], rs[nb][e], -mx);
-              }
-            }
-        }
-        uint32_t pb[G][NB][2];
-#pragma unroll
-        for (int u = 0; u < G; ++u)
+        for (int k = 0; k < kSteps; ++k) {
+          const uint32_t wa = ka.w[k / 2], wb = kc.w[k / 2], fa = sa[k / 4], fb = sb[k / 4];
+          const uint32_t a0 = mul_f16x2(k & 1 ? q4_pair<2>(wa) : q4_pair<0>(wa), fa);
+          const uint32_t a1 = mul_f16x2(k & 1 ? q4_pair<2>(wb) : q4_pair<0>(wb), fb);
+          const uint32_t a2 = mul_f16x2(k & 1 ? q4_pair<3>(wa) : q4_pair<1>(wa), fa);
+          const uint32_t a3 = mul_f16x2(k & 1 ? q4_pair<3>(wb) : q4_pair<1>(wb), fb);
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) pr[u][nb][e] = fast_exp2(pr[u][nb][e]);
-            l[nb][0] += pr[u][nb][0] + pr[u][nb][2];
-            l[nb][1] += pr[u][nb][1] + pr[u][nb][3];
-            pb[u][nb][0] = transpose8(pack_f16x2(pr[u][nb][0], pr[u][nb][1]));
-            pb[u][nb][1] = transpose8(pack_f16x2(pr[u][nb][2], pr[u][nb][3]));
+            if (k == 0)
+              mma16816_first(sc[u][nb], a0, a1, a2, a3, q[nb][k][0], q[nb][k][1]);
+            else
+              mma16816(sc[u][nb], a0, a1, a2, a3, q[nb][k][0], q[nb][k][1]);
           }
+        }
+      }
+      if (masked) {
+        ChunkSeq cs;
+        cs.n = info.n;
+        cs.C = info.C;
+        cs.ks = info.ks;
 #pragma unroll
-        for (int u = 0; u < G; ++u) {
-          // V^T of keys va, vb and 8 + va, 8 + vb, channels from g D / 8 on (all of one scale)
-          const int kv = kb + 16 * u;
-          const VCodes<D> v0 = load_v(s, kv + va, g), v1 = load_v(s, kv + vb, g);
-          const VCodes<D> v2 = load_v(s, kv + 8 + va, g), v3 = load_v(s, kv + 8 + vb, g);
-          constexpr int kScales = D / kQ4Group;
-          const int vg = D == 128 ? g : g >> 1;
-          const uint32_t s01 = s.vs[(kv + va) * kScales + vg] | s.vs[(kv + vb) * kScales + vg] << 8;
-          const uint32_t s23 = s.vs[(kv + 8 + va) * kScales + vg] | s.vs[(kv + 8 + vb) * kScales + vg] << 8;
-          const uint32_t f01 = q4_scale_pair(s01), f23 = q4_scale_pair(s23);
-          constexpr uint32_t kLow = 0x0f0f0f0fu;
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int i = 0; i < D / 64; ++i) {
-            // bytes of two keys' codes of one channel
-            const uint32_t e01 = (v0.w[i] & kLow) | (v1.w[i] << 4 & ~kLow), d01 = (v0.w[i] >> 4 & kLow) | (v1.w[i] & ~kLow);
-            const uint32_t e23 = (v2.w[i] & kLow) | (v3.w[i] << 4 & ~kLow), d23 = (v2.w[i] >> 4 & kLow) | (v3.w[i] & ~kLow);
-            auto block = [&](int k, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
-              a0 = mul_f16x2(a0, f01);
-              a1 = mul_f16x2(a1, f01);
-              a2 = mul_f16x2(a2, f23);
-              a3 = mul_f16x2(a3, f23);
+          for (int e = 0; e < 2; ++e) {
+            const int tl = info.i0 + min((nb * 8 + 2 * t + e) / p.g, ntok - 1);
+            const int lo = key_lo(p.a, cs, tl), hi = key_hi(p.a, cs, tl), se = SINKS ? sink_end(p.a, cs, hi) : 0;
 #pragma unroll
-              for (int nb = 0; nb < NB; ++nb) mma16816(o[nb][k], a0, a1, a2, a3, pb[u][nb][0], pb[u][nb][1]);
-            };
-            block(4 * i, q4_pair<0>(e01), q4_pair<0>(d01), q4_pair<0>(e23), q4_pair<0>(d23));
-            block(4 * i + 1, q4_pair<1>(e01), q4_pair<1>(d01), q4_pair<1>(e23), q4_pair<1>(d23));
-            block(4 * i + 2, q4_pair<2>(e01), q4_pair<2>(d01), q4_pair<2>(e23), q4_pair<2>(d23));
-            block(4 * i + 3, q4_pair<3>(e01), q4_pair<3>(d01), q4_pair<3>(e23), q4_pair<3>(d23));
+            for (int u = 0; u < G; ++u)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const int key = key0 + kb + 16 * u + 8 * h + perm;
+                if (!((key >= lo && key < hi) || (SINKS && key >= cs.ks && key < se))) sc[u][nb][2 * h + e] = -INFINITY;
+              }
           }
+      }
+      // exponents; those of rows whose reference has to move again
+      float pr[G][NB][4];
+      bool above = false;
+#pragma unroll
+      for (int u = 0; u < G; ++u)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            pr[u][nb][e] = fmaf(sc[u][nb][e], rs[nb][e & 1], -m[nb][e & 1]);
+            above |= pr[u][nb][e] > kRescaleThreshold;
+          }
+      if (__any_sync(full, above)) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float mx = m[nb][e];
+#pragma unroll
+            for (int u = 0; u < G; ++u) mx = fmaxf(mx, fmaxf(sc[u][nb][e], sc[u][nb][e + 2]) * rs[nb][e]);
+            mx = fmaxf(mx, __shfl_xor_sync(full, mx, 4));
+            mx = fmaxf(mx, __shfl_xor_sync(full, mx, 8));
+            mx = fmaxf(mx, __shfl_xor_sync(full, mx, 16));
+            const float f = fast_exp2(m[nb][e] - mx);
+            m[nb][e] = mx;
+            l[nb][e] *= f;
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+              o[nb][k][e] *= f;
+              o[nb][k][e + 2] *= f;
+            }
+#pragma unroll
+            for (int u = 0; u < G; ++u) {
+              pr[u][nb][e] = fmaf(sc[u][nb][e], rs[nb][e], -mx);
+              pr[u][nb][e + 2] = fmaf(sc[u][nb][e + 2], rs[nb][e], -mx);
+            }
+          }
+      }
+      uint32_t pb[G][NB][2];
+#pragma unroll
+      for (int u = 0; u < G; ++u)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pr[u][nb][e] = fast_exp2(pr[u][nb][e]);
+          l[nb][0] += pr[u][nb][0] + pr[u][nb][2];
+          l[nb][1] += pr[u][nb][1] + pr[u][nb][3];
+          pb[u][nb][0] = transpose8(pack_f16x2(pr[u][nb][0], pr[u][nb][1]));
+          pb[u][nb][1] = transpose8(pack_f16x2(pr[u][nb][2], pr[u][nb][3]));
+        }
+#pragma unroll
+      for (int u = 0; u < G; ++u) {
+        // V^T of keys va, vb and 8 + va, 8 + vb, channels from g D / 8 on (all of one scale)
+        const int kv = kb + 16 * u;
+        const VCodes<D> v0 = load_v(s, kv + va, g), v1 = load_v(s, kv + vb, g);
+        const VCodes<D> v2 = load_v(s, kv + 8 + va, g), v3 = load_v(s, kv + 8 + vb, g);
+        constexpr int kScales = D / kQ4Group;
+        const int vg = D == 128 ? g : g >> 1;
+        const uint32_t s01 = s.vs[(kv + va) * kScales + vg] | s.vs[(kv + vb) * kScales + vg] << 8;
+        const uint32_t s23 = s.vs[(kv + 8 + va) * kScales + vg] | s.vs[(kv + 8 + vb) * kScales + vg] << 8;
+        const uint32_t f01 = q4_scale_pair(s01), f23 = q4_scale_pair(s23);
+        constexpr uint32_t kLow = 0x0f0f0f0fu;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          // bytes of two keys' codes of one channel
+          const uint32_t e01 = (v0.w[i] & kLow) | (v1.w[i] << 4 & ~kLow), d01 = (v0.w[i] >> 4 & kLow) | (v1.w[i] & ~kLow);
+          const uint32_t e23 = (v2.w[i] & kLow) | (v3.w[i] << 4 & ~kLow), d23 = (v2.w[i] >> 4 & kLow) | (v3.w[i] & ~kLow);
+          auto block = [&](int k, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+            a0 = mul_f16x2(a0, f01);
+            a1 = mul_f16x2(a1, f01);
+            a2 = mul_f16x2(a2, f23);
+            a3 = mul_f16x2(a3, f23);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma16816(o[nb][k], a0, a1, a2, a3, pb[u][nb][0], pb[u][nb][1]);
+          };
+          block(4 * i, q4_pair<0>(e01), q4_pair<0>(d01), q4_pair<0>(e23), q4_pair<0>(d23));
+          block(4 * i + 1, q4_pair<1>(e01), q4_pair<1>(d01), q4_pair<1>(e23), q4_pair<1>(d23));
+          block(4 * i + 2, q4_pair<2>(e01), q4_pair<2>(d01), q4_pair<2>(e23), q4_pair<2>(d23));
+          block(4 * i + 3, q4_pair<3>(e01), q4_pair<3>(d01), q4_pair<3>(e23), q4_pair<3>(d23));
         }
       }
     }

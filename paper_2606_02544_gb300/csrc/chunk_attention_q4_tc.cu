@@ -27,12 +27,13 @@
 // of this one.
 //
 // Bound and measured.  32 blocks of 16 tokens over 4096 rows (32 heads on 8,
-// D = 128; 155 MB, 23 us of copies) take 88 us, of 32 tokens 101.  The matrix
+// D = 128; 155 MB, 23 us of copies) take 83 us, of 32 tokens 92.  The matrix
 // instructions of a tile take half of its 2100 cycles; the rest are the chains
 // beside them, each of which is about as long: one warp of an SM partition
-// turns 32 rows of K and one 32 rows of V (29 instructions for 16 components;
-// with generic addresses 47, and 95 us), one does the softmax, one looks up
-// pages and copies.  Without the turning 80 us, without both 71.  Not faster: twelve turning warps
+// turns 32 rows of K and one 32 rows of V (29 instructions for 16 components),
+// one does the softmax, one looks up pages and copies.  (With 47 instructions,
+// by generic addresses, 95 us; then without the turning 80, without turning and
+// softmax 71.)  Not faster: twelve turning warps
 // and the softmax of a tile over eight warps (96: as many instructions more);
 // more rows in flight for each turning warp (110 to 118).  Sets of softmax warps
 // that took whole tiles in turns, each with one S: 106.
