@@ -569,8 +569,8 @@ SIMSD_API int simsd_q4_expand(int dtype, const simsd_q4_cache* cache, int num_pa
  * simsd_chunk_attention_q4 -- simsd_chunk_attention_sinks over a cache in 4
  * bits (sinks = 0: simsd_chunk_attention).  q and out are dtype.  The same
  * masks, error rules and limits.
- * SIMSD_BF16 with up to 256 query rows a sequence and KV head on average (T Hq
- * <= 256 Bt Hkv) reads the codes: keys and values are exact in the products'
+ * SIMSD_BF16 with up to 768 query rows a sequence and KV head on average (T Hq
+ * <= 768 Bt Hkv; heads of 64: 512) reads the codes: keys and values are exact in the products'
  * fp16, q is scaled by a power of two to its row's largest component,
  * probabilities are rounded to fp16.  More rows, and SIMSD_F32, go through an
  * image of the rows that are seen in dtype, with the cache's page ids, in the

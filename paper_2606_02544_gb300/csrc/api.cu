@@ -861,7 +861,7 @@ size_t simsd_chunk_q4_workspace_bytes(int dtype, int T, int Bt, int Hq, int Hkv,
     return 0;
   DeviceInfo info;
   if (device_info(&info) != SIMSD_OK) return 0;
-  const simsd::Q4Way way = simsd::chunk_q4_way(dtype, T, Bt, Hq, Hkv);
+  const simsd::Q4Way way = simsd::chunk_q4_way(dtype, T, Bt, Hq, Hkv, d);
   if (way == simsd::Q4Way::kCodes) return simsd::chunk_q4_workspace_bytes(T, Bt, Hq, Hkv, d, info.num_sms);
   if (way == simsd::Q4Way::kTiles) return simsd::chunk_q4_tc_workspace_bytes(d, info.num_sms);
   return 2 * q4_image_bytes(dtype, num_pages, Hkv, page_size, d) +
@@ -909,7 +909,7 @@ int simsd_chunk_attention_q4(int dtype, const void* q, int64_t q_stride, const i
   a.window = window;
   a.sinks = window > 0 ? sinks : 0;
   a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt(static_cast<float>(d));
-  const simsd::Q4Way way = simsd::chunk_q4_way(dtype, T, Bt, Hq, Hkv);
+  const simsd::Q4Way way = simsd::chunk_q4_way(dtype, T, Bt, Hq, Hkv, d);
   if (way != simsd::Q4Way::kImage) {
     // units of at least one token, key tiles of 128 rows, counted in 32 bits
     const long long max_keys = static_cast<long long>(max_pages) * page_size;

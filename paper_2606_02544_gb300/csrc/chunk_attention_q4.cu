@@ -674,19 +674,20 @@ cudaError_t launch_d(const Q4Params& p, int num_sms, cudaStream_t stream) {
 }  // namespace
 
 // By the query rows that a sequence has for a KV head on average.  Up to 16:
-// from the registers; up to 256: by tiles; more: through the image, which
-// costs one pass over the rows but then serves 256 of them a tile.  32
-// sequences of 4096 rows, heads of 128, 32 on 8: 20 rows 112 us from the
-// registers (in two blocks of 16) and 106 by tiles; 16 sequences: 256 rows 121
-// us by tiles and 153 through the image, 512 rows 215 and 206.
+// from the registers; up to 768, or 512 of heads of 64: by tiles; more: through
+// the image, which costs one pass over the rows but then serves 256 of them a
+// tile.  Heads of 128, 32 on 8: 32 sequences of 4096 rows, 20 query rows 95 us
+// from the registers (in two blocks of 16) and 84 by tiles; 16 sequences, 256
+// query rows 92 us by tiles and 153 through the image, 512 161 and 204, 768 233
+// and 260.  Heads of 64, 28 on 4: 448 78 and 81, 672 109 and 100.
 constexpr int kCodesRows = 16;
-constexpr int kTilesRows = 256;
-Q4Way chunk_q4_way(int dtype, int T, int Bt, int Hq, int Hkv) {
+constexpr int tiles_rows(int d) { return d == 128 ? 768 : 512; }
+Q4Way chunk_q4_way(int dtype, int T, int Bt, int Hq, int Hkv, int d) {
   if (dtype != SIMSD_BF16 || Bt > kChunkMaxSeqs) return Q4Way::kImage;
   const int g = Hq / Hkv;
   const long long rows = static_cast<long long>(T) * g;
   if (g <= kCodesRows && rows <= static_cast<long long>(kCodesRows) * Bt && Bt <= kMaxSeqs) return Q4Way::kCodes;
-  return g <= 128 && rows <= static_cast<long long>(kTilesRows) * Bt ? Q4Way::kTiles : Q4Way::kImage;
+  return g <= 128 && rows <= static_cast<long long>(tiles_rows(d)) * Bt ? Q4Way::kTiles : Q4Way::kImage;
 }
 
 size_t chunk_q4_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, int num_sms) {

@@ -188,7 +188,7 @@ cudaError_t launch_q4_expand_seen(int elem_bytes, const ChunkArgs& a, const sims
 // rows (chunk_attention_q4.cu), by codes turned into tiles for up to 128 rows
 // (chunk_attention_q4_tc.cu), or through an image in dtype.
 enum class Q4Way { kCodes, kTiles, kImage };
-Q4Way chunk_q4_way(int dtype, int T, int Bt, int Hq, int Hkv);
+Q4Way chunk_q4_way(int dtype, int T, int Bt, int Hq, int Hkv, int d);
 size_t chunk_q4_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, int num_sms);
 cudaError_t launch_chunk_attention_q4(const ChunkArgs& a, const simsd_q4_cache& c, int num_sms, cudaStream_t stream);
 size_t chunk_q4_tc_workspace_bytes(int d, int num_sms);

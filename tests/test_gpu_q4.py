@@ -268,7 +268,7 @@ def check(a, window=0, sinks=0, mask_block=1, softmax_scale=0.0):
     bf16 = a["q"].dtype == BF16
     kc, ks, vc, vs = (t.cpu().numpy() for t in c.tensors)
     kd, vd = ref.decode(kc, ks, c.k_unit), ref.decode(vc, vs, c.v_unit)
-    few = bf16 and T * Hq <= 256 * len(a["prefix_len"]) * c.Hkv  # by codes
+    few = bf16 and T * Hq <= (768 if d == 128 else 512) * len(a["prefix_len"]) * c.Hkv  # by codes
     if not few:  # a unit that is no power of two rounds the image
         kd, vd = (torch.from_numpy(x).float().to(a["q"].dtype).double().numpy() for x in (kd, vd))
 
@@ -321,6 +321,16 @@ def test_long_chunks(dtype, window, sinks):
     check(a, window, sinks, 4)
     a = attention_case(dtype, chunk, prefix, 6, 1, 64, 64, 4, window, sinks, units=(1.3, 0.7))
     check(a, window, sinks)
+    a = attention_case(dtype, [400], [70], 8, 2, 128, 16, 7, window, sinks, 4, units=(0.7, 2.0))
+    check(a, window, sinks, 4)
+
+
+@pytest.mark.parametrize("d,Hq,Hkv", [(128, 8, 2), (64, 8, 2), (128, 7, 1), (64, 9, 3)])
+def test_either_side_of_the_rule_of_ways(d, Hq, Hkv):
+    """The most rows that are attended to by codes, and one token more."""
+    most = (768 if d == 128 else 512) * Hkv // Hq
+    for n in (most, most + 1):
+        check(attention_case(BF16, [n], [100], Hq, Hkv, d, 16, n + Hq))
 
 
 @pytest.mark.parametrize("n,Hq,Hkv,d,window,sinks", [(1, 32, 8, 128, 0, 0), (16, 32, 8, 128, 0, 0), (32, 32, 8, 128, 0, 0),
