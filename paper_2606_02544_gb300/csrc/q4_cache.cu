@@ -21,7 +21,7 @@
 // Bound by memory: a token reads (Hq + 2 Hkv) d elements and writes Hq d and
 // 2 Hkv (d / 2 + d / 16) bytes.  16404 tokens of 32 heads on 8 of 128 in bf16
 // (355 MB) take 77 us, 4.6 TB/s, and the cache written out again as keys and
-// values (86 MB) 23 us more; a single token a sequence takes as long as the
+// values (86 MB) 12 us (7 TB/s, its reads from L2); a single token a sequence takes as long as the
 // host's two calls, 15 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -296,17 +296,38 @@ struct ExpandTo {
   void *k, *v;
   int num_pages, max_pages, page_size, Bt, Hkv;
   int32_t* err_word;  // null: nothing is raised
+  int wide;           // k and v are 32-byte aligned
 };
 
-__device__ __forceinline__ void put16(float* to, const uint32_t (&h)[8], float unit) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h[2 * i]));
-    const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&h[2 * i + 1]));
-    reinterpret_cast<float4*>(to)[i] = make_float4(a.x * unit, a.y * unit, b.x * unit, b.y * unit);
+__device__ __forceinline__ void st_global_256(void* p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+// 32 bytes; in one store where they are a whole sector (two of 16, with other
+// lanes' between them, cost L2 a partial sector each).
+__device__ __forceinline__ void put32(void* to, const uint32_t (&o)[8], bool wide) {
+  if (wide) {
+    st_global_256(to, o);
+  } else {
+    static_cast<uint4*>(to)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+    static_cast<uint4*>(to)[1] = make_uint4(o[4], o[5], o[6], o[7]);
   }
 }
-__device__ __forceinline__ void put16(__nv_bfloat16* to, const uint32_t (&h)[8], float unit) {
+__device__ __forceinline__ void put16(float* to, const uint32_t (&h)[8], float unit, bool wide) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t o[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h[4 * i + k]));
+      o[2 * k] = __float_as_uint(a.x * unit);
+      o[2 * k + 1] = __float_as_uint(a.y * unit);
+    }
+    put32(to + 8 * i, o, wide);
+  }
+}
+__device__ __forceinline__ void put16(__nv_bfloat16* to, const uint32_t (&h)[8], float unit, bool wide) {
   uint32_t o[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -314,8 +335,7 @@ __device__ __forceinline__ void put16(__nv_bfloat16* to, const uint32_t (&h)[8],
     const __nv_bfloat162 b = __floats2bfloat162_rn(a.x * unit, a.y * unit);
     o[i] = *reinterpret_cast<const uint32_t*>(&b);
   }
-  reinterpret_cast<uint4*>(to)[0] = make_uint4(o[0], o[1], o[2], o[3]);
-  reinterpret_cast<uint4*>(to)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+  put32(to, o, wide);
 }
 
 // One group: 8 bytes of codes and a scale to 16 values.
@@ -368,9 +388,9 @@ __device__ __forceinline__ void expand_rows(const ExpandTo& t, const int32_t* ta
         if (i < lo || i >= hi) continue;
         uint32_t h[8];
         group_values(kw[j], ks[j], h);
-        put16(static_cast<E*>(t.k) + (base + i) * kQ4Group, h, t.c.k_unit);
+        put16(static_cast<E*>(t.k) + (base + i) * kQ4Group, h, t.c.k_unit, t.wide);
         group_values(vw[j], vs[j], h);
-        put16(static_cast<E*>(t.v) + (base + i) * kQ4Group, h, t.c.v_unit);
+        put16(static_cast<E*>(t.v) + (base + i) * kQ4Group, h, t.c.v_unit, t.wide);
       }
     }
   }
@@ -408,6 +428,8 @@ __global__ void __launch_bounds__(kThreads) expand_seen_kernel(const __grid_cons
   }
 }
 
+int wide_ok(const void* k, const void* v) { return ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 31u) == 0; }
+
 // About 16 blocks an SM over all sequences.
 dim3 expand_grid(int Bt, int num_sms) {
   const int y = std::min(Bt, 65535);
@@ -424,7 +446,8 @@ cudaError_t launch_rope_q4(int elem_bytes, const RopeArgs& a, const simsd_q4_cac
 }
 
 cudaError_t launch_q4_expand(int elem_bytes, const ExpandArgs& a, int num_sms, cudaStream_t stream) {
-  const ExpandTo t{a.c, a.block_table, a.k_cache, a.v_cache, a.num_pages, a.max_pages, a.page_size, a.Bt, a.Hkv, a.err_word};
+  const ExpandTo t{a.c, a.block_table, a.k_cache, a.v_cache, a.num_pages, a.max_pages, a.page_size, a.Bt, a.Hkv, a.err_word,
+                   wide_ok(a.k_cache, a.v_cache)};
   auto* kern = elem_bytes == 4 ? (a.d == 128 ? expand_kernel<float, 128> : expand_kernel<float, 64>)
                                : (a.d == 128 ? expand_kernel<__nv_bfloat16, 128> : expand_kernel<__nv_bfloat16, 64>);
   return launch_overlapped(kern, expand_grid(a.Bt, num_sms), dim3(kThreads), 0, stream, 1u, t, a.first, a.last);
@@ -432,7 +455,8 @@ cudaError_t launch_q4_expand(int elem_bytes, const ExpandArgs& a, int num_sms, c
 
 cudaError_t launch_q4_expand_seen(int elem_bytes, const ChunkArgs& a, const simsd_q4_cache& c, void* k_image,
                                   void* v_image, int num_sms, cudaStream_t stream) {
-  const ExpandTo t{c, a.block_table, k_image, v_image, a.num_pages, a.max_pages, a.page_size, a.Bt, a.Hkv, nullptr};
+  const ExpandTo t{c, a.block_table, k_image, v_image, a.num_pages, a.max_pages, a.page_size, a.Bt, a.Hkv, nullptr,
+                   wide_ok(k_image, v_image)};
   auto* kern = elem_bytes == 4
                    ? (a.d == 128 ? expand_seen_kernel<float, 128> : expand_seen_kernel<float, 64>)
                    : (a.d == 128 ? expand_seen_kernel<__nv_bfloat16, 128> : expand_seen_kernel<__nv_bfloat16, 64>);

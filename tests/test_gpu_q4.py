@@ -192,6 +192,21 @@ def test_expand(dtype, d, P, units):
         assert torch.equal(out[i].cpu(), want)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_expand_to_arrays_at_odd_multiples_of_16_bytes(dtype):
+    g = torch.Generator().manual_seed(11)
+    cache = simsd.Q4Cache(*(torch.randint(0, 120, (5, 2, 16, w), dtype=torch.uint8, generator=g).cuda() for w in (32, 4) * 2))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    table, first, last = torch.arange(5, **i32)[None], torch.tensor([3], **i32), torch.tensor([77], **i32)
+    n, shift = 5 * 2 * 16 * 64, 16 // dtype.itemsize
+    outs = []
+    for k, v in ((0, 0), (shift, 0), (shift, shift)):
+        pair = [torch.full((n + 16,), 5.0, dtype=dtype, device="cuda")[at:at + n].view(5, 2, 16, 64) for at in (k, v)]
+        simsd.simsd_q4_expand(cache, table, first, last, *pair)
+        outs.append(torch.stack(pair))
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2]) and bool((outs[0] != 5).any())
+
+
 def test_expand_errors():
     g = torch.Generator().manual_seed(1)
     _, pool, table = layout([0] * 3, [40, 40, 40], 8, g)
