@@ -38,7 +38,7 @@
 // scores: about 2000 of the 2530 cycles, the two products 1024) for prompts,
 // HBM for single tokens.  Measured, 32 heads on 8, d 128: 8192 tokens of one
 // prompt 434 us (1.3 PFLOP/s of the two products, causal), 2048 after 32768
-// 765 us (1.5); 64 single tokens over 2048 to 8192 rows 210 us (6.4 TB/s); 8
+// 740 us (1.5); 64 single tokens over 2048 to 8192 rows 208 us (6.4 TB/s); 8
 // over 512 to 1024, 16 heads, 18 us, most of it one CTA's chain from the
 // tokens' offsets to its first tile and the second launch.  Single tokens are
 // units of one row block: the blocks take them in turns, so that a unit's
