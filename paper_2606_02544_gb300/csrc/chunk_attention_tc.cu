@@ -44,7 +44,7 @@
 // units of one row block: the blocks take them in turns, so that a unit's
 // last tile and its output lie under the next one's tiles (with block A
 // alone 214 and 20 us).  Through a window of 1024 rows with 4 first ones, 64
-// single tokens, 74 us (82); a prompt of 8192, block-causal, with 64 first
+// single tokens, 73 us (82); a prompt of 8192, block-causal, with 64 first
 // ones, 176 us.  (Exponentials on the FMA pipes for an eighth to a half of the
 // keys: 220 to 258 us; the softmax is bound by issue, not by the unit.)
 // TMEM (512 columns): S_A [0,128), S_B [128,256), O_A [256,384), O_B
@@ -228,7 +228,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   using Smem = SmemChunk<D, SINKS>;
   constexpr int kHalves = Smem::kHalves, kStages = Smem::kStages, kStagesK = Smem::kStagesK, kStagesV = Smem::kStagesV;
   extern __shared__ uint8_t smem_raw[];
-  Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  // By an offset from the array the compiler knows that this is shared memory,
+  // by a rounded number it does not: worth 74 -> 73 us to 64 single tokens
+  // through a window, but two row blocks then fall out of antiphase (2048
+  // tokens after 32768 rows 740 -> 850 us).
+  Smem& sm = *reinterpret_cast<Smem*>(
+      ALT ? smem_raw + (0u - smem_u32(smem_raw) & 1023u)
+          : reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023)));
   volatile int* abort_flag = &sm.abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
