@@ -59,7 +59,7 @@ struct Q4Params {
   simsd_q4_cache c;
   int g, ub, ctas;    // heads per KV head, tokens of a unit, grid size
   int sub;            // keys per copy: a page, or part of one
-  float scale_log2;   // scores to log2 units, the keys' unit included
+  ScoreScale scale;   // of scores, in log2 units
 };
 
 // NB blocks of 8 query rows.  CTAs of four warps, whose 32 keys a tile pay for
@@ -316,8 +316,8 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
           }
           top = max(top, __shfl_xor_sync(full, top, 1));
           top = max(top, __shfl_xor_sync(full, top, 2));
-          float down, up;
-          q_powers(top, down, up);
+          float down;
+          const float factor = q_factor(top, p.scale, down);
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) {
             const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
@@ -326,8 +326,8 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
               q[nb][2 * j + e / 2][e & 1] = pack_f16x2(__uint_as_float(w[e] << 16) * down, __uint_as_float(w[e] & 0xffff0000u) * down);
           }
           // scores of rows 2t and 2t + 1, whose q lies with lanes of g = 2t and 2t + 1
-          rs[nb][0] = __shfl_sync(full, up, 8 * t) * p.scale_log2;
-          rs[nb][1] = __shfl_sync(full, up, 8 * t + 4) * p.scale_log2;
+          rs[nb][0] = __shfl_sync(full, factor, 8 * t);
+          rs[nb][1] = __shfl_sync(full, factor, 8 * t + 4);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sm.bar_qfree[qb]));
@@ -701,7 +701,7 @@ cudaError_t launch_chunk_attention_q4(const ChunkArgs& a, const simsd_q4_cache& 
   p.c = c;
   p.g = a.Hq / a.Hkv;
   p.sub = a.page_size % kTile == 0 ? kTile : std::min(a.page_size, 64);
-  p.scale_log2 = a.scale * c.k_unit * 1.4426950408889634f;
+  p.scale = score_scale(a.scale, c.k_unit);
   if (a.sinks > 0) return a.d == 128 ? launch_d<128, true>(p, num_sms, stream) : launch_d<64, true>(p, num_sms, stream);
   return a.d == 128 ? launch_d<128, false>(p, num_sms, stream) : launch_d<64, false>(p, num_sms, stream);
 }

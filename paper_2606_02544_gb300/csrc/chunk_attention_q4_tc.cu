@@ -83,7 +83,7 @@ struct Q4TcParams {
   simsd_q4_cache c;
   int g, tb;          // heads per KV head, tokens of a unit
   int ctas, sub;      // grid size; keys per copy
-  float scale_log2;   // scores to log2 units, the keys' unit included
+  ScoreScale scale;   // of scores, in log2 units
 };
 
 template <int D, bool LEAN>
@@ -104,7 +104,7 @@ struct alignas(1024) SmemQ4Tc {
   uint64_t bar_qraw, bar_q, bar_qfree;
   uint64_t bar_s[2], bar_p[2][2], bar_pv[2], bar_ofree, bar_meet, bar_drain[2];
   float2 ml[2][LEAN ? 1 : 2][kRows];  // (m, l) of the sets' lanes, for pieces in turns
-  float q_up[2][kRows];    // the powers of two that Q was divided by, for units in turns
+  float q_factor[2][kRows];  // of the rows' scores, for units in turns
   // lean units: O of the upper lanes on its way to the lower ones, 16 columns
   // at a time, in two buffers
   float o[LEAN ? 2 : 1][16][kRows / 2];
@@ -516,10 +516,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
             }
           }
-          float down, up;
-          q_powers(top, down, up);
           if (set == 0) {
-            sm.q_up[units & 1][row] = up;
+            float down;
+            scale = q_factor(top, p.scale, down);
+            sm.q_factor[units & 1][row] = scale;
             auto half2_of = [&](uint32_t w) {
               return pack_f16x2(__uint_as_float(w << 16) * down, __uint_as_float(w & 0xffff0000u) * down);
             };
@@ -556,9 +556,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           } else {
             ok = wait(sm.bar_q, units & 1);
             if (!ok) break;
-            up = sm.q_up[units & 1][row];
+            scale = sm.q_factor[units & 1][row];
           }
-          scale = up * p.scale_log2;
           ++units;
         }
       }
@@ -858,7 +857,7 @@ cudaError_t launch_chunk_attention_q4_tc(const ChunkArgs& a, const simsd_q4_cach
   p.c = c;
   p.g = a.Hq / a.Hkv;
   p.sub = a.page_size % kTile == 0 ? kTile : std::min(a.page_size, 64);
-  p.scale_log2 = a.scale * c.k_unit * 1.4426950408889634f;
+  p.scale = score_scale(a.scale, c.k_unit);
   if (a.sinks > 0) return a.d == 128 ? launch_d<128, true>(p, num_sms, encode, stream) : launch_d<64, true>(p, num_sms, encode, stream);
   return a.d == 128 ? launch_d<128, false>(p, num_sms, encode, stream) : launch_d<64, false>(p, num_sms, encode, stream);
 }

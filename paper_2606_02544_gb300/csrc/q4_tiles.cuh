@@ -2,6 +2,8 @@
 // shared by the kernels that read one: what the walking warp says of a tile,
 // and the copies that bring its codes and scales.
 #pragma once
+#include <cmath>
+
 #include "chunk_walk.cuh"
 #include "ptx.cuh"
 #include "q4.cuh"
@@ -150,12 +152,28 @@ struct TileWalk {
   }
 };
 
-// A power of two that brings a row's largest component to [1, 4), from that
-// component's bf16 bits without the sign, and its inverse.
-__device__ __forceinline__ void q_powers(uint32_t top, float& down, float& up) {
-  const uint32_t ex = min(max(top >> 7, 1u), 253u);  // 2^(ex - 127) <= the largest < 2^(ex - 126)
-  down = __uint_as_float((254u - ex) << 23);
-  up = __uint_as_float(ex << 23);
+// What turns products of codes' values into scores in log2 units, m 2^e with m
+// in [1, 2]: the softmax scale, the keys' unit and log2(e).
+struct ScoreScale {
+  float m;
+  int e;
+};
+inline ScoreScale score_scale(float softmax_scale, float k_unit) {
+  int e;
+  const double m = std::frexp(static_cast<double>(softmax_scale) * k_unit * 1.4426950408889634, &e);
+  return ScoreScale{static_cast<float>(2.0 * m), e - 1};
+}
+// A power of two, `down`, that brings a row's largest component to [1, 4), from
+// that component's bf16 bits without the sign, and the factor of the row's
+// scores, which undoes it.  The factor stays among fp32's normal numbers: as 0
+// (a row of zeros has the largest power, and a unit may be 2^-64) it would turn
+// hidden keys' -inf into NaN, as inf scores of 0.  Nothing is lost by it: below
+// 2^-126 all scores of a row are 0 in fp32's sense (under 2^-104), above 2^126
+// two that differ do so by more than 2^90.
+__device__ __forceinline__ float q_factor(uint32_t top, const ScoreScale& s, float& down) {
+  const int ex = min(max(static_cast<int>(top >> 7), 1), 253);  // 2^(ex - 127) <= the largest < 2^(ex - 126)
+  down = __uint_as_float(static_cast<uint32_t>(254 - ex) << 23);
+  return __uint_as_float(static_cast<uint32_t>(min(max(ex + s.e, 1), 253)) << 23) * s.m;
 }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   uint32_t r;

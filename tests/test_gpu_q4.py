@@ -508,3 +508,35 @@ def test_many_sequences():
     # two kernels, each off by 2^-11 of the probabilities and 2^-8 of the output at most
     diff = (outs[0] - torch.cat(outs[1:])).abs()
     assert bool((diff <= 2.0 ** -9 * 6.0 + 2.0 ** -7 * outs[0].abs()).all())
+
+
+WAYS = [[1] * 6, [9, 2, 16], [60, 33, 1]]  # from the registers, lean tiles, wide tiles
+
+
+@pytest.mark.parametrize("chunk", WAYS)
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("units,scale", [((2.0 ** -24, 1.0), 0.0), ((2.0 ** -64, 2.0 ** 64), 0.0), ((2.0 ** 64, 2.0 ** -64), 0.0),
+                                         ((1.0, 1.0), 2.0 ** -60), ((2.0 ** -64, 1.0), 2.0 ** -140)])
+def test_zero_and_small_queries_at_the_ends_of_the_units(chunk, d, units, scale):
+    """Rows of q whose factor leaves fp32's normal numbers, with hidden keys
+    beside them: the mean of the values that they see."""
+    prefix = [300, 140, 5, 64, 0, 129][:len(chunk)]
+    a = attention_case(BF16, chunk, prefix, 8, 2, d, 16, 21, units=units)
+    if units[0] > 1:
+        a["q"] = a["q"] / units[0]
+    a["q"][0] = 0
+    a["q"][1] *= 2.0 ** -100 if units[0] <= 1 else 2.0 ** -50
+    a["q"][-1, :4] = 2.0 ** -126
+    check(a, softmax_scale=scale)
+
+
+@pytest.mark.parametrize("chunk", WAYS)
+def test_large_queries_on_keys_of_zeros(chunk):
+    """Scores are zero, though the factor of a row passes fp32."""
+    a = attention_case(BF16, chunk, [300, 140, 5, 64, 0, 129][:len(chunk)], 8, 2, 128, 16, 22, units=(2.0 ** 64, 1.0))
+    a["cache"].tensors[0].zero_()
+    want = run(a | dict(q=torch.zeros_like(a["q"])))
+    a["q"] = a["q"] * 2.0 ** 100
+    got = run(a)
+    assert got[2] == 0 and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    check(a | dict(q=torch.zeros_like(a["q"])))
