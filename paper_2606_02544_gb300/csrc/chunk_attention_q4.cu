@@ -51,7 +51,7 @@ namespace {
 constexpr int kTile = kQ4Tile;
 constexpr int kMaxSeqs = 8192;  // their tile counts fit the ring
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
-constexpr float kNoReference = -1.0e30f;   // of rows that have seen no key
+constexpr float kNoReference = -3.402823466e38f;  // of rows that have seen no key: the lowest number, below every score
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct Q4Params {
@@ -399,7 +399,9 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
               }
           }
       }
-      // exponents; those of rows whose reference has to move again
+      // exponents; those of rows whose reference has to move again.  Scores are
+      // rounded before the reference is taken off, as it was: far from zero a
+      // product that is not would differ from it by more than an exponent holds
       float pr[G][NB][4];
       bool above = false;
 #pragma unroll
@@ -408,7 +410,8 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            pr[u][nb][e] = fmaf(sc[u][nb][e], rs[nb][e & 1], -m[nb][e & 1]);
+            sc[u][nb][e] = __fmul_rn(sc[u][nb][e], rs[nb][e & 1]);
+            pr[u][nb][e] = sc[u][nb][e] - m[nb][e & 1];
             above |= pr[u][nb][e] > kRescaleThreshold;
           }
       if (__any_sync(full, above)) {
@@ -418,7 +421,7 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
           for (int e = 0; e < 2; ++e) {
             float mx = m[nb][e];
 #pragma unroll
-            for (int u = 0; u < G; ++u) mx = fmaxf(mx, fmaxf(sc[u][nb][e], sc[u][nb][e + 2]) * rs[nb][e]);
+            for (int u = 0; u < G; ++u) mx = fmaxf(mx, fmaxf(sc[u][nb][e], sc[u][nb][e + 2]));
             mx = fmaxf(mx, __shfl_xor_sync(full, mx, 4));
             mx = fmaxf(mx, __shfl_xor_sync(full, mx, 8));
             mx = fmaxf(mx, __shfl_xor_sync(full, mx, 16));
@@ -432,8 +435,8 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
             }
 #pragma unroll
             for (int u = 0; u < G; ++u) {
-              pr[u][nb][e] = fmaf(sc[u][nb][e], rs[nb][e], -mx);
-              pr[u][nb][e + 2] = fmaf(sc[u][nb][e + 2], rs[nb][e], -mx);
+              pr[u][nb][e] = sc[u][nb][e] - mx;
+              pr[u][nb][e + 2] = sc[u][nb][e + 2] - mx;
             }
           }
       }

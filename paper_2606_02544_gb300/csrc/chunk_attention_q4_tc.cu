@@ -518,8 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if (set == 0) {
             float down;
-            scale = q_factor(top, p.scale, down);
-            sm.q_factor[units & 1][row] = scale;
+            sm.q_factor[units & 1][row] = q_factor(top, p.scale, down);
             auto half2_of = [&](uint32_t w) {
               return pack_f16x2(__uint_as_float(w << 16) * down, __uint_as_float(w & 0xffff0000u) * down);
             };
@@ -556,8 +555,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           } else {
             ok = wait(sm.bar_q, units & 1);
             if (!ok) break;
-            scale = sm.q_factor[units & 1][row];
           }
+          scale = sm.q_factor[units & 1][row];
           ++units;
         }
       }
@@ -628,7 +627,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           const float neg_m = m_ref != -INFINITY ? -m_ref : 0.f;
-          const unsigned long long sc2 = f32x2(scale, scale), nm2 = f32x2(neg_m, neg_m);
+          const unsigned long long sc2 = f32x2(scale, scale), nm2 = f32x2(neg_m, neg_m), zero2 = f32x2(0.f, 0.f);
           unsigned long long acc[4] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f), f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
           if constexpr (LEAN) {
             // the keys of the other half of the lanes
@@ -641,8 +640,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint32_t pk[16];
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
+              // Scores are rounded before the reference is taken off, as it was:
+              // far from zero a product that is not would differ from it by more
+              // than an exponent holds.  (In one step 1 to 2% faster; by a
+              // branch that only such rows take, slower than by two steps.)
               float e0, e1;
-              f32x2_split(fma_f32x2(f32x2(__uint_as_float(xs[q][2 * k]), __uint_as_float(xs[q][2 * k + 1])), sc2, nm2), e0, e1);
+              const unsigned long long s2 = fma_f32x2(f32x2(__uint_as_float(xs[q][2 * k]), __uint_as_float(xs[q][2 * k + 1])), sc2, zero2);
+              f32x2_split(add_f32x2(s2, nm2), e0, e1);
               const float p0 = fast_exp2(e0), p1 = fast_exp2(e1);
               acc[k & 3] = add_f32x2(acc[k & 3], f32x2(p0, p1));
               pk[k] = pack_f16x2(p0, p1);

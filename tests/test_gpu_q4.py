@@ -540,3 +540,38 @@ def test_large_queries_on_keys_of_zeros(chunk):
     got = run(a)
     assert got[2] == 0 and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     check(a | dict(q=torch.zeros_like(a["q"])))
+
+
+@pytest.mark.parametrize("chunk", WAYS)
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("level", [20, 25, 29, 33, 60, 100, 126])
+def test_scores_far_from_zero(chunk, sign, level):
+    """Two levels of scores around 2^level in log2 units, of either sign: the
+    mean of the values at the higher one.  Far apart as the two are, equal
+    scores have weights of equal bits, so that what is left is 2^-11 for them
+    in fp16, 2^-8 for the output and 2^-23 a sum."""
+    prefix = [300, 140, 5, 64, 0, 129][:len(chunk)]
+    a = attention_case(BF16, chunk, prefix, 8, 2, 128, 16, 23, units=(2.0 ** 64, 1.0))
+    kc, ks = a["cache"].tensors[:2]
+    kc.zero_()
+    kc[..., 0] = torch.where(torch.arange(16, device="cuda") % 3 == 0, 7, 5).to(torch.uint8)  # 6 and 3
+    ks[ks != 127] = 56  # 1
+    a["q"].zero_()
+    a["q"][..., 0] = sign * 1.3359375 * 2.0 ** (level - 64)
+    out, lse, word = run(a, softmax_scale=0.1)
+    assert word == 0
+    start, table = a["token_start"].tolist(), a["block_table"].cpu().numpy()
+    v = ref.decode(*(t.cpu().numpy() for t in a["cache"].tensors[2:]))
+    unit = sign * float(np.float32(0.1)) * 1.3359375 * 2.0 ** level
+    for b, n in enumerate(prefix):
+        for i in range(chunk[b]):
+            r = np.arange(n + i + 1)
+            best = r % 16 % 3 == 0 if sign > 0 or len(r) == 1 else r % 16 % 3 != 0
+            rows = v[table[b, r[best] // 16], :, r[best] % 16].repeat(4, 1)
+            want, size = rows.mean(0), np.abs(rows).mean(0)
+            got = out[start[b] + i].double().cpu().numpy()
+            assert np.all(np.abs(got - want) <= (size * 2.0 ** -11 + np.abs(want) * 2.0 ** -8) * (1 + 2.0 ** -7)
+                          + size * (len(r) // 128 + 72) * 2.0 ** -22), (b, i)
+            score = unit * (6 if best[0] else 3)
+            lw = score + math.log(best.sum())
+            assert np.all(np.abs(lse[start[b] + i].double().cpu().numpy() - lw) <= 2.0 ** -21 * abs(lw)), (b, i)
