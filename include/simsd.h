@@ -572,7 +572,8 @@ SIMSD_API int simsd_q4_expand(int dtype, const simsd_q4_cache* cache, int num_pa
  * SIMSD_BF16 with up to 768 query rows a sequence and KV head on average (T Hq
  * <= 768 Bt Hkv; heads of 64: 512) reads the codes: keys and values are exact in the products'
  * fp16, q is scaled by a power of two to its row's largest component,
- * probabilities are rounded to fp16.  More rows, and SIMSD_F32, go through an
+ * probabilities are rounded to fp16 (by 2^-11 of each, or 2^-32 of a row's
+ * largest where that is more).  More rows, and SIMSD_F32, go through an
  * image of the rows that are seen in dtype, with the cache's page ids, in the
  * workspace (num_pages Hkv page_size d elements of keys and of values): make
  * the workspace once for all layers of a model.

@@ -2,8 +2,8 @@
 // paged cache in 4 bits (Sec. 3.3: the prefix is read from a KV cache).
 //
 // Mathematics.  As in chunk_attention_tc.cu: one pass over the keys with a
-// running reference maximum and sum (fp32; the reference moves only when a
-// score exceeds it by 2^8).  Keys and values are scale times code: 6
+// running reference and sum (fp32; q4_tiles.cuh says where the reference lies
+// and when it moves).  Keys and values are scale times code: 6
 // significant bits, exact in fp16.  q is multiplied by a power of two that
 // brings its row's largest component to [1, 4) and is then exact in fp16 too,
 // but for components below 2^-14 of the largest (off by 2^-25 of it at most).
@@ -50,7 +50,6 @@ namespace {
 
 constexpr int kTile = kQ4Tile;
 constexpr int kMaxSeqs = 8192;  // their tile counts fit the ring
-constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr float kNoReference = -3.402823466e38f;  // of rows that have seen no key: the lowest number, below every score
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -412,19 +411,20 @@ __global__ void __launch_bounds__(Cfg<D, NB>::kThreads, Cfg<D, NB>::kCtas) chunk
           for (int e = 0; e < 4; ++e) {
             sc[u][nb][e] = __fmul_rn(sc[u][nb][e], rs[nb][e & 1]);
             pr[u][nb][e] = sc[u][nb][e] - m[nb][e & 1];
-            above |= pr[u][nb][e] > kRescaleThreshold;
+            above |= pr[u][nb][e] > kMoveAbove;
           }
       if (__any_sync(full, above)) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float mx = m[nb][e];
+            float mx = kNoReference;
 #pragma unroll
             for (int u = 0; u < G; ++u) mx = fmaxf(mx, fmaxf(sc[u][nb][e], sc[u][nb][e + 2]));
             mx = fmaxf(mx, __shfl_xor_sync(full, mx, 4));
             mx = fmaxf(mx, __shfl_xor_sync(full, mx, 8));
             mx = fmaxf(mx, __shfl_xor_sync(full, mx, 16));
+            mx = fmaxf(m[nb][e], mx - kHeadroom);
             const float f = fast_exp2(m[nb][e] - mx);
             m[nb][e] = mx;
             l[nb][e] *= f;

@@ -5,7 +5,7 @@
 // Mathematics.  As in chunk_attention_q4.cu: keys and values are exact in
 // fp16, q is brought to fp16 by a power of two a row, probabilities are
 // rounded to fp16, S and O are accumulated in fp32; the softmax is that of
-// chunk_attention_tc.cu.
+// chunk_attention_tc.cu but for the place of its reference (q4_tiles.cuh).
 //
 // A unit is (KV head, sequence, up to 128 query rows), a tile 128 keys.  The
 // codes and scales of a tile (18 KB) come by bulk copies; eight warps turn
@@ -75,7 +75,6 @@ constexpr uint32_t kColO = 256;  // + 128 per set
 constexpr uint32_t kColQ = 384;  // lean units: Q
 constexpr int kHalfBytes = kTile * 128;  // 128 rows x 64 fp16
 constexpr int kInfos = 8;                // tiles that the walk is ahead of the last reader
-constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct Q4TcParams {
@@ -605,11 +604,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             return fmax3(fmax3(r[0], r[1], r[2]), fmax3(r[3], r[4], r[5]), fmaxf(r[6], r[7]));
           };
           const float mx = max_of() * scale;
-          const bool move = seen && mx != -INFINITY && (m_ref == -INFINITY || mx > m_ref + kRescaleThreshold);
+          const bool move = seen && mx != -INFINITY && (m_ref == -INFINITY || mx > m_ref + kMoveAbove);
           if (__any_sync(full, move)) {
-            const float f = move && m_ref != -INFINITY ? fast_exp2(m_ref - mx) : 1.0f;
+            const float f = move && m_ref != -INFINITY ? fast_exp2(m_ref - (mx - kHeadroom)) : 1.0f;
             l_sum *= f;
-            if (move) m_ref = mx;
+            if (move) m_ref = mx - kHeadroom;
             if (!(flags & kFirst)) {
               // O holds the piece's earlier tiles once the PV before this one is done
               ok = wait(sm.bar_pv[buf ^ 1], ((c - 1) >> 1) & 1);

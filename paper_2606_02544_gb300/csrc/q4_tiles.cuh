@@ -175,6 +175,12 @@ __device__ __forceinline__ float q_factor(uint32_t top, const ScoreScale& s, flo
   down = __uint_as_float(static_cast<uint32_t>(254 - ex) << 23);
   return __uint_as_float(static_cast<uint32_t>(min(max(ex + s.e, 1), 253)) << 23) * s.m;
 }
+// Probabilities in fp16 have 2^-24 as their smallest number: with a weight of 1
+// for the largest, keys 2^25 times smaller would count in the sum and not in
+// the output (2^18 of them at 2^-25.5, 0.5% of a row).  So a reference is set
+// kHeadroom below the maximum, for which the largest weighs 2^7, and is left
+// until a score is kMoveAbove above it: 2^15, below fp16's 65504.
+constexpr float kHeadroom = 7.0f, kMoveAbove = 15.0f;  // log2 units
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));

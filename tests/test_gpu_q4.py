@@ -575,3 +575,38 @@ def test_scores_far_from_zero(chunk, sign, level):
             score = unit * (6 if best[0] else 3)
             lw = score + math.log(best.sum())
             assert np.all(np.abs(lse[start[b] + i].double().cpu().numpy() - lw) <= 2.0 ** -21 * abs(lw)), (b, i)
+
+
+@pytest.mark.parametrize("T", [1, 9, 40])  # from the registers, lean tiles, wide tiles
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_keys_far_below_one(T, d):
+    """A first row whose score is 25.5 log2 units above all others', which are
+    2^18: what they add up to, 2^-7.5 of the whole, is not lost, though a CTA
+    has all of a sequence.  A probability is off by 2^-32 of the largest one's
+    (fp16's 2^-25, of weights of 2^7 for it), so their sum by 2^-14, the output
+    by 2^-8.  A sum of weights is one of 2^11 tiles with two additions each to
+    a thread's, all after the first row's 2^7: each is off by half a step, 2^-24
+    of the whole, so the sum, and with it the output and e^lse, by 2^-12."""
+    n, P, seqs = 2 ** 18, 128, 912
+    i32 = dict(dtype=torch.int32, device="cuda")
+    pages = n // P + 1
+    cache = simsd.Q4Cache.zeros(pages, 1, P, d)
+    kc, ks, vc, vs = cache.tensors
+    ks.fill_(56)  # scale 1
+    vs.fill_(56)
+    vc.fill_(0x22)  # 1
+    table = torch.randperm(pages, generator=torch.Generator().manual_seed(1)).int()[None].cuda()
+    first = int(table[0, 0])
+    kc[first, 0, 0, 0] = 7  # 6, in component 0
+    vc[first, 0, 0] = 0
+    q = torch.zeros(seqs * T, 4, d, dtype=BF16, device="cuda")
+    q[..., 0] = 1
+    scale = float(np.float32(25.5 * math.log(2) / 6))
+    out, lse, word = run(dict(q=q, token_start=torch.arange(seqs + 1, **i32) * T, prefix_len=torch.full((seqs,), n, **i32),
+                              cache=cache, block_table=table.repeat(seqs, 1)), softmax_scale=scale)
+    assert word == 0
+    rest = np.tile((n + np.arange(T)) * math.exp(-6 * scale), seqs)
+    want = torch.from_numpy(rest / (1 + rest))[:, None, None].cuda()
+    assert bool(((out.double() - want).abs() <= n * 2.0 ** -32 + (2.0 ** -8 + 2.0 ** -12) * want).all())
+    total = 6 * scale + torch.from_numpy(np.log1p(rest))[:, None].cuda()
+    assert bool(((lse.double() - total).abs() <= 2.0 ** -21 * (1 + total) + 2.0 ** -12).all())
