@@ -15,7 +15,14 @@ constexpr int kQ4Group = 16;
 // so that the largest component falls on 6, to nearest (at most 448, NaN for
 // NaN); never 0, so that x / scale is defined.
 __device__ __forceinline__ uint32_t q4_scale(float top) {
-  const uint32_t s = __nv_cvt_float_to_fp8(top * (1.f / 6.f), __NV_SATFINITE, __NV_E4M3);
+  // top / 6 correctly rounded: the product with fl(1 / 6) and one step of
+  // correction by its residual (Markstein 1990).  The product alone puts some
+  // numbers next below a border between two scales on it.  (An infinity, and
+  // only that, has no residual.)
+  float y = top * (1.f / 6.f);
+  const float z = fmaf(fmaf(-6.f, y, top), 1.f / 6.f, y);
+  if (top < INFINITY) y = z;
+  const uint32_t s = __nv_cvt_float_to_fp8(y, __NV_SATFINITE, __NV_E4M3);
   return s == 0 ? 1u : s;
 }
 __device__ __forceinline__ float q4_scale_value(uint32_t s) {

@@ -7,8 +7,8 @@
 // to nearest in 4 bits; the rotated key is taken as it is in fp32, without a
 // rounding to the type before.  x / s is x fl(1 / s) with one step of
 // correction by its residual (Markstein 1990), which makes it correctly
-// rounded, so that ties of 16-bit values go to the even code; top / 6 is a
-// product with fl(1 / 6), exact where it is a tie between two scales.
+// rounded, so that ties of 16-bit values go to the even code; max |x| / 6 is
+// formed the same way.
 // Written out, s times a code has 6 significant bits: exact in fp16 and bf16.
 //
 // A thread owns eight components: a row of 128 is half a warp's (of 64, a

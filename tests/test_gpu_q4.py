@@ -610,3 +610,29 @@ def test_many_keys_far_below_one(T, d):
     assert bool(((out.double() - want).abs() <= n * 2.0 ** -32 + (2.0 ** -8 + 2.0 ** -12) * want).all())
     total = 6 * scale + torch.from_numpy(np.log1p(rest))[:, None].cuda()
     assert bool(((lse.double() - total).abs() <= 2.0 ** -21 * (1 + total) + 2.0 ** -12).all())
+
+
+def test_scales_next_to_their_borders():
+    """Groups whose largest component lies on a border between two scales, or
+    one step of fp32 beside it: the nearest scale, on the border the even one
+    (a border times 6 is exact in fp32)."""
+    borders = (ref.SCALES[1:126] + ref.SCALES[2:127]) / 2
+    top = np.float32(6 * borders)
+    assert np.array_equal(top.astype(np.float64), 6 * borders)
+    x = np.concatenate([[np.nextafter(t, np.float32(0)), t, np.nextafter(t, np.float32(np.inf))] for t in top])
+    x = np.concatenate([x, -x, [0] * (-2 * len(x) % 4)]).astype(np.float32)
+    T = len(x) // 4
+    v = torch.zeros(T, 4, 16)
+    v[:, :, 5] = torch.from_numpy(x).view(T, 4)
+    v = v.view(T, 1, 64).cuda()
+    i32 = dict(dtype=torch.int32, device="cuda")
+    pages = (T + 7) // 8
+    cache = simsd.Q4Cache.zeros(pages, 1, 8, 64)
+    q = torch.empty_like(v)
+    # (at position 0 keys are turned by nothing)
+    simsd.simsd_rope_append_q4(simsd.simsd_rope_plan_init("half", 64, THETA), v, v, v, torch.tensor([0, T], **i32),
+                               torch.zeros(1, **i32), q, cache, torch.arange(pages, **i32)[None], positions=torch.zeros(T, **i32))
+    want = ref.encode(v.double().cpu().numpy()[:, 0])
+    for c, s in (cache.tensors[:2], cache.tensors[2:]):
+        got = ref.decode(*(t.view(pages * 8, -1)[:T].cpu().numpy() for t in (c, s)))
+        assert np.array_equal(got, want)
