@@ -533,10 +533,10 @@ typedef struct simsd_q4_cache {
 
 /*
  * simsd_rope_append_q4 -- simsd_rope_append to a cache in 4 bits.  A group's
- * scale is the largest magnitude of (rotated) x / unit over 6, rounded to the
- * nearest 8-bit number, at least 2^-9 and at most 448; a code is the nearest
- * to x / (unit scale), ties to the even one, at most 6 in magnitude.  Keys are
- * rotated in fp32 and not rounded to dtype before.  A group that holds NaN
+ * scale is the largest magnitude of y = (rotated) x / unit, a number of fp32,
+ * over 6, rounded to the nearest 8-bit number, at least 2^-9 and at most 448; a
+ * code is the nearest to y / scale, ties to the even one, at most 6 in
+ * magnitude.  Keys are rotated in fp32 and not rounded to dtype before.  A group that holds NaN
  * reads back as NaN.  d is 64 or 128; all else, q_out and the error rules
  * included, is as for simsd_rope_append.
  */

@@ -226,9 +226,13 @@ __global__ void __launch_bounds__(kThreads, 3) rope_q4_kernel(const __grid_const
     if (tk.row < 0) continue;
     auto put = [&](float (&x)[8], int h, float unit, void* codes, void* scales) {
       if (unit != 1.f) {
+        // (correctly rounded as the quotients below; what passes fp32 stays an infinity)
         const float inv = 1.f / unit;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= inv;
+        for (int e = 0; e < 8; ++e) {
+          const float y = x[e] * inv, z = fmaf(fmaf(-y, unit, x[e]), inv, y);
+          x[e] = fabsf(y) < INFINITY ? z : y;
+        }
       }
       uint32_t top = 0;  // as bits: a NaN is above every number
 #pragma unroll

@@ -636,3 +636,45 @@ def test_scales_next_to_their_borders():
     for c, s in (cache.tensors[:2], cache.tensors[2:]):
         got = ref.decode(*(t.view(pages * 8, -1)[:T].cpu().numpy() for t in (c, s)))
         assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("unit", [0.7, 3.3, 1.7e-5, 1e10])
+def test_quotients_by_the_unit(unit):
+    """Components on the borders between two codes and next to them, times a
+    unit that is no power of two: codes of x / unit as fp32 has it, correctly
+    rounded, ties to the even code."""
+    u = np.float32(unit)
+    rng = np.random.RandomState(3)
+    T = 300
+    s = ref.SCALES[rng.randint(8, 126, (T, 4))]
+    x = (((ref.LEVELS[1:] + ref.LEVELS[:-1]) / 2)[rng.randint(0, 7, (T, 4, 16))] * s[..., None]).astype(np.float32) * u
+    x[..., 0] = np.float32(6 * s) * u
+    step = rng.randint(-2, 3, x.shape)
+    for k in (1, 2):
+        x = np.where(step >= k, np.nextafter(x, np.float32(np.inf)), np.where(step <= -k, np.nextafter(x, np.float32(0)), x))
+    x = (x * rng.choice([-1, 1], x.shape)).astype(np.float32)
+    v = torch.from_numpy(x).view(T, 1, 64).cuda()
+    i32 = dict(dtype=torch.int32, device="cuda")
+    pages = (T + 7) // 8
+    cache = simsd.Q4Cache.zeros(pages, 1, 8, 64, float(u), float(u))
+    simsd.simsd_rope_append_q4(simsd.simsd_rope_plan_init("half", 64, THETA), v, v, v, torch.tensor([0, T], **i32),
+                               torch.zeros(1, **i32), torch.empty_like(v), cache, torch.arange(pages, **i32)[None],
+                               positions=torch.zeros(T, **i32))
+    want = ref.encode((x / u).astype(np.float64)).reshape(T, 64)
+    for c, s in (cache.tensors[:2], cache.tensors[2:]):
+        got = ref.decode(*(t.view(pages * 8, -1)[:T].cpu().numpy() for t in (c, s)))
+        assert np.array_equal(got, want)
+
+
+def test_quotients_that_pass_fp32():
+    """x / unit beyond fp32 is an infinity: the largest scale, 6 or -6."""
+    v = torch.zeros(1, 1, 64, device="cuda")
+    v[0, 0, 0], v[0, 0, 20] = 1e30, -3e38
+    i32 = dict(dtype=torch.int32, device="cuda")
+    cache = simsd.Q4Cache.zeros(1, 1, 8, 64, 2.0 ** -64, 2.0 ** -63 * 1.3)
+    simsd.simsd_rope_append_q4(simsd.simsd_rope_plan_init("half", 64, THETA), v, v, v, torch.tensor([0, 1], **i32),
+                               torch.zeros(1, **i32), torch.empty_like(v), cache, torch.zeros(1, 1, **i32))
+    want = np.zeros(64)
+    want[0], want[20] = 2688, -2688
+    for c, s in (cache.tensors[:2], cache.tensors[2:]):
+        assert np.array_equal(ref.decode(*(t[0, 0, 0].cpu().numpy() for t in (c, s))), want)
