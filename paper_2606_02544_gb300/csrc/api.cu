@@ -947,8 +947,9 @@ int check_pages(int32_t* block_table, int32_t* refs, int num_pages, int Bt, int 
   if (num_pages < 0 || Bt < 0 || max_pages < 0) return arg_fail("sizes");
   if (Bt > simsd::kPagesMaxSeqs) return unsupported("more than 65536 sequences");
   if (num_pages > 0x7fff0000) return unsupported("too many pages");
-  if (Bt == 0 || max_pages == 0) return SIMSD_OK;
-  if (!block_table || (num_pages > 0 && !refs)) return arg_fail("null pointer");
+  if (Bt == 0) return SIMSD_OK;
+  // (the counts are read whatever the table)
+  if ((max_pages > 0 && !block_table) || (num_pages > 0 && !refs)) return arg_fail("null pointer");
   if (!aligned16(refs)) return arg_fail("refs must be 16-byte aligned");
   return SIMSD_OK;
 }

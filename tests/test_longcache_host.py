@@ -154,3 +154,16 @@ def test_binding_refuses_wrong_tensors():
         q = torch.zeros(2, 4, 64)
         simsd.simsd_chunk_attention_sinks(q, i(2), i(1), torch.zeros(3, 2, 8, 64), torch.zeros(3, 2, 8, 64), i(1, 2),
                                           torch.zeros(2, 4, 64), 8, 1)
+
+
+@pytest.mark.parametrize("mp", [4, 0])
+def test_counts_are_looked_at_whatever_the_table(lib, mp):
+    """A table of no columns does not excuse counts that are null or not on a
+    16-byte boundary: they are read all the same."""
+    a, n = arrays()
+    for refs in (None, odd):
+        assert lib.simsd_pages_extend(one, one, one, refs, 10, 4, mp, 8, None, None) == BAD
+        assert lib.simsd_pages_release(one, one, one, 3, one, refs, 10, 4, mp, 8, None, None) == BAD
+        assert lib.simsd_pages_fork(a, n, one, one, 1, one, one, refs, 10, 4, mp, 8, one, 1 << 20, None, None) == BAD
+        assert lib.simsd_pages_compact(a, n, one, refs, 10, 4, mp, None, one, 1 << 20, None, None) == BAD
+    assert lib.simsd_pages_extend(one, one, one, one, 10, 0, mp, 8, None, None) == 0
