@@ -301,6 +301,7 @@ struct ExpandTo {
   int num_pages, max_pages, page_size, Bt, Hkv;
   int32_t* err_word;  // null: nothing is raised
   int wide;           // k and v are 32-byte aligned
+  int round;          // pages whose (page, head) are counted in 2^30 (nearly always all)
 };
 
 __device__ __forceinline__ void st_global_256(void* p, const uint32_t (&v)[8]) {
@@ -362,39 +363,43 @@ __device__ __forceinline__ void group_values(uint2 w, uint32_t scale, uint32_t (
 template <typename E, int D>
 __device__ __forceinline__ void expand_rows(const ExpandTo& t, const int32_t* table, int r0, int r1) {
   constexpr int G = D / kQ4Group;
-  const int P = t.page_size, k0 = r0 / P, units = ((r1 + P - 1) / P - k0) * t.Hkv, per = P * G;
+  const int P = t.page_size, per = P * G;
   const int wide = min(per, kThreads), sub = threadIdx.x / wide, at = threadIdx.x - sub * wide, turn = kThreads / wide;
-  for (int u = blockIdx.x * turn + sub; u < units; u += gridDim.x * turn) {
-    const int k = u / t.Hkv, pg = table[k0 + k];
-    if (pg < 0 || pg >= t.num_pages) {
-      if (t.err_word) raise_error(t.err_word, SIMSD_EW_PAGE);
-      continue;
-    }
-    // (the page's rows of the range; page k0 + k < 2^31 / P)
-    const int first = (k0 + k) * P, lo = max(0, r0 - first) * G, hi = min(P, r1 - first) * G;
-    const long long base = (static_cast<long long>(pg) * t.Hkv + (u - k * t.Hkv)) * per;
-    constexpr int U = 2;  // groups of a thread whose loads are issued together
-    for (int i0 = at; i0 < hi; i0 += U * wide) {
-      uint2 kw[U], vw[U];
-      uint32_t ks[U], vs[U];
-#pragma unroll
-      for (int j = 0; j < U; ++j) {
-        const int i = i0 + j * wide;
-        const long long g = base + (i >= lo && i < hi ? i : max(lo, i0));  // (a row of the range in any case)
-        kw[j] = static_cast<const uint2*>(t.c.k_codes)[g];
-        vw[j] = static_cast<const uint2*>(t.c.v_codes)[g];
-        ks[j] = static_cast<const uint8_t*>(t.c.k_scales)[g];
-        vs[j] = static_cast<const uint8_t*>(t.c.v_scales)[g];
+  const int end = (r1 - 1) / P + 1;
+  for (int k0 = r0 / P; k0 < end; k0 += min(t.round, end - k0)) {
+    const int units = min(t.round, end - k0) * t.Hkv;
+    for (int u = blockIdx.x * turn + sub; u < units; u += gridDim.x * turn) {
+      const int k = u / t.Hkv, pg = table[k0 + k];
+      if (pg < 0 || pg >= t.num_pages) {
+        if (t.err_word) raise_error(t.err_word, SIMSD_EW_PAGE);
+        continue;
       }
+      // (the page's rows of the range; page k0 + k < 2^31 / P)
+      const int first = (k0 + k) * P, lo = max(0, r0 - first) * G, hi = min(P, r1 - first) * G;
+      const long long base = (static_cast<long long>(pg) * t.Hkv + (u - k * t.Hkv)) * per;
+      constexpr int U = 2;  // groups of a thread whose loads are issued together
+      for (int i0 = at; i0 < hi; i0 += U * wide) {
+        uint2 kw[U], vw[U];
+        uint32_t ks[U], vs[U];
 #pragma unroll
-      for (int j = 0; j < U; ++j) {
-        const int i = i0 + j * wide;
-        if (i < lo || i >= hi) continue;
-        uint32_t h[8];
-        group_values(kw[j], ks[j], h);
-        put16(static_cast<E*>(t.k) + (base + i) * kQ4Group, h, t.c.k_unit, t.wide);
-        group_values(vw[j], vs[j], h);
-        put16(static_cast<E*>(t.v) + (base + i) * kQ4Group, h, t.c.v_unit, t.wide);
+        for (int j = 0; j < U; ++j) {
+          const int i = i0 + j * wide;
+          const long long g = base + (i >= lo && i < hi ? i : max(lo, i0));  // (a row of the range in any case)
+          kw[j] = static_cast<const uint2*>(t.c.k_codes)[g];
+          vw[j] = static_cast<const uint2*>(t.c.v_codes)[g];
+          ks[j] = static_cast<const uint8_t*>(t.c.k_scales)[g];
+          vs[j] = static_cast<const uint8_t*>(t.c.v_scales)[g];
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+          const int i = i0 + j * wide;
+          if (i < lo || i >= hi) continue;
+          uint32_t h[8];
+          group_values(kw[j], ks[j], h);
+          put16(static_cast<E*>(t.k) + (base + i) * kQ4Group, h, t.c.k_unit, t.wide);
+          group_values(vw[j], vs[j], h);
+          put16(static_cast<E*>(t.v) + (base + i) * kQ4Group, h, t.c.v_unit, t.wide);
+        }
       }
     }
   }
@@ -451,7 +456,7 @@ cudaError_t launch_rope_q4(int elem_bytes, const RopeArgs& a, const simsd_q4_cac
 
 cudaError_t launch_q4_expand(int elem_bytes, const ExpandArgs& a, int num_sms, cudaStream_t stream) {
   const ExpandTo t{a.c, a.block_table, a.k_cache, a.v_cache, a.num_pages, a.max_pages, a.page_size, a.Bt, a.Hkv, a.err_word,
-                   wide_ok(a.k_cache, a.v_cache)};
+                   wide_ok(a.k_cache, a.v_cache), (1 << 30) / a.Hkv};
   auto* kern = elem_bytes == 4 ? (a.d == 128 ? expand_kernel<float, 128> : expand_kernel<float, 64>)
                                : (a.d == 128 ? expand_kernel<__nv_bfloat16, 128> : expand_kernel<__nv_bfloat16, 64>);
   return launch_overlapped(kern, expand_grid(a.Bt, num_sms), dim3(kThreads), 0, stream, 1u, t, a.first, a.last);
@@ -460,7 +465,7 @@ cudaError_t launch_q4_expand(int elem_bytes, const ExpandArgs& a, int num_sms, c
 cudaError_t launch_q4_expand_seen(int elem_bytes, const ChunkArgs& a, const simsd_q4_cache& c, void* k_image,
                                   void* v_image, int num_sms, cudaStream_t stream) {
   const ExpandTo t{c, a.block_table, k_image, v_image, a.num_pages, a.max_pages, a.page_size, a.Bt, a.Hkv, nullptr,
-                   wide_ok(k_image, v_image)};
+                   wide_ok(k_image, v_image), (1 << 30) / a.Hkv};
   auto* kern = elem_bytes == 4
                    ? (a.d == 128 ? expand_seen_kernel<float, 128> : expand_seen_kernel<float, 64>)
                    : (a.d == 128 ? expand_seen_kernel<__nv_bfloat16, 128> : expand_seen_kernel<__nv_bfloat16, 64>);

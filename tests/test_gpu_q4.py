@@ -678,3 +678,46 @@ def test_quotients_that_pass_fp32():
     want[0], want[20] = 2688, -2688
     for c, s in (cache.tensors[:2], cache.tensors[2:]):
         assert np.array_equal(ref.decode(*(t[0, 0, 0].cpu().numpy() for t in (c, s))), want)
+
+
+def test_expand_near_the_last_row():
+    """Rows next to 2^31, where a row number plus a page passes 32 bits."""
+    P, d = 704, 64
+    max_pages = 0x7fffff00 // P
+    top = max_pages * P
+    assert top + P - 1 >= 2 ** 31
+    i32 = dict(dtype=torch.int32, device="cuda")
+    cache = simsd.Q4Cache.zeros(2, 1, P, d)
+    for t in cache.tensors:
+        t.random_(0, 127)
+    table = torch.full((1, max_pages), -1, **i32)
+    table[0, -2], table[0, -1] = 1, 0
+    outs = []
+    for tb, first, last in ((table, top - P - 9, top), (torch.tensor([[1, 0]], **i32), P - 9, 2 * P)):
+        out = [torch.full((2, 1, P, d), 5.0, dtype=BF16, device="cuda") for _ in range(2)]
+        err = torch.zeros(1, **i32)
+        simsd.simsd_q4_expand(cache, tb, torch.tensor([first], **i32), torch.tensor([last], **i32), *out, err_word=err)
+        assert simsd.simsd_check_error(err) == 0
+        outs.append(torch.stack(out))
+    assert torch.equal(outs[0], outs[1]) and bool((outs[0][:, 0] != 5).any()) and bool((outs[0][:, 1, 0, :P - 9] == 5).all())
+
+
+def test_expand_of_more_than_2_to_the_31_pages_and_heads():
+    """2^19 entries (of one page, but for the first and the last) of 4096
+    heads: all that they name is written."""
+    Hkv, P, d, n = 4096, 8, 64, 2 ** 19 + 3
+    i32 = dict(dtype=torch.int32, device="cuda")
+    cache = simsd.Q4Cache.zeros(3, Hkv, P, d)
+    for t in cache.tensors:
+        t.random_(0, 127)
+    table = torch.ones(1, n, **i32)
+    table[0, 0], table[0, -1] = 0, 2
+    outs = []
+    for tb in (table, torch.tensor([[0, 1, 2]], **i32)):
+        out = [torch.full((3, Hkv, P, d), 5.0, dtype=BF16, device="cuda") for _ in range(2)]
+        err = torch.zeros(1, **i32)
+        last = tb.shape[1] * P
+        simsd.simsd_q4_expand(cache, tb, torch.zeros(1, **i32), torch.tensor([last], **i32), *out, err_word=err)
+        assert simsd.simsd_check_error(err) == 0
+        outs.append(torch.stack(out))
+    assert torch.equal(outs[0], outs[1]) and not bool((outs[0] == 5).flatten(2).all(2).any())
