@@ -619,10 +619,21 @@ typedef struct simsd_page_array {
  * SIMSD_EW_PREFIX_LEN, a page among them that another entry shares (a
  * sequence cut back into pages that it shares with a fork)
  * SIMSD_EW_SHARED: that sequence gets no page.
+ *
+ * simsd_pages_extend_granted -- the same, and says which sequences may go on:
+ *   granted [Bt] int32 out: lens[b] where every entry of the rows names a page
+ *     of the sequence's own, -1 where the sequence was refused or its pages did
+ *     not suffice (with too few free pages those that want none may go on)
+ * As prefix_len of the calls that append and attend, -1 keeps a sequence from
+ * being written (SIMSD_EW_PREFIX_LEN besides, and outputs of zero).  granted and
+ * lens do not overlap.
  */
 SIMSD_API int simsd_pages_extend(const int32_t* lens, const int32_t* add, int32_t* block_table, int32_t* refs,
                                  int num_pages, int Bt, int max_pages, int page_size, int32_t* err_word,
                                  void* stream);
+SIMSD_API int simsd_pages_extend_granted(const int32_t* lens, const int32_t* add, int32_t* block_table, int32_t* refs,
+                                         int num_pages, int Bt, int max_pages, int page_size, int32_t* granted,
+                                         int32_t* err_word, void* stream);
 
 /*
  * simsd_pages_release -- sequence seq[i] (NULL: i, n = Bt) lets go of the

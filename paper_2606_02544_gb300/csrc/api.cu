@@ -973,8 +973,11 @@ int check_arrays(const simsd_page_array* arrays, int n, int num_pages, simsd::Pa
 
 }  // namespace
 
-int simsd_pages_extend(const int32_t* lens, const int32_t* add, int32_t* block_table, int32_t* refs, int num_pages,
-                       int Bt, int max_pages, int page_size, int32_t* err_word, void* stream) {
+namespace {
+
+// simsd_pages_extend (granted null) and simsd_pages_extend_granted.
+int pages_extend_impl(const int32_t* lens, const int32_t* add, int32_t* block_table, int32_t* refs, int num_pages,
+                      int Bt, int max_pages, int page_size, int32_t* granted, int32_t* err_word, void* stream) {
   int rc = check_pages(block_table, refs, num_pages, Bt, max_pages);
   if (rc == SIMSD_OK) rc = check_rows(max_pages, page_size);
   if (rc != SIMSD_OK) return rc;
@@ -988,6 +991,7 @@ int simsd_pages_extend(const int32_t* lens, const int32_t* add, int32_t* block_t
   a.add = add;
   a.block_table = block_table;
   a.refs = refs;
+  a.granted = granted;
   a.err_word = err_word;
   a.num_pages = num_pages;
   a.Bt = Bt;
@@ -995,6 +999,20 @@ int simsd_pages_extend(const int32_t* lens, const int32_t* add, int32_t* block_t
   a.page_size = page_size;
   cudaError_t e = simsd::launch_pages_extend(a, as_stream(stream));
   return e == cudaSuccess ? SIMSD_OK : cuda_fail(e, "pages_extend launch");
+}
+
+}  // namespace
+
+int simsd_pages_extend(const int32_t* lens, const int32_t* add, int32_t* block_table, int32_t* refs, int num_pages,
+                       int Bt, int max_pages, int page_size, int32_t* err_word, void* stream) {
+  return pages_extend_impl(lens, add, block_table, refs, num_pages, Bt, max_pages, page_size, nullptr, err_word, stream);
+}
+
+int simsd_pages_extend_granted(const int32_t* lens, const int32_t* add, int32_t* block_table, int32_t* refs,
+                               int num_pages, int Bt, int max_pages, int page_size, int32_t* granted,
+                               int32_t* err_word, void* stream) {
+  if (Bt > 0 && (!granted || granted == lens)) return arg_fail("granted: null, or lens itself");
+  return pages_extend_impl(lens, add, block_table, refs, num_pages, Bt, max_pages, page_size, granted, err_word, stream);
 }
 
 int simsd_pages_release(const int32_t* seq, const int32_t* first, const int32_t* last, int n, int32_t* block_table,

@@ -203,7 +203,7 @@ struct PageArrays {
 struct PagesArgs {
   PageArrays pages;
   const int32_t *seq, *src, *dst, *first, *last, *add;
-  int32_t *lens, *block_table, *refs, *live;
+  int32_t *lens, *block_table, *refs, *live, *granted;
   void* workspace;
   int32_t* err_word;
   int n, num_pages, Bt, max_pages, page_size;

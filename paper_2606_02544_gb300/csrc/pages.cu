@@ -193,6 +193,11 @@ __global__ void __launch_bounds__(kPlanThreads, 1) extend_kernel(const __grid_co
   uint32_t err = 0;
   Span mine{0, 0, true};
   int mine_n = 0, mine_at = 0, total = 0;
+  // (granted: whether a sequence was refused is said as soon as that is known,
+  // too few free pages for those that want one below)
+  auto say = [&](int b, bool ok) {
+    if (a.granted && b < a.Bt) a.granted[b] = ok ? a.lens[b] : -1;
+  };
   auto look = [&](int b, Span& s, uint32_t* e) {
     s = Span{0, 0, true};
     if (b < a.Bt) {
@@ -203,7 +208,10 @@ __global__ void __launch_bounds__(kPlanThreads, 1) extend_kernel(const __grid_co
   };
   for (int b0 = 0; b0 < a.Bt; b0 += kPlanThreads) {
     Span s;
-    const int n = look(b0 + tid, s, &err);
+    uint32_t here = 0;
+    const int n = look(b0 + tid, s, &here);
+    say(b0 + tid, here == 0);
+    err |= here;
     int turn;
     const int at = total + block_inclusive(sm.sum, n, turn) - n;
     if (b0 == 0) {
@@ -217,6 +225,11 @@ __global__ void __launch_bounds__(kPlanThreads, 1) extend_kernel(const __grid_co
   if (total == 0) return;
   if (find_free(sm, a.refs, a.num_pages, first, 0, total) < total) {
     if (tid == 0) raise_error(a.err_word, SIMSD_EW_POOL);
+    for (int b0 = 0; a.granted && b0 < a.Bt; b0 += kPlanThreads) {
+      Span s;
+      uint32_t ignored = 0;
+      if (look(b0 + tid, s, &ignored) > 0) say(b0 + tid, false);
+    }
     return;
   }
   // Requests are numbered by sequence, then entry.  A round hands out the

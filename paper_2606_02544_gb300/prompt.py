@@ -87,12 +87,21 @@ class PromptCache:
     def append_chunk(self, qkv, token_start):
         """One chunk of every layer: qkv [L][T][Hq + 2 Hkv][d] (rows of the
         layers' projections), token_start [Bt+1].  Returns the attention
-        outputs [L][T][Hq][d] and advances the prefix lengths."""
+        outputs [L][T][Hq][d] and advances the prefix lengths.
+
+        With a pool, sequences that get no pages (too few are free:
+        SIMSD_EW_POOL in err, and those that want none go on; or they would
+        write to a page that another one shares, having been cut back:
+        SIMSD_EW_SHARED) stay as they were: length, pages and rows, with
+        outputs of zero.  Their rows can be given again once pages are free."""
         T = qkv.shape[1]
         Hq, Hkv = self.Hq, self.Hkv
         lengths = token_start[1:] - token_start[:-1]
+        lens = self.prefix_len
         if self.pooled:
-            simsd.simsd_pages_extend(self.prefix_len, lengths, self.block_table, self.refs, self.P, err_word=self.err)
+            lens = torch.empty_like(lens)  # -1: a sequence that is not to be written
+            simsd.simsd_pages_extend(self.prefix_len, lengths, self.block_table, self.refs, self.P, err_word=self.err,
+                                     granted=lens)
         out = torch.empty(self.L, T, Hq, self.d, dtype=self.dtype, device=self.device)
         q = torch.empty(T, Hq, self.d, dtype=self.dtype, device=self.device)
         sizes = (self.code, T, self.Bt, Hq, Hkv, self.d, self.max_pages, self.P)
@@ -100,23 +109,23 @@ class PromptCache:
                            else simsd.simsd_chunk_workspace_bytes(*sizes))
         for l in range(self.L):
             x = qkv[l]
-            args = (self.plan, x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], token_start, self.prefix_len, q)
+            args = (self.plan, x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], token_start, lens, q)
             if self.bits == 4:
                 simsd.simsd_rope_append_q4(*args, self.q4[l], self.block_table, err_word=self.err)
-                simsd.simsd_chunk_attention_q4(q, token_start, self.prefix_len, self.q4[l], self.block_table, out[l],
+                simsd.simsd_chunk_attention_q4(q, token_start, lens, self.q4[l], self.block_table, out[l],
                                                mask_block=self.mask_block, window=self.window, sinks=self.sinks,
                                                workspace=ws, err_word=self.err)
                 continue
             cache = (self.k_cache[l], self.v_cache[l], self.block_table)
             simsd.simsd_rope_append(*args, *cache, err_word=self.err)
             if self.window:
-                simsd.simsd_chunk_attention_sinks(q, token_start, self.prefix_len, *cache, out[l], self.window,
+                simsd.simsd_chunk_attention_sinks(q, token_start, lens, *cache, out[l], self.window,
                                                   self.sinks, mask_block=self.mask_block, workspace=ws,
                                                   err_word=self.err)
             else:
-                simsd.simsd_chunk_attention(q, token_start, self.prefix_len, *cache, out[l],
+                simsd.simsd_chunk_attention(q, token_start, lens, *cache, out[l],
                                             mask_block=self.mask_block, workspace=ws, err_word=self.err)
-        self.prefix_len += lengths
+        self.prefix_len += lengths.masked_fill(lens < 0, 0) if self.pooled else lengths
         if self.pooled and self.window:
             # the next token sees rows from prefix_len + 1 - window on, and the first ones
             first = torch.full_like(self.prefix_len, self.sinks)

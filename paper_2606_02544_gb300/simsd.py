@@ -36,7 +36,7 @@ EXPORTED = ("simsd_build_mask", "simsd_verify_workspace_bytes", "simsd_verify_at
             "simsd_rope_plan_init", "simsd_rope_rotate", "simsd_rope_append", "simsd_chunk_workspace_bytes",
             "simsd_chunk_attention", "simsd_chunk_attention_sinks", "simsd_rope_append_q4", "simsd_q4_expand",
             "simsd_chunk_q4_workspace_bytes", "simsd_chunk_attention_q4", "simsd_pages_extend",
-            "simsd_pages_release", "simsd_pages_workspace_bytes", "simsd_pages_fork", "simsd_pages_compact",
+            "simsd_pages_extend_granted", "simsd_pages_release", "simsd_pages_workspace_bytes", "simsd_pages_fork", "simsd_pages_compact",
             "simsd_sample", "simsd_check_error", "simsd_debug_expire_next_wait",
             "simsd_last_error", "simsd_version")
 DEBUG_WAIT_ATTENTION, DEBUG_WAIT_ACCEPT = 1, 2
@@ -120,6 +120,7 @@ def load_library(path: str = LIB_PATH):
             lib.simsd_chunk_attention_q4.argtypes = [I, P, S, P, P, P, P, I, P, I, I, I, I, I, I, I, I, I, I, F, P, P,
                                                      P, Z, P, P]
             lib.simsd_pages_extend.argtypes = [P, P, P, P, I, I, I, I, P, P]
+            lib.simsd_pages_extend_granted.argtypes = [P, P, P, P, I, I, I, I, P, P, P]
             lib.simsd_pages_release.argtypes = [P, P, P, I, P, P, I, I, I, I, P, P]
             lib.simsd_pages_workspace_bytes.argtypes = [I, I]
             lib.simsd_pages_workspace_bytes.restype = Z
@@ -133,7 +134,7 @@ def load_library(path: str = LIB_PATH):
                          "simsd_plan_accept", "simsd_rope_plan_init", "simsd_rope_rotate", "simsd_rope_append",
                          "simsd_chunk_attention", "simsd_chunk_attention_sinks", "simsd_rope_append_q4",
                          "simsd_q4_expand", "simsd_chunk_attention_q4", "simsd_pages_extend",
-                         "simsd_pages_release", "simsd_pages_fork", "simsd_pages_compact", "simsd_sample"):
+                         "simsd_pages_extend_granted", "simsd_pages_release", "simsd_pages_fork", "simsd_pages_compact", "simsd_sample"):
                 getattr(lib, name).restype = ctypes.c_int
             _lib = lib
     return _lib
@@ -726,18 +727,25 @@ def _current(dev):
     return dev >= 0 and (_devices == 1 or dev == torch._C._cuda_getDevice())
 
 
-def simsd_pages_extend(lens, add, block_table, refs, page_size, err_word=None, stream=None):
-    """Pages for the rows [lens[b], lens[b] + add[b]) that have none."""
+def simsd_pages_extend(lens, add, block_table, refs, page_size, err_word=None, stream=None, granted=None):
+    """Pages for the rows [lens[b], lens[b] + add[b]) that have none; granted
+    [Bt] int32 out (simsd_pages_extend_granted): lens[b] where sequence b may
+    go on, -1 where not."""
     Bt, max_pages = block_table.shape
     num_pages, dev = refs.shape[0], block_table.get_device()
     if not (lens.dtype is add.dtype is refs.dtype is block_table.dtype is _I32
             and lens.numel() == add.numel() == Bt and refs.numel() == num_pages
             and lens.is_contiguous() and add.is_contiguous() and refs.is_contiguous() and block_table.is_contiguous()
-            and lens.get_device() == add.get_device() == refs.get_device() == dev and _current(dev)):
-        _pages_wrong(dev, block_table, refs, dict(lens=(lens, Bt), add=(add, Bt)))
-    rc = (_lib or load_library()).simsd_pages_extend(
-        lens.data_ptr(), add.data_ptr(), block_table.data_ptr(), refs.data_ptr(), num_pages, Bt, max_pages, page_size,
-        _error_word(err_word, dev), _raw_stream(stream, dev))
+            and lens.get_device() == add.get_device() == refs.get_device() == dev and _current(dev)
+            and (granted is None or granted.dtype is _I32 and granted.numel() == Bt and granted.is_contiguous()
+                 and granted.get_device() == dev)):
+        _pages_wrong(dev, block_table, refs, dict(lens=(lens, Bt), add=(add, Bt))
+                     | ({} if granted is None else dict(granted=(granted, Bt))))
+    args = (lens.data_ptr(), add.data_ptr(), block_table.data_ptr(), refs.data_ptr(), num_pages, Bt, max_pages, page_size)
+    rest = (_error_word(err_word, dev), _raw_stream(stream, dev))
+    lib = _lib or load_library()
+    rc = (lib.simsd_pages_extend(*args, *rest) if granted is None
+          else lib.simsd_pages_extend_granted(*args, granted.data_ptr(), *rest))
     if rc:
         _check(rc, "simsd_pages_extend")
 

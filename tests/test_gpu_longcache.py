@@ -177,3 +177,66 @@ def test_graph_outlives_a_larger_workspace():
     cache.prefix_len.copy_(lens)
     graph.replay()
     assert torch.equal(got, want) and simsd.simsd_check_error(cache.err) == 0
+
+
+def near(a, b):
+    """Rows of calls whose other rows differ (they may be cut elsewhere, or go
+    another way): each off by 2^-8 (fp32: 2^-16) of values of 8 at most."""
+    return bool(((a.double() - b.double()).abs() <= 16 * 2.0 ** (-8 if a.dtype == BF16 else -16)).all())
+
+
+@pytest.mark.parametrize("dtype,bits", [(BF16, None), (BF16, 4), (F32, 4)])
+def test_a_chunk_without_pages_can_be_made_again(dtype, bits):
+    """Too few free pages: sequences that want one stay as they were, with
+    outputs of zero, those that want none go on; after a release the same rows
+    have the outputs that a larger pool gives."""
+    small, large = (PromptCache(LAYERS, 4, HQ, HKV, D, P, 512, plan(), dtype=dtype, bits=bits, pages=n) for n in (12, 60))
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x, start = chunk(g, dtype, 60, 33, 20, 40)  # 4 + 3 + 2 + 3 pages
+    for c in (small, large):
+        c.append_chunk(x, start)
+    assert simsd.simsd_check_error(small.err) == 0 and int((small.refs == 0).sum()) == 0
+    state = [t.clone() for t in (small.block_table, small.refs)]
+    parts = [t.clone() for t in small.page_set.tensors]
+    x, start = chunk(g, dtype, 2, 30, 1, 20)  # sequences 1 and 3 want pages
+    got, want = small.append_chunk(x, start), large.append_chunk(x, start)
+    assert simsd.simsd_check_error(small.err) & simsd.EW_POOL
+    small.err.zero_()
+    assert small.prefix_len.tolist() == [62, 33, 21, 40]
+    assert near(got[:, :2], want[:, :2]) and near(got[:, 32:33], want[:, 32:33])
+    assert bool((got[:, 2:32] == 0).all()) and bool((got[:, 33:] == 0).all())
+    assert torch.equal(small.block_table, state[0]) and torch.equal(small.refs, state[1])
+    for b in (1, 3):
+        held = state[0][b][state[0][b] >= 0].long()
+        # (bytes: rows that nobody has written may hold NaN)
+        assert all(torch.equal(t.view(torch.uint8)[:, held], s.view(torch.uint8)[:, held]) for t, s in zip(small.page_set.tensors, parts))
+    small.release(torch.tensor([2], **I32))
+    again = torch.tensor([0, 0, 30, 30, 30], **I32)  # sequence 1 (2 pages), then 3
+    out = small.append_chunk(x[:, 2:32], again)
+    assert near(out, want[:, 2:32])
+    small.release(torch.tensor([0], **I32))
+    out = small.append_chunk(x[:, 33:], torch.tensor([0, 0, 0, 0, 20], **I32))
+    assert near(out, want[:, 33:])
+    assert simsd.simsd_check_error(small.err) == 0 and small.prefix_len.tolist() == [0, 63, 0, 60]
+
+
+@pytest.mark.parametrize("bits", [None, 4])
+def test_a_sequence_cut_back_into_shared_pages_writes_nothing(bits):
+    """A fork cut back into a page that it shares with its source: its rows are
+    refused, the source goes on with its own."""
+    cache, alone = (PromptCache(LAYERS, 2, HQ, HKV, D, P, 256, plan(), bits=bits, pages=20) for _ in range(2))
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x, start = chunk(g, BF16, 40, 0)
+    for c in (cache, alone):
+        c.append_chunk(x, start)
+    cache.fork(torch.tensor([0], **I32), torch.tensor([1], **I32))
+    cache.prefix_len[1] = 20  # in the second page of three
+    x, start = chunk(g, BF16, 1, 1)
+    out = cache.append_chunk(x, start)
+    want = alone.append_chunk(x[:, :1].contiguous(), torch.tensor([0, 1, 1], **I32))
+    assert simsd.simsd_check_error(cache.err) & simsd.EW_SHARED
+    assert near(out[:, :1], want) and bool((out[:, 1] == 0).all()) and cache.prefix_len.tolist() == [41, 20]
+    cache.err.zero_()
+    x, start = chunk(g, BF16, 1, 0)
+    assert near(cache.append_chunk(x, start), alone.append_chunk(x, start))
+    assert simsd.simsd_check_error(cache.err) == 0

@@ -375,3 +375,42 @@ def test_pools_past_four_gigabytes():
     assert table.tolist() == [[2, 1], [2, 0]] and int(live) == 3 and refs[:3].tolist() == [1, 1, 2]
     assert bool((cache[0, 2] == 7).all()) and torch.equal(cache[0, 1], cache[0, 0])
     assert simsd.simsd_check_error(err) == 0
+
+
+@pytest.mark.parametrize("Bt,free", [(24, 400), (24, 3), (1500, 20000), (1500, 700)])
+def test_extend_says_which_sequences_may_go_on(Bt, free):
+    """Lengths of sequences that have their pages, -1 for those that were
+    refused, and with too few free pages for all that want one."""
+    P, max_pages = 4, 40
+    i32 = dict(dtype=torch.int32, device="cuda")
+    rng = np.random.RandomState(Bt + free)
+    used = Bt * 3
+    table = np.full((Bt, max_pages), -1)
+    table[:, :3] = rng.permutation(used).reshape(Bt, 3)
+    refs = np.zeros(used + free, dtype=int)
+    refs[:used] = 1
+    lens, add = np.full(Bt, 10), rng.choice([0, 2, 3, 7, 50, 130], Bt)
+    kind = np.arange(Bt) % 8
+    table[kind == 1, 2] = table[0, 2]  # shared (with sequence 0 too)
+    refs[:used] = np.bincount(table[:, :3].ravel(), minlength=used)
+    lens[kind == 2] = -3
+    add[kind == 3] = 151  # past the table
+    table[kind == 4, 2] = used + free + 7
+    add[kind == 5] = -1
+    wants = np.array([sum(table[b, k] == -1 for k in range(lens[b] // P, -(-(lens[b] + add[b]) // P)))
+                      if add[b] > 0 and lens[b] >= 0 and lens[b] + add[b] <= max_pages * P else 0 for b in range(Bt)])
+    wrong = (kind == 2) | (kind == 3) | (kind == 5) | ((kind == 4) & (add > 0)) | ((kind == 1) & (add > 0))
+    wrong[0] = add[0] > 0
+    wants[wrong] = 0
+    short = wants.sum() > free
+    assert short == (free in (3, 700))
+    t = lambda x: torch.tensor(np.asarray(x), **i32)  # noqa: E731
+    got, err, tab, cnt = torch.full((Bt,), 77, **i32), torch.zeros(1, **i32), t(table), t(refs)
+    plain = [t(table), t(refs), torch.zeros(1, **i32)]
+    simsd.simsd_pages_extend(t(lens), t(add), tab, cnt, P, err_word=err, granted=got)
+    simsd.simsd_pages_extend(t(lens), t(add), plain[0], plain[1], P, err_word=plain[2])
+    assert all(torch.equal(a, b) for a, b in zip((tab, cnt, err), plain))
+    no = wrong | ((wants > 0) if short else False)
+    assert np.array_equal(got.cpu().numpy(), np.where(no, -1, lens))
+    word = simsd.simsd_check_error(err)
+    assert bool(word & simsd.EW_POOL) == short and word & simsd.EW_PREFIX_LEN and torch.equal(tab, t(table)) == short

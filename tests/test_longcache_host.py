@@ -167,3 +167,13 @@ def test_counts_are_looked_at_whatever_the_table(lib, mp):
         assert lib.simsd_pages_fork(a, n, one, one, 1, one, one, refs, 10, 4, mp, 8, one, 1 << 20, None, None) == BAD
         assert lib.simsd_pages_compact(a, n, one, refs, 10, 4, mp, None, one, 1 << 20, None, None) == BAD
     assert lib.simsd_pages_extend(one, one, one, one, 10, 0, mp, 8, None, None) == 0
+
+
+def test_granted_is_a_place_of_its_own(lib):
+    tail = (10, 4, 4, 8)
+    assert lib.simsd_pages_extend_granted(one, one, one, one, *tail, None, None, None) == BAD
+    assert lib.simsd_pages_extend_granted(one, one, one, one, *tail, one, None, None) == BAD
+    assert lib.simsd_pages_extend_granted(one, one, None, one, *tail, ctypes.c_void_p(512), None, None) == BAD
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(ValueError):
+        simsd.simsd_pages_extend(i(2), i(2), i(2, 4), i(8), 4, granted=i(3))
