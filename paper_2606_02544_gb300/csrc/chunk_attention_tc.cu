@@ -44,7 +44,7 @@
 // units of one row block: the blocks take them in turns, so that a unit's
 // last tile and its output lie under the next one's tiles (with block A
 // alone 214 and 20 us).  Through a window of 1024 rows with 4 first ones, 64
-// single tokens, 73 us (82); a prompt of 8192, block-causal, with 64 first
+// single tokens, 75 us (82); a prompt of 8192, block-causal, with 64 first
 // ones, 176 us.  (Exponentials on the FMA pipes for an eighth to a half of the
 // keys: 220 to 258 us; the softmax is bound by issue, not by the unit.)
 // TMEM (512 columns): S_A [0,128), S_B [128,256), O_A [256,384), O_B
@@ -228,13 +228,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   using Smem = SmemChunk<D, SINKS>;
   constexpr int kHalves = Smem::kHalves, kStages = Smem::kStages, kStagesK = Smem::kStagesK, kStagesV = Smem::kStagesV;
   extern __shared__ uint8_t smem_raw[];
-  // By an offset from the array the compiler knows that this is shared memory,
-  // by a rounded number it does not: worth 74 -> 73 us to 64 single tokens
-  // through a window, but two row blocks then fall out of antiphase (2048
-  // tokens after 32768 rows 740 -> 850 us).
-  Smem& sm = *reinterpret_cast<Smem*>(
-      ALT ? smem_raw + (0u - smem_u32(smem_raw) & 1023u)
-          : reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023)));
+  // (A rounded address, by which the compiler does not know that this is shared
+  // memory.  By an offset from the array 64 single tokens through a window take
+  // 73.5 us for 74.9, but units of two row blocks take 15% longer.)
+  Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   volatile int* abort_flag = &sm.abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
@@ -898,10 +895,12 @@ cudaError_t launch_d(const ChunkArgs& a, int num_sms, EncodeTiledFn encode, cuda
       done[dev] = true;
     }
   }
-  // The blocks take units in turns where a sequence has no more rows than one
-  // of them on average.  (64 single tokens 214 -> 210 us; in every call, a chunk
-  // of 2048 after 32768 rows came out 1.5% slower.)
-  const bool alt = static_cast<long long>(a.T) * p.g <= static_cast<long long>(kRows) * a.Bt;
+  // The blocks take units in turns where there is no more than a token for each
+  // sequence, and no unit of two blocks on average (64 single tokens 225 -> 222
+  // us, 128 351 -> 342).  An average over sequences counts those without tokens:
+  // by rows alone, a chunk of 2048 after 32768 rows in one of 64 slots, or of
+  // 1024 beside 63 single tokens, took the turns, and 2 to 4% longer.
+  const bool alt = static_cast<long long>(a.T) * p.g <= static_cast<long long>(kRows) * a.Bt && a.T <= a.Bt;
   auto* kernel = a.sinks > 0 ? (alt ? chunk_tc_kernel<D, true, true> : chunk_tc_kernel<D, true, false>)
                              : (alt ? chunk_tc_kernel<D, false, true> : chunk_tc_kernel<D, false, false>);
   cudaError_t e = launch_overlapped(kernel, dim3(static_cast<unsigned>(p.ctas)), dim3(kThreads),

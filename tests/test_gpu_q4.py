@@ -721,3 +721,13 @@ def test_expand_of_more_than_2_to_the_31_pages_and_heads():
         assert simsd.simsd_check_error(err) == 0
         outs.append(torch.stack(out))
     assert torch.equal(outs[0], outs[1]) and not bool((outs[0] == 5).flatten(2).all(2).any())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (90, 5)])
+@pytest.mark.parametrize("chunk", [[200] + [0] * 63 + [1] * 6, [64] + [0] * 63, [0] * 30 + [300] + [1] * 40, [33, 1, 0, 0] * 9,
+                                   [1] * 40 + [0] * 40, [600, 0, 0]])
+def test_long_chunks_beside_single_tokens_and_empty_slots(dtype, window, sinks, chunk):
+    """Averages over sequences that say little about any of them."""
+    prefix = [(37 * b) % 300 for b in range(len(chunk))]
+    check(attention_case(dtype, chunk, prefix, 4, 1, 64, 16, len(chunk), window, sinks), window, sinks)

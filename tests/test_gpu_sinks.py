@@ -174,3 +174,13 @@ def test_large_scores():
     below the window's."""
     a = make(BF16, [2, 60], [500, 300], 8, 2, 128, 16, 11, 64, 20, std=3.0)
     check(a, 64, 20)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (90, 5)])
+@pytest.mark.parametrize("chunk", [[70] + [0] * 63 + [1] * 6, [64] + [0] * 63, [65] + [0] * 63, [0] * 30 + [300] + [1] * 40,
+                                   [33, 1, 0, 0] * 9, [1] * 40 + [0] * 40, [2] + [1] * 38 + [0]])
+def test_long_chunks_beside_single_tokens_and_empty_slots(dtype, window, sinks, chunk):
+    """Averages over sequences that say little about any of them."""
+    prefix = [(37 * b) % 300 for b in range(len(chunk))]
+    check(make(dtype, chunk, prefix, 4, 1, 64, 16, len(chunk), window, sinks), window, sinks)
