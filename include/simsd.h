@@ -475,7 +475,9 @@ SIMSD_API int simsd_rope_append(int dtype, const simsd_rope_plan* plan, const vo
  * neighbouring tokens sees sets SIMSD_EW_PAGE and zeroes the rows of that
  * group.  A value row that is not finite may also reach the rows of tokens
  * up to 256 Hkv/Hq places before the first that sees it (0 times it is not 0);
- * rows that no token of such a group sees are never used.
+ * rows that no token of such a group sees are never used.  SIMSD_BF16 takes
+ * scores (scale q.k) within +-2^29; rows with larger ones may come out as zero
+ * or NaN.
  */
 SIMSD_API size_t simsd_chunk_workspace_bytes(int dtype, int T, int Bt, int Hq, int Hkv, int d, int max_pages,
                                              int page_size);

@@ -92,8 +92,9 @@ class PromptCache:
         With a pool, sequences that get no pages (too few are free:
         SIMSD_EW_POOL in err, and those that want none go on; or they would
         write to a page that another one shares, having been cut back:
-        SIMSD_EW_SHARED) stay as they were: length, pages and rows, with
-        outputs of zero.  Their rows can be given again once pages are free."""
+        SIMSD_EW_SHARED; SIMSD_EW_PREFIX_LEN besides) stay as they were:
+        length, pages and rows, with outputs of zero.  Their rows can be given
+        again once pages are free."""
         T = qkv.shape[1]
         Hq, Hkv = self.Hq, self.Hkv
         lengths = token_start[1:] - token_start[:-1]

@@ -184,3 +184,34 @@ def test_long_chunks_beside_single_tokens_and_empty_slots(dtype, window, sinks, 
     """Averages over sequences that say little about any of them."""
     prefix = [(37 * b) % 300 for b in range(len(chunk))]
     check(make(dtype, chunk, prefix, 4, 1, 64, 16, len(chunk), window, sinks), window, sinks)
+
+
+@pytest.mark.parametrize("dtype,level", [(BF16, 20), (BF16, 25), (BF16, 29), (F32, 29), (F32, 120)])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("chunk", [[1] * 4, [60, 33, 1, 90]])
+def test_scores_far_from_zero(dtype, level, sign, chunk):
+    """Two levels of scores of either sign, the higher one of magnitude up to
+    2^29 (fp32: further): the mean of the values at it."""
+    prefix = [300, 140, 5, 64]
+    a = make(dtype, chunk, prefix, 8, 2, 64, 16, 31, 0, 0, hide=False)
+    a["k_cache"].zero_()
+    a["k_cache"][..., 0] = torch.where(torch.arange(16, device="cuda") % 3 == 0, 1.0, 0.5).to(dtype)
+    a["q"].zero_()
+    a["q"][..., 0] = sign * 1.3359375 * 2.0 ** level
+    scale = float(np.float32(0.7))
+    out, lse, word = run(a, window=0, sinks=0, softmax_scale=scale)
+    assert word == 0
+    start, table = a["token_start"].tolist(), a["block_table"].cpu().numpy()
+    v = a["v_cache"].double().cpu().numpy()
+    for b, n in enumerate(prefix):
+        for i in range(chunk[b]):
+            r = np.arange(n + i + 1)
+            best = r % 16 % 3 == 0 if sign > 0 or len(r) == 1 else r % 16 % 3 != 0
+            rows = v[table[b, r[best] // 16], :, r[best] % 16].repeat(4, 1)
+            want, size = rows.mean(0), np.abs(rows).mean(0)
+            got = out[start[b] + i].double().cpu().numpy()
+            # equal weights in bf16 are off by 2^-8 of their like in the sum, outputs by 2^-8
+            tol = (size + np.abs(want)) * 2.0 ** -8 * (1 + 2.0 ** -7) if dtype == BF16 else size * 2.0 ** -20
+            assert np.all(np.abs(got - want) <= tol + size * (len(r) // 64 + 72) * 2.0 ** -22), (b, i)
+            lw = sign * scale * 1.3359375 * 2.0 ** level * (1.0 if best[0] else 0.5) + math.log(best.sum())
+            assert np.all(np.abs(lse[start[b] + i].double().cpu().numpy() - lw) <= 2.0 ** -21 * abs(lw)), (b, i)
