@@ -620,7 +620,7 @@ typedef struct simsd_page_array {
  * length or addend that is negative or passes the table sets
  * SIMSD_EW_PREFIX_LEN, a page among them that another entry shares (a
  * sequence cut back into pages that it shares with a fork)
- * SIMSD_EW_SHARED: that sequence gets no page.
+ * SIMSD_EW_SHARED: that sequence gets no page.  Bt max_pages is below 2^31.
  *
  * simsd_pages_extend_granted -- the same, and says which sequences may go on:
  *   granted [Bt] int32 out: lens[b] where every entry of the rows names a page

@@ -981,6 +981,8 @@ int pages_extend_impl(const int32_t* lens, const int32_t* add, int32_t* block_ta
   int rc = check_pages(block_table, refs, num_pages, Bt, max_pages);
   if (rc == SIMSD_OK) rc = check_rows(max_pages, page_size);
   if (rc != SIMSD_OK) return rc;
+  // (entries that want a page are counted in 32 bits)
+  if (static_cast<long long>(Bt) * max_pages >= (1ll << 31)) return unsupported("2^31 table entries or more");
   if (Bt == 0) return SIMSD_OK;
   if (!lens || !add) return arg_fail("null pointer");
   DeviceInfo info;

@@ -177,3 +177,11 @@ def test_granted_is_a_place_of_its_own(lib):
     i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
     with pytest.raises(ValueError):
         simsd.simsd_pages_extend(i(2), i(2), i(2, 4), i(8), 4, granted=i(3))
+
+
+def test_tables_whose_wanted_pages_pass_32_bits_are_refused(lib):
+    """65536 sequences of 32768 entries each may want 2^31 pages, which a count
+    of 32 bits has as a negative number: none were handed out, nor an error set."""
+    assert lib.simsd_pages_extend(one, one, one, one, 1 << 20, 65536, 1 << 15, 8, None, None) == UNSUPPORTED
+    assert lib.simsd_pages_extend_granted(one, one, one, one, 1 << 20, 65535, 1 << 16, 8, ctypes.c_void_p(512), None,
+                                          None) == UNSUPPORTED
