@@ -26,10 +26,11 @@
 // own, merged at the end of a unit through shared memory.  A unit cut by a
 // run's end leaves partial (O, m, l), which a second launch merges.
 //
-// Bound: the issue of instructions, some 280 for 16 keys (64 conversions and
-// 64 products with a scale among them), and what few warps can hide of their
-// latencies: 64 single tokens over 2048 to 8192 rows, 32 heads on 8 of 128, read
-// 377 MB in 77 us (4.9 TB/s).
+// Bound: what twelve warps an SM can hide of their latencies: some 280
+// instructions for 16 keys (64 conversions and 64 products with a scale among
+// them) take 53% of the issue slots, the reads 56% of DRAM's rate.  64 single
+// tokens over 2048 to 8192 rows, 32 heads on 8 of 128, read 377 MB in 79 us (4.8
+// TB/s).
 //
 // Every mbarrier wait is bounded; after one expires the CTA raises
 // SIMSD_EW_TIMEOUT, every warp leaves its loop and the copies in flight are
@@ -63,7 +64,8 @@ struct Q4Params {
 
 // NB blocks of 8 query rows.  CTAs of four warps, whose 32 keys a tile pay for
 // what a tile costs beside its products; as many an SM as registers allow.
-// One block, 64 single tokens over 2048 to 8192 rows: 77 us (four CTAs, with 96
+// One block, 64 single tokens over 2048 to 8192 rows: 79 us (77 when this was
+// chosen; four CTAs, with 96
 // registers a thread, 81; eight warps of 16 keys, two CTAs, then 113 for 87).  Two,
 // 32 blocks of 4 tokens over these: 67 us (eight warps of 16 keys, one CTA, 84).
 template <int D, int NB>
@@ -681,8 +683,9 @@ cudaError_t launch_d(const Q4Params& p, int num_sms, cudaStream_t stream) {
 // the image, which costs one pass over the rows but then serves 256 of them a
 // tile.  Heads of 128, 32 on 8: 32 sequences of 4096 rows, 20 query rows 95 us
 // from the registers (in two blocks of 16) and 84 by tiles; 16 sequences, 256
-// query rows 92 us by tiles and 153 through the image, 512 161 and 204, 768 233
-// and 260.  Heads of 64, 28 on 4: 448 78 and 81, 672 109 and 100.
+// query rows 94 us by tiles and 139 through the image, 512 167 and 192, 768 240
+// and 246, 1024 313 and 296.  Heads of 64, 28 on 4: 448 80 and 78, 511 97 and 95,
+// 672 111 and 98 (by tiles there is no image to be held).
 constexpr int kCodesRows = 16;
 constexpr int tiles_rows(int d) { return d == 128 ? 768 : 512; }
 Q4Way chunk_q4_way(int dtype, int T, int Bt, int Hq, int Hkv, int d) {

@@ -27,7 +27,7 @@
 // of this one.
 //
 // Bound and measured.  32 blocks of 16 tokens over 4096 rows (32 heads on 8,
-// D = 128; 155 MB, 23 us of copies) take 83 us, of 32 tokens 92.  The matrix
+// D = 128; 155 MB, 23 us of copies) take 84 us, of 32 tokens 94.  The matrix
 // instructions of a tile take half of its 2100 cycles; the rest are the chains
 // beside them, each of which is about as long: one warp of an SM partition
 // turns 32 rows of K and one 32 rows of V (29 instructions for 16 components),

@@ -37,15 +37,15 @@
 // Bound: the softmax (exponentials, conversions and maxima of 2 x 128 x 128
 // scores: about 2000 of the 2530 cycles, the two products 1024) for prompts,
 // HBM for single tokens.  Measured, 32 heads on 8, d 128: 8192 tokens of one
-// prompt 434 us (1.3 PFLOP/s of the two products, causal), 2048 after 32768
-// 740 us (1.5); 64 single tokens over 2048 to 8192 rows 208 us (6.4 TB/s); 8
+// prompt 424 us (1.3 PFLOP/s of the two products, causal), 2048 after 32768
+// 740 us (1.5); 64 single tokens over 2048 to 8192 rows 210 us (6.4 TB/s); 8
 // over 512 to 1024, 16 heads, 18 us, most of it one CTA's chain from the
 // tokens' offsets to its first tile and the second launch.  Single tokens are
 // units of one row block: the blocks take them in turns, so that a unit's
 // last tile and its output lie under the next one's tiles (with block A
 // alone 214 and 20 us).  Through a window of 1024 rows with 4 first ones, 64
 // single tokens, 75 us (82); a prompt of 8192, block-causal, with 64 first
-// ones, 176 us.  (Exponentials on the FMA pipes for an eighth to a half of the
+// ones, 177 us.  (Exponentials on the FMA pipes for an eighth to a half of the
 // keys: 220 to 258 us; the softmax is bound by issue, not by the unit.)
 // TMEM (512 columns): S_A [0,128), S_B [128,256), O_A [256,384), O_B
 // [384,512); P (bf16) overwrites the first 64 columns of its S.

@@ -185,8 +185,9 @@ cudaError_t launch_q4_expand_seen(int elem_bytes, const ChunkArgs& a, const sims
                                   void* v_image, int num_sms, cudaStream_t stream);
 
 // Attention over a cache in 4 bits: by codes in the registers of few query
-// rows (chunk_attention_q4.cu), by codes turned into tiles for up to 128 rows
-// (chunk_attention_q4_tc.cu), or through an image in dtype.
+// rows (chunk_attention_q4.cu), by codes turned into tiles of which 128 rows at
+// a time make use (chunk_attention_q4_tc.cu), or through an image in dtype.
+// chunk_q4_way has the rule.
 enum class Q4Way { kCodes, kTiles, kImage };
 Q4Way chunk_q4_way(int dtype, int T, int Bt, int Hq, int Hkv, int d);
 size_t chunk_q4_workspace_bytes(int T, int Bt, int Hq, int Hkv, int d, int num_sms);

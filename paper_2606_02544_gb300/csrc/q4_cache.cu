@@ -20,7 +20,7 @@
 //
 // Bound by memory: a token reads (Hq + 2 Hkv) d elements and writes Hq d and
 // 2 Hkv (d / 2 + d / 16) bytes.  16404 tokens of 32 heads on 8 of 128 in bf16
-// (355 MB) take 77 us, 4.6 TB/s, and the cache written out again as keys and
+// (355 MB) take 78 us, 4.5 TB/s, and the cache written out again as keys and
 // values (86 MB) 12 us (7 TB/s, its reads from L2); a single token a sequence takes as long as the
 // host's two calls, 15 us.
 #include <cuda_bf16.h>
