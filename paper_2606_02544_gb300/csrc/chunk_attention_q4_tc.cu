@@ -604,7 +604,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             return fmax3(fmax3(r[0], r[1], r[2]), fmax3(r[3], r[4], r[5]), fmaxf(r[6], r[7]));
           };
           const float mx = max_of() * scale;
-          const bool move = seen && mx != -INFINITY && (m_ref == -INFINITY || mx > m_ref + kMoveAbove);
+          // (by their difference: far from zero the sum of a reference and 15 is not)
+          const bool move = seen && mx != -INFINITY && mx - m_ref > kMoveAbove;
           if (__any_sync(full, move)) {
             const float f = move && m_ref != -INFINITY ? fast_exp2(m_ref - (mx - kHeadroom)) : 1.0f;
             l_sum *= f;

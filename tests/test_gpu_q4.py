@@ -731,3 +731,31 @@ def test_long_chunks_beside_single_tokens_and_empty_slots(dtype, window, sinks, 
     """Averages over sequences that say little about any of them."""
     prefix = [(37 * b) % 300 for b in range(len(chunk))]
     check(attention_case(dtype, chunk, prefix, 4, 1, 64, 16, len(chunk), window, sinks), window, sinks)
+
+
+@pytest.mark.parametrize("T", [1, 9, 60])
+@pytest.mark.parametrize("level", [23, 24, 25, 26, 27, 28])
+def test_scores_far_from_zero_that_rise(T, level):
+    """Scores of about 2^level in log2 units, from the second tile on 5 to 30
+    above those of the first, where a sum of such a score and a small number is
+    rounded to a multiple of up to 32: no weight passes fp16, and the output is
+    a mean of the values."""
+    n, P, seqs = 300, 16, 64
+    i32 = dict(dtype=torch.int32, device="cuda")
+    pages = (n + T + P - 1) // P
+    cache = simsd.Q4Cache.zeros(pages, 1, P, 64)
+    kc, ks, vc, vs = cache.tensors
+    ks.fill_(56)
+    vs.fill_(56)
+    kc[:, :, :, 0] = 2  # 1 in component 0
+    kc[8:, :, :, 8] = 2  # and, from row 128 on, in component 16
+    vc.fill_(0x22)  # 1
+    vc[8:] = 0x44  # 2
+    q = torch.zeros(seqs * T, 4, 64, dtype=BF16, device="cuda")
+    sign = torch.where(torch.arange(seqs * T, device="cuda") % 2 == 0, 1.0, -1.0)[:, None]
+    q[..., 0] = sign * 2.0 ** level * math.log(2)
+    q[..., 16] = torch.linspace(5, 30, seqs * T * 4, device="cuda").view(seqs * T, 4) * math.log(2)
+    out, lse, word = run(dict(q=q, token_start=torch.arange(seqs + 1, **i32) * T, prefix_len=torch.full((seqs,), n, **i32),
+                              cache=cache, block_table=torch.arange(pages, **i32).repeat(seqs, 1)), softmax_scale=1.0)
+    assert word == 0 and bool(torch.isfinite(lse).all())
+    assert bool(((out >= 1) & (out <= 2)).all())
